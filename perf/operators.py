@@ -189,7 +189,7 @@ def _quantise(x):
     """e4m3 codes and scale bytes: the scale is the smallest power of two (from 2^-110) under which no magnitude exceeds 448."""
     x = x.float()
     m, e = torch.frexp(x.abs().amax(-1))
-    e = (e - 9 + (m > 0.875).int()).clamp(min=-110)
+    e = torch.where(m > 0, e - 9 + (m > 0.875).int(), -110).clamp(min=-110)
     return torch.ldexp(x, -e[..., None]).to(torch.float8_e4m3fn), (e + 127).to(torch.uint8)
 
 
@@ -311,7 +311,7 @@ def exact(c, seed):
                     out[x][pg, :, slot] = rows
                     continue
                 m, e = torch.frexp(rows.abs().amax(-1) / 448)
-                e = (e - (m == 0.5).int()).clamp(min=-110)
+                e = torch.where(m > 0, e - (m == 0.5).int(), -110).clamp(min=-110)
                 rows = torch.ldexp(rows, -e[..., None])
                 # four significant bits, steps of 2^-9 at the low end; rounding to even
                 unit = torch.ldexp(torch.ones_like(rows), (torch.frexp(rows)[1] - 4).clamp(min=-9))
