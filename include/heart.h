@@ -226,6 +226,88 @@ int heart_step_host(const heart_config *cfg, const void *Q_host, const void *K_h
 int heart_drift_static(const heart_config *cfg, const void *Q, const void *K, const double *delta,
                        heart_state *st, double *drift_out, uint8_t *refresh_out, heart_stream_t stream);
 
+/* ---- A paged cache of keys and values, and attention over it ----
+ *
+ * For generation chunk by chunk (a few video frames, or tokens, at a time): the keys and values of earlier tokens stay in
+ * pages, new tokens are stored with heart_cache_write and attend to their whole sequence with heart_cache_attn;
+ * heart_cache_read brings tokens back for the calls above, which take whole tensors.  (No counterpart in the paper, whose
+ * models denoise all frames of a clip together.)
+ *
+ * S sequences; sequence s has kv_len[s] tokens, the new ones included.  Its token j lies in page page_table[s, j / page],
+ * slot j % page.  The packed tensors have T rows; rows row_start[s] .. row_start[s+1] - 1 are the LAST n_s tokens of sequence s, in
+ * order, so row row_start[s] + i is the token at position p = kv_len[s] - n_s + i.  (p < 0: there is no such token.  It is not
+ * written, reads as zeros, and attends to nothing.)  Rows outside row_start[0] .. row_start[S] - 1 belong to no sequence and
+ * are left as they are.  Pages may be shared by sequences; two tokens written to one slot by one call leave it undefined.
+ *
+ * row_start [S+1], kv_len [S] and page_table [S, table_stride] are DEVICE arrays of int32, read when the kernels run (a
+ * captured graph may be replayed with other contents).  What they hold is checked there: row_start is to ascend within
+ * [0, T], kv_len to lie in [0, table_stride * page], page_table entries of tokens that exist to lie in [0, n_pages) (the
+ * others are not looked at).  A violation is reported as HEART_ERR_DEVICE_CHECK through heart_get_status; lengths and starts are then taken as
+ * the nearest valid ones, tokens of a page out of range are not written and read as zeros, and nothing outside the tensors is touched. */
+#define HEART_CACHE_BF16 0
+#define HEART_CACHE_E4M3 1
+
+typedef struct {
+  int32_t S, T;                /* sequences (>= 1), rows of the packed tensors (>= 1)                        */
+  int32_t Hq, Hkv, D;          /* query heads, key heads (query head h reads key head h / (Hq / Hkv); Hq / Hkv
+                                  at most 128); D must be 128                                                */
+  int32_t page;                /* tokens a page: 16, 32, 64 or 128                                           */
+  int32_t n_pages;             /* pages of the pools                                                         */
+  int32_t table_stride;        /* row pitch of page_table in entries; table_stride * page < 2^31 - 256       */
+  int32_t kind;                /* HEART_CACHE_BF16 or HEART_CACHE_E4M3                                       */
+  int32_t max_new;             /* most new tokens of a sequence, 0 = unknown: selects kernels by it; any
+                                  lengths give the right results                                             */
+  int32_t causal;              /* 0: all tokens of the sequence are visible; g > 0: those up to the end of the
+                                  query's group of g tokens (1: token by token, the tokens of a frame: frame
+                                  by frame)                                                                  */
+  int32_t window;              /* 0: none; w > 0: only the last w of those ...                               */
+  int32_t sink;                /* ... and the first `sink` tokens of the sequence                            */
+  uint32_t flags;              /* 0                                                                          */
+  int64_t q_stride_t, q_stride_h;   /* elements, of Q and O; both 0 = contiguous [T,Hq,D]                    */
+  int64_t kv_stride_t, kv_stride_h; /* of the packed K and V of write and read; both 0 = contiguous [T,Hkv,D]  */
+  int64_t pool_stride_page, pool_stride_h, pool_stride_t; /* of both pools; all 0 = contiguous [n_pages,Hkv,page,D] */
+  double scale;                /* logit scale; <= 0 selects 1/sqrt(D)                                        */
+} heart_cache_config;
+
+/* The pools: bf16 or e4m3 elements, head_dim contiguous, 16-byte aligned, strides multiples of 16 bytes.  With
+ * HEART_CACHE_E4M3 a token of a head also has a scale byte b in k_scale / v_scale [n_pages, Hkv, page] (16-byte aligned): its
+ * elements are the codes times 2^(b - 127), or all NaN for b = 255.  (Codes 0x7f and 0xff are never written here; read back they
+ * count as +-480.)  NULL for HEART_CACHE_BF16. */
+typedef struct {
+  void *k, *v;
+  uint8_t *k_scale, *v_scale;
+} heart_cache;
+
+/* Bytes of scratch that the three calls below need (256-byte aligned, zero-filled before first use; heart_get_status reads its
+ * status).  Host-only; 0 for an invalid or unsupported config.  A workspace serves one call at a time: calls that share one are
+ * ordered, by a stream or by events, replays of captured graphs too. */
+size_t heart_cache_workspace_bytes(const heart_cache_config *cfg /* host */);
+
+/* Stores the new tokens' K and V (bf16) in their pages.  HEART_CACHE_E4M3: for every token and head, x = 2^e * code with the
+ * smallest integer e >= -110 such that no |x| exceeds 448 * 2^e, codes rounded to nearest even (magnitudes above 1.875 * 2^127 count as
+ * that, so that no code stands for more than a bf16 number); a row that holds an infinity or a NaN gets codes 0 and the scale byte
+ * 255.  Slots of other tokens are left as they are. */
+int heart_cache_write(const heart_cache_config *cfg, const void *K, const void *V, const heart_cache *cache /* host struct */,
+                      const int32_t *page_table, const int32_t *row_start, const int32_t *kv_len, void *workspace,
+                      heart_stream_t stream);
+
+/* The tokens of the rows out of their pages, as bf16 (exactly: an e4m3 element times its scale is a bf16 number). */
+int heart_cache_read(const heart_cache_config *cfg, const heart_cache *cache, const int32_t *page_table,
+                     const int32_t *row_start, const int32_t *kv_len, void *K_out, void *V_out, void *workspace,
+                     heart_stream_t stream);
+
+/* Attention of the new tokens over their sequences' pages (the new tokens' own keys are read from there, so
+ * heart_cache_write comes first).  The query at position p sees the tokens j < end with j >= end - window or j < sink (all
+ * j < end without a window), where end = kv_len[s], or with causal = g > 0 the smaller of it and (p / g + 1) * g:
+ *   o = sum_j softmax_j(scale * <q, k_j>) v_j;  bf16 in, fp32 accumulate, bf16 out (RNE); lse [T, Hq] fp32 natural-log
+ *   sum-exp of the scaled logits, or NULL.
+ * A query without keys gets zeros and lse = -inf.  What a row does not see has no part in it, whatever it holds (pages hold
+ * anything behind a sequence's end); a row that sees a key or value that is not finite has elements that are not finite.
+ * Weights below 2^-100 of a row's largest may count as zero. */
+int heart_cache_attn(const heart_cache_config *cfg, const void *Q, const heart_cache *cache, const int32_t *page_table,
+                     const int32_t *row_start, const int32_t *kv_len, void *O, float *lse, void *workspace,
+                     heart_stream_t stream);
+
 /* ---- Analysis quantities (not on the layer-step path; nothing else reads their results) ---- */
 
 /* Full-token drift between two steps of the same layer -- Eq. full-token drift, the costly

@@ -1,0 +1,129 @@
+// A paged cache of keys and values: geometry, workspace, and the device code that the kernels on it share.
+#pragma once
+#include <cuda.h>
+
+#include "common.cuh"
+
+namespace heart {
+
+constexpr int kKeyStep = 128;  // keys are processed in steps of 128, from token 0 of a sequence
+constexpr int kCacheCtas = 148;  // persistent CTAs of an attention launch, one per SM
+
+// Geometry derived from a validated heart_cache_config.
+struct CacheGeom {
+  int S, T, Hq, Hkv, G, page, n_pages, table_stride, e4m3, max_new, causal, window, sink;
+  long long qt, qh, kvt, kvh;  // element strides: Q and O, packed K and V
+  long long pp, ph, pt;        // the pools
+  double scale;
+};
+
+// What the kernels on the cache read on the device.
+struct CacheIndex {
+  const int32_t *table, *row_start, *kv_len;
+  int32_t *status;
+  int S, T, page_log2, n_pages, table_stride;
+  int causal, window, sink;
+};
+
+struct CacheWorkspace {
+  int32_t *status;    // [64] word 0: sticky device-check code
+  int32_t *arrivals;  // [kCacheCtas] parts of a shared tile that are there (zero between launches)
+  float *parts;       // [2 * kCacheCtas][128][128] parts of tiles: unnormalised sums of values
+  float2 *part_l;     // [2 * kCacheCtas][128] their row sums and references
+  int4 *tiles;        // [max_tiles + 1] tiles of a head (see cache_tiles.cu)
+  int32_t *tile_first;  // [max_tiles + 1] key steps before a tile
+  size_t bytes;
+};
+
+// Tiles of a head: a sequence ends at most one of them early.
+__host__ inline size_t cache_max_tiles(const CacheGeom &g) { return (size_t)g.S + (size_t)g.T / (128 / g.G); }
+
+__host__ inline CacheWorkspace carve_cache(const CacheGeom &g, void *base) {
+  CacheWorkspace w;
+  char *p = static_cast<char *>(base);
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    char *at = p + off;
+    off += align256(bytes);
+    return at;
+  };
+  w.status = reinterpret_cast<int32_t *>(take(64 * sizeof(int32_t)));
+  w.arrivals = reinterpret_cast<int32_t *>(take(kCacheCtas * sizeof(int32_t)));
+  w.parts = reinterpret_cast<float *>(take(sizeof(float) * 2 * kCacheCtas * 128 * kD));
+  w.part_l = reinterpret_cast<float2 *>(take(sizeof(float2) * 2 * kCacheCtas * 128));
+  w.tiles = reinterpret_cast<int4 *>(take(sizeof(int4) * (cache_max_tiles(g) + 1)));
+  w.tile_first = reinterpret_cast<int32_t *>(take(sizeof(int32_t) * (cache_max_tiles(g) + 1)));
+  w.bytes = off;
+  return w;
+}
+
+int make_cache_geom(const heart_cache_config *c, CacheGeom *g);
+
+cudaError_t launch_cache_write(const CacheGeom &g, const CacheIndex &ix, const void *K, const void *V, const heart_cache &c,
+                               cudaStream_t s, int *launches);
+cudaError_t launch_cache_read(const CacheGeom &g, const CacheIndex &ix, const heart_cache &c, void *K, void *V, cudaStream_t s,
+                              int *launches);
+// Attention by query rows in registers (few rows a sequence and head) or by 128-row tiles.
+bool cache_rows_kernel_fits(const CacheGeom &g);
+cudaError_t launch_cache_rows(const CacheGeom &g, const CacheIndex &ix, const CacheWorkspace &w, const void *Q, const heart_cache &c,
+                              void *O, float *lse, cudaStream_t s, int *launches);
+
+// A pool as a tensor map: boxes of `rows` slots of one head (of bf16, `halves` halves of their 128 dims).
+bool make_pool_map(CUtensorMap *m, const void *base, const CacheGeom &g, int rows, int halves);
+
+#ifdef __CUDACC__
+// A sequence as its arrays describe it, brought into range (and reported) where they do not hold what they should.
+struct Sequence {
+  int row, n, len;  // first row, new tokens, tokens
+};
+__device__ __forceinline__ Sequence sequence(const CacheIndex &ix, int s) {
+  int r0 = __ldcg(&ix.row_start[s]), r1 = __ldcg(&ix.row_start[s + 1]), len = __ldcg(&ix.kv_len[s]);
+  const int most = ix.table_stride << ix.page_log2;
+  if (r0 < 0 || r1 < r0 || r1 > ix.T || len < 0 || len > most) {
+    atomicExch(ix.status, HEART_ERR_DEVICE_CHECK);
+    r0 = min(max(r0, 0), ix.T);
+    r1 = min(max(r1, r0), ix.T);
+    len = min(max(len, 0), most);
+  }
+  return {r0, r1 - r0, len};
+}
+// The page of token j < len of sequence s, or n_pages (reported) where the table holds none.
+__device__ __forceinline__ int page_of(const CacheIndex &ix, int s, int j) {
+  int page = __ldcg(&ix.table[(size_t)s * ix.table_stride + (j >> ix.page_log2)]);
+  if ((unsigned)page >= (unsigned)ix.n_pages) {
+    atomicExch(ix.status, HEART_ERR_DEVICE_CHECK);
+    page = ix.n_pages;
+  }
+  return page;
+}
+// Visible keys of the query at position p of a sequence of `len` tokens: [low, end) and [0, sink).
+struct Visible {
+  int low, end;
+};
+__device__ __forceinline__ Visible visible(const CacheIndex &ix, int p, int len) {
+  if (p < 0) return {0, 0};
+  int end = len;
+  if (ix.causal > 0) {
+    const int group = p - p % ix.causal;
+    end = ix.causal < len - group ? group + ix.causal : len;
+  }
+  return {ix.window > 0 && ix.window < end ? end - ix.window : 0, end};
+}
+// Key steps that the queries at positions p0 .. p1 see some key of: `sinks` steps from token 0 on, then those from step `first` on.
+// (One step without any visible key where there is none, so that the rows are written.)
+struct Span {
+  int sinks, first, steps;
+  __device__ __forceinline__ int step(int i) const { return i < sinks ? i : first + i - sinks; }
+};
+__device__ __forceinline__ Span span_of(const CacheIndex &ix, int p0, int p1, int len) {
+  const Visible a = visible(ix, max(p0, 0), len), b = visible(ix, p1, len);
+  if (p1 < 0 || b.end <= 0) return {0, 0, 1};
+  Span r;
+  r.first = a.low / kKeyStep;
+  r.sinks = min((min(ix.sink, a.low) + kKeyStep - 1) / kKeyStep, r.first);
+  r.steps = r.sinks + (b.end + kKeyStep - 1) / kKeyStep - r.first;
+  return r;
+}
+#endif
+
+}  // namespace heart

@@ -1,0 +1,613 @@
+// Attention over a paged cache for few query rows a sequence and key head: single tokens, drafted tokens, and any rows at all
+// as the plainest of the kernels.
+//
+// Every key and value is read once and used by 16 or 32 rows, so HBM bounds it: the products of 16 rows x 128 keys take 500
+// clocks of the warp-wide matrix instruction an SM, the 64 KB of the keys and values 2800 (bf16; 1400 as e4m3).  So the design is
+// about bytes in flight: one CTA an SM, eight warps, each with a ring of its own of 24 KB that tensor copies fill.  A warp takes 16 of
+// every 128 keys, with the running maximum and sum of its own keys, so nothing but the warp's own barrier is waited for until a tile's end.
+//
+// Work: rows of a sequence and key head, packed as (token, query head of the group), in tiles of 16 or 32; a tile's key steps are
+// 128 tokens each.  All steps of all tiles in one line, (sequence, head, tile, step), are cut into equal shares, one a CTA; what a
+// CTA has of a tile that it does not have whole goes to the workspace, and the CTA that brings the last part puts the tile together, its
+// parts in order: the result does not depend on which one came last.  Every CTA finds its share by itself from the sequences' lengths, so
+// the launch needs no plan and no lengths on the host, and a captured one follows the lengths.
+#include <cuda.h>
+
+#include "cache.cuh"
+#include "tc_ptx.cuh"
+
+namespace heart {
+using namespace tc;
+namespace {
+
+constexpr int kWarps = 8, kThreads = 32 * kWarps;
+constexpr int kKeys = 16;              // keys a warp takes at a time, kWarps * kKeys = kKeyStep
+constexpr int kRing = 24576;           // bytes a warp
+constexpr int kMaxStages = 6;
+constexpr int kMaxParts = 32;          // of a tile, about: the last CTA reads them all
+constexpr float kNoReference = -3.0e38f;
+constexpr float kMaxGrowth = 8.f;      // log2: the reference of a row moves when a maximum exceeds it by more
+
+struct RowsParams {
+  CacheIndex ix;
+  const uint16_t *Q;
+  uint16_t *O;
+  float *lse;
+  const uint8_t *k_scale, *v_scale;
+  long long qt, qh;
+  int Hq, Hkv, G;
+  float scale_log2;
+  int32_t *arrivals;
+  float *parts;
+  float2 *part_l;
+};
+
+struct RowsShared {
+  uint64_t full[kWarps][kMaxStages];
+  alignas(16) uint8_t scales[kWarps][kMaxStages][2 * kKeys];  // of the keys and of the values of a stage
+  float2 l[kWarps][32];   // row sums and references
+  long long total[kWarps];
+  int longest[kWarps];
+  int found;              // sequence of the CTA's first step
+  long long found_at;     // steps before it
+  int last;
+  int abort;
+};
+constexpr int kRowsSmem = kWarps * kRing + sizeof(RowsShared);
+
+__device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint4 lds_u4(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void bulk_load(void *dst, const void *src, int bytes, uint64_t *bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)), "l"(src), "r"(bytes),
+               "r"(smem_u32(bar))
+               : "memory");
+}
+// Four e4m3 codes as two pairs of bf16, (0, 2) and (1, 3): sign, exponent and mantissa are put at their places, the exponent is
+// set right by an exact product.
+__device__ __forceinline__ void e4m3_to_bf16(uint32_t w, uint32_t &even, uint32_t &odd) {
+  constexpr uint32_t kTwo120 = 0x7b807b80u;  // 2^120 twice
+  const uint32_t e = ((w << 4) & 0x07f007f0u) | ((w << 8) & 0x80008000u), o = ((w >> 4) & 0x07f007f0u) | (w & 0x80008000u);
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(even) : "r"(e), "r"(kTwo120));
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(odd) : "r"(o), "r"(kTwo120));
+}
+__device__ __forceinline__ float scale_of(uint32_t byte) { return byte == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(byte << 23); }
+__device__ __forceinline__ bool not_finite(uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
+
+template <int MT, bool E4m3>
+__global__ void __launch_bounds__(kThreads, 1)
+    cache_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const RowsParams p) {
+  constexpr int kRows = 16 * MT;
+  constexpr int kHalf = E4m3 ? 2048 : 4096;  // bytes of 16 keys, or values
+  constexpr int kStage = 2 * kHalf, kStages = kRing / kStage;
+  static_assert(kStages <= kMaxStages, "barriers");
+  extern __shared__ __align__(1024) unsigned char smem[];
+  RowsShared &sh = *reinterpret_cast<RowsShared *>(smem + kWarps * kRing);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  unsigned char *ring = smem + warp * kRing;
+  const uint32_t ring_at = smem_u32(ring);
+  const CacheIndex &ix = p.ix;
+
+  if (lane == 0)
+    for (int i = 0; i < kStages; ++i) mbar_init(&sh.full[warp][i], 1);
+  if (tid == 0) sh.abort = 0;
+  if (lane == 0) mbar_fence_init();
+  pdl_wait();
+  pdl_launch_dependents();
+
+  // ------------------------------------------------------------------ the CTA's share
+  auto tiles_of = [&](const Sequence &q) { return (int)(((long long)q.n * p.G + kRows - 1) / kRows); };
+  auto span = [&](const Sequence &q, int t) {
+    const int first = t * kRows, last = min((int)((long long)q.n * p.G), first + kRows) - 1;
+    return span_of(ix, q.len - q.n + first / p.G, q.len - q.n + last / p.G, q.len);
+  };
+  auto steps_of = [&](int s, int &longest) -> long long {  // of one head
+    const Sequence q = sequence(ix, s);
+    long long n = 0;
+    for (int t = 0; t < tiles_of(q); ++t) {
+      const int k = span(q, t).steps;
+      n += k;
+      longest = max(longest, k);
+    }
+    return n;
+  };
+  long long total = 0, mine = 0;
+  int longest = 1;
+  for (int s = tid; s < ix.S; s += kThreads) {
+    const long long n = steps_of(s, longest) * p.Hkv;
+    if (s < kThreads) mine = n;
+    total += n;
+  }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    total += __shfl_xor_sync(0xffffffffu, total, o);
+    longest = max(longest, __shfl_xor_sync(0xffffffffu, longest, o));
+  }
+  if (lane == 0) {
+    sh.total[warp] = total;
+    sh.longest[warp] = longest;
+  }
+  __syncthreads();
+  total = 0;
+#pragma unroll
+  for (int i = 0; i < kWarps; ++i) {
+    total += sh.total[i];
+    longest = max(longest, sh.longest[i]);
+  }
+  const long long share = max((total + gridDim.x - 1) / gridDim.x, (long long)(longest + kMaxParts - 1) / kMaxParts);
+  const long long u0 = blockIdx.x * share, u1 = min(total, u0 + share);
+  if (u0 >= u1) return;
+  long long before = 0;  // steps before the sequences of this round
+  for (int base = 0; base < ix.S; base += kThreads) {
+    int dummy = 0;
+    if (base > 0) mine = base + tid < ix.S ? steps_of(base + tid, dummy) * p.Hkv : 0;
+    long long upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long x = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += x;
+    }
+    __syncthreads();
+    if (lane == 31) sh.total[warp] = upto;
+    __syncthreads();
+    long long at = before, all = 0;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) {
+      if (i < warp) at += sh.total[i];
+      all += sh.total[i];
+    }
+    at += upto - mine;
+    if (at <= u0 && u0 < at + mine) {
+      sh.found = base + tid;
+      sh.found_at = at;
+    }
+    before += all;
+    if (before > u0) break;
+  }
+  __syncthreads();
+  int s = sh.found, h, t = 0;
+  Sequence q = sequence(ix, s);
+  long long u = u0;
+  int done;  // steps of the present tile before this share
+  {
+    int dummy = 0;
+    const long long per_head = steps_of(s, dummy);
+    long long rest = u0 - sh.found_at;
+    h = (int)(rest / per_head);
+    rest -= h * per_head;
+    for (int k; rest >= (k = span(q, t).steps); ++t) rest -= k;
+    done = (int)rest;
+  }
+
+  uint32_t issued = 0, taken = 0;  // stages of this warp's ring so far
+  bool ok = true;
+  const int g = lane >> 2, c = lane & 3;
+
+  for (;;) {
+    // ---------------------------------------------------------------- a tile, or part of one
+    const Span sp = span(q, t);
+    const int first_row = t * kRows, n_rows = min(kRows, (int)((long long)q.n * p.G) - first_row);
+    const int p0 = q.len - q.n + first_row / p.G, p1 = q.len - q.n + (first_row + n_rows - 1) / p.G;
+    const int end_step = (int)min((long long)sp.steps, done + (u1 - u));
+    const Visible va = visible(ix, p0, q.len), vb = visible(ix, p1, q.len);
+    auto some = [&](int k0) { return p1 >= 0 && k0 < vb.end && (k0 + kKeys > visible(ix, max(p0, 0), q.len).low || k0 < ix.sink); };
+    auto every = [&](int k0) { return p0 >= 0 && k0 + kKeys <= va.end && (k0 >= vb.low || k0 + kKeys <= ix.sink); };
+
+    int next = done - 1, next_page = 0;  // the step of the warp's next copy, and the page of its keys
+    auto key_of = [&](int i) { return sp.step(i) * kKeyStep + warp * kKeys; };
+    auto advance = [&]() {
+      do ++next;
+      while (next < end_step && !some(key_of(next)));
+      if (next < end_step) next_page = page_of(ix, s, key_of(next));
+    };
+    auto issue = [&]() {
+      if (next >= end_step) return;
+      const int st = issued % kStages, slot = key_of(next) & ((1 << ix.page_log2) - 1);
+      if (lane == 0) {
+        uint64_t *bar = &sh.full[warp][st];
+        mbar_expect_tx(bar, kStage + (E4m3 ? 2 * kKeys : 0));
+        tma_load_5d(ring + st * kStage, &map_k, bar, 0, slot, 0, h, next_page);
+        tma_load_5d(ring + st * kStage + kHalf, &map_v, bar, 0, slot, 0, h, next_page);
+        if (E4m3) {
+          const size_t at = (((size_t)min(next_page, ix.n_pages - 1) * p.Hkv + h) << ix.page_log2) + slot;
+          bulk_load(&sh.scales[warp][st][0], p.k_scale + at, kKeys, bar);
+          bulk_load(&sh.scales[warp][st][kKeys], p.v_scale + at, kKeys, bar);
+        }
+      }
+      ++issued;
+      advance();
+    };
+    advance();
+#pragma unroll 1
+    for (int i = 0; i < kStages; ++i) issue();
+
+    // The rows' queries as operands of the products: this lane's rows g and g + 8 of every 16.  (e4m3: the dims of a product are
+    // those that a lane finds together in a key's row, 32 * c + 4 * ks + (0, 2) and (1, 3).)
+    uint32_t qf[MT][8][4];
+    Visible vis[MT][2];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int row = m * 16 + r * 8 + g;
+        const bool real = row < n_rows;
+        const int i = (first_row + row) / p.G, head = h * p.G + (first_row + row) % p.G;
+        const uint16_t *src = p.Q + (long long)(q.row + i) * p.qt + head * p.qh;
+        vis[m][r] = real ? visible(ix, q.len - q.n + i, q.len) : Visible{0, 0x7fffffff};
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) {
+          uint32_t lo = 0u, hi = 0u;
+          if (real) {
+            if (E4m3) {
+              const uint2 x = *reinterpret_cast<const uint2 *>(src + c * 32 + ks * 4);
+              lo = __byte_perm(x.x, x.y, 0x5410);
+              hi = __byte_perm(x.x, x.y, 0x7632);
+            } else {
+              lo = *reinterpret_cast<const uint32_t *>(src + ks * 16 + c * 2);
+              hi = *reinterpret_cast<const uint32_t *>(src + ks * 16 + c * 2 + 8);
+            }
+          }
+          qf[m][ks][r] = lo;
+          qf[m][ks][2 + r] = hi;
+        }
+      }
+    float o[MT][16][4] = {};
+    float ref[MT][2], sum[MT][2];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) ref[m][0] = ref[m][1] = kNoReference, sum[m][0] = sum[m][1] = 0.f;
+
+#pragma unroll 1
+    for (int i = done; i < end_step; ++i) {
+      const int k0 = key_of(i);
+      if (!some(k0)) continue;
+      const int st = taken % kStages;
+      if (!mbar_wait(&sh.full[warp][st], (taken / kStages) & 1, &sh.abort)) ok = false;
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      const uint32_t k_at = ring_at + st * kStage, v_at = k_at + kHalf;
+      const bool whole = every(k0);
+      float x[MT][2][4] = {};
+      // ---- scores
+      if (E4m3) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const uint4 w = lds_u4(k_at + (n * 8 + g) * 128 + (((c * 2 + j) ^ g) << 4));
+            const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              uint32_t b0, b1;
+              e4m3_to_bf16(ww[k], b0, b1);
+#pragma unroll
+              for (int m = 0; m < MT; ++m) mma_bf16(x[m][n], qf[m][j * 4 + k], b0, b1);
+            }
+          }
+      } else {
+        const int key = ((lane >> 4) << 3) + (lane & 7);
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) {
+          const int chunk = ks * 2 + ((lane >> 3) & 1);
+          uint32_t b[4];
+          ldmatrix4(b, k_at + (chunk >> 3) * 2048 + key * 128 + (((chunk ^ key) & 7) << 4));
+#pragma unroll
+          for (int m = 0; m < MT; ++m) {
+            mma_bf16(x[m][0], qf[m][ks], b[0], b[1]);
+            mma_bf16(x[m][1], qf[m][ks], b[2], b[3]);
+          }
+        }
+      }
+      float ks4[4], vs4[4];  // the scales of this lane's keys 2c, 2c+1, 2c+8, 2c+9
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int key = (k >> 1) * 8 + c * 2 + (k & 1);
+        ks4[k] = E4m3 ? scale_of(sh.scales[warp][st][key]) * p.scale_log2 : p.scale_log2;
+        vs4[k] = E4m3 ? scale_of(sh.scales[warp][st][kKeys + key]) : 1.f;
+      }
+      // ---- weights
+      auto hidden = [&](const Visible &v, int k) { return k >= v.end || (k < v.low && k >= ix.sink); };
+      uint32_t pf[MT][4];
+      bool moved = false;
+      float alpha[MT][2];
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          float top = -INFINITY;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            float &y = x[m][k >> 1][r * 2 + (k & 1)];
+            y *= ks4[k];
+            if (!whole && hidden(vis[m][r], k0 + (k >> 1) * 8 + c * 2 + (k & 1))) y = -INFINITY;
+            top = fmaxf(top, y);
+          }
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+          alpha[m][r] = 1.f;
+          if (top > ref[m][r] + kMaxGrowth) {
+            alpha[m][r] = ex2(ref[m][r] - top);
+            ref[m][r] = top;
+            moved = true;
+          }
+        }
+      if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          sum[m][0] *= alpha[m][0];
+          sum[m][1] *= alpha[m][1];
+#pragma unroll
+          for (int n = 0; n < 16; ++n) {
+            o[m][n][0] *= alpha[m][0];
+            o[m][n][1] *= alpha[m][0];
+            o[m][n][2] *= alpha[m][1];
+            o[m][n][3] *= alpha[m][1];
+          }
+        }
+      }
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          float w[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float y = x[m][k >> 1][r * 2 + (k & 1)];
+            w[k] = ex2(y - ref[m][r]);
+            sum[m][r] += w[k];
+            if (E4m3) w[k] = !whole && y == -INFINITY ? 0.f : w[k] * vs4[k];  // (a hidden token's scale may be NaN)
+          }
+          pf[m][r] = pack_bf16x2(w[0], w[1]);
+          pf[m][2 + r] = pack_bf16x2(w[2], w[3]);
+        }
+      if (!E4m3 && !whole) {
+        // Values that are not finite must not reach rows that do not see them (0 * inf is NaN): they are taken out, and rows that
+        // do see them are marked.
+        uint32_t bad = 0u;
+#pragma unroll 1
+        for (int j = 0; j < 8; ++j) {
+          const uint4 v = lds_u4(v_at + (j * 32 + lane) * 16);
+          if (not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w)) bad |= 1u << ((j * 4 + (lane >> 3)) & 15);
+        }
+        bad = __reduce_or_sync(0xffffffffu, bad);
+        if (bad) {
+#pragma unroll 1
+          for (int j = 0; j < 8; ++j)
+            if (bad >> ((j * 4 + (lane >> 3)) & 15) & 1u) *reinterpret_cast<uint4 *>(ring + st * kStage + kHalf + (j * 32 + lane) * 16) = make_uint4(0u, 0u, 0u, 0u);
+          async_proxy_fence();
+          __syncwarp();
+#pragma unroll 1
+          for (uint32_t todo = bad; todo; todo &= todo - 1) {
+            const int key = k0 + __ffs(todo) - 1;
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+              for (int r = 0; r < 2; ++r)
+                if (!hidden(vis[m][r], key)) sum[m][r] = __uint_as_float(0x7fc00000u);
+          }
+        }
+      }
+      // ---- values
+      if (E4m3) {
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {  // 16 dims each: even ones and odd ones
+          uint32_t b[4];
+          const int key = lane & 15, chunk = j + (lane >> 4);
+          ldmatrix4_trans(b, v_at + key * 128 + (((chunk ^ key) & 7) << 4));
+          uint32_t e0, o0, e1, o1;
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            e4m3_to_bf16(b[2 * k], e0, o0);
+            e4m3_to_bf16(b[2 * k + 1], e1, o1);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+              mma_bf16(o[m][(j + k) * 2], pf[m], e0, e1);
+              mma_bf16(o[m][(j + k) * 2 + 1], pf[m], o0, o1);
+            }
+          }
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {  // 16 dims each
+          uint32_t b[4];
+          const int key = lane & 15, chunk = j * 2 + (lane >> 4);
+          ldmatrix4_trans(b, v_at + (chunk >> 3) * 2048 + key * 128 + (((chunk ^ key) & 7) << 4));
+#pragma unroll
+          for (int m = 0; m < MT; ++m) {
+            mma_bf16(o[m][j * 2], pf[m], b[0], b[1]);
+            mma_bf16(o[m][j * 2 + 1], pf[m], b[2], b[3]);
+          }
+        }
+      }
+      __syncwarp();  // the stage has been read
+      ++taken;
+      issue();
+    }
+    if (!ok) {  // (copies that have not come are waited for once more, so that none lands in memory that is someone else's)
+      for (; taken < issued; ++taken) {
+        const long long since = clock64();
+        while (!mbar_try_wait(&sh.full[warp][taken % kStages], (taken / kStages) & 1) && clock64() - since < kWaitLimitCycles) {
+        }
+      }
+      next = end_step;
+    }
+
+    // ---------------------------------------------------------------- the warps' sums put together
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        sum[m][r] += __shfl_xor_sync(0xffffffffu, sum[m][r], 1);
+        sum[m][r] += __shfl_xor_sync(0xffffffffu, sum[m][r], 2);
+        const int row = m * 16 + r * 8 + g;
+        if (c == 0) sh.l[warp][row] = make_float2(sum[m][r], ref[m][r]);
+        float *to = reinterpret_cast<float *>(ring) + row * 128;
+#pragma unroll
+        for (int n = 0; n < 16; ++n) {
+          // dims of these two columns: e4m3 products take even and odd dims of 16 apart
+          if (E4m3) {
+            if (n & 1) continue;
+            *reinterpret_cast<float4 *>(to + n * 8 + c * 4) =
+                make_float4(o[m][n][r * 2], o[m][n + 1][r * 2], o[m][n][r * 2 + 1], o[m][n + 1][r * 2 + 1]);
+          } else {
+            *reinterpret_cast<float2 *>(to + n * 8 + c * 2) = make_float2(o[m][n][r * 2], o[m][n][r * 2 + 1]);
+          }
+        }
+      }
+    __syncthreads();
+    const bool all = done == 0 && end_step == sp.steps;
+    const long long tile_at = u - done;  // the tile's first step
+    const int c0 = (int)(tile_at / share), c1 = (int)((tile_at + sp.steps - 1) / share);
+    const int part = 2 * blockIdx.x + (done == 0 ? 1 : 0);
+    auto write_row = [&](int row, int d, float4 v, float l, float m) {  // four dims
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const int i = (first_row + row) / p.G, head = h * p.G + (first_row + row) % p.G;
+      *reinterpret_cast<uint2 *>(p.O + (long long)(q.row + i) * p.qt + head * p.qh + d) =
+          make_uint2(pack_bf16x2(v.x * inv, v.y * inv), pack_bf16x2(v.z * inv, v.w * inv));
+      if (d == 0 && p.lse != nullptr) p.lse[(long long)(q.row + i) * p.Hq + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+    };
+    for (int row = warp; row < n_rows; row += kWarps) {
+      const int d = lane * 4;
+      float m = kNoReference, l = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) m = fmaxf(m, sh.l[w][row].y);
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float2 lm = sh.l[w][row];
+        const float f = ex2(lm.y - m);
+        const float4 y = *reinterpret_cast<const float4 *>(smem + w * kRing + row * 512 + d * 4);
+        l = fmaf(lm.x, f, l);
+        v.x = fmaf(y.x, f, v.x);
+        v.y = fmaf(y.y, f, v.y);
+        v.z = fmaf(y.z, f, v.z);
+        v.w = fmaf(y.w, f, v.w);
+      }
+      if (sh.abort) l = __uint_as_float(0x7fc00000u);
+      if (all) {
+        write_row(row, d, v, l, m);
+      } else {
+        __stcg(reinterpret_cast<float4 *>(p.parts + ((size_t)part * 128 + row) * 128 + d), v);
+        if (lane == 0) __stcg(&p.part_l[part * 128 + row], make_float2(l, m));
+      }
+    }
+    if (!all) {
+      __threadfence();
+      __syncthreads();
+      if (tid == 0) {
+        const bool last = atomicAdd(&p.arrivals[c0], 1) == c1 - c0;
+        if (last) p.arrivals[c0] = 0;
+        sh.last = last;
+        __threadfence();
+      }
+      __syncthreads();
+      if (sh.last) {
+        for (int row = warp; row < n_rows; row += kWarps) {
+          const int d = lane * 4;
+          auto place = [&](int i) { return (2 * (c0 + i) + (i == 0 ? 1 : 0)) * 128 + row; };
+          float m = kNoReference, l = 0.f;
+          for (int i = lane; i <= c1 - c0; i += 32) m = fmaxf(m, __ldcg(&p.part_l[place(i)]).y);
+#pragma unroll
+          for (int k = 16; k; k >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
+          float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+          for (int i = 0; i <= c1 - c0; ++i) {
+            const float2 lm = __ldcg(&p.part_l[place(i)]);
+            const float4 y = __ldcg(reinterpret_cast<const float4 *>(p.parts + (size_t)place(i) * 128 + d));
+            const float f = ex2(lm.y - m);
+            l = fmaf(lm.x, f, l);
+            v.x = fmaf(y.x, f, v.x);
+            v.y = fmaf(y.y, f, v.y);
+            v.z = fmaf(y.z, f, v.z);
+            v.w = fmaf(y.w, f, v.w);
+          }
+          write_row(row, d, v, l, m);
+        }
+      }
+    }
+    // ---------------------------------------------------------------- the next tile
+    u += end_step - done;
+    if (u >= u1) break;
+    done = 0;
+    if (++t == tiles_of(q)) {
+      t = 0;
+      if (++h == p.Hkv) {
+        h = 0;
+        do q = sequence(ix, ++s);
+        while (q.n == 0 && s + 1 < ix.S);
+      }
+    }
+    async_proxy_fence();  // the rings held sums: behind them come copies
+    __syncthreads();
+  }
+  if (tid == 0 && sh.abort) atomicExch(ix.status, HEART_ERR_DEVICE_CHECK);
+}
+
+}  // namespace
+
+// A pool as (bytes of a row, slot, half row, head, page): a box is `rows` slots of one head, 128-byte rows, swizzled.
+bool make_pool_map(CUtensorMap *m, const void *base, const CacheGeom &g, int rows, int halves) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (!fn) return false;
+  const int bytes = g.e4m3 ? 1 : 2;
+  cuuint64_t dims[5] = {(cuuint64_t)128 / bytes, (cuuint64_t)g.page, (cuuint64_t)bytes, (cuuint64_t)g.Hkv, (cuuint64_t)g.n_pages};
+  cuuint64_t strides[4] = {(cuuint64_t)g.pt * bytes, 128, (cuuint64_t)g.ph * bytes, (cuuint64_t)g.pp * bytes};
+  cuuint32_t box[5] = {(cuuint32_t)128 / bytes, (cuuint32_t)rows, (cuuint32_t)(g.e4m3 ? 1 : halves), 1, 1};
+  cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+  return fn(m, g.e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void *>(base), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+namespace {
+
+template <int MT, bool E4m3>
+cudaError_t launch(const CacheGeom &g, const RowsParams &p, const CUtensorMap &mk, const CUtensorMap &mv, cudaStream_t s, int *launches) {
+  cudaError_t e = allow_shared_memory(cache_rows_kernel<MT, E4m3>, kRowsSmem);
+  if (e != cudaSuccess) return e;
+  ++*launches;
+  return launch_pdl(cache_rows_kernel<MT, E4m3>, dim3(kCacheCtas), dim3(kThreads), kRowsSmem, s, mk, mv, p);
+}
+
+}  // namespace
+
+bool cache_rows_kernel_fits(const CacheGeom &g) { return true; }
+
+cudaError_t launch_cache_rows(const CacheGeom &g, const CacheIndex &ix, const CacheWorkspace &w, const void *Q, const heart_cache &c,
+                              void *O, float *lse, cudaStream_t s, int *launches) {
+  CUtensorMap mk, mv;
+  if (!make_pool_map(&mk, c.k, g, kKeys, 2) || !make_pool_map(&mv, c.v, g, kKeys, 2)) return cudaErrorInvalidValue;
+  RowsParams p = {};
+  p.ix = ix;
+  p.Q = static_cast<const uint16_t *>(Q);
+  p.O = static_cast<uint16_t *>(O);
+  p.lse = lse;
+  p.k_scale = c.k_scale;
+  p.v_scale = c.v_scale;
+  p.qt = g.qt;
+  p.qh = g.qh;
+  p.Hq = g.Hq;
+  p.Hkv = g.Hkv;
+  p.G = g.G;
+  p.scale_log2 = (float)(g.scale * 1.4426950408889634);
+  p.arrivals = w.arrivals;
+  p.parts = w.parts;
+  p.part_l = w.part_l;
+  const bool two = (long long)g.max_new * g.G > 16;
+  if (g.e4m3) return two ? launch<2, true>(g, p, mk, mv, s, launches) : launch<1, true>(g, p, mk, mv, s, launches);
+  return two ? launch<2, false>(g, p, mk, mv, s, launches) : launch<1, false>(g, p, mk, mv, s, launches);
+}
+
+}  // namespace heart

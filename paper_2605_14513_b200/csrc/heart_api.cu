@@ -6,6 +6,7 @@
 #include <stdio.h>
 #include <string.h>
 
+#include "cache.cuh"
 #include "common.cuh"
 
 using namespace heart;
@@ -60,7 +61,79 @@ int heart::make_geom(const heart_config *c, Geom *g) {
   return HEART_OK;
 }
 
+// The same for a heart_cache_config.
+int heart::make_cache_geom(const heart_cache_config *c, CacheGeom *g) {
+  if (c == nullptr) return HEART_ERR_INVALID;
+  if (c->S <= 0 || c->T <= 0 || c->Hq <= 0 || c->Hkv <= 0 || c->n_pages <= 0 || c->table_stride <= 0) return HEART_ERR_INVALID;
+  if (c->max_new < 0 || c->causal < 0 || c->window < 0 || c->sink < 0 || c->flags != 0) return HEART_ERR_INVALID;
+  if (c->kind != HEART_CACHE_BF16 && c->kind != HEART_CACHE_E4M3) return HEART_ERR_INVALID;
+  if (c->Hq % c->Hkv != 0) return HEART_ERR_INVALID;
+  if (c->D != kD || c->Hq / c->Hkv > 128) return HEART_ERR_UNSUPPORTED;
+  if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return HEART_ERR_UNSUPPORTED;
+  constexpr long long kMost = (1LL << 31) - 256;  // rows, tokens and slots are counted in 32 bits
+  if ((long long)c->table_stride * c->page >= kMost || (long long)c->T * c->Hq >= kMost || c->S >= (1 << 30)) return HEART_ERR_UNSUPPORTED;
+  g->S = c->S;
+  g->T = c->T;
+  g->Hq = c->Hq;
+  g->Hkv = c->Hkv;
+  g->G = c->Hq / c->Hkv;
+  g->page = c->page;
+  g->n_pages = c->n_pages;
+  g->table_stride = c->table_stride;
+  g->e4m3 = c->kind == HEART_CACHE_E4M3;
+  g->max_new = c->max_new == 0 || c->max_new > c->T ? c->T : c->max_new;
+  g->causal = c->causal;
+  g->window = c->window;
+  g->sink = c->sink;
+  auto strides_ok = [](long long a, long long b, int multiple) {
+    constexpr long long kMostStride = 1LL << 38;
+    return a >= kD && b >= kD && a < kMostStride && b < kMostStride && a % multiple == 0 && b % multiple == 0;
+  };
+  const bool q_plain = c->q_stride_t == 0 && c->q_stride_h == 0, kv_plain = c->kv_stride_t == 0 && c->kv_stride_h == 0;
+  const bool pool_plain = c->pool_stride_page == 0 && c->pool_stride_h == 0 && c->pool_stride_t == 0;
+  g->qt = q_plain ? (long long)c->Hq * kD : c->q_stride_t;
+  g->qh = q_plain ? kD : c->q_stride_h;
+  g->kvt = kv_plain ? (long long)c->Hkv * kD : c->kv_stride_t;
+  g->kvh = kv_plain ? kD : c->kv_stride_h;
+  g->pt = pool_plain ? kD : c->pool_stride_t;
+  g->ph = pool_plain ? (long long)c->page * kD : c->pool_stride_h;
+  g->pp = pool_plain ? (long long)c->Hkv * c->page * kD : c->pool_stride_page;
+  const int multiple = g->e4m3 ? 16 : 8;
+  if (!strides_ok(g->qt, g->qh, 8) || !strides_ok(g->kvt, g->kvh, 8) || !strides_ok(g->pt, g->ph, multiple) || !strides_ok(g->pp, g->pp, multiple))
+    return HEART_ERR_INVALID;
+  if (!isfinite(c->scale)) return HEART_ERR_INVALID;
+  g->scale = c->scale > 0.0 ? c->scale : 1.0 / sqrt((double)kD);
+  if (g->scale < 1e-30 || g->scale > 1e30) return HEART_ERR_INVALID;  // (a normal fp32 number)
+  return HEART_OK;
+}
+
 namespace {
+
+// What the three calls on a cache check alike, and the arrays as the kernels take them.
+int cache_call(const heart_cache_config *cfg, const heart_cache *cache, const int32_t *page_table, const int32_t *row_start,
+               const int32_t *kv_len, void *workspace, CacheGeom *g, CacheWorkspace *w, CacheIndex *ix) {
+  const int rc = make_cache_geom(cfg, g);
+  if (rc != HEART_OK) return rc;
+  if (!cache || !cache->k || !cache->v || !page_table || !row_start || !kv_len || !workspace) return HEART_ERR_INVALID;
+  if (!aligned16(cache->k) || !aligned16(cache->v) || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return HEART_ERR_INVALID;
+  if (((reinterpret_cast<uintptr_t>(page_table) | reinterpret_cast<uintptr_t>(row_start) | reinterpret_cast<uintptr_t>(kv_len)) & 3u) != 0)
+    return HEART_ERR_INVALID;
+  if (g->e4m3 && (!cache->k_scale || !cache->v_scale || !aligned16(cache->k_scale) || !aligned16(cache->v_scale))) return HEART_ERR_INVALID;
+  *w = carve_cache(*g, workspace);
+  ix->table = page_table;
+  ix->row_start = row_start;
+  ix->kv_len = kv_len;
+  ix->status = w->status;
+  ix->S = g->S;
+  ix->T = g->T;
+  ix->page_log2 = g->page == 16 ? 4 : g->page == 32 ? 5 : g->page == 64 ? 6 : 7;
+  ix->n_pages = g->n_pages;
+  ix->table_stride = g->table_stride;
+  ix->causal = g->causal;
+  ix->window = g->window;
+  ix->sink = g->sink;
+  return HEART_OK;
+}
 
 bool state_ok(const heart_state *st) {
   return st && st->anchor_q && st->anchor_k && st->has_anchor && st->mask_bits && st->kv_idx && st->kv_cnt;
@@ -365,6 +438,57 @@ int heart_mask_iou(const heart_config *cfg, const uint32_t *mask_a, const uint32
   return HEART_OK;
 }
 
+size_t heart_cache_workspace_bytes(const heart_cache_config *cfg) {
+  CacheGeom g;
+  if (make_cache_geom(cfg, &g) != HEART_OK) return 0;
+  return carve_cache(g, nullptr).bytes;
+}
+
+int heart_cache_write(const heart_cache_config *cfg, const void *K, const void *V, const heart_cache *cache,
+                      const int32_t *page_table, const int32_t *row_start, const int32_t *kv_len, void *workspace,
+                      heart_stream_t stream) {
+  CacheGeom g;
+  CacheWorkspace w;
+  CacheIndex ix;
+  const int rc = cache_call(cfg, cache, page_table, row_start, kv_len, workspace, &g, &w, &ix);
+  if (rc != HEART_OK) return rc;
+  if (!K || !V || !aligned16(K) || !aligned16(V)) return HEART_ERR_INVALID;
+  g_launches = 0;
+  cudaError_t e = launch_cache_write(g, ix, K, V, *cache, static_cast<cudaStream_t>(stream), &g_launches);
+  if (e != cudaSuccess) return cuda_fail(e, "cache_write");
+  return HEART_OK;
+}
+
+int heart_cache_read(const heart_cache_config *cfg, const heart_cache *cache, const int32_t *page_table,
+                     const int32_t *row_start, const int32_t *kv_len, void *K_out, void *V_out, void *workspace,
+                     heart_stream_t stream) {
+  CacheGeom g;
+  CacheWorkspace w;
+  CacheIndex ix;
+  const int rc = cache_call(cfg, cache, page_table, row_start, kv_len, workspace, &g, &w, &ix);
+  if (rc != HEART_OK) return rc;
+  if (!K_out || !V_out || !aligned16(K_out) || !aligned16(V_out)) return HEART_ERR_INVALID;
+  g_launches = 0;
+  cudaError_t e = launch_cache_read(g, ix, *cache, K_out, V_out, static_cast<cudaStream_t>(stream), &g_launches);
+  if (e != cudaSuccess) return cuda_fail(e, "cache_read");
+  return HEART_OK;
+}
+
+int heart_cache_attn(const heart_cache_config *cfg, const void *Q, const heart_cache *cache, const int32_t *page_table,
+                     const int32_t *row_start, const int32_t *kv_len, void *O, float *lse, void *workspace,
+                     heart_stream_t stream) {
+  CacheGeom g;
+  CacheWorkspace w;
+  CacheIndex ix;
+  const int rc = cache_call(cfg, cache, page_table, row_start, kv_len, workspace, &g, &w, &ix);
+  if (rc != HEART_OK) return rc;
+  if (!Q || !O || !aligned16(Q) || !aligned16(O) || (reinterpret_cast<uintptr_t>(lse) & 3u)) return HEART_ERR_INVALID;
+  g_launches = 0;
+  cudaError_t e = launch_cache_rows(g, ix, w, Q, *cache, O, lse, static_cast<cudaStream_t>(stream), &g_launches);
+  if (e != cudaSuccess) return cuda_fail(e, "cache_attention");
+  return HEART_OK;
+}
+
 size_t heart_band_error_workspace_bytes(int32_t C, int32_t T, int32_t H, int32_t W) {
   if (C < 1 || T < 1 || H < 1 || W < 1 || (long long)C * T * H * W > (1LL << 31)) return 0;
   return band_error_workspace_bytes(C, T, H, W);
@@ -402,7 +526,9 @@ const char *heart_strerror(int code) {
   switch (code) {
     case HEART_OK: return "ok";
     case HEART_ERR_INVALID: return "invalid argument (null pointer, size, stride or alignment)";
-    case HEART_ERR_UNSUPPORTED: return "unsupported shape (head_dim must be 128, block 64 or 128, at most 1024 blocks)";
+    case HEART_ERR_UNSUPPORTED:
+      return "unsupported shape (head_dim must be 128, block 64 or 128, at most 1024 blocks; caches: page 16, 32, 64 or 128, at most 128 query heads a "
+             "key head, fewer than 2^31 rows and tokens)";
     case HEART_ERR_CUDA: return g_errbuf[0] ? g_errbuf : "CUDA error";
     case HEART_ERR_TOO_LARGE: return "shape needs more scratch than the built-in HEART_STATIC_SCRATCH_BYTES array holds";
     case HEART_ERR_INFEASIBLE: return "no assignment of one candidate per head meets the sparsity budget";

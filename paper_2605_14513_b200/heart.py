@@ -18,6 +18,7 @@ OK, ERR_INVALID, ERR_UNSUPPORTED, ERR_CUDA, ERR_DEVICE_CHECK, ERR_TOO_LARGE, ERR
 STATIC_SCRATCH_BYTES = 16 << 20
 FORCE_REFRESH, FORCE_DENSE, BLOCK_MEANS_VALID, ESTIMATOR_ANTIDIAG = 1, 2, 4, 8
 MAX_BLOCKS = 1024
+CACHE_BF16, CACHE_E4M3 = 0, 1
 
 # Every symbol include/heart.h declares.
 SYMBOLS = (
@@ -25,7 +26,7 @@ SYMBOLS = (
     "heart_block_sparse_attn", "heart_step", "heart_step_host", "heart_get_status", "heart_strerror",
     "heart_last_launch_count", "heart_drift_static", "heart_full_token_drift", "heart_mask_iou",
     "heart_band_error_workspace_bytes", "heart_band_error", "heart_drift_workspace_bytes",
-    "heart_assign_thresholds",
+    "heart_assign_thresholds", "heart_cache_workspace_bytes", "heart_cache_write", "heart_cache_read", "heart_cache_attn",
 )
 
 
@@ -40,6 +41,17 @@ class Config(C.Structure):
 class StateStruct(C.Structure):
     _fields_ = [("anchor_q", C.c_void_p), ("anchor_k", C.c_void_p), ("has_anchor", C.c_void_p),
                 ("mask_bits", C.c_void_p), ("kv_idx", C.c_void_p), ("kv_cnt", C.c_void_p)]
+
+
+class CacheConfig(C.Structure):
+    _fields_ = ([(x, C.c_int32) for x in ("S", "T", "Hq", "Hkv", "D", "page", "n_pages", "table_stride", "kind", "max_new", "causal",
+                                          "window", "sink")] + [("flags", C.c_uint32)] +
+                [(x, C.c_int64) for x in ("q_stride_t", "q_stride_h", "kv_stride_t", "kv_stride_h", "pool_stride_page", "pool_stride_h",
+                                          "pool_stride_t")] + [("scale", C.c_double)])
+
+
+class CacheStruct(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
 
 
 class HeartError(RuntimeError):
@@ -95,8 +107,13 @@ def load(path):
         l.heart_assign_thresholds.argtypes = [vp, vp, C.c_int32, C.c_int32, C.c_double, vp, C.POINTER(C.c_double),
                                               C.POINTER(C.c_double), C.POINTER(C.c_int32)]
         l.heart_assign_thresholds.restype = C.c_int
+        l.heart_cache_workspace_bytes.argtypes = [C.POINTER(CacheConfig)]
+        l.heart_cache_workspace_bytes.restype = C.c_size_t
+        l.heart_cache_write.argtypes = [C.POINTER(CacheConfig), vp, vp, C.POINTER(CacheStruct)] + [vp] * 5
+        l.heart_cache_read.argtypes = [C.POINTER(CacheConfig), C.POINTER(CacheStruct)] + [vp] * 7
+        l.heart_cache_attn.argtypes = [C.POINTER(CacheConfig), vp, C.POINTER(CacheStruct)] + [vp] * 7
         for fn in ("heart_state_reset", "heart_drift", "heart_predict_mask", "heart_block_sparse_attn",
-                   "heart_step", "heart_step_host", "heart_get_status"):
+                   "heart_step", "heart_step_host", "heart_get_status", "heart_cache_write", "heart_cache_read", "heart_cache_attn"):
             getattr(l, fn).restype = C.c_int
     return l
 
@@ -224,6 +241,105 @@ def heart_drift_static(cfg, Q, K, delta, st: State, drift_out=None, refresh_out=
     16 MiB array (shapes that need more raise ERR_TOO_LARGE).  Calls on one device must not overlap."""
     _check(lib().heart_drift_static(C.byref(cfg), _ptr(Q), _ptr(K), _ptr(delta), C.byref(st.struct),
                                     _ptr(drift_out), _ptr(refresh_out), _stream()))
+
+
+# ---- A paged cache of keys and values, and attention over it (include/heart.h has the definitions).
+
+
+def make_cache_config(S, T, Hq, Hkv, page, n_pages, table_stride, kind=CACHE_BF16, D=128, max_new=0, causal=0, window=0, sink=0, scale=0.0,
+                      q_strides=(0, 0), kv_strides=(0, 0), pool_strides=(0, 0, 0)) -> CacheConfig:
+    """S sequences, T rows of the packed tensors.  Strides in elements: (token, head) of Q and O, (token, head) of the
+    packed K and V, (page, head, token) of the pools; zeros select the contiguous layouts."""
+    return CacheConfig(S, T, Hq, Hkv, D, page, n_pages, table_stride, kind, max_new, causal, window, sink, 0, *q_strides, *kv_strides,
+                       *pool_strides, scale)
+
+
+class Cache:
+    """Caller-owned pools of a paged cache (device tensors + the C struct that points at them): new ones, zero-filled, or the
+    tensors given.  k, v: [n_pages, Hkv, page, D] elements as cfg lays them out, bf16 or float8_e4m3fn; k_scale, v_scale
+    (e4m3): uint8 [n_pages, Hkv, page]."""
+
+    def __init__(self, cfg: CacheConfig, k=None, v=None, k_scale=None, v_scale=None, device="cuda"):
+        e4m3 = cfg.kind == CACHE_E4M3
+        shape = (cfg.n_pages, cfg.Hkv, cfg.page)
+        dtype = torch.float8_e4m3fn if e4m3 else torch.bfloat16
+
+        def new(*a):
+            return torch.zeros(a, dtype=torch.uint8 if e4m3 else dtype, device=device).view(dtype)
+
+        self.k, self.v = (new(*shape, cfg.D) if x is None else x for x in (k, v))
+        self.k_scale, self.v_scale = ((torch.zeros(shape, dtype=torch.uint8, device=device) if x is None and e4m3 else x)
+                                      for x in (k_scale, v_scale))
+        strides = (cfg.pool_stride_page, cfg.pool_stride_h, cfg.pool_stride_t)
+        for x in (self.k, self.v):
+            plain = (cfg.Hkv * cfg.page * cfg.D, cfg.page * cfg.D, cfg.D)
+            if (x.dtype != dtype or tuple(x.shape) != shape + (cfg.D,) or not x.is_cuda or x.device != self.k.device or x.stride(3) != 1 or
+                    any(n > 1 and have != want for n, have, want in zip(shape, x.stride(), strides if any(strides) else plain))):
+                raise ValueError(f"a pool has to be {dtype} {shape + (cfg.D,)} on a GPU, in cfg's layout: got {x.dtype} {tuple(x.shape)}, strides {x.stride()}")
+        for x in (self.k_scale, self.v_scale) if e4m3 else ():
+            if x.dtype != torch.uint8 or tuple(x.shape) != shape or x.device != self.k.device or not x.is_contiguous():
+                raise ValueError(f"scales have to be contiguous uint8 {shape} beside the pools: got {x.dtype} {tuple(x.shape)}")
+        self.device = self.k.get_device()
+        self.struct = CacheStruct(*(None if x is None else x.data_ptr() for x in (self.k, self.v, self.k_scale, self.v_scale)))
+
+
+def cache_workspace_bytes(cfg: CacheConfig) -> int:
+    return int(lib().heart_cache_workspace_bytes(C.byref(cfg)))
+
+
+def new_cache_workspace(cfg: CacheConfig, device="cuda") -> torch.Tensor:
+    n = cache_workspace_bytes(cfg)
+    if n == 0:
+        raise HeartError(ERR_UNSUPPORTED)
+    return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+def _cache_call(cfg, cache, rows, heads, strides, tensors, page_table, row_start, kv_len, ws):
+    """Checks what the library cannot see (types, sizes, devices); rows: the number of rows of the packed `tensors`."""
+    device = cache.device
+    for x in tensors:
+        if x.dtype != torch.bfloat16 or x.numel() != rows * heads * 128 or x.get_device() != device or x.stride(-1) != 1:
+            raise ValueError(f"packed tensors have to be bf16, {rows} rows x {heads} heads x 128, beside the cache: got {x.dtype} {tuple(x.shape)} on {x.device}")
+        if strides == (0, 0) and not x.is_contiguous():
+            raise ValueError(f"a packed tensor that is not contiguous needs its strides in the config: got {tuple(x.shape)}, strides {x.stride()}")
+    for x, n in ((page_table, cfg.S * cfg.table_stride), (row_start, cfg.S + 1), (kv_len, cfg.S)):
+        if x.dtype != torch.int32 or x.numel() != n or x.get_device() != device or not x.is_contiguous():
+            raise ValueError(f"page_table, row_start and kv_len have to be contiguous int32 of {cfg.S} x {cfg.table_stride}, {cfg.S + 1} and {cfg.S} "
+                             f"entries beside the cache: got {x.dtype} {tuple(x.shape)} on {x.device}")
+    if ws.get_device() != device or ws.numel() * ws.element_size() < cache_workspace_bytes(cfg):
+        raise ValueError(f"the workspace has to have cache_workspace_bytes(cfg) = {cache_workspace_bytes(cfg)} bytes beside the cache")
+
+
+def _on(device, call, *args):
+    """The call on the current stream of the tensors' device."""
+    if device == torch.cuda.current_device():
+        return _check(call(*args, _stream()))
+    with torch.cuda.device(device):
+        return _check(call(*args, _stream()))
+
+
+def heart_cache_write(cfg, K, V, cache: Cache, page_table, row_start, kv_len, ws):
+    """Stores the packed rows of K and V (bf16 [T, Hkv, D]), the last tokens of their sequences, in their pages."""
+    _cache_call(cfg, cache, cfg.T, cfg.Hkv, (cfg.kv_stride_t, cfg.kv_stride_h), (K, V), page_table, row_start, kv_len, ws)
+    _on(cache.device, lib().heart_cache_write, C.byref(cfg), _ptr(K), _ptr(V), C.byref(cache.struct), _ptr(page_table), _ptr(row_start),
+        _ptr(kv_len), _ptr(ws))
+
+
+def heart_cache_read(cfg, cache: Cache, page_table, row_start, kv_len, K_out, V_out, ws):
+    """The last tokens of the sequences out of their pages into the packed rows of K_out and V_out (bf16 [T, Hkv, D])."""
+    _cache_call(cfg, cache, cfg.T, cfg.Hkv, (cfg.kv_stride_t, cfg.kv_stride_h), (K_out, V_out), page_table, row_start, kv_len, ws)
+    _on(cache.device, lib().heart_cache_read, C.byref(cfg), C.byref(cache.struct), _ptr(page_table), _ptr(row_start), _ptr(kv_len),
+        _ptr(K_out), _ptr(V_out), _ptr(ws))
+
+
+def heart_cache_attn(cfg, Q, cache: Cache, page_table, row_start, kv_len, O, ws, lse=None):
+    """Attention of the packed rows of Q (bf16 [T, Hq, D]), the last tokens of their sequences, over the sequences' pages
+    into O; lse: optional fp32 [T, Hq]."""
+    _cache_call(cfg, cache, cfg.T, cfg.Hq, (cfg.q_stride_t, cfg.q_stride_h), (Q, O), page_table, row_start, kv_len, ws)
+    if lse is not None and (lse.dtype != torch.float32 or lse.numel() != cfg.T * cfg.Hq or lse.get_device() != cache.device or not lse.is_contiguous()):
+        raise ValueError(f"lse has to be contiguous fp32 [{cfg.T}, {cfg.Hq}] beside the cache: got {lse.dtype} {tuple(lse.shape)} on {lse.device}")
+    _on(cache.device, lib().heart_cache_attn, C.byref(cfg), _ptr(Q), C.byref(cache.struct), _ptr(page_table), _ptr(row_start), _ptr(kv_len),
+        _ptr(O), _ptr(lse), _ptr(ws))
 
 
 def heart_full_token_drift(cfg, Qa, Ka, Qb, Kb, drift_out, ws):
