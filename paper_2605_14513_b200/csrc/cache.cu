@@ -123,7 +123,6 @@ __device__ __forceinline__ uint32_t from_e4m3x2(uint32_t codes, float scale) {
   const float lo = bf16_low(t) * 0x1p120f * scale, hi = bf16_high(t) * 0x1p120f * scale;
   return __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632);
 }
-__device__ __forceinline__ float scale_of(uint32_t byte) { return byte == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(byte << 23); }
 
 template <bool E4m3>
 __global__ void __launch_bounds__(32 * kWarps) cache_read_kernel(const CopyParams p) {
@@ -164,7 +163,7 @@ __global__ void __launch_bounds__(32 * kWarps) cache_read_kernel(const CopyParam
   for (int u = 0; u < kHeads; ++u) {
     if (h0 + u >= p.Hkv) break;
     if (E4m3) {
-      const float scale = scale_of(b[u]);
+      const float scale = cache_scale(b[u]);
       const uint2 c = make_uint2(x[u].x, x[u].y);
       x[u] = make_uint4(from_e4m3x2(c.x & 0xffffu, scale), from_e4m3x2(c.x >> 16, scale), from_e4m3x2(c.y & 0xffffu, scale),
                         from_e4m3x2(c.y >> 16, scale));

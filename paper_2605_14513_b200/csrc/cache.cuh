@@ -27,11 +27,12 @@ struct CacheIndex {
 
 struct CacheWorkspace {
   int32_t *status;    // [64] word 0: sticky device-check code
-  int32_t *arrivals;  // [kCacheCtas] parts of a shared tile that are there (zero between launches)
+  int32_t *arrivals;  // [2][kCacheCtas] parts of a shared tile that are there: the rows kernel's (zero between launches), the tile kernel's
   float *parts;       // [2 * kCacheCtas][128][128] parts of tiles: unnormalised sums of values
   float2 *part_l;     // [2 * kCacheCtas][128] their row sums and references
-  int4 *tiles;        // [max_tiles + 1] tiles of a head (see cache_tiles.cu)
-  int32_t *tile_first;  // [max_tiles + 1] key steps before a tile
+  void *tiles;        // [max_tiles] tiles of a head, 32 bytes each (see cache_tiles.cu)
+  long long *tile_first;  // [max_tiles + 1] key steps before a tile
+  int *tile_head;     // [64] number of tiles, most steps of a tile
   size_t bytes;
 };
 
@@ -48,11 +49,12 @@ __host__ inline CacheWorkspace carve_cache(const CacheGeom &g, void *base) {
     return at;
   };
   w.status = reinterpret_cast<int32_t *>(take(64 * sizeof(int32_t)));
-  w.arrivals = reinterpret_cast<int32_t *>(take(kCacheCtas * sizeof(int32_t)));
+  w.arrivals = reinterpret_cast<int32_t *>(take(2 * kCacheCtas * sizeof(int32_t)));
   w.parts = reinterpret_cast<float *>(take(sizeof(float) * 2 * kCacheCtas * 128 * kD));
   w.part_l = reinterpret_cast<float2 *>(take(sizeof(float2) * 2 * kCacheCtas * 128));
-  w.tiles = reinterpret_cast<int4 *>(take(sizeof(int4) * (cache_max_tiles(g) + 1)));
-  w.tile_first = reinterpret_cast<int32_t *>(take(sizeof(int32_t) * (cache_max_tiles(g) + 1)));
+  w.tiles = take(32 * cache_max_tiles(g));
+  w.tile_first = reinterpret_cast<long long *>(take(sizeof(long long) * (cache_max_tiles(g) + 1)));
+  w.tile_head = reinterpret_cast<int *>(take(64 * sizeof(int)));
   w.bytes = off;
   return w;
 }
@@ -63,15 +65,21 @@ cudaError_t launch_cache_write(const CacheGeom &g, const CacheIndex &ix, const v
                                cudaStream_t s, int *launches);
 cudaError_t launch_cache_read(const CacheGeom &g, const CacheIndex &ix, const heart_cache &c, void *K, void *V, cudaStream_t s,
                               int *launches);
-// Attention by query rows in registers (few rows a sequence and head) or by 128-row tiles.
-bool cache_rows_kernel_fits(const CacheGeom &g);
+// Attention by 16 or 32 query rows in registers, or by tiles of 128: the former where a sequence and key head has so few rows.
+constexpr int kRowsOfRowsKernel = 32;
 cudaError_t launch_cache_rows(const CacheGeom &g, const CacheIndex &ix, const CacheWorkspace &w, const void *Q, const heart_cache &c,
                               void *O, float *lse, cudaStream_t s, int *launches);
+cudaError_t launch_cache_tiles(const CacheGeom &g, const CacheIndex &ix, const CacheWorkspace &w, const void *Q, const heart_cache &c,
+                               void *O, float *lse, cudaStream_t s, int *launches);
 
 // A pool as a tensor map: boxes of `rows` slots of one head (of bf16, `halves` halves of their 128 dims).
 bool make_pool_map(CUtensorMap *m, const void *base, const CacheGeom &g, int rows, int halves);
 
 #ifdef __CUDACC__
+// A scale byte as a number: 2^(byte - 127), NaN for 255.
+__device__ __forceinline__ float cache_scale(uint32_t byte) {
+  return __uint_as_float(byte == 255u ? 0x7fc00000u : byte == 0u ? 0x00400000u : byte << 23);
+}
 // A sequence as its arrays describe it, brought into range (and reported) where they do not hold what they should.
 struct Sequence {
   int row, n, len;  // first row, new tokens, tokens

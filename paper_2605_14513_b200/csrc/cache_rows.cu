@@ -84,7 +84,6 @@ __device__ __forceinline__ void e4m3_to_bf16(uint32_t w, uint32_t &even, uint32_
   asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(even) : "r"(e), "r"(kTwo120));
   asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(odd) : "r"(o), "r"(kTwo120));
 }
-__device__ __forceinline__ float scale_of(uint32_t byte) { return byte == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(byte << 23); }
 __device__ __forceinline__ bool not_finite(uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
 
 template <int MT, bool E4m3>
@@ -314,8 +313,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const int key = (k >> 1) * 8 + c * 2 + (k & 1);
-        ks4[k] = E4m3 ? scale_of(sh.scales[warp][st][key]) * p.scale_log2 : p.scale_log2;
-        vs4[k] = E4m3 ? scale_of(sh.scales[warp][st][kKeys + key]) : 1.f;
+        ks4[k] = E4m3 ? cache_scale(sh.scales[warp][st][key]) * p.scale_log2 : p.scale_log2;
+        vs4[k] = E4m3 ? cache_scale(sh.scales[warp][st][kKeys + key]) : 1.f;
       }
       // ---- weights
       auto hidden = [&](const Visible &v, int k) { return k >= v.end || (k < v.low && k >= ix.sink); };
@@ -582,8 +581,6 @@ cudaError_t launch(const CacheGeom &g, const RowsParams &p, const CUtensorMap &m
 }
 
 }  // namespace
-
-bool cache_rows_kernel_fits(const CacheGeom &g) { return true; }
 
 cudaError_t launch_cache_rows(const CacheGeom &g, const CacheIndex &ix, const CacheWorkspace &w, const void *Q, const heart_cache &c,
                               void *O, float *lse, cudaStream_t s, int *launches) {

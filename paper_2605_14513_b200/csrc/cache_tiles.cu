@@ -1,0 +1,1134 @@
+// Attention over a paged cache for many query rows a sequence and key head, on the sm_100a tensor cores.
+//
+// A tile is 128 rows: 128 / G tokens of a sequence with the G query heads of one key head.  Keys are processed 128 at a time, one
+// CTA an SM, two softmax warpgroups that take a tile's key steps (nearly) in turn, scores double-buffered in tensor memory; the
+// reasons are those at the top of attn_tc.cu, and so are what bounds it (the tensor pipe 1024 clocks a step, the special-function
+// units 1024, shared memory 1280) and the way two warpgroups agree on a row's reference.  What differs:
+//   * Keys and values come page by page, 128 / page boxes for every 128 keys, with the page numbers fetched a step ahead.
+//   * Rows see different keys.  Steps that some row does not see whole have a path of their own, outside of the loop over the steps:
+//     hidden scores become -inf in tensor memory, and values that are not finite (what lies behind a sequence's end is anyone's) are
+//     taken out of shared memory first, because the product reads them with weight 0; rows that do see such a value are marked.
+//   * All steps of all tiles, (key head, tile, step) in one line, are cut into equal shares, one a CTA, so that the launch ends on all
+//     SMs at once whatever the lengths are.  Parts of a tile go to the workspace; the CTA that brings the last one puts them together, in
+//     order: the result does not depend on which one that is.
+//
+// e4m3 caches.  Converting keys and values to bf16 for 128 rows costs as many instructions as the softmax does.  Keys need none: a bf16 query has
+// 8 significant bits and a code 4, so a query row, scaled by a power of two, is the sum of two rows of codes, to 2^-18 of its
+// largest element, and two products with the keys' codes at twice the rate take the time of one in bf16.  Weights are
+// not split that way (many keys of little weight each would be lost): values are converted, by a fourth warpgroup, and multiplied by
+// their tokens' scales on the way, which is exact.  The keys' scales multiply the scores.
+//
+// Warp roles: 0-3, 4-7 softmax; 8 issues S = Q K^T; 9 V producer; 10 K and Q producer (finds the CTA's tiles); 11 issues
+// O += P V; 12-15 (e4m3) convert.  Tensor memory: O (128 columns) | S[2] (2 x 128) | P[2] (2 x 64).
+// Every wait is bounded; one that runs out raises the CTA's abort flag and the status word, and its roles stop.
+#include "cache.cuh"
+#include "tc_ptx.cuh"
+
+namespace heart {
+using namespace tc;
+namespace {
+
+constexpr int kWarpQK = 8, kWarpV = 9, kWarpK = 10, kWarpPV = 11, kWarpConvert = 12;
+constexpr int kTileBytes = 32768;  // 128 rows x 128 dims of bf16: [2 dim halves][128 rows][64], 128-byte swizzle
+constexpr int kCodeBytes = 16384;  // the same as e4m3: [128 rows][128]
+constexpr int kPartRing = 4;
+constexpr int kMaxParts = 12;      // of a tile, about
+constexpr float kNoReference = -3.0e38f;
+constexpr float kHeadroom = 16.f, kMaxGrowth = 8.f;  // see attn_tc.cu
+constexpr uint32_t kShortWait = 500;
+
+// A tile of a head as the plan kernel writes it.
+struct Tile {
+  int s, row, tokens, p0;         // sequence; first packed row; new tokens; position of the first
+  int len, sinks, first, steps;   // tokens of the sequence; its key steps (see Span)
+};
+static_assert(sizeof(Tile) == 32, "two words of 16 bytes");
+
+// Part of a tile that a CTA takes: steps a .. b - 1 for key head h.
+struct Part {
+  Tile t;
+  int h, a, b;       // b < 0: no part left
+  int c0, parts;     // first CTA with a part of the tile, and how many there are
+  int pad[3];
+};
+static_assert(sizeof(Part) == 64, "lanes copy words");
+
+template <bool E4m3>
+struct Layout {
+  static constexpr int kThreads = E4m3 ? 512 : 384;
+  static constexpr int kRegsSoftmax = E4m3 ? 184 : 224, kRegsHelper = E4m3 ? 64 : 56, kRegsConvert = 80;  // sums: the registers at launch
+  static constexpr int kReaders = E4m3 ? 15 : 11;  // of announced parts: softmax warps, issuers, V producer, converters
+  static constexpr int kKey = E4m3 ? kCodeBytes : kTileBytes;
+  // Q, K, V (of which the products read), codes of V
+  static constexpr int kOffQ = 0, kOffK = 2 * kTileBytes, kOffV = kOffK + 2 * kKey, kOffCodes = kOffV + 2 * kTileBytes;
+  static constexpr int kOffShared = kOffCodes + (E4m3 ? 2 * kCodeBytes : 0);
+};
+
+struct TileShared {
+  uint64_t q_full[2], k_full[2], v_full[2];
+  uint64_t q_ready[2];     // e4m3: Q as codes
+  uint64_t v_ready[2];     // e4m3: V_g converted; bf16: V_g has nothing in it that is not finite, if its step is masked
+  uint64_t codes_free[2];  // e4m3: the codes of V_g have been read
+  uint64_t s_full[2], s_free[2], p_full[2], pv_done[2], m_ready[2][4];  // as in attn_tc.cu
+  uint64_t o_full[2], o_free, out_done[2];
+  uint64_t part_full[kPartRing], part_empty[kPartRing];
+  uint64_t drain[2];
+  uint64_t stored[2], told[2];  // a warpgroup's part of a tile is in the workspace; it is the last one or not
+  Part part[kPartRing];
+  Part written[2][8];        // the part to write, per softmax warp
+  Tile k_tile[2], v_tile;    // the K producer's present and next tile, by its part & 1, the V producer's (helper warps have few registers)
+  uint32_t entry[4];         // steps in flight: step | masked << 31
+  float m[2][128];           // references after step g
+  float2 l[4][2][128];       // row sums and references: per part & 3 and warpgroup (a warpgroup may be two short parts ahead of one that writes)
+  alignas(16) float k_scale[8][128];  // e4m3, steps in flight, by g & 7: read behind the hand-back of the scores, before the reference of step g is there
+  alignas(16) float v_scale[2][128];
+  float q_scale[2][128];     // e4m3: what the scores of a row are to be multiplied by
+  uint32_t bad[4][4];        // keys of a masked step that are not finite, by g & 3
+  uint32_t tmem_base;
+  int last[2];
+  int abort;
+};
+template <bool E4m3>
+constexpr int kSmem = Layout<E4m3>::kOffShared + sizeof(TileShared);
+static_assert(kSmem<true> <= 232448 && kSmem<false> <= 232448, "shared memory of an SM");
+
+struct TileParams {
+  CacheIndex ix;
+  const Tile *tiles;
+  const long long *first;  // [tiles + 1] key steps before a tile of a head
+  const int *head;         // number of tiles, most steps of a tile
+  int32_t *arrivals;
+  float4 *parts;           // [2 * CTAs][32][128]: four dims of a row
+  float2 *part_l;          // [2 * CTAs][128]
+  uint16_t *O;
+  float *lse;
+  const uint8_t *k_scale, *v_scale;
+  long long qt, qh;
+  int Hq, Hkv, G;
+  float scale_log2;
+};
+
+__device__ __forceinline__ float fmax3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+// Weights 2^(s*c - m) of 32 scores of a row, packed to bf16, and their sums (of the weights before they are rounded: the log-sum-exp
+// is then good to 32 bits).
+__device__ __forceinline__ void exp32(const uint32_t *s, uint64_t c2, uint64_t neg_m2, uint32_t *pk, uint64_t (&sums)[2]) {
+#pragma unroll
+  for (int i = 0; i < 32; i += 4) {
+    float x0, x1, x2, x3;
+    unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), c2, neg_m2), x0, x1);
+    unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(s[i + 2]), __uint_as_float(s[i + 3])), c2, neg_m2), x2, x3);
+    x0 = ex2(x0), x1 = ex2(x1), x2 = ex2(x2), x3 = ex2(x3);
+    sums[0] = add_f32x2(sums[0], pack_f32x2(x0, x1));
+    sums[1] = add_f32x2(sums[1], pack_f32x2(x2, x3));
+    pk[i >> 1] = pack_bf16x2(x0, x1);
+    pk[(i >> 1) + 1] = pack_bf16x2(x2, x3);
+  }
+}
+__device__ __forceinline__ float max64(const uint32_t *s) {
+  float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+  for (int i = 0; i < 64; i += 8)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) m[j] = fmax3(m[j], __uint_as_float(s[i + 2 * j]), __uint_as_float(s[i + 2 * j + 1]));
+  return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+}
+// D[tmem] (+)= A[smem] * B[smem], e4m3
+__device__ __forceinline__ void mma_ss_e4m3(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__host__ __device__ constexpr uint32_t idesc_e4m3_f32(int M, int N) {
+  return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);  // D f32, A and B e4m3 (0), K-major
+}
+__device__ __forceinline__ uint4 lds_u4(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void sts_u4(uint32_t addr, uint4 v) {
+  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ bool not_finite(uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
+// ---------------------------------------------------------------------- plan
+// The tiles of a head, sequence by sequence, and the key steps before each.  One CTA.
+__global__ void __launch_bounds__(1024) cache_plan_kernel(const CacheIndex ix, int tokens_per_tile, Tile *__restrict__ tiles,
+                                                          long long *__restrict__ first, int *__restrict__ head, int32_t *__restrict__ arrivals, int most) {
+  __shared__ long long sums[32];
+  __shared__ int base[1024];
+  const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+  pdl_wait();
+  pdl_launch_dependents();
+  for (int i = t; i < kCacheCtas; i += 1024) arrivals[i] = 0;
+  auto scan = [&](long long mine, long long &all) {  // exclusive, over the CTA
+    long long x = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    __syncthreads();
+    if (lane == 31) sums[warp] = x;
+    __syncthreads();
+    long long before = x - mine;
+    all = 0;
+    for (int i = 0; i < 32; ++i) {
+      if (i < warp) before += sums[i];
+      all += sums[i];
+    }
+    return before;
+  };
+  int n_tiles = 0, longest = 1;
+  for (int s0 = 0; s0 < ix.S; s0 += 1024) {
+    const int mine = s0 + t < ix.S ? (sequence(ix, s0 + t).n + tokens_per_tile - 1) / tokens_per_tile : 0;
+    long long all;
+    base[t] = (int)min(n_tiles + scan(mine, all), (long long)most);
+    __syncthreads();
+    for (int i = warp; i < 1024 && s0 + i < ix.S; i += 32) {  // a warp a sequence
+      const Sequence q = sequence(ix, s0 + i);
+      for (int k = lane; k * tokens_per_tile < q.n && base[i] + k < most; k += 32) {
+        Tile x;
+        x.s = s0 + i;
+        x.row = q.row + k * tokens_per_tile;
+        x.tokens = min(tokens_per_tile, q.n - k * tokens_per_tile);
+        x.p0 = q.len - q.n + k * tokens_per_tile;
+        x.len = q.len;
+        const Span sp = span_of(ix, x.p0, x.p0 + x.tokens - 1, q.len);
+        x.sinks = sp.sinks;
+        x.first = sp.first;
+        x.steps = sp.steps;
+        tiles[base[i] + k] = x;
+      }
+    }
+    n_tiles = (int)min(n_tiles + all, (long long)most);  // (more: starts that do not ascend, which are reported)
+    __syncthreads();
+  }
+  long long before = 0;
+  for (int t0 = 0; t0 < n_tiles; t0 += 1024) {
+    const int mine = t0 + t < n_tiles ? tiles[t0 + t].steps : 0;
+    longest = max(longest, mine);
+    long long all;
+    const long long at = before + scan(mine, all);
+    if (t0 + t < n_tiles) first[t0 + t] = at;
+    before += all;
+  }
+  longest = __reduce_max_sync(0xffffffffu, longest);
+  __syncthreads();
+  if (lane == 0) sums[warp] = longest;
+  __syncthreads();
+  if (t == 0) {
+    for (int i = 0; i < 32; ++i) longest = max(longest, (int)sums[i]);
+    first[n_tiles] = before;
+    head[0] = n_tiles;
+    head[1] = longest;
+  }
+}
+
+// ---------------------------------------------------------------------- attention
+template <bool E4m3>
+__global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
+    cache_tile_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                      const __grid_constant__ CUtensorMap map_v, const TileParams p) {
+  using L = Layout<E4m3>;
+  extern __shared__ __align__(1024) unsigned char smem[];
+  TileShared &sh = *reinterpret_cast<TileShared *>(smem + L::kOffShared);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const CacheIndex &ix = p.ix;
+  volatile int *abort = &sh.abort;
+
+  // ------------------------------------------------------------------ set-up
+  if (tid == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sh.q_full[i], 1);
+      mbar_init(&sh.k_full[i], 1);
+      mbar_init(&sh.v_full[i], 1);
+      mbar_init(&sh.q_ready[i], 4);
+      mbar_init(&sh.v_ready[i], E4m3 ? 4 : 1);
+      mbar_init(&sh.codes_free[i], 4);
+      mbar_init(&sh.s_full[i], 1);
+      mbar_init(&sh.s_free[i], 4);
+      mbar_init(&sh.p_full[i], 4);
+      mbar_init(&sh.pv_done[i], 1);
+      for (int q = 0; q < 4; ++q) mbar_init(&sh.m_ready[i][q], 1);
+      mbar_init(&sh.o_full[i], 1);
+      mbar_init(&sh.out_done[i], 4);
+      mbar_init(&sh.drain[i], 1);
+      mbar_init(&sh.stored[i], 4);
+      mbar_init(&sh.told[i], 1);
+    }
+    for (int i = 0; i < kPartRing; ++i) {
+      mbar_init(&sh.part_full[i], 1);
+      mbar_init(&sh.part_empty[i], L::kReaders);
+    }
+    mbar_init(&sh.o_free, 4);
+    sh.abort = 0;
+    mbar_fence_init();
+  }
+  if (warp == kWarpQK) {
+    tmem_alloc(&sh.tmem_base, 512);
+    tmem_relinquish();
+  }
+  if (warp == kWarpK && lane == 0) {
+    tma_prefetch_desc(&map_q);
+    tma_prefetch_desc(&map_k);
+    tma_prefetch_desc(&map_v);
+  }
+  pdl_wait();
+  pdl_launch_dependents();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = sh.tmem_base;
+
+  // Bounded waits of a whole warp; ok turns false when one runs out or the CTA aborts.
+  bool ok = true;
+  auto wait = [&](uint64_t *bar, uint32_t parity) {
+    uint32_t since = 0;
+#pragma unroll 1
+    while (__builtin_expect(!__all_sync(0xffffffffu, mbar_try_wait(bar, parity)), 0)) {
+      const uint32_t now = clock() | 1u;
+      if (since == 0) since = now;
+      if (__any_sync(0xffffffffu, *abort != 0 || now - since > (uint32_t)kWaitLimitCycles)) {
+        *abort = 1;
+        return ok = false;
+      }
+    }
+    return ok;
+  };
+  // The announced part n into registers' reach; false: none left (or abort).
+  auto part_at = [&](int n) -> const Part * {
+    if (!wait(&sh.part_full[n % kPartRing], (n / kPartRing) & 1)) return nullptr;
+    return &sh.part[n % kPartRing];
+  };
+  auto done_with_part = [&](int n) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sh.part_empty[n % kPartRing]);
+  };
+  auto settle = [&](uint64_t *bar, uint32_t parity) {
+    const uint32_t t0 = clock();
+    while (!mbar_try_wait(bar, parity) && (uint32_t)clock() - t0 < 40000000u) {
+    }
+  };
+  auto settle_pair = [&](uint64_t *bar, int issued) {  // the last two of `issued` copies on a pair of barriers
+#pragma unroll 1
+    for (int i = issued > 2 ? issued - 2 : 0; i < issued; ++i) settle(&bar[i & 1], (i >> 1) & 1);
+  };
+  auto desc_at = [](uint64_t desc, uint32_t off16) -> uint64_t {
+    return (desc & 0xffffffff00000000ull) | (uint32_t)((uint32_t)desc + off16);
+  };
+  auto drain_products = [&](bool leader, uint64_t *bar) {
+    if (!*abort) return;
+    if (leader) tc_commit(bar);
+    __syncwarp();
+    settle(bar, 0);
+  };
+  const int page_log2 = ix.page_log2, n_boxes = 128 >> page_log2;
+  auto key_of = [](const Tile &t, int i) { return (i < t.sinks ? i : t.first + i - t.sinks) * kKeyStep; };
+  // The page that lane i < n_boxes copies of the step at key k0.
+  auto pages_of = [&](const Tile &t, int k0) {
+    const int k = k0 + (lane << page_log2);
+    return lane < n_boxes && k < t.len ? page_of(ix, t.s, k) : ix.n_pages;  // (a page out of range: zeros)
+  };
+  auto load_pages = [&](unsigned char *dst, const CUtensorMap *map, uint64_t *bar, int h, int page) {
+    if (lane == 0) mbar_expect_tx(bar, L::kKey);
+    __syncwarp();
+    if (lane < n_boxes) {
+      unsigned char *to = dst + (lane << (page_log2 + 7));
+      tma_load_5d(to, map, bar, 0, 0, 0, h, page);
+      if (!E4m3 && n_boxes > 1) tma_load_5d(to + kTileBytes / 2, map, bar, 0, 0, 1, h, page);
+    }
+  };
+  // e4m3: the scale bytes of keys 4 * lane .. 4 * lane + 3 of a step, 127 where there are none
+  auto scales_of = [&](const uint8_t *scales, const Tile &t, int k0, int h, int page) -> uint32_t {
+    const int mine = __shfl_sync(0xffffffffu, page, (lane * 4) >> page_log2), k = k0 + lane * 4;
+    if (k >= t.len || mine >= ix.n_pages) return 0x7f7f7f7fu;
+    return __ldcg(reinterpret_cast<const uint32_t *>(scales + ((((size_t)mine * p.Hkv + h) << page_log2) + (k & ((1 << page_log2) - 1)))));
+  };
+  // Whether some row of the tile does not see all keys of the step at k0.
+  struct Whole {
+    int end, low;
+  };
+  auto whole_of = [&](const Tile &t) -> Whole {
+    return {t.p0 >= 0 ? visible(ix, t.p0, t.len).end : 0, visible(ix, t.p0 + t.tokens - 1, t.len).low};
+  };
+  auto masked_at = [&](const Whole &w, int k0) {
+    return !(k0 + kKeyStep <= w.end && (k0 >= w.low || k0 + kKeyStep <= ix.sink));
+  };
+
+  // ------------------------------------------------------------------ roles
+  if (warp >= kWarpConvert) {
+    setmaxnreg_dec<L::kRegsConvert>();
+  } else if (warp >= kWarpQK) {
+    setmaxnreg_dec<L::kRegsHelper>();
+  }
+  if (warp == kWarpK) {
+    // ===== the CTA's parts; K and Q producer
+    const int n_tiles = __ldcg(&p.head[0]), longest = __ldcg(&p.head[1]);
+    const long long per_head = __ldcg(&p.first[n_tiles]), total = per_head * p.Hkv;
+    const long long share = max((total + gridDim.x - 1) / gridDim.x, (long long)(longest + kMaxParts - 1) / kMaxParts);
+    long long u = blockIdx.x * share;
+    const long long u1 = min(total, u + share);
+    int h = 0, tile = 0, a = 0;
+    if (u < u1) {
+      h = (int)(u / per_head);
+      const long long rest = u - h * per_head;
+      int hi = n_tiles;  // first[tile] <= rest < first[hi]
+      while (hi - tile > 1) {
+        const int step = (hi - tile + 31) / 32, at = tile + lane * step;
+        const bool below = at < hi && (lane == 0 || __ldcg(&p.first[at]) <= rest);
+        const int n = __popc(__ballot_sync(0xffffffffu, below));
+        tile += (n - 1) * step;
+        hi = min(hi, tile + step);
+      }
+      a = (int)(rest - __ldcg(&p.first[tile]));
+    }
+    auto fetch = [&](Tile &to, int i) {
+      __syncwarp();
+      if (lane < 8) reinterpret_cast<int *>(&to)[lane] = __ldcg(reinterpret_cast<const int *>(&p.tiles[i]) + lane);
+      __syncwarp();
+    };
+    int g = 0, n = 0;
+    bool q_busy[2] = {false, false};
+    int page = 0, page_next = 0;
+    uint32_t ks = 0, ks_next = 0, vs = 0, vs_next = 0;
+    if (u < u1) {
+      const Tile &t = sh.k_tile[0];
+      fetch(sh.k_tile[0], tile);
+      page = pages_of(t, key_of(t, a));
+      if (E4m3) ks = scales_of(p.k_scale, t, key_of(t, a), h, page), vs = scales_of(p.v_scale, t, key_of(t, a), h, page);
+    }
+#pragma unroll 1
+    for (;; ++n) {
+      if (n >= kPartRing && !wait(&sh.part_empty[n % kPartRing], (n / kPartRing - 1) & 1)) break;
+      const bool any = u < u1;
+      const Tile &t = sh.k_tile[n & 1], &t_next = sh.k_tile[(n & 1) ^ 1];
+      const int b = any ? (int)min((long long)t.steps, a + (u1 - u)) : -1;
+      if (lane == 0) {
+        Part &x = sh.part[n % kPartRing];
+        x.t = t;
+        x.h = h;
+        x.a = a;
+        x.b = b;
+        const long long at = u - a;
+        x.c0 = (int)(at / share);
+        x.parts = any ? (int)((at + t.steps - 1) / share) - x.c0 + 1 : 0;
+        mbar_arrive(&sh.part_full[n % kPartRing]);
+      }
+      __syncwarp();
+      if (!any) break;
+      // the next part, ahead of time
+      const bool more = u + (b - a) < u1;
+      int h_next = h, tile_next = tile + 1;
+      if (tile_next == n_tiles) tile_next = 0, ++h_next;
+      if (more) fetch(sh.k_tile[(n & 1) ^ 1], tile_next);
+      const Whole whole = whole_of(t);
+#pragma unroll 1
+      for (int i = a; i < b; ++i, ++g) {
+        const int k0 = key_of(t, i);
+        if (i + 1 < b) {
+          page_next = pages_of(t, key_of(t, i + 1));
+        } else if (more) {
+          page_next = pages_of(t_next, key_of(t_next, 0));
+        }
+        if (g >= 2 && !wait(&sh.s_full[g & 1], ((g - 2) >> 1) & 1)) break;
+        bool masked = masked_at(whole, k0);
+        if (E4m3) {
+          // scales as numbers, and the tokens that have none
+          float f[4];
+          uint32_t bad[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t kb = (ks >> (8 * j)) & 255u, vb = (vs >> (8 * j)) & 255u;
+            f[j] = kb == 255u ? 1.f : cache_scale(kb);  // (more than 0: hidden scores of -inf stay -inf)
+            bad[j] = __ballot_sync(0xffffffffu, kb == 255u || vb == 255u);
+          }
+          *reinterpret_cast<float4 *>(&sh.k_scale[g & 7][lane * 4]) = make_float4(f[0], f[1], f[2], f[3]);
+          if (lane < 4) sh.bad[g & 3][lane] = lane == 0 ? bad[0] : lane == 1 ? bad[1] : lane == 2 ? bad[2] : bad[3];
+          masked |= (bad[0] | bad[1] | bad[2] | bad[3]) != 0u;
+        }
+        if (lane == 0) sh.entry[g & 3] = (uint32_t)(k0 / kKeyStep) | (masked ? 1u << 31 : 0u);
+        __syncwarp();
+        load_pages(smem + L::kOffK + (g & 1) * L::kKey, &map_k, &sh.k_full[g & 1], h, page);
+        if (i == a) {
+          if (n >= 2 && !wait(&sh.out_done[n & 1], ((n - 2) >> 1) & 1)) {
+            ++g;
+            break;
+          }
+          const int rows = 128 / p.G * p.G;
+          if (lane == 0) {
+            unsigned char *q = smem + L::kOffQ + (n & 1) * kTileBytes;
+            mbar_expect_tx(&sh.q_full[n & 1], 2 * rows * 128);
+            tma_load_5d(q, &map_q, &sh.q_full[n & 1], 0, 0, t.row, 0, h);
+            tma_load_5d(q + kTileBytes / 2, &map_q, &sh.q_full[n & 1], 0, 0, t.row, 1, h);
+          }
+          q_busy[n & 1] = true;
+        }
+        if (E4m3) {
+          const bool last = i + 1 == b;
+          if (!last || more) {
+            const int k_next = last ? key_of(t_next, 0) : key_of(t, i + 1);
+            ks_next = scales_of(p.k_scale, last ? t_next : t, k_next, last ? h_next : h, page_next);
+            vs_next = scales_of(p.v_scale, last ? t_next : t, k_next, last ? h_next : h, page_next);
+          }
+        }
+        page = page_next;
+        ks = ks_next;
+        vs = vs_next;
+      }
+      if (!ok) break;
+      u += b - a;
+      a = 0;
+      tile = tile_next;
+      h = h_next;
+    }
+    if (*abort) {
+      settle_pair(sh.k_full, g);
+      const int nq = n + (q_busy[n & 1] ? 1 : 0);
+      settle_pair(sh.q_full, nq);
+    }
+  } else if (warp == kWarpV) {
+    // ===== V producer
+    int g = 0;
+#pragma unroll 1
+    for (int n = 0; ok; ++n) {
+      const Part *x = part_at(n);
+      if (x == nullptr || x->b < 0) break;
+      const Tile &t = sh.v_tile;
+      const int h = x->h, a = x->a, b = x->b;
+      if (lane < 8) reinterpret_cast<int *>(&sh.v_tile)[lane] = reinterpret_cast<const int *>(&x->t)[lane];
+      done_with_part(n);
+      const Whole whole = whole_of(t);
+      int page = pages_of(t, key_of(t, a)), page_next = 0;
+      uint32_t vs = 0, vs_next = 0;
+      if (E4m3) vs = scales_of(p.v_scale, t, key_of(t, a), h, page);
+#pragma unroll 1
+      for (int i = a; i < b; ++i, ++g) {
+        const int k0 = key_of(t, i), at = g & 1;
+        if (i + 1 < b) page_next = pages_of(t, key_of(t, i + 1));
+        if (E4m3) {
+          if (g >= 2 && !wait(&sh.codes_free[at], ((g - 2) >> 1) & 1)) break;
+          float f[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t vb = (vs >> (8 * j)) & 255u;
+            // (behind the sequence's end, or not finite: nothing)
+            f[j] = vb == 255u || k0 + lane * 4 + j >= t.len ? 0.f : cache_scale(vb);
+          }
+          *reinterpret_cast<float4 *>(&sh.v_scale[at][lane * 4]) = make_float4(f[0], f[1], f[2], f[3]);
+          __syncwarp();
+          load_pages(smem + L::kOffCodes + at * kCodeBytes, &map_v, &sh.v_full[at], h, page);
+          if (i + 1 < b) vs_next = scales_of(p.v_scale, t, key_of(t, i + 1), h, page_next);
+        } else {
+          if (g >= 2 && !wait(&sh.pv_done[at], ((g - 2) >> 1) & 1)) break;
+          load_pages(smem + L::kOffV + at * kTileBytes, &map_v, &sh.v_full[at], h, page);
+          if (masked_at(whole, k0)) {
+            if (!wait(&sh.v_full[at], (g >> 1) & 1)) {
+              ++g;
+              break;
+            }
+            // values that are not finite: [2 dim halves][128 keys][8 x 16 bytes]
+            const uint32_t v_at = smem_u32(smem + L::kOffV + at * kTileBytes);
+            uint32_t bad[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+#pragma unroll 4
+              for (int j = 0; j < 16; ++j) {  // 32 keys: 8 pieces of 4 keys in each half
+                const uint4 v = lds_u4(v_at + (j >> 3) * (kTileBytes / 2) + w * 4096 + (j & 7) * 512 + lane * 16);
+                if (not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w)) bad[w] |= 1u << ((j & 7) * 4 + (lane >> 3));
+              }
+              bad[w] = __reduce_or_sync(0xffffffffu, bad[w]);
+            }
+            if (bad[0] | bad[1] | bad[2] | bad[3]) {
+#pragma unroll
+              for (int w = 0; w < 4; ++w)
+#pragma unroll 1
+                for (uint32_t todo = bad[w]; todo; todo &= todo - 1) {
+                  const int key = w * 32 + __ffs(todo) - 1;
+                  if (lane < 16) sts_u4(v_at + (lane >> 3) * (kTileBytes / 2) + key * 128 + (lane & 7) * 16, make_uint4(0u, 0u, 0u, 0u));
+                }
+              async_proxy_fence();
+            }
+            if (lane < 4) sh.bad[g & 3][lane] = lane == 0 ? bad[0] : lane == 1 ? bad[1] : lane == 2 ? bad[2] : bad[3];
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sh.v_ready[at]);
+        }
+        page = page_next;
+        vs = vs_next;
+      }
+    }
+    if (*abort) settle_pair(sh.v_full, g);
+  } else if (warp == kWarpQK) {
+    // ===== issuer of the score products
+    const uint64_t q_desc = smem_desc_sw128(smem_u32(smem + L::kOffQ), 16, 1024);
+    const uint64_t k_desc = smem_desc_sw128(smem_u32(smem + L::kOffK), 16, 1024);
+    const bool leader = elect_one();
+    uint32_t g = 0;
+#pragma unroll 1
+    for (int n = 0; ok; ++n) {
+      const Part *x = part_at(n);
+      if (x == nullptr || x->b < 0) break;
+      const int n_steps = x->b - x->a;
+      done_with_part(n);
+      wait(E4m3 ? &sh.q_ready[n & 1] : &sh.q_full[n & 1], (n >> 1) & 1);
+      const uint64_t qd = desc_at(q_desc, (n & 1) * (kTileBytes >> 4));
+#pragma unroll 1
+      for (int i = 0; i < n_steps; ++i, ++g) {  // S_g = Q K_g^T
+        const uint32_t b = g & 1;
+        if (g >= 2) wait(&sh.s_free[b], ((g - 2) >> 1) & 1);
+        if (!wait(&sh.k_full[b], (g >> 1) & 1)) break;
+        tc_fence_after();
+        if (leader) {
+          const uint64_t kd = desc_at(k_desc, b * (L::kKey >> 4));
+#pragma unroll
+          for (int ks = 0; ks < 8; ++ks) {
+            if (E4m3)  // the high parts of the queries, the low parts
+              mma_ss_e4m3(tmem + 128 + b * 128, desc_at(qd, (ks >> 2) * 1024 + (ks & 3) * 2), desc_at(kd, (ks & 3) * 2), idesc_e4m3_f32(128, 128), ks > 0 ? 1u : 0u);
+            else
+              mma_ss(tmem + 128 + b * 128, desc_at(qd, (ks >> 2) * 1024 + (ks & 3) * 2), desc_at(kd, (ks >> 2) * 1024 + (ks & 3) * 2),
+                     idesc_bf16_f32(128, 128, false, false), ks > 0 ? 1u : 0u);
+          }
+          tc_commit(&sh.s_full[b]);
+        }
+        __syncwarp();
+      }
+    }
+    drain_products(leader, &sh.drain[0]);
+  } else if (warp == kWarpPV) {
+    // ===== issuer of the value products
+    constexpr uint32_t idesc = idesc_bf16_f32(128, 128, false, true);
+    const uint64_t v_desc = smem_desc_sw128(smem_u32(smem + L::kOffV), kTileBytes / 2, 1024);
+    const bool leader = elect_one();
+    uint32_t g = 0;
+#pragma unroll 1
+    for (int n = 0; ok; ++n) {
+      const Part *x = part_at(n);
+      if (x == nullptr || x->b < 0) break;
+      const int n_steps = x->b - x->a;
+      done_with_part(n);
+      if (n > 0) wait(&sh.o_free, (n - 1) & 1);
+#pragma unroll 1
+      for (int i = 0; i < n_steps; ++i, ++g) {  // O (+)= P_g V_g
+        const uint32_t b = g & 1;
+        wait(E4m3 ? &sh.v_ready[b] : &sh.v_full[b], (g >> 1) & 1);
+        if (!wait(&sh.p_full[b], (g >> 1) & 1)) break;
+        tc_fence_after();
+        if (leader) {
+          const uint64_t vd = desc_at(v_desc, b * (kTileBytes >> 4));
+#pragma unroll
+          for (int ks = 0; ks < 8; ++ks)
+            mma_ts(tmem, tmem + 384 + b * 64 + ks * 8, desc_at(vd, ks * 128), idesc, (i > 0 || ks > 0) ? 1u : 0u);
+          if (i == n_steps - 1) tc_commit(&sh.o_full[n & 1]);
+          tc_commit(&sh.pv_done[b]);
+        }
+        __syncwarp();
+      }
+    }
+    drain_products(leader, &sh.drain[1]);
+  } else if (warp >= kWarpConvert) {
+    // ===== converters (e4m3): a thread a row of Q, a key of V
+    const int r = tid - kWarpConvert * 32;
+    uint32_t g = 0;
+#pragma unroll 1
+    for (int n = 0; ok; ++n) {
+      const Part *x = part_at(n);
+      if (x == nullptr || x->b < 0) break;
+      const int n_steps = x->b - x->a;
+      done_with_part(n);
+      // Q: q = 2^k (high + low), codes of both; the row's place in the first half holds the high parts, in the second the low ones
+      if (!wait(&sh.q_full[n & 1], (n >> 1) & 1)) break;
+      {
+        const uint32_t at = smem_u32(smem + L::kOffQ + (n & 1) * kTileBytes) + r * 128;
+        uint32_t top = 0u;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const uint4 q = lds_u4(at + (j >> 3) * (kTileBytes / 2) + (((j ^ r) & 7) << 4));
+          top = __vmaxu2(top, __vmaxu2(__vmaxu2(q.x & 0x7fff7fffu, q.y & 0x7fff7fffu), __vmaxu2(q.z & 0x7fff7fffu, q.w & 0x7fff7fffu)));
+        }
+        top = max(top & 0xffffu, top >> 16);
+        // the smallest power of two under which the largest magnitude is at most 448 (see heart_cache_write)
+        const int k = min(max((int)(top >> 7) - 135 + ((top & 0x7fu) > 0x60u ? 1 : 0), -100), 120);
+        const float inv = __uint_as_float((uint32_t)(127 - k) << 23);
+        sh.q_scale[n & 1][r] = top < 0x7f80u ? p.scale_log2 * __uint_as_float((uint32_t)(127 + k) << 23) : __uint_as_float(0x7fc00000u);
+        auto split = [&](uint32_t w, uint32_t &hi, uint32_t &lo) {  // two elements
+          const float x0 = __uint_as_float(w << 16) * inv, x1 = __uint_as_float(w & 0xffff0000u) * inv;
+          uint16_t c;
+          asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(x1), "f"(x0));
+          hi = c;
+          uint32_t y;
+          asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y) : "h"(c));
+          float y0, y1;
+          asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, h;\n\t}" : "=f"(y0), "=f"(y1) : "r"(y));
+          asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(x1 - y1), "f"(x0 - y0));
+          lo = c;
+        };
+        uint4 low[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {  // 16 dims: pieces 2j and 2j + 1 of the row, to piece j of either half (the first one's has been read by then)
+          uint32_t hi[8], lo[8];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint4 q = lds_u4(at + (j >> 2) * (kTileBytes / 2) + (((2 * j + i) ^ r) & 7) * 16);
+            split(q.x, hi[4 * i], lo[4 * i]);
+            split(q.y, hi[4 * i + 1], lo[4 * i + 1]);
+            split(q.z, hi[4 * i + 2], lo[4 * i + 2]);
+            split(q.w, hi[4 * i + 3], lo[4 * i + 3]);
+          }
+          sts_u4(at + (((j ^ r) & 7) << 4), make_uint4(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16, hi[4] | hi[5] << 16, hi[6] | hi[7] << 16));
+          low[j] = make_uint4(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16, lo[4] | lo[5] << 16, lo[6] | lo[7] << 16);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sts_u4(at + kTileBytes / 2 + (((j ^ r) & 7) << 4), low[j]);
+        async_proxy_fence();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.q_ready[n & 1]);
+      }
+#pragma unroll 1
+      for (int i = 0; i < n_steps; ++i, ++g) {
+        const uint32_t b = g & 1;
+        if (!wait(&sh.v_full[b], (g >> 1) & 1)) break;
+        const uint32_t from = smem_u32(smem + L::kOffCodes + b * kCodeBytes) + r * 128;
+        const uint32_t to = smem_u32(smem + L::kOffV + b * kTileBytes) + r * 128;
+        const float scale = sh.v_scale[b][r];
+        // a code's bits at their places in bf16 stand for 2^-120 of its value
+        const bool large = scale > 128.f;  // (2^120 times it is no bf16 number)
+        const uint32_t f = __float_as_uint(large ? 0x1p120f : scale * 0x1p120f) >> 16, f2 = f | f << 16;
+        const uint32_t rest = __float_as_uint(large ? scale : 1.f) >> 16, rest2 = rest | rest << 16;
+        const bool any_large = __any_sync(0xffffffffu, large);
+        if (g >= 2 && !wait(&sh.pv_done[b], ((g - 2) >> 1) & 1)) break;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {  // 16 dims, in fours: dims 0, 2, 1, 3 (the output puts them right)
+          const uint4 w = lds_u4(from + (((j ^ r) & 7) << 4));
+          const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+          uint32_t o[8];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            o[2 * k] = mul_bf16x2(((ws[k] << 4) & 0x07f007f0u) | ((ws[k] << 8) & 0x80008000u), f2);
+            o[2 * k + 1] = mul_bf16x2(((ws[k] >> 4) & 0x07f007f0u) | (ws[k] & 0x80008000u), f2);
+          }
+          if (any_large)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) o[k] = mul_bf16x2(o[k], rest2);
+          const uint32_t half = to + (j >> 2) * (kTileBytes / 2);
+          sts_u4(half + ((((j & 3) * 2) ^ (r & 7)) << 4), make_uint4(o[0], o[1], o[2], o[3]));
+          sts_u4(half + ((((j & 3) * 2 + 1) ^ (r & 7)) << 4), make_uint4(o[4], o[5], o[6], o[7]));
+        }
+        async_proxy_fence();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(&sh.v_ready[b]);
+          mbar_arrive(&sh.codes_free[b]);
+        }
+      }
+    }
+  } else {
+    // ===== softmax / correction / output: thread = one row
+    setmaxnreg_inc<L::kRegsSoftmax>();
+    const uint32_t w = warp >> 2, quarter = warp & 3;
+    const int row = quarter * 32 + lane;
+    const uint32_t o_addr = tmem + (quarter << 21), s_addr = o_addr + 128, p_addr = o_addr + 384;
+    float c = p.scale_log2;
+    auto arrive = [&](uint64_t *bar) {  // this warp's tensor-memory accesses so far are ordered before it
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar);
+    };
+    uint32_t g0 = 0, nt = 0;  // key steps before the present part, parts before it
+    int n_steps = 0, h = 0;   // of the present part; this warpgroup's next step of it
+    bool leads = w == 0;
+    uint32_t pending = 0;     // the part before is this warpgroup's to write: 1 behind its first step of the next one, 2 before
+    bool live = true;
+    float m_ref = kNoReference, l_run = 0.f;
+    enum { kNothing, kNotThere, kMask, kRescale } why = kNothing;  // why the loop over the steps was left
+    bool masked = false;
+    float alpha = 1.f;
+    auto advance = [&]() -> bool {  // steps 0, 3, 5, 7 .. and 1, 2, 4, 6 ..; true if the output of the part before comes first
+      const bool first = h < 2;
+      h += first ? 3 - 2 * h : 2;
+      return first && pending != 0;
+    };
+    // Hidden keys of step g get a score of -inf; rows that see a key or value that is not finite are marked.
+    auto mask_keys = [&](uint32_t g, uint32_t e) {
+      const uint32_t s_at = s_addr + (g & 1) * 128;
+      const Part &x = sh.written[nt & 1][warp];
+      const int k0 = (int)(e & 0x7fffffffu) * kKeyStep;
+      const Visible v = visible(ix, x.t.p0 + row / p.G, x.t.len);
+      const int end = v.end - k0, low = v.low - k0, sink = ix.sink - k0;
+      tc_fence_after();
+#pragma unroll 1
+      for (int col = 0; col < 128; col += 16) {
+        uint32_t y[16];
+        tmem_ld16(s_at + col, y);
+        tmem_wait_ld();
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (col + i >= end || (col + i < low && col + i >= sink)) y[i] = 0xff800000u;
+        tmem_st16(s_at + col, y);
+      }
+      tmem_wait_st();
+      if (!E4m3) wait(&sh.v_ready[g & 1], (g >> 1) & 1);
+#pragma unroll 1
+      for (int j = 0; j < 4; ++j)
+#pragma unroll 1
+        for (uint32_t todo = sh.bad[g & 3][j]; todo; todo &= todo - 1) {
+          const int k = E4m3 ? (__ffs(todo) - 1) * 4 + j : j * 32 + __ffs(todo) - 1;
+          if (k < end && (k >= low || k < sink)) l_run = __uint_as_float(0x7fc00000u);
+        }
+    };
+    auto end_part = [&]() {
+      if (n_steps == 0) return;
+      const int last = n_steps - 1;
+      const bool mine = leads == (last == 0 || (last > 2 && (last & 1)));  // had the last step
+      leads = !mine;
+      const bool at_once = n_steps == 1;
+      if (mine == at_once) {
+        pending = at_once ? 2 : 1;
+        if (at_once) sh.l[nt & 3][w ^ 1][row] = make_float2(0.f, kNoReference);  // (the other one had no step)
+      }
+      g0 += n_steps;
+      ++nt;
+    };
+    int n_part = 0;
+    uint32_t n_stored = 0;  // parts that this warpgroup has left in the workspace
+    auto next = [&]() {
+      const Part *x = part_at(n_part);
+      live = x != nullptr && x->b >= 0;
+      if (!live) return;
+      if (lane < 16) reinterpret_cast<int *>(&sh.written[nt & 1][warp])[lane] = reinterpret_cast<const int *>(x)[lane];
+      n_steps = x->b - x->a;
+      done_with_part(n_part);  // (a warp barrier: all lanes see the copy)
+      ++n_part;
+      h = leads ? 0 : 1;
+      m_ref = kNoReference;
+      l_run = 0.f;
+    };
+    for (;;) {
+      if (pending != 2)
+#pragma unroll 1
+      while (h < n_steps) {
+        const uint32_t g = g0 + h, b = g & 1, s_at = s_addr + b * 128, p_at = p_addr + b * 64;
+        const bool m_there = mbar_try_wait(&sh.m_ready[b ^ 1][quarter], ((g - 1) >> 1) & 1, kShortWait) || g == 0;
+        const bool there = mbar_try_wait(&sh.s_full[b], (g >> 1) & 1, kShortWait) && m_there;
+        if (__builtin_expect(!__all_sync(0xffffffffu, there), 0)) {
+          why = kNotThere;
+          break;
+        }
+        const uint32_t e = sh.entry[g & 3];
+        tc_fence_after();
+        if (E4m3) c = sh.q_scale[nt & 1][row];
+        const float m_prev = h > 0 ? sh.m[b ^ 1][row] : kNoReference;
+        uint64_t sums[2] = {0ull, 0ull};
+        bool moved = false;
+        auto new_reference = [&](float x_max) -> bool {
+          const bool grow = x_max > m_ref + kMaxGrowth;
+          const float m_new = grow ? x_max + kHeadroom : m_ref;
+          sh.m[b][row] = m_new;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sh.m_ready[b][quarter]);
+          if (__builtin_expect(!__any_sync(0xffffffffu, grow), 1)) return false;
+          moved = true;
+          alpha = ex2(m_ref - m_new);
+          l_run *= alpha;
+          m_ref = m_new;
+          return true;
+        };
+        if (__builtin_expect((e >> 31) && !masked, 0)) {
+          why = kMask;
+          break;
+        }
+        uint32_t s[128], pk[32];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) tmem_ld32(s_at + q * 32, *reinterpret_cast<uint32_t(*)[32]>(&s[q * 32]));
+        l_run *= ex2(m_ref - m_prev);
+        m_ref = m_prev;
+        tmem_wait_ld();
+        arrive(&sh.s_free[b]);
+        if (E4m3) {
+#pragma unroll
+          for (int i = 0; i < 128; i += 4) {
+            const float4 f = *reinterpret_cast<const float4 *>(&sh.k_scale[g & 7][i]);
+            float a0, a1;
+            unpack_f32x2(mul_f32x2(pack_f32x2(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), pack_f32x2(f.x, f.y)), a0, a1);
+            s[i] = __float_as_uint(a0), s[i + 1] = __float_as_uint(a1);
+            unpack_f32x2(mul_f32x2(pack_f32x2(__uint_as_float(s[i + 2]), __uint_as_float(s[i + 3])), pack_f32x2(f.z, f.w)), a0, a1);
+            s[i + 2] = __float_as_uint(a0), s[i + 3] = __float_as_uint(a1);
+          }
+        }
+        const uint64_t c2 = pack_f32x2(c, c);
+        uint64_t neg_m2;
+        bool again = false;
+#pragma unroll 1
+        do {
+          neg_m2 = pack_f32x2(-m_ref, -m_ref);
+          sums[0] = sums[1] = 0ull;
+          exp32(&s[0], c2, neg_m2, &pk[0], sums);
+          const float x_max = fmaxf(max64(&s[0]), max64(&s[64])) * c;
+          again = !again && new_reference(x_max);
+        } while (__builtin_expect(again, 0));
+        const bool p_done = g < 2 || mbar_test_wait(&sh.pv_done[b], ((g - 2) >> 1) & 1);
+        exp32(&s[32], c2, neg_m2, &pk[16], sums);
+        if (__builtin_expect(!__all_sync(0xffffffffu, p_done), 0)) wait(&sh.pv_done[b], ((g - 2) >> 1) & 1);
+        tc_fence_after();
+        tmem_st32(p_at, pk);
+        exp32(&s[64], c2, neg_m2, &pk[0], sums);
+        exp32(&s[96], c2, neg_m2, &pk[16], sums);
+        tmem_st32(p_at + 32, pk);
+        float s0, s1, s2, s3;
+        unpack_f32x2(sums[0], s0, s1);
+        unpack_f32x2(sums[1], s2, s3);
+        l_run += (s0 + s1) + (s2 + s3);
+        if (h >= n_steps - 3) sh.l[nt & 3][w][row] = make_float2(l_run, m_ref);
+        if (!ok) break;
+        if (__builtin_expect(moved && h > 0, 0)) {
+          why = kRescale;
+          break;
+        }
+        tmem_wait_st();
+        arrive(&sh.p_full[b]);
+        masked = false;
+        if (__builtin_expect(advance(), 0)) break;
+      }
+      if (why != kNothing && ok) {
+        const uint32_t g = g0 + h, b = g & 1;
+        if (why == kNotThere) {
+          if (g > 0) wait(&sh.m_ready[b ^ 1][quarter], ((g - 1) >> 1) & 1);
+          wait(&sh.s_full[b], (g >> 1) & 1);
+        } else if (why == kMask) {
+          mask_keys(g, sh.entry[g & 3]);
+          masked = true;
+        } else {
+          // O changes scale: the products of the steps before have to be complete
+          if (wait(&sh.pv_done[b ^ 1], ((g - 1) >> 1) & 1)) {
+            tc_fence_after();
+            const uint64_t alpha2 = pack_f32x2(alpha, alpha);
+#pragma unroll 1
+            for (int ch = 0; ch < 8; ++ch) {
+              uint32_t v[16];
+              tmem_ld16(o_addr + ch * 16, v);
+              tmem_wait_ld();
+#pragma unroll
+              for (int i = 0; i < 16; i += 2) {
+                float lo, hi;
+                unpack_f32x2(mul_f32x2(pack_f32x2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), alpha2), lo, hi);
+                v[i] = __float_as_uint(lo);
+                v[i + 1] = __float_as_uint(hi);
+              }
+              tmem_st16(o_addr + ch * 16, v);
+            }
+            tmem_wait_st();
+            arrive(&sh.p_full[b]);
+            masked = false;
+            advance();
+          }
+        }
+        const bool whole_step = why == kRescale;
+        why = kNothing;
+        if (ok && !whole_step) continue;
+      }
+      if (!ok) break;
+      if (pending) {
+        // ===== the output of the part before
+        const uint32_t w_last = pending == 2 ? w : w ^ 1;
+        pending = 0;
+        const uint32_t q_buf = (nt - 1) & 1;
+        const Part &to = sh.written[q_buf][warp];
+        if (!wait(&sh.o_full[q_buf], ((nt - 1) >> 1) & 1)) break;
+        tc_fence_after();
+        const float2 last = sh.l[(nt - 1) & 3][w_last][row], other = sh.l[(nt - 1) & 3][w_last ^ 1][row];
+        float l = last.x + other.x * ex2(other.y - last.y), m = last.y;
+        const int n_rows = to.t.tokens * p.G;
+        const bool whole = to.a == 0 && to.b == to.t.steps;
+        const uint32_t out = smem_u32(smem + L::kOffQ + q_buf * kTileBytes + quarter * (kTileBytes / 4));  // the place of its Q: 32 rows a warp
+        const int slot = 2 * blockIdx.x + (to.a == 0 ? 1 : 0);
+        // 64 dims of the row as bf16, O / l, into shared memory
+        auto stage = [&](const uint32_t (&v)[64], int half, float inv) {
+          const uint64_t inv2 = pack_f32x2(inv, inv);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            uint32_t x[4];
+#pragma unroll
+            for (int k = 0; k < 4; k += 2) {
+              float a0, a1, a2, a3;
+              unpack_f32x2(mul_f32x2(pack_f32x2(__uint_as_float(v[i * 8 + 2 * k]), __uint_as_float(v[i * 8 + 2 * k + 1])), inv2), a0, a1);
+              unpack_f32x2(mul_f32x2(pack_f32x2(__uint_as_float(v[i * 8 + 2 * k + 2]), __uint_as_float(v[i * 8 + 2 * k + 3])), inv2), a2, a3);
+              x[k] = E4m3 ? pack_bf16x2(a0, a2) : pack_bf16x2(a0, a1);  // (converted values: dims 0, 2, 1, 3 of four)
+              x[k + 1] = E4m3 ? pack_bf16x2(a1, a3) : pack_bf16x2(a2, a3);
+            }
+            sts_u4(out + half * (kTileBytes / 8) + lane * 128 + ((i ^ (lane & 7)) << 4), make_uint4(x[0], x[1], x[2], x[3]));
+          }
+        };
+        float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+          uint32_t v[64];
+          tmem_ld32(o_addr + half * 64, *reinterpret_cast<uint32_t(*)[32]>(&v[0]));
+          tmem_ld32(o_addr + half * 64 + 32, *reinterpret_cast<uint32_t(*)[32]>(&v[32]));
+          tmem_wait_ld();
+          if (half == 1) arrive(&sh.o_free);
+          if (whole) {
+            stage(v, half, inv);
+          } else if (row < n_rows) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              __stcg(&p.parts[((size_t)slot * 32 + half * 16 + i) * 128 + row],
+                     make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3])));
+          }
+        }
+        bool write = whole;
+        if (!whole) {
+          if (row < n_rows) __stcg(&p.part_l[slot * 128 + row], make_float2(l, m));
+          __threadfence();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sh.stored[w]);
+          if (quarter == 0) {
+            if (!wait(&sh.stored[w], n_stored & 1)) break;
+            if (lane == 0) {
+              sh.last[w] = atomicAdd(&p.arrivals[to.c0], 1) == to.parts - 1;
+              __threadfence();
+              mbar_arrive(&sh.told[w]);
+            }
+            __syncwarp();
+          }
+          if (!wait(&sh.told[w], n_stored & 1)) break;
+          ++n_stored;
+          write = sh.last[w] != 0;
+          if (write && row < n_rows) {
+            auto place = [&](int i) { return 2 * (to.c0 + i) + (i == 0 ? 1 : 0); };
+            m = kNoReference;
+            l = 0.f;
+#pragma unroll 4
+            for (int i = 0; i < to.parts; ++i) m = fmaxf(m, __ldcg(&p.part_l[place(i) * 128 + row]).y);
+#pragma unroll 4
+            for (int i = 0; i < to.parts; ++i) {
+              const float2 lm = __ldcg(&p.part_l[place(i) * 128 + row]);
+              l = fmaf(lm.x, ex2(lm.y - m), l);
+            }
+            inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll 1
+            for (int half = 0; half < 2; ++half) {
+              uint32_t v[64];
+#pragma unroll
+              for (int i = 0; i < 64; ++i) v[i] = 0u;
+#pragma unroll 1
+              for (int i = 0; i < to.parts; ++i) {
+                const float f = ex2(__ldcg(&p.part_l[place(i) * 128 + row]).y - m);
+                const float4 *src = &p.parts[((size_t)place(i) * 32 + half * 16) * 128 + row];
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                  const float4 y = __ldcg(src + k * 128);
+                  v[4 * k] = __float_as_uint(fmaf(y.x, f, __uint_as_float(v[4 * k])));
+                  v[4 * k + 1] = __float_as_uint(fmaf(y.y, f, __uint_as_float(v[4 * k + 1])));
+                  v[4 * k + 2] = __float_as_uint(fmaf(y.z, f, __uint_as_float(v[4 * k + 2])));
+                  v[4 * k + 3] = __float_as_uint(fmaf(y.w, f, __uint_as_float(v[4 * k + 3])));
+                }
+              }
+              stage(v, half, inv);
+            }
+          }
+        }
+        if (write) {
+          __syncwarp();
+          // two rows at a time, 16 lanes each
+#pragma unroll 1
+          for (int i = 0; i < 16; ++i) {
+            const int mine = i * 2 + (lane >> 4), r = (int)quarter * 32 + mine, piece = lane & 15;
+            const uint4 v = lds_u4(out + (piece >> 3) * (kTileBytes / 8) + mine * 128 + (((piece ^ mine) & 7) << 4));
+            if (r < n_rows)
+              *reinterpret_cast<uint4 *>(p.O + (long long)(to.t.row + r / p.G) * p.qt + (long long)(to.h * p.G + r % p.G) * p.qh + piece * 8) = v;
+          }
+          if (p.lse != nullptr && row < n_rows)
+            p.lse[(long long)(to.t.row + row / p.G) * p.Hq + to.h * p.G + row % p.G] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+        }
+        async_proxy_fence();  // (copies come to the place of Q)
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.out_done[q_buf]);
+      }
+      if (h < n_steps) continue;
+      if (!live) break;
+      end_part();
+      next();
+    }
+  }
+
+  // ------------------------------------------------------------------ tear-down
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kWarpQK) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+  if (tid == 0 && sh.abort) atomicExch(ix.status, HEART_ERR_DEVICE_CHECK);
+}
+
+// Q as (64 dims, query head of its key head, token, dim half, key head): a box is the tokens of a tile with their G heads.
+bool make_query_map(CUtensorMap *m, const void *Q, const CacheGeom &g) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (!fn) return false;
+  cuuint64_t dims[5] = {64, (cuuint64_t)g.G, (cuuint64_t)g.T, 2, (cuuint64_t)g.Hkv};
+  cuuint64_t strides[4] = {(cuuint64_t)g.qh * 2, (cuuint64_t)g.qt * 2, 128, (cuuint64_t)g.qh * g.G * 2};
+  cuuint32_t box[5] = {64, (cuuint32_t)g.G, (cuuint32_t)(128 / g.G), 1, 1};
+  cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void *>(Q), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <bool E4m3>
+cudaError_t launch(const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap &mv, const TileParams &p, cudaStream_t s) {
+  cudaError_t e = allow_shared_memory(cache_tile_kernel<E4m3>, kSmem<E4m3>);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(cache_tile_kernel<E4m3>, dim3(kCacheCtas), dim3(Layout<E4m3>::kThreads), kSmem<E4m3>, s, mq, mk, mv, p);
+}
+
+}  // namespace
+
+cudaError_t launch_cache_tiles(const CacheGeom &g, const CacheIndex &ix, const CacheWorkspace &w, const void *Q, const heart_cache &c,
+                               void *O, float *lse, cudaStream_t s, int *launches) {
+  CUtensorMap mq, mk, mv;
+  const int halves = g.page == 128 ? 2 : 1;
+  if (!make_query_map(&mq, Q, g) || !make_pool_map(&mk, c.k, g, g.page, halves) || !make_pool_map(&mv, c.v, g, g.page, halves)) return cudaErrorInvalidValue;
+  TileParams p = {};
+  p.ix = ix;
+  p.tiles = reinterpret_cast<const Tile *>(w.tiles);
+  p.first = w.tile_first;
+  p.head = w.tile_head;
+  p.arrivals = w.arrivals + kCacheCtas;
+  p.parts = reinterpret_cast<float4 *>(w.parts);
+  p.part_l = w.part_l;
+  p.O = static_cast<uint16_t *>(O);
+  p.lse = lse;
+  p.k_scale = c.k_scale;
+  p.v_scale = c.v_scale;
+  p.qt = g.qt;
+  p.qh = g.qh;
+  p.Hq = g.Hq;
+  p.Hkv = g.Hkv;
+  p.G = g.G;
+  p.scale_log2 = (float)(g.scale * 1.4426950408889634);
+  cudaError_t e = launch_pdl(cache_plan_kernel, dim3(1), dim3(1024), 0, s, ix, 128 / g.G, reinterpret_cast<Tile *>(w.tiles), w.tile_first, w.tile_head,
+                             p.arrivals, (int)cache_max_tiles(g));
+  if (e != cudaSuccess) return e;
+  ++*launches;
+  e = g.e4m3 ? launch<true>(mq, mk, mv, p, s) : launch<false>(mq, mk, mv, p, s);
+  if (e == cudaSuccess) ++*launches;
+  return e;
+}
+
+}  // namespace heart

@@ -484,7 +484,9 @@ int heart_cache_attn(const heart_cache_config *cfg, const void *Q, const heart_c
   if (rc != HEART_OK) return rc;
   if (!Q || !O || !aligned16(Q) || !aligned16(O) || (reinterpret_cast<uintptr_t>(lse) & 3u)) return HEART_ERR_INVALID;
   g_launches = 0;
-  cudaError_t e = launch_cache_rows(g, ix, w, Q, *cache, O, lse, static_cast<cudaStream_t>(stream), &g_launches);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  cudaError_t e = (long long)g.max_new * g.G <= kRowsOfRowsKernel ? launch_cache_rows(g, ix, w, Q, *cache, O, lse, s, &g_launches)
+                                                                  : launch_cache_tiles(g, ix, w, Q, *cache, O, lse, s, &g_launches);
   if (e != cudaSuccess) return cuda_fail(e, "cache_attention");
   return HEART_OK;
 }

@@ -156,6 +156,19 @@ def test_attention(heart, name, kind, layout):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("name", ATTENTION)
+def test_attention_by_tiles(heart, name, kind):
+    """The kernel for many rows, which a call takes that does not say how few there are, and the same bits every time."""
+    c = Case(**{**ATTENTION[name], "pad": 140}, kind=kind, seed=len(name) + 1)
+    d = Device(heart, c, max_new=0)
+    O, lse = d.attention()
+    assert heart.heart_get_status(d.ws) == 0
+    check_attention(c, O, lse)
+    P, l2 = d.attention()
+    assert same(O, P) and same(lse, l2)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
 def test_strided_rows(heart, kind):
     """Q and O inside larger tensors, as a fused projection leaves them."""
     c = Case([200, 90], [40, 3], Hq=4, Hkv=2, kind=kind, causal=1)
