@@ -80,6 +80,26 @@ bool make_pool_map(CUtensorMap *m, const void *base, const CacheGeom &g, int row
 __device__ __forceinline__ float cache_scale(uint32_t byte) {
   return __uint_as_float(byte == 255u ? 0x7fc00000u : byte == 0u ? 0x00400000u : byte << 23);
 }
+// The scale of a row of codes whose largest bf16 magnitude has the bits `top`, as heart_cache_write has it (from 2^-100 on), NaN where
+// that is not finite; inv: one over it.
+__device__ __forceinline__ float code_scale(uint32_t top, float &inv) {
+  const int e = min(max((int)(top >> 7) - 135 + ((top & 0x7fu) > 0x60u ? 1 : 0), -100), 120);
+  inv = __uint_as_float((uint32_t)(127 - e) << 23);
+  return __uint_as_float(top < 0x7f80u ? (uint32_t)(127 + e) << 23 : 0x7fc00000u);
+}
+// Two bf16 numbers times inv as the sums of two e4m3 codes each: the codes nearest to them, and to what is left.
+__device__ __forceinline__ void split_codes(uint32_t w, float inv, uint32_t &high, uint32_t &low) {
+  const float x0 = __uint_as_float(w << 16) * inv, x1 = __uint_as_float(w & 0xffff0000u) * inv;
+  uint16_t c;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(x1), "f"(x0));
+  high = c;
+  uint32_t y;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y) : "h"(c));
+  float y0, y1;
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, h;\n\t}" : "=f"(y0), "=f"(y1) : "r"(y));
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(x1 - y1), "f"(x0 - y0));
+  low = c;
+}
 // A sequence as its arrays describe it, brought into range (and reported) where they do not hold what they should.
 struct Sequence {
   int row, n, len;  // first row, new tokens, tokens
@@ -95,15 +115,17 @@ __device__ __forceinline__ Sequence sequence(const CacheIndex &ix, int s) {
   }
   return {r0, r1 - r0, len};
 }
-// The page of token j < len of sequence s, or n_pages (reported) where the table holds none.
-__device__ __forceinline__ int page_of(const CacheIndex &ix, int s, int j) {
-  int page = __ldcg(&ix.table[(size_t)s * ix.table_stride + (j >> ix.page_log2)]);
-  if ((unsigned)page >= (unsigned)ix.n_pages) {
-    atomicExch(ix.status, HEART_ERR_DEVICE_CHECK);
-    page = ix.n_pages;
-  }
-  return page;
+// The table's entry for token j < len of sequence s, and the page that it stands for: n_pages (reported) where it is none.  (Apart, so that
+// an entry can be asked for ahead of its use.)
+__device__ __forceinline__ int page_entry(const CacheIndex &ix, int s, int j) {
+  return __ldcg(&ix.table[(size_t)s * ix.table_stride + (j >> ix.page_log2)]);
 }
+__device__ __forceinline__ int checked_page(const CacheIndex &ix, int page) {
+  if ((unsigned)page < (unsigned)ix.n_pages) return page;
+  atomicExch(ix.status, HEART_ERR_DEVICE_CHECK);
+  return ix.n_pages;
+}
+__device__ __forceinline__ int page_of(const CacheIndex &ix, int s, int j) { return checked_page(ix, page_entry(ix, s, j)); }
 // Visible keys of the query at position p of a sequence of `len` tokens: [low, end) and [0, sink).
 struct Visible {
   int low, end;
@@ -119,17 +141,19 @@ __device__ __forceinline__ Visible visible(const CacheIndex &ix, int p, int len)
 }
 // Key steps that the queries at positions p0 .. p1 see some key of: `sinks` steps from token 0 on, then those from step `first` on.
 // (One step without any visible key where there is none, so that the rows are written.)
+template <int Step = kKeyStep>
 struct Span {
   int sinks, first, steps;
   __device__ __forceinline__ int step(int i) const { return i < sinks ? i : first + i - sinks; }
 };
-__device__ __forceinline__ Span span_of(const CacheIndex &ix, int p0, int p1, int len) {
+template <int Step = kKeyStep>
+__device__ __forceinline__ Span<Step> span_of(const CacheIndex &ix, int p0, int p1, int len) {
   const Visible a = visible(ix, max(p0, 0), len), b = visible(ix, p1, len);
   if (p1 < 0 || b.end <= 0) return {0, 0, 1};
-  Span r;
-  r.first = a.low / kKeyStep;
-  r.sinks = min((min(ix.sink, a.low) + kKeyStep - 1) / kKeyStep, r.first);
-  r.steps = r.sinks + (b.end + kKeyStep - 1) / kKeyStep - r.first;
+  Span<Step> r;
+  r.first = a.low / Step;
+  r.sinks = min((min(ix.sink, a.low) + Step - 1) / Step, r.first);
+  r.steps = r.sinks + (b.end + Step - 1) / Step - r.first;
   return r;
 }
 #endif

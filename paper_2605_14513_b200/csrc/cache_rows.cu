@@ -4,7 +4,17 @@
 // Every key and value is read once and used by 16 or 32 rows, so HBM bounds it: the products of 16 rows x 128 keys take 500
 // clocks of the warp-wide matrix instruction an SM, the 64 KB of the keys and values 2800 (bf16; 1400 as e4m3).  So the design is
 // about bytes in flight: one CTA an SM, eight warps, each with a ring of its own of 24 KB that tensor copies fill.  A warp takes 16 of
-// every 128 keys, with the running maximum and sum of its own keys, so nothing but the warp's own barrier is waited for until a tile's end.
+// every 128 keys (32 of 256 where they are e4m3 and the rows 16), with the running maximum and sum of its own keys, so nothing but the warp's own barrier is waited for
+// until a tile's end.
+//
+// With eight warps an SM what comes next are instructions: 900 for 16 keys, converting keys and values from e4m3 to bf16, took 4700 clocks.
+// The conversion to f16 is one instruction for two codes, so e4m3 caches are multiplied in f16, which holds codes exactly:
+//   * a query row, scaled by a power of two to a largest element in [2^14, 2^15), is in f16 what it is in bf16 (but for elements below
+//     2^-32 of the largest, which lose bits);
+//   * weights lie between 0 and 2^14, the largest so far at 2^6 to 2^14: one below 2^-31 of it counts as zero;
+//   * values are code * 2^(e - E), e the token's exponent and E the largest so far: exact down to 2^-15 of the largest scale, and to 2^-33 of the
+//     largest value below.  E moves O as a row's reference does.
+// (The warp-wide products of e4m3 codes themselves are carried out as conversions and f16 products here, 96 for the 64 in the source.)
 //
 // Work: rows of a sequence and key head, packed as (token, query head of the group), in tiles of 16 or 32; a tile's key steps are
 // 128 tokens each.  All steps of all tiles in one line, (sequence, head, tile, step), are cut into equal shares, one a CTA; what a
@@ -21,12 +31,12 @@ using namespace tc;
 namespace {
 
 constexpr int kWarps = 8, kThreads = 32 * kWarps;
-constexpr int kKeys = 16;              // keys a warp takes at a time, kWarps * kKeys = kKeyStep
 constexpr int kRing = 24576;           // bytes a warp
 constexpr int kMaxStages = 6;
 constexpr int kMaxParts = 32;          // of a tile, about: the last CTA reads them all
 constexpr float kNoReference = -3.0e38f;
 constexpr float kMaxGrowth = 8.f;      // log2: the reference of a row moves when a maximum exceeds it by more
+constexpr float kHeadroomE4m3 = 6.f;   // log2 of the largest weight when the reference has moved
 
 struct RowsParams {
   CacheIndex ix;
@@ -44,12 +54,13 @@ struct RowsParams {
 
 struct RowsShared {
   uint64_t full[kWarps][kMaxStages];
-  alignas(16) uint8_t scales[kWarps][kMaxStages][2 * kKeys];  // of the keys and of the values of a stage
+  alignas(16) uint8_t scales[kWarps][kMaxStages][64];  // e4m3: of the keys and of the values of a stage
   float2 l[kWarps][32];   // row sums and references
   long long total[kWarps];
   int longest[kWarps];
   int found;              // sequence of the CTA's first step
-  long long found_at;     // steps before it
+  int found_q[3];
+  long long found_at, found_steps;  // steps before it, and of one of its heads
   int last;
   int abort;
 };
@@ -59,6 +70,32 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], 
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// Two codes as f16, and two fp32 numbers.
+__device__ __forceinline__ uint32_t codes_to_f16x2(uint32_t codes) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\t}" : "=r"(r) : "r"(codes));
+  return r;
+}
+__device__ __forceinline__ uint32_t high_codes_to_f16x2(uint32_t codes) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}" : "=r"(r) : "r"(codes));
+  return r;
+}
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
 }
 __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
@@ -76,22 +113,18 @@ __device__ __forceinline__ void bulk_load(void *dst, const void *src, int bytes,
                "r"(smem_u32(bar))
                : "memory");
 }
-// Four e4m3 codes as two pairs of bf16, (0, 2) and (1, 3): sign, exponent and mantissa are put at their places, the exponent is
-// set right by an exact product.
-__device__ __forceinline__ void e4m3_to_bf16(uint32_t w, uint32_t &even, uint32_t &odd) {
-  constexpr uint32_t kTwo120 = 0x7b807b80u;  // 2^120 twice
-  const uint32_t e = ((w << 4) & 0x07f007f0u) | ((w << 8) & 0x80008000u), o = ((w >> 4) & 0x07f007f0u) | (w & 0x80008000u);
-  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(even) : "r"(e), "r"(kTwo120));
-  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(odd) : "r"(o), "r"(kTwo120));
-}
 __device__ __forceinline__ bool not_finite(uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
+
+// Keys that a warp takes at a time (32 of them leave a lane too few registers for 32 rows, and for keys of 256 bytes the ring too few stages).
+__host__ __device__ constexpr int keys_of(int MT, bool e4m3) { return e4m3 && MT == 1 ? 32 : 16; }
 
 template <int MT, bool E4m3>
 __global__ void __launch_bounds__(kThreads, 1)
     cache_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const RowsParams p) {
   constexpr int kRows = 16 * MT;
-  constexpr int kHalf = E4m3 ? 2048 : 4096;  // bytes of 16 keys, or values
-  constexpr int kStage = 2 * kHalf, kStages = kRing / kStage;
+  constexpr int kKeys = keys_of(MT, E4m3), kStep = kWarps * kKeys, kTiles = kKeys / 8;  // keys a warp takes at a time, a step, products of 8 keys
+  constexpr int kKeysLog2 = kKeys == 32 ? 5 : 4;
+  constexpr int kHalf = kKeys * kD * (E4m3 ? 1 : 2), kStage = 2 * kHalf, kStages = kRing / kStage;  // bytes of a warp's keys, or values
   static_assert(kStages <= kMaxStages, "barriers");
   extern __shared__ __align__(1024) unsigned char smem[];
   RowsShared &sh = *reinterpret_cast<RowsShared *>(smem + kWarps * kRing);
@@ -100,10 +133,11 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t ring_at = smem_u32(ring);
   const CacheIndex &ix = p.ix;
 
-  if (lane == 0)
+  if (lane == 0) {
     for (int i = 0; i < kStages; ++i) mbar_init(&sh.full[warp][i], 1);
+    mbar_fence_init();
+  }
   if (tid == 0) sh.abort = 0;
-  if (lane == 0) mbar_fence_init();
   pdl_wait();
   pdl_launch_dependents();
 
@@ -111,10 +145,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   auto tiles_of = [&](const Sequence &q) { return (int)(((long long)q.n * p.G + kRows - 1) / kRows); };
   auto span = [&](const Sequence &q, int t) {
     const int first = t * kRows, last = min((int)((long long)q.n * p.G), first + kRows) - 1;
-    return span_of(ix, q.len - q.n + first / p.G, q.len - q.n + last / p.G, q.len);
+    return span_of<kStep>(ix, q.len - q.n + first / p.G, q.len - q.n + last / p.G, q.len);
   };
-  auto steps_of = [&](int s, int &longest) -> long long {  // of one head
-    const Sequence q = sequence(ix, s);
+  auto steps_of = [&](const Sequence &q, int &longest) -> long long {  // of one head
     long long n = 0;
     for (int t = 0; t < tiles_of(q); ++t) {
       const int k = span(q, t).steps;
@@ -124,11 +157,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     return n;
   };
   long long total = 0, mine = 0;
+  Sequence q = {0, 0, 0};
   int longest = 1;
   for (int s = tid; s < ix.S; s += kThreads) {
-    const long long n = steps_of(s, longest) * p.Hkv;
-    if (s < kThreads) mine = n;
-    total += n;
+    const Sequence x = sequence(ix, s);
+    const long long n = steps_of(x, longest);
+    if (s < kThreads) mine = n, q = x;
+    total += n * p.Hkv;
   }
 #pragma unroll
   for (int o = 16; o; o >>= 1) {
@@ -152,8 +187,11 @@ __global__ void __launch_bounds__(kThreads, 1)
   long long before = 0;  // steps before the sequences of this round
   for (int base = 0; base < ix.S; base += kThreads) {
     int dummy = 0;
-    if (base > 0) mine = base + tid < ix.S ? steps_of(base + tid, dummy) * p.Hkv : 0;
-    long long upto = mine;
+    if (base > 0) {
+      q = base + tid < ix.S ? sequence(ix, base + tid) : Sequence{0, 0, 0};
+      mine = steps_of(q, dummy);
+    }
+    long long upto = mine * p.Hkv;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const long long x = __shfl_up_sync(0xffffffffu, upto, o);
@@ -168,65 +206,78 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (i < warp) at += sh.total[i];
       all += sh.total[i];
     }
-    at += upto - mine;
-    if (at <= u0 && u0 < at + mine) {
+    at += upto - mine * p.Hkv;
+    if (at <= u0 && u0 < at + mine * p.Hkv) {
       sh.found = base + tid;
+      sh.found_q[0] = q.row, sh.found_q[1] = q.n, sh.found_q[2] = q.len;
       sh.found_at = at;
+      sh.found_steps = mine;
     }
     before += all;
     if (before > u0) break;
   }
   __syncthreads();
   int s = sh.found, h, t = 0;
-  Sequence q = sequence(ix, s);
+  q = {sh.found_q[0], sh.found_q[1], sh.found_q[2]};
   long long u = u0;
   int done;  // steps of the present tile before this share
   {
-    int dummy = 0;
-    const long long per_head = steps_of(s, dummy);
     long long rest = u0 - sh.found_at;
-    h = (int)(rest / per_head);
-    rest -= h * per_head;
+    h = (int)(rest / sh.found_steps);
+    rest -= h * sh.found_steps;
     for (int k; rest >= (k = span(q, t).steps); ++t) rest -= k;
     done = (int)rest;
   }
 
-  uint32_t issued = 0, taken = 0;  // stages of this warp's ring so far
+  int put = 0, take = 0;            // the stages that come next, to fill and to use
+  uint32_t parity = 0;              // of the barriers of the stages, a bit each, for their next use
   bool ok = true;
   const int g = lane >> 2, c = lane & 3;
+  const int box_log2 = min(ix.page_log2, kKeysLog2), boxes = kKeys >> box_log2;
 
   for (;;) {
     // ---------------------------------------------------------------- a tile, or part of one
-    const Span sp = span(q, t);
+    const Span<kStep> sp = span(q, t);
     const int first_row = t * kRows, n_rows = min(kRows, (int)((long long)q.n * p.G) - first_row);
     const int p0 = q.len - q.n + first_row / p.G, p1 = q.len - q.n + (first_row + n_rows - 1) / p.G;
     const int end_step = (int)min((long long)sp.steps, done + (u1 - u));
-    const Visible va = visible(ix, p0, q.len), vb = visible(ix, p1, q.len);
-    auto some = [&](int k0) { return p1 >= 0 && k0 < vb.end && (k0 + kKeys > visible(ix, max(p0, 0), q.len).low || k0 < ix.sink); };
-    auto every = [&](int k0) { return p0 >= 0 && k0 + kKeys <= va.end && (k0 >= vb.low || k0 + kKeys <= ix.sink); };
+    // keys that some row sees: some_low .. some_end - 1 and the sinks; that every row does: every_low .. every_end - 1 and the sinks
+    int some_low, some_end, every_low, every_end;
+    {
+      const Visible a = visible(ix, max(p0, 0), q.len), b = visible(ix, p1, q.len);
+      some_low = a.low, some_end = b.end;
+      every_low = b.low, every_end = p0 < 0 ? 0 : a.end;
+    }
+    auto some = [&](int k0) { return k0 < some_end && (k0 + kKeys > some_low || k0 < ix.sink); };
 
-    int next = done - 1, next_page = 0;  // the step of the warp's next copy, and the page of its keys
-    auto key_of = [&](int i) { return sp.step(i) * kKeyStep + warp * kKeys; };
+    auto key_of = [&](int i) { return (i < sp.sinks ? i : sp.first + i - sp.sinks) * kStep + warp * kKeys; };
+    int next = done - 1, next_key = 0, next_page = 0;  // the warp's next copy: its step and keys, lane i: the table's entry for its box i
+    int in_flight = 0;
     auto advance = [&]() {
-      do ++next;
-      while (next < end_step && !some(key_of(next)));
-      if (next < end_step) next_page = page_of(ix, s, key_of(next));
+      do next_key = key_of(++next);
+      while (next < end_step && !some(next_key));
+      const int k = next_key + (lane << box_log2);
+      if (next < end_step && lane < boxes) next_page = k < q.len ? page_entry(ix, s, k) : -1;
     };
     auto issue = [&]() {
       if (next >= end_step) return;
-      const int st = issued % kStages, slot = key_of(next) & ((1 << ix.page_log2) - 1);
-      if (lane == 0) {
-        uint64_t *bar = &sh.full[warp][st];
-        mbar_expect_tx(bar, kStage + (E4m3 ? 2 * kKeys : 0));
-        tma_load_5d(ring + st * kStage, &map_k, bar, 0, slot, 0, h, next_page);
-        tma_load_5d(ring + st * kStage + kHalf, &map_v, bar, 0, slot, 0, h, next_page);
+      uint64_t *bar = &sh.full[warp][put];
+      if (lane == 0) mbar_expect_tx(bar, kStage + (E4m3 ? 2 * kKeys : 0));
+      if (boxes > 1) __syncwarp();
+      if (lane < boxes) {
+        const int slot = next_key & ((1 << ix.page_log2) - 1);
+        const int page = next_key + (lane << box_log2) < q.len ? checked_page(ix, next_page) : ix.n_pages;  // (out of range: zeros)
+        unsigned char *to = ring + put * kStage + (lane << (box_log2 + (E4m3 ? 7 : 8)));
+        tma_load_5d(to, &map_k, bar, 0, slot, 0, h, page);
+        tma_load_5d(to + kHalf, &map_v, bar, 0, slot, 0, h, page);
         if (E4m3) {
-          const size_t at = (((size_t)min(next_page, ix.n_pages - 1) * p.Hkv + h) << ix.page_log2) + slot;
-          bulk_load(&sh.scales[warp][st][0], p.k_scale + at, kKeys, bar);
-          bulk_load(&sh.scales[warp][st][kKeys], p.v_scale + at, kKeys, bar);
+          const size_t at = (((size_t)min(page, ix.n_pages - 1) * p.Hkv + h) << ix.page_log2) + slot;
+          bulk_load(&sh.scales[warp][put][lane << box_log2], p.k_scale + at, 1 << box_log2, bar);
+          bulk_load(&sh.scales[warp][put][kKeys + (lane << box_log2)], p.v_scale + at, 1 << box_log2, bar);
         }
       }
-      ++issued;
+      put = put + 1 == kStages ? 0 : put + 1;
+      ++in_flight;
       advance();
     };
     advance();
@@ -234,8 +285,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int i = 0; i < kStages; ++i) issue();
 
     // The rows' queries as operands of the products: this lane's rows g and g + 8 of every 16.  (e4m3: the dims of a product are
-    // those that a lane finds together in a key's row, 32 * c + 4 * ks + (0, 2) and (1, 3).)
+    // those that a lane finds together in a key's row, 32 * c + 4 * step + 0 .. 3.)
     uint32_t qf[MT][8][4];
+    float row_scale[MT][2];
     Visible vis[MT][2];
 #pragma unroll
     for (int m = 0; m < MT; ++m)
@@ -246,25 +298,40 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int i = (first_row + row) / p.G, head = h * p.G + (first_row + row) % p.G;
         const uint16_t *src = p.Q + (long long)(q.row + i) * p.qt + head * p.qh;
         vis[m][r] = real ? visible(ix, q.len - q.n + i, q.len) : Visible{0, 0x7fffffff};
+        row_scale[m][r] = p.scale_log2;
+        if (E4m3) {
+          uint4 x[4];
+          uint32_t top = 0u;
 #pragma unroll
-        for (int ks = 0; ks < 8; ++ks) {
-          uint32_t lo = 0u, hi = 0u;
-          if (real) {
-            if (E4m3) {
-              const uint2 x = *reinterpret_cast<const uint2 *>(src + c * 32 + ks * 4);
-              lo = __byte_perm(x.x, x.y, 0x5410);
-              hi = __byte_perm(x.x, x.y, 0x7632);
-            } else {
-              lo = *reinterpret_cast<const uint32_t *>(src + ks * 16 + c * 2);
-              hi = *reinterpret_cast<const uint32_t *>(src + ks * 16 + c * 2 + 8);
-            }
+          for (int k = 0; k < 4; ++k) {
+            x[k] = real ? *reinterpret_cast<const uint4 *>(src + c * 32 + k * 8) : make_uint4(0u, 0u, 0u, 0u);
+            top = __vmaxu2(top, __vmaxu2(__vmaxu2(x[k].x & 0x7fff7fffu, x[k].y & 0x7fff7fffu), __vmaxu2(x[k].z & 0x7fff7fffu, x[k].w & 0x7fff7fffu)));
           }
-          qf[m][ks][r] = lo;
-          qf[m][ks][2 + r] = hi;
+          top = max(top & 0xffffu, top >> 16);
+          top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+          top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+          const int e = min(max((int)(top >> 7) - 127 - 14, -100), 120);  // the largest element: 2^14 * 2^e to 2^15 * 2^e
+          const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+          row_scale[m][r] = top < 0x7f80u ? p.scale_log2 * __uint_as_float((uint32_t)(127 + e) << 23) : __uint_as_float(0x7fc00000u);
+          auto to_f16 = [&](uint32_t w) { return pack_f16x2(__uint_as_float(w << 16) * inv, __uint_as_float(w & 0xffff0000u) * inv); };
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            qf[m][2 * k][r] = to_f16(x[k].x);
+            qf[m][2 * k][2 + r] = to_f16(x[k].y);
+            qf[m][2 * k + 1][r] = to_f16(x[k].z);
+            qf[m][2 * k + 1][2 + r] = to_f16(x[k].w);
+          }
+        } else {
+#pragma unroll
+          for (int ks = 0; ks < 8; ++ks) {
+            qf[m][ks][r] = real ? *reinterpret_cast<const uint32_t *>(src + ks * 16 + c * 2) : 0u;
+            qf[m][ks][2 + r] = real ? *reinterpret_cast<const uint32_t *>(src + ks * 16 + c * 2 + 8) : 0u;
+          }
         }
       }
     float o[MT][16][4] = {};
     float ref[MT][2], sum[MT][2];
+    uint32_t v_exp = 0;  // e4m3: O stands for 2^(v_exp - 127) of its value
 #pragma unroll
     for (int m = 0; m < MT; ++m) ref[m][0] = ref[m][1] = kNoReference, sum[m][0] = sum[m][1] = 0.f;
 
@@ -272,29 +339,59 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int i = done; i < end_step; ++i) {
       const int k0 = key_of(i);
       if (!some(k0)) continue;
-      const int st = taken % kStages;
-      if (!mbar_wait(&sh.full[warp][st], (taken / kStages) & 1, &sh.abort)) ok = false;
+      if (!mbar_wait(&sh.full[warp][take], (parity >> take) & 1, &sh.abort)) ok = false;
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
-      const uint32_t k_at = ring_at + st * kStage, v_at = k_at + kHalf;
-      const bool whole = every(k0);
-      float x[MT][2][4] = {};
+      const uint32_t k_at = ring_at + take * kStage, v_at = k_at + kHalf;
+      const bool whole = k0 + kKeys <= every_end && (k0 >= every_low || k0 + kKeys <= ix.sink);
+      float x[MT][kTiles][4] = {};
+      uint32_t vs[kTiles];  // e4m3: this lane's values are to be multiplied by these, two keys at a time
       // ---- scores
       if (E4m3) {
+        const uint8_t *scales = sh.scales[warp][take];
+        {  // the largest exponent of the values
+          const uint32_t vb = lane < kKeys && k0 + lane < q.len ? scales[kKeys + lane] : 0u;
+          const uint32_t top = __reduce_max_sync(0xffffffffu, vb == 255u ? 0u : vb);
+          if (top > v_exp) {
+            const float f = cache_scale(max((int)(v_exp - top) + 127, 1));
+            v_exp = top;
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+              for (int n = 0; n < 16; ++n)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) o[m][n][k] *= f;
+          }
+        }
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n) {
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             const uint4 w = lds_u4(k_at + (n * 8 + g) * 128 + (((c * 2 + j) ^ g) << 4));
-            const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+            const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              uint32_t b0, b1;
-              e4m3_to_bf16(ww[k], b0, b1);
+              const uint32_t b0 = codes_to_f16x2(ws[k]), b1 = high_codes_to_f16x2(ws[k]);
 #pragma unroll
-              for (int m = 0; m < MT; ++m) mma_bf16(x[m][n], qf[m][j * 4 + k], b0, b1);
+              for (int m = 0; m < MT; ++m) mma_f16(x[m][n], qf[m][j * 4 + k], b0, b1);
             }
           }
+          const uint32_t kb = *reinterpret_cast<const uint16_t *>(&scales[n * 8 + c * 2]);
+          const uint32_t vb = *reinterpret_cast<const uint16_t *>(&scales[kKeys + n * 8 + c * 2]);
+          auto factor = [&](uint32_t b, int key) {  // (behind the sequence's end, or not finite: nothing)
+            return b == 255u || k0 + key >= q.len ? 0.f : cache_scale(max((int)(b - v_exp) + 127, 1));
+          };
+          vs[n] = pack_f16x2(factor(vb & 255u, n * 8 + c * 2), factor(vb >> 8, n * 8 + c * 2 + 1));
+          // a token whose key or value is not finite
+          const float k_lo = cache_scale((vb & 255u) == 255u ? 255u : kb & 255u), k_hi = cache_scale((vb >> 8) == 255u ? 255u : kb >> 8);
+#pragma unroll
+          for (int m = 0; m < MT; ++m) {
+            x[m][n][0] *= k_lo;
+            x[m][n][1] *= k_hi;
+            x[m][n][2] *= k_lo;
+            x[m][n][3] *= k_hi;
+          }
+        }
       } else {
         const int key = ((lane >> 4) << 3) + (lane & 7);
 #pragma unroll
@@ -309,16 +406,17 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
       }
-      float ks4[4], vs4[4];  // the scales of this lane's keys 2c, 2c+1, 2c+8, 2c+9
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int key = (k >> 1) * 8 + c * 2 + (k & 1);
-        ks4[k] = E4m3 ? cache_scale(sh.scales[warp][st][key]) * p.scale_log2 : p.scale_log2;
-        vs4[k] = E4m3 ? cache_scale(sh.scales[warp][st][kKeys + key]) : 1.f;
-      }
       // ---- weights
       auto hidden = [&](const Visible &v, int k) { return k >= v.end || (k < v.low && k >= ix.sink); };
-      uint32_t pf[MT][4];
+      if (!whole) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              if (hidden(vis[m][k >> 1], k0 + n * 8 + c * 2 + (k & 1))) x[m][n][k] = -INFINITY;
+      }
       bool moved = false;
       float alpha[MT][2];
 #pragma unroll
@@ -327,18 +425,15 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int r = 0; r < 2; ++r) {
           float top = -INFINITY;
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            float &y = x[m][k >> 1][r * 2 + (k & 1)];
-            y *= ks4[k];
-            if (!whole && hidden(vis[m][r], k0 + (k >> 1) * 8 + c * 2 + (k & 1))) y = -INFINITY;
-            top = fmaxf(top, y);
-          }
+          for (int n = 0; n < kTiles; ++n) top = fmaxf(top, fmaxf(x[m][n][2 * r], x[m][n][2 * r + 1]));
           top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
           top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+          top *= row_scale[m][r];
           alpha[m][r] = 1.f;
-          if (top > ref[m][r] + kMaxGrowth) {
-            alpha[m][r] = ex2(ref[m][r] - top);
-            ref[m][r] = top;
+          if (top > ref[m][r] + (E4m3 ? kHeadroomE4m3 : 0.f) + kMaxGrowth) {
+            const float to = E4m3 ? top - kHeadroomE4m3 : top;
+            alpha[m][r] = ex2(ref[m][r] - to);
+            ref[m][r] = to;
             moved = true;
           }
         }
@@ -356,21 +451,24 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
       }
+      uint32_t pf[MT][kTiles / 2][4];
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          float w[4];
+        for (int n = 0; n < kTiles; ++n)
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float y = x[m][k >> 1][r * 2 + (k & 1)];
-            w[k] = ex2(y - ref[m][r]);
-            sum[m][r] += w[k];
-            if (E4m3) w[k] = !whole && y == -INFINITY ? 0.f : w[k] * vs4[k];  // (a hidden token's scale may be NaN)
+          for (int r = 0; r < 2; ++r) {
+            float w[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const float y = x[m][n][2 * r + k];
+              w[k] = ex2(fmaf(y, row_scale[m][r], -ref[m][r]));
+              // (what is hidden is nothing, even to a query that is not finite)
+              if (E4m3 && !whole && y == -INFINITY) w[k] = 0.f;
+              sum[m][r] += w[k];
+            }
+            pf[m][n >> 1][(n & 1) * 2 + r] = E4m3 ? pack_f16x2(w[0], w[1]) : pack_bf16x2(w[0], w[1]);
           }
-          pf[m][r] = pack_bf16x2(w[0], w[1]);
-          pf[m][2 + r] = pack_bf16x2(w[2], w[3]);
-        }
       if (!E4m3 && !whole) {
         // Values that are not finite must not reach rows that do not see them (0 * inf is NaN): they are taken out, and rows that
         // do see them are marked.
@@ -384,7 +482,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (bad) {
 #pragma unroll 1
           for (int j = 0; j < 8; ++j)
-            if (bad >> ((j * 4 + (lane >> 3)) & 15) & 1u) *reinterpret_cast<uint4 *>(ring + st * kStage + kHalf + (j * 32 + lane) * 16) = make_uint4(0u, 0u, 0u, 0u);
+            if (bad >> ((j * 4 + (lane >> 3)) & 15) & 1u) *reinterpret_cast<uint4 *>(ring + take * kStage + kHalf + (j * 32 + lane) * 16) = make_uint4(0u, 0u, 0u, 0u);
           async_proxy_fence();
           __syncwarp();
 #pragma unroll 1
@@ -399,50 +497,68 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       // ---- values
-      if (E4m3) {
 #pragma unroll
-        for (int j = 0; j < 8; j += 2) {  // 16 dims each: even ones and odd ones
-          uint32_t b[4];
-          const int key = lane & 15, chunk = j + (lane >> 4);
-          ldmatrix4_trans(b, v_at + key * 128 + (((chunk ^ key) & 7) << 4));
-          uint32_t e0, o0, e1, o1;
+      for (int b16 = 0; b16 < kTiles / 2; ++b16) {  // 16 keys each
+        const int key = lane & 15;
+        if (E4m3) {
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            e4m3_to_bf16(b[2 * k], e0, o0);
-            e4m3_to_bf16(b[2 * k + 1], e1, o1);
+          for (int j = 0; j < 8; j += 2) {  // 16 dims each: even ones and odd ones
+            uint32_t b[4];
+            const int chunk = j + (lane >> 4);
+            ldmatrix4_trans(b, v_at + b16 * 2048 + key * 128 + (((chunk ^ key) & 7) << 4));
 #pragma unroll
-            for (int m = 0; m < MT; ++m) {
-              mma_bf16(o[m][(j + k) * 2], pf[m], e0, e1);
-              mma_bf16(o[m][(j + k) * 2 + 1], pf[m], o0, o1);
+            for (int k = 0; k < 2; ++k) {
+              // codes of two dims of a key and of the next: the even dims of both, the odd ones
+              const uint32_t lo = __byte_perm(b[2 * k], 0, 0x3120), hi = __byte_perm(b[2 * k + 1], 0, 0x3120);
+              const uint32_t e0 = mul_f16x2(codes_to_f16x2(lo), vs[b16 * 2]), o0 = mul_f16x2(high_codes_to_f16x2(lo), vs[b16 * 2]);
+              const uint32_t e1 = mul_f16x2(codes_to_f16x2(hi), vs[b16 * 2 + 1]), o1 = mul_f16x2(high_codes_to_f16x2(hi), vs[b16 * 2 + 1]);
+#pragma unroll
+              for (int m = 0; m < MT; ++m) {
+                mma_f16(o[m][(j + k) * 2], pf[m][b16], e0, e1);
+                mma_f16(o[m][(j + k) * 2 + 1], pf[m][b16], o0, o1);
+              }
             }
           }
-        }
-      } else {
+        } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {  // 16 dims each
-          uint32_t b[4];
-          const int key = lane & 15, chunk = j * 2 + (lane >> 4);
-          ldmatrix4_trans(b, v_at + (chunk >> 3) * 2048 + key * 128 + (((chunk ^ key) & 7) << 4));
+          for (int j = 0; j < 8; ++j) {  // 16 dims each
+            uint32_t b[4];
+            const int chunk = j * 2 + (lane >> 4);
+            ldmatrix4_trans(b, v_at + (chunk >> 3) * 2048 + key * 128 + (((chunk ^ key) & 7) << 4));
 #pragma unroll
-          for (int m = 0; m < MT; ++m) {
-            mma_bf16(o[m][j * 2], pf[m], b[0], b[1]);
-            mma_bf16(o[m][j * 2 + 1], pf[m], b[2], b[3]);
+            for (int m = 0; m < MT; ++m) {
+              mma_bf16(o[m][j * 2], pf[m][b16], b[0], b[1]);
+              mma_bf16(o[m][j * 2 + 1], pf[m][b16], b[2], b[3]);
+            }
           }
         }
       }
       __syncwarp();  // the stage has been read
-      ++taken;
+      parity ^= 1u << take;
+      take = take + 1 == kStages ? 0 : take + 1;
+      --in_flight;
       issue();
     }
     if (!ok) {  // (copies that have not come are waited for once more, so that none lands in memory that is someone else's)
-      for (; taken < issued; ++taken) {
+      for (; in_flight > 0; --in_flight) {
         const long long since = clock64();
-        while (!mbar_try_wait(&sh.full[warp][taken % kStages], (taken / kStages) & 1) && clock64() - since < kWaitLimitCycles) {
+        while (!mbar_try_wait(&sh.full[warp][take], (parity >> take) & 1) && clock64() - since < kWaitLimitCycles) {
         }
+        parity ^= 1u << take;
+        take = take + 1 == kStages ? 0 : take + 1;
       }
       next = end_step;
     }
 
+    if (E4m3) {
+      const float f = cache_scale(v_exp);
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int n = 0; n < 16; ++n)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) o[m][n][k] *= f;
+    }
     // ---------------------------------------------------------------- the warps' sums put together
 #pragma unroll
     for (int m = 0; m < MT; ++m)
@@ -584,8 +700,10 @@ cudaError_t launch(const CacheGeom &g, const RowsParams &p, const CUtensorMap &m
 
 cudaError_t launch_cache_rows(const CacheGeom &g, const CacheIndex &ix, const CacheWorkspace &w, const void *Q, const heart_cache &c,
                               void *O, float *lse, cudaStream_t s, int *launches) {
+  const bool two = (long long)g.max_new * g.G > 16;
+  const int box = g.page < keys_of(two ? 2 : 1, g.e4m3) ? g.page : keys_of(two ? 2 : 1, g.e4m3);
   CUtensorMap mk, mv;
-  if (!make_pool_map(&mk, c.k, g, kKeys, 2) || !make_pool_map(&mv, c.v, g, kKeys, 2)) return cudaErrorInvalidValue;
+  if (!make_pool_map(&mk, c.k, g, box, 2) || !make_pool_map(&mv, c.v, g, box, 2)) return cudaErrorInvalidValue;
   RowsParams p = {};
   p.ix = ix;
   p.Q = static_cast<const uint16_t *>(Q);
@@ -602,7 +720,6 @@ cudaError_t launch_cache_rows(const CacheGeom &g, const CacheIndex &ix, const Ca
   p.arrivals = w.arrivals;
   p.parts = w.parts;
   p.part_l = w.part_l;
-  const bool two = (long long)g.max_new * g.G > 16;
   if (g.e4m3) return two ? launch<2, true>(g, p, mk, mv, s, launches) : launch<1, true>(g, p, mk, mv, s, launches);
   return two ? launch<2, false>(g, p, mk, mv, s, launches) : launch<1, false>(g, p, mk, mv, s, launches);
 }

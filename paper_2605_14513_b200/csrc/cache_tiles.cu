@@ -211,7 +211,7 @@ __global__ void __launch_bounds__(1024) cache_plan_kernel(const CacheIndex ix, i
         x.tokens = min(tokens_per_tile, q.n - k * tokens_per_tile);
         x.p0 = q.len - q.n + k * tokens_per_tile;
         x.len = q.len;
-        const Span sp = span_of(ix, x.p0, x.p0 + x.tokens - 1, q.len);
+        const Span<> sp = span_of(ix, x.p0, x.p0 + x.tokens - 1, q.len);
         x.sinks = sp.sinks;
         x.first = sp.first;
         x.steps = sp.steps;
@@ -342,10 +342,13 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
   };
   const int page_log2 = ix.page_log2, n_boxes = 128 >> page_log2;
   auto key_of = [](const Tile &t, int i) { return (i < t.sinks ? i : t.first + i - t.sinks) * kKeyStep; };
-  // The page that lane i < n_boxes copies of the step at key k0.
-  auto pages_of = [&](const Tile &t, int k0) {
+  // The table's entry for what lane i < n_boxes copies of the step at key k0 (asked for a step ahead), and the page that it stands for.
+  auto entries_of = [&](const Tile &t, int k0) {
     const int k = k0 + (lane << page_log2);
-    return lane < n_boxes && k < t.len ? page_of(ix, t.s, k) : ix.n_pages;  // (a page out of range: zeros)
+    return lane < n_boxes && k < t.len ? page_entry(ix, t.s, k) : 0;
+  };
+  auto pages_of = [&](const Tile &t, int k0, int entry) {
+    return lane < n_boxes && k0 + (lane << page_log2) < t.len ? checked_page(ix, entry) : ix.n_pages;  // (a page out of range: zeros)
   };
   auto load_pages = [&](unsigned char *dst, const CUtensorMap *map, uint64_t *bar, int h, int page) {
     if (lane == 0) mbar_expect_tx(bar, L::kKey);
@@ -407,12 +410,12 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
     };
     int g = 0, n = 0;
     bool q_busy[2] = {false, false};
-    int page = 0, page_next = 0;
-    uint32_t ks = 0, ks_next = 0, vs = 0, vs_next = 0;
+    int page = 0, entry_next = 0;
+    uint32_t ks = 0, vs = 0;
     if (u < u1) {
       const Tile &t = sh.k_tile[0];
       fetch(sh.k_tile[0], tile);
-      page = pages_of(t, key_of(t, a));
+      page = pages_of(t, key_of(t, a), entries_of(t, key_of(t, a)));
       if (E4m3) ks = scales_of(p.k_scale, t, key_of(t, a), h, page), vs = scales_of(p.v_scale, t, key_of(t, a), h, page);
     }
 #pragma unroll 1
@@ -443,11 +446,10 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
 #pragma unroll 1
       for (int i = a; i < b; ++i, ++g) {
         const int k0 = key_of(t, i);
-        if (i + 1 < b) {
-          page_next = pages_of(t, key_of(t, i + 1));
-        } else if (more) {
-          page_next = pages_of(t_next, key_of(t_next, 0));
-        }
+        const bool last = i + 1 == b;
+        const Tile &t_then = last ? t_next : t;  // the step behind this one
+        const int k_then = last && !more ? 0 : key_of(t_then, last ? 0 : i + 1);
+        if (!last || more) entry_next = entries_of(t_then, k_then);
         if (g >= 2 && !wait(&sh.s_full[g & 1], ((g - 2) >> 1) & 1)) break;
         bool masked = masked_at(whole, k0);
         if (E4m3) {
@@ -481,17 +483,13 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
           }
           q_busy[n & 1] = true;
         }
-        if (E4m3) {
-          const bool last = i + 1 == b;
-          if (!last || more) {
-            const int k_next = last ? key_of(t_next, 0) : key_of(t, i + 1);
-            ks_next = scales_of(p.k_scale, last ? t_next : t, k_next, last ? h_next : h, page_next);
-            vs_next = scales_of(p.v_scale, last ? t_next : t, k_next, last ? h_next : h, page_next);
+        if (!last || more) {
+          page = pages_of(t_then, k_then, entry_next);
+          if (E4m3) {
+            ks = scales_of(p.k_scale, t_then, k_then, last ? h_next : h, page);
+            vs = scales_of(p.v_scale, t_then, k_then, last ? h_next : h, page);
           }
         }
-        page = page_next;
-        ks = ks_next;
-        vs = vs_next;
       }
       if (!ok) break;
       u += b - a;
@@ -516,13 +514,14 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
       if (lane < 8) reinterpret_cast<int *>(&sh.v_tile)[lane] = reinterpret_cast<const int *>(&x->t)[lane];
       done_with_part(n);
       const Whole whole = whole_of(t);
-      int page = pages_of(t, key_of(t, a)), page_next = 0;
-      uint32_t vs = 0, vs_next = 0;
+      int page = pages_of(t, key_of(t, a), entries_of(t, key_of(t, a))), entry_next = 0;
+      uint32_t vs = 0;
       if (E4m3) vs = scales_of(p.v_scale, t, key_of(t, a), h, page);
 #pragma unroll 1
       for (int i = a; i < b; ++i, ++g) {
         const int k0 = key_of(t, i), at = g & 1;
-        if (i + 1 < b) page_next = pages_of(t, key_of(t, i + 1));
+        const int k_then = i + 1 < b ? key_of(t, i + 1) : 0;
+        if (i + 1 < b) entry_next = entries_of(t, k_then);
         if (E4m3) {
           if (g >= 2 && !wait(&sh.codes_free[at], ((g - 2) >> 1) & 1)) break;
           float f[4];
@@ -535,7 +534,6 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
           *reinterpret_cast<float4 *>(&sh.v_scale[at][lane * 4]) = make_float4(f[0], f[1], f[2], f[3]);
           __syncwarp();
           load_pages(smem + L::kOffCodes + at * kCodeBytes, &map_v, &sh.v_full[at], h, page);
-          if (i + 1 < b) vs_next = scales_of(p.v_scale, t, key_of(t, i + 1), h, page_next);
         } else {
           if (g >= 2 && !wait(&sh.pv_done[at], ((g - 2) >> 1) & 1)) break;
           load_pages(smem + L::kOffV + at * kTileBytes, &map_v, &sh.v_full[at], h, page);
@@ -571,8 +569,10 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
           __syncwarp();
           if (lane == 0) mbar_arrive(&sh.v_ready[at]);
         }
-        page = page_next;
-        vs = vs_next;
+        if (i + 1 < b) {
+          page = pages_of(t, k_then, entry_next);
+          if (E4m3) vs = scales_of(p.v_scale, t, k_then, h, page);
+        }
       }
     }
     if (*abort) settle_pair(sh.v_full, g);
@@ -664,22 +664,8 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
           top = __vmaxu2(top, __vmaxu2(__vmaxu2(q.x & 0x7fff7fffu, q.y & 0x7fff7fffu), __vmaxu2(q.z & 0x7fff7fffu, q.w & 0x7fff7fffu)));
         }
         top = max(top & 0xffffu, top >> 16);
-        // the smallest power of two under which the largest magnitude is at most 448 (see heart_cache_write)
-        const int k = min(max((int)(top >> 7) - 135 + ((top & 0x7fu) > 0x60u ? 1 : 0), -100), 120);
-        const float inv = __uint_as_float((uint32_t)(127 - k) << 23);
-        sh.q_scale[n & 1][r] = top < 0x7f80u ? p.scale_log2 * __uint_as_float((uint32_t)(127 + k) << 23) : __uint_as_float(0x7fc00000u);
-        auto split = [&](uint32_t w, uint32_t &hi, uint32_t &lo) {  // two elements
-          const float x0 = __uint_as_float(w << 16) * inv, x1 = __uint_as_float(w & 0xffff0000u) * inv;
-          uint16_t c;
-          asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(x1), "f"(x0));
-          hi = c;
-          uint32_t y;
-          asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y) : "h"(c));
-          float y0, y1;
-          asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, h;\n\t}" : "=f"(y0), "=f"(y1) : "r"(y));
-          asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(x1 - y1), "f"(x0 - y0));
-          lo = c;
-        };
+        float inv;
+        sh.q_scale[n & 1][r] = p.scale_log2 * code_scale(top, inv);
         uint4 low[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {  // 16 dims: pieces 2j and 2j + 1 of the row, to piece j of either half (the first one's has been read by then)
@@ -687,10 +673,10 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const uint4 q = lds_u4(at + (j >> 2) * (kTileBytes / 2) + (((2 * j + i) ^ r) & 7) * 16);
-            split(q.x, hi[4 * i], lo[4 * i]);
-            split(q.y, hi[4 * i + 1], lo[4 * i + 1]);
-            split(q.z, hi[4 * i + 2], lo[4 * i + 2]);
-            split(q.w, hi[4 * i + 3], lo[4 * i + 3]);
+            split_codes(q.x, inv, hi[4 * i], lo[4 * i]);
+            split_codes(q.y, inv, hi[4 * i + 1], lo[4 * i + 1]);
+            split_codes(q.z, inv, hi[4 * i + 2], lo[4 * i + 2]);
+            split_codes(q.w, inv, hi[4 * i + 3], lo[4 * i + 3]);
           }
           sts_u4(at + (((j ^ r) & 7) << 4), make_uint4(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16, hi[4] | hi[5] << 16, hi[6] | hi[7] << 16));
           low[j] = make_uint4(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16, lo[4] | lo[5] << 16, lo[6] | lo[7] << 16);
@@ -958,6 +944,9 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
         const bool whole = to.a == 0 && to.b == to.t.steps;
         const uint32_t out = smem_u32(smem + L::kOffQ + q_buf * kTileBytes + quarter * (kTileBytes / 4));  // the place of its Q: 32 rows a warp
         const int slot = 2 * blockIdx.x + (to.a == 0 ? 1 : 0);
+        // e4m3: a row without any key whose query is not finite has sums that are no numbers
+        const bool none = E4m3 && to.t.p0 + row / p.G < 0;
+        if (none) l = 0.f;
         // 64 dims of the row as bf16, O / l, into shared memory
         auto stage = [&](const uint32_t (&v)[64], int half, float inv) {
           const uint64_t inv2 = pack_f32x2(inv, inv);
@@ -972,6 +961,7 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
               x[k] = E4m3 ? pack_bf16x2(a0, a2) : pack_bf16x2(a0, a1);  // (converted values: dims 0, 2, 1, 3 of four)
               x[k + 1] = E4m3 ? pack_bf16x2(a1, a3) : pack_bf16x2(a2, a3);
             }
+            if (none) x[0] = x[1] = x[2] = x[3] = 0u;
             sts_u4(out + half * (kTileBytes / 8) + lane * 128 + ((i ^ (lane & 7)) << 4), make_uint4(x[0], x[1], x[2], x[3]));
           }
         };
