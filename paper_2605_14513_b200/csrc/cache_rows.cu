@@ -38,6 +38,13 @@ constexpr float kNoReference = -3.0e38f;
 constexpr float kMaxGrowth = 8.f;      // log2: the reference of a row moves when a maximum exceeds it by more
 constexpr float kHeadroomE4m3 = 6.f;   // log2 of the largest weight when the reference has moved
 
+struct True {
+  static constexpr bool value = true;
+};
+struct False {
+  static constexpr bool value = false;
+};
+
 struct RowsParams {
   CacheIndex ix;
   const uint16_t *Q;
@@ -55,6 +62,8 @@ struct RowsParams {
 struct RowsShared {
   uint64_t full[kWarps][kMaxStages];
   alignas(16) uint8_t scales[kWarps][kMaxStages][64];  // e4m3: of the keys and of the values of a stage
+  alignas(16) float k_factor[kWarps][32];   // e4m3: what the scores of a warp's keys are to be multiplied by,
+  alignas(16) uint16_t v_factor[kWarps][32];  // and its values, in f16
   float2 l[kWarps][32];   // row sums and references
   long long total[kWarps];
   int longest[kWarps];
@@ -348,10 +357,15 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint32_t vs[kTiles];  // e4m3: this lane's values are to be multiplied by these, two keys at a time
       // ---- scores
       if (E4m3) {
-        const uint8_t *scales = sh.scales[warp][take];
-        {  // the largest exponent of the values
-          const uint32_t vb = lane < kKeys && k0 + lane < q.len ? scales[kKeys + lane] : 0u;
-          const uint32_t top = __reduce_max_sync(0xffffffffu, vb == 255u ? 0u : vb);
+        {
+          // the scales, a lane a key, as numbers for all lanes: 2^e of the key (NaN where the token's key or value is not finite), 2^(e - E) of
+          // the value (nothing behind the sequence's end and where it is not finite)
+          const int key = lane & (kKeys - 1);
+          const uint32_t kb = sh.scales[warp][take][key];
+          uint32_t vb = sh.scales[warp][take][kKeys + key];
+          const float k_scale = cache_scale(vb == 255u ? 255u : kb);
+          if (vb == 255u || k0 + key >= q.len) vb = 0u;
+          const uint32_t top = __reduce_max_sync(0xffffffffu, vb);
           if (top > v_exp) {
             const float f = cache_scale(max((int)(v_exp - top) + 127, 1));
             v_exp = top;
@@ -362,6 +376,12 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) o[m][n][k] *= f;
           }
+          const float v_scale = vb == 0u ? 0.f : cache_scale(max((int)(vb - v_exp) + 127, 1));
+          if (lane < kKeys) {
+            sh.k_factor[warp][lane] = k_scale;
+            sh.v_factor[warp][lane] = (uint16_t)pack_f16x2(v_scale, 0.f);
+          }
+          __syncwarp();
         }
 #pragma unroll
         for (int n = 0; n < kTiles; ++n) {
@@ -376,20 +396,14 @@ __global__ void __launch_bounds__(kThreads, 1)
               for (int m = 0; m < MT; ++m) mma_f16(x[m][n], qf[m][j * 4 + k], b0, b1);
             }
           }
-          const uint32_t kb = *reinterpret_cast<const uint16_t *>(&scales[n * 8 + c * 2]);
-          const uint32_t vb = *reinterpret_cast<const uint16_t *>(&scales[kKeys + n * 8 + c * 2]);
-          auto factor = [&](uint32_t b, int key) {  // (behind the sequence's end, or not finite: nothing)
-            return b == 255u || k0 + key >= q.len ? 0.f : cache_scale(max((int)(b - v_exp) + 127, 1));
-          };
-          vs[n] = pack_f16x2(factor(vb & 255u, n * 8 + c * 2), factor(vb >> 8, n * 8 + c * 2 + 1));
-          // a token whose key or value is not finite
-          const float k_lo = cache_scale((vb & 255u) == 255u ? 255u : kb & 255u), k_hi = cache_scale((vb >> 8) == 255u ? 255u : kb >> 8);
+          const float2 f = *reinterpret_cast<const float2 *>(&sh.k_factor[warp][n * 8 + c * 2]);
+          vs[n] = *reinterpret_cast<const uint32_t *>(&sh.v_factor[warp][n * 8 + c * 2]);
 #pragma unroll
           for (int m = 0; m < MT; ++m) {
-            x[m][n][0] *= k_lo;
-            x[m][n][1] *= k_hi;
-            x[m][n][2] *= k_lo;
-            x[m][n][3] *= k_hi;
+            x[m][n][0] *= f.x;
+            x[m][n][1] *= f.y;
+            x[m][n][2] *= f.x;
+            x[m][n][3] *= f.y;
           }
         }
       } else {
@@ -452,23 +466,27 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       uint32_t pf[MT][kTiles / 2][4];
+      auto weights = [&](auto masked) {
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
+        for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int n = 0; n < kTiles; ++n)
+          for (int n = 0; n < kTiles; ++n)
 #pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            float w[2];
+            for (int r = 0; r < 2; ++r) {
+              float w[2];
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              const float y = x[m][n][2 * r + k];
-              w[k] = ex2(fmaf(y, row_scale[m][r], -ref[m][r]));
-              // (what is hidden is nothing, even to a query that is not finite)
-              if (E4m3 && !whole && y == -INFINITY) w[k] = 0.f;
-              sum[m][r] += w[k];
+              for (int k = 0; k < 2; ++k) {
+                const float y = x[m][n][2 * r + k];
+                w[k] = ex2(fmaf(y, row_scale[m][r], -ref[m][r]));
+                // (what is hidden is nothing, even to a query that is not finite)
+                if (decltype(masked)::value && y == -INFINITY) w[k] = 0.f;
+                sum[m][r] += w[k];
+              }
+              pf[m][n >> 1][(n & 1) * 2 + r] = E4m3 ? pack_f16x2(w[0], w[1]) : pack_bf16x2(w[0], w[1]);
             }
-            pf[m][n >> 1][(n & 1) * 2 + r] = E4m3 ? pack_f16x2(w[0], w[1]) : pack_bf16x2(w[0], w[1]);
-          }
+      };
+      if (E4m3 && !whole) weights(True{});
+      else weights(False{});
       if (!E4m3 && !whole) {
         // Values that are not finite must not reach rows that do not see them (0 * inf is NaN): they are taken out, and rows that
         // do see them are marked.

@@ -18,8 +18,8 @@
 // not split that way (many keys of little weight each would be lost): values are converted, by a fourth warpgroup, and multiplied by
 // their tokens' scales on the way, which is exact.  The keys' scales multiply the scores.
 //
-// Warp roles: 0-3, 4-7 softmax; 8 issues S = Q K^T; 9 V producer; 10 K and Q producer (finds the CTA's tiles); 11 issues
-// O += P V; 12-15 (e4m3) convert.  Tensor memory: O (128 columns) | S[2] (2 x 128) | P[2] (2 x 64).
+// Warp roles: 0-3, 4-7 softmax; 8 issues S = Q K^T; 9 copies V; 10 finds the CTA's parts and the pages of their steps, copies K and Q; 11
+// issues O += P V; 12-15 (e4m3) convert.  Tensor memory: O (128 columns) | S[2] (2 x 128) | P[2] (2 x 64).
 // Every wait is bounded; one that runs out raises the CTA's abort flag and the status word, and its roles stop.
 #include "cache.cuh"
 #include "tc_ptx.cuh"
@@ -31,6 +31,7 @@ namespace {
 constexpr int kWarpQK = 8, kWarpV = 9, kWarpK = 10, kWarpPV = 11, kWarpConvert = 12;
 constexpr int kTileBytes = 32768;  // 128 rows x 128 dims of bf16: [2 dim halves][128 rows][64], 128-byte swizzle
 constexpr int kCodeBytes = 16384;  // the same as e4m3: [128 rows][128]
+constexpr int kSteps = 16;         // key steps in flight (K is up to four steps ahead of the value products)
 constexpr int kPartRing = 4;
 constexpr int kMaxParts = 12;      // of a tile, about
 constexpr float kNoReference = -3.0e38f;
@@ -53,11 +54,18 @@ struct Part {
 };
 static_assert(sizeof(Part) == 64, "lanes copy words");
 
+// A key step of a CTA, some steps ahead of its use.
+struct Step {
+  int key, keys, h, flags;  // first key, keys of the sequence from there on, key head
+  int page[8];
+};
+constexpr int kStepMasked = 1, kStepStarts = 2, kStepEnd = 4;  // some row does not see all of its keys; first step of a part; no step left
+
 template <bool E4m3>
 struct Layout {
   static constexpr int kThreads = E4m3 ? 512 : 384;
   static constexpr int kRegsSoftmax = E4m3 ? 184 : 224, kRegsHelper = E4m3 ? 64 : 56, kRegsConvert = 80;  // sums: the registers at launch
-  static constexpr int kReaders = E4m3 ? 15 : 11;  // of announced parts: softmax warps, issuers, V producer, converters
+  static constexpr int kReaders = 11;  // of announced parts: softmax warps, issuers, V producer
   static constexpr int kKey = E4m3 ? kCodeBytes : kTileBytes;
   // Q, K, V (of which the products read), codes of V
   static constexpr int kOffQ = 0, kOffK = 2 * kTileBytes, kOffV = kOffK + 2 * kKey, kOffCodes = kOffV + 2 * kTileBytes;
@@ -72,18 +80,18 @@ struct TileShared {
   uint64_t s_full[2], s_free[2], p_full[2], pv_done[2], m_ready[2][4];  // as in attn_tc.cu
   uint64_t o_full[2], o_free, out_done[2];
   uint64_t part_full[kPartRing], part_empty[kPartRing];
+  uint64_t step_full[kSteps];
+  uint64_t scales_full[8];  // e4m3: the factors of a step's keys are there
   uint64_t drain[2];
   uint64_t stored[2], told[2];  // a warpgroup's part of a tile is in the workspace; it is the last one or not
   Part part[kPartRing];
   Part written[2][8];        // the part to write, per softmax warp
-  Tile k_tile[2], v_tile;    // the K producer's present and next tile, by its part & 1, the V producer's (helper warps have few registers)
-  uint32_t entry[4];         // steps in flight: step | masked << 31
+  Step step[kSteps];
   float m[2][128];           // references after step g
   float2 l[4][2][128];       // row sums and references: per part & 3 and warpgroup (a warpgroup may be two short parts ahead of one that writes)
-  alignas(16) float k_scale[8][128];  // e4m3, steps in flight, by g & 7: read behind the hand-back of the scores, before the reference of step g is there
-  alignas(16) float v_scale[2][128];
+  alignas(16) float k_scale[8][128], v_scale[8][128];  // e4m3, by g & 7
   float q_scale[2][128];     // e4m3: what the scores of a row are to be multiplied by
-  uint32_t bad[4][4];        // keys of a masked step that are not finite, by g & 3
+  alignas(16) uint32_t bad[8][4];  // keys that are not finite (bf16: of masked steps), by g & 7: written ahead by two steps at most, read before P_g is
   uint32_t tmem_base;
   int last[2];
   int abort;
@@ -279,6 +287,8 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
       mbar_init(&sh.part_empty[i], L::kReaders);
     }
     mbar_init(&sh.o_free, 4);
+    for (int i = 0; i < kSteps; ++i) mbar_init(&sh.step_full[i], 1);
+    for (int i = 0; i < 8; ++i) mbar_init(&sh.scales_full[i], 4);
     sh.abort = 0;
     mbar_fence_init();
   }
@@ -342,14 +352,6 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
   };
   const int page_log2 = ix.page_log2, n_boxes = 128 >> page_log2;
   auto key_of = [](const Tile &t, int i) { return (i < t.sinks ? i : t.first + i - t.sinks) * kKeyStep; };
-  // The table's entry for what lane i < n_boxes copies of the step at key k0 (asked for a step ahead), and the page that it stands for.
-  auto entries_of = [&](const Tile &t, int k0) {
-    const int k = k0 + (lane << page_log2);
-    return lane < n_boxes && k < t.len ? page_entry(ix, t.s, k) : 0;
-  };
-  auto pages_of = [&](const Tile &t, int k0, int entry) {
-    return lane < n_boxes && k0 + (lane << page_log2) < t.len ? checked_page(ix, entry) : ix.n_pages;  // (a page out of range: zeros)
-  };
   auto load_pages = [&](unsigned char *dst, const CUtensorMap *map, uint64_t *bar, int h, int page) {
     if (lane == 0) mbar_expect_tx(bar, L::kKey);
     __syncwarp();
@@ -358,12 +360,6 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
       tma_load_5d(to, map, bar, 0, 0, 0, h, page);
       if (!E4m3 && n_boxes > 1) tma_load_5d(to + kTileBytes / 2, map, bar, 0, 0, 1, h, page);
     }
-  };
-  // e4m3: the scale bytes of keys 4 * lane .. 4 * lane + 3 of a step, 127 where there are none
-  auto scales_of = [&](const uint8_t *scales, const Tile &t, int k0, int h, int page) -> uint32_t {
-    const int mine = __shfl_sync(0xffffffffu, page, (lane * 4) >> page_log2), k = k0 + lane * 4;
-    if (k >= t.len || mine >= ix.n_pages) return 0x7f7f7f7fu;
-    return __ldcg(reinterpret_cast<const uint32_t *>(scales + ((((size_t)mine * p.Hkv + h) << page_log2) + (k & ((1 << page_log2) - 1)))));
   };
   // Whether some row of the tile does not see all keys of the step at k0.
   struct Whole {
@@ -383,12 +379,14 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
     setmaxnreg_dec<L::kRegsHelper>();
   }
   if (warp == kWarpK) {
-    // ===== the CTA's parts; K and Q producer
+    // ===== the CTA's parts; K and Q producer.  What a step's other warps need to know is said before its copy is waited for.  (Little code: it
+    // is one of many places that the warps of an SM are in, see attn_tc.cu.  A warp of its own that looked ahead by five steps, with ten times
+    // the instructions, ran at three quarters of the rate.)
     const int n_tiles = __ldcg(&p.head[0]), longest = __ldcg(&p.head[1]);
     const long long per_head = __ldcg(&p.first[n_tiles]), total = per_head * p.Hkv;
     const long long share = max((total + gridDim.x - 1) / gridDim.x, (long long)(longest + kMaxParts - 1) / kMaxParts);
+    const long long u1 = min(total, (blockIdx.x + 1) * share);
     long long u = blockIdx.x * share;
-    const long long u1 = min(total, u + share);
     int h = 0, tile = 0, a = 0;
     if (u < u1) {
       h = (int)(u / per_head);
@@ -403,104 +401,88 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
       }
       a = (int)(rest - __ldcg(&p.first[tile]));
     }
-    auto fetch = [&](Tile &to, int i) {
-      __syncwarp();
-      if (lane < 8) reinterpret_cast<int *>(&to)[lane] = __ldcg(reinterpret_cast<const int *>(&p.tiles[i]) + lane);
-      __syncwarp();
-    };
     int g = 0, n = 0;
-    bool q_busy[2] = {false, false};
-    int page = 0, entry_next = 0;
-    uint32_t ks = 0, vs = 0;
-    if (u < u1) {
-      const Tile &t = sh.k_tile[0];
-      fetch(sh.k_tile[0], tile);
-      page = pages_of(t, key_of(t, a), entries_of(t, key_of(t, a)));
-      if (E4m3) ks = scales_of(p.k_scale, t, key_of(t, a), h, page), vs = scales_of(p.v_scale, t, key_of(t, a), h, page);
-    }
+    auto fetch = [&](int i) {  // lane i < 8: a word of a tile
+      return lane < 8 ? __ldcg(reinterpret_cast<const int *>(&p.tiles[i]) + lane) : 0;
+    };
+    int word = u < u1 ? fetch(tile) : 0;
 #pragma unroll 1
     for (;; ++n) {
       if (n >= kPartRing && !wait(&sh.part_empty[n % kPartRing], (n / kPartRing - 1) & 1)) break;
+      Part &x = sh.part[n % kPartRing];
       const bool any = u < u1;
-      const Tile &t = sh.k_tile[n & 1], &t_next = sh.k_tile[(n & 1) ^ 1];
-      const int b = any ? (int)min((long long)t.steps, a + (u1 - u)) : -1;
+      if (lane < 8) reinterpret_cast<int *>(&x.t)[lane] = word;
+      __syncwarp();
+      const int b = any ? (int)min((long long)x.t.steps, a + (u1 - u)) : -1;
       if (lane == 0) {
-        Part &x = sh.part[n % kPartRing];
-        x.t = t;
         x.h = h;
         x.a = a;
         x.b = b;
         const long long at = u - a;
         x.c0 = (int)(at / share);
-        x.parts = any ? (int)((at + t.steps - 1) / share) - x.c0 + 1 : 0;
+        x.parts = any ? (int)((at + x.t.steps - 1) / share) - x.c0 + 1 : 0;
         mbar_arrive(&sh.part_full[n % kPartRing]);
       }
+      // (no other warp writes the ring: this one may go on reading the part)
       __syncwarp();
       if (!any) break;
-      // the next part, ahead of time
-      const bool more = u + (b - a) < u1;
-      int h_next = h, tile_next = tile + 1;
-      if (tile_next == n_tiles) tile_next = 0, ++h_next;
-      if (more) fetch(sh.k_tile[(n & 1) ^ 1], tile_next);
-      const Whole whole = whole_of(t);
+      u += b - a;
+      int h_next = h;
+      if (++tile == n_tiles) tile = 0, ++h_next;
+      if (u < u1) word = fetch(tile);  // ahead of its use
+      const Whole whole = whole_of(x.t);
+      const uint32_t len = x.t.len;
+      const int sinks = x.t.sinks, shift = x.t.first - x.t.sinks, sink = ix.sink;
+      const int32_t *table = ix.table + (size_t)x.t.s * ix.table_stride + lane;
+      const uint32_t ahead = lane < n_boxes ? lane << page_log2 : 0x7fffffff;  // from a step's first key to that of the lane's box
+      auto entry_of = [&](int k0) { return k0 + ahead < len ? __ldcg(table + (k0 >> page_log2)) : ix.n_pages; };
+      int k0 = (a < sinks ? a : a + shift) * kKeyStep, entry = entry_of(k0);
 #pragma unroll 1
       for (int i = a; i < b; ++i, ++g) {
-        const int k0 = key_of(t, i);
-        const bool last = i + 1 == b;
-        const Tile &t_then = last ? t_next : t;  // the step behind this one
-        const int k_then = last && !more ? 0 : key_of(t_then, last ? 0 : i + 1);
-        if (!last || more) entry_next = entries_of(t_then, k_then);
-        if (g >= 2 && !wait(&sh.s_full[g & 1], ((g - 2) >> 1) & 1)) break;
-        bool masked = masked_at(whole, k0);
-        if (E4m3) {
-          // scales as numbers, and the tokens that have none
-          float f[4];
-          uint32_t bad[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint32_t kb = (ks >> (8 * j)) & 255u, vb = (vs >> (8 * j)) & 255u;
-            f[j] = kb == 255u ? 1.f : cache_scale(kb);  // (more than 0: hidden scores of -inf stay -inf)
-            bad[j] = __ballot_sync(0xffffffffu, kb == 255u || vb == 255u);
-          }
-          *reinterpret_cast<float4 *>(&sh.k_scale[g & 7][lane * 4]) = make_float4(f[0], f[1], f[2], f[3]);
-          if (lane < 4) sh.bad[g & 3][lane] = lane == 0 ? bad[0] : lane == 1 ? bad[1] : lane == 2 ? bad[2] : bad[3];
-          masked |= (bad[0] | bad[1] | bad[2] | bad[3]) != 0u;
+        Step &y = sh.step[g % kSteps];
+        int page = entry;
+        if ((unsigned)page > (unsigned)ix.n_pages || (page == ix.n_pages && k0 + ahead < len)) page = checked_page(ix, entry);  // (out of range: zeros)
+        if (lane < 8) y.page[lane] = page;
+        if (lane == 0) {
+          y.key = k0;
+          y.keys = (int)len - k0;
+          y.h = h;
+          y.flags = (k0 + kKeyStep <= whole.end && (k0 >= whole.low || k0 + kKeyStep <= sink) ? 0 : kStepMasked) | (i == a ? kStepStarts : 0);
         }
-        if (lane == 0) sh.entry[g & 3] = (uint32_t)(k0 / kKeyStep) | (masked ? 1u << 31 : 0u);
         __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.step_full[g % kSteps]);
+        if (i + 1 < b) {
+          k0 = (i + 1 < sinks ? i + 1 : i + 1 + shift) * kKeyStep;
+          entry = entry_of(k0);
+        }
+        if (g >= 2 && !wait(&sh.s_full[g & 1], ((g - 2) >> 1) & 1)) break;
         load_pages(smem + L::kOffK + (g & 1) * L::kKey, &map_k, &sh.k_full[g & 1], h, page);
         if (i == a) {
           if (n >= 2 && !wait(&sh.out_done[n & 1], ((n - 2) >> 1) & 1)) {
             ++g;
             break;
           }
-          const int rows = 128 / p.G * p.G;
           if (lane == 0) {
             unsigned char *q = smem + L::kOffQ + (n & 1) * kTileBytes;
-            mbar_expect_tx(&sh.q_full[n & 1], 2 * rows * 128);
-            tma_load_5d(q, &map_q, &sh.q_full[n & 1], 0, 0, t.row, 0, h);
-            tma_load_5d(q + kTileBytes / 2, &map_q, &sh.q_full[n & 1], 0, 0, t.row, 1, h);
-          }
-          q_busy[n & 1] = true;
-        }
-        if (!last || more) {
-          page = pages_of(t_then, k_then, entry_next);
-          if (E4m3) {
-            ks = scales_of(p.k_scale, t_then, k_then, last ? h_next : h, page);
-            vs = scales_of(p.v_scale, t_then, k_then, last ? h_next : h, page);
+            mbar_expect_tx(&sh.q_full[n & 1], 2 * (128 / p.G * p.G) * 128);
+            tma_load_5d(q, &map_q, &sh.q_full[n & 1], 0, 0, x.t.row, 0, h);
+            tma_load_5d(q + kTileBytes / 2, &map_q, &sh.q_full[n & 1], 0, 0, x.t.row, 1, h);
           }
         }
       }
       if (!ok) break;
-      u += b - a;
       a = 0;
-      tile = tile_next;
       h = h_next;
+    }
+    if (E4m3 && ok) {  // for those who look ahead
+      if (lane == 0) {
+        sh.step[g % kSteps].flags = kStepEnd;
+        mbar_arrive(&sh.step_full[g % kSteps]);
+      }
     }
     if (*abort) {
       settle_pair(sh.k_full, g);
-      const int nq = n + (q_busy[n & 1] ? 1 : 0);
-      settle_pair(sh.q_full, nq);
+      settle_pair(sh.q_full, n + 1);
     }
   } else if (warp == kWarpV) {
     // ===== V producer
@@ -509,69 +491,47 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
     for (int n = 0; ok; ++n) {
       const Part *x = part_at(n);
       if (x == nullptr || x->b < 0) break;
-      const Tile &t = sh.v_tile;
-      const int h = x->h, a = x->a, b = x->b;
-      if (lane < 8) reinterpret_cast<int *>(&sh.v_tile)[lane] = reinterpret_cast<const int *>(&x->t)[lane];
+      const int n_steps = x->b - x->a;
       done_with_part(n);
-      const Whole whole = whole_of(t);
-      int page = pages_of(t, key_of(t, a), entries_of(t, key_of(t, a))), entry_next = 0;
-      uint32_t vs = 0;
-      if (E4m3) vs = scales_of(p.v_scale, t, key_of(t, a), h, page);
 #pragma unroll 1
-      for (int i = a; i < b; ++i, ++g) {
-        const int k0 = key_of(t, i), at = g & 1;
-        const int k_then = i + 1 < b ? key_of(t, i + 1) : 0;
-        if (i + 1 < b) entry_next = entries_of(t, k_then);
-        if (E4m3) {
-          if (g >= 2 && !wait(&sh.codes_free[at], ((g - 2) >> 1) & 1)) break;
-          float f[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint32_t vb = (vs >> (8 * j)) & 255u;
-            // (behind the sequence's end, or not finite: nothing)
-            f[j] = vb == 255u || k0 + lane * 4 + j >= t.len ? 0.f : cache_scale(vb);
-          }
-          *reinterpret_cast<float4 *>(&sh.v_scale[at][lane * 4]) = make_float4(f[0], f[1], f[2], f[3]);
-          __syncwarp();
-          load_pages(smem + L::kOffCodes + at * kCodeBytes, &map_v, &sh.v_full[at], h, page);
-        } else {
-          if (g >= 2 && !wait(&sh.pv_done[at], ((g - 2) >> 1) & 1)) break;
-          load_pages(smem + L::kOffV + at * kTileBytes, &map_v, &sh.v_full[at], h, page);
-          if (masked_at(whole, k0)) {
+      for (int i = 0; i < n_steps; ++i, ++g) {
+        const int at = g & 1;
+        if (!wait(&sh.step_full[g % kSteps], (g / kSteps) & 1)) break;
+        const Step &y = sh.step[g % kSteps];
+        const int page = y.page[lane & 7], h = y.h;
+        const bool masked = y.flags & kStepMasked;
+        if (g >= 2 && !wait(E4m3 ? &sh.codes_free[at] : &sh.pv_done[at], ((g - 2) >> 1) & 1)) break;
+        load_pages(smem + (E4m3 ? L::kOffCodes : L::kOffV) + at * L::kKey, &map_v, &sh.v_full[at], h, page);
+        if (!E4m3) {
+          if (masked) {
             if (!wait(&sh.v_full[at], (g >> 1) & 1)) {
               ++g;
               break;
             }
             // values that are not finite: [2 dim halves][128 keys][8 x 16 bytes]
             const uint32_t v_at = smem_u32(smem + L::kOffV + at * kTileBytes);
-            uint32_t bad[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
+            uint32_t any = 0u;
+#pragma unroll 1
             for (int w = 0; w < 4; ++w) {
+              uint32_t bad = 0u;
 #pragma unroll 4
               for (int j = 0; j < 16; ++j) {  // 32 keys: 8 pieces of 4 keys in each half
                 const uint4 v = lds_u4(v_at + (j >> 3) * (kTileBytes / 2) + w * 4096 + (j & 7) * 512 + lane * 16);
-                if (not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w)) bad[w] |= 1u << ((j & 7) * 4 + (lane >> 3));
+                if (not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w)) bad |= 1u << ((j & 7) * 4 + (lane >> 3));
               }
-              bad[w] = __reduce_or_sync(0xffffffffu, bad[w]);
-            }
-            if (bad[0] | bad[1] | bad[2] | bad[3]) {
-#pragma unroll
-              for (int w = 0; w < 4; ++w)
+              bad = __reduce_or_sync(0xffffffffu, bad);
+              any |= bad;
+              if (lane == 0) sh.bad[g & 7][w] = bad;
 #pragma unroll 1
-                for (uint32_t todo = bad[w]; todo; todo &= todo - 1) {
-                  const int key = w * 32 + __ffs(todo) - 1;
-                  if (lane < 16) sts_u4(v_at + (lane >> 3) * (kTileBytes / 2) + key * 128 + (lane & 7) * 16, make_uint4(0u, 0u, 0u, 0u));
-                }
-              async_proxy_fence();
+              for (; bad; bad &= bad - 1) {
+                const int key = w * 32 + __ffs(bad) - 1;
+                if (lane < 16) sts_u4(v_at + (lane >> 3) * (kTileBytes / 2) + key * 128 + (lane & 7) * 16, make_uint4(0u, 0u, 0u, 0u));
+              }
             }
-            if (lane < 4) sh.bad[g & 3][lane] = lane == 0 ? bad[0] : lane == 1 ? bad[1] : lane == 2 ? bad[2] : bad[3];
+            if (any) async_proxy_fence();
           }
           __syncwarp();
           if (lane == 0) mbar_arrive(&sh.v_ready[at]);
-        }
-        if (i + 1 < b) {
-          page = pages_of(t, k_then, entry_next);
-          if (E4m3) vs = scales_of(p.v_scale, t, k_then, h, page);
         }
       }
     }
@@ -594,6 +554,7 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
       for (int i = 0; i < n_steps; ++i, ++g) {  // S_g = Q K_g^T
         const uint32_t b = g & 1;
         if (g >= 2) wait(&sh.s_free[b], ((g - 2) >> 1) & 1);
+        if (E4m3) wait(&sh.scales_full[g & 7], (g >> 3) & 1);  // (for the softmax warps)
         if (!wait(&sh.k_full[b], (g >> 1) & 1)) break;
         tc_fence_after();
         if (leader) {
@@ -644,63 +605,91 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
     }
     drain_products(leader, &sh.drain[1]);
   } else if (warp >= kWarpConvert) {
-    // ===== converters (e4m3): a thread a row of Q, a key of V
+    // ===== converters (e4m3): a thread a row of Q, a key of V.  Scales are asked for and made known two steps ahead.
     const int r = tid - kWarpConvert * 32;
-    uint32_t g = 0;
-#pragma unroll 1
-    for (int n = 0; ok; ++n) {
-      const Part *x = part_at(n);
-      if (x == nullptr || x->b < 0) break;
-      const int n_steps = x->b - x->a;
-      done_with_part(n);
-      // Q: q = 2^k (high + low), codes of both; the row's place in the first half holds the high parts, in the second the low ones
-      if (!wait(&sh.q_full[n & 1], (n >> 1) & 1)) break;
-      {
-        const uint32_t at = smem_u32(smem + L::kOffQ + (n & 1) * kTileBytes) + r * 128;
-        uint32_t top = 0u;
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const uint4 q = lds_u4(at + (j >> 3) * (kTileBytes / 2) + (((j ^ r) & 7) << 4));
-          top = __vmaxu2(top, __vmaxu2(__vmaxu2(q.x & 0x7fff7fffu, q.y & 0x7fff7fffu), __vmaxu2(q.z & 0x7fff7fffu, q.w & 0x7fff7fffu)));
-        }
-        top = max(top & 0xffffu, top >> 16);
-        float inv;
-        sh.q_scale[n & 1][r] = p.scale_log2 * code_scale(top, inv);
-        uint4 low[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {  // 16 dims: pieces 2j and 2j + 1 of the row, to piece j of either half (the first one's has been read by then)
-          uint32_t hi[8], lo[8];
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const uint4 q = lds_u4(at + (j >> 2) * (kTileBytes / 2) + (((2 * j + i) ^ r) & 7) * 16);
-            split_codes(q.x, inv, hi[4 * i], lo[4 * i]);
-            split_codes(q.y, inv, hi[4 * i + 1], lo[4 * i + 1]);
-            split_codes(q.z, inv, hi[4 * i + 2], lo[4 * i + 2]);
-            split_codes(q.w, inv, hi[4 * i + 3], lo[4 * i + 3]);
-          }
-          sts_u4(at + (((j ^ r) & 7) << 4), make_uint4(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16, hi[4] | hi[5] << 16, hi[6] | hi[7] << 16));
-          low[j] = make_uint4(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16, lo[4] | lo[5] << 16, lo[6] | lo[7] << 16);
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sts_u4(at + kTileBytes / 2 + (((j ^ r) & 7) << 4), low[j]);
-        async_proxy_fence();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.q_ready[n & 1]);
+    uint32_t n = 0;
+    bool ended = false;  // there is no step `asked`
+    uint32_t asked = 0;
+    uint32_t kb = 127u, vb = 127u;
+    auto ask = [&]() {  // the scale bytes of step `asked`
+      if (ended || !wait(&sh.step_full[asked % kSteps], (asked / kSteps) & 1)) return;
+      const Step &y = sh.step[asked % kSteps];
+      if (y.flags & kStepEnd) {
+        ended = true;
+        return;
       }
+      const int page = y.page[r >> page_log2];
+      kb = vb = 127u;
+      if (r < y.keys && page < ix.n_pages) {
+        const size_t at = (((size_t)page * p.Hkv + y.h) << page_log2) + ((y.key + r) & ((1 << page_log2) - 1));
+        kb = __ldcg(p.k_scale + at);
+        vb = __ldcg(p.v_scale + at);
+      }
+    };
+    auto tell = [&]() {  // and as numbers, with the tokens that have none
+      if (ended || !ok) return;
+      const bool bad = kb == 255u || vb == 255u, there = r < sh.step[asked % kSteps].keys;
+      sh.k_scale[asked & 7][r] = kb == 255u ? 1.f : cache_scale(kb);  // (more than 0: hidden scores of -inf stay -inf)
+      sh.v_scale[asked & 7][r] = vb == 255u || !there ? 0.f : cache_scale(vb);
+      const uint32_t all = __ballot_sync(0xffffffffu, bad);
+      if (lane == 0) sh.bad[asked & 7][warp - kWarpConvert] = all;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.scales_full[asked & 7]);
+      ++asked;
+    };
+    // Q: q = 2^k (high + low), codes of both; the row's place in the first half holds the high parts, in the second the low ones
+    auto split_queries = [&]() {
+      if (!wait(&sh.q_full[n & 1], (n >> 1) & 1)) return;
+      const uint32_t at = smem_u32(smem + L::kOffQ + (n & 1) * kTileBytes) + r * 128;
+      uint32_t top = 0u;
+#pragma unroll 4
+      for (int j = 0; j < 16; ++j) {
+        const uint4 q = lds_u4(at + (j >> 3) * (kTileBytes / 2) + (((j ^ r) & 7) << 4));
+        top = __vmaxu2(top, __vmaxu2(__vmaxu2(q.x & 0x7fff7fffu, q.y & 0x7fff7fffu), __vmaxu2(q.z & 0x7fff7fffu, q.w & 0x7fff7fffu)));
+      }
+      top = max(top & 0xffffu, top >> 16);
+      float inv;
+      sh.q_scale[n & 1][r] = p.scale_log2 * code_scale(top, inv);
+      uint4 low[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {  // 16 dims: pieces 2j and 2j + 1 of the row, to piece j of either half (the first one's has been read by then)
+        uint32_t hi[8], lo[8];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint4 q = lds_u4(at + (j >> 2) * (kTileBytes / 2) + (((2 * j + i) ^ r) & 7) * 16);
+          split_codes(q.x, inv, hi[4 * i], lo[4 * i]);
+          split_codes(q.y, inv, hi[4 * i + 1], lo[4 * i + 1]);
+          split_codes(q.z, inv, hi[4 * i + 2], lo[4 * i + 2]);
+          split_codes(q.w, inv, hi[4 * i + 3], lo[4 * i + 3]);
+        }
+        sts_u4(at + (((j ^ r) & 7) << 4), make_uint4(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16, hi[4] | hi[5] << 16, hi[6] | hi[7] << 16));
+        low[j] = make_uint4(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16, lo[4] | lo[5] << 16, lo[6] | lo[7] << 16);
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sts_u4(at + kTileBytes / 2 + (((j ^ r) & 7) << 4), low[j]);
+      async_proxy_fence();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.q_ready[n & 1]);
+      ++n;
+    };
+    // (g runs from -2 on: the first steps' scales and queries, before any values)
 #pragma unroll 1
-      for (int i = 0; i < n_steps; ++i, ++g) {
+    for (int g = -2; ok; ++g) {
+      ask();  // step g + 2
+      if (g >= 0) {
+        if (g >= (int)asked && ended) break;  // (steps are asked for ahead: all told of are done)
         const uint32_t b = g & 1;
         if (!wait(&sh.v_full[b], (g >> 1) & 1)) break;
         const uint32_t from = smem_u32(smem + L::kOffCodes + b * kCodeBytes) + r * 128;
         const uint32_t to = smem_u32(smem + L::kOffV + b * kTileBytes) + r * 128;
-        const float scale = sh.v_scale[b][r];
+        const float scale = sh.v_scale[g & 7][r];
         // a code's bits at their places in bf16 stand for 2^-120 of its value
         const bool large = scale > 128.f;  // (2^120 times it is no bf16 number)
         const uint32_t f = __float_as_uint(large ? 0x1p120f : scale * 0x1p120f) >> 16, f2 = f | f << 16;
         const uint32_t rest = __float_as_uint(large ? scale : 1.f) >> 16, rest2 = rest | rest << 16;
         const bool any_large = __any_sync(0xffffffffu, large);
         if (g >= 2 && !wait(&sh.pv_done[b], ((g - 2) >> 1) & 1)) break;
-#pragma unroll
+#pragma unroll 2
         for (int j = 0; j < 8; ++j) {  // 16 dims, in fours: dims 0, 2, 1, 3 (the output puts them right)
           const uint4 w = lds_u4(from + (((j ^ r) & 7) << 4));
           const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
@@ -724,6 +713,9 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
           mbar_arrive(&sh.codes_free[b]);
         }
       }
+      tell();
+      // the queries of the part that starts there
+      if (g + 2 < (int)asked && (sh.step[(g + 2) % kSteps].flags & kStepStarts)) split_queries();
     }
   } else {
     // ===== softmax / correction / output: thread = one row
@@ -752,10 +744,10 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
       return first && pending != 0;
     };
     // Hidden keys of step g get a score of -inf; rows that see a key or value that is not finite are marked.
-    auto mask_keys = [&](uint32_t g, uint32_t e) {
+    auto mask_keys = [&](uint32_t g) {
       const uint32_t s_at = s_addr + (g & 1) * 128;
       const Part &x = sh.written[nt & 1][warp];
-      const int k0 = (int)(e & 0x7fffffffu) * kKeyStep;
+      const int k0 = sh.step[g % kSteps].key;
       const Visible v = visible(ix, x.t.p0 + row / p.G, x.t.len);
       const int end = v.end - k0, low = v.low - k0, sink = ix.sink - k0;
       tc_fence_after();
@@ -774,8 +766,8 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
 #pragma unroll 1
       for (int j = 0; j < 4; ++j)
 #pragma unroll 1
-        for (uint32_t todo = sh.bad[g & 3][j]; todo; todo &= todo - 1) {
-          const int k = E4m3 ? (__ffs(todo) - 1) * 4 + j : j * 32 + __ffs(todo) - 1;
+        for (uint32_t todo = sh.bad[g & 7][j]; todo; todo &= todo - 1) {
+          const int k = j * 32 + __ffs(todo) - 1;
           if (k < end && (k >= low || k < sink)) l_run = __uint_as_float(0x7fc00000u);
         }
     };
@@ -817,7 +809,11 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
           why = kNotThere;
           break;
         }
-        const uint32_t e = sh.entry[g & 3];
+        bool special = sh.step[g % kSteps].flags & kStepMasked;
+        if (E4m3) {
+          const uint4 bad = *reinterpret_cast<const uint4 *>(sh.bad[g & 7]);
+          special |= (bad.x | bad.y | bad.z | bad.w) != 0u;
+        }
         tc_fence_after();
         if (E4m3) c = sh.q_scale[nt & 1][row];
         const float m_prev = h > 0 ? sh.m[b ^ 1][row] : kNoReference;
@@ -836,7 +832,7 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
           m_ref = m_new;
           return true;
         };
-        if (__builtin_expect((e >> 31) && !masked, 0)) {
+        if (__builtin_expect(special && !masked, 0)) {
           why = kMask;
           break;
         }
@@ -898,7 +894,7 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
           if (g > 0) wait(&sh.m_ready[b ^ 1][quarter], ((g - 1) >> 1) & 1);
           wait(&sh.s_full[b], (g >> 1) & 1);
         } else if (why == kMask) {
-          mask_keys(g, sh.entry[g & 3]);
+          mask_keys(g);
           masked = true;
         } else {
           // O changes scale: the products of the steps before have to be complete
