@@ -80,6 +80,27 @@ bool make_pool_map(CUtensorMap *m, const void *base, const CacheGeom &g, int row
 __device__ __forceinline__ float cache_scale(uint32_t byte) {
   return __uint_as_float(byte == 255u ? 0x7fc00000u : byte == 0u ? 0x00400000u : byte << 23);
 }
+// Two codes as f16, and two fp32 numbers.
+__device__ __forceinline__ uint32_t codes_to_f16x2(uint32_t codes) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\t}" : "=r"(r) : "r"(codes));
+  return r;
+}
+__device__ __forceinline__ uint32_t high_codes_to_f16x2(uint32_t codes) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}" : "=r"(r) : "r"(codes));
+  return r;
+}
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
 // The scale of a row of codes whose largest bf16 magnitude has the bits `top`, as heart_cache_write has it (from 2^-100 on), NaN where
 // that is not finite; inv: one over it.
 __device__ __forceinline__ float code_scale(uint32_t top, float &inv) {

@@ -15,8 +15,11 @@
 // e4m3 caches.  Converting keys and values to bf16 for 128 rows costs as many instructions as the softmax does.  Keys need none: a bf16 query has
 // 8 significant bits and a code 4, so a query row, scaled by a power of two, is the sum of two rows of codes, to 2^-18 of its
 // largest element, and two products with the keys' codes at twice the rate take the time of one in bf16.  Weights are
-// not split that way (many keys of little weight each would be lost): values are converted, by a fourth warpgroup, and multiplied by
-// their tokens' scales on the way, which is exact.  The keys' scales multiply the scores.
+// not split that way (many keys of little weight each would be lost): values are converted by a fourth warpgroup, to f16, which takes one
+// instruction for two codes, where bf16 takes nine for four (3900 clocks a step).  The keys' scales multiply the scores; the values' do not fit f16
+// whatever they are, so a step's values are code * 2^(e - E), E the largest exponent of the step, and its weights
+// 2^(score + E - m): the reference of a row is over score + E.  The sums, of 2^(score - m + E of the part's first step), take 2^(that - E) a
+// step.  A weight of less than 2^-29 of what was the largest when the reference moved counts as zero.
 //
 // Warp roles: 0-3, 4-7 softmax; 8 issues S = Q K^T; 9 copies V; 10 finds the CTA's parts and the pages of their steps, copies K and Q; 11
 // issues O += P V; 12-15 (e4m3) convert.  Tensor memory: O (128 columns) | S[2] (2 x 128) | P[2] (2 x 64).
@@ -36,6 +39,7 @@ constexpr int kPartRing = 4;
 constexpr int kMaxParts = 12;      // of a tile, about
 constexpr float kNoReference = -3.0e38f;
 constexpr float kHeadroom = 16.f, kMaxGrowth = 8.f;  // see attn_tc.cu
+constexpr float kHeadroomE4m3 = -4.f, kMaxGrowthE4m3 = 14.f;  // weights of f16: 2^4 where the reference moves, to 2^14
 constexpr uint32_t kShortWait = 500;
 
 // A tile of a head as the plan kernel writes it.
@@ -89,7 +93,10 @@ struct TileShared {
   Step step[kSteps];
   float m[2][128];           // references after step g
   float2 l[4][2][128];       // row sums and references: per part & 3 and warpgroup (a warpgroup may be two short parts ahead of one that writes)
-  alignas(16) float k_scale[8][128], v_scale[8][128];  // e4m3, by g & 7
+  alignas(16) float k_scale[8][128];  // e4m3, by g & 7
+  uint8_t v_scale[8][128];            // scale bytes, 0: nothing
+  int first_top[4];                   // the largest one of the first step, per part & 3
+  alignas(16) int v_top[8][4];        // the largest of 32 keys each
   float q_scale[2][128];     // e4m3: what the scores of a row are to be multiplied by
   alignas(16) uint32_t bad[8][4];  // keys that are not finite (bf16: of masked steps), by g & 7: written ahead by two steps at most, read before P_g is
   uint32_t tmem_base;
@@ -126,8 +133,9 @@ __device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
-// Weights 2^(s*c - m) of 32 scores of a row, packed to bf16, and their sums (of the weights before they are rounded: the log-sum-exp
+// Weights 2^(s*c - m) of 32 scores of a row, packed to bf16 or f16, and their sums (of the weights before they are rounded: the log-sum-exp
 // is then good to 32 bits).
+template <bool F16>
 __device__ __forceinline__ void exp32(const uint32_t *s, uint64_t c2, uint64_t neg_m2, uint32_t *pk, uint64_t (&sums)[2]) {
 #pragma unroll
   for (int i = 0; i < 32; i += 4) {
@@ -137,8 +145,8 @@ __device__ __forceinline__ void exp32(const uint32_t *s, uint64_t c2, uint64_t n
     x0 = ex2(x0), x1 = ex2(x1), x2 = ex2(x2), x3 = ex2(x3);
     sums[0] = add_f32x2(sums[0], pack_f32x2(x0, x1));
     sums[1] = add_f32x2(sums[1], pack_f32x2(x2, x3));
-    pk[i >> 1] = pack_bf16x2(x0, x1);
-    pk[(i >> 1) + 1] = pack_bf16x2(x2, x3);
+    pk[i >> 1] = F16 ? pack_f16x2(x0, x1) : pack_bf16x2(x0, x1);
+    pk[(i >> 1) + 1] = F16 ? pack_f16x2(x2, x3) : pack_bf16x2(x2, x3);
   }
 }
 __device__ __forceinline__ float max64(const uint32_t *s) {
@@ -158,6 +166,10 @@ __device__ __forceinline__ void mma_ss_e4m3(uint32_t d_tmem, uint64_t a_desc, ui
       "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
+// Instruction descriptor for kind::f16 with f16 A/B and fp32 accumulator.
+__host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N, bool a_mn_major, bool b_mn_major) {
+  return (1u << 4) | ((a_mn_major ? 1u : 0u) << 15) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
 __host__ __device__ constexpr uint32_t idesc_e4m3_f32(int M, int N) {
   return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);  // D f32, A and B e4m3 (0), K-major
 }
@@ -169,12 +181,12 @@ __device__ __forceinline__ uint4 lds_u4(uint32_t addr) {
 __device__ __forceinline__ void sts_u4(uint32_t addr, uint4 v) {
   asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
-__device__ __forceinline__ bool not_finite(uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
-__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
+// The largest scale byte of a step (that of the smallest scale where there is no value).
+__device__ __forceinline__ int top_scale(const int (&top)[4]) {
+  const int4 x = *reinterpret_cast<const int4 *>(top);
+  return max(max(max(x.x, x.y), max(x.z, x.w)), 17);
 }
+__device__ __forceinline__ bool not_finite(uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
 
 // ---------------------------------------------------------------------- plan
 // The tiles of a head, sequence by sequence, and the key steps before each.  One CTA.
@@ -575,7 +587,7 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
     drain_products(leader, &sh.drain[0]);
   } else if (warp == kWarpPV) {
     // ===== issuer of the value products
-    constexpr uint32_t idesc = idesc_bf16_f32(128, 128, false, true);
+    constexpr uint32_t idesc = E4m3 ? idesc_f16_f32(128, 128, false, true) : idesc_bf16_f32(128, 128, false, true);
     const uint64_t v_desc = smem_desc_sw128(smem_u32(smem + L::kOffV), kTileBytes / 2, 1024);
     const bool leader = elect_one();
     uint32_t g = 0;
@@ -630,9 +642,14 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
       if (ended || !ok) return;
       const bool bad = kb == 255u || vb == 255u, there = r < sh.step[asked % kSteps].keys;
       sh.k_scale[asked & 7][r] = kb == 255u ? 1.f : cache_scale(kb);  // (more than 0: hidden scores of -inf stay -inf)
-      sh.v_scale[asked & 7][r] = vb == 255u || !there ? 0.f : cache_scale(vb);
+      const uint32_t v = vb == 255u || !there ? 0u : vb;
+      sh.v_scale[asked & 7][r] = (uint8_t)v;
+      const uint32_t top = __reduce_max_sync(0xffffffffu, v);
       const uint32_t all = __ballot_sync(0xffffffffu, bad);
-      if (lane == 0) sh.bad[asked & 7][warp - kWarpConvert] = all;
+      if (lane == 0) {
+        sh.bad[asked & 7][warp - kWarpConvert] = all;
+        sh.v_top[asked & 7][warp - kWarpConvert] = (int)top;
+      }
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh.scales_full[asked & 7]);
       ++asked;
@@ -682,29 +699,19 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
         if (!wait(&sh.v_full[b], (g >> 1) & 1)) break;
         const uint32_t from = smem_u32(smem + L::kOffCodes + b * kCodeBytes) + r * 128;
         const uint32_t to = smem_u32(smem + L::kOffV + b * kTileBytes) + r * 128;
-        const float scale = sh.v_scale[g & 7][r];
-        // a code's bits at their places in bf16 stand for 2^-120 of its value
-        const bool large = scale > 128.f;  // (2^120 times it is no bf16 number)
-        const uint32_t f = __float_as_uint(large ? 0x1p120f : scale * 0x1p120f) >> 16, f2 = f | f << 16;
-        const uint32_t rest = __float_as_uint(large ? scale : 1.f) >> 16, rest2 = rest | rest << 16;
-        const bool any_large = __any_sync(0xffffffffu, large);
+        if (!wait(&sh.scales_full[g & 7], (g >> 3) & 1)) break;  // (the other warps' largest scales)
+        const int vs = sh.v_scale[g & 7][r];
+        const float f = vs == 0 ? 0.f : cache_scale(max(vs - top_scale(sh.v_top[g & 7]) + 127, 1));
+        const uint32_t f2 = pack_f16x2(f, f);
         if (g >= 2 && !wait(&sh.pv_done[b], ((g - 2) >> 1) & 1)) break;
 #pragma unroll 2
-        for (int j = 0; j < 8; ++j) {  // 16 dims, in fours: dims 0, 2, 1, 3 (the output puts them right)
+        for (int j = 0; j < 8; ++j) {  // 16 dims
           const uint4 w = lds_u4(from + (((j ^ r) & 7) << 4));
-          const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
-          uint32_t o[8];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            o[2 * k] = mul_bf16x2(((ws[k] << 4) & 0x07f007f0u) | ((ws[k] << 8) & 0x80008000u), f2);
-            o[2 * k + 1] = mul_bf16x2(((ws[k] >> 4) & 0x07f007f0u) | (ws[k] & 0x80008000u), f2);
-          }
-          if (any_large)
-#pragma unroll
-            for (int k = 0; k < 8; ++k) o[k] = mul_bf16x2(o[k], rest2);
           const uint32_t half = to + (j >> 2) * (kTileBytes / 2);
-          sts_u4(half + ((((j & 3) * 2) ^ (r & 7)) << 4), make_uint4(o[0], o[1], o[2], o[3]));
-          sts_u4(half + ((((j & 3) * 2 + 1) ^ (r & 7)) << 4), make_uint4(o[4], o[5], o[6], o[7]));
+          sts_u4(half + ((((j & 3) * 2) ^ (r & 7)) << 4), make_uint4(mul_f16x2(codes_to_f16x2(w.x), f2), mul_f16x2(high_codes_to_f16x2(w.x), f2),
+                                                                     mul_f16x2(codes_to_f16x2(w.y), f2), mul_f16x2(high_codes_to_f16x2(w.y), f2)));
+          sts_u4(half + ((((j & 3) * 2 + 1) ^ (r & 7)) << 4), make_uint4(mul_f16x2(codes_to_f16x2(w.z), f2), mul_f16x2(high_codes_to_f16x2(w.z), f2),
+                                                                         mul_f16x2(codes_to_f16x2(w.w), f2), mul_f16x2(high_codes_to_f16x2(w.w), f2)));
         }
         async_proxy_fence();
         __syncwarp();
@@ -735,6 +742,7 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
     uint32_t pending = 0;     // the part before is this warpgroup's to write: 1 behind its first step of the next one, 2 before
     bool live = true;
     float m_ref = kNoReference, l_run = 0.f;
+    int first_top = 0;        // e4m3: the largest scale byte of the part's first step
     enum { kNothing, kNotThere, kMask, kRescale } why = kNothing;  // why the loop over the steps was left
     bool masked = false;
     float alpha = 1.f;
@@ -815,13 +823,20 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
           special |= (bad.x | bad.y | bad.z | bad.w) != 0u;
         }
         tc_fence_after();
-        if (E4m3) c = sh.q_scale[nt & 1][row];
+        float shift = 0.f, l_factor = 1.f;  // e4m3: E of the step, 2^(E of the part's first step - E)
+        if (E4m3) {
+          c = sh.q_scale[nt & 1][row];
+          if (h < 2) first_top = top_scale(sh.v_top[g0 & 7]);
+          const int top = top_scale(sh.v_top[g & 7]);
+          shift = (float)(top - 127);
+          l_factor = cache_scale(min(max(first_top - top + 127, 1), 254));
+        }
         const float m_prev = h > 0 ? sh.m[b ^ 1][row] : kNoReference;
         uint64_t sums[2] = {0ull, 0ull};
         bool moved = false;
         auto new_reference = [&](float x_max) -> bool {
-          const bool grow = x_max > m_ref + kMaxGrowth;
-          const float m_new = grow ? x_max + kHeadroom : m_ref;
+          const bool grow = x_max > m_ref + (E4m3 ? kMaxGrowthE4m3 : kMaxGrowth);
+          const float m_new = grow ? x_max + (E4m3 ? kHeadroomE4m3 : kHeadroom) : m_ref;
           sh.m[b][row] = m_new;
           __syncwarp();
           if (lane == 0) mbar_arrive(&sh.m_ready[b][quarter]);
@@ -859,25 +874,28 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
         bool again = false;
 #pragma unroll 1
         do {
-          neg_m2 = pack_f32x2(-m_ref, -m_ref);
+          neg_m2 = pack_f32x2(shift - m_ref, shift - m_ref);
           sums[0] = sums[1] = 0ull;
-          exp32(&s[0], c2, neg_m2, &pk[0], sums);
-          const float x_max = fmaxf(max64(&s[0]), max64(&s[64])) * c;
+          exp32<E4m3>(&s[0], c2, neg_m2, &pk[0], sums);
+          const float x_max = fmaf(fmaxf(max64(&s[0]), max64(&s[64])), c, shift);
           again = !again && new_reference(x_max);
         } while (__builtin_expect(again, 0));
         const bool p_done = g < 2 || mbar_test_wait(&sh.pv_done[b], ((g - 2) >> 1) & 1);
-        exp32(&s[32], c2, neg_m2, &pk[16], sums);
+        exp32<E4m3>(&s[32], c2, neg_m2, &pk[16], sums);
         if (__builtin_expect(!__all_sync(0xffffffffu, p_done), 0)) wait(&sh.pv_done[b], ((g - 2) >> 1) & 1);
         tc_fence_after();
         tmem_st32(p_at, pk);
-        exp32(&s[64], c2, neg_m2, &pk[0], sums);
-        exp32(&s[96], c2, neg_m2, &pk[16], sums);
+        exp32<E4m3>(&s[64], c2, neg_m2, &pk[0], sums);
+        exp32<E4m3>(&s[96], c2, neg_m2, &pk[16], sums);
         tmem_st32(p_at + 32, pk);
         float s0, s1, s2, s3;
         unpack_f32x2(sums[0], s0, s1);
         unpack_f32x2(sums[1], s2, s3);
-        l_run += (s0 + s1) + (s2 + s3);
-        if (h >= n_steps - 3) sh.l[nt & 3][w][row] = make_float2(l_run, m_ref);
+        l_run = E4m3 ? fmaf((s0 + s1) + (s2 + s3), l_factor, l_run) : l_run + ((s0 + s1) + (s2 + s3));
+        if (h >= n_steps - 3) {
+          sh.l[nt & 3][w][row] = make_float2(l_run, m_ref);
+          if (E4m3) sh.first_top[nt & 3] = first_top;
+        }
         if (!ok) break;
         if (__builtin_expect(moved && h > 0, 0)) {
           why = kRescale;
@@ -935,7 +953,11 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
         if (!wait(&sh.o_full[q_buf], ((nt - 1) >> 1) & 1)) break;
         tc_fence_after();
         const float2 last = sh.l[(nt - 1) & 3][w_last][row], other = sh.l[(nt - 1) & 3][w_last ^ 1][row];
-        float l = last.x + other.x * ex2(other.y - last.y), m = last.y;
+        float l = last.x + other.x * ex2(other.y - last.y), m = last.y, o_factor = 1.f;
+        if (E4m3) {  // O and the row's sum in one unit: m less by E of the first step
+          o_factor = cache_scale(sh.first_top[(nt - 1) & 3]);
+          m -= (float)(sh.first_top[(nt - 1) & 3] - 127);
+        }
         const int n_rows = to.t.tokens * p.G;
         const bool whole = to.a == 0 && to.b == to.t.steps;
         const uint32_t out = smem_u32(smem + L::kOffQ + q_buf * kTileBytes + quarter * (kTileBytes / 4));  // the place of its Q: 32 rows a warp
@@ -954,8 +976,8 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
               float a0, a1, a2, a3;
               unpack_f32x2(mul_f32x2(pack_f32x2(__uint_as_float(v[i * 8 + 2 * k]), __uint_as_float(v[i * 8 + 2 * k + 1])), inv2), a0, a1);
               unpack_f32x2(mul_f32x2(pack_f32x2(__uint_as_float(v[i * 8 + 2 * k + 2]), __uint_as_float(v[i * 8 + 2 * k + 3])), inv2), a2, a3);
-              x[k] = E4m3 ? pack_bf16x2(a0, a2) : pack_bf16x2(a0, a1);  // (converted values: dims 0, 2, 1, 3 of four)
-              x[k + 1] = E4m3 ? pack_bf16x2(a1, a3) : pack_bf16x2(a2, a3);
+              x[k] = pack_bf16x2(a0, a1);
+              x[k + 1] = pack_bf16x2(a2, a3);
             }
             if (none) x[0] = x[1] = x[2] = x[3] = 0u;
             sts_u4(out + half * (kTileBytes / 8) + lane * 128 + ((i ^ (lane & 7)) << 4), make_uint4(x[0], x[1], x[2], x[3]));
@@ -970,12 +992,13 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
           tmem_wait_ld();
           if (half == 1) arrive(&sh.o_free);
           if (whole) {
-            stage(v, half, inv);
+            stage(v, half, inv * o_factor);
           } else if (row < n_rows) {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
               __stcg(&p.parts[((size_t)slot * 32 + half * 16 + i) * 128 + row],
-                     make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3])));
+                     make_float4(__uint_as_float(v[4 * i]) * o_factor, __uint_as_float(v[4 * i + 1]) * o_factor, __uint_as_float(v[4 * i + 2]) * o_factor,
+                                 __uint_as_float(v[4 * i + 3]) * o_factor));
           }
         }
         bool write = whole;
