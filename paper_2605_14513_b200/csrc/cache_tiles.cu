@@ -69,7 +69,7 @@ template <bool E4m3>
 struct Layout {
   static constexpr int kThreads = E4m3 ? 512 : 384;
   static constexpr int kRegsSoftmax = E4m3 ? 184 : 224, kRegsHelper = E4m3 ? 64 : 56, kRegsConvert = 80;  // sums: the registers at launch
-  static constexpr int kReaders = 11;  // of announced parts: softmax warps, issuers, V producer
+  static constexpr int kReaders = E4m3 ? 15 : 11;  // of announced parts: softmax warps, issuers, V producer, converters
   static constexpr int kKey = E4m3 ? kCodeBytes : kTileBytes;
   // Q, K, V (of which the products read), codes of V
   static constexpr int kOffQ = 0, kOffK = 2 * kTileBytes, kOffV = kOffK + 2 * kKey, kOffCodes = kOffV + 2 * kTileBytes;
@@ -96,9 +96,9 @@ struct TileShared {
   alignas(16) float k_scale[8][128];  // e4m3, by g & 7
   uint8_t v_scale[8][128];            // scale bytes, 0: nothing
   int first_top[4];                   // the largest one of the first step, per part & 3
-  alignas(16) int v_top[8][4];        // the largest of 32 keys each
+  int top[8];                         // the largest
   float q_scale[2][128];     // e4m3: what the scores of a row are to be multiplied by
-  alignas(16) uint32_t bad[8][4];  // keys that are not finite (bf16: of masked steps), by g & 7: written ahead by two steps at most, read before P_g is
+  alignas(16) uint32_t bad[8][4];  // keys that are not finite (bf16: of masked steps), by g & 7
   uint32_t tmem_base;
   int last[2];
   int abort;
@@ -180,11 +180,6 @@ __device__ __forceinline__ uint4 lds_u4(uint32_t addr) {
 }
 __device__ __forceinline__ void sts_u4(uint32_t addr, uint4 v) {
   asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
-}
-// The largest scale byte of a step (that of the smallest scale where there is no value).
-__device__ __forceinline__ int top_scale(const int (&top)[4]) {
-  const int4 x = *reinterpret_cast<const int4 *>(top);
-  return max(max(max(x.x, x.y), max(x.z, x.w)), 17);
 }
 __device__ __forceinline__ bool not_finite(uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
 
@@ -300,7 +295,7 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
     }
     mbar_init(&sh.o_free, 4);
     for (int i = 0; i < kSteps; ++i) mbar_init(&sh.step_full[i], 1);
-    for (int i = 0; i < 8; ++i) mbar_init(&sh.scales_full[i], 4);
+    for (int i = 0; i < 8; ++i) mbar_init(&sh.scales_full[i], 1);
     sh.abort = 0;
     mbar_fence_init();
   }
@@ -497,8 +492,56 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
       settle_pair(sh.q_full, n + 1);
     }
   } else if (warp == kWarpV) {
-    // ===== V producer
-    int g = 0;
+    // ===== V producer; e4m3: the scales of a step's tokens too, asked for and told of two steps ahead
+    int g = 0, asked = 0;
+    bool ended = !E4m3;
+    uint32_t kb = 0, vb = 0;  // scale bytes of keys 4 * lane .. 4 * lane + 3, 127 where there are none
+    auto ask = [&]() {
+      if (ended || !wait(&sh.step_full[asked % kSteps], (asked / kSteps) & 1)) return;
+      const Step &y = sh.step[asked % kSteps];
+      if (y.flags & kStepEnd) {
+        ended = true;
+        return;
+      }
+      const int page = y.page[(lane * 4) >> page_log2];
+      kb = vb = 0x7f7f7f7fu;
+      if (lane * 4 < y.keys && page < ix.n_pages) {
+        const size_t from = (((size_t)page * p.Hkv + y.h) << page_log2) + ((y.key + lane * 4) & ((1 << page_log2) - 1));
+        kb = __ldcg(reinterpret_cast<const uint32_t *>(p.k_scale + from));
+        vb = __ldcg(reinterpret_cast<const uint32_t *>(p.v_scale + from));
+      }
+    };
+    auto tell = [&]() {
+      if (ended || !ok) return;
+      const int keys = sh.step[asked % kSteps].keys - lane * 4;
+      float f[4];
+      uint32_t bad = 0u, top = 0u;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t k = (kb >> (8 * j)) & 255u, v = (vb >> (8 * j)) & 255u;
+        f[j] = k == 255u ? 1.f : cache_scale(k);  // (more than 0: hidden scores of -inf stay -inf)
+        if (k == 255u || v == 255u) bad |= 1u << j;
+        if (v == 255u || j >= keys) vb &= ~(255u << (8 * j));  // (nothing)
+        top = max(top, (vb >> (8 * j)) & 255u);
+      }
+      *reinterpret_cast<float4 *>(&sh.k_scale[asked & 7][lane * 4]) = make_float4(f[0], f[1], f[2], f[3]);
+      *reinterpret_cast<uint32_t *>(&sh.v_scale[asked & 7][lane * 4]) = vb;
+      top = __reduce_max_sync(0xffffffffu, top);
+      if (__any_sync(0xffffffffu, bad != 0u)) {  // a bit a key: eight lanes a word
+        bad <<= 4 * (lane & 7);
+#pragma unroll
+        for (int o = 1; o < 8; o <<= 1) bad |= __shfl_xor_sync(0xffffffffu, bad, o);
+      }
+      if ((lane & 7) == 0) sh.bad[asked & 7][lane >> 3] = bad;
+      if (lane == 0) sh.top[asked & 7] = max((int)top, 17);  // (where there is no value, the smallest scale's)
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.scales_full[asked & 7]);
+      ++asked;
+    };
+    for (int i = 0; i < 2; ++i) {
+      ask();
+      tell();
+    }
 #pragma unroll 1
     for (int n = 0; ok; ++n) {
       const Part *x = part_at(n);
@@ -508,12 +551,14 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
 #pragma unroll 1
       for (int i = 0; i < n_steps; ++i, ++g) {
         const int at = g & 1;
-        if (!wait(&sh.step_full[g % kSteps], (g / kSteps) & 1)) break;
+        if (!E4m3 && !wait(&sh.step_full[g % kSteps], (g / kSteps) & 1)) break;
+        if (E4m3) ask();
         const Step &y = sh.step[g % kSteps];
         const int page = y.page[lane & 7], h = y.h;
         const bool masked = y.flags & kStepMasked;
         if (g >= 2 && !wait(E4m3 ? &sh.codes_free[at] : &sh.pv_done[at], ((g - 2) >> 1) & 1)) break;
         load_pages(smem + (E4m3 ? L::kOffCodes : L::kOffV) + at * L::kKey, &map_v, &sh.v_full[at], h, page);
+        if (E4m3) tell();
         if (!E4m3) {
           if (masked) {
             if (!wait(&sh.v_full[at], (g >> 1) & 1)) {
@@ -617,43 +662,10 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
     }
     drain_products(leader, &sh.drain[1]);
   } else if (warp >= kWarpConvert) {
-    // ===== converters (e4m3): a thread a row of Q, a key of V.  Scales are asked for and made known two steps ahead.
+    // ===== converters (e4m3): a thread a row of Q, a key of V.  (Little besides the conversion itself: asked for here, the scales took 800
+    // clocks a step, of 3300.)
     const int r = tid - kWarpConvert * 32;
     uint32_t n = 0;
-    bool ended = false;  // there is no step `asked`
-    uint32_t asked = 0;
-    uint32_t kb = 127u, vb = 127u;
-    auto ask = [&]() {  // the scale bytes of step `asked`
-      if (ended || !wait(&sh.step_full[asked % kSteps], (asked / kSteps) & 1)) return;
-      const Step &y = sh.step[asked % kSteps];
-      if (y.flags & kStepEnd) {
-        ended = true;
-        return;
-      }
-      const int page = y.page[r >> page_log2];
-      kb = vb = 127u;
-      if (r < y.keys && page < ix.n_pages) {
-        const size_t at = (((size_t)page * p.Hkv + y.h) << page_log2) + ((y.key + r) & ((1 << page_log2) - 1));
-        kb = __ldcg(p.k_scale + at);
-        vb = __ldcg(p.v_scale + at);
-      }
-    };
-    auto tell = [&]() {  // and as numbers, with the tokens that have none
-      if (ended || !ok) return;
-      const bool bad = kb == 255u || vb == 255u, there = r < sh.step[asked % kSteps].keys;
-      sh.k_scale[asked & 7][r] = kb == 255u ? 1.f : cache_scale(kb);  // (more than 0: hidden scores of -inf stay -inf)
-      const uint32_t v = vb == 255u || !there ? 0u : vb;
-      sh.v_scale[asked & 7][r] = (uint8_t)v;
-      const uint32_t top = __reduce_max_sync(0xffffffffu, v);
-      const uint32_t all = __ballot_sync(0xffffffffu, bad);
-      if (lane == 0) {
-        sh.bad[asked & 7][warp - kWarpConvert] = all;
-        sh.v_top[asked & 7][warp - kWarpConvert] = (int)top;
-      }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&sh.scales_full[asked & 7]);
-      ++asked;
-    };
     // Q: q = 2^k (high + low), codes of both; the row's place in the first half holds the high parts, in the second the low ones
     auto split_queries = [&]() {
       if (!wait(&sh.q_full[n & 1], (n >> 1) & 1)) return;
@@ -689,22 +701,25 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
       if (lane == 0) mbar_arrive(&sh.q_ready[n & 1]);
       ++n;
     };
-    // (g runs from -2 on: the first steps' scales and queries, before any values)
+    int next_start = 0;  // first step of part n
+    bool ended = false;
+    // (g runs from -1 on: the queries of a part come two steps ahead of its values)
 #pragma unroll 1
-    for (int g = -2; ok; ++g) {
-      ask();  // step g + 2
+    for (int g = -1; ok; ++g) {
       if (g >= 0) {
-        if (g >= (int)asked && ended) break;  // (steps are asked for ahead: all told of are done)
+        if (g >= next_start) break;  // (the end: parts are taken ahead)
         const uint32_t b = g & 1;
-        if (!wait(&sh.v_full[b], (g >> 1) & 1)) break;
+        const bool v_there = mbar_test_wait(&sh.v_full[b], (g >> 1) & 1), p_there = g < 2 || mbar_test_wait(&sh.pv_done[b], ((g - 2) >> 1) & 1);
+        if (!__all_sync(0xffffffffu, v_there && p_there)) {
+          if (!wait(&sh.v_full[b], (g >> 1) & 1)) break;
+          if (g >= 2 && !wait(&sh.pv_done[b], ((g - 2) >> 1) & 1)) break;
+        }
         const uint32_t from = smem_u32(smem + L::kOffCodes + b * kCodeBytes) + r * 128;
         const uint32_t to = smem_u32(smem + L::kOffV + b * kTileBytes) + r * 128;
-        if (!wait(&sh.scales_full[g & 7], (g >> 3) & 1)) break;  // (the other warps' largest scales)
         const int vs = sh.v_scale[g & 7][r];
-        const float f = vs == 0 ? 0.f : cache_scale(max(vs - top_scale(sh.v_top[g & 7]) + 127, 1));
+        const float f = vs == 0 ? 0.f : cache_scale(max(vs - sh.top[g & 7] + 127, 1));
         const uint32_t f2 = pack_f16x2(f, f);
-        if (g >= 2 && !wait(&sh.pv_done[b], ((g - 2) >> 1) & 1)) break;
-#pragma unroll 2
+#pragma unroll 4
         for (int j = 0; j < 8; ++j) {  // 16 dims
           const uint4 w = lds_u4(from + (((j ^ r) & 7) << 4));
           const uint32_t half = to + (j >> 2) * (kTileBytes / 2);
@@ -720,9 +735,14 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
           mbar_arrive(&sh.codes_free[b]);
         }
       }
-      tell();
-      // the queries of the part that starts there
-      if (g + 2 < (int)asked && (sh.step[(g + 2) % kSteps].flags & kStepStarts)) split_queries();
+      while (ok && !ended && next_start <= g + 2) {
+        const Part *x = part_at(n);
+        ended = x == nullptr || x->b < 0;
+        if (ended) break;
+        next_start += x->b - x->a;
+        done_with_part(n);
+        split_queries();
+      }
     }
   } else {
     // ===== softmax / correction / output: thread = one row
@@ -826,8 +846,8 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
         float shift = 0.f, l_factor = 1.f;  // e4m3: E of the step, 2^(E of the part's first step - E)
         if (E4m3) {
           c = sh.q_scale[nt & 1][row];
-          if (h < 2) first_top = top_scale(sh.v_top[g0 & 7]);
-          const int top = top_scale(sh.v_top[g & 7]);
+          if (h < 2) first_top = sh.top[g0 & 7];
+          const int top = sh.top[g & 7];
           shift = (float)(top - 127);
           l_factor = cache_scale(min(max(first_top - top + 127, 1), 254));
         }
