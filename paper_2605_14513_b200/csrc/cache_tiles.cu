@@ -492,7 +492,7 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
       settle_pair(sh.q_full, n + 1);
     }
   } else if (warp == kWarpV) {
-    // ===== V producer; e4m3: the scales of a step's tokens too, asked for and told of two steps ahead
+    // ===== V producer; e4m3: the scales of a step's tokens too, told of two steps ahead, asked for three
     int g = 0, asked = 0;
     bool ended = !E4m3;
     uint32_t kb = 0, vb = 0;  // scale bytes of keys 4 * lane .. 4 * lane + 3, 127 where there are none
@@ -542,6 +542,7 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
       ask();
       tell();
     }
+    ask();
 #pragma unroll 1
     for (int n = 0; ok; ++n) {
       const Part *x = part_at(n);
@@ -552,13 +553,15 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
       for (int i = 0; i < n_steps; ++i, ++g) {
         const int at = g & 1;
         if (!E4m3 && !wait(&sh.step_full[g % kSteps], (g / kSteps) & 1)) break;
-        if (E4m3) ask();
         const Step &y = sh.step[g % kSteps];
         const int page = y.page[lane & 7], h = y.h;
         const bool masked = y.flags & kStepMasked;
         if (g >= 2 && !wait(E4m3 ? &sh.codes_free[at] : &sh.pv_done[at], ((g - 2) >> 1) & 1)) break;
         load_pages(smem + (E4m3 ? L::kOffCodes : L::kOffV) + at * L::kKey, &map_v, &sh.v_full[at], h, page);
-        if (E4m3) tell();
+        if (E4m3) {
+          tell();  // of step g + 2
+          ask();
+        }
         if (!E4m3) {
           if (masked) {
             if (!wait(&sh.v_full[at], (g >> 1) & 1)) {
@@ -719,8 +722,8 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
         const int vs = sh.v_scale[g & 7][r];
         const float f = vs == 0 ? 0.f : cache_scale(max(vs - sh.top[g & 7] + 127, 1));
         const uint32_t f2 = pack_f16x2(f, f);
-#pragma unroll 4
-        for (int j = 0; j < 8; ++j) {  // 16 dims
+#pragma unroll 1
+        for (int j = 0; j < 8; ++j) {  // 16 dims (instructions are what is short: 12 x 4680 over 12.7k 387 us, unrolled by 2, 4 and 8 399, 420 and 453)
           const uint4 w = lds_u4(from + (((j ^ r) & 7) << 4));
           const uint32_t half = to + (j >> 2) * (kTileBytes / 2);
           sts_u4(half + ((((j & 3) * 2) ^ (r & 7)) << 4), make_uint4(mul_f16x2(codes_to_f16x2(w.x), f2), mul_f16x2(high_codes_to_f16x2(w.x), f2),

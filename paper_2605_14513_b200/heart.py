@@ -7,6 +7,7 @@ fails loudly if it has not been built -- there is no CPU or eager fallback.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 import torch
@@ -281,6 +282,7 @@ class Cache:
                 raise ValueError(f"scales have to be contiguous uint8 {shape} beside the pools: got {x.dtype} {tuple(x.shape)}")
         self.device = self.k.get_device()
         self.struct = CacheStruct(*(None if x is None else x.data_ptr() for x in (self.k, self.v, self.k_scale, self.v_scale)))
+        self.ref = C.byref(self.struct)
 
 
 def cache_workspace_bytes(cfg: CacheConfig) -> int:
@@ -294,52 +296,62 @@ def new_cache_workspace(cfg: CacheConfig, device="cuda") -> torch.Tensor:
     return torch.zeros(n, dtype=torch.uint8, device=device)
 
 
-def _cache_call(cfg, cache, rows, heads, strides, tensors, page_table, row_start, kv_len, ws):
-    """Checks what the library cannot see (types, sizes, devices); rows: the number of rows of the packed `tensors`."""
-    device = cache.device
+@functools.lru_cache(maxsize=256)
+def _cache_workspace_bytes(S, T, Hq, Hkv):
+    """What the size of a workspace goes by."""
+    return cache_workspace_bytes(make_cache_config(S, T, Hq, Hkv, 64, 1, 1))
+
+
+def _cache_call(cfg, cache, heads, stride, tensors, page_table, row_start, kv_len, ws):
+    """Checks what the library cannot see (types, sizes, devices).  heads, stride: of the packed `tensors`."""
+    device, S, T = cache.device, cfg.S, cfg.T
+    n = T * heads * 128
     for x in tensors:
-        if x.dtype != torch.bfloat16 or x.numel() != rows * heads * 128 or x.get_device() != device or x.stride(-1) != 1:
-            raise ValueError(f"packed tensors have to be bf16, {rows} rows x {heads} heads x 128, beside the cache: got {x.dtype} {tuple(x.shape)} on {x.device}")
-        if strides == (0, 0) and not x.is_contiguous():
-            raise ValueError(f"a packed tensor that is not contiguous needs its strides in the config: got {tuple(x.shape)}, strides {x.stride()}")
-    for x, n in ((page_table, cfg.S * cfg.table_stride), (row_start, cfg.S + 1), (kv_len, cfg.S)):
-        if x.dtype != torch.int32 or x.numel() != n or x.get_device() != device or not x.is_contiguous():
-            raise ValueError(f"page_table, row_start and kv_len have to be contiguous int32 of {cfg.S} x {cfg.table_stride}, {cfg.S + 1} and {cfg.S} "
+        if x.dtype is not torch.bfloat16 or x.numel() != n or x.get_device() != device or not (x.is_contiguous() or stride and x.stride(-1) == 1):
+            raise ValueError(f"packed tensors have to be bf16, {T} rows x {heads} heads x 128, beside the cache, contiguous or with their strides in the "
+                             f"config: got {x.dtype} {tuple(x.shape)}, strides {x.stride()}, on {x.device}")
+    for x, n in ((page_table, S * cfg.table_stride), (row_start, S + 1), (kv_len, S)):
+        if x.dtype is not torch.int32 or x.numel() != n or x.get_device() != device or not x.is_contiguous():
+            raise ValueError(f"page_table, row_start and kv_len have to be contiguous int32 of {S} x {cfg.table_stride}, {S + 1} and {S} "
                              f"entries beside the cache: got {x.dtype} {tuple(x.shape)} on {x.device}")
-    if ws.get_device() != device or ws.numel() * ws.element_size() < cache_workspace_bytes(cfg):
+    if ws.get_device() != device or ws.numel() * ws.element_size() < _cache_workspace_bytes(S, T, cfg.Hq, cfg.Hkv):
         raise ValueError(f"the workspace has to have cache_workspace_bytes(cfg) = {cache_workspace_bytes(cfg)} bytes beside the cache")
 
 
-def _on(device, call, *args):
-    """The call on the current stream of the tensors' device."""
-    if device == torch.cuda.current_device():
-        return _check(call(*args, _stream()))
-    with torch.cuda.device(device):
-        return _check(call(*args, _stream()))
+def _cache_launch(call, cache, *args):
+    """The call on the current stream of the cache's device."""
+    device = cache.device
+    if device == torch._C._cuda_getDevice():
+        rc = call(*args, torch._C._cuda_getCurrentRawStream(device))
+    else:
+        with torch.cuda.device(device):
+            rc = call(*args, torch._C._cuda_getCurrentRawStream(device))
+    if rc != OK:
+        raise HeartError(rc)
 
 
 def heart_cache_write(cfg, K, V, cache: Cache, page_table, row_start, kv_len, ws):
     """Stores the packed rows of K and V (bf16 [T, Hkv, D]), the last tokens of their sequences, in their pages."""
-    _cache_call(cfg, cache, cfg.T, cfg.Hkv, (cfg.kv_stride_t, cfg.kv_stride_h), (K, V), page_table, row_start, kv_len, ws)
-    _on(cache.device, lib().heart_cache_write, C.byref(cfg), _ptr(K), _ptr(V), C.byref(cache.struct), _ptr(page_table), _ptr(row_start),
-        _ptr(kv_len), _ptr(ws))
+    _cache_call(cfg, cache, cfg.Hkv, cfg.kv_stride_t, (K, V), page_table, row_start, kv_len, ws)
+    _cache_launch(lib().heart_cache_write, cache, C.byref(cfg), K.data_ptr(), V.data_ptr(), cache.ref, page_table.data_ptr(), row_start.data_ptr(),
+                  kv_len.data_ptr(), ws.data_ptr())
 
 
 def heart_cache_read(cfg, cache: Cache, page_table, row_start, kv_len, K_out, V_out, ws):
     """The last tokens of the sequences out of their pages into the packed rows of K_out and V_out (bf16 [T, Hkv, D])."""
-    _cache_call(cfg, cache, cfg.T, cfg.Hkv, (cfg.kv_stride_t, cfg.kv_stride_h), (K_out, V_out), page_table, row_start, kv_len, ws)
-    _on(cache.device, lib().heart_cache_read, C.byref(cfg), C.byref(cache.struct), _ptr(page_table), _ptr(row_start), _ptr(kv_len),
-        _ptr(K_out), _ptr(V_out), _ptr(ws))
+    _cache_call(cfg, cache, cfg.Hkv, cfg.kv_stride_t, (K_out, V_out), page_table, row_start, kv_len, ws)
+    _cache_launch(lib().heart_cache_read, cache, C.byref(cfg), cache.ref, page_table.data_ptr(), row_start.data_ptr(), kv_len.data_ptr(),
+                  K_out.data_ptr(), V_out.data_ptr(), ws.data_ptr())
 
 
 def heart_cache_attn(cfg, Q, cache: Cache, page_table, row_start, kv_len, O, ws, lse=None):
     """Attention of the packed rows of Q (bf16 [T, Hq, D]), the last tokens of their sequences, over the sequences' pages
     into O; lse: optional fp32 [T, Hq]."""
-    _cache_call(cfg, cache, cfg.T, cfg.Hq, (cfg.q_stride_t, cfg.q_stride_h), (Q, O), page_table, row_start, kv_len, ws)
-    if lse is not None and (lse.dtype != torch.float32 or lse.numel() != cfg.T * cfg.Hq or lse.get_device() != cache.device or not lse.is_contiguous()):
+    _cache_call(cfg, cache, cfg.Hq, cfg.q_stride_t, (Q, O), page_table, row_start, kv_len, ws)
+    if lse is not None and (lse.dtype is not torch.float32 or lse.numel() != cfg.T * cfg.Hq or lse.get_device() != cache.device or not lse.is_contiguous()):
         raise ValueError(f"lse has to be contiguous fp32 [{cfg.T}, {cfg.Hq}] beside the cache: got {lse.dtype} {tuple(lse.shape)} on {lse.device}")
-    _on(cache.device, lib().heart_cache_attn, C.byref(cfg), _ptr(Q), C.byref(cache.struct), _ptr(page_table), _ptr(row_start), _ptr(kv_len),
-        _ptr(O), _ptr(lse), _ptr(ws))
+    _cache_launch(lib().heart_cache_attn, cache, C.byref(cfg), Q.data_ptr(), cache.ref, page_table.data_ptr(), row_start.data_ptr(), kv_len.data_ptr(),
+                  O.data_ptr(), _ptr(lse), ws.data_ptr())
 
 
 def heart_full_token_drift(cfg, Qa, Ka, Qb, Kb, drift_out, ws):
