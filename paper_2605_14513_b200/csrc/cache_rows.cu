@@ -33,7 +33,8 @@ namespace {
 constexpr int kWarps = 8, kThreads = 32 * kWarps;
 constexpr int kRing = 24576;           // bytes a warp
 constexpr int kMaxStages = 6;
-constexpr int kMaxParts = 32;          // of a tile, about: the last CTA reads them all
+constexpr int kMaxParts = 31;          // of a tile, and one more where shares cross tiles: the last CTA reads them, a lane a part
+constexpr int kApartRows = 6;          // rows of a tile whose sums have a place beside the rings
 constexpr float kNoReference = -3.0e38f;
 constexpr float kMaxGrowth = 8.f;      // log2: the reference of a row moves when a maximum exceeds it by more
 constexpr float kHeadroomE4m3 = 6.f;   // log2 of the largest weight when the reference has moved
@@ -59,7 +60,7 @@ struct RowsParams {
   float2 *part_l;
 };
 
-struct RowsShared {
+struct alignas(16) RowsShared {
   uint64_t full[kWarps][kMaxStages];
   alignas(16) uint8_t scales[kWarps][kMaxStages][64];  // e4m3: of the keys and of the values of a stage
   alignas(16) float k_factor[kWarps][32];   // e4m3: what the scores of a warp's keys are to be multiplied by,
@@ -73,7 +74,8 @@ struct RowsShared {
   int last;
   int abort;
 };
-constexpr int kRowsSmem = kWarps * kRing + sizeof(RowsShared);
+constexpr int kRowsSmem = kWarps * kRing + sizeof(RowsShared) + kWarps * kApartRows * 512;
+static_assert(kRowsSmem <= 232448 && sizeof(RowsShared) % 16 == 0, "shared memory of an SM");
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -126,6 +128,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_fence_init();
   }
   if (tid == 0) sh.abort = 0;
+  __syncthreads();
   pdl_wait();
   pdl_launch_dependents();
 
@@ -137,146 +140,204 @@ __global__ void __launch_bounds__(kThreads, 1)
   };
   auto steps_of = [&](const Sequence &q, int &longest) -> long long {  // of one head
     long long n = 0;
-    for (int t = 0; t < tiles_of(q); ++t) {
+    const int tiles = tiles_of(q);
+    for (int t = 0; t < tiles; ++t) {
       const int k = span(q, t).steps;
       n += k;
       longest = max(longest, k);
     }
     return n;
   };
-  long long total = 0, mine = 0;
+  auto quotient = [](long long a, long long b) -> long long {  // (of numbers that fit 32 bits as a rule: a tenth of the time)
+    return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
+  };
   Sequence q = {0, 0, 0};
-  int longest = 1;
-  for (int s = tid; s < ix.S; s += kThreads) {
-    const Sequence x = sequence(ix, s);
-    const long long n = steps_of(x, longest);
-    if (s < kThreads) mine = n, q = x;
-    total += n * p.Hkv;
-  }
+  int s, longest = 1;
+  long long share, u, u1, sequence_at, per_head;  // units of a CTA, its first one and the one behind its last; of the sequence, and of one of its heads
+  bool one_tile = false;                          // shares do not cross tiles
+  if (ix.S <= 32) {
+    // every warp by itself, a lane a sequence
+    if (lane < ix.S) q = sequence(ix, lane);
+    per_head = steps_of(q, longest);
+    longest = __reduce_max_sync(0xffffffffu, longest);
+    auto before_lane = [&](long long x, long long &all) {
+      const long long mine = x;
 #pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    total += __shfl_xor_sync(0xffffffffu, total, o);
-    longest = max(longest, __shfl_xor_sync(0xffffffffu, longest, o));
-  }
-  if (lane == 0) {
-    sh.total[warp] = total;
-    sh.longest[warp] = longest;
-  }
-  __syncthreads();
-  total = 0;
-#pragma unroll
-  for (int i = 0; i < kWarps; ++i) {
-    total += sh.total[i];
-    longest = max(longest, sh.longest[i]);
-  }
-  const long long share = max((total + gridDim.x - 1) / gridDim.x, (long long)(longest + kMaxParts - 1) / kMaxParts);
-  const long long u0 = blockIdx.x * share, u1 = min(total, u0 + share);
-  if (u0 >= u1) return;
-  long long before = 0;  // steps before the sequences of this round
-  for (int base = 0; base < ix.S; base += kThreads) {
-    int dummy = 0;
-    if (base > 0) {
-      q = base + tid < ix.S ? sequence(ix, base + tid) : Sequence{0, 0, 0};
-      mine = steps_of(q, dummy);
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+      }
+      all = __shfl_sync(0xffffffffu, x, 31);
+      return x - mine;
+    };
+    long long total;
+    sequence_at = before_lane(per_head * p.Hkv, total);
+    share = max(quotient(total + gridDim.x - 1, gridDim.x), (long long)(longest + kMaxParts - 1) / kMaxParts);
+    // Where each sequence and head is one tile and CTAs are enough, tiles begin with a share (a CTA with the end of one and the beginning of
+    // another takes twice as long as the others: 8 heads x 4100 tokens).
+    if (total < (1 << 20) && __all_sync(0xffffffffu, per_head == 0 || tiles_of(q) == 1)) {
+      const int steps = (int)per_head;
+      for (int more = 0; more <= (int)share / 4 + 1 && !one_tile; ++more) {
+        const int sh1 = (int)share + more, parts = (steps + sh1 - 1) / sh1;
+        if (__reduce_add_sync(0xffffffffu, parts * p.Hkv) <= (int)gridDim.x) {
+          one_tile = true;
+          share = sh1;
+          per_head = (long long)parts * sh1;
+        }
+      }
+      if (one_tile) sequence_at = before_lane(per_head * p.Hkv, total);
     }
-    long long upto = mine * p.Hkv;
+    u = blockIdx.x * share;
+    u1 = min(total, u + share);
+    if (u >= u1) return;
+    const uint32_t here = __ballot_sync(0xffffffffu, sequence_at <= u && u < sequence_at + per_head * p.Hkv);
+    s = __ffs(here) - 1;
+    q = {__shfl_sync(0xffffffffu, q.row, s), __shfl_sync(0xffffffffu, q.n, s), __shfl_sync(0xffffffffu, q.len, s)};
+    sequence_at = __shfl_sync(0xffffffffu, sequence_at, s);
+    per_head = __shfl_sync(0xffffffffu, per_head, s);
+  } else {
+    long long total = 0, mine = 0;
+    for (int i = tid; i < ix.S; i += kThreads) {
+      const Sequence x = sequence(ix, i);
+      const long long n = steps_of(x, longest);
+      if (i < kThreads) mine = n, q = x;
+      total += n * p.Hkv;
+    }
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long x = __shfl_up_sync(0xffffffffu, upto, o);
-      if (lane >= o) upto += x;
+    for (int o = 16; o; o >>= 1) {
+      total += __shfl_xor_sync(0xffffffffu, total, o);
+      longest = max(longest, __shfl_xor_sync(0xffffffffu, longest, o));
+    }
+    if (lane == 0) {
+      sh.total[warp] = total;
+      sh.longest[warp] = longest;
     }
     __syncthreads();
-    if (lane == 31) sh.total[warp] = upto;
-    __syncthreads();
-    long long at = before, all = 0;
+    total = 0;
 #pragma unroll
     for (int i = 0; i < kWarps; ++i) {
-      if (i < warp) at += sh.total[i];
-      all += sh.total[i];
+      total += sh.total[i];
+      longest = max(longest, sh.longest[i]);
     }
-    at += upto - mine * p.Hkv;
-    if (at <= u0 && u0 < at + mine * p.Hkv) {
-      sh.found = base + tid;
-      sh.found_q[0] = q.row, sh.found_q[1] = q.n, sh.found_q[2] = q.len;
-      sh.found_at = at;
-      sh.found_steps = mine;
+    share = max(quotient(total + gridDim.x - 1, gridDim.x), (long long)(longest + kMaxParts - 1) / kMaxParts);
+    u = blockIdx.x * share;
+    u1 = min(total, u + share);
+    if (u >= u1) return;
+    long long before = 0;  // steps before the sequences of this round
+    for (int base = 0; base < ix.S; base += kThreads) {
+      int dummy = 0;
+      if (base > 0) {
+        q = base + tid < ix.S ? sequence(ix, base + tid) : Sequence{0, 0, 0};
+        mine = steps_of(q, dummy);
+      }
+      long long upto = mine * p.Hkv;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long x = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += x;
+      }
+      __syncthreads();
+      if (lane == 31) sh.total[warp] = upto;
+      __syncthreads();
+      long long at = before, all = 0;
+#pragma unroll
+      for (int i = 0; i < kWarps; ++i) {
+        if (i < warp) at += sh.total[i];
+        all += sh.total[i];
+      }
+      at += upto - mine * p.Hkv;
+      if (at <= u && u < at + mine * p.Hkv) {
+        sh.found = base + tid;
+        sh.found_q[0] = q.row, sh.found_q[1] = q.n, sh.found_q[2] = q.len;
+        sh.found_at = at;
+        sh.found_steps = mine;
+      }
+      before += all;
+      if (before > u) break;
     }
-    before += all;
-    if (before > u0) break;
+    __syncthreads();
+    s = sh.found;
+    q = {sh.found_q[0], sh.found_q[1], sh.found_q[2]};
+    sequence_at = sh.found_at;
+    per_head = sh.found_steps;
   }
-  __syncthreads();
-  int s = sh.found, h, t = 0;
-  q = {sh.found_q[0], sh.found_q[1], sh.found_q[2]};
-  long long u = u0;
-  int done;  // steps of the present tile before this share
+  int h, t = 0, done;  // head, tile and the tile's steps before this share
   {
-    long long rest = u0 - sh.found_at;
-    h = (int)(rest / sh.found_steps);
-    rest -= h * sh.found_steps;
-    for (int k; rest >= (k = span(q, t).steps); ++t) rest -= k;
+    long long rest = u - sequence_at;
+    h = (int)quotient(rest, per_head);
+    rest -= h * per_head;
+    if (!one_tile)
+      for (int k; rest >= (k = span(q, t).steps); ++t) rest -= k;
     done = (int)rest;
   }
 
   int put = 0, take = 0;            // the stages that come next, to fill and to use
   uint32_t parity = 0;              // of the barriers of the stages, a bit each, for their next use
+  int in_flight = 0;
   bool ok = true;
   const int g = lane >> 2, c = lane & 3;
-  const int box_log2 = min(ix.page_log2, kKeysLog2), boxes = kKeys >> box_log2;
+  const int box_log2 = min(ix.page_log2, kKeysLog2), boxes_log2 = kKeysLog2 - box_log2, boxes = 1 << boxes_log2;
+  const int batch = 32 >> boxes_log2;  // steps whose entries of the table a warp asks for at once, a lane an entry
 
-  for (;;) {
-    // ---------------------------------------------------------------- a tile, or part of one
-    const Span<kStep> sp = span(q, t);
-    const int first_row = t * kRows, n_rows = min(kRows, (int)((long long)q.n * p.G) - first_row);
-    const int p0 = q.len - q.n + first_row / p.G, p1 = q.len - q.n + (first_row + n_rows - 1) / p.G;
-    const int end_step = (int)min((long long)sp.steps, done + (u1 - u));
-    // keys that some row sees: some_low .. some_end - 1 and the sinks; that every row does: every_low .. every_end - 1 and the sinks
-    int some_low, some_end, every_low, every_end;
-    {
-      const Visible a = visible(ix, max(p0, 0), q.len), b = visible(ix, p1, q.len);
-      some_low = a.low, some_end = b.end;
-      every_low = b.low, every_end = p0 < 0 ? 0 : a.end;
+  // ---------------------------------------------------------------- a tile, or part of one
+  int first_row, n_rows, p0, end_step, steps;
+  int sinks, first;                                 // see Span
+  int some_low, some_end, every_low, every_end;     // keys that some row sees, that every row does (besides the sinks)
+  int next, next_batch, entry, entry_then;          // the warp's next copy; the batch of steps whose entries are in `entry`
+  uint32_t qf[MT][8][4];
+  float row_scale[MT][2];
+  auto some = [&](int k0) { return k0 < some_end && (k0 + kKeys > some_low || k0 < ix.sink); };
+  auto key_of = [&](int i) { return (i < sinks ? i : first + i - sinks) * kStep + warp * kKeys; };
+  auto entries = [&](int at) {  // of the steps from `at` on
+    const int i = at + (lane >> boxes_log2), k = key_of(i) + ((lane & (boxes - 1)) << box_log2);
+    return i < end_step && k < q.len ? page_entry(ix, s, k) : -1;
+  };
+  auto issue = [&]() {
+    while (next < end_step && !some(key_of(next))) ++next;
+    if (next >= end_step) return;
+    while (next >= next_batch + batch) {
+      next_batch += batch;
+      entry = entry_then;
+      entry_then = entries(next_batch + batch);
     }
-    auto some = [&](int k0) { return k0 < some_end && (k0 + kKeys > some_low || k0 < ix.sink); };
-
-    auto key_of = [&](int i) { return (i < sp.sinks ? i : sp.first + i - sp.sinks) * kStep + warp * kKeys; };
-    int next = done - 1, next_key = 0, next_page = 0;  // the warp's next copy: its step and keys, lane i: the table's entry for its box i
-    int in_flight = 0;
-    auto advance = [&]() {
-      do next_key = key_of(++next);
-      while (next < end_step && !some(next_key));
-      const int k = next_key + (lane << box_log2);
-      if (next < end_step && lane < boxes) next_page = k < q.len ? page_entry(ix, s, k) : -1;
-    };
-    auto issue = [&]() {
-      if (next >= end_step) return;
-      uint64_t *bar = &sh.full[warp][put];
-      if (lane == 0) mbar_expect_tx(bar, kStage + (E4m3 ? 2 * kKeys : 0));
-      if (boxes > 1) __syncwarp();
-      if (lane < boxes) {
-        const int slot = next_key & ((1 << ix.page_log2) - 1);
-        const int page = next_key + (lane << box_log2) < q.len ? checked_page(ix, next_page) : ix.n_pages;  // (out of range: zeros)
-        unsigned char *to = ring + put * kStage + (lane << (box_log2 + (E4m3 ? 7 : 8)));
-        tma_load_5d(to, &map_k, bar, 0, slot, 0, h, page);
-        tma_load_5d(to + kHalf, &map_v, bar, 0, slot, 0, h, page);
-        if (E4m3) {
-          const size_t at = (((size_t)min(page, ix.n_pages - 1) * p.Hkv + h) << ix.page_log2) + slot;
-          bulk_load(&sh.scales[warp][put][lane << box_log2], p.k_scale + at, 1 << box_log2, bar);
-          bulk_load(&sh.scales[warp][put][kKeys + (lane << box_log2)], p.v_scale + at, 1 << box_log2, bar);
-        }
+    const int mine = __shfl_sync(0xffffffffu, entry, ((next - next_batch) << boxes_log2) + (lane & (boxes - 1)));
+    uint64_t *bar = &sh.full[warp][put];
+    if (lane == 0) mbar_expect_tx(bar, kStage + (E4m3 ? 2 * kKeys : 0));
+    if (boxes > 1) __syncwarp();
+    if (lane < boxes) {
+      const int k0 = key_of(next), slot = k0 & ((1 << ix.page_log2) - 1);
+      const int page = k0 + (lane << box_log2) < q.len ? checked_page(ix, mine) : ix.n_pages;  // (out of range: zeros)
+      unsigned char *to = ring + put * kStage + (lane << (box_log2 + (E4m3 ? 7 : 8)));
+      tma_load_5d(to, &map_k, bar, 0, slot, 0, h, page);
+      tma_load_5d(to + kHalf, &map_v, bar, 0, slot, 0, h, page);
+      if (E4m3) {
+        const size_t at = (((size_t)min(page, ix.n_pages - 1) * p.Hkv + h) << ix.page_log2) + slot;
+        bulk_load(&sh.scales[warp][put][lane << box_log2], p.k_scale + at, 1 << box_log2, bar);
+        bulk_load(&sh.scales[warp][put][kKeys + (lane << box_log2)], p.v_scale + at, 1 << box_log2, bar);
       }
-      put = put + 1 == kStages ? 0 : put + 1;
-      ++in_flight;
-      advance();
-    };
-    advance();
-#pragma unroll 1
-    for (int i = 0; i < kStages; ++i) issue();
-
+    }
+    put = put + 1 == kStages ? 0 : put + 1;
+    ++in_flight;
+    ++next;
+  };
+  // What the tile needs before its first step, all that comes from memory asked for together; the first copies.
+  auto start = [&]() {
+    const Span<kStep> sp = span(q, t);
+    sinks = sp.sinks, first = sp.first, steps = sp.steps;
+    first_row = t * kRows;
+    n_rows = min(kRows, (int)((long long)q.n * p.G) - first_row);
+    p0 = q.len - q.n + first_row / p.G;
+    const int p1 = q.len - q.n + (first_row + n_rows - 1) / p.G;
+    end_step = (int)min((long long)steps, done + (u1 - u));
+    next = done;
+    next_batch = done;
+    entry = entries(done);
+    entry_then = entries(done + batch);
+    const Visible a = visible(ix, max(p0, 0), q.len), b = visible(ix, p1, q.len);
+    some_low = a.low, some_end = p1 < 0 ? 0 : b.end;
+    every_low = b.low, every_end = p0 < 0 ? 0 : a.end;
     // The rows' queries as operands of the products: this lane's rows g and g + 8 of every 16.  (e4m3: the dims of a product are
-    // those that a lane finds together in a key's row, 32 * c + 4 * step + 0 .. 3.)
-    uint32_t qf[MT][8][4];
-    float row_scale[MT][2];
-    Visible vis[MT][2];
+    // those that a lane finds together in a key's row, 32 * c + 4 * step + 0 .. 3; as bf16 here, made f16 below.)
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -285,29 +346,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         const bool real = row < n_rows;
         const int i = (first_row + row) / p.G, head = h * p.G + (first_row + row) % p.G;
         const uint16_t *src = p.Q + (long long)(q.row + i) * p.qt + head * p.qh;
-        vis[m][r] = real ? visible(ix, q.len - q.n + i, q.len) : Visible{0, 0x7fffffff};
-        row_scale[m][r] = p.scale_log2;
         if (E4m3) {
-          uint4 x[4];
-          uint32_t top = 0u;
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            x[k] = real ? *reinterpret_cast<const uint4 *>(src + c * 32 + k * 8) : make_uint4(0u, 0u, 0u, 0u);
-            top = __vmaxu2(top, __vmaxu2(__vmaxu2(x[k].x & 0x7fff7fffu, x[k].y & 0x7fff7fffu), __vmaxu2(x[k].z & 0x7fff7fffu, x[k].w & 0x7fff7fffu)));
-          }
-          top = max(top & 0xffffu, top >> 16);
-          top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-          top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-          const int e = min(max((int)(top >> 7) - 127 - 14, -100), 120);  // the largest element: 2^14 * 2^e to 2^15 * 2^e
-          const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
-          row_scale[m][r] = top < 0x7f80u ? p.scale_log2 * __uint_as_float((uint32_t)(127 + e) << 23) : __uint_as_float(0x7fc00000u);
-          auto to_f16 = [&](uint32_t w) { return pack_f16x2(__uint_as_float(w << 16) * inv, __uint_as_float(w & 0xffff0000u) * inv); };
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            qf[m][2 * k][r] = to_f16(x[k].x);
-            qf[m][2 * k][2 + r] = to_f16(x[k].y);
-            qf[m][2 * k + 1][r] = to_f16(x[k].z);
-            qf[m][2 * k + 1][2 + r] = to_f16(x[k].w);
+            const uint4 x = real ? *reinterpret_cast<const uint4 *>(src + c * 32 + k * 8) : make_uint4(0u, 0u, 0u, 0u);
+            qf[m][2 * k][r] = x.x;
+            qf[m][2 * k][2 + r] = x.y;
+            qf[m][2 * k + 1][r] = x.z;
+            qf[m][2 * k + 1][2 + r] = x.w;
           }
         } else {
 #pragma unroll
@@ -315,6 +361,40 @@ __global__ void __launch_bounds__(kThreads, 1)
             qf[m][ks][r] = real ? *reinterpret_cast<const uint32_t *>(src + ks * 16 + c * 2) : 0u;
             qf[m][ks][2 + r] = real ? *reinterpret_cast<const uint32_t *>(src + ks * 16 + c * 2 + 8) : 0u;
           }
+        }
+      }
+#pragma unroll 1
+    for (int i = 0; i < kStages; ++i) issue();
+  };
+  start();
+
+  for (;;) {
+    // rows that are none see everything (and nothing of theirs is kept)
+    Visible vis[MT][2];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int row = m * 16 + r * 8 + g;
+        vis[m][r] = row < n_rows ? visible(ix, q.len - q.n + (first_row + row) / p.G, q.len) : Visible{0, 0x7fffffff};
+        row_scale[m][r] = p.scale_log2;
+        if (E4m3) {
+          uint32_t top = 0u;
+#pragma unroll
+          for (int ks = 0; ks < 8; ++ks) top = __vmaxu2(top, __vmaxu2(qf[m][ks][r] & 0x7fff7fffu, qf[m][ks][2 + r] & 0x7fff7fffu));
+          top = max(top & 0xffffu, top >> 16);
+          top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+          top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+          const int e = min(max((int)(top >> 7) - 127 - 14, -100), 120);  // the largest element: 2^14 * 2^e to 2^15 * 2^e
+          const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+          row_scale[m][r] = top < 0x7f80u ? p.scale_log2 * __uint_as_float((uint32_t)(127 + e) << 23) : __uint_as_float(0x7fc00000u);
+#pragma unroll
+          for (int ks = 0; ks < 8; ++ks)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const uint32_t w = qf[m][ks][2 * k + r];
+              qf[m][ks][2 * k + r] = pack_f16x2(__uint_as_float(w << 16) * inv, __uint_as_float(w & 0xffff0000u) * inv);
+            }
         }
       }
     float o[MT][16][4] = {};
@@ -544,9 +624,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         parity ^= 1u << take;
         take = take + 1 == kStages ? 0 : take + 1;
       }
-      next = end_step;
     }
-
     if (E4m3) {
       const float f = cache_scale(v_exp);
 #pragma unroll
@@ -557,6 +635,11 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int k = 0; k < 4; ++k) o[m][n][k] *= f;
     }
     // ---------------------------------------------------------------- the warps' sums put together
+    // A few rows have a place of their own, and the next tile's first copies go out ahead of this; more rows lie where the copies were.
+    // (Pieces of 32 bytes are swizzled by the row.)
+    const bool apart = MT == 1 && n_rows <= kApartRows;
+    unsigned char *sums = apart ? smem + kWarps * kRing + sizeof(RowsShared) : smem;
+    const int sums_pitch = apart ? kApartRows * 512 : kRing;
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -564,34 +647,52 @@ __global__ void __launch_bounds__(kThreads, 1)
         sum[m][r] += __shfl_xor_sync(0xffffffffu, sum[m][r], 1);
         sum[m][r] += __shfl_xor_sync(0xffffffffu, sum[m][r], 2);
         const int row = m * 16 + r * 8 + g;
+        if (row >= n_rows) continue;
         if (c == 0) sh.l[warp][row] = make_float2(sum[m][r], ref[m][r]);
-        float *to = reinterpret_cast<float *>(ring) + row * 128;
+        unsigned char *to = sums + warp * sums_pitch + row * 512;
 #pragma unroll
         for (int n = 0; n < 16; ++n) {
           // dims of these two columns: e4m3 products take even and odd dims of 16 apart
           if (E4m3) {
             if (n & 1) continue;
-            *reinterpret_cast<float4 *>(to + n * 8 + c * 4) =
+            *reinterpret_cast<float4 *>(to + ((n * 32 + c * 16) ^ ((row & 7) << 5))) =
                 make_float4(o[m][n][r * 2], o[m][n + 1][r * 2], o[m][n][r * 2 + 1], o[m][n + 1][r * 2 + 1]);
           } else {
-            *reinterpret_cast<float2 *>(to + n * 8 + c * 2) = make_float2(o[m][n][r * 2], o[m][n][r * 2 + 1]);
+            *reinterpret_cast<float2 *>(to + ((n * 32 + c * 8) ^ ((row & 7) << 5))) = make_float2(o[m][n][r * 2], o[m][n][r * 2 + 1]);
           }
         }
       }
-    __syncthreads();
-    const bool all = done == 0 && end_step == sp.steps;
+    // this tile's, for the rest of it, before the next one's take their places
+    const int rows = n_rows, row0 = first_row, out_row = q.row, out_head = h;
+    const bool all = done == 0 && end_step == steps;
     const long long tile_at = u - done;  // the tile's first step
-    const int c0 = (int)(tile_at / share), c1 = (int)((tile_at + sp.steps - 1) / share);
+    const int tile_steps = steps;
     const int part = 2 * blockIdx.x + (done == 0 ? 1 : 0);
+    u += end_step - done;
+    const bool more = !one_tile && u < u1;
+    if (more) {
+      done = 0;
+      if (++t == tiles_of(q)) {
+        t = 0;
+        if (++h == p.Hkv) {
+          h = 0;
+          do q = sequence(ix, ++s);
+          while (q.n == 0 && s + 1 < ix.S);
+        }
+      }
+      if (apart) start();
+    }
+    __syncthreads();
     auto write_row = [&](int row, int d, float4 v, float l, float m) {  // four dims
       const float inv = l == 0.f ? 0.f : 1.f / l;
-      const int i = (first_row + row) / p.G, head = h * p.G + (first_row + row) % p.G;
-      *reinterpret_cast<uint2 *>(p.O + (long long)(q.row + i) * p.qt + head * p.qh + d) =
+      const int i = (row0 + row) / p.G, head = out_head * p.G + (row0 + row) % p.G;
+      *reinterpret_cast<uint2 *>(p.O + (long long)(out_row + i) * p.qt + head * p.qh + d) =
           make_uint2(pack_bf16x2(v.x * inv, v.y * inv), pack_bf16x2(v.z * inv, v.w * inv));
-      if (d == 0 && p.lse != nullptr) p.lse[(long long)(q.row + i) * p.Hq + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+      if (d == 0 && p.lse != nullptr) p.lse[(long long)(out_row + i) * p.Hq + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
     };
-    for (int row = warp; row < n_rows; row += kWarps) {
-      const int d = lane * 4;
+    const int d = lane * 4;
+#pragma unroll 1
+    for (int row = warp; row < rows; row += kWarps) {
       float m = kNoReference, l = 0.f;
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) m = fmaxf(m, sh.l[w][row].y);
@@ -600,7 +701,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int w = 0; w < kWarps; ++w) {
         const float2 lm = sh.l[w][row];
         const float f = ex2(lm.y - m);
-        const float4 y = *reinterpret_cast<const float4 *>(smem + w * kRing + row * 512 + d * 4);
+        const float4 y = *reinterpret_cast<const float4 *>(sums + w * sums_pitch + row * 512 + ((d * 4) ^ ((row & 7) << 5)));
         l = fmaf(lm.x, f, l);
         v.x = fmaf(y.x, f, v.x);
         v.y = fmaf(y.y, f, v.y);
@@ -616,53 +717,54 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
     }
     if (!all) {
-      __threadfence();
+      const int c0 = (int)quotient(tile_at, share), parts = (int)quotient(tile_at + tile_steps - 1, share) - c0 + 1;
       __syncthreads();
       if (tid == 0) {
-        const bool last = atomicAdd(&p.arrivals[c0], 1) == c1 - c0;
+        __threadfence();  // (of what the CTA has stored before the barrier)
+        const bool last = atomicAdd(&p.arrivals[c0], 1) == parts - 1;
         if (last) p.arrivals[c0] = 0;
         sh.last = last;
         __threadfence();
       }
       __syncthreads();
       if (sh.last) {
-        for (int row = warp; row < n_rows; row += kWarps) {
-          const int d = lane * 4;
+#pragma unroll 1
+        for (int row = warp; row < rows; row += kWarps) {
           auto place = [&](int i) { return (2 * (c0 + i) + (i == 0 ? 1 : 0)) * 128 + row; };
-          float m = kNoReference, l = 0.f;
-          for (int i = lane; i <= c1 - c0; i += 32) m = fmaxf(m, __ldcg(&p.part_l[place(i)]).y);
+          const float2 mine = lane < parts ? __ldcg(&p.part_l[place(lane)]) : make_float2(0.f, kNoReference);  // (at most 32 parts)
+          float m = mine.y;
 #pragma unroll
           for (int k = 16; k; k >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
+          const float f = ex2(mine.y - m);
+          float l = mine.x * f;
+#pragma unroll
+          for (int k = 16; k; k >>= 1) l += __shfl_xor_sync(0xffffffffu, l, k);
           float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-          for (int i = 0; i <= c1 - c0; ++i) {
-            const float2 lm = __ldcg(&p.part_l[place(i)]);
-            const float4 y = __ldcg(reinterpret_cast<const float4 *>(p.parts + (size_t)place(i) * 128 + d));
-            const float f = ex2(lm.y - m);
-            l = fmaf(lm.x, f, l);
-            v.x = fmaf(y.x, f, v.x);
-            v.y = fmaf(y.y, f, v.y);
-            v.z = fmaf(y.z, f, v.z);
-            v.w = fmaf(y.w, f, v.w);
+#pragma unroll 1
+          for (int i0 = 0; i0 < parts; i0 += 12) {
+            float4 y[12];
+#pragma unroll
+            for (int k = 0; k < 12; ++k)
+              if (i0 + k < parts) y[k] = __ldcg(reinterpret_cast<const float4 *>(p.parts + (size_t)place(i0 + k) * 128 + d));
+#pragma unroll
+            for (int k = 0; k < 12; ++k) {
+              const float fk = __shfl_sync(0xffffffffu, f, (i0 + k) & 31);
+              if (i0 + k < parts) {
+                v.x = fmaf(y[k].x, fk, v.x);
+                v.y = fmaf(y[k].y, fk, v.y);
+                v.z = fmaf(y[k].z, fk, v.z);
+                v.w = fmaf(y[k].w, fk, v.w);
+              }
+            }
           }
           write_row(row, d, v, l, m);
         }
       }
     }
-    // ---------------------------------------------------------------- the next tile
-    u += end_step - done;
-    if (u >= u1) break;
-    done = 0;
-    if (++t == tiles_of(q)) {
-      t = 0;
-      if (++h == p.Hkv) {
-        h = 0;
-        do q = sequence(ix, ++s);
-        while (q.n == 0 && s + 1 < ix.S);
-      }
-    }
-    async_proxy_fence();  // the rings held sums: behind them come copies
+    if (!more) break;
+    if (!apart) async_proxy_fence();  // the rings held sums: behind them come copies
     __syncthreads();
+    if (!apart) start();
   }
   if (tid == 0 && sh.abort) atomicExch(ix.status, HEART_ERR_DEVICE_CHECK);
 }
