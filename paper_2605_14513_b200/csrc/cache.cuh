@@ -32,7 +32,8 @@ struct CacheWorkspace {
   float2 *part_l;     // [2 * kCacheCtas][128] their row sums and references
   void *tiles;        // [max_tiles] tiles of a head, 32 bytes each (see cache_tiles.cu)
   long long *tile_first;  // [max_tiles + 1] key steps before a tile
-  int *tile_head;     // [64] number of tiles, most steps of a tile
+  int *tile_head;     // [64] number of tiles of a head, rounds of them that are dealt
+  long long *cuts;    // [kCacheCtas + 1] the CTAs' shares of the other ones
   size_t bytes;
 };
 
@@ -55,6 +56,7 @@ __host__ inline CacheWorkspace carve_cache(const CacheGeom &g, void *base) {
   w.tiles = take(32 * cache_max_tiles(g));
   w.tile_first = reinterpret_cast<long long *>(take(sizeof(long long) * (cache_max_tiles(g) + 1)));
   w.tile_head = reinterpret_cast<int *>(take(64 * sizeof(int)));
+  w.cuts = reinterpret_cast<long long *>(take((kCacheCtas + 1) * sizeof(long long)));
   w.bytes = off;
   return w;
 }

@@ -8,9 +8,12 @@
 //   * Rows see different keys.  Steps that some row does not see whole have a path of their own, outside of the loop over the steps:
 //     hidden scores become -inf in tensor memory, and values that are not finite (what lies behind a sequence's end is anyone's) are
 //     taken out of shared memory first, because the product reads them with weight 0; rows that do see such a value are marked.
-//   * All steps of all tiles, (key head, tile, step) in one line, are cut into equal shares, one a CTA, so that the launch ends on all
-//     SMs at once whatever the lengths are.  Parts of a tile go to the workspace; the CTA that brings the last one puts them together, in
-//     order: the result does not depend on which one that is.
+//   * Where keys and values fit the L2 (12 x 4680 over 12680 e4m3 tokens 387 us, dealt 422), each CTA takes a run of tiles. Otherwise tiles, of
+//     one key head after the other, are dealt in turn, so that the CTAs read the same keys at a time (12 x 32760 over themselves, 201 MB
+//     of keys and values: 7.2 ms when every CTA had a run of tiles of its own, whose keys came from DRAM, 5.7 dealt), but for the last one to two
+//     rounds of them: the steps of those, in one line, are cut into shares that bring all CTAs to the same sum, so that the launch ends
+//     on all SMs at once whatever the lengths are.  Parts of a tile go to the workspace; the CTA that brings the last one puts them together,
+//     in order: the result does not depend on which one that is.
 //
 // e4m3 caches.  Converting keys and values to bf16 for 128 rows costs as many instructions as the softmax does.  Keys need none: a bf16 query has
 // 8 significant bits and a code 4, so a query row, scaled by a power of two, is the sum of two rows of codes, to 2^-18 of its
@@ -37,6 +40,7 @@ constexpr int kCodeBytes = 16384;  // the same as e4m3: [128 rows][128]
 constexpr int kSteps = 16;         // key steps in flight (K is up to four steps ahead of the value products)
 constexpr int kPartRing = 4;
 constexpr int kMaxParts = 12;      // of a tile, about
+constexpr long long kRunsUpTo = 64LL << 20;  // bytes of keys and values that stay in L2: a CTA takes a run of tiles
 constexpr float kNoReference = -3.0e38f;
 constexpr float kHeadroom = 16.f, kMaxGrowth = 8.f;  // see attn_tc.cu
 constexpr float kHeadroomE4m3 = -4.f, kMaxGrowthE4m3 = 14.f;  // weights of f16: 2^4 where the reference moves, to 2^14
@@ -111,7 +115,8 @@ struct TileParams {
   CacheIndex ix;
   const Tile *tiles;
   const long long *first;  // [tiles + 1] key steps before a tile of a head
-  const int *head;         // number of tiles, most steps of a tile
+  const int *head;         // number of tiles of a head, rounds of tiles that are dealt
+  const long long *cuts;   // [CTAs + 1] what follows, in shares: first step, counted from the first one that is not dealt
   int32_t *arrivals;
   float4 *parts;           // [2 * CTAs][32][128]: four dims of a row
   float2 *part_l;          // [2 * CTAs][128]
@@ -120,7 +125,9 @@ struct TileParams {
   const uint8_t *k_scale, *v_scale;
   long long qt, qh;
   int Hq, Hkv, G;
+  uint32_t inv_G;          // row / G = row * inv_G >> 16 for the rows of a tile
   float scale_log2;
+  __device__ __forceinline__ int token_of(int row) const { return (int)(((uint32_t)row * inv_G) >> 16); }
 };
 
 __device__ __forceinline__ float fmax3(float a, float b, float c) {
@@ -186,7 +193,8 @@ __device__ __forceinline__ bool not_finite(uint32_t x) { return (x & 0x7f80u) ==
 // ---------------------------------------------------------------------- plan
 // The tiles of a head, sequence by sequence, and the key steps before each.  One CTA.
 __global__ void __launch_bounds__(1024) cache_plan_kernel(const CacheIndex ix, int tokens_per_tile, Tile *__restrict__ tiles,
-                                                          long long *__restrict__ first, int *__restrict__ head, int32_t *__restrict__ arrivals, int most) {
+                                                          long long *__restrict__ first, int *__restrict__ head, long long *__restrict__ cuts,
+                                                          int32_t *__restrict__ arrivals, int most, int Hkv, int token_bytes) {
   __shared__ long long sums[32];
   __shared__ int base[1024];
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
@@ -212,9 +220,13 @@ __global__ void __launch_bounds__(1024) cache_plan_kernel(const CacheIndex ix, i
     return before;
   };
   int n_tiles = 0, longest = 1;
+  long long tokens = 0;  // of the sequences with tiles
   for (int s0 = 0; s0 < ix.S; s0 += 1024) {
-    const int mine = s0 + t < ix.S ? (sequence(ix, s0 + t).n + tokens_per_tile - 1) / tokens_per_tile : 0;
+    const Sequence own = s0 + t < ix.S ? sequence(ix, s0 + t) : Sequence{0, 0, 0};
+    const int mine = (own.n + tokens_per_tile - 1) / tokens_per_tile;
     long long all;
+    scan(mine > 0 ? own.len : 0, all);
+    tokens += all;
     base[t] = (int)min(n_tiles + scan(mine, all), (long long)most);
     __syncthreads();
     for (int i = warp; i < 1024 && s0 + i < ix.S; i += 32) {  // a warp a sequence
@@ -249,12 +261,48 @@ __global__ void __launch_bounds__(1024) cache_plan_kernel(const CacheIndex ix, i
   __syncthreads();
   if (lane == 0) sums[warp] = longest;
   __syncthreads();
-  if (t == 0) {
-    for (int i = 0; i < 32; ++i) longest = max(longest, (int)sums[i]);
-    first[n_tiles] = before;
-    head[0] = n_tiles;
-    head[1] = longest;
+  for (int i = 0; i < 32; ++i) longest = max(longest, (int)sums[i]);
+  const long long per_head = before, total = per_head * Hkv, all_tiles = (long long)n_tiles * Hkv;
+  int rounds = tokens * Hkv * token_bytes <= kRunsUpTo ? 0 : (int)max(all_tiles / kCacheCtas - 1, 0LL);
+  long long dealt = 0, most_dealt = 0;  // to CTA t, to the one with most
+  while (rounds > 0) {
+    dealt = 0;
+    if (t < kCacheCtas)
+      for (int k = 0; k < rounds; ++k) dealt += tiles[(int)((t + (long long)k * kCacheCtas) % n_tiles)].steps;
+    most_dealt = dealt;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) most_dealt = max(most_dealt, __shfl_xor_sync(0xffffffffu, most_dealt, o));
+    __syncthreads();
+    if (lane == 0) sums[warp] = most_dealt;
+    __syncthreads();
+    for (int i = 0; i < 32; ++i) most_dealt = max(most_dealt, sums[i]);
+    if (most_dealt * kCacheCtas <= total) break;
+    rounds = min(rounds - 1, (int)(rounds * (total / kCacheCtas) / most_dealt));  // (tiles of very different lengths: fewer of them are dealt)
   }
+  if (t == 0) {
+    first[n_tiles] = per_head;
+    head[0] = n_tiles;
+    head[1] = rounds;
+  }
+  if (rounds == 0) {  // equal shares, of tiles in not too many parts
+    const long long share = max((total + kCacheCtas - 1) / kCacheCtas, (long long)(longest + kMaxParts - 1) / kMaxParts);
+    if (t <= kCacheCtas) cuts[t] = min(t * share, total);
+    return;
+  }
+  // the least sum to which shares of at least one step can bring all
+  long long all;
+  scan(dealt, all);
+  const long long rest = total - all;  // a tile's step a CTA at least
+  // the sum lies in (lo, hi]
+  long long lo = (total + kCacheCtas - 1) / kCacheCtas - 1, hi = most_dealt + (rest + kCacheCtas - 1) / kCacheCtas;
+  while (hi - lo > 1) {
+    const long long sum = (lo + hi) / 2;
+    long long shares;
+    scan(t < kCacheCtas ? max(sum - dealt, 1LL) : 0, shares);
+    (shares >= rest ? hi : lo) = sum;
+  }
+  const long long at = scan(t < kCacheCtas ? max(hi - dealt, 1LL) : 0, all);
+  if (t <= kCacheCtas) cuts[t] = min(at, rest);
 }
 
 // ---------------------------------------------------------------------- attention
@@ -389,63 +437,91 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
     // ===== the CTA's parts; K and Q producer.  What a step's other warps need to know is said before its copy is waited for.  (Little code: it
     // is one of many places that the warps of an SM are in, see attn_tc.cu.  A warp of its own that looked ahead by five steps, with ten times
     // the instructions, ran at three quarters of the rate.)
-    const int n_tiles = __ldcg(&p.head[0]), longest = __ldcg(&p.head[1]);
-    const long long per_head = __ldcg(&p.first[n_tiles]), total = per_head * p.Hkv;
-    const long long share = max((total + gridDim.x - 1) / gridDim.x, (long long)(longest + kMaxParts - 1) / kMaxParts);
-    const long long u1 = min(total, (blockIdx.x + 1) * share);
-    long long u = blockIdx.x * share;
-    int h = 0, tile = 0, a = 0;
-    if (u < u1) {
-      h = (int)(u / per_head);
-      const long long rest = u - h * per_head;
+    const int n_tiles = __ldcg(&p.head[0]), rounds = __ldcg(&p.head[1]);
+    const long long per_head = __ldcg(&p.first[n_tiles]);
+    const long long u0 = __ldcg(&p.cuts[blockIdx.x]), u1 = __ldcg(&p.cuts[blockIdx.x + 1]);
+    const long long dealt = (long long)rounds * gridDim.x;  // tiles
+    long long u = u0;  // of the share: the part's first step
+    int h, tile, a = 0;
+    auto share_begins = [&]() {
+      // the line's first step, as a step of all heads
+      const int h0 = (int)(dealt / n_tiles);
+      const long long at = u + (h0 * per_head + __ldcg(&p.first[(int)(dealt - (long long)h0 * n_tiles)]));
+      h = (int)(at / per_head);
+      const long long rest = at - h * per_head;
+      tile = 0;
       int hi = n_tiles;  // first[tile] <= rest < first[hi]
       while (hi - tile > 1) {
-        const int step = (hi - tile + 31) / 32, at = tile + lane * step;
-        const bool below = at < hi && (lane == 0 || __ldcg(&p.first[at]) <= rest);
+        const int step = (hi - tile + 31) / 32, i = tile + lane * step;
+        const bool below = i < hi && (lane == 0 || __ldcg(&p.first[i]) <= rest);
         const int n = __popc(__ballot_sync(0xffffffffu, below));
         tile += (n - 1) * step;
         hi = min(hi, tile + step);
       }
       a = (int)(rest - __ldcg(&p.first[tile]));
-    }
+    };
+    auto holder = [&](long long at) {  // the CTA whose share has this step
+      int n = 0;
+      for (int c = lane; c < kCacheCtas; c += 32) n += __ldcg(&p.cuts[c]) <= at ? 1 : 0;
+      return (int)__reduce_add_sync(0xffffffffu, (unsigned)n) - 1;
+    };
+    int k = 0;  // tiles of this CTA that it has been dealt so far
+    auto next_dealt = [&]() {
+      const long long i = blockIdx.x + (long long)k * gridDim.x;
+      h = (int)(i / n_tiles);
+      tile = (int)(i - (long long)h * n_tiles);
+    };
     int g = 0, n = 0;
     auto fetch = [&](int i) {  // lane i < 8: a word of a tile
       return lane < 8 ? __ldcg(reinterpret_cast<const int *>(&p.tiles[i]) + lane) : 0;
     };
-    int word = u < u1 ? fetch(tile) : 0;
+    h = tile = 0;
+    if (rounds > 0) next_dealt();
+    else if (u < u1) share_begins();
+    int word = rounds > 0 || u < u1 ? fetch(tile) : 0;
 #pragma unroll 1
     for (;; ++n) {
       if (n >= kPartRing && !wait(&sh.part_empty[n % kPartRing], (n / kPartRing - 1) & 1)) break;
       Part &x = sh.part[n % kPartRing];
-      const bool any = u < u1;
+      const bool from_line = k >= rounds, any = !from_line || u < u1;
       if (lane < 8) reinterpret_cast<int *>(&x.t)[lane] = word;
       __syncwarp();
-      const int b = any ? (int)min((long long)x.t.steps, a + (u1 - u)) : -1;
+      const int b = !any ? -1 : from_line ? (int)min((long long)x.t.steps, a + (u1 - u)) : x.t.steps;
+      int c0 = blockIdx.x, parts = 1;
+      if (any && b - a < x.t.steps) {
+        c0 = holder(u - a);
+        parts = holder(u - a + x.t.steps - 1) - c0 + 1;
+      }
       if (lane == 0) {
         x.h = h;
         x.a = a;
         x.b = b;
-        const long long at = u - a;
-        x.c0 = (int)(at / share);
-        x.parts = any ? (int)((at + x.t.steps - 1) / share) - x.c0 + 1 : 0;
+        x.c0 = c0;
+        x.parts = parts;
         mbar_arrive(&sh.part_full[n % kPartRing]);
       }
       // (no other warp writes the ring: this one may go on reading the part)
       __syncwarp();
       if (!any) break;
-      u += b - a;
-      int h_next = h;
-      if (++tile == n_tiles) tile = 0, ++h_next;
-      if (u < u1) word = fetch(tile);  // ahead of its use
+      const int a_now = a, h_now = h;
+      a = 0;
+      if (!from_line) {
+        if (++k < rounds) next_dealt();
+        else if (u < u1) share_begins();
+      } else {
+        u += b - a_now;
+        if (++tile == n_tiles) tile = 0, ++h;
+      }
+      if (k < rounds || u < u1) word = fetch(tile);  // ahead of its use
       const Whole whole = whole_of(x.t);
       const uint32_t len = x.t.len;
       const int sinks = x.t.sinks, shift = x.t.first - x.t.sinks, sink = ix.sink;
       const int32_t *table = ix.table + (size_t)x.t.s * ix.table_stride + lane;
       const uint32_t ahead = lane < n_boxes ? lane << page_log2 : 0x7fffffff;  // from a step's first key to that of the lane's box
       auto entry_of = [&](int k0) { return k0 + ahead < len ? __ldcg(table + (k0 >> page_log2)) : ix.n_pages; };
-      int k0 = (a < sinks ? a : a + shift) * kKeyStep, entry = entry_of(k0);
+      int k0 = (a_now < sinks ? a_now : a_now + shift) * kKeyStep, entry = entry_of(k0);
 #pragma unroll 1
-      for (int i = a; i < b; ++i, ++g) {
+      for (int i = a_now; i < b; ++i, ++g) {
         Step &y = sh.step[g % kSteps];
         int page = entry;
         if ((unsigned)page > (unsigned)ix.n_pages || (page == ix.n_pages && k0 + ahead < len)) page = checked_page(ix, entry);  // (out of range: zeros)
@@ -453,8 +529,8 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
         if (lane == 0) {
           y.key = k0;
           y.keys = (int)len - k0;
-          y.h = h;
-          y.flags = (k0 + kKeyStep <= whole.end && (k0 >= whole.low || k0 + kKeyStep <= sink) ? 0 : kStepMasked) | (i == a ? kStepStarts : 0);
+          y.h = h_now;
+          y.flags = (k0 + kKeyStep <= whole.end && (k0 >= whole.low || k0 + kKeyStep <= sink) ? 0 : kStepMasked) | (i == a_now ? kStepStarts : 0);
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.step_full[g % kSteps]);
@@ -463,8 +539,8 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
           entry = entry_of(k0);
         }
         if (g >= 2 && !wait(&sh.s_full[g & 1], ((g - 2) >> 1) & 1)) break;
-        load_pages(smem + L::kOffK + (g & 1) * L::kKey, &map_k, &sh.k_full[g & 1], h, page);
-        if (i == a) {
+        load_pages(smem + L::kOffK + (g & 1) * L::kKey, &map_k, &sh.k_full[g & 1], h_now, page);
+        if (i == a_now) {
           if (n >= 2 && !wait(&sh.out_done[n & 1], ((n - 2) >> 1) & 1)) {
             ++g;
             break;
@@ -472,14 +548,12 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
           if (lane == 0) {
             unsigned char *q = smem + L::kOffQ + (n & 1) * kTileBytes;
             mbar_expect_tx(&sh.q_full[n & 1], 2 * (128 / p.G * p.G) * 128);
-            tma_load_5d(q, &map_q, &sh.q_full[n & 1], 0, 0, x.t.row, 0, h);
-            tma_load_5d(q + kTileBytes / 2, &map_q, &sh.q_full[n & 1], 0, 0, x.t.row, 1, h);
+            tma_load_5d(q, &map_q, &sh.q_full[n & 1], 0, 0, x.t.row, 0, h_now);
+            tma_load_5d(q + kTileBytes / 2, &map_q, &sh.q_full[n & 1], 0, 0, x.t.row, 1, h_now);
           }
         }
       }
       if (!ok) break;
-      a = 0;
-      h = h_next;
     }
     if (E4m3 && ok) {  // for those who look ahead
       if (lane == 0) {
@@ -779,7 +853,7 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
       const uint32_t s_at = s_addr + (g & 1) * 128;
       const Part &x = sh.written[nt & 1][warp];
       const int k0 = sh.step[g % kSteps].key;
-      const Visible v = visible(ix, x.t.p0 + row / p.G, x.t.len);
+      const Visible v = visible(ix, x.t.p0 + p.token_of(row), x.t.len);
       const int end = v.end - k0, low = v.low - k0, sink = ix.sink - k0;
       tc_fence_after();
 #pragma unroll 1
@@ -986,7 +1060,7 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
         const uint32_t out = smem_u32(smem + L::kOffQ + q_buf * kTileBytes + quarter * (kTileBytes / 4));  // the place of its Q: 32 rows a warp
         const int slot = 2 * blockIdx.x + (to.a == 0 ? 1 : 0);
         // e4m3: a row without any key whose query is not finite has sums that are no numbers
-        const bool none = E4m3 && to.t.p0 + row / p.G < 0;
+        const bool none = E4m3 && to.t.p0 + p.token_of(row) < 0;
         if (none) l = 0.f;
         // 64 dims of the row as bf16, O / l, into shared memory
         auto stage = [&](const uint32_t (&v)[64], int half, float inv) {
@@ -1079,15 +1153,16 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
         if (write) {
           __syncwarp();
           // two rows at a time, 16 lanes each
+          uint16_t *o_row = p.O + (long long)to.t.row * p.qt + (long long)(to.h * p.G) * p.qh + (lane & 15) * 8;
 #pragma unroll 1
           for (int i = 0; i < 16; ++i) {
             const int mine = i * 2 + (lane >> 4), r = (int)quarter * 32 + mine, piece = lane & 15;
             const uint4 v = lds_u4(out + (piece >> 3) * (kTileBytes / 8) + mine * 128 + (((piece ^ mine) & 7) << 4));
-            if (r < n_rows)
-              *reinterpret_cast<uint4 *>(p.O + (long long)(to.t.row + r / p.G) * p.qt + (long long)(to.h * p.G + r % p.G) * p.qh + piece * 8) = v;
+            const int token = p.token_of(r);
+            if (r < n_rows) *reinterpret_cast<uint4 *>(o_row + (long long)token * p.qt + (long long)(r - token * p.G) * p.qh) = v;
           }
           if (p.lse != nullptr && row < n_rows)
-            p.lse[(long long)(to.t.row + row / p.G) * p.Hq + to.h * p.G + row % p.G] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+            p.lse[(long long)(to.t.row + p.token_of(row)) * p.Hq + to.h * p.G + row - p.token_of(row) * p.G] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
         }
         async_proxy_fence();  // (copies come to the place of Q)
         __syncwarp();
@@ -1141,6 +1216,7 @@ cudaError_t launch_cache_tiles(const CacheGeom &g, const CacheIndex &ix, const C
   p.tiles = reinterpret_cast<const Tile *>(w.tiles);
   p.first = w.tile_first;
   p.head = w.tile_head;
+  p.cuts = w.cuts;
   p.arrivals = w.arrivals + kCacheCtas;
   p.parts = reinterpret_cast<float4 *>(w.parts);
   p.part_l = w.part_l;
@@ -1153,9 +1229,10 @@ cudaError_t launch_cache_tiles(const CacheGeom &g, const CacheIndex &ix, const C
   p.Hq = g.Hq;
   p.Hkv = g.Hkv;
   p.G = g.G;
+  p.inv_G = (65536u + g.G - 1) / g.G;
   p.scale_log2 = (float)(g.scale * 1.4426950408889634);
   cudaError_t e = launch_pdl(cache_plan_kernel, dim3(1), dim3(1024), 0, s, ix, 128 / g.G, reinterpret_cast<Tile *>(w.tiles), w.tile_first, w.tile_head,
-                             p.arrivals, (int)cache_max_tiles(g));
+                             w.cuts, p.arrivals, (int)cache_max_tiles(g), g.Hkv, g.e4m3 ? 2 * kD : 4 * kD);
   if (e != cudaSuccess) return e;
   ++*launches;
   e = g.e4m3 ? launch<true>(mq, mk, mv, p, s) : launch<false>(mq, mk, mv, p, s);
