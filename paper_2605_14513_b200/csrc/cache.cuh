@@ -30,13 +30,14 @@ struct CacheWorkspace {
   int32_t *arrivals;  // [2][kCacheCtas] parts of a shared tile that are there: the rows kernel's (zero between launches), the tile kernel's
   float *parts;       // [2 * kCacheCtas][128][128] parts of tiles: unnormalised sums of values
   float2 *part_l;     // [2 * kCacheCtas][128] their row sums and references
-  void *tiles;        // [max_tiles] tiles of a head, 32 bytes each (see cache_tiles.cu)
+  void *tiles;        // [max_tiles] tiles of a head (see cache_tiles.cu)
   long long *tile_first;  // [max_tiles + 1] key steps before a tile
   int *tile_head;     // [64] number of tiles of a head, rounds of them that are dealt
   long long *cuts;    // [kCacheCtas + 1] the CTAs' shares of the other ones
   size_t bytes;
 };
 
+constexpr size_t kTileRecord = 48;
 // Tiles of a head: a sequence ends at most one of them early.
 __host__ inline size_t cache_max_tiles(const CacheGeom &g) { return (size_t)g.S + (size_t)g.T / (128 / g.G); }
 
@@ -53,7 +54,7 @@ __host__ inline CacheWorkspace carve_cache(const CacheGeom &g, void *base) {
   w.arrivals = reinterpret_cast<int32_t *>(take(2 * kCacheCtas * sizeof(int32_t)));
   w.parts = reinterpret_cast<float *>(take(sizeof(float) * 2 * kCacheCtas * 128 * kD));
   w.part_l = reinterpret_cast<float2 *>(take(sizeof(float2) * 2 * kCacheCtas * 128));
-  w.tiles = take(32 * cache_max_tiles(g));
+  w.tiles = take(kTileRecord * cache_max_tiles(g));
   w.tile_first = reinterpret_cast<long long *>(take(sizeof(long long) * (cache_max_tiles(g) + 1)));
   w.tile_head = reinterpret_cast<int *>(take(64 * sizeof(int)));
   w.cuts = reinterpret_cast<long long *>(take((kCacheCtas + 1) * sizeof(long long)));

@@ -38,7 +38,7 @@ constexpr int kWarpQK = 8, kWarpV = 9, kWarpK = 10, kWarpPV = 11, kWarpConvert =
 constexpr int kTileBytes = 32768;  // 128 rows x 128 dims of bf16: [2 dim halves][128 rows][64], 128-byte swizzle
 constexpr int kCodeBytes = 16384;  // the same as e4m3: [128 rows][128]
 constexpr int kSteps = 16;         // key steps in flight (K is up to four steps ahead of the value products)
-constexpr int kPartRing = 4;
+constexpr int kPartRing = 8;       // parts are announced a part ahead
 constexpr int kMaxParts = 12;      // of a tile, about
 constexpr long long kRunsUpTo = 64LL << 20;  // bytes of keys and values that stay in L2: a CTA takes a run of tiles
 constexpr float kNoReference = -3.0e38f;
@@ -50,8 +50,11 @@ constexpr uint32_t kShortWait = 500;
 struct Tile {
   int s, row, tokens, p0;         // sequence; first packed row; new tokens; position of the first
   int len, sinks, first, steps;   // tokens of the sequence; its key steps (see Span)
+  int every_low, every_end;       // all rows see the keys every_low .. every_end - 1 (and of the sinks those before every_end)
+  int some_low, some_end;         // some row sees them
 };
-static_assert(sizeof(Tile) == 32, "two words of 16 bytes");
+constexpr int kTileWords = sizeof(Tile) / 4;
+static_assert(sizeof(Tile) == kTileRecord, "the workspace has room for it");
 
 // Part of a tile that a CTA takes: steps a .. b - 1 for key head h.
 struct Part {
@@ -60,7 +63,8 @@ struct Part {
   int c0, parts;     // first CTA with a part of the tile, and how many there are
   int pad[3];
 };
-static_assert(sizeof(Part) == 64, "lanes copy words");
+constexpr int kPartWords = sizeof(Part) / 4;
+static_assert(kPartWords <= 32, "lanes copy words");
 
 // A key step of a CTA, some steps ahead of its use.
 struct Step {
@@ -102,7 +106,8 @@ struct TileShared {
   int first_top[4];                   // the largest one of the first step, per part & 3
   int top[8];                         // the largest
   float q_scale[2][128];     // e4m3: what the scores of a row are to be multiplied by
-  alignas(16) uint32_t bad[8][4];  // keys that are not finite (bf16: of masked steps), by g & 7
+  alignas(16) uint32_t bad[8][4];     // e4m3: keys that are not finite, by g & 7
+  alignas(16) uint8_t not_finite[4][128];  // bf16: rows that see a value that is not finite, per part & 3
   uint32_t tmem_base;
   int last[2];
   int abort;
@@ -188,15 +193,22 @@ __device__ __forceinline__ uint4 lds_u4(uint32_t addr) {
 __device__ __forceinline__ void sts_u4(uint32_t addr, uint4 v) {
   asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
-__device__ __forceinline__ bool not_finite(uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
+// Whether one of eight bf16 numbers is not finite: an exponent field of ones carries into the sign's place.
+__device__ __forceinline__ bool not_finite(const uint4 &x) {
+  auto carry = [](uint32_t w) { return (w & 0x7f807f80u) + 0x00800080u; };
+  return ((carry(x.x) | carry(x.y) | carry(x.z) | carry(x.w)) & 0x80008000u) != 0u;
+}
 
 // ---------------------------------------------------------------------- plan
+constexpr int kSmallPlan = 4096;
 // The tiles of a head, sequence by sequence, and the key steps before each.  One CTA.
 __global__ void __launch_bounds__(1024) cache_plan_kernel(const CacheIndex ix, int tokens_per_tile, Tile *__restrict__ tiles,
                                                           long long *__restrict__ first, int *__restrict__ head, long long *__restrict__ cuts,
                                                           int32_t *__restrict__ arrivals, int most, int Hkv, int token_bytes) {
   __shared__ long long sums[32];
   __shared__ int base[1024];
+  __shared__ int steps[kSmallPlan];  // of the first tiles: as a rule all
+  auto steps_of = [&](int i) { return i < kSmallPlan ? steps[i] : tiles[i].steps; };
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
   pdl_wait();
   pdl_launch_dependents();
@@ -242,7 +254,13 @@ __global__ void __launch_bounds__(1024) cache_plan_kernel(const CacheIndex ix, i
         x.sinks = sp.sinks;
         x.first = sp.first;
         x.steps = sp.steps;
+        const Visible v0 = visible(ix, max(x.p0, 0), q.len), v1 = visible(ix, x.p0 + x.tokens - 1, q.len);
+        x.every_low = v1.low;
+        x.every_end = x.p0 >= 0 ? v0.end : 0;
+        x.some_low = v0.low;
+        x.some_end = v1.end;
         tiles[base[i] + k] = x;
+        if (base[i] + k < kSmallPlan) steps[base[i] + k] = sp.steps;
       }
     }
     n_tiles = (int)min(n_tiles + all, (long long)most);  // (more: starts that do not ascend, which are reported)
@@ -250,7 +268,7 @@ __global__ void __launch_bounds__(1024) cache_plan_kernel(const CacheIndex ix, i
   }
   long long before = 0;
   for (int t0 = 0; t0 < n_tiles; t0 += 1024) {
-    const int mine = t0 + t < n_tiles ? tiles[t0 + t].steps : 0;
+    const int mine = t0 + t < n_tiles ? steps_of(t0 + t) : 0;
     longest = max(longest, mine);
     long long all;
     const long long at = before + scan(mine, all);
@@ -268,7 +286,10 @@ __global__ void __launch_bounds__(1024) cache_plan_kernel(const CacheIndex ix, i
   while (rounds > 0) {
     dealt = 0;
     if (t < kCacheCtas)
-      for (int k = 0; k < rounds; ++k) dealt += tiles[(int)((t + (long long)k * kCacheCtas) % n_tiles)].steps;
+      for (int k = 0, i = t % n_tiles, by = kCacheCtas % n_tiles; k < rounds; ++k) {
+        dealt += steps_of(i);
+        i = i + by < n_tiles ? i + by : i + by - n_tiles;
+      }
     most_dealt = dealt;
 #pragma unroll
     for (int o = 16; o; o >>= 1) most_dealt = max(most_dealt, __shfl_xor_sync(0xffffffffu, most_dealt, o));
@@ -416,17 +437,6 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
       if (!E4m3 && n_boxes > 1) tma_load_5d(to + kTileBytes / 2, map, bar, 0, 0, 1, h, page);
     }
   };
-  // Whether some row of the tile does not see all keys of the step at k0.
-  struct Whole {
-    int end, low;
-  };
-  auto whole_of = [&](const Tile &t) -> Whole {
-    return {t.p0 >= 0 ? visible(ix, t.p0, t.len).end : 0, visible(ix, t.p0 + t.tokens - 1, t.len).low};
-  };
-  auto masked_at = [&](const Whole &w, int k0) {
-    return !(k0 + kKeyStep <= w.end && (k0 >= w.low || k0 + kKeyStep <= ix.sink));
-  };
-
   // ------------------------------------------------------------------ roles
   if (warp >= kWarpConvert) {
     setmaxnreg_dec<L::kRegsConvert>();
@@ -462,7 +472,8 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
     };
     auto holder = [&](long long at) {  // the CTA whose share has this step
       int n = 0;
-      for (int c = lane; c < kCacheCtas; c += 32) n += __ldcg(&p.cuts[c]) <= at ? 1 : 0;
+#pragma unroll
+      for (int c = 0; c < kCacheCtas; c += 32) n += c + lane < kCacheCtas && __ldcg(&p.cuts[c + lane]) <= at ? 1 : 0;
       return (int)__reduce_add_sync(0xffffffffu, (unsigned)n) - 1;
     };
     int k = 0;  // tiles of this CTA that it has been dealt so far
@@ -472,19 +483,28 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
       tile = (int)(i - (long long)h * n_tiles);
     };
     int g = 0, n = 0;
-    auto fetch = [&](int i) {  // lane i < 8: a word of a tile
-      return lane < 8 ? __ldcg(reinterpret_cast<const int *>(&p.tiles[i]) + lane) : 0;
+    auto fetch = [&](int i) {  // lane i: a word of a tile
+      return lane < kTileWords ? __ldcg(reinterpret_cast<const int *>(&p.tiles[i]) + lane) : 0;
     };
     h = tile = 0;
     if (rounds > 0) next_dealt();
     else if (u < u1) share_begins();
     int word = rounds > 0 || u < u1 ? fetch(tile) : 0;
-#pragma unroll 1
-    for (;; ++n) {
-      if (n >= kPartRing && !wait(&sh.part_empty[n % kPartRing], (n / kPartRing - 1) & 1)) break;
-      Part &x = sh.part[n % kPartRing];
-      const bool from_line = k >= rounds, any = !from_line || u < u1;
-      if (lane < 8) reinterpret_cast<int *>(&x.t)[lane] = word;
+    // from a step's first key to that of the lane's box
+    const uint32_t ahead = lane < n_boxes ? lane << page_log2 : 0x7fffffff;
+    auto key_at = [&](const Tile &t, int i) { return (i < t.sinks ? i : t.first + i - t.sinks) * kKeyStep; };
+    auto entry_of = [&](const Tile &t, int k0) {
+      return k0 + ahead < (uint32_t)t.len ? __ldcg(ix.table + ((size_t)t.s * ix.table_stride + lane + (k0 >> page_log2))) : ix.n_pages;
+    };
+    // Announces part m (or the end), and asks for its first pages and the tile behind it.
+    bool any;
+    int entry = 0;
+    auto announce = [&](int m) {
+      if (m >= kPartRing && !wait(&sh.part_empty[m % kPartRing], (m / kPartRing - 1) & 1)) return;
+      Part &x = sh.part[m % kPartRing];
+      const bool from_line = k >= rounds;
+      any = !from_line || u < u1;
+      if (lane < kTileWords) reinterpret_cast<int *>(&x.t)[lane] = word;
       __syncwarp();
       const int b = !any ? -1 : from_line ? (int)min((long long)x.t.steps, a + (u1 - u)) : x.t.steps;
       int c0 = blockIdx.x, parts = 1;
@@ -498,45 +518,49 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
         x.b = b;
         x.c0 = c0;
         x.parts = parts;
-        mbar_arrive(&sh.part_full[n % kPartRing]);
+        mbar_arrive(&sh.part_full[m % kPartRing]);
       }
-      // (no other warp writes the ring: this one may go on reading the part)
-      __syncwarp();
-      if (!any) break;
-      const int a_now = a, h_now = h;
-      a = 0;
+      __syncwarp();  // (no other warp writes the ring: this one goes on reading the part)
+      if (!any) return;
+      entry = entry_of(x.t, key_at(x.t, a));
       if (!from_line) {
+        a = 0;
         if (++k < rounds) next_dealt();
         else if (u < u1) share_begins();
       } else {
-        u += b - a_now;
+        u += b - a;
+        a = 0;
         if (++tile == n_tiles) tile = 0, ++h;
       }
-      if (k < rounds || u < u1) word = fetch(tile);  // ahead of its use
-      const Whole whole = whole_of(x.t);
+      if (k < rounds || u < u1) word = fetch(tile);
+    };
+    announce(0);
+#pragma unroll 1
+    for (; ok && any; ++n) {
+      const Part &x = sh.part[n % kPartRing];
+      const int a_now = x.a, b = x.b, h_now = x.h;
       const uint32_t len = x.t.len;
-      const int sinks = x.t.sinks, shift = x.t.first - x.t.sinks, sink = ix.sink;
+      const int sinks = x.t.sinks, shift = x.t.first - x.t.sinks, sink = ix.sink, every_low = x.t.every_low, every_end = x.t.every_end;
       const int32_t *table = ix.table + (size_t)x.t.s * ix.table_stride + lane;
-      const uint32_t ahead = lane < n_boxes ? lane << page_log2 : 0x7fffffff;  // from a step's first key to that of the lane's box
-      auto entry_of = [&](int k0) { return k0 + ahead < len ? __ldcg(table + (k0 >> page_log2)) : ix.n_pages; };
-      int k0 = (a_now < sinks ? a_now : a_now + shift) * kKeyStep, entry = entry_of(k0);
+      int k0 = key_at(x.t, a_now);
 #pragma unroll 1
       for (int i = a_now; i < b; ++i, ++g) {
         Step &y = sh.step[g % kSteps];
         int page = entry;
-        if ((unsigned)page > (unsigned)ix.n_pages || (page == ix.n_pages && k0 + ahead < len)) page = checked_page(ix, entry);  // (out of range: zeros)
+        // (out of range: zeros)
+        if ((unsigned)page >= (unsigned)ix.n_pages) page = k0 + ahead < len ? checked_page(ix, page) : ix.n_pages;
         if (lane < 8) y.page[lane] = page;
         if (lane == 0) {
           y.key = k0;
           y.keys = (int)len - k0;
           y.h = h_now;
-          y.flags = (k0 + kKeyStep <= whole.end && (k0 >= whole.low || k0 + kKeyStep <= sink) ? 0 : kStepMasked) | (i == a_now ? kStepStarts : 0);
+          y.flags = (k0 + kKeyStep <= every_end && (k0 >= every_low || k0 + kKeyStep <= sink) ? 0 : kStepMasked) | (i == a_now ? kStepStarts : 0);
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.step_full[g % kSteps]);
         if (i + 1 < b) {
           k0 = (i + 1 < sinks ? i + 1 : i + 1 + shift) * kKeyStep;
-          entry = entry_of(k0);
+          entry = k0 + ahead < len ? __ldcg(table + (k0 >> page_log2)) : ix.n_pages;
         }
         if (g >= 2 && !wait(&sh.s_full[g & 1], ((g - 2) >> 1) & 1)) break;
         load_pages(smem + L::kOffK + (g & 1) * L::kKey, &map_k, &sh.k_full[g & 1], h_now, page);
@@ -553,7 +577,7 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
           }
         }
       }
-      if (!ok) break;
+      if (ok) announce(n + 1);  // (before the copies of the last steps are used)
     }
     if (E4m3 && ok) {  // for those who look ahead
       if (lane == 0) {
@@ -621,7 +645,9 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
     for (int n = 0; ok; ++n) {
       const Part *x = part_at(n);
       if (x == nullptr || x->b < 0) break;
-      const int n_steps = x->b - x->a;
+      const int n_steps = x->b - x->a, every_low = x->t.every_low, every_end = x->t.every_end, some_low = x->t.some_low,
+                some_end = x->t.some_end, len = x->t.len, p0 = x->t.p0;
+      if (!E4m3) *reinterpret_cast<uint32_t *>(&sh.not_finite[n & 3][lane * 4]) = 0u;
       done_with_part(n);
 #pragma unroll 1
       for (int i = 0; i < n_steps; ++i, ++g) {
@@ -642,27 +668,47 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
               ++g;
               break;
             }
-            // values that are not finite: [2 dim halves][128 keys][8 x 16 bytes]
-            const uint32_t v_at = smem_u32(smem + L::kOffV + at * kTileBytes);
-            uint32_t any = 0u;
+            // Values that no row sees are taken out as they are, those that some rows see looked at: [2 dim halves][128 keys][8 x 16 bytes],
+            // 16 keys at a time, a lane 16 bytes of each half of every fourth.
+            const uint32_t v_at = smem_u32(smem + L::kOffV + at * kTileBytes) + lane * 16;
+            const int k0 = y.key;
 #pragma unroll 1
-            for (int w = 0; w < 4; ++w) {
-              uint32_t bad = 0u;
-#pragma unroll 4
-              for (int j = 0; j < 16; ++j) {  // 32 keys: 8 pieces of 4 keys in each half
-                const uint4 v = lds_u4(v_at + (j >> 3) * (kTileBytes / 2) + w * 4096 + (j & 7) * 512 + lane * 16);
-                if (not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w)) bad |= 1u << ((j & 7) * 4 + (lane >> 3));
+            for (int c = 0; c < 128; c += 16) {
+              const int key = k0 + c, mine = key + (lane >> 3);
+              if (key + 16 <= every_end && (key >= every_low || key + 16 <= ix.sink)) continue;
+              uint4 v[4], w[4];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) v[j] = lds_u4(v_at + (c + 4 * j) * 128), w[j] = lds_u4(v_at + kTileBytes / 2 + (c + 4 * j) * 128);
+              uint32_t out = 0u;   // bits j: key 4 * j of this lane is to be taken out, bits 4 + j: though rows see it
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const int kj = mine + 4 * j;
+                const bool seen = kj < some_end && (kj >= some_low || kj < ix.sink);
+                if (!seen) out |= 1u << j;
+                else if (not_finite(v[j]) || not_finite(w[j])) out |= 17u << j;
               }
-              bad = __reduce_or_sync(0xffffffffu, bad);
-              any |= bad;
-              if (lane == 0) sh.bad[g & 7][w] = bad;
+              if (__all_sync(0xffffffffu, out == 0u)) continue;
+#pragma unroll
+              for (int o = 1; o < 8; o <<= 1) out |= __shfl_xor_sync(0xffffffffu, out, o);  // (the eight lanes of a key)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                if (out >> j & 1u) {
+                  sts_u4(v_at + (c + 4 * j) * 128, make_uint4(0u, 0u, 0u, 0u));
+                  sts_u4(v_at + kTileBytes / 2 + (c + 4 * j) * 128, make_uint4(0u, 0u, 0u, 0u));
+                }
+              }
+              if (__any_sync(0xffffffffu, out > 15u)) {  // rows that see such a key: 16 rows for each of a key's lanes
 #pragma unroll 1
-              for (; bad; bad &= bad - 1) {
-                const int key = w * 32 + __ffs(bad) - 1;
-                if (lane < 16) sts_u4(v_at + (lane >> 3) * (kTileBytes / 2) + key * 128 + (lane & 7) * 16, make_uint4(0u, 0u, 0u, 0u));
+                for (int j = 0; j < 4; ++j)
+#pragma unroll 1
+                  for (int r = lane & 7; r < 128 && (out >> (4 + j) & 1u); r += 8) {
+                    const Visible see = visible(ix, p0 + p.token_of(r), len);
+                    const int kj = mine + 4 * j;
+                    if (kj < see.end && (kj >= see.low || kj < ix.sink)) sh.not_finite[n & 3][r] = 1;
+                  }
               }
             }
-            if (any) async_proxy_fence();
+            async_proxy_fence();
           }
           __syncwarp();
           if (lane == 0) mbar_arrive(&sh.v_ready[at]);
@@ -724,6 +770,7 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
       for (int i = 0; i < n_steps; ++i, ++g) {  // O (+)= P_g V_g
         const uint32_t b = g & 1;
         wait(E4m3 ? &sh.v_ready[b] : &sh.v_full[b], (g >> 1) & 1);
+        if (!E4m3 && (sh.step[g % kSteps].flags & kStepMasked)) wait(&sh.v_ready[b], (g >> 1) & 1);
         if (!wait(&sh.p_full[b], (g >> 1) & 1)) break;
         tc_fence_after();
         if (leader) {
@@ -858,6 +905,7 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
       tc_fence_after();
 #pragma unroll 1
       for (int col = 0; col < 128; col += 16) {
+        if (__all_sync(0xffffffffu, col + 16 <= end && (col >= low || col + 16 <= sink))) continue;
         uint32_t y[16];
         tmem_ld16(s_at + col, y);
         tmem_wait_ld();
@@ -867,9 +915,8 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
         tmem_st16(s_at + col, y);
       }
       tmem_wait_st();
-      if (!E4m3) wait(&sh.v_ready[g & 1], (g >> 1) & 1);
 #pragma unroll 1
-      for (int j = 0; j < 4; ++j)
+      for (int j = 0; E4m3 && j < 4; ++j)
 #pragma unroll 1
         for (uint32_t todo = sh.bad[g & 7][j]; todo; todo &= todo - 1) {
           const int k = j * 32 + __ffs(todo) - 1;
@@ -895,7 +942,7 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
       const Part *x = part_at(n_part);
       live = x != nullptr && x->b >= 0;
       if (!live) return;
-      if (lane < 16) reinterpret_cast<int *>(&sh.written[nt & 1][warp])[lane] = reinterpret_cast<const int *>(x)[lane];
+      if (lane < kPartWords) reinterpret_cast<int *>(&sh.written[nt & 1][warp])[lane] = reinterpret_cast<const int *>(x)[lane];
       n_steps = x->b - x->a;
       done_with_part(n_part);  // (a warp barrier: all lanes see the copy)
       ++n_part;
@@ -1062,6 +1109,7 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
         // e4m3: a row without any key whose query is not finite has sums that are no numbers
         const bool none = E4m3 && to.t.p0 + p.token_of(row) < 0;
         if (none) l = 0.f;
+        if (!E4m3 && sh.not_finite[(nt - 1) & 3][row]) l = __uint_as_float(0x7fc00000u);
         // 64 dims of the row as bf16, O / l, into shared memory
         auto stage = [&](const uint32_t (&v)[64], int half, float inv) {
           const uint64_t inv2 = pack_f32x2(inv, inv);
