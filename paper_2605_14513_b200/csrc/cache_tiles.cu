@@ -612,24 +612,27 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
     auto tell = [&]() {
       if (ended || !ok) return;
       const int keys = sh.step[asked % kSteps].keys - lane * 4;
+      // (bytes with a meaning of their own, and a step that ends early, come seldom)
+      const bool special = (__vcmpeq4(kb, 0xffffffffu) | __vcmpeq4(vb, 0xffffffffu) | __vcmpeq4(kb, 0u)) != 0u || keys < 4;
+      uint32_t bad = 0u;
       float f[4];
-      uint32_t bad = 0u, top = 0u;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t k = (kb >> (8 * j)) & 255u, v = (vb >> (8 * j)) & 255u;
-        f[j] = k == 255u ? 1.f : cache_scale(k);  // (more than 0: hidden scores of -inf stay -inf)
-        if (k == 255u || v == 255u) bad |= 1u << j;
-        if (v == 255u || j >= keys) vb &= ~(255u << (8 * j));  // (nothing)
-        top = max(top, (vb >> (8 * j)) & 255u);
-      }
-      *reinterpret_cast<float4 *>(&sh.k_scale[asked & 7][lane * 4]) = make_float4(f[0], f[1], f[2], f[3]);
-      *reinterpret_cast<uint32_t *>(&sh.v_scale[asked & 7][lane * 4]) = vb;
-      top = __reduce_max_sync(0xffffffffu, top);
-      if (__any_sync(0xffffffffu, bad != 0u)) {  // a bit a key: eight lanes a word
-        bad <<= 4 * (lane & 7);
+      for (int j = 0; j < 4; ++j) f[j] = __uint_as_float(__byte_perm(kb, 0, 0x0444 | j << 12) >> 1);  // 2^(byte - 127)
+      if (__any_sync(0xffffffffu, special)) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t k = (kb >> (8 * j)) & 255u, v = (vb >> (8 * j)) & 255u;
+          f[j] = k == 255u ? 1.f : cache_scale(k);  // (more than 0: hidden scores of -inf stay -inf)
+          if (k == 255u || v == 255u) bad |= 1u << j;
+          if (v == 255u || j >= keys) vb &= ~(255u << (8 * j));  // (nothing)
+        }
+        bad <<= 4 * (lane & 7);  // a bit a key: eight lanes a word
 #pragma unroll
         for (int o = 1; o < 8; o <<= 1) bad |= __shfl_xor_sync(0xffffffffu, bad, o);
       }
+      const uint32_t two = __vmaxu4(vb, vb >> 16), top = __reduce_max_sync(0xffffffffu, max(two & 255u, (two >> 8) & 255u));
+      *reinterpret_cast<float4 *>(&sh.k_scale[asked & 7][lane * 4]) = make_float4(f[0], f[1], f[2], f[3]);
+      *reinterpret_cast<uint32_t *>(&sh.v_scale[asked & 7][lane * 4]) = vb;
       if ((lane & 7) == 0) sh.bad[asked & 7][lane >> 3] = bad;
       if (lane == 0) sh.top[asked & 7] = max((int)top, 17);  // (where there is no value, the smallest scale's)
       __syncwarp();
