@@ -63,8 +63,6 @@ struct RowsParams {
 struct alignas(16) RowsShared {
   uint64_t full[kWarps][kMaxStages];
   alignas(16) uint8_t scales[kWarps][kMaxStages][64];  // e4m3: of the keys and of the values of a stage
-  alignas(16) float k_factor[kWarps][32];   // e4m3: what the scores of a warp's keys are to be multiplied by,
-  alignas(16) uint16_t v_factor[kWarps][32];  // and its values, in f16
   float2 l[kWarps][32];   // row sums and references
   long long total[kWarps];
   int longest[kWarps];
@@ -105,14 +103,21 @@ __device__ __forceinline__ void bulk_load(void *dst, const void *src, int bytes,
 }
 __device__ __forceinline__ bool not_finite(uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
 
-// Keys that a warp takes at a time (32 of them leave a lane too few registers for 32 rows, and for keys of 256 bytes the ring too few stages).
-__host__ __device__ constexpr int keys_of(int MT, bool e4m3) { return e4m3 && MT == 1 ? 32 : 16; }
+// The 8 x 8 matrix of 16-bit numbers that the warp holds, a row to four lanes, transposed.
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
+}
 
-template <int MT, bool E4m3>
+// Keys that a warp takes at a time (32 of them leave a lane too few registers for 32 rows, and for keys of 256 bytes the ring too few stages).
+__host__ __device__ constexpr int keys_of(int NT, bool e4m3) { return e4m3 && NT <= 2 ? 32 : 16; }
+
+template <int NT, bool E4m3>
 __global__ void __launch_bounds__(kThreads, 1)
     cache_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const RowsParams p) {
-  constexpr int kRows = 16 * MT;
-  constexpr int kKeys = keys_of(MT, E4m3), kStep = kWarps * kKeys, kTiles = kKeys / 8;  // keys a warp takes at a time, a step, products of 8 keys
+  constexpr int kRows = 8 * NT;
+  constexpr int kKeys = keys_of(NT, E4m3), kStep = kWarps * kKeys, kTiles = kKeys / 16;  // keys a warp takes at a time, a step, products of 16 keys
   constexpr int kKeysLog2 = kKeys == 32 ? 5 : 4;
   constexpr int kHalf = kKeys * kD * (E4m3 ? 1 : 2), kStage = 2 * kHalf, kStages = kRing / kStage;  // bytes of a warp's keys, or values
   static_assert(kStages <= kMaxStages, "barriers");
@@ -284,8 +289,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   int sinks, first;                                 // see Span
   int some_low, some_end, every_low, every_end;     // keys that some row sees, that every row does (besides the sinks)
   int next, next_batch, entry, entry_then;          // the warp's next copy; the batch of steps whose entries are in `entry`
-  uint32_t qf[MT][8][4];
-  float row_scale[MT][2];
+  uint32_t qf[NT][8][2];
   auto some = [&](int k0) { return k0 < some_end && (k0 + kKeys > some_low || k0 < ix.sink); };
   auto key_of = [&](int i) { return (i < sinks ? i : first + i - sinks) * kStep + warp * kKeys; };
   auto entries = [&](int at) {  // of the steps from `at` on
@@ -336,72 +340,73 @@ __global__ void __launch_bounds__(kThreads, 1)
     const Visible a = visible(ix, max(p0, 0), q.len), b = visible(ix, p1, q.len);
     some_low = a.low, some_end = p1 < 0 ? 0 : b.end;
     every_low = b.low, every_end = p0 < 0 ? 0 : a.end;
-    // The rows' queries as operands of the products: this lane's rows g and g + 8 of every 16.  (e4m3: the dims of a product are
+    // The rows' queries as operands of the products, this lane's the row g of every 8.  (e4m3: the dims of a product are
     // those that a lane finds together in a key's row, 32 * c + 4 * step + 0 .. 3; as bf16 here, made f16 below.)
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (int m = 0; m < NT; ++m) {
+      const int row = m * 8 + g;
+      const bool real = row < n_rows;
+      const int i = (first_row + row) / p.G, head = h * p.G + (first_row + row) % p.G;
+      const uint16_t *src = p.Q + (long long)(q.row + i) * p.qt + head * p.qh;
+      if (E4m3) {
 #pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const int row = m * 16 + r * 8 + g;
-        const bool real = row < n_rows;
-        const int i = (first_row + row) / p.G, head = h * p.G + (first_row + row) % p.G;
-        const uint16_t *src = p.Q + (long long)(q.row + i) * p.qt + head * p.qh;
-        if (E4m3) {
+        for (int k = 0; k < 4; ++k) {
+          const uint4 x = real ? *reinterpret_cast<const uint4 *>(src + c * 32 + k * 8) : make_uint4(0u, 0u, 0u, 0u);
+          qf[m][2 * k][0] = x.x;
+          qf[m][2 * k][1] = x.y;
+          qf[m][2 * k + 1][0] = x.z;
+          qf[m][2 * k + 1][1] = x.w;
+        }
+      } else {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const uint4 x = real ? *reinterpret_cast<const uint4 *>(src + c * 32 + k * 8) : make_uint4(0u, 0u, 0u, 0u);
-            qf[m][2 * k][r] = x.x;
-            qf[m][2 * k][2 + r] = x.y;
-            qf[m][2 * k + 1][r] = x.z;
-            qf[m][2 * k + 1][2 + r] = x.w;
-          }
-        } else {
-#pragma unroll
-          for (int ks = 0; ks < 8; ++ks) {
-            qf[m][ks][r] = real ? *reinterpret_cast<const uint32_t *>(src + ks * 16 + c * 2) : 0u;
-            qf[m][ks][2 + r] = real ? *reinterpret_cast<const uint32_t *>(src + ks * 16 + c * 2 + 8) : 0u;
-          }
+        for (int ks = 0; ks < 8; ++ks) {
+          qf[m][ks][0] = real ? *reinterpret_cast<const uint32_t *>(src + ks * 16 + c * 2) : 0u;
+          qf[m][ks][1] = real ? *reinterpret_cast<const uint32_t *>(src + ks * 16 + c * 2 + 8) : 0u;
         }
       }
+    }
 #pragma unroll 1
     for (int i = 0; i < kStages; ++i) issue();
   };
   start();
 
   for (;;) {
-    // rows that are none see everything (and nothing of theirs is kept)
-    Visible vis[MT][2];
+    // Of the scores and sums a lane has the rows 2c and 2c + 1 of every 8.  (Rows that are none see everything, and nothing of theirs is kept.)
+    Visible vis[NT][2];
+    float row_scale[NT][2];
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (int m = 0; m < NT; ++m) {
+      float scale = p.scale_log2;
+      if (E4m3) {
+        uint32_t top = 0u;
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) top = __vmaxu2(top, __vmaxu2(qf[m][ks][0] & 0x7fff7fffu, qf[m][ks][1] & 0x7fff7fffu));
+        top = max(top & 0xffffu, top >> 16);
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const int e = min(max((int)(top >> 7) - 127 - 14, -100), 120);  // the largest element: 2^14 * 2^e to 2^15 * 2^e
+        const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+        scale = top < 0x7f80u ? scale * __uint_as_float((uint32_t)(127 + e) << 23) : __uint_as_float(0x7fc00000u);
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const uint32_t w = qf[m][ks][k];
+            qf[m][ks][k] = pack_f16x2(__uint_as_float(w << 16) * inv, __uint_as_float(w & 0xffff0000u) * inv);
+          }
+      }
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
-        const int row = m * 16 + r * 8 + g;
+        const int row = m * 8 + c * 2 + r;
+        row_scale[m][r] = E4m3 ? __shfl_sync(0xffffffffu, scale, (c * 2 + r) * 4) : scale;
         vis[m][r] = row < n_rows ? visible(ix, q.len - q.n + (first_row + row) / p.G, q.len) : Visible{0, 0x7fffffff};
-        row_scale[m][r] = p.scale_log2;
-        if (E4m3) {
-          uint32_t top = 0u;
-#pragma unroll
-          for (int ks = 0; ks < 8; ++ks) top = __vmaxu2(top, __vmaxu2(qf[m][ks][r] & 0x7fff7fffu, qf[m][ks][2 + r] & 0x7fff7fffu));
-          top = max(top & 0xffffu, top >> 16);
-          top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-          top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-          const int e = min(max((int)(top >> 7) - 127 - 14, -100), 120);  // the largest element: 2^14 * 2^e to 2^15 * 2^e
-          const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
-          row_scale[m][r] = top < 0x7f80u ? p.scale_log2 * __uint_as_float((uint32_t)(127 + e) << 23) : __uint_as_float(0x7fc00000u);
-#pragma unroll
-          for (int ks = 0; ks < 8; ++ks)
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              const uint32_t w = qf[m][ks][2 * k + r];
-              qf[m][ks][2 * k + r] = pack_f16x2(__uint_as_float(w << 16) * inv, __uint_as_float(w & 0xffff0000u) * inv);
-            }
-        }
       }
-    float o[MT][16][4] = {};
-    float ref[MT][2], sum[MT][2];
+    }
+    float o[NT][8][4] = {};
+    float ref[NT][2], sum[NT][2];
     uint32_t v_exp = 0;  // e4m3: O stands for 2^(v_exp - 127) of its value
 #pragma unroll
-    for (int m = 0; m < MT; ++m) ref[m][0] = ref[m][1] = kNoReference, sum[m][0] = sum[m][1] = 0.f;
+    for (int m = 0; m < NT; ++m) ref[m][0] = ref[m][1] = kNoReference, sum[m][0] = sum[m][1] = 0.f;
 
 #pragma unroll 1
     for (int i = done; i < end_step; ++i) {
@@ -412,95 +417,88 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!ok) break;
       const uint32_t k_at = ring_at + take * kStage, v_at = k_at + kHalf;
       const bool whole = k0 + kKeys <= every_end && (k0 >= every_low || k0 + kKeys <= ix.sink);
-      float x[MT][kTiles][4] = {};
-      uint32_t vs[kTiles];  // e4m3: this lane's values are to be multiplied by these, two keys at a time
-      // ---- scores
+      float x[NT][kTiles][4] = {};
+      uint32_t vs[kTiles][2];  // e4m3: this lane's values are to be multiplied by these, two keys at a time
+      // ---- scores: keys g and g + 8 of every 16, rows 2c and 2c + 1
       if (E4m3) {
-        {
-          // the scales, a lane a key, as numbers for all lanes: 2^e of the key (NaN where the token's key or value is not finite), 2^(e - E) of
-          // the value (nothing behind the sequence's end and where it is not finite)
-          const int key = lane & (kKeys - 1);
-          const uint32_t kb = sh.scales[warp][take][key];
-          uint32_t vb = sh.scales[warp][take][kKeys + key];
-          const float k_scale = cache_scale(vb == 255u ? 255u : kb);
-          if (vb == 255u || k0 + key >= q.len) vb = 0u;
-          const uint32_t top = __reduce_max_sync(0xffffffffu, vb);
-          if (top > v_exp) {
-            const float f = cache_scale(max((int)(v_exp - top) + 127, 1));
-            v_exp = top;
+        // the scales, a lane a key: 2^e of the key (NaN where the token's key or value is not finite), 2^(e - E) of the value (nothing behind the
+        // sequence's end and where it is not finite)
+        const int key = lane & (kKeys - 1);
+        const uint32_t kb = sh.scales[warp][take][key];
+        uint32_t vb = sh.scales[warp][take][kKeys + key];
+        const float k_scale = cache_scale(vb == 255u ? 255u : kb);
+        if (vb == 255u || k0 + key >= q.len) vb = 0u;
+        const uint32_t top = __reduce_max_sync(0xffffffffu, vb);
+        if (top > v_exp) {
+          const float f = cache_scale(max((int)(v_exp - top) + 127, 1));
+          v_exp = top;
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
+          for (int m = 0; m < NT; ++m)
 #pragma unroll
-              for (int n = 0; n < 16; ++n)
+            for (int n = 0; n < 8; ++n)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) o[m][n][k] *= f;
-          }
-          const float v_scale = vb == 0u ? 0.f : cache_scale(max((int)(vb - v_exp) + 127, 1));
-          if (lane < kKeys) {
-            sh.k_factor[warp][lane] = k_scale;
-            sh.v_factor[warp][lane] = (uint16_t)pack_f16x2(v_scale, 0.f);
-          }
-          __syncwarp();
+              for (int k = 0; k < 4; ++k) o[m][n][k] *= f;
         }
+        const float v_scale = vb == 0u ? 0.f : cache_scale(max((int)(vb - v_exp) + 127, 1));
+        const uint32_t pair = pack_f16x2(v_scale, __shfl_down_sync(0xffffffffu, v_scale, 1));
 #pragma unroll
-        for (int n = 0; n < kTiles; ++n) {
+        for (int t = 0; t < kTiles; ++t) {
+          vs[t][0] = __shfl_sync(0xffffffffu, pair, t * 16 + c * 2);
+          vs[t][1] = __shfl_sync(0xffffffffu, pair, t * 16 + 8 + c * 2);
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            const uint4 w = lds_u4(k_at + (n * 8 + g) * 128 + (((c * 2 + j) ^ g) << 4));
-            const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+            const uint4 lo = lds_u4(k_at + (t * 16 + g) * 128 + (((c * 2 + j) ^ g) << 4)), hi = lds_u4(k_at + (t * 16 + 8 + g) * 128 + (((c * 2 + j) ^ g) << 4));
+            const uint32_t l[4] = {lo.x, lo.y, lo.z, lo.w}, u[4] = {hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              const uint32_t b0 = codes_to_f16x2(ws[k]), b1 = high_codes_to_f16x2(ws[k]);
+              const uint32_t a[4] = {codes_to_f16x2(l[k]), codes_to_f16x2(u[k]), high_codes_to_f16x2(l[k]), high_codes_to_f16x2(u[k])};
 #pragma unroll
-              for (int m = 0; m < MT; ++m) mma_f16(x[m][n], qf[m][j * 4 + k], b0, b1);
+              for (int m = 0; m < NT; ++m) mma_f16(x[m][t], a, qf[m][j * 4 + k][0], qf[m][j * 4 + k][1]);
             }
           }
-          const float2 f = *reinterpret_cast<const float2 *>(&sh.k_factor[warp][n * 8 + c * 2]);
-          vs[n] = *reinterpret_cast<const uint32_t *>(&sh.v_factor[warp][n * 8 + c * 2]);
+          const float f_lo = __shfl_sync(0xffffffffu, k_scale, t * 16 + g), f_hi = __shfl_sync(0xffffffffu, k_scale, t * 16 + 8 + g);
 #pragma unroll
-          for (int m = 0; m < MT; ++m) {
-            x[m][n][0] *= f.x;
-            x[m][n][1] *= f.y;
-            x[m][n][2] *= f.x;
-            x[m][n][3] *= f.y;
+          for (int m = 0; m < NT; ++m) {
+            x[m][t][0] *= f_lo;
+            x[m][t][1] *= f_lo;
+            x[m][t][2] *= f_hi;
+            x[m][t][3] *= f_hi;
           }
         }
       } else {
-        const int key = ((lane >> 4) << 3) + (lane & 7);
+        const int key = lane & 15;
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) {
-          const int chunk = ks * 2 + ((lane >> 3) & 1);
-          uint32_t b[4];
-          ldmatrix4(b, k_at + (chunk >> 3) * 2048 + key * 128 + (((chunk ^ key) & 7) << 4));
+          const int chunk = ks * 2 + (lane >> 4);
+          uint32_t a[4];
+          ldmatrix4(a, k_at + (chunk >> 3) * 2048 + key * 128 + (((chunk ^ key) & 7) << 4));
 #pragma unroll
-          for (int m = 0; m < MT; ++m) {
-            mma_bf16(x[m][0], qf[m][ks], b[0], b[1]);
-            mma_bf16(x[m][1], qf[m][ks], b[2], b[3]);
-          }
+          for (int m = 0; m < NT; ++m) mma_bf16(x[m][0], a, qf[m][ks][0], qf[m][ks][1]);
         }
       }
       // ---- weights
       auto hidden = [&](const Visible &v, int k) { return k >= v.end || (k < v.low && k >= ix.sink); };
       if (!whole) {
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int m = 0; m < NT; ++m)
 #pragma unroll
-          for (int n = 0; n < kTiles; ++n)
+          for (int t = 0; t < kTiles; ++t)
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-              if (hidden(vis[m][k >> 1], k0 + n * 8 + c * 2 + (k & 1))) x[m][n][k] = -INFINITY;
+              if (hidden(vis[m][k & 1], k0 + t * 16 + g + (k >> 1) * 8)) x[m][t][k] = -INFINITY;
       }
       bool moved = false;
-      float alpha[MT][2];
+      float alpha[NT][2];
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
+      for (int m = 0; m < NT; ++m)
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           float top = -INFINITY;
 #pragma unroll
-          for (int n = 0; n < kTiles; ++n) top = fmaxf(top, fmaxf(x[m][n][2 * r], x[m][n][2 * r + 1]));
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+          for (int t = 0; t < kTiles; ++t) top = fmaxf(top, fmaxf(x[m][t][r], x[m][t][2 + r]));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
           top *= row_scale[m][r];
           alpha[m][r] = 1.f;
           if (top > ref[m][r] + (E4m3 ? kHeadroomE4m3 : 0.f) + kMaxGrowth) {
@@ -512,37 +510,34 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
+        for (int m = 0; m < NT; ++m) {
           sum[m][0] *= alpha[m][0];
           sum[m][1] *= alpha[m][1];
 #pragma unroll
-          for (int n = 0; n < 16; ++n) {
-            o[m][n][0] *= alpha[m][0];
-            o[m][n][1] *= alpha[m][0];
-            o[m][n][2] *= alpha[m][1];
-            o[m][n][3] *= alpha[m][1];
-          }
+          for (int n = 0; n < 8; ++n)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) o[m][n][k] *= alpha[m][k & 1];
         }
       }
-      uint32_t pf[MT][kTiles / 2][4];
+      uint32_t pf[NT][kTiles][2];  // as operands: row g, keys 2c, 2c + 1 of every 8
       auto weights = [&](auto masked) {
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int m = 0; m < NT; ++m)
 #pragma unroll
-          for (int n = 0; n < kTiles; ++n)
+          for (int t = 0; t < kTiles; ++t) {
+            float w[4];
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-              float w[2];
-#pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                const float y = x[m][n][2 * r + k];
-                w[k] = ex2(fmaf(y, row_scale[m][r], -ref[m][r]));
-                // (what is hidden is nothing, even to a query that is not finite)
-                if (decltype(masked)::value && y == -INFINITY) w[k] = 0.f;
-                sum[m][r] += w[k];
-              }
-              pf[m][n >> 1][(n & 1) * 2 + r] = E4m3 ? pack_f16x2(w[0], w[1]) : pack_bf16x2(w[0], w[1]);
+            for (int k = 0; k < 4; ++k) {
+              const float y = x[m][t][k];
+              w[k] = ex2(fmaf(y, row_scale[m][k & 1], -ref[m][k & 1]));
+              // (what is hidden is nothing, even to a query that is not finite)
+              if (decltype(masked)::value && y == -INFINITY) w[k] = 0.f;
             }
+            sum[m][0] += w[0] + w[2];
+            sum[m][1] += w[1] + w[3];
+            pf[m][t][0] = transposed(E4m3 ? pack_f16x2(w[0], w[1]) : pack_bf16x2(w[0], w[1]));
+            pf[m][t][1] = transposed(E4m3 ? pack_f16x2(w[2], w[3]) : pack_bf16x2(w[2], w[3]));
+          }
       };
       if (E4m3 && !whole) weights(True{});
       else weights(False{});
@@ -566,47 +561,42 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (uint32_t todo = bad; todo; todo &= todo - 1) {
             const int key = k0 + __ffs(todo) - 1;
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
+            for (int m = 0; m < NT; ++m)
 #pragma unroll
               for (int r = 0; r < 2; ++r)
                 if (!hidden(vis[m][r], key)) sum[m][r] = __uint_as_float(0x7fc00000u);
           }
         }
       }
-      // ---- values
+      // ---- values: of every 16 dims the dims g and g + 8 (e4m3: 2g and 2g + 1), rows 2c and 2c + 1
 #pragma unroll
-      for (int b16 = 0; b16 < kTiles / 2; ++b16) {  // 16 keys each
-        const int key = lane & 15;
+      for (int t = 0; t < kTiles; ++t) {
         if (E4m3) {
+          const int key = lane & 15;
 #pragma unroll
-          for (int j = 0; j < 8; j += 2) {  // 16 dims each: even ones and odd ones
+          for (int j = 0; j < 8; j += 2) {
             uint32_t b[4];
             const int chunk = j + (lane >> 4);
-            ldmatrix4_trans(b, v_at + b16 * 2048 + key * 128 + (((chunk ^ key) & 7) << 4));
+            ldmatrix4_trans(b, v_at + t * 2048 + key * 128 + (((chunk ^ key) & 7) << 4));
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
               // codes of two dims of a key and of the next: the even dims of both, the odd ones
               const uint32_t lo = __byte_perm(b[2 * k], 0, 0x3120), hi = __byte_perm(b[2 * k + 1], 0, 0x3120);
-              const uint32_t e0 = mul_f16x2(codes_to_f16x2(lo), vs[b16 * 2]), o0 = mul_f16x2(high_codes_to_f16x2(lo), vs[b16 * 2]);
-              const uint32_t e1 = mul_f16x2(codes_to_f16x2(hi), vs[b16 * 2 + 1]), o1 = mul_f16x2(high_codes_to_f16x2(hi), vs[b16 * 2 + 1]);
+              const uint32_t a[4] = {mul_f16x2(codes_to_f16x2(lo), vs[t][0]), mul_f16x2(high_codes_to_f16x2(lo), vs[t][0]),
+                                     mul_f16x2(codes_to_f16x2(hi), vs[t][1]), mul_f16x2(high_codes_to_f16x2(hi), vs[t][1])};
 #pragma unroll
-              for (int m = 0; m < MT; ++m) {
-                mma_f16(o[m][(j + k) * 2], pf[m][b16], e0, e1);
-                mma_f16(o[m][(j + k) * 2 + 1], pf[m][b16], o0, o1);
-              }
+              for (int m = 0; m < NT; ++m) mma_f16(o[m][j + k], a, pf[m][t][0], pf[m][t][1]);
             }
           }
         } else {
+          const int key = (lane >> 4) * 8 + (lane & 7);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {  // 16 dims each
-            uint32_t b[4];
-            const int chunk = j * 2 + (lane >> 4);
-            ldmatrix4_trans(b, v_at + (chunk >> 3) * 2048 + key * 128 + (((chunk ^ key) & 7) << 4));
+          for (int j = 0; j < 8; ++j) {
+            uint32_t a[4];
+            const int chunk = j * 2 + ((lane >> 3) & 1);
+            ldmatrix4_trans(a, v_at + (chunk >> 3) * 2048 + key * 128 + (((chunk ^ key) & 7) << 4));
 #pragma unroll
-            for (int m = 0; m < MT; ++m) {
-              mma_bf16(o[m][j * 2], pf[m][b16], b[0], b[1]);
-              mma_bf16(o[m][j * 2 + 1], pf[m][b16], b[2], b[3]);
-            }
+            for (int m = 0; m < NT; ++m) mma_bf16(o[m][j], a, pf[m][t][0], pf[m][t][1]);
           }
         }
       }
@@ -625,40 +615,30 @@ __global__ void __launch_bounds__(kThreads, 1)
         take = take + 1 == kStages ? 0 : take + 1;
       }
     }
-    if (E4m3) {
-      const float f = cache_scale(v_exp);
-#pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int n = 0; n < 16; ++n)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) o[m][n][k] *= f;
-    }
     // ---------------------------------------------------------------- the warps' sums put together
     // A few rows have a place of their own, and the next tile's first copies go out ahead of this; more rows lie where the copies were.
     // (Pieces of 32 bytes are swizzled by the row.)
-    const bool apart = MT == 1 && n_rows <= kApartRows;
+    const bool apart = NT <= 2 && n_rows <= kApartRows;
     unsigned char *sums = apart ? smem + kWarps * kRing + sizeof(RowsShared) : smem;
     const int sums_pitch = apart ? kApartRows * 512 : kRing;
+    const float o_scale = E4m3 ? cache_scale(v_exp) : 1.f;
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (int m = 0; m < NT; ++m)
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
-        sum[m][r] += __shfl_xor_sync(0xffffffffu, sum[m][r], 1);
-        sum[m][r] += __shfl_xor_sync(0xffffffffu, sum[m][r], 2);
-        const int row = m * 16 + r * 8 + g;
+#pragma unroll
+        for (int k = 4; k < 32; k <<= 1) sum[m][r] += __shfl_xor_sync(0xffffffffu, sum[m][r], k);
+        const int row = m * 8 + c * 2 + r;
         if (row >= n_rows) continue;
-        if (c == 0) sh.l[warp][row] = make_float2(sum[m][r], ref[m][r]);
+        if (g == 0) sh.l[warp][row] = make_float2(sum[m][r], ref[m][r]);
         unsigned char *to = sums + warp * sums_pitch + row * 512;
 #pragma unroll
-        for (int n = 0; n < 16; ++n) {
-          // dims of these two columns: e4m3 products take even and odd dims of 16 apart
+        for (int n = 0; n < 8; ++n) {
           if (E4m3) {
-            if (n & 1) continue;
-            *reinterpret_cast<float4 *>(to + ((n * 32 + c * 16) ^ ((row & 7) << 5))) =
-                make_float4(o[m][n][r * 2], o[m][n + 1][r * 2], o[m][n][r * 2 + 1], o[m][n + 1][r * 2 + 1]);
+            *reinterpret_cast<float2 *>(to + ((n * 64 + g * 8) ^ ((row & 7) << 5))) = make_float2(o[m][n][r] * o_scale, o[m][n][2 + r] * o_scale);
           } else {
-            *reinterpret_cast<float2 *>(to + ((n * 32 + c * 8) ^ ((row & 7) << 5))) = make_float2(o[m][n][r * 2], o[m][n][r * 2 + 1]);
+            *reinterpret_cast<float *>(to + ((n * 64 + g * 4) ^ ((row & 7) << 5))) = o[m][n][r];
+            *reinterpret_cast<float *>(to + ((n * 64 + 32 + g * 4) ^ ((row & 7) << 5))) = o[m][n][2 + r];
           }
         }
       }
@@ -787,20 +767,20 @@ bool make_pool_map(CUtensorMap *m, const void *base, const CacheGeom &g, int row
 
 namespace {
 
-template <int MT, bool E4m3>
+template <int NT, bool E4m3>
 cudaError_t launch(const CacheGeom &g, const RowsParams &p, const CUtensorMap &mk, const CUtensorMap &mv, cudaStream_t s, int *launches) {
-  cudaError_t e = allow_shared_memory(cache_rows_kernel<MT, E4m3>, kRowsSmem);
+  cudaError_t e = allow_shared_memory(cache_rows_kernel<NT, E4m3>, kRowsSmem);
   if (e != cudaSuccess) return e;
   ++*launches;
-  return launch_pdl(cache_rows_kernel<MT, E4m3>, dim3(kCacheCtas), dim3(kThreads), kRowsSmem, s, mk, mv, p);
+  return launch_pdl(cache_rows_kernel<NT, E4m3>, dim3(kCacheCtas), dim3(kThreads), kRowsSmem, s, mk, mv, p);
 }
 
 }  // namespace
 
 cudaError_t launch_cache_rows(const CacheGeom &g, const CacheIndex &ix, const CacheWorkspace &w, const void *Q, const heart_cache &c,
                               void *O, float *lse, cudaStream_t s, int *launches) {
-  const bool two = (long long)g.max_new * g.G > 16;
-  const int box = g.page < keys_of(two ? 2 : 1, g.e4m3) ? g.page : keys_of(two ? 2 : 1, g.e4m3);
+  const long long rows = (long long)g.max_new * g.G;
+  const int NT = rows <= 8 ? 1 : rows <= 16 ? 2 : 4, box = g.page < keys_of(NT, g.e4m3) ? g.page : keys_of(NT, g.e4m3);
   CUtensorMap mk, mv;
   if (!make_pool_map(&mk, c.k, g, box, 2) || !make_pool_map(&mv, c.v, g, box, 2)) return cudaErrorInvalidValue;
   RowsParams p = {};
@@ -819,8 +799,9 @@ cudaError_t launch_cache_rows(const CacheGeom &g, const CacheIndex &ix, const Ca
   p.arrivals = w.arrivals;
   p.parts = w.parts;
   p.part_l = w.part_l;
-  if (g.e4m3) return two ? launch<2, true>(g, p, mk, mv, s, launches) : launch<1, true>(g, p, mk, mv, s, launches);
-  return two ? launch<2, false>(g, p, mk, mv, s, launches) : launch<1, false>(g, p, mk, mv, s, launches);
+  if (g.e4m3)
+    return NT == 1 ? launch<1, true>(g, p, mk, mv, s, launches) : NT == 2 ? launch<2, true>(g, p, mk, mv, s, launches) : launch<4, true>(g, p, mk, mv, s, launches);
+  return NT == 1 ? launch<1, false>(g, p, mk, mv, s, launches) : NT == 2 ? launch<2, false>(g, p, mk, mv, s, launches) : launch<4, false>(g, p, mk, mv, s, launches);
 }
 
 }  // namespace heart
