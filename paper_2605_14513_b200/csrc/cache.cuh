@@ -68,8 +68,9 @@ cudaError_t launch_cache_write(const CacheGeom &g, const CacheIndex &ix, const v
                                cudaStream_t s, int *launches);
 cudaError_t launch_cache_read(const CacheGeom &g, const CacheIndex &ix, const heart_cache &c, void *K, void *V, cudaStream_t s,
                               int *launches);
-// Attention by 16 or 32 query rows in registers, or by tiles of 128: the former where a sequence and key head has so few rows.
-constexpr int kRowsOfRowsKernel = 32;
+// Attention by 8 or 16 query rows in registers, or by tiles of 128: the former where a sequence and key head has so few rows.  (20 sequences of 4000
+// tokens, 32 heads on 8, bf16: four new tokens, 16 rows, 71 us; eight, 32 rows, 189 by rows and 75 by tiles.)
+constexpr int kRowsOfRowsKernel = 16;
 cudaError_t launch_cache_rows(const CacheGeom &g, const CacheIndex &ix, const CacheWorkspace &w, const void *Q, const heart_cache &c,
                               void *O, float *lse, cudaStream_t s, int *launches);
 cudaError_t launch_cache_tiles(const CacheGeom &g, const CacheIndex &ix, const CacheWorkspace &w, const void *Q, const heart_cache &c,

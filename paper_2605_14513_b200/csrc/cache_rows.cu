@@ -1,11 +1,12 @@
-// Attention over a paged cache for few query rows a sequence and key head: single tokens, drafted tokens, and any rows at all
-// as the plainest of the kernels.
+// Attention over a paged cache for few query rows a sequence and key head: single tokens and drafted tokens.
 //
-// Every key and value is read once and used by 16 or 32 rows, so HBM bounds it: the products of 16 rows x 128 keys take 500
-// clocks of the warp-wide matrix instruction an SM, the 64 KB of the keys and values 2800 (bf16; 1400 as e4m3).  So the design is
+// Every key and value is read once and used by 8 or 16 rows, so HBM bounds it: a step of 128 keys is 64 KB, 2800 clocks of an SM's share of
+// the bandwidth (1400 as e4m3), and its products take 256 clocks of the warp-wide matrix instruction for every 8 rows.  So the design is
 // about bytes in flight: one CTA an SM, eight warps, each with a ring of its own of 24 KB that tensor copies fill.  A warp takes 16 of
-// every 128 keys (32 of 256 where they are e4m3 and the rows 16), with the running maximum and sum of its own keys, so nothing but the warp's own barrier is waited for
-// until a tile's end.
+// every 128 keys (32 of 256 where they are e4m3), with the running maximum and sum of its own keys, so nothing but the warp's own barrier is
+// waited for until a tile's end.  Keys and values are the first operands of the products, rows the second: a product has 16 of the former and 8 of
+// the latter, and most calls have no more rows.  (Rows first, 16 of them: 20 x 8001 tokens e4m3, 32 heads on 8, 91 us, now 75; 12 warps with
+// smaller rings 74, and one token over 4k 11.5 us instead of 10.8.)
 //
 // With eight warps an SM what comes next are instructions: 900 for 16 keys, converting keys and values from e4m3 to bf16, took 4700 clocks.
 // The conversion to f16 is one instruction for two codes, so e4m3 caches are multiplied in f16, which holds codes exactly:
@@ -16,11 +17,11 @@
 //     largest value below.  E moves O as a row's reference does.
 // (The warp-wide products of e4m3 codes themselves are carried out as conversions and f16 products here, 96 for the 64 in the source.)
 //
-// Work: rows of a sequence and key head, packed as (token, query head of the group), in tiles of 16 or 32; a tile's key steps are
-// 128 tokens each.  All steps of all tiles in one line, (sequence, head, tile, step), are cut into equal shares, one a CTA; what a
-// CTA has of a tile that it does not have whole goes to the workspace, and the CTA that brings the last part puts the tile together, its
-// parts in order: the result does not depend on which one came last.  Every CTA finds its share by itself from the sequences' lengths, so
-// the launch needs no plan and no lengths on the host, and a captured one follows the lengths.
+// Work: rows of a sequence and key head, packed as (token, query head of the group), in tiles of 8 or 16; all key steps of all tiles in one line,
+// (sequence, head, tile, step), are cut into equal shares, one a CTA; what a CTA has of a tile that it does not have whole goes to the
+// workspace, and the CTA that brings the last part puts the tile together, its parts in order: the result does not depend on which
+// one came last.  Every CTA finds its share by itself from the sequences' lengths, so the launch needs no plan and no lengths on the host, and a
+// captured one follows the lengths.
 #include <cuda.h>
 
 #include "cache.cuh"
@@ -32,7 +33,7 @@ namespace {
 
 constexpr int kWarps = 8, kThreads = 32 * kWarps;
 constexpr int kRing = 24576;           // bytes a warp
-constexpr int kMaxStages = 6;
+constexpr int kMaxStages = 3;
 constexpr int kMaxParts = 31;          // of a tile, and one more where shares cross tiles: the last CTA reads them, a lane a part
 constexpr int kApartRows = 6;          // rows of a tile whose sums have a place beside the rings
 constexpr float kNoReference = -3.0e38f;
@@ -63,7 +64,7 @@ struct RowsParams {
 struct alignas(16) RowsShared {
   uint64_t full[kWarps][kMaxStages];
   alignas(16) uint8_t scales[kWarps][kMaxStages][64];  // e4m3: of the keys and of the values of a stage
-  float2 l[kWarps][32];   // row sums and references
+  float2 l[kWarps][16];   // row sums and references
   long long total[kWarps];
   int longest[kWarps];
   int found;              // sequence of the CTA's first step
@@ -110,14 +111,14 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
   return r;
 }
 
-// Keys that a warp takes at a time (32 of them leave a lane too few registers for 32 rows, and for keys of 256 bytes the ring too few stages).
-__host__ __device__ constexpr int keys_of(int NT, bool e4m3) { return e4m3 && NT <= 2 ? 32 : 16; }
+// Keys that a warp takes at a time, 4 KB of them.
+__host__ __device__ constexpr int keys_of(bool e4m3) { return e4m3 ? 32 : 16; }
 
 template <int NT, bool E4m3>
 __global__ void __launch_bounds__(kThreads, 1)
     cache_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const RowsParams p) {
   constexpr int kRows = 8 * NT;
-  constexpr int kKeys = keys_of(NT, E4m3), kStep = kWarps * kKeys, kTiles = kKeys / 16;  // keys a warp takes at a time, a step, products of 16 keys
+  constexpr int kKeys = keys_of(E4m3), kStep = kWarps * kKeys, kTiles = kKeys / 16;  // keys a warp takes at a time, a step, products of 16 keys
   constexpr int kKeysLog2 = kKeys == 32 ? 5 : 4;
   constexpr int kHalf = kKeys * kD * (E4m3 ? 1 : 2), kStage = 2 * kHalf, kStages = kRing / kStage;  // bytes of a warp's keys, or values
   static_assert(kStages <= kMaxStages, "barriers");
@@ -618,7 +619,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ---------------------------------------------------------------- the warps' sums put together
     // A few rows have a place of their own, and the next tile's first copies go out ahead of this; more rows lie where the copies were.
     // (Pieces of 32 bytes are swizzled by the row.)
-    const bool apart = NT <= 2 && n_rows <= kApartRows;
+    const bool apart = n_rows <= kApartRows;
     unsigned char *sums = apart ? smem + kWarps * kRing + sizeof(RowsShared) : smem;
     const int sums_pitch = apart ? kApartRows * 512 : kRing;
     const float o_scale = E4m3 ? cache_scale(v_exp) : 1.f;
@@ -779,8 +780,7 @@ cudaError_t launch(const CacheGeom &g, const RowsParams &p, const CUtensorMap &m
 
 cudaError_t launch_cache_rows(const CacheGeom &g, const CacheIndex &ix, const CacheWorkspace &w, const void *Q, const heart_cache &c,
                               void *O, float *lse, cudaStream_t s, int *launches) {
-  const long long rows = (long long)g.max_new * g.G;
-  const int NT = rows <= 8 ? 1 : rows <= 16 ? 2 : 4, box = g.page < keys_of(NT, g.e4m3) ? g.page : keys_of(NT, g.e4m3);
+  const int NT = (long long)g.max_new * g.G <= 8 ? 1 : 2, box = g.page < keys_of(g.e4m3) ? g.page : keys_of(g.e4m3);
   CUtensorMap mk, mv;
   if (!make_pool_map(&mk, c.k, g, box, 2) || !make_pool_map(&mv, c.v, g, box, 2)) return cudaErrorInvalidValue;
   RowsParams p = {};
@@ -799,9 +799,8 @@ cudaError_t launch_cache_rows(const CacheGeom &g, const CacheIndex &ix, const Ca
   p.arrivals = w.arrivals;
   p.parts = w.parts;
   p.part_l = w.part_l;
-  if (g.e4m3)
-    return NT == 1 ? launch<1, true>(g, p, mk, mv, s, launches) : NT == 2 ? launch<2, true>(g, p, mk, mv, s, launches) : launch<4, true>(g, p, mk, mv, s, launches);
-  return NT == 1 ? launch<1, false>(g, p, mk, mv, s, launches) : NT == 2 ? launch<2, false>(g, p, mk, mv, s, launches) : launch<4, false>(g, p, mk, mv, s, launches);
+  if (g.e4m3) return NT == 1 ? launch<1, true>(g, p, mk, mv, s, launches) : launch<2, true>(g, p, mk, mv, s, launches);
+  return NT == 1 ? launch<1, false>(g, p, mk, mv, s, launches) : launch<2, false>(g, p, mk, mv, s, launches);
 }
 
 }  // namespace heart
