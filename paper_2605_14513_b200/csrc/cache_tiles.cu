@@ -208,6 +208,7 @@ __global__ void __launch_bounds__(1024) cache_plan_kernel(const CacheIndex ix, i
   __shared__ long long sums[32];
   __shared__ int base[1024];
   __shared__ int steps[kSmallPlan];  // of the first tiles: as a rule all
+  __shared__ Sequence own[32];
   auto steps_of = [&](int i) { return i < kSmallPlan ? steps[i] : tiles[i].steps; };
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
   pdl_wait();
@@ -233,47 +234,84 @@ __global__ void __launch_bounds__(1024) cache_plan_kernel(const CacheIndex ix, i
   };
   int n_tiles = 0, longest = 1;
   long long tokens = 0;  // of the sequences with tiles
-  for (int s0 = 0; s0 < ix.S; s0 += 1024) {
-    const Sequence own = s0 + t < ix.S ? sequence(ix, s0 + t) : Sequence{0, 0, 0};
-    const int mine = (own.n + tokens_per_tile - 1) / tokens_per_tile;
-    long long all;
-    scan(mine > 0 ? own.len : 0, all);
-    tokens += all;
-    base[t] = (int)min(n_tiles + scan(mine, all), (long long)most);
-    __syncthreads();
-    for (int i = warp; i < 1024 && s0 + i < ix.S; i += 32) {  // a warp a sequence
-      const Sequence q = sequence(ix, s0 + i);
-      for (int k = lane; k * tokens_per_tile < q.n && base[i] + k < most; k += 32) {
-        Tile x;
-        x.s = s0 + i;
-        x.row = q.row + k * tokens_per_tile;
-        x.tokens = min(tokens_per_tile, q.n - k * tokens_per_tile);
-        x.p0 = q.len - q.n + k * tokens_per_tile;
-        x.len = q.len;
-        const Span<> sp = span_of(ix, x.p0, x.p0 + x.tokens - 1, q.len);
-        x.sinks = sp.sinks;
-        x.first = sp.first;
-        x.steps = sp.steps;
-        const Visible v0 = visible(ix, max(x.p0, 0), q.len), v1 = visible(ix, x.p0 + x.tokens - 1, q.len);
-        x.every_low = v1.low;
-        x.every_end = x.p0 >= 0 ? v0.end : 0;
-        x.some_low = v0.low;
-        x.some_end = v1.end;
-        tiles[base[i] + k] = x;
-        if (base[i] + k < kSmallPlan) steps[base[i] + k] = sp.steps;
-      }
-    }
-    n_tiles = (int)min(n_tiles + all, (long long)most);  // (more: starts that do not ascend, which are reported)
-    __syncthreads();
-  }
+  auto make_tile = [&](int i, int s, const Sequence &q, int k) {
+    Tile x;
+    x.s = s;
+    x.row = q.row + k * tokens_per_tile;
+    x.tokens = min(tokens_per_tile, q.n - k * tokens_per_tile);
+    x.p0 = q.len - q.n + k * tokens_per_tile;
+    x.len = q.len;
+    const Span<> sp = span_of(ix, x.p0, x.p0 + x.tokens - 1, q.len);
+    x.sinks = sp.sinks;
+    x.first = sp.first;
+    x.steps = sp.steps;
+    const Visible v0 = visible(ix, max(x.p0, 0), q.len), v1 = visible(ix, x.p0 + x.tokens - 1, q.len);
+    x.every_low = v1.low;
+    x.every_end = x.p0 >= 0 ? v0.end : 0;
+    x.some_low = v0.low;
+    x.some_end = v1.end;
+    tiles[i] = x;
+    if (i < kSmallPlan) steps[i] = sp.steps;
+    return sp.steps;
+  };
   long long before = 0;
-  for (int t0 = 0; t0 < n_tiles; t0 += 1024) {
-    const int mine = t0 + t < n_tiles ? steps_of(t0 + t) : 0;
-    longest = max(longest, mine);
-    long long all;
-    const long long at = before + scan(mine, all);
-    if (t0 + t < n_tiles) first[t0 + t] = at;
-    before += all;
+  if (ix.S <= 32) {  // a lane a sequence, then a thread a tile
+    const Sequence q = lane < ix.S ? sequence(ix, lane) : Sequence{0, 0, 0};
+    const int mine = (q.n + tokens_per_tile - 1) / tokens_per_tile;
+    long long upto = mine, sum = mine > 0 ? q.len : 0;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += y;
+      sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    }
+    tokens = sum;
+    n_tiles = (int)min(__shfl_sync(0xffffffffu, upto, 31), (long long)most);
+    if (warp == 0) {
+      base[lane] = (int)min(upto - mine, (long long)most);
+      own[lane] = q;
+    }
+    __syncthreads();
+    for (int t0 = 0; t0 < n_tiles; t0 += 1024) {
+      const int i = t0 + t;
+      int here = 0;
+      if (i < n_tiles) {
+        int s = 0;  // the last sequence whose tiles begin at i or before
+#pragma unroll
+        for (int o = 16; o; o >>= 1)
+          if (s + o < ix.S && base[s + o] <= i) s += o;
+        here = make_tile(i, s, own[s], i - base[s]);
+      }
+      longest = max(longest, here);
+      long long all;
+      const long long at = before + scan(here, all);
+      if (i < n_tiles) first[i] = at;
+      before += all;
+    }
+  } else {
+    for (int s0 = 0; s0 < ix.S; s0 += 1024) {
+      const Sequence q = s0 + t < ix.S ? sequence(ix, s0 + t) : Sequence{0, 0, 0};
+      const int mine = (q.n + tokens_per_tile - 1) / tokens_per_tile;
+      long long all;
+      scan(mine > 0 ? q.len : 0, all);
+      tokens += all;
+      base[t] = (int)min(n_tiles + scan(mine, all), (long long)most);
+      __syncthreads();
+      for (int i = warp; i < 1024 && s0 + i < ix.S; i += 32) {  // a warp a sequence
+        const Sequence q = sequence(ix, s0 + i);
+        for (int k = lane; k * tokens_per_tile < q.n && base[i] + k < most; k += 32) make_tile(base[i] + k, s0 + i, q, k);
+      }
+      n_tiles = (int)min(n_tiles + all, (long long)most);  // (more: starts that do not ascend, which are reported)
+      __syncthreads();
+    }
+    for (int t0 = 0; t0 < n_tiles; t0 += 1024) {
+      const int here = t0 + t < n_tiles ? steps_of(t0 + t) : 0;
+      longest = max(longest, here);
+      long long all;
+      const long long at = before + scan(here, all);
+      if (t0 + t < n_tiles) first[t0 + t] = at;
+      before += all;
+    }
   }
   longest = __reduce_max_sync(0xffffffffu, longest);
   __syncthreads();
