@@ -339,9 +339,9 @@ __global__ void __launch_bounds__(1024) cache_plan_kernel(const CacheIndex ix, i
     rounds = min(rounds - 1, (int)(rounds * (total / kCacheCtas) / most_dealt));  // (tiles of very different lengths: fewer of them are dealt)
   }
   if (t == 0) {
-    first[n_tiles] = per_head;
     head[0] = n_tiles;
     head[1] = rounds;
+    *reinterpret_cast<long long *>(&head[2]) = per_head;
   }
   if (rounds == 0) {  // equal shares, of tiles in not too many parts
     const long long share = max((total + kCacheCtas - 1) / kCacheCtas, (long long)(longest + kMaxParts - 1) / kMaxParts);
@@ -486,7 +486,7 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
     // is one of many places that the warps of an SM are in, see attn_tc.cu.  A warp of its own that looked ahead by five steps, with ten times
     // the instructions, ran at three quarters of the rate.)
     const int n_tiles = __ldcg(&p.head[0]), rounds = __ldcg(&p.head[1]);
-    const long long per_head = __ldcg(&p.first[n_tiles]);
+    const long long per_head = __ldcg(reinterpret_cast<const long long *>(&p.head[2]));
     const long long u0 = __ldcg(&p.cuts[blockIdx.x]), u1 = __ldcg(&p.cuts[blockIdx.x + 1]);
     const long long dealt = (long long)rounds * gridDim.x;  // tiles
     long long u = u0;  // of the share: the part's first step
@@ -494,25 +494,33 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
     auto share_begins = [&]() {
       // the line's first step, as a step of all heads
       const int h0 = (int)(dealt / n_tiles);
-      const long long at = u + (h0 * per_head + __ldcg(&p.first[(int)(dealt - (long long)h0 * n_tiles)]));
+      const int t0 = (int)(dealt - (long long)h0 * n_tiles);
+      const long long at = u + h0 * per_head + (t0 > 0 ? __ldcg(&p.first[t0]) : 0);
       h = (int)(at / per_head);
       const long long rest = at - h * per_head;
       tile = 0;
       int hi = n_tiles;  // first[tile] <= rest < first[hi]
+      long long begins = 0;
       while (hi - tile > 1) {
         const int step = (hi - tile + 31) / 32, i = tile + lane * step;
-        const bool below = i < hi && (lane == 0 || __ldcg(&p.first[i]) <= rest);
-        const int n = __popc(__ballot_sync(0xffffffffu, below));
+        const long long f = i < hi ? __ldcg(&p.first[i]) : 0;
+        const int n = __popc(__ballot_sync(0xffffffffu, i < hi && (lane == 0 || f <= rest)));
+        begins = __shfl_sync(0xffffffffu, f, n - 1);
         tile += (n - 1) * step;
         hi = min(hi, tile + step);
       }
-      a = (int)(rest - __ldcg(&p.first[tile]));
+      a = (int)(rest - begins);
     };
-    auto holder = [&](long long at) {  // the CTA whose share has this step
-      int n = 0;
+    auto holders = [&](long long at, long long to, int &c0, int &c1) {  // the CTAs whose shares have these steps
+      uint32_t n = 0;
 #pragma unroll
-      for (int c = 0; c < kCacheCtas; c += 32) n += c + lane < kCacheCtas && __ldcg(&p.cuts[c + lane]) <= at ? 1 : 0;
-      return (int)__reduce_add_sync(0xffffffffu, (unsigned)n) - 1;
+      for (int c = 0; c < kCacheCtas; c += 32) {
+        const long long cut = c + lane < kCacheCtas ? __ldcg(&p.cuts[c + lane]) : 1LL << 62;
+        n += (cut <= at ? 1u : 0u) + (cut <= to ? 1u << 16 : 0u);
+      }
+      n = __reduce_add_sync(0xffffffffu, n);
+      c0 = (int)(n & 0xffffu) - 1;
+      c1 = (int)(n >> 16) - 1;
     };
     int k = 0;  // tiles of this CTA that it has been dealt so far
     auto next_dealt = [&]() {
@@ -547,8 +555,9 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
       const int b = !any ? -1 : from_line ? (int)min((long long)x.t.steps, a + (u1 - u)) : x.t.steps;
       int c0 = blockIdx.x, parts = 1;
       if (any && b - a < x.t.steps) {
-        c0 = holder(u - a);
-        parts = holder(u - a + x.t.steps - 1) - c0 + 1;
+        int c1;
+        holders(u - a, u - a + x.t.steps - 1, c0, c1);
+        parts = c1 - c0 + 1;
       }
       if (lane == 0) {
         x.h = h;
@@ -1190,12 +1199,12 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
         bool write = whole;
         if (!whole) {
           if (row < n_rows) __stcg(&p.part_l[slot * 128 + row], make_float2(l, m));
-          __threadfence();
           __syncwarp();
           if (lane == 0) mbar_arrive(&sh.stored[w]);
           if (quarter == 0) {
             if (!wait(&sh.stored[w], n_stored & 1)) break;
             if (lane == 0) {
+              __threadfence();  // (of what the warpgroup has stored, which the barrier has shown this thread)
               sh.last[w] = atomicAdd(&p.arrivals[to.c0], 1) == to.parts - 1;
               __threadfence();
               mbar_arrive(&sh.told[w]);
