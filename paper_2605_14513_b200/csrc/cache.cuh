@@ -112,17 +112,16 @@ __device__ __forceinline__ float code_scale(uint32_t top, float &inv) {
   inv = __uint_as_float((uint32_t)(127 - e) << 23);
   return __uint_as_float(top < 0x7f80u ? (uint32_t)(127 + e) << 23 : 0x7fc00000u);
 }
-// Two bf16 numbers times inv as the sums of two e4m3 codes each: the codes nearest to them, and to what is left.
+// Two bf16 numbers times inv (a power of two that makes them 448 at most) as the sums of two e4m3 codes each: the codes nearest to them,
+// and to what is left.  In f16, which holds the products but for bits below 2^-24, and the differences.
 __device__ __forceinline__ void split_codes(uint32_t w, float inv, uint32_t &high, uint32_t &low) {
-  const float x0 = __uint_as_float(w << 16) * inv, x1 = __uint_as_float(w & 0xffff0000u) * inv;
+  const uint32_t x = pack_f16x2(__uint_as_float(w << 16) * inv, __uint_as_float(w & 0xffff0000u) * inv);
   uint16_t c;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(x1), "f"(x0));
+  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(c) : "r"(x));
   high = c;
-  uint32_t y;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(y) : "h"(c));
-  float y0, y1;
-  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, h;\n\t}" : "=f"(y0), "=f"(y1) : "r"(y));
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(x1 - y1), "f"(x0 - y0));
+  uint32_t left;
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(left) : "r"(x), "r"(codes_to_f16x2(high)));
+  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(c) : "r"(left));
   low = c;
 }
 // A sequence as its arrays describe it, brought into range (and reported) where they do not hold what they should.
