@@ -271,8 +271,8 @@ typedef struct {
 
 /* The pools: bf16 or e4m3 elements, head_dim contiguous, 16-byte aligned, strides multiples of 16 bytes.  With
  * HEART_CACHE_E4M3 a token of a head also has a scale byte b in k_scale / v_scale [n_pages, Hkv, page] (16-byte aligned): its
- * elements are the codes times 2^(b - 127), or all NaN for b = 255.  (Codes 0x7f and 0xff are never written here; read back they
- * count as +-480.)  NULL for HEART_CACHE_BF16. */
+ * elements are the codes times 2^(b - 127), or all NaN for b = 255.  (Codes 0x7f and 0xff and the byte 0 are never written here:
+ * they stand for no number.)  NULL for HEART_CACHE_BF16. */
 typedef struct {
   void *k, *v;
   uint8_t *k_scale, *v_scale;
@@ -303,7 +303,8 @@ int heart_cache_read(const heart_cache_config *cfg, const heart_cache *cache, co
  *   sum-exp of the scaled logits, or NULL.
  * A query without keys gets zeros and lse = -inf.  What a row does not see has no part in it, whatever it holds (pages hold
  * anything behind a sequence's end); a row that sees a key or value that is not finite has elements that are not finite.
- * Weights below 2^-100 of a row's largest may count as zero. */
+ * Unnormalised sums stay below 2^15 * (visible keys) * max |v|: finite for |v| up to 2^90 whatever the lengths and logits.  Weights below
+ * 2^-29 of a row's largest may count as zero. */
 int heart_cache_attn(const heart_cache_config *cfg, const void *Q, const heart_cache *cache, const int32_t *page_table,
                      const int32_t *row_start, const int32_t *kv_len, void *O, float *lse, void *workspace,
                      heart_stream_t stream);

@@ -15,6 +15,7 @@ struct CacheGeom {
   long long qt, qh, kvt, kvh;  // element strides: Q and O, packed K and V
   long long pp, ph, pt;        // the pools
   double scale;
+  int test_skip;  // test-hook builds only (see the attention kernels)
 };
 
 // What the kernels on the cache read on the device.

@@ -65,7 +65,14 @@ int heart::make_geom(const heart_config *c, Geom *g) {
 int heart::make_cache_geom(const heart_cache_config *c, CacheGeom *g) {
   if (c == nullptr) return HEART_ERR_INVALID;
   if (c->S <= 0 || c->T <= 0 || c->Hq <= 0 || c->Hkv <= 0 || c->n_pages <= 0 || c->table_stride <= 0) return HEART_ERR_INVALID;
-  if (c->max_new < 0 || c->causal < 0 || c->window < 0 || c->sink < 0 || c->flags != 0) return HEART_ERR_INVALID;
+#ifdef HEART_TEST_HOOKS
+  g->test_skip = c->flags == 0x80000000u;
+  const uint32_t flags = c->flags & 0x7fffffffu;
+#else
+  g->test_skip = 0;
+  const uint32_t flags = c->flags;
+#endif
+  if (c->max_new < 0 || c->causal < 0 || c->window < 0 || c->sink < 0 || flags != 0) return HEART_ERR_INVALID;
   if (c->kind != HEART_CACHE_BF16 && c->kind != HEART_CACHE_E4M3) return HEART_ERR_INVALID;
   if (c->Hq % c->Hkv != 0) return HEART_ERR_INVALID;
   if (c->D != kD || c->Hq / c->Hkv > 128) return HEART_ERR_UNSUPPORTED;
