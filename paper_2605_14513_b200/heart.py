@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes as C
 import functools
 import os
+import struct
 
 import torch
 
@@ -255,6 +256,15 @@ def make_cache_config(S, T, Hq, Hkv, page, n_pages, table_stride, kind=CACHE_BF1
                        *pool_strides, scale)
 
 
+_cache_layout = struct.Struct("12x4i4xi52x3q").unpack_from  # Hkv, D, page, n_pages; kind; the pools' strides
+
+
+def _full_layout(layout):
+    """With the strides of contiguous pools in the place of zeros."""
+    Hkv, D, page, n_pages, kind, *strides = layout
+    return layout if any(strides) else (Hkv, D, page, n_pages, kind, Hkv * page * D, page * D, D)
+
+
 class Cache:
     """Caller-owned pools of a paged cache (device tensors + the C struct that points at them): new ones, zero-filled, or the
     tensors given.  k, v: [n_pages, Hkv, page, D] elements as cfg lays them out, bf16 or float8_e4m3fn; k_scale, v_scale
@@ -281,6 +291,7 @@ class Cache:
             if x.dtype != torch.uint8 or tuple(x.shape) != shape or x.device != self.k.device or not x.is_contiguous():
                 raise ValueError(f"scales have to be contiguous uint8 {shape} beside the pools: got {x.dtype} {tuple(x.shape)}")
         self.device = self.k.get_device()
+        self.layout = _cache_layout(cfg)
         self.struct = CacheStruct(*(None if x is None else x.data_ptr() for x in (self.k, self.v, self.k_scale, self.v_scale)))
         self.ref = C.byref(self.struct)
 
@@ -302,19 +313,36 @@ def _cache_workspace_bytes(S, T, Hq, Hkv):
     return cache_workspace_bytes(make_cache_config(S, T, Hq, Hkv, 64, 1, 1))
 
 
-def _cache_call(cfg, cache, heads, stride, tensors, page_table, row_start, kv_len, ws):
-    """Checks what the library cannot see (types, sizes, devices).  heads, stride: of the packed `tensors`."""
+def _has_strides(x, T, heads, stride_t, stride_h):
+    """Whether x can be a packed tensor of these strides: all that they reach is x's, and x, where it is [T, heads, D] or
+    [heads, T, D] (behind ones), has them itself."""
+    room = x.untyped_storage().nbytes() // x.element_size() - x.storage_offset()
+    if x.stride(-1) != 1 or stride_t < 0 or stride_h < 0 or (T - 1) * stride_t + (heads - 1) * stride_h + 128 > room:
+        return False
+    if x.dim() < 3 or x.shape[-3:].numel() != x.numel():
+        return True
+    have = tuple(zip(x.shape, x.stride()))[-3:-1]
+    return any(all(n == m and (n == 1 or a == b) for (n, a), (m, b) in zip(have, want))
+               for want in (((T, stride_t), (heads, stride_h)), ((heads, stride_h), (T, stride_t))))
+
+
+def _cache_call(cfg, cache, heads, stride_t, stride_h, tensors, page_table, row_start, kv_len, ws):
+    """Checks what the library cannot see (types, sizes, devices).  heads, strides: of the packed `tensors`."""
     device, S, T = cache.device, cfg.S, cfg.T
+    layout = _cache_layout(cfg)
+    if layout != cache.layout and _full_layout(layout) != _full_layout(cache.layout):
+        raise ValueError("the cache was made for a config with other pools (Hkv, D, page, n_pages, kind or strides)")
     n = T * heads * 128
     for x in tensors:
-        if x.dtype is not torch.bfloat16 or x.numel() != n or x.get_device() != device or not (x.is_contiguous() or stride and x.stride(-1) == 1):
+        if (x.dtype is not torch.bfloat16 or x.numel() != n or x.get_device() != device or
+                not (_has_strides(x, T, heads, stride_t, stride_h) if stride_t else x.is_contiguous())):
             raise ValueError(f"packed tensors have to be bf16, {T} rows x {heads} heads x 128, beside the cache, contiguous or with their strides in the "
                              f"config: got {x.dtype} {tuple(x.shape)}, strides {x.stride()}, on {x.device}")
     for x, n in ((page_table, S * cfg.table_stride), (row_start, S + 1), (kv_len, S)):
         if x.dtype is not torch.int32 or x.numel() != n or x.get_device() != device or not x.is_contiguous():
             raise ValueError(f"page_table, row_start and kv_len have to be contiguous int32 of {S} x {cfg.table_stride}, {S + 1} and {S} "
                              f"entries beside the cache: got {x.dtype} {tuple(x.shape)} on {x.device}")
-    if ws.get_device() != device or ws.numel() * ws.element_size() < _cache_workspace_bytes(S, T, cfg.Hq, cfg.Hkv):
+    if ws.get_device() != device or not ws.is_contiguous() or ws.numel() * ws.element_size() < _cache_workspace_bytes(S, T, cfg.Hq, cfg.Hkv):
         raise ValueError(f"the workspace has to have cache_workspace_bytes(cfg) = {cache_workspace_bytes(cfg)} bytes beside the cache")
 
 
@@ -332,14 +360,14 @@ def _cache_launch(call, cache, *args):
 
 def heart_cache_write(cfg, K, V, cache: Cache, page_table, row_start, kv_len, ws):
     """Stores the packed rows of K and V (bf16 [T, Hkv, D]), the last tokens of their sequences, in their pages."""
-    _cache_call(cfg, cache, cfg.Hkv, cfg.kv_stride_t, (K, V), page_table, row_start, kv_len, ws)
+    _cache_call(cfg, cache, cfg.Hkv, cfg.kv_stride_t, cfg.kv_stride_h, (K, V), page_table, row_start, kv_len, ws)
     _cache_launch(lib().heart_cache_write, cache, C.byref(cfg), K.data_ptr(), V.data_ptr(), cache.ref, page_table.data_ptr(), row_start.data_ptr(),
                   kv_len.data_ptr(), ws.data_ptr())
 
 
 def heart_cache_read(cfg, cache: Cache, page_table, row_start, kv_len, K_out, V_out, ws):
     """The last tokens of the sequences out of their pages into the packed rows of K_out and V_out (bf16 [T, Hkv, D])."""
-    _cache_call(cfg, cache, cfg.Hkv, cfg.kv_stride_t, (K_out, V_out), page_table, row_start, kv_len, ws)
+    _cache_call(cfg, cache, cfg.Hkv, cfg.kv_stride_t, cfg.kv_stride_h, (K_out, V_out), page_table, row_start, kv_len, ws)
     _cache_launch(lib().heart_cache_read, cache, C.byref(cfg), cache.ref, page_table.data_ptr(), row_start.data_ptr(), kv_len.data_ptr(),
                   K_out.data_ptr(), V_out.data_ptr(), ws.data_ptr())
 
@@ -347,7 +375,7 @@ def heart_cache_read(cfg, cache: Cache, page_table, row_start, kv_len, K_out, V_
 def heart_cache_attn(cfg, Q, cache: Cache, page_table, row_start, kv_len, O, ws, lse=None):
     """Attention of the packed rows of Q (bf16 [T, Hq, D]), the last tokens of their sequences, over the sequences' pages
     into O; lse: optional fp32 [T, Hq]."""
-    _cache_call(cfg, cache, cfg.Hq, cfg.q_stride_t, (Q, O), page_table, row_start, kv_len, ws)
+    _cache_call(cfg, cache, cfg.Hq, cfg.q_stride_t, cfg.q_stride_h, (Q, O), page_table, row_start, kv_len, ws)
     if lse is not None and (lse.dtype is not torch.float32 or lse.numel() != cfg.T * cfg.Hq or lse.get_device() != cache.device or not lse.is_contiguous()):
         raise ValueError(f"lse has to be contiguous fp32 [{cfg.T}, {cfg.Hq}] beside the cache: got {lse.dtype} {tuple(lse.shape)} on {lse.device}")
     _cache_launch(lib().heart_cache_attn, cache, C.byref(cfg), Q.data_ptr(), cache.ref, page_table.data_ptr(), row_start.data_ptr(), kv_len.data_ptr(),

@@ -1,6 +1,7 @@
 """The calls on a paged cache: sizes, struct layout and what is refused, without a GPU."""
 import ctypes as C
 import math
+import types
 
 import pytest
 import torch
@@ -98,6 +99,49 @@ def test_pools_on_the_host_are_refused(heart):
     k = torch.zeros((9, 2, 64, 128), dtype=torch.bfloat16)
     with pytest.raises(ValueError):
         heart.Cache(cfg, k, k)
+
+
+def fake_cache(heart, cfg):
+    """As far as the checks of a call look at it, on the host."""
+    return types.SimpleNamespace(device=-1, layout=heart._cache_layout(cfg))
+
+
+def call(heart, cfg, cache, x, heads=2, strides=(0, 0)):
+    ints = [torch.zeros(n, dtype=torch.int32) for n in (cfg.S * cfg.table_stride, cfg.S + 1, cfg.S)]
+    ws = torch.zeros(heart.cache_workspace_bytes(cfg), dtype=torch.uint8)
+    heart._cache_call(cfg, cache, heads, *strides, (x,), *ints, ws)
+
+
+def test_a_cache_of_other_pools_is_refused(heart):
+    cfg = config(heart)
+    cache = fake_cache(heart, cfg)
+    x = torch.zeros((cfg.T, 2, 128), dtype=torch.bfloat16)
+    call(heart, cfg, cache, x)
+    call(heart, config(heart, causal=3, window=5, max_new=2), cache, x)
+    call(heart, config(heart, pool_stride_page=2 * cfg.page * 128, pool_stride_h=cfg.page * 128, pool_stride_t=128), cache, x)  # the same, spelt out
+    for change in (dict(n_pages=cfg.n_pages + 1), dict(page=2 * cfg.page), dict(kind=1), dict(Hkv=1),
+                   dict(pool_stride_page=2 * cfg.page * 128, pool_stride_h=128, pool_stride_t=256)):
+        with pytest.raises(ValueError):
+            call(heart, config(heart, **change), cache, x)
+
+
+def test_packed_tensors_that_do_not_hold_their_strides_are_refused(heart):
+    cfg = config(heart)
+    cache, T = fake_cache(heart, cfg), cfg.T
+    plain = torch.zeros((T, 2, 128), dtype=torch.bfloat16)
+    wide = torch.zeros((T, 3, 128), dtype=torch.bfloat16)
+    call(heart, cfg, cache, plain)
+    call(heart, cfg, cache, plain, strides=(256, 128))
+    call(heart, cfg, cache, wide[:, :2], strides=(384, 128))
+    call(heart, cfg, cache, wide[:, 1:], strides=(384, 128))
+    call(heart, cfg, cache, torch.zeros((2, T, 128), dtype=torch.bfloat16), strides=(128, T * 128))
+    call(heart, cfg, cache, torch.zeros((1, 2, T, 128), dtype=torch.bfloat16), strides=(128, T * 128))
+    call(heart, cfg, cache, plain.flatten(), strides=(256, 128))
+    for x, strides in ((wide[:, :2], (0, 0)), (plain, (384, 128)), (plain, (128, T * 128)), (wide[:, :2], (256, 128)),
+                       (plain.flatten(), (384, 128)), (plain.transpose(1, 2), (256, 128)), (plain, (256, -128)), (plain.float(), (256, 128)),
+                       (torch.zeros((2, T, 128), dtype=torch.bfloat16), (256, 128))):
+        with pytest.raises(ValueError):
+            call(heart, cfg, cache, x, strides=strides)
 
 
 def test_the_definition_of_the_codes():
