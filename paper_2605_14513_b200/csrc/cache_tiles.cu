@@ -8,11 +8,10 @@
 //   * Rows see different keys.  Steps that some row does not see whole have a path of their own, outside of the loop over the steps:
 //     hidden scores become -inf in tensor memory, and values that are not finite (what lies behind a sequence's end is anyone's) are
 //     taken out of shared memory first, because the product reads them with weight 0; rows that do see such a value are marked.
-//   * Where keys and values fit the L2 (12 x 4680 over 12680 e4m3 tokens 387 us, dealt 422), each CTA takes a run of tiles. Otherwise tiles, of
-//     one key head after the other, are dealt in turn, so that the CTAs read the same keys at a time (12 x 32760 over themselves, 201 MB
-//     of keys and values: 7.2 ms when every CTA had a run of tiles of its own, whose keys came from DRAM, 5.7 dealt), but for the last one to two
-//     rounds of them: the steps of those, in one line, are cut into shares that bring all CTAs to the same sum, so that the launch ends
-//     on all SMs at once whatever the lengths are.  Parts of a tile go to the workspace; the CTA that brings the last one puts them together,
+//   * Tiles, of one key head after the other, are dealt in turn, so that the CTAs read the same keys at a time (12 x 32760 over themselves, 201 MB
+//     of keys and values: 7.2 ms when every CTA had a run of tiles of its own, whose keys came from DRAM, 5.7 dealt; where they fit the L2 both
+//     take the same time), but for the last one to two rounds of them: the steps of those, in one line, are cut into shares that
+//     bring all CTAs to the same sum, so that the launch ends on all SMs at once whatever the lengths are.  Parts of a tile go to the workspace; the CTA that brings the last one puts them together,
 //     in order: the result does not depend on which one that is.
 //
 // e4m3 caches.  Converting keys and values to bf16 for 128 rows costs as many instructions as the softmax does.  Keys need none: a bf16 query has
@@ -40,11 +39,11 @@ constexpr int kCodeBytes = 16384;  // the same as e4m3: [128 rows][128]
 constexpr int kSteps = 16;         // key steps in flight (K is up to four steps ahead of the value products)
 constexpr int kPartRing = 8;       // parts are announced a part ahead
 constexpr int kMaxParts = 12;      // of a tile, about
-constexpr long long kRunsUpTo = 64LL << 20;  // bytes of keys and values that stay in L2: a CTA takes a run of tiles
 constexpr float kNoReference = -3.0e38f;
 constexpr float kHeadroom = 16.f, kMaxGrowth = 8.f;  // see attn_tc.cu
 constexpr float kHeadroomE4m3 = -4.f, kMaxGrowthE4m3 = 14.f;  // weights of f16: 2^4 where the reference moves, to 2^14
 constexpr uint32_t kShortWait = 500;
+constexpr int kRowsAtOnce = 4;  // of queries that are split
 
 // A tile of a head as the plan kernel writes it.
 struct Tile {
@@ -106,6 +105,7 @@ struct TileShared {
   int first_top[4];                   // the largest one of the first step, per part & 3
   int top[8];                         // the largest
   float q_scale[2][128];     // e4m3: what the scores of a row are to be multiplied by
+  alignas(16) uint8_t zeros[128];     // e4m3: what the codes of a token count as that is none
   alignas(16) uint32_t bad[8][4];     // e4m3: keys that are not finite, by g & 7
   alignas(16) uint8_t not_finite[4][128];  // bf16: rows that see a value that is not finite, per part & 3
   uint32_t tmem_base;
@@ -191,6 +191,12 @@ __device__ __forceinline__ uint4 lds_u4(uint32_t addr) {
   asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
   return v;
 }
+__device__ __forceinline__ uint2 lds_u2(uint32_t addr) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void sts_u1(uint32_t addr, uint32_t v) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
 __device__ __forceinline__ void sts_u4(uint32_t addr, uint4 v) {
   asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
@@ -205,7 +211,7 @@ constexpr int kSmallPlan = 4096;
 // The tiles of a head, sequence by sequence, and the key steps before each.  One CTA.
 __global__ void __launch_bounds__(1024) cache_plan_kernel(const CacheIndex ix, int tokens_per_tile, Tile *__restrict__ tiles,
                                                           long long *__restrict__ first, int *__restrict__ head, long long *__restrict__ cuts,
-                                                          int32_t *__restrict__ arrivals, int most, int Hkv, int token_bytes) {
+                                                          int32_t *__restrict__ arrivals, int most, int Hkv) {
   __shared__ long long sums[32];
   __shared__ int base[1024];
   __shared__ int steps[kSmallPlan];  // of the first tiles: as a rule all
@@ -234,7 +240,6 @@ __global__ void __launch_bounds__(1024) cache_plan_kernel(const CacheIndex ix, i
     return before;
   };
   int n_tiles = 0, longest = 1;
-  long long tokens = 0;  // of the sequences with tiles
   auto make_tile = [&](int i, int s, const Sequence &q, int k) {
     Tile x;
     x.s = s;
@@ -259,14 +264,12 @@ __global__ void __launch_bounds__(1024) cache_plan_kernel(const CacheIndex ix, i
   if (ix.S <= 32) {  // a lane a sequence, then a thread a tile
     const Sequence q = lane < ix.S ? sequence(ix, lane) : Sequence{0, 0, 0};
     const int mine = (q.n + tokens_per_tile - 1) / tokens_per_tile;
-    long long upto = mine, sum = mine > 0 ? q.len : 0;
+    long long upto = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const long long y = __shfl_up_sync(0xffffffffu, upto, o);
       if (lane >= o) upto += y;
-      sum += __shfl_xor_sync(0xffffffffu, sum, o);
     }
-    tokens = sum;
     n_tiles = (int)min(__shfl_sync(0xffffffffu, upto, 31), (long long)most);
     if (warp == 0) {
       base[lane] = (int)min(upto - mine, (long long)most);
@@ -294,8 +297,6 @@ __global__ void __launch_bounds__(1024) cache_plan_kernel(const CacheIndex ix, i
       const Sequence q = s0 + t < ix.S ? sequence(ix, s0 + t) : Sequence{0, 0, 0};
       const int mine = (q.n + tokens_per_tile - 1) / tokens_per_tile;
       long long all;
-      scan(mine > 0 ? q.len : 0, all);
-      tokens += all;
       base[t] = (int)min(n_tiles + scan(mine, all), (long long)most);
       __syncthreads();
       for (int i = warp; i < 1024 && s0 + i < ix.S; i += 32) {  // a warp a sequence
@@ -320,7 +321,7 @@ __global__ void __launch_bounds__(1024) cache_plan_kernel(const CacheIndex ix, i
   __syncthreads();
   for (int i = 0; i < 32; ++i) longest = max(longest, (int)sums[i]);
   const long long per_head = before, total = per_head * Hkv, all_tiles = (long long)n_tiles * Hkv;
-  int rounds = tokens * Hkv * token_bytes <= kRunsUpTo ? 0 : (int)max(all_tiles / kCacheCtas - 1, 0LL);
+  int rounds = (int)max(all_tiles / kCacheCtas - 1, 0LL);
   long long dealt = 0, most_dealt = 0;  // to CTA t, to the one with most
   while (rounds > 0) {
     dealt = 0;
@@ -405,6 +406,7 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
     for (int i = 0; i < kSteps; ++i) mbar_init(&sh.step_full[i], 1);
     for (int i = 0; i < 8; ++i) mbar_init(&sh.scales_full[i], 1);
     sh.abort = 0;
+    for (int i = 0; i < 8; ++i) reinterpret_cast<uint4 *>(sh.zeros)[i] = make_uint4(0u, 0u, 0u, 0u);
     mbar_fence_init();
   }
   if (warp == kWarpQK) {
@@ -844,41 +846,38 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
     // clocks a step, of 3300.)
     const int r = tid - kWarpConvert * 32;
     uint32_t n = 0;
-    // Q: q = 2^k (high + low), codes of both; the row's place in the first half holds the high parts, in the second the low ones
+    // Q: q = 2^k (high + low), codes of both; the row's place in the first half holds the high parts, in the second the low ones.  A row at
+    // a time, a lane four dims of it, so that all of it has been read before anything is written.  (40 heads x 4680 over
+    // 33k: 2.84 ms; a thread a row, whose loops keep half a row, 3.03; two and eight rows at once 2.91.)
     auto split_queries = [&]() {
       if (!wait(&sh.q_full[n & 1], (n >> 1) & 1)) return;
-      const uint32_t at = smem_u32(smem + L::kOffQ + (n & 1) * kTileBytes) + r * 128;
-      uint32_t top = 0u;
-#pragma unroll 2
-      for (int j = 0; j < 16; ++j) {
-        const uint4 q = lds_u4(at + (j >> 3) * (kTileBytes / 2) + (((j ^ r) & 7) << 4));
-        top = __vmaxu2(top, __vmaxu2(__vmaxu2(q.x & 0x7fff7fffu, q.y & 0x7fff7fffu), __vmaxu2(q.z & 0x7fff7fffu, q.w & 0x7fff7fffu)));
-      }
-      top = max(top & 0xffffu, top >> 16);
-      float inv;
-      sh.q_scale[n & 1][r] = p.scale_log2 * code_scale(top, inv);
-      uint4 low[8];
-      // (a loop, with the low parts put where they belong by comparing: as 8 pieces of code, fetched anew for every tile, 6 prompts x 24
-      // heads took 202 us instead of 184)
+      const uint32_t at = smem_u32(smem + L::kOffQ + (n & 1) * kTileBytes);
+      const uint32_t from = at + (lane >> 4) * (kTileBytes / 2) + (lane & 1) * 8, to = at + (lane & 3) * 4;
 #pragma unroll 1
-      for (int j = 0; j < 8; ++j) {  // 16 dims: pieces 2j and 2j + 1 of the row, to piece j of either half (the first one's has been read by then)
-        uint32_t hi[8], lo[8];
+      for (int i = r & ~31; i < (r | 31); i += kRowsAtOnce) {
+        uint2 q[kRowsAtOnce];
+        uint32_t top[kRowsAtOnce];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const uint4 q = lds_u4(at + (j >> 2) * (kTileBytes / 2) + (((2 * j + i) ^ r) & 7) * 16);
-          split_codes(q.x, inv, hi[4 * i], lo[4 * i]);
-          split_codes(q.y, inv, hi[4 * i + 1], lo[4 * i + 1]);
-          split_codes(q.z, inv, hi[4 * i + 2], lo[4 * i + 2]);
-          split_codes(q.w, inv, hi[4 * i + 3], lo[4 * i + 3]);
+        for (int j = 0; j < kRowsAtOnce; ++j) q[j] = lds_u2(from + (i + j) * 128 + ((((lane >> 1) ^ (i + j)) & 7) << 4));
+#pragma unroll
+        for (int j = 0; j < kRowsAtOnce; ++j) {
+          const uint32_t two = __vmaxu2(q[j].x & 0x7fff7fffu, q[j].y & 0x7fff7fffu);
+          top[j] = __reduce_max_sync(0xffffffffu, max(two & 0xffffu, two >> 16));
         }
-        sts_u4(at + (((j ^ r) & 7) << 4), make_uint4(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16, hi[4] | hi[5] << 16, hi[6] | hi[7] << 16));
-        const uint4 x = make_uint4(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16, lo[4] | lo[5] << 16, lo[6] | lo[7] << 16);
+        __syncwarp();
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (i == j) low[i] = x;
+        for (int j = 0; j < kRowsAtOnce; ++j) {
+          float inv;
+          const float scale = code_scale(top[j], inv);
+          if (lane == 0) sh.q_scale[n & 1][i + j] = p.scale_log2 * scale;
+          uint32_t hi[2], lo[2];
+          split_codes(q[j].x, inv, hi[0], lo[0]);
+          split_codes(q[j].y, inv, hi[1], lo[1]);
+          const uint32_t place = to + (i + j) * 128 + ((((lane >> 2) ^ (i + j)) & 7) << 4);
+          sts_u1(place, hi[0] | hi[1] << 16);
+          sts_u1(place + kTileBytes / 2, lo[0] | lo[1] << 16);
+        }
       }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) sts_u4(at + kTileBytes / 2 + (((j ^ r) & 7) << 4), low[j]);
       async_proxy_fence();
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh.q_ready[n & 1]);
@@ -897,15 +896,16 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
           if (!wait(&sh.v_full[b], (g >> 1) & 1)) break;
           if (g >= 2 && !wait(&sh.pv_done[b], ((g - 2) >> 1) & 1)) break;
         }
-        const uint32_t from = smem_u32(smem + L::kOffCodes + b * kCodeBytes) + r * 128;
         const uint32_t to = smem_u32(smem + L::kOffV + b * kTileBytes) + r * 128;
         const int vs = sh.v_scale[g & 7][r];
         const float f = vs == 0 ? 0.f : cache_scale(max(vs - sh.top[g & 7] + 127, 1));
-        const uint32_t f2 = pack_f16x2(f, f), keep = vs == 0 ? 0u : 0xffffffffu;  // (codes behind a sequence's end may be no numbers)
+        const uint32_t f2 = pack_f16x2(f, f);
+        // (Codes behind a sequence's end may be no numbers, and 0 * NaN is NaN.  Masked with four instructions in the loop, 40 heads x 4680 over 33k took
+        // 3.48 ms instead of 3.03.)
+        const uint32_t from = vs == 0 ? smem_u32(sh.zeros) : smem_u32(smem + L::kOffCodes + b * kCodeBytes) + r * 128;
 #pragma unroll 1
-        for (int j = 0; j < 8; ++j) {  // 16 dims (instructions are what is short: 12 x 4680 over 12.7k 387 us, unrolled by 2, 4 and 8 399, 420 and 453)
-          uint4 w = lds_u4(from + (((j ^ r) & 7) << 4));
-          w.x &= keep, w.y &= keep, w.z &= keep, w.w &= keep;
+        for (int j = 0; j < 8; ++j) {  // 16 dims (instructions are what is short: 12 x 4680 over 12.7k, when this was written, 387 us, unrolled by 2, 4 and 8 399, 420 and 453)
+          const uint4 w = lds_u4(from + (((j ^ r) & 7) << 4));
           const uint32_t half = to + (j >> 2) * (kTileBytes / 2);
           sts_u4(half + ((((j & 3) * 2) ^ (r & 7)) << 4), make_uint4(mul_f16x2(codes_to_f16x2(w.x), f2), mul_f16x2(high_codes_to_f16x2(w.x), f2),
                                                                      mul_f16x2(codes_to_f16x2(w.y), f2), mul_f16x2(high_codes_to_f16x2(w.y), f2)));
@@ -1341,7 +1341,7 @@ cudaError_t launch_cache_tiles(const CacheGeom &g, const CacheIndex &ix, const C
   p.test_skip = g.test_skip;
   p.scale_log2 = (float)(g.scale * 1.4426950408889634);
   cudaError_t e = launch_pdl(cache_plan_kernel, dim3(1), dim3(1024), 0, s, ix, 128 / g.G, reinterpret_cast<Tile *>(w.tiles), w.tile_first, w.tile_head,
-                             w.cuts, p.arrivals, (int)cache_max_tiles(g), g.Hkv, g.e4m3 ? 2 * kD : 4 * kD);
+                             w.cuts, p.arrivals, (int)cache_max_tiles(g), g.Hkv);
   if (e != cudaSuccess) return e;
   ++*launches;
   e = g.e4m3 ? launch<true>(mq, mk, mv, p, s) : launch<false>(mq, mk, mv, p, s);
