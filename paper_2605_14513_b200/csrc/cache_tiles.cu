@@ -732,6 +732,11 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
             for (int c = 0; c < 128; c += 16) {
               const int key = k0 + c, mine = key + (lane >> 3);
               if (key + 16 <= every_end && (key >= every_low || key + 16 <= ix.sink)) continue;
+              if (key >= some_end || (key + 16 <= some_low && key >= ix.sink)) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sts_u4(v_at + (j & 1) * (kTileBytes / 2) + (c + 4 * (j >> 1)) * 128, make_uint4(0u, 0u, 0u, 0u));
+                continue;
+              }
               uint4 v[4], w[4];
 #pragma unroll
               for (int j = 0; j < 4; ++j) v[j] = lds_u4(v_at + (c + 4 * j) * 128), w[j] = lds_u4(v_at + kTileBytes / 2 + (c + 4 * j) * 128);
@@ -963,16 +968,18 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
       const Visible v = visible(ix, x.t.p0 + p.token_of(row), x.t.len);
       const int end = v.end - k0, low = v.low - k0, sink = ix.sink - k0;
       tc_fence_after();
+      auto below = [](int n) { return n <= 0 ? 0u : 0xffffffffu >> (32 - min(n, 32)); };  // bits 0 .. n - 1
 #pragma unroll 1
-      for (int col = 0; col < 128; col += 16) {
-        if (__all_sync(0xffffffffu, col + 16 <= end && (col >= low || col + 16 <= sink))) continue;
-        uint32_t y[16];
-        tmem_ld16(s_at + col, y);
+      for (int col = 0; col < 128; col += 32) {
+        const uint32_t seen = below(end - col) & (~below(low - col) | below(sink - col));
+        if (__all_sync(0xffffffffu, seen == 0xffffffffu)) continue;
+        uint32_t y[32];
+        tmem_ld32(s_at + col, y);
         tmem_wait_ld();
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (col + i >= end || (col + i < low && col + i >= sink)) y[i] = 0xff800000u;
-        tmem_st16(s_at + col, y);
+        for (int i = 0; i < 32; ++i)
+          if (!(seen >> i & 1u)) y[i] = 0xff800000u;
+        tmem_st32(s_at + col, y);
       }
       tmem_wait_st();
 #pragma unroll 1
