@@ -32,13 +32,13 @@ struct CacheWorkspace {
   float *parts;       // [2 * kCacheCtas][128][128] parts of tiles: unnormalised sums of values
   float2 *part_l;     // [2 * kCacheCtas][128] their row sums and references
   void *tiles;        // [max_tiles] tiles of a head (see cache_tiles.cu)
-  long long *tile_first;  // [max_tiles + 1] key steps before a tile
+  long long *tile_first;  // [max_tiles + 1] cost of the tiles before a tile, in key steps
   int *tile_head;     // [64] number of tiles of a head, rounds of them that are dealt
   long long *cuts;    // [kCacheCtas + 1] the CTAs' shares of the other ones
   size_t bytes;
 };
 
-constexpr size_t kTileRecord = 48;
+constexpr size_t kTileRecord = 52;
 // Tiles of a head: a sequence ends at most one of them early.
 __host__ inline size_t cache_max_tiles(const CacheGeom &g) { return (size_t)g.S + (size_t)g.T / (128 / g.G); }
 

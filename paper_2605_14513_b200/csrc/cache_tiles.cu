@@ -11,7 +11,9 @@
 //   * Tiles, of one key head after the other, are dealt in turn, so that the CTAs read the same keys at a time (12 x 32760 over themselves, 201 MB
 //     of keys and values: 7.2 ms when every CTA had a run of tiles of its own, whose keys came from DRAM, 5.7 dealt; where they fit the L2 both
 //     take the same time), but for the last one to two rounds of them: the steps of those, in one line, are cut into shares that
-//     bring all CTAs to the same sum, so that the launch ends on all SMs at once whatever the lengths are.  Parts of a tile go to the workspace; the CTA that brings the last one puts them together,
+//     bring all CTAs to the same sum, so that the launch ends on all SMs at once whatever the lengths are.  The sum counts a tile's beginning
+//     and end as four steps and a step that some row does not see whole as three (12 x 4680 over 32760, causal by frames, 770 us with
+//     steps alone, now 738; 6 prompts x 24 heads 130, now 126; other weights near these give the same), unless the launch has less than two tiles a CTA.  Parts of a tile go to the workspace; the CTA that brings the last one puts them together,
 //     in order: the result does not depend on which one that is.
 //
 // e4m3 caches.  Converting keys and values to bf16 for 128 rows costs as many instructions as the softmax does.  Keys need none: a bf16 query has
@@ -37,6 +39,7 @@ constexpr int kWarpQK = 8, kWarpV = 9, kWarpK = 10, kWarpPV = 11, kWarpConvert =
 constexpr int kTileBytes = 32768;  // 128 rows x 128 dims of bf16: [2 dim halves][128 rows][64], 128-byte swizzle
 constexpr int kCodeBytes = 16384;  // the same as e4m3: [128 rows][128]
 constexpr int kSteps = 16;         // key steps in flight (K is up to four steps ahead of the value products)
+constexpr int kTileCost = 4, kMaskCost = 2;  // of a tile and of a step that some row does not see whole, in steps
 constexpr int kPartRing = 8;       // parts are announced a part ahead
 constexpr int kMaxParts = 12;      // of a tile, about
 constexpr float kNoReference = -3.0e38f;
@@ -51,6 +54,7 @@ struct Tile {
   int len, sinks, first, steps;   // tokens of the sequence; its key steps (see Span)
   int every_low, every_end;       // all rows see the keys every_low .. every_end - 1 (and of the sinks those before every_end)
   int some_low, some_end;         // some row sees them
+  int extra;                      // what else it costs, in steps
 };
 constexpr int kTileWords = sizeof(Tile) / 4;
 static_assert(sizeof(Tile) == kTileRecord, "the workspace has room for it");
@@ -119,9 +123,9 @@ static_assert(kSmem<true> <= 232448 && kSmem<false> <= 232448, "shared memory of
 struct TileParams {
   CacheIndex ix;
   const Tile *tiles;
-  const long long *first;  // [tiles + 1] key steps before a tile of a head
+  const long long *first;  // [tiles] cost of what is before a tile of a head, in steps
   const int *head;         // number of tiles of a head, rounds of tiles that are dealt
-  const long long *cuts;   // [CTAs + 1] what follows, in shares: first step, counted from the first one that is not dealt
+  const long long *cuts;   // [CTAs + 1] where the shares of what follows begin, counted from the first tile that is not dealt
   int32_t *arrivals;
   float4 *parts;           // [2 * CTAs][32][128]: four dims of a row
   float2 *part_l;          // [2 * CTAs][128]
@@ -211,12 +215,12 @@ constexpr int kSmallPlan = 4096;
 // The tiles of a head, sequence by sequence, and the key steps before each.  One CTA.
 __global__ void __launch_bounds__(1024) cache_plan_kernel(const CacheIndex ix, int tokens_per_tile, Tile *__restrict__ tiles,
                                                           long long *__restrict__ first, int *__restrict__ head, long long *__restrict__ cuts,
-                                                          int32_t *__restrict__ arrivals, int most, int Hkv) {
+                                                          int32_t *__restrict__ arrivals, int most, int Hkv, bool weigh) {
   __shared__ long long sums[32];
   __shared__ int base[1024];
-  __shared__ int steps[kSmallPlan];  // of the first tiles: as a rule all
+  __shared__ int costs[kSmallPlan];  // of the first tiles: as a rule all
   __shared__ Sequence own[32];
-  auto steps_of = [&](int i) { return i < kSmallPlan ? steps[i] : tiles[i].steps; };
+  auto cost_of = [&](int i) { return i < kSmallPlan ? costs[i] : tiles[i].steps + tiles[i].extra; };
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
   pdl_wait();
   pdl_launch_dependents();
@@ -256,9 +260,12 @@ __global__ void __launch_bounds__(1024) cache_plan_kernel(const CacheIndex ix, i
     x.every_end = x.p0 >= 0 ? v0.end : 0;
     x.some_low = v0.low;
     x.some_end = v1.end;
+    const int whole = max(x.every_end / kKeyStep - max((x.every_low + kKeyStep - 1) / kKeyStep, x.first), 0) + min(min(ix.sink, x.every_end) / kKeyStep, x.sinks);
+    x.extra = weigh ? kTileCost + kMaskCost * max(x.steps - whole, 0) : 0;
     tiles[i] = x;
-    if (i < kSmallPlan) steps[i] = sp.steps;
-    return sp.steps;
+    const int cost = x.steps + x.extra;
+    if (i < kSmallPlan) costs[i] = cost;
+    return cost;
   };
   long long before = 0;
   if (ix.S <= 32) {  // a lane a sequence, then a thread a tile
@@ -307,7 +314,7 @@ __global__ void __launch_bounds__(1024) cache_plan_kernel(const CacheIndex ix, i
       __syncthreads();
     }
     for (int t0 = 0; t0 < n_tiles; t0 += 1024) {
-      const int here = t0 + t < n_tiles ? steps_of(t0 + t) : 0;
+      const int here = t0 + t < n_tiles ? cost_of(t0 + t) : 0;
       longest = max(longest, here);
       long long all;
       const long long at = before + scan(here, all);
@@ -327,7 +334,7 @@ __global__ void __launch_bounds__(1024) cache_plan_kernel(const CacheIndex ix, i
     dealt = 0;
     if (t < kCacheCtas)
       for (int k = 0, i = t % n_tiles, by = kCacheCtas % n_tiles; k < rounds; ++k) {
-        dealt += steps_of(i);
+        dealt += cost_of(i);
         i = i + by < n_tiles ? i + by : i + by - n_tiles;
       }
     most_dealt = dealt;
@@ -493,7 +500,7 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
     const long long u0 = __ldcg(&p.cuts[blockIdx.x]), u1 = __ldcg(&p.cuts[blockIdx.x + 1]);
     const long long dealt = (long long)rounds * gridDim.x;  // tiles
     long long u = u0;  // of the share: the part's first step
-    int h, tile, a = 0;
+    int h, tile, off = 0;  // ... and what of its tile lies before it
     auto share_begins = [&]() {
       // the line's first step, as a step of all heads
       const int h0 = (int)(dealt / n_tiles);
@@ -512,7 +519,7 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
         tile += (n - 1) * step;
         hi = min(hi, tile + step);
       }
-      a = (int)(rest - begins);
+      off = (int)(rest - begins);
     };
     auto holders = [&](long long at, long long to, int &c0, int &c1) {  // the CTAs whose shares have these steps
       uint32_t n = 0;
@@ -555,11 +562,14 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
       any = !from_line || u < u1;
       if (lane < kTileWords) reinterpret_cast<int *>(&x.t)[lane] = word;
       __syncwarp();
-      const int b = !any ? -1 : from_line ? (int)min((long long)x.t.steps, a + (u1 - u)) : x.t.steps;
+      // (a tile in the line: its extra cost, its steps)
+      const int steps = x.t.steps, extra = x.t.extra, a = max(off - extra, 0);
+      int b = any ? from_line ? (int)min((long long)steps, off + (u1 - u) - extra) : steps : -1;
+      if (b <= a) b = -1, any = false;  // (the share ends before the tile's first step)
       int c0 = blockIdx.x, parts = 1;
-      if (any && b - a < x.t.steps) {
+      if (any && b - a < steps) {
         int c1;
-        holders(u - a, u - a + x.t.steps - 1, c0, c1);
+        holders(u - off + extra, u - off + extra + steps - 1, c0, c1);
         parts = c1 - c0 + 1;
       }
       if (lane == 0) {
@@ -574,12 +584,11 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
       if (!any) return;
       entry = entry_of(x.t, key_at(x.t, a));
       if (!from_line) {
-        a = 0;
         if (++k < rounds) next_dealt();
         else if (u < u1) share_begins();
       } else {
-        u += b - a;
-        a = 0;
+        u += extra + b - off;
+        off = 0;
         if (++tile == n_tiles) tile = 0, ++h;
       }
       if (k < rounds || u < u1) word = fetch(tile);
@@ -1348,7 +1357,7 @@ cudaError_t launch_cache_tiles(const CacheGeom &g, const CacheIndex &ix, const C
   p.test_skip = g.test_skip;
   p.scale_log2 = (float)(g.scale * 1.4426950408889634);
   cudaError_t e = launch_pdl(cache_plan_kernel, dim3(1), dim3(1024), 0, s, ix, 128 / g.G, reinterpret_cast<Tile *>(w.tiles), w.tile_first, w.tile_head,
-                             w.cuts, p.arrivals, (int)cache_max_tiles(g), g.Hkv);
+                             w.cuts, p.arrivals, (int)cache_max_tiles(g), g.Hkv, (long long)cache_max_tiles(g) * g.Hkv >= 2 * kCacheCtas);
   if (e != cudaSuccess) return e;
   ++*launches;
   e = g.e4m3 ? launch<true>(mq, mk, mv, p, s) : launch<false>(mq, mk, mv, p, s);
