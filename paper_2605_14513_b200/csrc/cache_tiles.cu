@@ -225,23 +225,33 @@ __global__ void __launch_bounds__(1024) cache_plan_kernel(const CacheIndex ix, i
   pdl_wait();
   pdl_launch_dependents();
   for (int i = t; i < kCacheCtas; i += 1024) arrivals[i] = 0;
-  auto scan = [&](long long mine, long long &all) {  // exclusive, over the CTA
-    long long x = mine;
+  auto upto_lane = [&](long long x) {  // inclusive, over the warp
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const long long y = __shfl_up_sync(0xffffffffu, x, o);
       if (lane >= o) x += y;
     }
+    return x;
+  };
+  auto scan = [&](long long mine, long long &all) {  // exclusive, over the CTA
+    const long long x = upto_lane(mine);
     __syncthreads();
     if (lane == 31) sums[warp] = x;
     __syncthreads();
-    long long before = x - mine;
-    all = 0;
-    for (int i = 0; i < 32; ++i) {
-      if (i < warp) before += sums[i];
-      all += sums[i];
-    }
-    return before;
+    const long long warps = upto_lane(sums[lane]), before = __shfl_sync(0xffffffffu, warps, max(warp - 1, 0));
+    all = __shfl_sync(0xffffffffu, warps, 31);
+    return x - mine + (warp > 0 ? before : 0);
+  };
+  auto largest = [&](long long x) {  // over the CTA
+#pragma unroll
+    for (int o = 16; o; o >>= 1) x = max(x, __shfl_xor_sync(0xffffffffu, x, o));
+    __syncthreads();
+    if (lane == 0) sums[warp] = x;
+    __syncthreads();
+    x = sums[lane];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) x = max(x, __shfl_xor_sync(0xffffffffu, x, o));
+    return x;
   };
   int n_tiles = 0, longest = 1;
   auto make_tile = [&](int i, int s, const Sequence &q, int k) {
@@ -271,12 +281,7 @@ __global__ void __launch_bounds__(1024) cache_plan_kernel(const CacheIndex ix, i
   if (ix.S <= 32) {  // a lane a sequence, then a thread a tile
     const Sequence q = lane < ix.S ? sequence(ix, lane) : Sequence{0, 0, 0};
     const int mine = (q.n + tokens_per_tile - 1) / tokens_per_tile;
-    long long upto = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long y = __shfl_up_sync(0xffffffffu, upto, o);
-      if (lane >= o) upto += y;
-    }
+    const long long upto = upto_lane(mine);
     n_tiles = (int)min(__shfl_sync(0xffffffffu, upto, 31), (long long)most);
     if (warp == 0) {
       base[lane] = (int)min(upto - mine, (long long)most);
@@ -322,11 +327,7 @@ __global__ void __launch_bounds__(1024) cache_plan_kernel(const CacheIndex ix, i
       before += all;
     }
   }
-  longest = __reduce_max_sync(0xffffffffu, longest);
-  __syncthreads();
-  if (lane == 0) sums[warp] = longest;
-  __syncthreads();
-  for (int i = 0; i < 32; ++i) longest = max(longest, (int)sums[i]);
+  longest = (int)largest(longest);
   const long long per_head = before, total = per_head * Hkv, all_tiles = (long long)n_tiles * Hkv;
   int rounds = (int)max(all_tiles / kCacheCtas - 1, 0LL);
   long long dealt = 0, most_dealt = 0;  // to CTA t, to the one with most
@@ -337,13 +338,7 @@ __global__ void __launch_bounds__(1024) cache_plan_kernel(const CacheIndex ix, i
         dealt += cost_of(i);
         i = i + by < n_tiles ? i + by : i + by - n_tiles;
       }
-    most_dealt = dealt;
-#pragma unroll
-    for (int o = 16; o; o >>= 1) most_dealt = max(most_dealt, __shfl_xor_sync(0xffffffffu, most_dealt, o));
-    __syncthreads();
-    if (lane == 0) sums[warp] = most_dealt;
-    __syncthreads();
-    for (int i = 0; i < 32; ++i) most_dealt = max(most_dealt, sums[i]);
+    most_dealt = largest(dealt);
     if (most_dealt * kCacheCtas <= total) break;
     rounds = min(rounds - 1, (int)(rounds * (total / kCacheCtas) / most_dealt));  // (tiles of very different lengths: fewer of them are dealt)
   }
@@ -357,16 +352,25 @@ __global__ void __launch_bounds__(1024) cache_plan_kernel(const CacheIndex ix, i
     if (t <= kCacheCtas) cuts[t] = min(t * share, total);
     return;
   }
-  // the least sum to which shares of at least one step can bring all
+  // the least sum to which shares of at least one step can bring all: every warp looks for it by itself, a lane five CTAs
+  __shared__ long long of_cta[kCacheCtas];
+  if (t < kCacheCtas) of_cta[t] = dealt;
   long long all;
   scan(dealt, all);
   const long long rest = total - all;  // a tile's step a CTA at least
+  long long five[5];
+#pragma unroll
+  for (int i = 0; i < 5; ++i) five[i] = i * 32 + lane < kCacheCtas ? of_cta[i * 32 + lane] : 1LL << 62;
   // the sum lies in (lo, hi]
   long long lo = (total + kCacheCtas - 1) / kCacheCtas - 1, hi = most_dealt + (rest + kCacheCtas - 1) / kCacheCtas;
   while (hi - lo > 1) {
     const long long sum = (lo + hi) / 2;
-    long long shares;
-    scan(t < kCacheCtas ? max(sum - dealt, 1LL) : 0, shares);
+    long long shares = 0;
+#pragma unroll
+    for (int i = 0; i < 5; ++i)
+      if (i * 32 + lane < kCacheCtas) shares += max(sum - five[i], 1LL);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) shares += __shfl_xor_sync(0xffffffffu, shares, o);
     (shares >= rest ? hi : lo) = sum;
   }
   const long long at = scan(t < kCacheCtas ? max(hi - dealt, 1LL) : 0, all);
