@@ -204,10 +204,11 @@ __device__ __forceinline__ void sts_u1(uint32_t addr, uint32_t v) { asm volatile
 __device__ __forceinline__ void sts_u4(uint32_t addr, uint4 v) {
   asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
-// Whether one of eight bf16 numbers is not finite: an exponent field of ones carries into the sign's place.
-__device__ __forceinline__ bool not_finite(const uint4 &x) {
-  auto carry = [](uint32_t w) { return (w & 0x7f807f80u) + 0x00800080u; };
-  return ((carry(x.x) | carry(x.y) | carry(x.z) | carry(x.w)) & 0x80008000u) != 0u;
+// Zero as long as all of the bf16 numbers so far are finite, NaN from the first one on that is not: 0 * x + sum.
+__device__ __forceinline__ uint32_t add_zero_times(const uint4 &x, uint32_t sum) {
+  auto add = [&](uint32_t w) { asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(sum) : "r"(w), "r"(0u)); };
+  add(x.x), add(x.y), add(x.z), add(x.w);
+  return sum;
 }
 
 // ---------------------------------------------------------------------- plan
@@ -759,7 +760,7 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
                 const int kj = mine + 4 * j;
                 const bool seen = kj < some_end && (kj >= some_low || kj < ix.sink);
                 if (!seen) out |= 1u << j;
-                else if (not_finite(v[j]) || not_finite(w[j])) out |= 17u << j;
+                else if (add_zero_times(w[j], add_zero_times(v[j], 0u)) != 0u) out |= 17u << j;
               }
               if (__all_sync(0xffffffffu, out == 0u)) continue;
 #pragma unroll
