@@ -79,7 +79,7 @@ constexpr int kStepMasked = 1, kStepStarts = 2, kStepEnd = 4;  // some row does 
 template <bool E4m3>
 struct Layout {
   static constexpr int kThreads = E4m3 ? 512 : 384;
-  static constexpr int kRegsSoftmax = E4m3 ? 184 : 224, kRegsHelper = E4m3 ? 64 : 56, kRegsConvert = 80;  // sums: the registers at launch
+  static constexpr int kRegsSoftmax = E4m3 ? 192 : 224, kRegsHelper = 56, kRegsConvert = 72;  // sums: the registers at launch
   static constexpr int kReaders = E4m3 ? 15 : 11;  // of announced parts: softmax warps, issuers, V producer, converters
   static constexpr int kKey = E4m3 ? kCodeBytes : kTileBytes;
   // Q, K, V (of which the products read), codes of V
@@ -923,7 +923,7 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
         // 3.48 ms instead of 3.03.)
         const uint32_t from = vs == 0 ? smem_u32(sh.zeros) : smem_u32(smem + L::kOffCodes + b * kCodeBytes) + r * 128;
 #pragma unroll 1
-        for (int j = 0; j < 8; ++j) {  // 16 dims (instructions are what is short: 12 x 4680 over 12.7k, when this was written, 387 us, unrolled by 2, 4 and 8 399, 420 and 453)
+        for (int j = 0; j < 8; ++j) {  // 16 dims (instructions are what is short: 12 x 4680 over 12.7k 368 us, unrolled by 2 and 4 372 and 375; 6 prompts x 24 heads 161, 165 and 173)
           const uint4 w = lds_u4(from + (((j ^ r) & 7) << 4));
           const uint32_t half = to + (j >> 2) * (kTileBytes / 2);
           sts_u4(half + ((((j & 3) * 2) ^ (r & 7)) << 4), make_uint4(mul_f16x2(codes_to_f16x2(w.x), f2), mul_f16x2(high_codes_to_f16x2(w.x), f2),
