@@ -24,8 +24,6 @@ def bits(x):
     return x.contiguous().view(torch.uint8).cpu()
 
 
-
-
 @pytest.mark.parametrize("max_new", [1, 0])
 @pytest.mark.parametrize("seed", range(3))
 def test_pages_hold_anything_behind_a_sequence(heart, seed, max_new):
@@ -208,6 +206,30 @@ def test_dealt_tiles(heart):
         # (as check_attention: a weight is rounded once, the result once)
         assert ((O[:, h].double() - want).abs() <= (2 ** -8 + 2 ** -12) * most + 2 ** -8 * want.abs()).all()
         assert ((lse[:, h].double() - torch.logsumexp(logits, -1)).abs() <= 2 ** -14).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("name", ["ragged prompts", "more sequences", "one long among short", "short among long"])
+def test_several_tiles_a_cta(heart, name, kind):
+    """Tiles of unlike cost: masked and whole steps, long and short, sequences by the lane and by the thread."""
+    g = torch.Generator().manual_seed(11)
+    if name == "ragged prompts":
+        new = torch.randint(1, 700, (6,), generator=g).tolist()
+        kw = dict(new=new, lens=[n + int(torch.randint(0, 500, (1,), generator=g)) for n in new], Hq=24, Hkv=8, causal=1, window=256, sink=4)
+    elif name == "more sequences":
+        new = torch.randint(0, 90, (50,), generator=g).tolist()
+        kw = dict(new=new, lens=[n + int(torch.randint(0, 300, (1,), generator=g)) for n in new], Hq=12, Hkv=6, causal=16, page=32)
+    elif name == "one long among short":
+        kw = dict(new=[60] + [40] * 60, lens=[6000] + [40] * 60, Hq=8, Hkv=8, causal=1, page=64)
+    else:
+        kw = dict(new=[40] * 41, lens=[900] * 20 + [40] + [900] * 20, Hq=10, Hkv=10, page=128)
+    c = Case(**kw, kind=kind, pad=9, seed=3)
+    d = Device(heart, c)
+    O, lse = d.attention()
+    assert heart.heart_get_status(d.ws) == 0
+    check_attention(c, O, lse)
+    again = d.attention()
+    assert torch.equal(bits(O), bits(again[0])) and torch.equal(bits(lse), bits(again[1]))
 
 
 @pytest.mark.parametrize("kind", ["bf16", "e4m3"])
