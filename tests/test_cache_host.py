@@ -103,13 +103,15 @@ def test_pools_on_the_host_are_refused(heart):
 
 def fake_cache(heart, cfg):
     """As far as the checks of a call look at it, on the host."""
-    return types.SimpleNamespace(device=-1, layout=heart._cache_layout(cfg))
+    return types.SimpleNamespace(device=-1, layout=heart._cache_layout(cfg), fields=heart._cache_fields(cfg))
 
 
-def call(heart, cfg, cache, x, heads=2, strides=(0, 0)):
+def call(heart, cfg, cache, x, strides=(0, 0)):
+    cfg = heart.CacheConfig.from_buffer_copy(cfg)
+    cfg.kv_stride_t, cfg.kv_stride_h = strides
     ints = [torch.zeros(n, dtype=torch.int32) for n in (cfg.S * cfg.table_stride, cfg.S + 1, cfg.S)]
     ws = torch.zeros(heart.cache_workspace_bytes(cfg), dtype=torch.uint8)
-    heart._cache_call(cfg, cache, heads, *strides, (x,), *ints, ws)
+    heart._cache_call(cfg, cache, False, (x,), *ints, ws)
 
 
 def test_a_cache_of_other_pools_is_refused(heart):
