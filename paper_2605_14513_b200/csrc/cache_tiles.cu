@@ -13,8 +13,9 @@
 //     take the same time), but for the last one to two rounds of them: the steps of those, in one line, are cut into shares that
 //     bring all CTAs to the same sum, so that the launch ends on all SMs at once whatever the lengths are.  The sum counts a tile's beginning
 //     and end as four steps and a step that some row does not see whole as three (12 x 4680 over 32760, causal by frames, 770 us with
-//     steps alone, now 738; 6 prompts x 24 heads 130, now 126; other weights near these give the same), unless the launch has less than two tiles a CTA.  Parts of a tile go to the workspace; the CTA that brings the last one puts them together,
-//     in order: the result does not depend on which one that is.
+//     steps alone, now 738; 6 prompts x 24 heads 130, now 126; other weights near these give the same), unless the launch has less
+//     than two tiles a CTA.  Parts of a tile go to the workspace; the CTA that brings the last one puts them together, in order: the
+//     result does not depend on which one that is.
 //
 // e4m3 caches.  Converting keys and values to bf16 for 128 rows costs as many instructions as the softmax does.  Keys need none: a bf16 query has
 // 8 significant bits and a code 4, so a query row, scaled by a power of two, is the sum of two rows of codes, to 2^-18 of its
@@ -74,7 +75,7 @@ struct Step {
   int key, keys, h, flags;  // first key, keys of the sequence from there on, key head
   int page[8];
 };
-constexpr int kStepMasked = 1, kStepStarts = 2, kStepEnd = 4;  // some row does not see all of its keys; first step of a part; no step left
+constexpr int kStepMasked = 1, kStepEnd = 2;  // some row does not see all of its keys; no step left
 
 template <bool E4m3>
 struct Layout {
@@ -618,7 +619,7 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
           y.key = k0;
           y.keys = (int)len - k0;
           y.h = h_now;
-          y.flags = (k0 + kKeyStep <= every_end && (k0 >= every_low || k0 + kKeyStep <= sink) ? 0 : kStepMasked) | (i == a_now ? kStepStarts : 0);
+          y.flags = k0 + kKeyStep <= every_end && (k0 >= every_low || k0 + kKeyStep <= sink) ? 0 : kStepMasked;
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.step_full[g % kSteps]);
@@ -923,7 +924,7 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
         // 3.48 ms instead of 3.03.)
         const uint32_t from = vs == 0 ? smem_u32(sh.zeros) : smem_u32(smem + L::kOffCodes + b * kCodeBytes) + r * 128;
 #pragma unroll 1
-        for (int j = 0; j < 8; ++j) {  // 16 dims (instructions are what is short: 12 x 4680 over 12.7k 368 us, unrolled by 2 and 4 372 and 375; 6 prompts x 24 heads 161, 165 and 173)
+        for (int j = 0; j < 8; ++j) {  // 16 dims (fetches of instructions are what is short: unrolled by 1, 2 and 4, 6 prompts x 24 heads 161, 165 and 173 us)
           const uint4 w = lds_u4(from + (((j ^ r) & 7) << 4));
           const uint32_t half = to + (j >> 2) * (kTileBytes / 2);
           sts_u4(half + ((((j & 3) * 2) ^ (r & 7)) << 4), make_uint4(mul_f16x2(codes_to_f16x2(w.x), f2), mul_f16x2(high_codes_to_f16x2(w.x), f2),
