@@ -12,9 +12,10 @@
 // The conversion to f16 is one instruction for two codes, so e4m3 caches are multiplied in f16, which holds codes exactly:
 //   * a query row, scaled by a power of two to a largest element in [2^14, 2^15), is in f16 what it is in bf16 (but for elements below
 //     2^-32 of the largest, which lose bits);
-//   * weights lie between 0 and 2^14, the largest so far at 2^6 to 2^14: one below 2^-31 of it counts as zero;
-//   * values are code * 2^(e - E), e the token's exponent and E the largest so far: exact down to 2^-15 of the largest scale, and to 2^-33 of the
-//     largest value below.  E moves O as a row's reference does.
+//   * values are the codes; a token's scale 2^e goes into its weight, behind the mask, so that what a row does not see has no part in it: the product takes
+//     2^(score + e - m), between 0 and 2^14, the row's largest so far at 2^6 to 2^14.  One below 2^-31 of it counts as zero.
+//   * the row sum, of 2^(score - m'), has a reference of its own, a lane's: scales may be any number of binades apart.  (Eight exponentials more for 32
+//     keys, and no multiplication of values: 64 single tokens over up to 16k, 32 heads on 8, 246 us, and 251 with the scales multiplied into values.)
 // (The warp-wide products of e4m3 codes themselves are carried out as conversions and f16 products here, 96 for the 64 in the source.)
 //
 // Work: rows of a sequence and key head, packed as (token, query head of the group), in tiles of 8 or 16; all key steps of all tiles in one line,
@@ -65,7 +66,8 @@ struct RowsParams {
 struct alignas(16) RowsShared {
   uint64_t full[kWarps][kMaxStages];
   alignas(16) uint8_t scales[kWarps][kMaxStages][64];  // e4m3: of the keys and of the values of a stage
-  float2 l[kWarps][16];   // row sums and references
+  float2 l[kWarps][16];   // row sums and their references
+  float o_ref[kWarps][16];  // e4m3: references of the sums of values
   long long total[kWarps];
   int longest[kWarps];
   int found;              // sequence of the CTA's first step
@@ -412,9 +414,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     float o[NT][8][4] = {};
     float ref[NT][2], sum[NT][2];
-    uint32_t v_exp = 0;  // e4m3: O stands for 2^(v_exp - 127) of its value
+    float sum_ref[NT][2];  // e4m3: of this lane's sums
 #pragma unroll
-    for (int m = 0; m < NT; ++m) ref[m][0] = ref[m][1] = kNoReference, sum[m][0] = sum[m][1] = 0.f;
+    for (int m = 0; m < NT; ++m) ref[m][0] = ref[m][1] = sum_ref[m][0] = sum_ref[m][1] = kNoReference, sum[m][0] = sum[m][1] = 0.f;
 
 #pragma unroll 1
     for (int i = done; i < end_step; ++i) {
@@ -426,33 +428,16 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t k_at = ring_at + take * kStage, v_at = k_at + kHalf;
       const bool whole = k0 + kKeys <= every_end && (k0 >= every_low || k0 + kKeys <= ix.sink);
       float x[NT][kTiles][4] = {};
-      uint32_t vs[kTiles][2];  // e4m3: this lane's values are to be multiplied by these, two keys at a time
+      float v_exp = 0.f;  // e4m3: the exponent of the value of key `lane`
       // ---- scores: keys g and g + 8 of every 16, rows 2c and 2c + 1
       if (E4m3) {
-        // the scales, a lane a key: 2^e of the key (NaN where the token's key or value is not finite), 2^(e - E) of the value (nothing behind the
-        // sequence's end and where it is not finite)
+        // the scales, a lane a key: 2^e of the key (NaN where the token's key or value is not finite), e of the value
         const int key = lane & (kKeys - 1);
-        const uint32_t kb = sh.scales[warp][take][key];
-        uint32_t vb = sh.scales[warp][take][kKeys + key];
+        const uint32_t kb = sh.scales[warp][take][key], vb = sh.scales[warp][take][kKeys + key];
         const float k_scale = cache_scale(vb == 255u ? 255u : kb);
-        if (vb == 255u || k0 + key >= q.len) vb = 0u;
-        const uint32_t top = __reduce_max_sync(0xffffffffu, vb);
-        if (top > v_exp) {
-          const float f = cache_scale(max((int)(v_exp - top) + 127, 1));
-          v_exp = top;
-#pragma unroll
-          for (int m = 0; m < NT; ++m)
-#pragma unroll
-            for (int n = 0; n < 8; ++n)
-#pragma unroll
-              for (int k = 0; k < 4; ++k) o[m][n][k] *= f;
-        }
-        const float v_scale = vb == 0u ? 0.f : cache_scale(max((int)(vb - v_exp) + 127, 1));
-        const uint32_t pair = pack_f16x2(v_scale, __shfl_down_sync(0xffffffffu, v_scale, 1));
+        v_exp = (float)((int)vb - 127);
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) {
-          vs[t][0] = __shfl_sync(0xffffffffu, pair, t * 16 + c * 2);
-          vs[t][1] = __shfl_sync(0xffffffffu, pair, t * 16 + 8 + c * 2);
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             const uint4 lo = lds_u4(k_at + (t * 16 + g) * 128 + (((c * 2 + j) ^ g) << 4)), hi = lds_u4(k_at + (t * 16 + 8 + g) * 128 + (((c * 2 + j) ^ g) << 4));
@@ -495,6 +480,41 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int k = 0; k < 4; ++k)
               if (hidden(vis[m][k & 1], k0 + t * 16 + g + (k >> 1) * 8)) x[m][t][k] = -INFINITY;
       }
+      if (E4m3) {
+        // the row sums, each lane's over its own keys; then scores with the exponents of the values
+        auto sums = [&](auto masked) {
+#pragma unroll
+          for (int m = 0; m < NT; ++m)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+              float top = -INFINITY;
+#pragma unroll
+              for (int t = 0; t < kTiles; ++t) top = fmaxf(top, fmaxf(x[m][t][r], x[m][t][2 + r]));
+              top *= row_scale[m][r];
+              if (top > sum_ref[m][r] + kMaxGrowth) {
+                sum[m][r] *= ex2(sum_ref[m][r] - top);
+                sum_ref[m][r] = top;
+              }
+            }
+#pragma unroll
+          for (int t = 0; t < kTiles; ++t) {
+            const float e_lo = __shfl_sync(0xffffffffu, v_exp, t * 16 + g), e_hi = __shfl_sync(0xffffffffu, v_exp, t * 16 + 8 + g);
+#pragma unroll
+            for (int m = 0; m < NT; ++m)
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const float y = x[m][t][k], w = ex2(fmaf(y, row_scale[m][k & 1], -sum_ref[m][k & 1]));
+                const float z = fmaf(y, row_scale[m][k & 1], k < 2 ? e_lo : e_hi);
+                // (what is hidden is nothing, even to a query that is not finite)
+                const bool none = decltype(masked)::value && y == -INFINITY;
+                sum[m][k & 1] += none ? 0.f : w;
+                x[m][t][k] = none ? -INFINITY : z;
+              }
+          }
+        };
+        if (whole) sums(False{});
+        else sums(True{});
+      }
       bool moved = false;
       float alpha[NT][2];
 #pragma unroll
@@ -507,7 +527,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
           top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
           top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-          top *= row_scale[m][r];
+          if (!E4m3) top *= row_scale[m][r];
           alpha[m][r] = 1.f;
           if (top > ref[m][r] + (E4m3 ? kHeadroomE4m3 : 0.f) + kMaxGrowth) {
             const float to = E4m3 ? top - kHeadroomE4m3 : top;
@@ -519,8 +539,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
         for (int m = 0; m < NT; ++m) {
-          sum[m][0] *= alpha[m][0];
-          sum[m][1] *= alpha[m][1];
+          if (!E4m3) {
+            sum[m][0] *= alpha[m][0];
+            sum[m][1] *= alpha[m][1];
+          }
 #pragma unroll
           for (int n = 0; n < 8; ++n)
 #pragma unroll
@@ -528,27 +550,20 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       uint32_t pf[NT][kTiles][2];  // as operands: row g, keys 2c, 2c + 1 of every 8
-      auto weights = [&](auto masked) {
 #pragma unroll
-        for (int m = 0; m < NT; ++m)
+      for (int m = 0; m < NT; ++m)
 #pragma unroll
-          for (int t = 0; t < kTiles; ++t) {
-            float w[4];
+        for (int t = 0; t < kTiles; ++t) {
+          float w[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const float y = x[m][t][k];
-              w[k] = ex2(fmaf(y, row_scale[m][k & 1], -ref[m][k & 1]));
-              // (what is hidden is nothing, even to a query that is not finite)
-              if (decltype(masked)::value && y == -INFINITY) w[k] = 0.f;
-            }
+          for (int k = 0; k < 4; ++k) w[k] = ex2(E4m3 ? x[m][t][k] - ref[m][k & 1] : fmaf(x[m][t][k], row_scale[m][k & 1], -ref[m][k & 1]));
+          if (!E4m3) {
             sum[m][0] += w[0] + w[2];
             sum[m][1] += w[1] + w[3];
-            pf[m][t][0] = transposed(E4m3 ? pack_f16x2(w[0], w[1]) : pack_bf16x2(w[0], w[1]));
-            pf[m][t][1] = transposed(E4m3 ? pack_f16x2(w[2], w[3]) : pack_bf16x2(w[2], w[3]));
           }
-      };
-      if (E4m3 && !whole) weights(True{});
-      else weights(False{});
+          pf[m][t][0] = transposed(E4m3 ? pack_f16x2(w[0], w[1]) : pack_bf16x2(w[0], w[1]));
+          pf[m][t][1] = transposed(E4m3 ? pack_f16x2(w[2], w[3]) : pack_bf16x2(w[2], w[3]));
+        }
       if (!E4m3 && !whole) {
         // Values that are not finite must not reach rows that do not see them (0 * inf is NaN): they are taken out, and rows that
         // do see them are marked.
@@ -597,8 +612,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int k = 0; k < 2; ++k) {
               // codes of two dims of a key and of the next: the even dims of both, the odd ones
               const uint32_t lo = __byte_perm(b[2 * k], 0, 0x3120), hi = __byte_perm(b[2 * k + 1], 0, 0x3120);
-              const uint32_t a[4] = {mul_f16x2(codes_to_f16x2(lo), vs[t][0]), mul_f16x2(high_codes_to_f16x2(lo), vs[t][0]),
-                                     mul_f16x2(codes_to_f16x2(hi), vs[t][1]), mul_f16x2(high_codes_to_f16x2(hi), vs[t][1])};
+              const uint32_t a[4] = {codes_to_f16x2(lo), high_codes_to_f16x2(lo), codes_to_f16x2(hi), high_codes_to_f16x2(hi)};
 #pragma unroll
               for (int m = 0; m < NT; ++m) mma_f16(o[m][j + k], a, pf[m][t][0], pf[m][t][1]);
             }
@@ -636,21 +650,30 @@ __global__ void __launch_bounds__(kThreads, 1)
     const bool apart = n_rows <= kApartRows;
     unsigned char *sums = apart ? smem + kWarps * kRing + sizeof(RowsShared) : smem;
     const int sums_pitch = apart ? kApartRows * 512 : kRing;
-    const float o_scale = E4m3 ? cache_scale(v_exp) : 1.f;
 #pragma unroll
     for (int m = 0; m < NT; ++m)
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
+        if (E4m3) {
+          float most = sum_ref[m][r];
+#pragma unroll
+          for (int k = 4; k < 32; k <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, k));
+          sum[m][r] *= ex2(sum_ref[m][r] - most);
+          sum_ref[m][r] = most;
+        }
 #pragma unroll
         for (int k = 4; k < 32; k <<= 1) sum[m][r] += __shfl_xor_sync(0xffffffffu, sum[m][r], k);
         const int row = m * 8 + c * 2 + r;
         if (row >= n_rows) continue;
-        if (g == 0) sh.l[warp][row] = make_float2(sum[m][r], ref[m][r]);
+        if (g == 0) {
+          sh.l[warp][row] = make_float2(sum[m][r], E4m3 ? sum_ref[m][r] : ref[m][r]);
+          if (E4m3) sh.o_ref[warp][row] = ref[m][r];
+        }
         unsigned char *to = sums + warp * sums_pitch + row * 512;
 #pragma unroll
         for (int n = 0; n < 8; ++n) {
           if (E4m3) {
-            *reinterpret_cast<float2 *>(to + ((n * 64 + g * 8) ^ ((row & 7) << 5))) = make_float2(o[m][n][r] * o_scale, o[m][n][2 + r] * o_scale);
+            *reinterpret_cast<float2 *>(to + ((n * 64 + g * 8) ^ ((row & 7) << 5))) = make_float2(o[m][n][r], o[m][n][2 + r]);
           } else {
             *reinterpret_cast<float *>(to + ((n * 64 + g * 4) ^ ((row & 7) << 5))) = o[m][n][r];
             *reinterpret_cast<float *>(to + ((n * 64 + 32 + g * 4) ^ ((row & 7) << 5))) = o[m][n][2 + r];
@@ -688,20 +711,27 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int d = lane * 4;
 #pragma unroll 1
     for (int row = warp; row < rows; row += kWarps) {
-      float m = kNoReference, l = 0.f;
+      float m = kNoReference, m_o = kNoReference, l = 0.f;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) m = fmaxf(m, sh.l[w][row].y);
+      for (int w = 0; w < kWarps; ++w) {
+        m = fmaxf(m, sh.l[w][row].y);
+        if (E4m3) m_o = fmaxf(m_o, sh.o_ref[w][row]);
+      }
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {
         const float2 lm = sh.l[w][row];
-        const float f = ex2(lm.y - m);
+        const float f = ex2(lm.y - m), f_o = E4m3 ? ex2(sh.o_ref[w][row] - m_o) : f;
         const float4 y = *reinterpret_cast<const float4 *>(sums + w * sums_pitch + row * 512 + ((d * 4) ^ ((row & 7) << 5)));
         l = fmaf(lm.x, f, l);
-        v.x = fmaf(y.x, f, v.x);
-        v.y = fmaf(y.y, f, v.y);
-        v.z = fmaf(y.z, f, v.z);
-        v.w = fmaf(y.w, f, v.w);
+        v.x = fmaf(y.x, f_o, v.x);
+        v.y = fmaf(y.y, f_o, v.y);
+        v.z = fmaf(y.z, f_o, v.z);
+        v.w = fmaf(y.w, f_o, v.w);
+      }
+      if (E4m3) {  // in units of the row sum
+        const float f = ex2(m_o - m);
+        v = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
       }
       if (sh.abort) l = __uint_as_float(0x7fc00000u);
       if (all) {
