@@ -35,6 +35,8 @@ struct CacheWorkspace {
   long long *tile_first;  // [max_tiles + 1] cost of the tiles before a tile, in key steps
   int *tile_head;     // [64] number of tiles of a head, rounds of them that are dealt
   long long *cuts;    // [kCacheCtas + 1] the CTAs' shares of the other ones
+  int *any_redo;      // [kCacheCtas] 1 where a CTA that looked at the scales found something to do again by rows
+  uint8_t *redo;      // [S * Hkv] 1: the sequence and key head is to be done again
   size_t bytes;
 };
 
@@ -59,6 +61,8 @@ __host__ inline CacheWorkspace carve_cache(const CacheGeom &g, void *base) {
   w.tile_first = reinterpret_cast<long long *>(take(sizeof(long long) * (cache_max_tiles(g) + 1)));
   w.tile_head = reinterpret_cast<int *>(take(64 * sizeof(int)));
   w.cuts = reinterpret_cast<long long *>(take((kCacheCtas + 1) * sizeof(long long)));
+  w.any_redo = reinterpret_cast<int *>(take(kCacheCtas * sizeof(int)));
+  w.redo = reinterpret_cast<uint8_t *>(take((size_t)g.S * g.Hkv));
   w.bytes = off;
   return w;
 }
@@ -74,6 +78,9 @@ cudaError_t launch_cache_read(const CacheGeom &g, const CacheIndex &ix, const he
 constexpr int kRowsOfRowsKernel = 16;
 cudaError_t launch_cache_rows(const CacheGeom &g, const CacheIndex &ix, const CacheWorkspace &w, const void *Q, const heart_cache &c,
                               void *O, float *lse, cudaStream_t s, int *launches);
+// Behind the tile kernel, for e4m3: by rows what `looked` CTAs have put down in w.redo (most often nothing).
+cudaError_t launch_cache_redo(const CacheGeom &g, const CacheIndex &ix, const CacheWorkspace &w, const void *Q, const heart_cache &c,
+                              void *O, float *lse, int looked, cudaStream_t s, int *launches);
 cudaError_t launch_cache_tiles(const CacheGeom &g, const CacheIndex &ix, const CacheWorkspace &w, const void *Q, const heart_cache &c,
                                void *O, float *lse, cudaStream_t s, int *launches);
 

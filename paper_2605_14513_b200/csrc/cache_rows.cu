@@ -23,6 +23,9 @@
 // workspace, and the CTA that brings the last part puts the tile together, its parts in order: the result does not depend on which
 // one came last.  Every CTA finds its share by itself from the sequences' lengths, so the launch needs no plan and no lengths on the host, and a
 // captured one follows the lengths.
+//
+// Behind the tile kernel of an e4m3 cache the same code does those sequences and key heads again whose scales that kernel cannot hold, whole tiles
+// of 16 rows dealt in turn; as a rule there are none, and the launch ends at once.
 #include <cuda.h>
 
 #include "cache.cuh"
@@ -61,6 +64,9 @@ struct RowsParams {
   int32_t *arrivals;
   float *parts;
   float2 *part_l;
+  const uint8_t *redo;   // see CacheWorkspace
+  const int *any_redo;
+  int looked;
 };
 
 struct alignas(16) RowsShared {
@@ -117,7 +123,7 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
 // Keys that a warp takes at a time, 4 KB of them.
 __host__ __device__ constexpr int keys_of(bool e4m3) { return e4m3 ? 32 : 16; }
 
-template <int NT, bool E4m3>
+template <int NT, bool E4m3, bool Redo>
 __global__ void __launch_bounds__(kThreads, 1)
     cache_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const RowsParams p) {
   constexpr int kRows = 8 * NT;
@@ -140,6 +146,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncthreads();
   pdl_wait();
   pdl_launch_dependents();
+  if (Redo && !__syncthreads_or(tid < p.looked && __ldcg(&p.any_redo[tid]) != 0)) return;
 
   // ------------------------------------------------------------------ the CTA's share
   auto tiles_of = [&](const Sequence &q) { return (int)(((long long)q.n * p.G + kRows - 1) / kRows); };
@@ -164,7 +171,37 @@ __global__ void __launch_bounds__(kThreads, 1)
   int s, longest = 1;
   long long share, u, u1, sequence_at, per_head;  // units of a CTA, its first one and the one behind its last; of the sequence, and of one of its heads
   bool one_tile = false;                          // shares do not cross tiles
-  if (ix.S <= 32) {
+  int h = 0, t = 0, done = 0;                     // head, tile and the tile's steps before this share
+  // to be done again: the next tile of this CTA, whole
+  long long pair = 0;
+  auto next_redo = [&]() {
+    const long long pairs = (long long)ix.S * p.Hkv;
+    t += (int)gridDim.x;
+    while (pair < pairs) {
+      const uint32_t word = __ldcg(reinterpret_cast<const uint32_t *>(p.redo) + (pair >> 2)) >> (8 * (pair & 3));
+      if (word == 0u) {
+        pair = (pair | 3) + 1;
+        continue;
+      }
+      pair += (__ffs(word) - 1) >> 3;
+      if (pair >= pairs) break;  // (the last word has bytes of no pair)
+      s = (int)(pair / p.Hkv);
+      h = (int)(pair - (long long)s * p.Hkv);
+      q = sequence(ix, s);
+      const int tiles = tiles_of(q);
+      if (t < tiles) return true;
+      t -= tiles;
+      ++pair;
+    }
+    return false;
+  };
+  if (Redo) {
+    t = (int)blockIdx.x - (int)gridDim.x;
+    if (!next_redo()) return;
+    share = 1;
+    sequence_at = per_head = u = 0;
+    u1 = 1LL << 62;
+  } else if (ix.S <= 32) {
     // every warp by itself, a lane a sequence
     if (lane < ix.S) q = sequence(ix, lane);
     per_head = steps_of(q, longest);
@@ -270,8 +307,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     sequence_at = sh.found_at;
     per_head = sh.found_steps;
   }
-  int h, t = 0, done;  // head, tile and the tile's steps before this share
-  {
+  if (!Redo) {
     long long rest = u - sequence_at;
     h = (int)quotient(rest, per_head);
     rest -= h * per_head;
@@ -687,10 +723,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int tile_steps = steps;
     const int part = 2 * blockIdx.x + (done == 0 ? 1 : 0);
     u += end_step - done;
-    const bool more = !one_tile && u < u1;
+    const bool more = Redo ? next_redo() : !one_tile && u < u1;
     if (more) {
       done = 0;
-      if (++t == tiles_of(q)) {
+      if (!Redo && ++t == tiles_of(q)) {
         t = 0;
         if (++h == p.Hkv) {
           h = 0;
@@ -812,21 +848,18 @@ bool make_pool_map(CUtensorMap *m, const void *base, const CacheGeom &g, int row
 
 namespace {
 
-template <int NT, bool E4m3>
-cudaError_t launch(const CacheGeom &g, const RowsParams &p, const CUtensorMap &mk, const CUtensorMap &mv, cudaStream_t s, int *launches) {
-  cudaError_t e = allow_shared_memory(cache_rows_kernel<NT, E4m3>, kRowsSmem);
-  if (e != cudaSuccess) return e;
-  ++*launches;
-  return launch_pdl(cache_rows_kernel<NT, E4m3>, dim3(kCacheCtas), dim3(kThreads), kRowsSmem, s, mk, mv, p);
-}
-
-}  // namespace
-
-cudaError_t launch_cache_rows(const CacheGeom &g, const CacheIndex &ix, const CacheWorkspace &w, const void *Q, const heart_cache &c,
-                              void *O, float *lse, cudaStream_t s, int *launches) {
-  const int NT = (long long)g.max_new * g.G <= 8 ? 1 : 2, box = g.page < keys_of(g.e4m3) ? g.page : keys_of(g.e4m3);
+template <int NT, bool E4m3, bool Redo>
+cudaError_t launch(const CacheGeom &g, const RowsParams &p, const heart_cache &c, cudaStream_t s, int *launches) {
+  const int box = g.page < keys_of(E4m3) ? g.page : keys_of(E4m3);
   CUtensorMap mk, mv;
   if (!make_pool_map(&mk, c.k, g, box, 2) || !make_pool_map(&mv, c.v, g, box, 2)) return cudaErrorInvalidValue;
+  cudaError_t e = allow_shared_memory(cache_rows_kernel<NT, E4m3, Redo>, kRowsSmem);
+  if (e != cudaSuccess) return e;
+  ++*launches;
+  return launch_pdl(cache_rows_kernel<NT, E4m3, Redo>, dim3(kCacheCtas), dim3(kThreads), kRowsSmem, s, mk, mv, p);
+}
+
+RowsParams rows_params(const CacheGeom &g, const CacheIndex &ix, const CacheWorkspace &w, const void *Q, const heart_cache &c, void *O, float *lse) {
   RowsParams p = {};
   p.ix = ix;
   p.Q = static_cast<const uint16_t *>(Q);
@@ -844,8 +877,27 @@ cudaError_t launch_cache_rows(const CacheGeom &g, const CacheIndex &ix, const Ca
   p.arrivals = w.arrivals;
   p.parts = w.parts;
   p.part_l = w.part_l;
-  if (g.e4m3) return NT == 1 ? launch<1, true>(g, p, mk, mv, s, launches) : launch<2, true>(g, p, mk, mv, s, launches);
-  return NT == 1 ? launch<1, false>(g, p, mk, mv, s, launches) : launch<2, false>(g, p, mk, mv, s, launches);
+  return p;
+}
+
+}  // namespace
+
+cudaError_t launch_cache_rows(const CacheGeom &g, const CacheIndex &ix, const CacheWorkspace &w, const void *Q, const heart_cache &c,
+                              void *O, float *lse, cudaStream_t s, int *launches) {
+  const RowsParams p = rows_params(g, ix, w, Q, c, O, lse);
+  const bool eight = (long long)g.max_new * g.G <= 8;
+  if (g.e4m3) return eight ? launch<1, true, false>(g, p, c, s, launches) : launch<2, true, false>(g, p, c, s, launches);
+  return eight ? launch<1, false, false>(g, p, c, s, launches) : launch<2, false, false>(g, p, c, s, launches);
+}
+
+cudaError_t launch_cache_redo(const CacheGeom &g, const CacheIndex &ix, const CacheWorkspace &w, const void *Q, const heart_cache &c,
+                              void *O, float *lse, int looked, cudaStream_t s, int *launches) {
+  RowsParams p = rows_params(g, ix, w, Q, c, O, lse);
+  p.test_skip = 0;
+  p.redo = w.redo;
+  p.any_redo = w.any_redo;
+  p.looked = looked;
+  return launch<2, true, true>(g, p, c, s, launches);
 }
 
 }  // namespace heart

@@ -24,11 +24,20 @@
 // instruction for two codes, where bf16 takes nine for four (3900 clocks a step).  The keys' scales multiply the scores; the values' do not fit f16
 // whatever they are, so a step's values are code * 2^(e - E), E the largest exponent of the step, and its weights
 // 2^(score + E - m): the reference of a row is over score + E.  The sums, of 2^(score - m + E of the part's first step), take 2^(that - E) a
-// step.  A weight of less than 2^-29 of what was the largest when the reference moved counts as zero.
+// step.
+// That is right where exponents lie near each other.  Of the tokens that some row of a sequence sees those of a step may be kScaleSpan
+// binades apart: a product of a weight and a scale then counts as zero only below 2^-23 of the row's largest (f16 has 2^-25, the largest is at 2^6 and
+// more of the step's E).  From step to step E may move by kScaleRange, which costs nothing (the sums have 32 bits); but a value of zero, which has its
+// step's E, is to raise no row's reference by more than kScaleSpan above what other steps have.  CTAs of the plan launch look at all scales, while one of them plans (the
+// V producer, which has them at hand, sets the pace: looked at there, 12 heads x 4680 over 12 680 took 459 us instead of 371); a sequence and key head that is beyond these is
+// done again by rows (cache_rows.cu), where a weight has its own token's scale: all of 12 heads x 4680 over 12 680 2.9 ms, one of them 0.2 ms.  The look and the second launch
+// cost 2 to 4 us a call.
 //
 // Warp roles: 0-3, 4-7 softmax; 8 issues S = Q K^T; 9 copies V; 10 finds the CTA's parts and the pages of their steps, copies K and Q; 11
 // issues O += P V; 12-15 (e4m3) convert.  Tensor memory: O (128 columns) | S[2] (2 x 128) | P[2] (2 x 64).
 // Every wait is bounded; one that runs out raises the CTA's abort flag and the status word, and its roles stop.
+#include <algorithm>
+
 #include "cache.cuh"
 #include "tc_ptx.cuh"
 
@@ -45,7 +54,9 @@ constexpr int kPartRing = 8;       // parts are announced a part ahead
 constexpr int kMaxParts = 12;      // of a tile, about
 constexpr float kNoReference = -3.0e38f;
 constexpr float kHeadroom = 16.f, kMaxGrowth = 8.f;  // see attn_tc.cu
-constexpr float kHeadroomE4m3 = -4.f, kMaxGrowthE4m3 = 14.f;  // weights of f16: 2^4 where the reference moves, to 2^14
+constexpr float kHeadroomE4m3 = -6.f, kMaxGrowthE4m3 = 15.f;  // weights of f16: 2^6 where the reference moves, to 2^15
+constexpr int kScaleSpan = 8, kScaleRange = 40;  // see above
+constexpr int kNoValue = 17, kNoValueAs = 97;    // scale bytes up to this, of values below 2^-101, count as zeros; the E (as a byte) of a step of such ones
 constexpr uint32_t kShortWait = 500;
 constexpr int kRowsAtOnce = 4;  // of queries that are split
 
@@ -72,10 +83,11 @@ static_assert(kPartWords <= 32, "lanes copy words");
 
 // A key step of a CTA, some steps ahead of its use.
 struct Step {
-  int key, keys, h, flags;  // first key, keys of the sequence from there on, key head
+  int key, seen, h, flags;  // first key; e4m3: see kStepUnseen; key head
   int page[8];
 };
 constexpr int kStepMasked = 1, kStepEnd = 2;  // some row does not see all of its keys; no step left
+constexpr uint32_t kStepUnseen = 1u << 31;    // no row of the tile sees its keys before bits 8-15 (but for the sinks), nor those from bits 0-7 on
 
 template <bool E4m3>
 struct Layout {
@@ -213,11 +225,113 @@ __device__ __forceinline__ uint32_t add_zero_times(const uint4 &x, uint32_t sum)
 }
 
 // ---------------------------------------------------------------------- plan
+// The scales of the values that the rows of a sequence see, for a key head: 1 if they are further apart than the tile kernel holds (see the
+// top of the file).  2^warps_log2 warps a sequence and key head, a lane 16 tokens, eight lanes a key step.
+struct ScaleLook {
+  const uint8_t *v_scale;
+  uint8_t *redo;
+  int *any_redo;
+  int warps_log2;
+};
+__device__ __forceinline__ void look_at_scales(const CacheIndex &ix, const ScaleLook &p, int Hkv) {
+  // Of a group of warps: a step whose scales are too far apart; what E may be, least and most; the least that it is in a step with values; the most in one
+  // with values of zero.
+  __shared__ int far[32], least[32], most[32], valued[32], raised[32];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cta = blockIdx.x - 1, ctas = gridDim.x - 1;
+  const int warps = 1 << p.warps_log2, groups = 32 >> p.warps_log2, group = warp >> p.warps_log2;
+  const long long pairs = (long long)ix.S * Hkv;
+  bool any = false;
+  for (long long first = (long long)cta * groups; first < pairs; first += (long long)ctas * groups) {
+    const long long pair = first + group;
+    if (threadIdx.x < 32) far[threadIdx.x] = 0, least[threadIdx.x] = valued[threadIdx.x] = 255, most[threadIdx.x] = raised[threadIdx.x] = 0;
+    __syncthreads();
+    if (pair < pairs) {
+      const int s = (int)(pair / Hkv), h = (int)(pair - (long long)s * Hkv);
+      const Sequence q = sequence(ix, s);
+      const int len = q.n > 0 ? q.len : 0, low = visible(ix, max(q.len - q.n, 0), q.len).low, sinks = min(ix.sink, low);
+      int lo_top = 255, hi_top = 0, valued_top = 255, zero_top = 0, span = 0;
+      // the sinks' steps, then those of the window
+      const int first_step = max(low / kKeyStep, (sinks + kKeyStep - 1) / kKeyStep), sink_steps = (sinks + kKeyStep - 1) / kKeyStep;
+      const int steps = sink_steps + max((len + kKeyStep - 1) / kKeyStep - first_step, 0);
+#pragma unroll 2
+      for (int i = (warp & (warps - 1)) * 4 + (lane >> 3); i < ((steps + 3) & ~3); i += warps * 4) {
+        const int k0 = (i < sink_steps ? i : first_step + i - sink_steps) * kKeyStep + (lane & 7) * 16;
+        uint4 b = make_uint4(0u, 0u, 0u, 0u);
+        const bool there = i < steps && k0 < len;
+        if (there) {
+          const int page = page_entry(ix, s, k0);  // (out of range: values of zero, and reported by the tile kernel)
+          if ((unsigned)page < (unsigned)ix.n_pages)
+            b = __ldcg(reinterpret_cast<const uint4 *>(p.v_scale + ((((size_t)page * Hkv + h) << ix.page_log2) + (k0 & ((1 << ix.page_log2) - 1)))));
+        }
+        // all 16 bytes, in 16-bit halves; one by one where some token is not seen or a byte has a meaning of its own
+        const uint32_t w[4] = {b.x, b.y, b.z, b.w};
+        uint32_t lows = 0xffffffffu, tops = 0u;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t even = w[j] & 0x00ff00ffu, odd = w[j] >> 8 & 0x00ff00ffu;
+          lows = __vminu2(lows, __vminu2(even, odd));
+          tops = __vmaxu2(tops, __vmaxu2(even, odd));
+        }
+        int lowest = min(lows & 0xffffu, lows >> 16), highest = max(tops & 0xffffu, tops >> 16), seen = 1, zero = 0;
+        if (!there || k0 + 16 > len || (k0 < low && k0 + 16 > sinks) || lowest <= kNoValue || highest == 255) {
+          lowest = 255, highest = seen = 0;
+#pragma unroll 1
+          for (int k = k0; there && k < k0 + 16; ++k) {
+            const int i = k - k0, byte = (int)((i < 8 ? i < 4 ? b.x : b.y : i < 12 ? b.z : b.w) >> (8 * (i & 3)) & 255u);
+            if (k >= len || (k < low && k >= sinks)) continue;
+            seen = 1;
+            if (byte <= kNoValue) zero = 1;
+            else if (byte < 255) lowest = min(lowest, byte), highest = max(highest, byte);
+          }
+        }
+#pragma unroll
+        for (int o = 1; o < 8; o <<= 1) {
+          lowest = min(lowest, __shfl_xor_sync(0xffffffffu, lowest, o));
+          highest = max(highest, __shfl_xor_sync(0xffffffffu, highest, o));
+          seen |= __shfl_xor_sync(0xffffffffu, seen, o);
+          zero |= __shfl_xor_sync(0xffffffffu, zero, o);
+        }
+        span = max(span, highest - lowest);
+        if (seen) {
+          // (a tile may see less of the step, and with values of zero among that nothing else)
+          const int top = highest > 0 ? highest : kNoValueAs;
+          lo_top = min(lo_top, zero ? min(top, kNoValueAs) : top);
+          hi_top = max(hi_top, zero ? max(top, kNoValueAs) : top);
+          if (highest > 0) valued_top = min(valued_top, top);
+          if (zero) zero_top = max(zero_top, max(top, kNoValueAs));
+        }
+      }
+      lo_top = __reduce_min_sync(0xffffffffu, lo_top);
+      valued_top = __reduce_min_sync(0xffffffffu, valued_top);
+      hi_top = __reduce_max_sync(0xffffffffu, hi_top);
+      zero_top = __reduce_max_sync(0xffffffffu, zero_top);
+      span = __reduce_max_sync(0xffffffffu, span);
+      if (lane == 0) {
+        if (span > kScaleSpan) far[group] = 1;
+        atomicMin(&least[group], lo_top);
+        atomicMin(&valued[group], valued_top);
+        atomicMax(&most[group], hi_top);
+        atomicMax(&raised[group], zero_top);
+      }
+    }
+    __syncthreads();
+    if (pair < pairs && (warp & (warps - 1)) == 0 && lane == 0) {
+      const bool redo = far[group] != 0 || most[group] - least[group] > kScaleRange || raised[group] - valued[group] > kScaleSpan;
+      p.redo[pair] = redo;
+      any |= redo;
+    }
+    __syncthreads();
+  }
+  any = __syncthreads_or(any);
+  if (threadIdx.x == 0) p.any_redo[cta] = any;
+}
+
 constexpr int kSmallPlan = 4096;
-// The tiles of a head, sequence by sequence, and the key steps before each.  One CTA.
+// The tiles of a head, sequence by sequence, and the key steps before each.  One CTA; the others look at an e4m3 cache's scales.
+template <bool Look>
 __global__ void __launch_bounds__(1024) cache_plan_kernel(const CacheIndex ix, int tokens_per_tile, Tile *__restrict__ tiles,
                                                           long long *__restrict__ first, int *__restrict__ head, long long *__restrict__ cuts,
-                                                          int32_t *__restrict__ arrivals, int most, int Hkv, bool weigh) {
+                                                          int32_t *__restrict__ arrivals, int most, int Hkv, bool weigh, const ScaleLook look) {
   __shared__ long long sums[32];
   __shared__ int base[1024];
   __shared__ int costs[kSmallPlan];  // of the first tiles: as a rule all
@@ -225,6 +339,9 @@ __global__ void __launch_bounds__(1024) cache_plan_kernel(const CacheIndex ix, i
   auto cost_of = [&](int i) { return i < kSmallPlan ? costs[i] : tiles[i].steps + tiles[i].extra; };
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
   pdl_wait();
+  // (No word to the tile kernel from those that look: its CTAs come when they have ended, and so to all SMs in their order.  Prompts of 6 x 24 heads took 162 us when they
+  // came to the SMs that were free first.)
+  if (Look && blockIdx.x > 0) return look_at_scales(ix, look, Hkv);
   pdl_launch_dependents();
   for (int i = t; i < kCacheCtas; i += 1024) arrivals[i] = 0;
   auto upto_lane = [&](long long x) {  // inclusive, over the warp
@@ -617,9 +734,13 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
         if (lane < 8) y.page[lane] = page;
         if (lane == 0) {
           y.key = k0;
-          y.keys = (int)len - k0;
           y.h = h_now;
           y.flags = k0 + kKeyStep <= every_end && (k0 >= every_low || k0 + kKeyStep <= sink) ? 0 : kStepMasked;
+          if (E4m3) y.seen = 0;
+          if (E4m3 && y.flags != 0) {
+            const int low = x.t.some_low - k0, end = x.t.some_end - k0;
+            if (low > 0 || end < kKeyStep) y.seen = (int)(kStepUnseen | min(max(low, 0), kKeyStep) << 8 | min(max(end, 0), kKeyStep));
+          }
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.step_full[g % kSteps]);
@@ -658,7 +779,7 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
     // ===== V producer; e4m3: the scales of a step's tokens too, told of two steps ahead, asked for three
     int g = 0, asked = 0;
     bool ended = !E4m3;
-    uint32_t kb = 0, vb = 0;  // scale bytes of keys 4 * lane .. 4 * lane + 3, 127 where there are none
+    uint32_t kb = 0, vb = 0;  // scale bytes of keys 4 * lane .. 4 * lane + 3; where there are none, 127 and nothing
     auto ask = [&]() {
       if (ended || !wait(&sh.step_full[asked % kSteps], (asked / kSteps) & 1)) return;
       const Step &y = sh.step[asked % kSteps];
@@ -667,8 +788,8 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
         return;
       }
       const int page = y.page[(lane * 4) >> page_log2];
-      kb = vb = 0x7f7f7f7fu;
-      if (lane * 4 < y.keys && page < ix.n_pages) {
+      kb = 0x7f7f7f7fu, vb = 0u;
+      if (page < ix.n_pages) {
         const size_t from = (((size_t)page * p.Hkv + y.h) << page_log2) + ((y.key + lane * 4) & ((1 << page_log2) - 1));
         kb = __ldcg(reinterpret_cast<const uint32_t *>(p.k_scale + from));
         vb = __ldcg(reinterpret_cast<const uint32_t *>(p.v_scale + from));
@@ -676,20 +797,23 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
     };
     auto tell = [&]() {
       if (ended || !ok) return;
-      const int keys = sh.step[asked % kSteps].keys - lane * 4;
-      // (bytes with a meaning of their own, and a step that ends early, come seldom)
-      const bool special = (__vcmpeq4(kb, 0xffffffffu) | __vcmpeq4(vb, 0xffffffffu) | __vcmpeq4(kb, 0u)) != 0u || keys < 4;
+      const Step &y = sh.step[asked % kSteps];
+      // (bytes with a meaning of their own, and a step with keys that no row sees, come seldom)
+      const bool special = (__vcmpeq4(kb, 0xffffffffu) | __vcmpeq4(vb, 0xffffffffu) | __vcmpeq4(kb, 0u)) != 0u || y.seen < 0;
       uint32_t bad = 0u;
       float f[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) f[j] = __uint_as_float(__byte_perm(kb, 0, 0x0444 | j << 12) >> 1);  // 2^(byte - 127)
       if (__any_sync(0xffffffffu, special)) {
+        const int low = y.seen < 0 ? y.seen >> 8 & 255 : 0, end = y.seen < 0 ? y.seen & 255 : kKeyStep;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const uint32_t k = (kb >> (8 * j)) & 255u, v = (vb >> (8 * j)) & 255u;
+          const int i = lane * 4 + j;
+          const bool seen = i < end && (i >= low || y.key + i < ix.sink);
           f[j] = k == 255u ? 1.f : cache_scale(k);  // (more than 0: hidden scores of -inf stay -inf)
           if (k == 255u || v == 255u) bad |= 1u << j;
-          if (v == 255u || j >= keys) vb &= ~(255u << (8 * j));  // (nothing)
+          if (v == 255u || !seen) vb &= ~(255u << (8 * j));  // (nothing)
         }
         bad <<= 4 * (lane & 7);  // a bit a key: eight lanes a word
 #pragma unroll
@@ -699,7 +823,7 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
       *reinterpret_cast<float4 *>(&sh.k_scale[asked & 7][lane * 4]) = make_float4(f[0], f[1], f[2], f[3]);
       *reinterpret_cast<uint32_t *>(&sh.v_scale[asked & 7][lane * 4]) = vb;
       if ((lane & 7) == 0) sh.bad[asked & 7][lane >> 3] = bad;
-      if (lane == 0) sh.top[asked & 7] = max((int)top, 17);  // (where there is no value, the smallest scale's)
+      if (lane == 0) sh.top[asked & 7] = top > kNoValue ? (int)top : kNoValueAs;
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh.scales_full[asked & 7]);
       ++asked;
@@ -1362,13 +1486,28 @@ cudaError_t launch_cache_tiles(const CacheGeom &g, const CacheIndex &ix, const C
   p.inv_G = (65536u + g.G - 1) / g.G;
   p.test_skip = g.test_skip;
   p.scale_log2 = (float)(g.scale * 1.4426950408889634);
-  cudaError_t e = launch_pdl(cache_plan_kernel, dim3(1), dim3(1024), 0, s, ix, 128 / g.G, reinterpret_cast<Tile *>(w.tiles), w.tile_first, w.tile_head,
-                             w.cuts, p.arrivals, (int)cache_max_tiles(g), g.Hkv, (long long)cache_max_tiles(g) * g.Hkv >= 2 * kCacheCtas);
+  const int most = (int)cache_max_tiles(g);
+  const bool weigh = (long long)most * g.Hkv >= 2 * kCacheCtas;
+  cudaError_t e;
+  int looked = 0;
+  if (g.e4m3) {  // CTAs that look at scales: as many warps a sequence and key head as leave one for each, or all at once
+    ScaleLook look = {c.v_scale, w.redo, w.any_redo, 5};
+    const long long pairs = (long long)g.S * g.Hkv;
+    while (look.warps_log2 > 0 && pairs > (long long)(kCacheCtas - 1) << (5 - look.warps_log2)) --look.warps_log2;
+    const int groups = 32 >> look.warps_log2;
+    looked = (int)std::min((pairs + groups - 1) / groups, (long long)kCacheCtas - 1);
+    e = launch_pdl(cache_plan_kernel<true>, dim3(1 + looked), dim3(1024), 0, s, ix, 128 / g.G, reinterpret_cast<Tile *>(w.tiles), w.tile_first, w.tile_head,
+                   w.cuts, p.arrivals, most, g.Hkv, weigh, look);
+  } else {
+    e = launch_pdl(cache_plan_kernel<false>, dim3(1), dim3(1024), 0, s, ix, 128 / g.G, reinterpret_cast<Tile *>(w.tiles), w.tile_first, w.tile_head, w.cuts,
+                   p.arrivals, most, g.Hkv, weigh, ScaleLook{});
+  }
   if (e != cudaSuccess) return e;
   ++*launches;
   e = g.e4m3 ? launch<true>(mq, mk, mv, p, s) : launch<false>(mq, mk, mv, p, s);
-  if (e == cudaSuccess) ++*launches;
-  return e;
+  if (e != cudaSuccess) return e;
+  ++*launches;
+  return g.e4m3 ? launch_cache_redo(g, ix, w, Q, c, O, lse, looked, s, launches) : cudaSuccess;
 }
 
 }  // namespace heart

@@ -61,15 +61,15 @@ def product_bound(c):
 
 def check(c, O, lse, rows=None):
     """As cache_cases.check_attention, with one term more: a weight of f16 is off by 2^-25 at most where it is below 2^-14, and the row's largest
-    product of a weight and a scale is held as 1 at least (2^6 by rows; by tiles 2^8, of which up to 2^8 is the span of a step's
-    scales): each key's part is off by 2^-25 of that product times its code."""
+    product of a weight and a scale is held as 2^-2 at least (2^6, by tiles less the span of a step's scales, up to 2^8): each
+    key's part is off by 2^-23 of that product times its code."""
     want, want_lse = c.attention()
     n = int(c.row_start[-1])
     O, lse = O.cpu(), lse.cpu()
     assert (O[n:] == 77).all() and (lse[n:] == 55).all()
     at = torch.arange(n) if rows is None else rows
     got, want = O[at].double(), want[at]
-    bound = (2 ** -8 + 2 ** -12) * c.weight_bound()[at] + 2 ** -8 * want.abs() + 2 ** -25 * product_bound(c)[at] + 1e-30
+    bound = (2 ** -8 + 2 ** -12) * c.weight_bound()[at] + 2 ** -8 * want.abs() + 2 ** -23 * product_bound(c)[at] + 1e-30
     worst = (got - want).abs() / bound
     empty = want_lse[at] == -math.inf
     assert (got[empty] == 0).all() and (lse[at][empty] == -math.inf).all()
@@ -85,7 +85,7 @@ def attend(heart, c, **kw):
     return out
 
 
-BOTH = pytest.mark.parametrize("max_new", [1], ids=["rows"])
+BOTH = pytest.mark.parametrize("max_new", [1, 0], ids=["rows", "tiles"])
 
 
 def scatter(lo, hi):
@@ -173,3 +173,79 @@ def test_zero_values_beside_others(heart, gain, zeros, max_new):
 
     c = e4m3_case([390, 300], [3, 140], edit, gain, Hq=4, Hkv=2, page=64)
     check(c, *attend(heart, c, max_new=max_new))
+
+
+@pytest.mark.parametrize("how", ["zeros first", "zeros at times", "rising", "falling", "rising far", "falling far", "far apart", "one without weight"])
+@pytest.mark.parametrize("gain", [-40, 0, 20, 60])
+def test_parts_of_many_steps(heart, gain, how):
+    """As many heads as give a CTA several steps of a tile."""
+    def edit(c, k, v, g):
+        v *= 2.0 ** gain
+        L = c.lens[0]
+        page, slot = slots(c, 0, torch.arange(L))
+        step = torch.arange(L) // 128
+        if how == "zeros first":
+            v[page[:300], :, slot[:300]] = 0.0
+        elif how == "zeros at times":
+            v[page[::50], :, slot[::50]] = 0.0
+            v[page[640:768], :, slot[640:768]] = 0.0
+        elif how == "far apart":
+            scatter(-30, 30)(c, k, v, g)
+        elif how == "one without weight":
+            c.Q = (c.Q.float() * 0.1 + 1.0).to(torch.bfloat16)
+            k[page[200], :, slot[200]] = -9.0
+            v[page[200], :, slot[200]] *= 2.0 ** 30
+        else:
+            by = {"rising": 3, "falling": -3, "rising far": 6, "falling far": -6}[how]
+            v[page, :, slot] *= torch.exp2((by * step).float().clamp(max=85 - gain))[:, None, None]
+
+    c = e4m3_case([1500], [290], edit, gain, Hq=48, Hkv=24, page=64, causal=1)
+    check(c, *attend(heart, c))
+
+
+@pytest.mark.parametrize("S", [3, 40])
+def test_other_heads_keep_their_bits(heart, S):
+    """Scales far apart in one sequence and key head: what the others get does not change by a bit, now or in the next call."""
+    lens = [200 + 31 * (i % 5) for i in range(S)]
+    new = [60 + 13 * (i % 4) for i in range(S)]
+    for G in (1, 3, 8):
+        c = e4m3_case(lens, new, lambda *a: None, G, Hq=3 * G, Hkv=3, causal=1, page=32, pad=40)
+        d = Device(heart, c, max_new=0)
+        want = d.attention()
+        far = e4m3_case(lens, new, lambda *a: None, G, Hq=3 * G, Hkv=3, causal=1, page=32, pad=40)
+        page, slot = slots(far, 2, torch.arange(0, lens[2], 3))
+        far.v_scale[page, 1, slot] += 40
+        e = Device(heart, far, max_new=0)
+        e.ws = d.ws
+        O, lse = e.attention()
+        r0, n = int(c.row_start[2]), new[2]
+        rows = torch.zeros((c.T, 3 * G), dtype=torch.bool)
+        rows[r0:r0 + n, G:2 * G] = True
+        assert torch.equal(bits(O.cpu()[~rows]), bits(want[0].cpu()[~rows])) and torch.equal(lse.cpu()[~rows], want[1].cpu()[~rows])
+        check(far, O, lse)
+        again = e.attention()
+        assert torch.equal(bits(O), bits(again[0])) and torch.equal(bits(lse), bits(again[1]))
+        after = d.attention()
+        assert torch.equal(bits(after[0]), bits(want[0])) and torch.equal(bits(after[1]), bits(want[1]))
+        assert heart.heart_get_status(d.ws) == 0
+
+
+def test_captured_calls_with_scales_far_apart(heart):
+    """One captured call, replayed over a cache whose scales are alike, far apart, and alike again."""
+    near = e4m3_case([300, 140], [150, 140], lambda *a: None, 1, Hq=4, Hkv=2, causal=1)
+    far = e4m3_case([300, 140], [150, 140], scatter(-30, 30), 1, Hq=4, Hkv=2, causal=1)
+    d = Device(heart, near)
+    want = d.attention()
+    O, lse = torch.full_like(d.Q, 77.0), torch.full((near.T, 4), 55.0, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        heart.heart_cache_attn(d.cfg, d.Q, d.cache, *d.where, O, d.ws, lse=lse)
+    for c in (near, far, near, far):
+        d.cache.v.view(torch.uint8).copy_(c.v.view(torch.uint8))
+        d.cache.v_scale.copy_(c.v_scale)
+        graph.replay()
+        if c is near:
+            assert torch.equal(bits(O), bits(want[0])) and torch.equal(bits(lse), bits(want[1]))
+        else:
+            check(c, O, lse)
+    assert heart.heart_get_status(d.ws) == 0
