@@ -112,6 +112,8 @@ __device__ __forceinline__ void bulk_load(void *dst, const void *src, int bytes,
                : "memory");
 }
 __device__ __forceinline__ bool not_finite(uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
+// Of four codes, the top bits of those that are no numbers, 0x7f or 0xff (and other bits).
+__device__ __forceinline__ uint32_t ends_of(uint32_t codes) { return (codes & 0x7f7f7f7fu) + 0x01010101u; }
 
 // The 8 x 8 matrix of 16-bit numbers that the warp holds, a row to four lanes, transposed.
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {
@@ -600,20 +602,31 @@ __global__ void __launch_bounds__(kThreads, 1)
           pf[m][t][0] = transposed(E4m3 ? pack_f16x2(w[0], w[1]) : pack_bf16x2(w[0], w[1]));
           pf[m][t][1] = transposed(E4m3 ? pack_f16x2(w[2], w[3]) : pack_bf16x2(w[2], w[3]));
         }
-      if (!E4m3 && !whole) {
-        // Values that are not finite must not reach rows that do not see them (0 * inf is NaN): they are taken out, and rows that
-        // do see them are marked.
+      if (!whole) {
+        // Values that are not finite (codes that are no numbers) must not reach rows that do not see them (0 * inf is NaN): they are taken out, and
+        // rows that do see them are marked.
         uint32_t bad = 0u;
+        if (E4m3) {  // a lane a key, 16 bytes at a time in an order without bank conflicts
+          uint32_t ends = 0u;  // a byte's top bit: 0x7f, 0xff
 #pragma unroll 1
-        for (int j = 0; j < 8; ++j) {
-          const uint4 v = lds_u4(v_at + (j * 32 + lane) * 16);
-          if (not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w)) bad |= 1u << ((j * 4 + (lane >> 3)) & 15);
+          for (int j = 0; j < 8; ++j) {
+            const uint4 v = lds_u4(v_at + lane * 128 + ((j ^ (lane & 7)) << 4));
+            ends |= ends_of(v.x) | ends_of(v.y) | ends_of(v.z) | ends_of(v.w);
+          }
+          bad = __ballot_sync(0xffffffffu, (ends & 0x80808080u) != 0u);
+        } else {
+#pragma unroll 1
+          for (int j = 0; j < 8; ++j) {
+            const uint4 v = lds_u4(v_at + (j * 32 + lane) * 16);
+            if (not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w)) bad |= 1u << ((j * 4 + (lane >> 3)) & 15);
+          }
+          bad = __reduce_or_sync(0xffffffffu, bad);
         }
-        bad = __reduce_or_sync(0xffffffffu, bad);
         if (bad) {
 #pragma unroll 1
           for (int j = 0; j < 8; ++j)
-            if (bad >> ((j * 4 + (lane >> 3)) & 15) & 1u) *reinterpret_cast<uint4 *>(ring + take * kStage + kHalf + (j * 32 + lane) * 16) = make_uint4(0u, 0u, 0u, 0u);
+            if (bad >> (E4m3 ? lane : (j * 4 + (lane >> 3)) & 15) & 1u)
+              *reinterpret_cast<uint4 *>(ring + take * kStage + kHalf + (E4m3 ? lane * 128 + j * 16 : (j * 32 + lane) * 16)) = make_uint4(0u, 0u, 0u, 0u);
           async_proxy_fence();
           __syncwarp();
 #pragma unroll 1
@@ -626,13 +639,6 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (!hidden(vis[m][r], key)) sum[m][r] = __uint_as_float(0x7fc00000u);
           }
         }
-      }
-      if (E4m3 && k0 + kKeys > q.len) {  // codes behind a sequence's end may be no numbers (0 * NaN is NaN)
-        if (lane < kKeys && k0 + lane >= q.len)
-#pragma unroll
-          for (int j = 0; j < 8; ++j) *reinterpret_cast<uint4 *>(ring + take * kStage + kHalf + lane * 128 + j * 16) = make_uint4(0u, 0u, 0u, 0u);
-        async_proxy_fence();
-        __syncwarp();
       }
       // ---- values: of every 16 dims the dims g and g + 8 (e4m3: 2g and 2g + 1), rows 2c and 2c + 1
 #pragma unroll

@@ -150,6 +150,8 @@ struct TileParams {
   uint32_t inv_G;          // row / G = row * inv_G >> 16 for the rows of a tile
   float scale_log2;
   int test_skip;           // test-hook builds only: CTA 0 leaves out its second copy of values
+  uint8_t *redo;           // see CacheWorkspace
+  int *any_redo;
   __device__ __forceinline__ int token_of(int row) const { return (int)(((uint32_t)row * inv_G) >> 16); }
 };
 
@@ -1342,6 +1344,17 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
           tmem_ld32(o_addr + half * 64 + 32, *reinterpret_cast<uint32_t(*)[32]>(&v[32]));
           tmem_wait_ld();
           if (half == 1) arrive(&sh.o_free);
+          // A code that is no number, in a token that some rows see and others do not, has reached them all (0 * NaN is NaN): rows do it
+          // again.  (Looked at by the converters, in the steps that some row does not see whole, 12 x 4680 over 12 680 took 415 us instead of 390.)
+          if (E4m3) {
+            uint64_t zero = 0ull;
+#pragma unroll
+            for (int i = 0; i < 64; i += 2) zero = fma_f32x2(pack_f32x2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), 0ull, zero);
+            if (zero != 0ull && l == l && !none && row < n_rows) {
+              p.redo[(size_t)to.t.s * p.Hkv + to.h] = 1;
+              p.any_redo[0] = 1;
+            }
+          }
           if (whole) {
             stage(v, half, inv * o_factor);
           } else if (row < n_rows) {
@@ -1486,6 +1499,8 @@ cudaError_t launch_cache_tiles(const CacheGeom &g, const CacheIndex &ix, const C
   p.inv_G = (65536u + g.G - 1) / g.G;
   p.test_skip = g.test_skip;
   p.scale_log2 = (float)(g.scale * 1.4426950408889634);
+  p.redo = w.redo;
+  p.any_redo = w.any_redo;
   const int most = (int)cache_max_tiles(g);
   const bool weigh = (long long)most * g.Hkv >= 2 * kCacheCtas;
   cudaError_t e;

@@ -127,7 +127,7 @@ def test_large_values_of_tokens_that_come_later(heart, gain, max_new):
 @BOTH
 @pytest.mark.parametrize("seed", range(3))
 def test_tokens_before_a_window_hold_anything(heart, seed, max_new):
-    """Any scale byte in tokens of the sequence that no new one sees: the same bits as without them."""
+    """Any code, any scale byte, in tokens of the sequence that no new one sees: the same bits as without them."""
     for page in (16, 64, 128):
         c = Case([700, 90, 400], [5, 20, 1], Hq=4, Hkv=2, page=page, kind="e4m3", causal=1, window=60 + 17 * seed, sink=3, garbage=False, seed=seed, pad=40)
         want = attend(heart, c, max_new=max_new)
@@ -136,6 +136,9 @@ def test_tokens_before_a_window_hold_anything(heart, seed, max_new):
             first = c.lens[s] - c.new[s] + 1 - c.window
             page_, slot = slots(c, s, torch.arange(3, max(3, first)))
             n = page_.numel()
+            for x in (c.k, c.v):
+                b = torch.randint(0, 256, (n, c.Hkv, D), generator=g, dtype=torch.uint8)
+                x.view(torch.uint8)[page_, :, slot] = b | (torch.rand(b.shape, generator=g) < 0.2).to(torch.uint8) * 0x7f
             for x in (c.k_scale, c.v_scale):
                 x[page_, :, slot] = torch.randint(0, 256, (n, c.Hkv), generator=g, dtype=torch.uint8)
         got = attend(heart, c, max_new=max_new)
@@ -201,6 +204,23 @@ def test_parts_of_many_steps(heart, gain, how):
 
     c = e4m3_case([1500], [290], edit, gain, Hq=48, Hkv=24, page=64, causal=1)
     check(c, *attend(heart, c))
+
+
+@BOTH
+@pytest.mark.parametrize("pool", ["k", "v"])
+def test_codes_that_are_no_numbers(heart, pool, max_new):
+    """A code of 0x7f in a token: rows before it are what they are without it, rows that see it are no numbers."""
+    for new in (6, 140):
+        c, without = (Case([new + 50], [new], Hq=2, kind="e4m3", causal=1, page=16, garbage=False, pad=40) for _ in range(2))
+        clean = attend(heart, without, max_new=max_new)
+        page, slot = slots(c, 0, 50 + new // 2)
+        getattr(c, pool).view(torch.uint8)[page, :, slot, 77] = 0x7f
+        O, lse = attend(heart, c, max_new=max_new)
+        n = new // 2
+        # (by tiles another kernel may have brought them: both are within the bound)
+        check(without, *(torch.cat([x[:n], y[n:]]) for x, y in zip((O, lse), clean)), rows=torch.arange(n))
+        assert torch.isfinite(O[:n]).all() and torch.isfinite(lse[:n]).all()
+        assert not torch.isfinite(O[n:new].float()).all(-1).any()
 
 
 @pytest.mark.parametrize("S", [3, 40])
