@@ -243,7 +243,7 @@ int heart_drift_static(const heart_config *cfg, const void *Q, const void *K, co
  * captured graph may be replayed with other contents).  What they hold is checked there: row_start is to ascend within
  * [0, T], kv_len to lie in [0, table_stride * page], page_table entries of tokens that exist to lie in [0, n_pages) (the
  * others are not looked at).  A violation is reported as HEART_ERR_DEVICE_CHECK through heart_get_status; lengths and starts are then taken as
- * the nearest valid ones, tokens of a page out of range are not written, are read as zeros and count as zeros, or as NaN, in the
+ * the nearest valid ones, tokens of a page out of range are not written, are read as zeros and count as keys and values of zero in the
  * attention, and nothing outside the tensors is touched.  No output overlaps an input. */
 #define HEART_CACHE_BF16 0
 #define HEART_CACHE_E4M3 1

@@ -122,6 +122,9 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
   return r;
 }
 
+// Scale bytes of tokens that there are not: the smallest, so that their values of zero raise no row's reference.
+__device__ alignas(16) const uint8_t kNoScales[32] = {};
+
 // Keys that a warp takes at a time, 4 KB of them.
 __host__ __device__ constexpr int keys_of(bool e4m3) { return e4m3 ? 32 : 16; }
 
@@ -360,9 +363,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       tma_load_5d(to, &map_k, bar, 0, slot, 0, h, page);
       tma_load_5d(to + kHalf, &map_v, bar, 0, slot, 0, h, page);
       if (E4m3) {
-        const size_t at = (((size_t)min(page, ix.n_pages - 1) * p.Hkv + h) << ix.page_log2) + slot;
-        bulk_load(&sh.scales[warp][put][lane << box_log2], p.k_scale + at, 1 << box_log2, bar);
-        bulk_load(&sh.scales[warp][put][kKeys + (lane << box_log2)], p.v_scale + at, 1 << box_log2, bar);
+        const size_t at = (((size_t)page * p.Hkv + h) << ix.page_log2) + slot;
+        bulk_load(&sh.scales[warp][put][lane << box_log2], page < ix.n_pages ? p.k_scale + at : kNoScales, 1 << box_log2, bar);
+        bulk_load(&sh.scales[warp][put][kKeys + (lane << box_log2)], page < ix.n_pages ? p.v_scale + at : kNoScales, 1 << box_log2, bar);
       }
     }
 #ifdef HEART_TEST_HOOKS

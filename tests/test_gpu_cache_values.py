@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-from cache_cases import Case, Device, quantise
+from cache_cases import Case, Device, check_attention, quantise
 
 pytestmark = pytest.mark.gpu
 
@@ -269,3 +269,34 @@ def test_captured_calls_with_scales_far_apart(heart):
         else:
             check(c, O, lse)
     assert heart.heart_get_status(d.ws) == 0
+
+
+@BOTH
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("page", [16, 64])
+def test_tokens_of_pages_that_there_are_not_count_as_zeros(heart, page, kind, max_new):
+    """An entry out of range: its tokens are keys and values of zero, whatever the scales of the pool's last page are."""
+    for gone in (2, -1):
+        c = Case([200, 150], [5, 40], Hq=4, Hkv=2, page=page, kind=kind, causal=1, garbage=False, pad=40, spare=3)
+        used = set(c.table.flatten().tolist())
+        zeros, = [p for p in range(c.n_pages - 1) if p not in used][:1]
+        c.table[0, 1] = zeros
+        for x in (c.k, c.v):
+            x.view(torch.uint8 if kind == "e4m3" else torch.bfloat16)[zeros] = 0
+        if kind == "e4m3":
+            c.k_scale[zeros], c.v_scale[zeros] = 127, 127
+        d = Device(heart, c, max_new=max_new)
+        d.where[0][0, 1] = c.n_pages if gone == 2 else gone
+        if kind == "e4m3":
+            d.cache.v_scale[-1], d.cache.k_scale[-1] = 250, 255
+            c.v_scale[-1], c.k_scale[-1] = 250, 255
+        if c.n_pages - 1 in used:  # the last page is to be nobody's: its tokens go to a free one
+            free = [p for p in range(c.n_pages - 1) if p not in used and p != zeros][0]
+            c.table[c.table == c.n_pages - 1] = free
+            d.where[0][d.where[0] == c.n_pages - 1] = free
+        O, lse = d.attention()
+        assert heart.heart_get_status(d.ws) == heart.ERR_DEVICE_CHECK
+        if kind == "e4m3":
+            check(c, O, lse)
+        else:
+            check_attention(c, O, lse)
