@@ -1015,7 +1015,9 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
         for (int j = 0; j < kRowsAtOnce; ++j) {
           float inv;
           const float scale = code_scale(top[j], inv);
-          if (lane == 0) sh.q_scale[n & 1][i + j] = p.scale_log2 * scale;
+          // (at least a normal number: the -inf of what is hidden is to stay that, for queries of zero and a small scale too)
+          const float q_scale = p.scale_log2 * scale;
+          if (lane == 0) sh.q_scale[n & 1][i + j] = q_scale < 0x1p-126f ? 0x1p-126f : q_scale;
           uint32_t hi[2], lo[2];
           split_codes(q[j].x, inv, hi[0], lo[0]);
           split_codes(q[j].y, inv, hi[1], lo[1]);

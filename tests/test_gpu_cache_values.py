@@ -300,3 +300,18 @@ def test_tokens_of_pages_that_there_are_not_count_as_zeros(heart, page, kind, ma
             check(c, O, lse)
         else:
             check_attention(c, O, lse)
+
+
+@BOTH
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("scale", [1e-30, 1e-20, 1e-10])
+def test_queries_of_zeros_and_a_small_scale(heart, scale, kind, max_new):
+    """The mean of the values that a row sees: a query's own scale times the call's is below the 32-bit numbers."""
+    c = Case([200, 30], [40, 30], Hq=4, Hkv=2, page=16, kind=kind, causal=1, scale=scale, garbage=False, pad=40)
+    c.Q[::2] = 0.0
+    c.Q[1::4] = (c.Q[1::4].float() * 2.0 ** -100).to(torch.bfloat16)
+    O, lse = attend(heart, c, max_new=max_new)
+    if kind == "e4m3":
+        check(c, O, lse)
+    else:
+        check_attention(c, O, lse)
