@@ -51,6 +51,13 @@ __device__ __forceinline__ Sequence sequence_of(const CacheIndex &ix, int row, i
   return sequence(ix, s);
 }
 
+// More than 32 sequences: all of them looked at, each by one thread of the launch (a row's way to its slot passes a few).
+__device__ __forceinline__ void check_sequences(const CacheIndex &ix) {
+  if (ix.S <= 32) return;
+  const long long threads = (long long)gridDim.x * gridDim.y * blockDim.x;
+  for (long long s = ((long long)blockIdx.y * gridDim.x + blockIdx.x) * blockDim.x + threadIdx.x; s < ix.S; s += threads) sequence(ix, (int)s);
+}
+
 // The token's slot as an offset in elements (heads apart) and its number among the scales; false: there is none.
 __device__ __forceinline__ bool slot_of(const CopyParams &p, int row, int lane, bool &belongs, long long &at, long long &scale_at) {
   int s;
@@ -96,6 +103,7 @@ __global__ void __launch_bounds__(32 * kWarps) cache_write_kernel(const CopyPara
   const int h1 = min(p.Hkv, (int)(blockIdx.y + 1) * p.heads), count = h1 - (int)blockIdx.y * p.heads;
   pdl_wait();
   pdl_launch_dependents();
+  check_sequences(p.ix);
   if (row >= p.ix.T) return;
   const uint16_t *src = (values ? p.V : p.K) + row * p.kvt + h * p.kvh + i * 8;
   uint4 x[kUnroll][2];
@@ -169,6 +177,7 @@ __global__ void __launch_bounds__(32 * kWarps) cache_read_kernel(const CopyParam
   const int h1 = min(p.Hkv, (int)(blockIdx.y + 1) * p.heads), count = h1 - (int)blockIdx.y * p.heads;
   pdl_wait();
   pdl_launch_dependents();
+  check_sequences(p.ix);
   if (row >= p.ix.T) return;
   bool belongs;
   long long at = 0, scale_at = 0;
