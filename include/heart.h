@@ -303,7 +303,9 @@ int heart_cache_read(const heart_cache_config *cfg, const heart_cache *cache, co
  *   o = sum_j softmax_j(scale * <q, k_j>) v_j;  bf16 in, fp32 accumulate, bf16 out (RNE); lse [T, Hq] fp32 natural-log
  *   sum-exp of the scaled logits, or NULL.
  * A query without keys gets zeros and lse = -inf.  What a row does not see has no part in it, whatever it holds (pages hold
- * anything behind a sequence's end); a row that sees a key or value that is not finite has elements that are not finite.
+ * anything behind a sequence's end).  A row that sees a value that is not finite, a key with a NaN, or one with an infinity whose logit is +inf or NaN,
+ * has elements that are not finite; a logit of -inf (a bf16 key with an infinity of the sign that makes it that) has no weight, as if the row did not see the
+ * key.  A token of an e4m3 cache whose key or value was not finite (scale byte 255) or holds a code that is no number does that to every row that sees it.
  * Unnormalised sums stay below 2^15 * (visible keys) * max |v|: finite for |v| up to 2^90 whatever the lengths and logits.  Weights below
  * 2^-29 of a row's largest may count as zero. */
 int heart_cache_attn(const heart_cache_config *cfg, const void *Q, const heart_cache *cache, const int32_t *page_table,

@@ -315,3 +315,37 @@ def test_queries_of_zeros_and_a_small_scale(heart, scale, kind, max_new):
         check(c, O, lse)
     else:
         check_attention(c, O, lse)
+
+
+@BOTH
+@pytest.mark.parametrize("which", ["one", "all"])
+def test_keys_of_infinity(heart, which, max_new):
+    """A bf16 key with an infinity: rows whose logit it makes -inf are as if they did not see it (zeros where they see nothing else), rows whose logit it makes
+    +inf are no numbers."""
+    new = 20
+    c = Case([60], [new], Hq=4, Hkv=2, page=16, pad=40, garbage=False, window=0 if which == "one" else 1)
+    bad = 30 if which == "one" else 59  # (a window of one, no order: all rows see the last token alone)
+    page, slot = slots(c, 0, bad)
+    c.k[page, 0, slot, 5] = math.inf
+    sign = torch.where(torch.arange(new) % 2 == 0, 1.0, -1.0)
+    c.Q[:new, :, 5] = (c.Q[:new, :, 5].float().abs() + 0.5).mul(sign[:, None]).to(torch.bfloat16)
+    O, lse = (x.cpu() for x in attend(heart, c, max_new=max_new))
+    plus = torch.zeros((c.T, 4), dtype=torch.bool)
+    plus[:new:2, :2] = True  # (the heads of the first key head)
+    assert not torch.isfinite(O[plus].float()).any() and not torch.isfinite(lse[plus]).any()
+    minus, other = torch.zeros_like(plus), torch.zeros_like(plus)
+    minus[1:new:2, :2] = True
+    other[:new, 2:] = True
+
+    def agree(rows):  # (the bound of cache_cases.check_attention)
+        want, want_lse = c.attention()
+        assert ((O.double() - want).abs() <= (2 ** -8 + 2 ** -12) * c.weight_bound() + 2 ** -8 * want.abs())[rows].all()
+        assert ((lse.double() - want_lse).abs() <= 2 ** -14)[rows].all()
+
+    agree(other)
+    if which == "all":
+        assert (O[minus] == 0).all() and (lse[minus] == -math.inf).all()
+    else:
+        c.k[page, 0, slot] = 0.0
+        c.seen = lambda s: (torch.arange(60) != bad).expand(new, 60)
+        agree(minus)
