@@ -29,6 +29,7 @@ struct CacheIndex {
 struct CacheWorkspace {
   int32_t *status;    // [64] word 0: sticky device-check code
   int32_t *arrivals;  // [2][kCacheCtas] parts of a shared tile that are there: the rows kernel's (zero between launches), the tile kernel's
+  int *found;         // [kCacheCtas][8] what CTAs that look at the scales of one sequence and key head have found (zero between launches)
   float *parts;       // [2 * kCacheCtas][128][128] parts of tiles: unnormalised sums of values
   float2 *part_l;     // [2 * kCacheCtas][128] their row sums and references
   void *tiles;        // [max_tiles] tiles of a head (see cache_tiles.cu)
@@ -55,6 +56,7 @@ __host__ inline CacheWorkspace carve_cache(const CacheGeom &g, void *base) {
   };
   w.status = reinterpret_cast<int32_t *>(take(64 * sizeof(int32_t)));
   w.arrivals = reinterpret_cast<int32_t *>(take(2 * kCacheCtas * sizeof(int32_t)));
+  w.found = reinterpret_cast<int *>(take(8 * kCacheCtas * sizeof(int)));
   w.parts = reinterpret_cast<float *>(take(sizeof(float) * 2 * kCacheCtas * 128 * kD));
   w.part_l = reinterpret_cast<float2 *>(take(sizeof(float2) * 2 * kCacheCtas * 128));
   w.tiles = take(kTileRecord * cache_max_tiles(g));

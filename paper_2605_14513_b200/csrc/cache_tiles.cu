@@ -228,12 +228,13 @@ __device__ __forceinline__ uint32_t add_zero_times(const uint4 &x, uint32_t sum)
 
 // ---------------------------------------------------------------------- plan
 // The scales of the values that the rows of a sequence see, for a key head: 1 if they are further apart than the tile kernel holds (see the
-// top of the file).  2^warps_log2 warps a sequence and key head, a lane 16 tokens, eight lanes a key step.
+// top of the file).  2^warps_log2 warps a sequence and key head, or `ctas` CTAs each, a lane 16 tokens, eight lanes a key step.
 struct ScaleLook {
   const uint8_t *v_scale;
   uint8_t *redo;
   int *any_redo;
-  int warps_log2;
+  int warps_log2, ctas;
+  int *found;  // [kCacheCtas][8], where a sequence and key head has CTAs: what they have found, how many have; zero between launches
 };
 __device__ __forceinline__ void look_at_scales(const CacheIndex &ix, const ScaleLook &p, int Hkv) {
   // Of a group of warps: a step whose scales are too far apart; what E may be, least and most; the least that it is in a step with values; the most in one
@@ -242,8 +243,9 @@ __device__ __forceinline__ void look_at_scales(const CacheIndex &ix, const Scale
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cta = blockIdx.x - 1, ctas = gridDim.x - 1;
   const int warps = 1 << p.warps_log2, groups = 32 >> p.warps_log2, group = warp >> p.warps_log2;
   const long long pairs = (long long)ix.S * Hkv;
+  const int part = cta % p.ctas;  // (several CTAs: one round)
   bool any = false;
-  for (long long first = (long long)cta * groups; first < pairs; first += (long long)ctas * groups) {
+  for (long long first = (long long)(cta / p.ctas) * groups; first < pairs; first += (long long)ctas * groups) {
     const long long pair = first + group;
     if (threadIdx.x < 32) far[threadIdx.x] = 0, least[threadIdx.x] = valued[threadIdx.x] = 255, most[threadIdx.x] = raised[threadIdx.x] = 0;
     __syncthreads();
@@ -256,7 +258,7 @@ __device__ __forceinline__ void look_at_scales(const CacheIndex &ix, const Scale
       const int first_step = max(low / kKeyStep, (sinks + kKeyStep - 1) / kKeyStep), sink_steps = (sinks + kKeyStep - 1) / kKeyStep;
       const int steps = sink_steps + max((len + kKeyStep - 1) / kKeyStep - first_step, 0);
 #pragma unroll 2
-      for (int i = (warp & (warps - 1)) * 4 + (lane >> 3); i < ((steps + 3) & ~3); i += warps * 4) {
+      for (int i = (part * warps + (warp & (warps - 1))) * 4 + (lane >> 3); i < ((steps + 3) & ~3); i += p.ctas * warps * 4) {
         const int k0 = (i < sink_steps ? i : first_step + i - sink_steps) * kKeyStep + (lane & 7) * 16;
         uint4 b = make_uint4(0u, 0u, 0u, 0u);
         const bool there = i < steps && k0 < len;
@@ -318,9 +320,24 @@ __device__ __forceinline__ void look_at_scales(const CacheIndex &ix, const Scale
     }
     __syncthreads();
     if (pair < pairs && (warp & (warps - 1)) == 0 && lane == 0) {
-      const bool redo = far[group] != 0 || most[group] - least[group] > kScaleRange || raised[group] - valued[group] > kScaleSpan;
-      p.redo[pair] = redo;
-      any |= redo;
+      int found[5] = {far[group], 255 - least[group], most[group], 255 - valued[group], raised[group]};
+      bool all = true;
+      if (p.ctas > 1) {
+        int *const at = p.found + 8 * (int)pair;
+        for (int k = 0; k < 5; ++k) atomicMax(&at[k], found[k]);
+        __threadfence();
+        all = atomicAdd(&at[5], 1) == p.ctas - 1;
+        if (all) {
+          __threadfence();
+          for (int k = 0; k < 5; ++k) found[k] = atomicExch(&at[k], 0);
+          at[5] = 0;
+        }
+      }
+      if (all) {
+        const bool redo = found[0] != 0 || found[2] + found[1] - 255 > kScaleRange || found[4] + found[3] - 255 > kScaleSpan;
+        p.redo[pair] = redo;
+        any |= redo;
+      }
     }
     __syncthreads();
   }
@@ -1507,12 +1524,15 @@ cudaError_t launch_cache_tiles(const CacheGeom &g, const CacheIndex &ix, const C
   const bool weigh = (long long)most * g.Hkv >= 2 * kCacheCtas;
   cudaError_t e;
   int looked = 0;
-  if (g.e4m3) {  // CTAs that look at scales: as many warps a sequence and key head as leave one for each, or all at once
-    ScaleLook look = {c.v_scale, w.redo, w.any_redo, 5};
+  if (g.e4m3) {  // CTAs that look at scales: as many warps a sequence and key head as leave one for each, or a CTA for every 16384 tokens that it may have (one: a
+                 // prompt of 512, 12 heads, 28 us; twelve: 31; 100 tokens of one head over 200k: 185 with one, 177 with thirteen)
+    ScaleLook look = {c.v_scale, w.redo, w.any_redo, 5, 1, w.found};
     const long long pairs = (long long)g.S * g.Hkv;
     while (look.warps_log2 > 0 && pairs > (long long)(kCacheCtas - 1) << (5 - look.warps_log2)) --look.warps_log2;
     const int groups = 32 >> look.warps_log2;
-    looked = (int)std::min((pairs + groups - 1) / groups, (long long)kCacheCtas - 1);
+    const long long rounds = ((long long)g.table_stride * g.page + 16383) / 16384;
+    look.ctas = (int)std::max(std::min((kCacheCtas - 1) / pairs, rounds), 1LL);
+    looked = (int)std::min((pairs + groups - 1) / groups * look.ctas, (long long)kCacheCtas - 1);
     e = launch_pdl(cache_plan_kernel<true>, dim3(1 + looked), dim3(1024), 0, s, ix, 128 / g.G, reinterpret_cast<Tile *>(w.tiles), w.tile_first, w.tile_head,
                    w.cuts, p.arrivals, most, g.Hkv, weigh, look);
   } else {

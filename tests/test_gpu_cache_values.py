@@ -349,3 +349,31 @@ def test_keys_of_infinity(heart, which, max_new):
         c.k[page, 0, slot] = 0.0
         c.seen = lambda s: (torch.arange(60) != bad).expand(new, 60)
         agree(minus)
+
+
+@pytest.mark.parametrize("heads", [1, 2, 8])
+def test_one_token_of_a_long_context(heart, heads):
+    """A large value of no weight, wherever it is: several CTAs look at the scales of a key head."""
+    for at in (5, 127, 15000, 29999):
+        def edit(c, k, v, g):
+            c.Q = (c.Q.float() * 0.1 + 1.0).to(torch.bfloat16)
+            page, slot = slots(c, 0, at)
+            k[page, heads - 1, slot] = -9.0
+            v[page, heads - 1, slot] *= 2.0 ** 30
+
+        c = e4m3_case([30000], [20], edit, at, Hq=heads, Hkv=heads, page=128)
+        check(c, *attend(heart, c, max_new=0))
+
+
+@pytest.mark.parametrize("S,heads", [(200, 1), (640, 8)])
+def test_one_token_of_many_sequences(heart, S, heads):
+    """More sequences and key heads than CTAs, and than warps that look at once."""
+    lens = [10 + s % 9 for s in range(S)]
+
+    def edit(c, k, v, g):
+        for s in (0, S // 2 + 1, S - 1):
+            page, slot = slots(c, s, lens[s] - 1)
+            v[page, heads - 1, slot] *= 2.0 ** 30
+
+    c = e4m3_case(lens, [1 + s % 3 for s in range(S)], edit, S, Hq=heads, Hkv=heads, causal=1, page=16)
+    check(c, *attend(heart, c, max_new=0))
