@@ -143,12 +143,6 @@ struct AttnParams {
   int test_skip;
 };
 
-__device__ __forceinline__ float fmax3(float a, float b, float c) {
-  float r;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-  return r;
-}
-
 struct Sums {
   float a, b, c, d;
 };
@@ -166,14 +160,6 @@ __device__ __forceinline__ void exp32(const uint32_t *s, uint64_t c2, uint64_t n
     add_bf16x2_to_f32(sums.a, sums.b, pk[i >> 1]);
     add_bf16x2_to_f32(sums.c, sums.d, pk[(i >> 1) + 1]);
   }
-}
-__device__ __forceinline__ float max64(const uint32_t *s) {
-  float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-  for (int i = 0; i < 64; i += 8)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) m[j] = fmax3(m[j], __uint_as_float(s[i + 2 * j]), __uint_as_float(s[i + 2 * j + 1]));
-  return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
 }
 
 struct PlanParams {

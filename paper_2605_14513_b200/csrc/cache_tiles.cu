@@ -155,11 +155,6 @@ struct TileParams {
   __device__ __forceinline__ int token_of(int row) const { return (int)(((uint32_t)row * inv_G) >> 16); }
 };
 
-__device__ __forceinline__ float fmax3(float a, float b, float c) {
-  float r;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-  return r;
-}
 __device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
   uint64_t d;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
@@ -181,14 +176,6 @@ __device__ __forceinline__ void exp32(const uint32_t *s, uint64_t c2, uint64_t n
     pk[(i >> 1) + 1] = F16 ? pack_f16x2(x2, x3) : pack_bf16x2(x2, x3);
   }
 }
-__device__ __forceinline__ float max64(const uint32_t *s) {
-  float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-  for (int i = 0; i < 64; i += 8)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) m[j] = fmax3(m[j], __uint_as_float(s[i + 2 * j]), __uint_as_float(s[i + 2 * j + 1]));
-  return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
-}
 // D[tmem] (+)= A[smem] * B[smem], e4m3
 __device__ __forceinline__ void mma_ss_e4m3(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -204,11 +191,6 @@ __host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N, bool a_mn_maj
 }
 __host__ __device__ constexpr uint32_t idesc_e4m3_f32(int M, int N) {
   return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);  // D f32, A and B e4m3 (0), K-major
-}
-__device__ __forceinline__ uint4 lds_u4(uint32_t addr) {
-  uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
-  return v;
 }
 __device__ __forceinline__ uint2 lds_u2(uint32_t addr) {
   uint2 v;
@@ -617,7 +599,6 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
     settle(bar, 0);
   };
   const int page_log2 = ix.page_log2, n_boxes = 128 >> page_log2;
-  auto key_of = [](const Tile &t, int i) { return (i < t.sinks ? i : t.first + i - t.sinks) * kKeyStep; };
   auto load_pages = [&](unsigned char *dst, const CUtensorMap *map, uint64_t *bar, int h, int page) {
     if (lane == 0) mbar_expect_tx(bar, L::kKey);
     __syncwarp();
