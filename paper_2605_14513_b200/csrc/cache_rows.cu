@@ -178,13 +178,21 @@ __global__ void __launch_bounds__(kThreads, 1)
     const long long pairs = (long long)ix.S * p.Hkv;
     t += (int)gridDim.x;
     while (pair < pairs) {
-      const uint32_t word = __ldcg(reinterpret_cast<const uint32_t *>(p.redo) + (pair >> 2)) >> (8 * (pair & 3));
-      if (word == 0u) {
-        pair = (pair | 3) + 1;
+      // the next one that is marked among 128, a lane four of them
+      const long long base = pair & ~127LL, mine = base + lane * 4;
+      uint32_t marks = 0u;
+      if (mine + 3 >= pair && mine < pairs) {
+        marks = __ldcg(reinterpret_cast<const uint32_t *>(p.redo + mine));
+        if (mine < pair) marks &= 0xffffffffu << (8 * (int)(pair - mine));
+        if (mine + 4 > pairs) marks &= 0xffffffffu >> (8 * (int)(mine + 4 - pairs));  // (bytes of no pair)
+      }
+      const uint32_t some = __ballot_sync(0xffffffffu, marks != 0u);
+      if (some == 0u) {
+        pair = base + 128;
         continue;
       }
-      pair += (__ffs(word) - 1) >> 3;
-      if (pair >= pairs) break;  // (the last word has bytes of no pair)
+      const int first = __ffs(some) - 1;
+      pair = base + first * 4 + ((__ffs(__shfl_sync(0xffffffffu, marks, first)) - 1) >> 3);
       s = (int)(pair / p.Hkv);
       h = (int)(pair - (long long)s * p.Hkv);
       q = sequence(ix, s);
