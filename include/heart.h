@@ -241,7 +241,7 @@ int heart_drift_static(const heart_config *cfg, const void *Q, const void *K, co
  *
  * row_start [S+1], kv_len [S] and page_table [S, table_stride] are DEVICE arrays of int32, read when the kernels run (a
  * captured graph may be replayed with other contents).  What they hold is checked there: row_start is to ascend within
- * [0, T], kv_len to lie in [0, table_stride * page], page_table entries of tokens that exist to lie in [0, n_pages) (the
+ * [0, T], kv_len to lie in [0, table_stride * page], page_table entries of tokens that a call stores, reads or attends to to lie in [0, n_pages) (the
  * others are not looked at).  A violation is reported as HEART_ERR_DEVICE_CHECK through heart_get_status; lengths and starts are then taken as
  * the nearest valid ones, tokens of a page out of range are not written, are read as zeros and count as keys and values of zero in the
  * attention, and nothing outside the tensors is touched.  No output overlaps an input. */
@@ -256,8 +256,9 @@ typedef struct {
   int32_t n_pages;             /* pages of the pools                                                         */
   int32_t table_stride;        /* row pitch of page_table in entries; table_stride * page < 2^31 - 256       */
   int32_t kind;                /* HEART_CACHE_BF16 or HEART_CACHE_E4M3                                       */
-  int32_t max_new;             /* most new tokens of a sequence, 0 = unknown: selects kernels by it; any
-                                  lengths give the right results                                             */
+  int32_t max_new;             /* most new tokens of a sequence: selects kernels by it; any lengths give the
+                                  right results.  0 = unknown: taken as many, so that single tokens are
+                                  right but slow (tiles of 128 rows); a program that decodes says 1          */
   int32_t causal;              /* 0: all tokens of the sequence are visible; g > 0: those up to the end of the
                                   query's group of g tokens (1: token by token, the tokens of a frame: frame
                                   by frame)                                                                  */
@@ -306,8 +307,13 @@ int heart_cache_read(const heart_cache_config *cfg, const heart_cache *cache, co
  * anything behind a sequence's end).  A row that sees a value that is not finite, a key with a NaN, or one with an infinity whose logit is +inf or NaN,
  * has elements that are not finite; a logit of -inf (a bf16 key with an infinity of the sign that makes it that) has no weight, as if the row did not see the
  * key.  A token of an e4m3 cache whose key or value was not finite (scale byte 255) or holds a code that is no number does that to every row that sees it.
- * Unnormalised sums stay below 2^15 * (visible keys) * max |v|: finite for |v| up to 2^90 whatever the lengths and logits.  Weights below
- * 2^-29 of a row's largest may count as zero. */
+ * Roundings besides that of the result: sums and the softmax's statistics have 32 bits.  bf16: a weight is rounded to bf16 for the product with the
+ * values (the row sum takes it unrounded).  e4m3: a weight, times its value's scale, is rounded to f16, a code is exact; where that product is
+ * below 2^-23 of the row's largest, or the weight below 2^-23 of the row's largest, it may count as zero.  Values with a scale byte up to 17 (below 2^-101) may too.
+ * With many rows an e4m3 query is the sum of two codes a dim, off by up to 2^-18 of the row's largest element.
+ * Unnormalised sums stay below 2^15 * (visible keys) * max |v|: finite for |v| and |k| up to 2^90 whatever the lengths, and the logits while they are.
+ * An e4m3 cache's speed depends on its scales where rows are many: a sequence and key head whose values differ in scale by more than 2^8 within 128 tokens (zeros
+ * apart) or 2^40 overall, or hold codes that are no numbers, is computed a second time, which takes some six times as long. */
 int heart_cache_attn(const heart_cache_config *cfg, const void *Q, const heart_cache *cache, const int32_t *page_table,
                      const int32_t *row_start, const int32_t *kv_len, void *O, float *lse, void *workspace,
                      heart_stream_t stream);

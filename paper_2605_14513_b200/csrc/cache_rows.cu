@@ -5,7 +5,7 @@
 // about bytes in flight: one CTA an SM, eight warps, each with a ring of its own of 24 KB that tensor copies fill.  A warp takes 16 of
 // every 128 keys (32 of 256 where they are e4m3), with the running maximum and sum of its own keys, so nothing but the warp's own barrier is
 // waited for until a tile's end.  Keys and values are the first operands of the products, rows the second: a product has 16 of the former and 8 of
-// the latter, and most calls have no more rows.  (Rows first, 16 of them: 20 x 8001 tokens e4m3, 32 heads on 8, 91 us, now 75; 12 warps with
+// the latter, and most calls have no more rows.  (Rows first, 16 of them: 20 x 8001 tokens e4m3, 32 heads on 8, 91 us against 75; 12 warps with
 // smaller rings 74, and one token over 4k 11.5 us instead of 10.8.)
 //
 // With eight warps an SM what comes next are instructions: 900 for 16 keys, converting keys and values from e4m3 to bf16, took 4700 clocks.

@@ -29,13 +29,16 @@
 // binades apart: a product of a weight and a scale then counts as zero only below 2^-23 of the row's largest (f16 has 2^-25, the largest is at 2^6 and
 // more of the step's E).  From step to step E may move by kScaleRange, which costs nothing (the sums have 32 bits); but a value of zero, which has its
 // step's E, is to raise no row's reference by more than kScaleSpan above what other steps have.  CTAs of the plan launch look at all scales, while one of them plans (the
-// V producer, which has them at hand, sets the pace: looked at there, 12 heads x 4680 over 12 680 took 459 us instead of 371); a sequence and key head that is beyond these is
+// V producer, which has them at hand, sets the pace: looked at there, 12 heads x 4680 over 12 680 took 459 us instead of 378); a sequence and key head that is beyond these is
 // done again by rows (cache_rows.cu), where a weight has its own token's scale: all of 12 heads x 4680 over 12 680 2.9 ms, one of them 0.2 ms.  The look and the second launch
 // cost 2 to 4 us a call.
 //
 // Warp roles: 0-3, 4-7 softmax; 8 issues S = Q K^T; 9 copies V; 10 finds the CTA's parts and the pages of their steps, copies K and Q; 11
 // issues O += P V; 12-15 (e4m3) convert.  Tensor memory: O (128 columns) | S[2] (2 x 128) | P[2] (2 x 64).
 // Every wait is bounded; one that runs out raises the CTA's abort flag and the status word, and its roles stop.
+//
+// Times of long launches in this file were taken with pauses between the calls; back to back for a second, at the power limit, 40 heads x 4680 over 33k takes
+// 3.3 ms where it has 2.8 to 2.9 then, and 12 x 4680 over 32760, causal by frames, 0.83 where it has 0.72.
 #include <algorithm>
 
 #include "cache.cuh"

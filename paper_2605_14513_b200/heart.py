@@ -250,7 +250,8 @@ def heart_drift_static(cfg, Q, K, delta, st: State, drift_out=None, refresh_out=
 
 def make_cache_config(S, T, Hq, Hkv, page, n_pages, table_stride, kind=CACHE_BF16, D=128, max_new=0, causal=0, window=0, sink=0, scale=0.0,
                       q_strides=(0, 0), kv_strides=(0, 0), pool_strides=(0, 0, 0)) -> CacheConfig:
-    """S sequences, T rows of the packed tensors.  Strides in elements: (token, head) of Q and O, (token, head) of the
+    """S sequences, T rows of the packed tensors.  max_new, the most new tokens of a sequence, selects the kernel: 0 (not known) is right for any
+    lengths, but slow where there are few (say 1 for a step of single tokens).  Strides in elements: (token, head) of Q and O, (token, head) of the
     packed K and V, (page, head, token) of the pools; zeros select the contiguous layouts."""
     return CacheConfig(S, T, Hq, Hkv, D, page, n_pages, table_stride, kind, max_new, causal, window, sink, 0, *q_strides, *kv_strides,
                        *pool_strides, scale)
