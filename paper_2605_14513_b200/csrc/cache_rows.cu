@@ -15,7 +15,7 @@
 //   * values are the codes; a token's scale 2^e goes into its weight, behind the mask, so that what a row does not see has no part in it: the product takes
 //     2^(score + e - m), between 0 and 2^14, the row's largest so far at 2^6 to 2^14.  One below 2^-31 of it counts as zero.
 //   * the row sum, of 2^(score - m'), has a reference of its own, a lane's: scales may be any number of binades apart.  (Eight exponentials more for 32
-//     keys, and no multiplication of values: 64 single tokens over up to 16k, 32 heads on 8, 246 us, and 251 with the scales multiplied into values.)
+//     keys, and no multiplication of values: 64 single tokens over up to 16k, 32 heads on 8, 251 us, and as long with the scales multiplied into values.)
 // (The warp-wide products of e4m3 codes themselves are carried out as conversions and f16 products here, 96 for the 64 in the source.)
 //
 // Work: rows of a sequence and key head, packed as (token, query head of the group), in tiles of 8 or 16; all key steps of all tiles in one line,
@@ -515,7 +515,46 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       // ---- weights
       auto hidden = [&](const Visible &v, int k) { return k >= v.end || (k < v.low && k >= ix.sink); };
+      // Values that are not finite (codes that are no numbers) must not reach rows that do not see them (0 * inf is NaN): they are taken out, and
+      // rows that do see them are marked.  (e4m3: ahead of the weights.  Behind them 64 single tokens over up to 16k took 255 us instead of 251.)
+      auto look_at_values = [&]() {
+        uint32_t bad = 0u;
+        if (E4m3) {  // a lane a key, 16 bytes at a time in an order without bank conflicts
+          uint32_t ends = 0u;  // a byte's top bit: 0x7f, 0xff
+#pragma unroll 1
+          for (int j = 0; j < 8; ++j) {
+            const uint4 v = lds_u4(v_at + lane * 128 + ((j ^ (lane & 7)) << 4));
+            ends |= ends_of(v.x) | ends_of(v.y) | ends_of(v.z) | ends_of(v.w);
+          }
+          bad = __ballot_sync(0xffffffffu, (ends & 0x80808080u) != 0u);
+        } else {
+#pragma unroll 1
+          for (int j = 0; j < 8; ++j) {
+            const uint4 v = lds_u4(v_at + (j * 32 + lane) * 16);
+            if (not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w)) bad |= 1u << ((j * 4 + (lane >> 3)) & 15);
+          }
+          bad = __reduce_or_sync(0xffffffffu, bad);
+        }
+        if (bad) {
+#pragma unroll 1
+          for (int j = 0; j < 8; ++j)
+            if (bad >> (E4m3 ? lane : (j * 4 + (lane >> 3)) & 15) & 1u)
+              *reinterpret_cast<uint4 *>(ring + take * kStage + kHalf + (E4m3 ? lane * 128 + j * 16 : (j * 32 + lane) * 16)) = make_uint4(0u, 0u, 0u, 0u);
+          async_proxy_fence();
+          __syncwarp();
+#pragma unroll 1
+          for (uint32_t todo = bad; todo; todo &= todo - 1) {
+            const int key = k0 + __ffs(todo) - 1;
+#pragma unroll
+            for (int m = 0; m < NT; ++m)
+#pragma unroll
+              for (int r = 0; r < 2; ++r)
+                if (!hidden(vis[m][r], key)) sum[m][r] = __uint_as_float(0x7fc00000u);
+          }
+        }
+      };
       if (!whole) {
+        if (E4m3) look_at_values();
 #pragma unroll
         for (int m = 0; m < NT; ++m)
 #pragma unroll
@@ -608,44 +647,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           pf[m][t][0] = transposed(E4m3 ? pack_f16x2(w[0], w[1]) : pack_bf16x2(w[0], w[1]));
           pf[m][t][1] = transposed(E4m3 ? pack_f16x2(w[2], w[3]) : pack_bf16x2(w[2], w[3]));
         }
-      if (!whole) {
-        // Values that are not finite (codes that are no numbers) must not reach rows that do not see them (0 * inf is NaN): they are taken out, and
-        // rows that do see them are marked.
-        uint32_t bad = 0u;
-        if (E4m3) {  // a lane a key, 16 bytes at a time in an order without bank conflicts
-          uint32_t ends = 0u;  // a byte's top bit: 0x7f, 0xff
-#pragma unroll 1
-          for (int j = 0; j < 8; ++j) {
-            const uint4 v = lds_u4(v_at + lane * 128 + ((j ^ (lane & 7)) << 4));
-            ends |= ends_of(v.x) | ends_of(v.y) | ends_of(v.z) | ends_of(v.w);
-          }
-          bad = __ballot_sync(0xffffffffu, (ends & 0x80808080u) != 0u);
-        } else {
-#pragma unroll 1
-          for (int j = 0; j < 8; ++j) {
-            const uint4 v = lds_u4(v_at + (j * 32 + lane) * 16);
-            if (not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w)) bad |= 1u << ((j * 4 + (lane >> 3)) & 15);
-          }
-          bad = __reduce_or_sync(0xffffffffu, bad);
-        }
-        if (bad) {
-#pragma unroll 1
-          for (int j = 0; j < 8; ++j)
-            if (bad >> (E4m3 ? lane : (j * 4 + (lane >> 3)) & 15) & 1u)
-              *reinterpret_cast<uint4 *>(ring + take * kStage + kHalf + (E4m3 ? lane * 128 + j * 16 : (j * 32 + lane) * 16)) = make_uint4(0u, 0u, 0u, 0u);
-          async_proxy_fence();
-          __syncwarp();
-#pragma unroll 1
-          for (uint32_t todo = bad; todo; todo &= todo - 1) {
-            const int key = k0 + __ffs(todo) - 1;
-#pragma unroll
-            for (int m = 0; m < NT; ++m)
-#pragma unroll
-              for (int r = 0; r < 2; ++r)
-                if (!hidden(vis[m][r], key)) sum[m][r] = __uint_as_float(0x7fc00000u);
-          }
-        }
-      }
+      if (!E4m3 && !whole) look_at_values();
       // ---- values: of every 16 dims the dims g and g + 8 (e4m3: 2g and 2g + 1), rows 2c and 2c + 1
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) {
