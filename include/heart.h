@@ -280,7 +280,7 @@ typedef struct {
   uint8_t *k_scale, *v_scale;
 } heart_cache;
 
-/* Bytes of scratch that the three calls below need (256-byte aligned, zero-filled before first use; heart_get_status reads its
+/* Bytes of scratch that the calls below need (256-byte aligned, zero-filled before first use; heart_get_status reads its
  * status).  Host-only; 0 for an invalid or unsupported config.  A workspace serves one call at a time: calls that share one are
  * ordered, by a stream or by events, replays of captured graphs too. */
 size_t heart_cache_workspace_bytes(const heart_cache_config *cfg /* host */);
@@ -317,6 +317,68 @@ int heart_cache_read(const heart_cache_config *cfg, const heart_cache *cache, co
 int heart_cache_attn(const heart_cache_config *cfg, const void *Q, const heart_cache *cache, const int32_t *page_table,
                      const int32_t *row_start, const int32_t *kv_len, void *O, float *lse, void *workspace,
                      heart_stream_t stream);
+
+/* Pages for new tokens, and the arrays that the calls above read, made on the GPU from the sequences' lengths (of cfg: S, T, page, n_pages,
+ * table_stride).  free_pages [n_pages] holds the numbers of the free pages, free_count [1] how many: a stack, taken from its end.  Sequence s has kv_len[s] tokens
+ * and gets new_len[s] more:
+ *   its ceil((kv_len + new_len) / page) - ceil(kv_len / page) new pages go into page_table, behind those that it has; the sequences take theirs
+ *   one behind the other, sequence s its i-th one from free_pages[free_count - 1 - (pages of the sequences before it) - i];
+ *   row_start [S+1] = the exclusive sums of new_len and their total; kv_len_out = kv_len + new_len; free_count_out = what is left;
+ *   slots [T] (or NULL): page * (tokens a page) + slot of every row's token, -1 for rows behind the last sequence.
+ * free_pages itself and all other entries of page_table stay as they are (the pages taken are those behind the new count).  new_len 0 is allowed.
+ * All arrays are DEVICE arrays, int32 but for slots (int64); kv_len_out may be kv_len and free_count_out may be free_count (a captured call then
+ * goes on from where the last replay ended), nothing else overlaps.
+ * A call that cannot be done is not begun: where a length is negative or more than table_stride * page tokens, the rows are more than T, the pages more than there
+ * are, or free_count is not in [0, n_pages], no table entry changes, row_start becomes zeros and slots -1 (so that calls
+ * that follow do nothing), lengths and count are passed on as they were, and heart_get_status reports HEART_ERR_DEVICE_CHECK. */
+int heart_cache_extend(const heart_cache_config *cfg, const int32_t *new_len, const int32_t *kv_len, const int32_t *free_pages,
+                       const int32_t *free_count, int32_t *page_table, int32_t *row_start, int32_t *kv_len_out, int32_t *free_count_out,
+                       int64_t *slots, void *workspace, heart_stream_t stream);
+
+/* The pages of the sequences with ended[s] != 0 (uint8 [S]) back on the stack: the first ceil(kv_len / page) entries of their rows of
+ * page_table, in order, one sequence behind the other, to free_pages[free_count ..]; kv_len_out is 0 for them and kv_len for
+ * the others, free_count_out the new count.  page_table is not written.  Pages that sequences share are not counted: end them by one sequence only.  Not begun,
+ * as above, where the length of one that has ended is out of range or the list would get more than n_pages entries. */
+int heart_cache_release(const heart_cache_config *cfg, const uint8_t *ended, const int32_t *kv_len, int32_t *free_pages,
+                        const int32_t *free_count, const int32_t *page_table, int32_t *kv_len_out, int32_t *free_count_out,
+                        void *workspace, heart_stream_t stream);
+
+/* ---- Cross attention: to states of another length ----
+ *
+ * A video model's blocks attend to a prompt beside their own tokens, a decoder to its encoder's states: S sequences, each with rows of queries and
+ * rows of keys and values of its own.  (Not part of the paper's path, which replaces self attention; the layers around it are these.)
+ *   Queries are packed, T rows: those of sequence s are q_start[s] .. q_start[s+1] - 1.  Rows outside q_start[0] .. q_start[S] - 1 belong to no sequence and are
+ *   left as they are.  Its keys and values are the rows k_start[s] .. k_start[s] + k_len[s] - 1 of K and V, of Tk rows: packed, padded,
+ *   the same ones for several sequences, in any order.
+ *   o = sum_j softmax_j(scale * <q, k_j>) v_j;  bf16 in, fp32 accumulate, bf16 out (RNE); lse [T, Hq] fp32 natural-log sum-exp of the scaled logits,
+ *   or NULL.  Queries of a sequence with k_len = 0 get zeros and lse = -inf.
+ * q_start [S+1], k_start [S] and k_len [S] are DEVICE arrays of int32, read when the kernels run (a captured graph may be replayed with other contents).  What
+ * they hold is checked there: q_start is to ascend within [0, T], a sequence's rows of K to lie in [0, Tk).  A violation is reported as
+ * HEART_ERR_DEVICE_CHECK through heart_get_status; starts and lengths are then taken as the nearest valid ones, and nothing outside the tensors is touched.
+ * No output overlaps an input.
+ * Rows of K and V that are not the sequence's have no part in a row, whatever they hold.  A row that sees a value that is not finite, a key with a NaN, or one with an
+ * infinity whose logit is +inf or NaN, has elements that are not finite; a logit of -inf has no weight.
+ * Roundings besides that of the result: a weight is rounded to bf16 for the product with the values (the row sum takes it unrounded); sums and the
+ * softmax's statistics have 32 bits. */
+typedef struct {
+  int32_t S, T, Tk;            /* sequences, rows of Q and O, rows of K and V (>= 1 each)                      */
+  int32_t Hq, Hkv, D;          /* as in heart_cache_config                                                    */
+  int32_t max_q;               /* most queries of a sequence: selects kernels by it; any lengths give the
+                                  right results.  0 = unknown: taken as many, so that single tokens are right
+                                  but slow (tiles of 128 rows); a program that decodes says 1                 */
+  uint32_t flags;              /* 0                                                                           */
+  int64_t q_stride_t, q_stride_h;   /* elements, of Q and O; both 0 = contiguous [T,Hq,D]                     */
+  int64_t kv_stride_t, kv_stride_h; /* of K and V; both 0 = contiguous [Tk,Hkv,D]                             */
+  double scale;                /* logit scale; <= 0 selects 1/sqrt(D)                                         */
+} heart_cross_config;
+
+/* Bytes of scratch that the call below needs (256-byte aligned, zero-filled before first use; heart_get_status reads its status).  Host-only; 0 for an
+ * invalid or unsupported config.  A workspace serves one call at a time, as those of the cache do. */
+size_t heart_cross_workspace_bytes(const heart_cross_config *cfg /* host */);
+
+/* Base pointers 16-byte aligned, strides multiples of 8 elements, head_dim contiguous. */
+int heart_cross_attn(const heart_cross_config *cfg, const void *Q, const void *K, const void *V, const int32_t *q_start,
+                     const int32_t *k_start, const int32_t *k_len, void *O, float *lse, void *workspace, heart_stream_t stream);
 
 /* ---- Analysis quantities (not on the layer-step path; nothing else reads their results) ---- */
 

@@ -27,7 +27,7 @@ struct CacheIndex {
 };
 
 struct CacheWorkspace {
-  int32_t *status;    // [64] word 0: sticky device-check code
+  int32_t *status;    // [64] word 0: sticky device-check code; kTableTicketWord: CTAs of a table launch that have ended (zero between launches)
   int32_t *arrivals;  // [2][kCacheCtas] parts of a shared tile that are there: the rows kernel's (zero between launches), the tile kernel's
   int *found;         // [kCacheCtas][8] what CTAs that look at the scales of one sequence and key head have found (zero between launches)
   float *parts;       // [2 * kCacheCtas][128][128] parts of tiles: unnormalised sums of values
@@ -41,6 +41,7 @@ struct CacheWorkspace {
   size_t bytes;
 };
 
+constexpr int kTableTicketWord = 8;
 constexpr size_t kTileRecord = 52;
 // Tiles of a head: a sequence ends at most one of them early.
 __host__ inline size_t cache_max_tiles(const CacheGeom &g) { return (size_t)g.S + (size_t)g.T / (128 / g.G); }
@@ -85,6 +86,13 @@ cudaError_t launch_cache_redo(const CacheGeom &g, const CacheIndex &ix, const Ca
                               void *O, float *lse, int looked, cudaStream_t s, int *launches);
 cudaError_t launch_cache_tiles(const CacheGeom &g, const CacheIndex &ix, const CacheWorkspace &w, const void *Q, const heart_cache &c,
                                void *O, float *lse, cudaStream_t s, int *launches);
+
+cudaError_t launch_cache_extend(const CacheGeom &g, const CacheWorkspace &w, const int32_t *new_len, const int32_t *kv_len, const int32_t *free_pages,
+                                const int32_t *free_count, int32_t *page_table, int32_t *row_start, int32_t *kv_len_out, int32_t *free_count_out,
+                                int64_t *slots, cudaStream_t s, int *launches);
+cudaError_t launch_cache_release(const CacheGeom &g, const CacheWorkspace &w, const uint8_t *ended, const int32_t *kv_len, int32_t *free_pages,
+                                 const int32_t *free_count, const int32_t *page_table, int32_t *kv_len_out, int32_t *free_count_out, cudaStream_t s,
+                                 int *launches);
 
 // A pool as a tensor map: boxes of `rows` slots of one head (of bf16, `halves` halves of their 128 dims).
 bool make_pool_map(CUtensorMap *m, const void *base, const CacheGeom &g, int rows, int halves);
@@ -137,6 +145,7 @@ __device__ __forceinline__ void split_codes(uint32_t w, float inv, uint32_t &hig
 // A sequence as its arrays describe it, brought into range (and reported) where they do not hold what they should.
 struct Sequence {
   int row, n, len;  // first row, new tokens, tokens
+  int key;          // cross attention: first row of keys and values
 };
 __device__ __forceinline__ Sequence sequence(const CacheIndex &ix, int s) {
   int r0 = __ldcg(&ix.row_start[s]), r1 = __ldcg(&ix.row_start[s + 1]), len = __ldcg(&ix.kv_len[s]);
@@ -147,7 +156,7 @@ __device__ __forceinline__ Sequence sequence(const CacheIndex &ix, int s) {
     r1 = min(max(r1, r0), ix.T);
     len = min(max(len, 0), most);
   }
-  return {r0, r1 - r0, len};
+  return {r0, r1 - r0, len, 0};
 }
 // The table's entry for token j < len of sequence s, and the page that it stands for: n_pages (reported) where it is none.  (Apart, so that
 // an entry can be asked for ahead of its use.)

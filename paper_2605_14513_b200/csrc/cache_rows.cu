@@ -1,4 +1,4 @@
-// Attention over a paged cache for few query rows a sequence and key head: single tokens and drafted tokens.
+// Attention over a paged cache, or cross attention, for few query rows a sequence and key head: single tokens and drafted tokens.
 //
 // Every key and value is read once and used by 8 or 16 rows, so HBM bounds it: a step of 128 keys is 64 KB, 2800 clocks of an SM's share of
 // the bandwidth (1400 as e4m3), and its products take 256 clocks of the warp-wide matrix instruction for every 8 rows.  So the design is
@@ -24,11 +24,14 @@
 // one came last.  Every CTA finds its share by itself from the sequences' lengths, so the launch needs no plan and no lengths on the host, and a
 // captured one follows the lengths.
 //
+// Cross attention: keys and values are rows of packed tensors from some row on, a box of 16 of them wherever they begin, and every row sees all of its
+// sequence's; all else is the same.
+//
 // Behind the tile kernel of an e4m3 cache the same code does those sequences and key heads again whose scales that kernel cannot hold, whole tiles
 // of 16 rows dealt in turn; as a rule there are none, and the launch ends at once.
 #include <cuda.h>
 
-#include "cache.cuh"
+#include "cross.cuh"
 #include "tc_ptx.cuh"
 
 namespace heart {
@@ -77,7 +80,7 @@ struct alignas(16) RowsShared {
   long long total[kWarps];
   int longest[kWarps];
   int found;              // sequence of the CTA's first step
-  int found_q[3];
+  int found_q[4];
   long long found_at, found_steps;  // steps before it, and of one of its heads
   int last;
   int abort;
@@ -123,7 +126,7 @@ __device__ alignas(16) const uint8_t kNoScales[32] = {};
 // Keys that a warp takes at a time, 4 KB of them.
 __host__ __device__ constexpr int keys_of(bool e4m3) { return e4m3 ? 32 : 16; }
 
-template <int NT, bool E4m3, bool Redo>
+template <int NT, bool E4m3, bool Redo, bool Cross>
 __global__ void __launch_bounds__(kThreads, 1)
     cache_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const RowsParams p) {
   constexpr int kRows = 8 * NT;
@@ -149,10 +152,13 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (Redo && !__syncthreads_or(tid < p.looked && __ldcg(&p.any_redo[tid]) != 0)) return;
 
   // ------------------------------------------------------------------ the CTA's share
+  auto sequence_at_place = [&](int i) { return Cross ? cross_sequence(ix, i) : sequence(ix, i); };
+  // of a token of the sequence's rows; cross attention: they have none among the keys, and see all of them
+  auto position = [&](const Sequence &q, int token) { return Cross ? 0 : q.len - q.n + token; };
   auto tiles_of = [&](const Sequence &q) { return (int)(((long long)q.n * p.G + kRows - 1) / kRows); };
   auto span = [&](const Sequence &q, int t) {
     const int first = t * kRows, last = min((int)((long long)q.n * p.G), first + kRows) - 1;
-    return span_of<kStep>(ix, q.len - q.n + first / p.G, q.len - q.n + last / p.G, q.len);
+    return span_of<kStep>(ix, position(q, first / p.G), position(q, last / p.G), q.len);
   };
   auto steps_of = [&](const Sequence &q, int &longest) -> long long {  // of one head
     long long n = 0;
@@ -167,7 +173,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   auto quotient = [](long long a, long long b) -> long long {  // (of numbers that fit 32 bits as a rule: a tenth of the time)
     return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
   };
-  Sequence q = {0, 0, 0};
+  Sequence q = {0, 0, 0, 0};
   int s, longest = 1;
   long long share, u, u1, sequence_at, per_head;  // units of a CTA, its first one and the one behind its last; of the sequence, and of one of its heads
   bool one_tile = false;                          // shares do not cross tiles
@@ -195,7 +201,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       pair = base + first * 4 + ((__ffs(__shfl_sync(0xffffffffu, marks, first)) - 1) >> 3);
       s = (int)(pair / p.Hkv);
       h = (int)(pair - (long long)s * p.Hkv);
-      q = sequence(ix, s);
+      q = sequence_at_place(s);
       const int tiles = tiles_of(q);
       if (t < tiles) return true;
       t -= tiles;
@@ -211,7 +217,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     u1 = 1LL << 62;
   } else if (ix.S <= 32) {
     // every warp by itself, a lane a sequence
-    if (lane < ix.S) q = sequence(ix, lane);
+    if (lane < ix.S) q = sequence_at_place(lane);
     per_head = steps_of(q, longest);
     longest = __reduce_max_sync(0xffffffffu, longest);
     auto before_lane = [&](long long x, long long &all) {
@@ -246,13 +252,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (u >= u1) return;
     const uint32_t here = __ballot_sync(0xffffffffu, sequence_at <= u && u < sequence_at + per_head * p.Hkv);
     s = __ffs(here) - 1;
-    q = {__shfl_sync(0xffffffffu, q.row, s), __shfl_sync(0xffffffffu, q.n, s), __shfl_sync(0xffffffffu, q.len, s)};
+    q = {__shfl_sync(0xffffffffu, q.row, s), __shfl_sync(0xffffffffu, q.n, s), __shfl_sync(0xffffffffu, q.len, s),
+         Cross ? __shfl_sync(0xffffffffu, q.key, s) : 0};
     sequence_at = __shfl_sync(0xffffffffu, sequence_at, s);
     per_head = __shfl_sync(0xffffffffu, per_head, s);
   } else {
     long long total = 0, mine = 0;
     for (int i = tid; i < ix.S; i += kThreads) {
-      const Sequence x = sequence(ix, i);
+      const Sequence x = sequence_at_place(i);
       const long long n = steps_of(x, longest);
       if (i < kThreads) mine = n, q = x;
       total += n * p.Hkv;
@@ -281,7 +288,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int base = 0; base < ix.S; base += kThreads) {
       int dummy = 0;
       if (base > 0) {
-        q = base + tid < ix.S ? sequence(ix, base + tid) : Sequence{0, 0, 0};
+        q = base + tid < ix.S ? sequence_at_place(base + tid) : Sequence{0, 0, 0, 0};
         mine = steps_of(q, dummy);
       }
       long long upto = mine * p.Hkv;
@@ -302,7 +309,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       at += upto - mine * p.Hkv;
       if (at <= u && u < at + mine * p.Hkv) {
         sh.found = base + tid;
-        sh.found_q[0] = q.row, sh.found_q[1] = q.n, sh.found_q[2] = q.len;
+        sh.found_q[0] = q.row, sh.found_q[1] = q.n, sh.found_q[2] = q.len, sh.found_q[3] = q.key;
         sh.found_at = at;
         sh.found_steps = mine;
       }
@@ -311,7 +318,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     __syncthreads();
     s = sh.found;
-    q = {sh.found_q[0], sh.found_q[1], sh.found_q[2]};
+    q = {sh.found_q[0], sh.found_q[1], sh.found_q[2], sh.found_q[3]};
     sequence_at = sh.found_at;
     per_head = sh.found_steps;
   }
@@ -329,7 +336,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   int in_flight = 0;
   bool ok = true;
   const int g = lane >> 2, c = lane & 3;
-  const int box_log2 = min(ix.page_log2, kKeysLog2), boxes_log2 = kKeysLog2 - box_log2, boxes = 1 << boxes_log2;
+  const int box_log2 = Cross ? kKeysLog2 : min(ix.page_log2, kKeysLog2), boxes_log2 = kKeysLog2 - box_log2, boxes = 1 << boxes_log2;
   const int batch = 32 >> boxes_log2;  // steps whose entries of the table a warp asks for at once, a lane an entry
 
   // ---------------------------------------------------------------- a tile, or part of one
@@ -342,12 +349,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   auto key_of = [&](int i) { return (i < sinks ? i : first + i - sinks) * kStep + warp * kKeys; };
   auto entries = [&](int at) {  // of the steps from `at` on
     const int i = at + (lane >> boxes_log2), k = key_of(i) + ((lane & (boxes - 1)) << box_log2);
-    return i < end_step && k < q.len ? page_entry(ix, s, k) : -1;
+    return !Cross && i < end_step && k < q.len ? page_entry(ix, s, k) : -1;
   };
   auto issue = [&]() {
     while (next < end_step && !some(key_of(next))) ++next;
     if (next >= end_step) return;
-    while (next >= next_batch + batch) {
+    while (!Cross && next >= next_batch + batch) {
       next_batch += batch;
       entry = entry_then;
       entry_then = entries(next_batch + batch);
@@ -359,7 +366,13 @@ __global__ void __launch_bounds__(kThreads, 1)
 #endif
     if (lane == 0) mbar_expect_tx(bar, kStage + (E4m3 ? 2 * kKeys : 0));
     if (boxes > 1) __syncwarp();
-    if (lane < boxes) {
+    if (Cross) {
+      if (lane == 0) {
+        const int row = q.key + key_of(next);  // (behind the last row: zeros)
+        tma_load_5d(ring + put * kStage, &map_k, bar, 0, row, 0, h, 0);
+        tma_load_5d(ring + put * kStage + kHalf, &map_v, bar, 0, row, 0, h, 0);
+      }
+    } else if (lane < boxes) {
       const int k0 = key_of(next), slot = k0 & ((1 << ix.page_log2) - 1);
       const int page = k0 + (lane << box_log2) < q.len ? checked_page(ix, mine) : ix.n_pages;  // (out of range: zeros)
       unsigned char *to = ring + put * kStage + (lane << (box_log2 + (E4m3 ? 7 : 8)));
@@ -384,8 +397,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     sinks = sp.sinks, first = sp.first, steps = sp.steps;
     first_row = t * kRows;
     n_rows = min(kRows, (int)((long long)q.n * p.G) - first_row);
-    p0 = q.len - q.n + first_row / p.G;
-    const int p1 = q.len - q.n + (first_row + n_rows - 1) / p.G;
+    p0 = position(q, first_row / p.G);
+    const int p1 = position(q, (first_row + n_rows - 1) / p.G);
     end_step = (int)min((long long)steps, done + (u1 - u));
     next = done;
     next_batch = done;
@@ -453,7 +466,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int r = 0; r < 2; ++r) {
         const int row = m * 8 + c * 2 + r;
         row_scale[m][r] = E4m3 ? __shfl_sync(0xffffffffu, scale, (c * 2 + r) * 4) : scale;
-        vis[m][r] = row < n_rows ? visible(ix, q.len - q.n + (first_row + row) / p.G, q.len) : Visible{0, 0x7fffffff};
+        vis[m][r] = row < n_rows ? visible(ix, position(q, (first_row + row) / p.G), q.len) : Visible{0, 0x7fffffff};
       }
     }
     float o[NT][8][4] = {};
@@ -744,7 +757,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         t = 0;
         if (++h == p.Hkv) {
           h = 0;
-          do q = sequence(ix, ++s);
+          do q = sequence_at_place(++s);
           while (q.n == 0 && s + 1 < ix.S);
         }
       }
@@ -860,17 +873,33 @@ bool make_pool_map(CUtensorMap *m, const void *base, const CacheGeom &g, int row
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool make_states_map(CUtensorMap *m, const void *base, const CrossGeom &g, int rows) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (!fn) return false;
+  cuuint64_t dims[5] = {64, (cuuint64_t)g.Tk, 2, (cuuint64_t)g.Hkv, 1};
+  cuuint64_t strides[4] = {(cuuint64_t)g.kt * 2, 128, (cuuint64_t)g.kh * 2, (cuuint64_t)g.kh * 2};
+  cuuint32_t box[5] = {64, (cuuint32_t)rows, 2, 1, 1};
+  cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 namespace {
+
+template <int NT, bool E4m3, bool Redo, bool Cross>
+cudaError_t launch(const RowsParams &p, const CUtensorMap &mk, const CUtensorMap &mv, cudaStream_t s, int *launches) {
+  cudaError_t e = allow_shared_memory(cache_rows_kernel<NT, E4m3, Redo, Cross>, kRowsSmem);
+  if (e != cudaSuccess) return e;
+  ++*launches;
+  return launch_pdl(cache_rows_kernel<NT, E4m3, Redo, Cross>, dim3(kCacheCtas), dim3(kThreads), kRowsSmem, s, mk, mv, p);
+}
 
 template <int NT, bool E4m3, bool Redo>
 cudaError_t launch(const CacheGeom &g, const RowsParams &p, const heart_cache &c, cudaStream_t s, int *launches) {
   const int box = g.page < keys_of(E4m3) ? g.page : keys_of(E4m3);
   CUtensorMap mk, mv;
   if (!make_pool_map(&mk, c.k, g, box, 2) || !make_pool_map(&mv, c.v, g, box, 2)) return cudaErrorInvalidValue;
-  cudaError_t e = allow_shared_memory(cache_rows_kernel<NT, E4m3, Redo>, kRowsSmem);
-  if (e != cudaSuccess) return e;
-  ++*launches;
-  return launch_pdl(cache_rows_kernel<NT, E4m3, Redo>, dim3(kCacheCtas), dim3(kThreads), kRowsSmem, s, mk, mv, p);
+  return launch<NT, E4m3, Redo, false>(p, mk, mv, s, launches);
 }
 
 RowsParams rows_params(const CacheGeom &g, const CacheIndex &ix, const CacheWorkspace &w, const void *Q, const heart_cache &c, void *O, float *lse) {
@@ -902,6 +931,28 @@ cudaError_t launch_cache_rows(const CacheGeom &g, const CacheIndex &ix, const Ca
   const bool eight = (long long)g.max_new * g.G <= 8;
   if (g.e4m3) return eight ? launch<1, true, false>(g, p, c, s, launches) : launch<2, true, false>(g, p, c, s, launches);
   return eight ? launch<1, false, false>(g, p, c, s, launches) : launch<2, false, false>(g, p, c, s, launches);
+}
+
+cudaError_t launch_cross_rows(const CrossGeom &g, const CacheIndex &ix, const CrossWorkspace &w, const void *Q, const void *K, const void *V, void *O,
+                              float *lse, cudaStream_t s, int *launches) {
+  CUtensorMap mk, mv;
+  if (!make_states_map(&mk, K, g, keys_of(false)) || !make_states_map(&mv, V, g, keys_of(false))) return cudaErrorInvalidValue;
+  RowsParams p = {};
+  p.ix = ix;
+  p.Q = static_cast<const uint16_t *>(Q);
+  p.O = static_cast<uint16_t *>(O);
+  p.lse = lse;
+  p.qt = g.qt;
+  p.qh = g.qh;
+  p.Hq = g.Hq;
+  p.Hkv = g.Hkv;
+  p.G = g.G;
+  p.scale_log2 = (float)(g.scale * 1.4426950408889634);
+  p.test_skip = g.test_skip;
+  p.arrivals = w.arrivals;
+  p.parts = w.parts;
+  p.part_l = w.part_l;
+  return (long long)g.max_q * g.G <= 8 ? launch<1, false, false, true>(p, mk, mv, s, launches) : launch<2, false, false, true>(p, mk, mv, s, launches);
 }
 
 cudaError_t launch_cache_redo(const CacheGeom &g, const CacheIndex &ix, const CacheWorkspace &w, const void *Q, const heart_cache &c,

@@ -1,0 +1,64 @@
+// Cross attention: geometry, workspace, and what its two kernels share.
+#pragma once
+#include "cache.cuh"
+
+namespace heart {
+
+// Geometry derived from a validated heart_cross_config.
+struct CrossGeom {
+  int S, T, Tk, Hq, Hkv, G, max_q;
+  long long qt, qh, kt, kh;  // element strides: Q and O, K and V
+  double scale;
+  int test_skip;  // test-hook builds only (see the attention kernels)
+};
+
+struct CrossWorkspace {
+  int32_t *status;    // [64] word 0: sticky device-check code
+  int32_t *arrivals;  // [kCacheCtas] parts of a shared tile that are there (zero between launches)
+  float *parts;       // [2 * kCacheCtas][128][128] parts of tiles: unnormalised sums of values
+  float2 *part_l;     // [2 * kCacheCtas][128] their row sums and references
+  size_t bytes;
+};
+
+__host__ inline CrossWorkspace carve_cross(void *base) {
+  CrossWorkspace w;
+  char *p = static_cast<char *>(base);
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    char *at = p + off;
+    off += align256(bytes);
+    return at;
+  };
+  w.status = reinterpret_cast<int32_t *>(take(64 * sizeof(int32_t)));
+  w.arrivals = reinterpret_cast<int32_t *>(take(kCacheCtas * sizeof(int32_t)));
+  w.parts = reinterpret_cast<float *>(take(sizeof(float) * 2 * kCacheCtas * 128 * kD));
+  w.part_l = reinterpret_cast<float2 *>(take(sizeof(float2) * 2 * kCacheCtas * 128));
+  w.bytes = off;
+  return w;
+}
+
+int make_cross_geom(const heart_cross_config *c, CrossGeom *g);
+
+// ix: row_start and kv_len are the starts of the queries and the numbers of keys, table the first rows of the keys, table_stride the rows of K.
+cudaError_t launch_cross_rows(const CrossGeom &g, const CacheIndex &ix, const CrossWorkspace &w, const void *Q, const void *K, const void *V, void *O,
+                              float *lse, cudaStream_t s, int *launches);
+
+// K or V as (64 dims, row, dim half, head): a box is both halves of `rows` rows of one head, from any row on, 128-byte rows, swizzled.
+bool make_states_map(CUtensorMap *m, const void *base, const CrossGeom &g, int rows);
+
+#ifdef __CUDACC__
+// Sequence s as its arrays describe it, brought into range (and reported) where they do not hold what they should.
+__device__ __forceinline__ Sequence cross_sequence(const CacheIndex &ix, int s) {
+  int r0 = __ldcg(&ix.row_start[s]), r1 = __ldcg(&ix.row_start[s + 1]), len = __ldcg(&ix.kv_len[s]), k0 = __ldcg(&ix.table[s]);
+  const int rows = ix.table_stride;
+  if (r0 < 0 || r1 < r0 || r1 > ix.T || len < 0 || len > rows || (len > 0 && (k0 < 0 || k0 > rows - len))) {
+    atomicExch(ix.status, HEART_ERR_DEVICE_CHECK);
+    r0 = min(max(r0, 0), ix.T);
+    r1 = min(max(r1, r0), ix.T);
+    len = min(max(len, 0), rows);
+  }
+  return {r0, r1 - r0, len, min(max(k0, 0), rows - len)};
+}
+#endif
+
+}  // namespace heart

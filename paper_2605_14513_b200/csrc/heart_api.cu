@@ -2,12 +2,13 @@
 // No device memory is allocated here and nothing synchronises except heart_get_status.
 #include <math.h>
 
+#include <initializer_list>
 #include <mutex>
 #include <stdio.h>
 #include <string.h>
 
-#include "cache.cuh"
 #include "common.cuh"
+#include "cross.cuh"
 
 using namespace heart;
 
@@ -114,6 +115,44 @@ int heart::make_cache_geom(const heart_cache_config *c, CacheGeom *g) {
   return HEART_OK;
 }
 
+// The same for a heart_cross_config.
+int heart::make_cross_geom(const heart_cross_config *c, CrossGeom *g) {
+  if (c == nullptr) return HEART_ERR_INVALID;
+  if (c->S <= 0 || c->T <= 0 || c->Tk <= 0 || c->Hq <= 0 || c->Hkv <= 0 || c->max_q < 0) return HEART_ERR_INVALID;
+#ifdef HEART_TEST_HOOKS
+  g->test_skip = c->flags == 0x80000000u;
+  const uint32_t flags = c->flags & 0x7fffffffu;
+#else
+  g->test_skip = 0;
+  const uint32_t flags = c->flags;
+#endif
+  if (flags != 0 || c->Hq % c->Hkv != 0) return HEART_ERR_INVALID;
+  if (c->D != kD || c->Hq / c->Hkv > 128) return HEART_ERR_UNSUPPORTED;
+  constexpr long long kMost = (1LL << 31) - 256;  // rows are counted in 32 bits
+  if ((long long)c->T * c->Hq >= kMost || c->Tk >= kMost || c->S >= (1 << 30)) return HEART_ERR_UNSUPPORTED;
+  g->S = c->S;
+  g->T = c->T;
+  g->Tk = c->Tk;
+  g->Hq = c->Hq;
+  g->Hkv = c->Hkv;
+  g->G = c->Hq / c->Hkv;
+  g->max_q = c->max_q == 0 || c->max_q > c->T ? c->T : c->max_q;
+  auto strides_ok = [](long long a, long long b) {
+    constexpr long long kMostStride = 1LL << 38;
+    return a >= kD && b >= kD && a < kMostStride && b < kMostStride && a % 8 == 0 && b % 8 == 0;
+  };
+  const bool q_plain = c->q_stride_t == 0 && c->q_stride_h == 0, kv_plain = c->kv_stride_t == 0 && c->kv_stride_h == 0;
+  g->qt = q_plain ? (long long)c->Hq * kD : c->q_stride_t;
+  g->qh = q_plain ? kD : c->q_stride_h;
+  g->kt = kv_plain ? (long long)c->Hkv * kD : c->kv_stride_t;
+  g->kh = kv_plain ? kD : c->kv_stride_h;
+  if (!strides_ok(g->qt, g->qh) || !strides_ok(g->kt, g->kh)) return HEART_ERR_INVALID;
+  if (!isfinite(c->scale)) return HEART_ERR_INVALID;
+  g->scale = c->scale > 0.0 ? c->scale : 1.0 / sqrt((double)kD);
+  if (g->scale < 1e-30 || g->scale > 1e30) return HEART_ERR_INVALID;  // (a normal fp32 number)
+  return HEART_OK;
+}
+
 namespace {
 
 // What the three calls on a cache check alike, and the arrays as the kernels take them.
@@ -140,6 +179,13 @@ int cache_call(const heart_cache_config *cfg, const heart_cache *cache, const in
   ix->window = g->window;
   ix->sink = g->sink;
   return HEART_OK;
+}
+
+// Arrays of 32-bit words that a call needs.
+bool words_ok(std::initializer_list<const void *> words) {
+  for (const void *p : words)
+    if (!p || (reinterpret_cast<uintptr_t>(p) & 3u)) return false;
+  return true;
 }
 
 bool state_ok(const heart_state *st) {
@@ -481,6 +527,65 @@ int heart_cache_read(const heart_cache_config *cfg, const heart_cache *cache, co
   return HEART_OK;
 }
 
+size_t heart_cross_workspace_bytes(const heart_cross_config *cfg) {
+  CrossGeom g;
+  if (make_cross_geom(cfg, &g) != HEART_OK) return 0;
+  return carve_cross(nullptr).bytes;
+}
+
+int heart_cross_attn(const heart_cross_config *cfg, const void *Q, const void *K, const void *V, const int32_t *q_start, const int32_t *k_start,
+                     const int32_t *k_len, void *O, float *lse, void *workspace, heart_stream_t stream) {
+  CrossGeom g;
+  const int rc = make_cross_geom(cfg, &g);
+  if (rc != HEART_OK) return rc;
+  if (!Q || !K || !V || !O || !aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O)) return HEART_ERR_INVALID;
+  if (!words_ok({q_start, k_start, k_len}) || (reinterpret_cast<uintptr_t>(lse) & 3u)) return HEART_ERR_INVALID;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return HEART_ERR_INVALID;
+  const CrossWorkspace w = carve_cross(workspace);
+  CacheIndex ix = {};
+  ix.table = k_start;
+  ix.row_start = q_start;
+  ix.kv_len = k_len;
+  ix.status = w.status;
+  ix.S = g.S;
+  ix.T = g.T;
+  ix.table_stride = g.Tk;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  g_launches = 0;
+  cudaError_t e = launch_cross_rows(g, ix, w, Q, K, V, O, lse, s, &g_launches);
+  if (e != cudaSuccess) return cuda_fail(e, "cross_attention");
+  return HEART_OK;
+}
+
+int heart_cache_extend(const heart_cache_config *cfg, const int32_t *new_len, const int32_t *kv_len, const int32_t *free_pages,
+                       const int32_t *free_count, int32_t *page_table, int32_t *row_start, int32_t *kv_len_out, int32_t *free_count_out,
+                       int64_t *slots, void *workspace, heart_stream_t stream) {
+  CacheGeom g;
+  const int rc = make_cache_geom(cfg, &g);
+  if (rc != HEART_OK) return rc;
+  if (!words_ok({new_len, kv_len, free_pages, free_count, page_table, row_start, kv_len_out, free_count_out})) return HEART_ERR_INVALID;
+  if ((reinterpret_cast<uintptr_t>(slots) & 7u) || !workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return HEART_ERR_INVALID;
+  g_launches = 0;
+  cudaError_t e = launch_cache_extend(g, carve_cache(g, workspace), new_len, kv_len, free_pages, free_count, page_table, row_start, kv_len_out,
+                                      free_count_out, slots, static_cast<cudaStream_t>(stream), &g_launches);
+  if (e != cudaSuccess) return cuda_fail(e, "cache_extend");
+  return HEART_OK;
+}
+
+int heart_cache_release(const heart_cache_config *cfg, const uint8_t *ended, const int32_t *kv_len, int32_t *free_pages, const int32_t *free_count,
+                        const int32_t *page_table, int32_t *kv_len_out, int32_t *free_count_out, void *workspace, heart_stream_t stream) {
+  CacheGeom g;
+  const int rc = make_cache_geom(cfg, &g);
+  if (rc != HEART_OK) return rc;
+  if (!ended || !words_ok({kv_len, free_pages, free_count, page_table, kv_len_out, free_count_out})) return HEART_ERR_INVALID;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return HEART_ERR_INVALID;
+  g_launches = 0;
+  cudaError_t e = launch_cache_release(g, carve_cache(g, workspace), ended, kv_len, free_pages, free_count, page_table, kv_len_out, free_count_out,
+                                       static_cast<cudaStream_t>(stream), &g_launches);
+  if (e != cudaSuccess) return cuda_fail(e, "cache_release");
+  return HEART_OK;
+}
+
 int heart_cache_attn(const heart_cache_config *cfg, const void *Q, const heart_cache *cache, const int32_t *page_table,
                      const int32_t *row_start, const int32_t *kv_len, void *O, float *lse, void *workspace,
                      heart_stream_t stream) {
@@ -536,8 +641,8 @@ const char *heart_strerror(int code) {
     case HEART_OK: return "ok";
     case HEART_ERR_INVALID: return "invalid argument (null pointer, size, stride or alignment)";
     case HEART_ERR_UNSUPPORTED:
-      return "unsupported shape (head_dim must be 128, block 64 or 128, at most 1024 blocks; caches: page 16, 32, 64 or 128, at most 128 query heads a "
-             "key head, fewer than 2^31 rows and tokens)";
+      return "unsupported shape (head_dim must be 128, block 64 or 128, at most 1024 blocks; caches: page 16, 32, 64 or 128; caches and cross "
+             "attention: at most 128 query heads a key head, fewer than 2^31 rows and tokens)";
     case HEART_ERR_CUDA: return g_errbuf[0] ? g_errbuf : "CUDA error";
     case HEART_ERR_TOO_LARGE: return "shape needs more scratch than the built-in HEART_STATIC_SCRATCH_BYTES array holds";
     case HEART_ERR_INFEASIBLE: return "no assignment of one candidate per head meets the sparsity budget";

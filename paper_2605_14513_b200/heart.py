@@ -29,6 +29,7 @@ SYMBOLS = (
     "heart_last_launch_count", "heart_drift_static", "heart_full_token_drift", "heart_mask_iou",
     "heart_band_error_workspace_bytes", "heart_band_error", "heart_drift_workspace_bytes",
     "heart_assign_thresholds", "heart_cache_workspace_bytes", "heart_cache_write", "heart_cache_read", "heart_cache_attn",
+    "heart_cache_extend", "heart_cache_release", "heart_cross_workspace_bytes", "heart_cross_attn",
 )
 
 
@@ -54,6 +55,11 @@ class CacheConfig(C.Structure):
 
 class CacheStruct(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+
+
+class CrossConfig(C.Structure):
+    _fields_ = ([(x, C.c_int32) for x in ("S", "T", "Tk", "Hq", "Hkv", "D", "max_q")] + [("flags", C.c_uint32)] +
+                [(x, C.c_int64) for x in ("q_stride_t", "q_stride_h", "kv_stride_t", "kv_stride_h")] + [("scale", C.c_double)])
 
 
 class HeartError(RuntimeError):
@@ -114,8 +120,14 @@ def load(path):
         l.heart_cache_write.argtypes = [C.POINTER(CacheConfig), vp, vp, C.POINTER(CacheStruct)] + [vp] * 5
         l.heart_cache_read.argtypes = [C.POINTER(CacheConfig), C.POINTER(CacheStruct)] + [vp] * 7
         l.heart_cache_attn.argtypes = [C.POINTER(CacheConfig), vp, C.POINTER(CacheStruct)] + [vp] * 7
+        l.heart_cache_extend.argtypes = [C.POINTER(CacheConfig)] + [vp] * 11
+        l.heart_cache_release.argtypes = [C.POINTER(CacheConfig)] + [vp] * 9
+        l.heart_cross_workspace_bytes.argtypes = [C.POINTER(CrossConfig)]
+        l.heart_cross_workspace_bytes.restype = C.c_size_t
+        l.heart_cross_attn.argtypes = [C.POINTER(CrossConfig)] + [vp] * 10
         for fn in ("heart_state_reset", "heart_drift", "heart_predict_mask", "heart_block_sparse_attn",
-                   "heart_step", "heart_step_host", "heart_get_status", "heart_cache_write", "heart_cache_read", "heart_cache_attn"):
+                   "heart_step", "heart_step_host", "heart_get_status", "heart_cache_write", "heart_cache_read", "heart_cache_attn",
+                   "heart_cache_extend", "heart_cache_release", "heart_cross_attn"):
             getattr(l, fn).restype = C.c_int
     return l
 
@@ -353,7 +365,11 @@ def _cache_call(cfg, cache, query, tensors, page_table, row_start, kv_len, ws):
 
 def _cache_launch(call, cache, *args):
     """The call on the current stream of the cache's device."""
-    device = cache.device
+    _launch(call, cache.device, *args)
+
+
+def _launch(call, device, *args):
+    """The call on the device's current stream."""
     if device == torch._C._cuda_getDevice():
         rc = call(*args, torch._C._cuda_getCurrentRawStream(device))
     else:
@@ -385,6 +401,95 @@ def heart_cache_attn(cfg, Q, cache: Cache, page_table, row_start, kv_len, O, ws,
         raise ValueError(f"lse has to be contiguous fp32 [{cfg.T}, {cfg.Hq}] beside the cache: got {lse.dtype} {tuple(lse.shape)} on {lse.device}")
     _cache_launch(lib().heart_cache_attn, cache, C.byref(cfg), Q.data_ptr(), cache.ref, page_table.data_ptr(), row_start.data_ptr(), kv_len.data_ptr(),
                   O.data_ptr(), _ptr(lse), ws.data_ptr())
+
+
+def _table_call(cfg, arrays, ws):
+    """Checks the arrays of a table call, (name, tensor, type, entries), and the workspace: on one device, which it returns."""
+    device = ws.get_device()
+    for name, x, dtype, n in arrays:
+        if x.dtype is not dtype or x.numel() != n or x.get_device() != device or not x.is_contiguous():
+            raise ValueError(f"{name} has to be contiguous {dtype} of {n} entries beside the workspace: got {x.dtype} {tuple(x.shape)} on {x.device}")
+    if device < 0 or not ws.is_contiguous() or ws.nbytes < _cache_workspace_bytes(cfg.S, cfg.T, cfg.Hq, cfg.Hkv):
+        raise ValueError(f"the workspace has to have cache_workspace_bytes(cfg) = {cache_workspace_bytes(cfg)} bytes on a GPU")
+    return device
+
+
+def heart_cache_extend(cfg, new_len, kv_len, free_pages, free_count, page_table, row_start, ws, slots=None, kv_len_out=None, free_count_out=None):
+    """Gives the sequences (kv_len: int32 [S]) pages for new_len more tokens from the stack free_pages (int32 [n_pages], free_count [1] of them) and
+    writes page_table, row_start and, if given, slots (int64 [T]).  Lengths and count go to kv_len_out and free_count_out, or are updated in place."""
+    kv_len_out = kv_len if kv_len_out is None else kv_len_out
+    free_count_out = free_count if free_count_out is None else free_count_out
+    S, i32 = cfg.S, torch.int32
+    arrays = [("new_len", new_len, i32, S), ("kv_len", kv_len, i32, S), ("free_pages", free_pages, i32, cfg.n_pages), ("free_count", free_count, i32, 1),
+              ("page_table", page_table, i32, S * cfg.table_stride), ("row_start", row_start, i32, S + 1), ("kv_len_out", kv_len_out, i32, S),
+              ("free_count_out", free_count_out, i32, 1)]
+    if slots is not None:
+        arrays.append(("slots", slots, torch.int64, cfg.T))
+    device = _table_call(cfg, arrays, ws)
+    _launch(lib().heart_cache_extend, device, C.byref(cfg), *(x.data_ptr() for _, x, _, _ in arrays[:8]), _ptr(slots), ws.data_ptr())
+
+
+def heart_cache_release(cfg, ended, kv_len, free_pages, free_count, page_table, ws, kv_len_out=None, free_count_out=None):
+    """Puts the pages of the sequences with ended (uint8 [S]) back on the stack; lengths (0 for those) and count as in heart_cache_extend."""
+    kv_len_out = kv_len if kv_len_out is None else kv_len_out
+    free_count_out = free_count if free_count_out is None else free_count_out
+    S, i32 = cfg.S, torch.int32
+    arrays = [("ended", ended, torch.uint8, S), ("kv_len", kv_len, i32, S), ("free_pages", free_pages, i32, cfg.n_pages), ("free_count", free_count, i32, 1),
+              ("page_table", page_table, i32, S * cfg.table_stride), ("kv_len_out", kv_len_out, i32, S), ("free_count_out", free_count_out, i32, 1)]
+    device = _table_call(cfg, arrays, ws)
+    _launch(lib().heart_cache_release, device, C.byref(cfg), *(x.data_ptr() for _, x, _, _ in arrays), ws.data_ptr())
+
+
+# ---- Cross attention: to states of another length.
+
+
+def make_cross_config(S, T, Tk, Hq, Hkv, max_q=0, D=128, scale=0.0, q_strides=(0, 0), kv_strides=(0, 0)) -> CrossConfig:
+    """S sequences, T rows of Q and O, Tk rows of K and V.  max_q, the most queries of a sequence, selects the kernel: 0 (not known) is right for
+    any lengths, but slow where there are few (say 1 for a step of single tokens).  Strides in elements: (token, head) of Q and O, and of K and V; zeros
+    select the contiguous layouts."""
+    return CrossConfig(S, T, Tk, Hq, Hkv, D, max_q, 0, *q_strides, *kv_strides, scale)
+
+
+def cross_workspace_bytes(cfg: CrossConfig) -> int:
+    return int(lib().heart_cross_workspace_bytes(C.byref(cfg)))
+
+
+def new_cross_workspace(cfg: CrossConfig, device="cuda") -> torch.Tensor:
+    n = cross_workspace_bytes(cfg)
+    if n == 0:
+        raise HeartError(ERR_UNSUPPORTED)
+    return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+_cross_fields = struct.Struct("=7iI4qd").unpack_from
+
+
+@functools.lru_cache(maxsize=1)
+def _cross_workspace_bytes():
+    """(It has one size.)"""
+    return cross_workspace_bytes(make_cross_config(1, 1, 1, 1, 1))
+
+
+def heart_cross_attn(cfg, Q, K, V, q_start, k_start, k_len, O, ws, lse=None):
+    """Attention of the packed rows of Q (bf16 [T, Hq, D], sequence s from q_start[s] to q_start[s + 1]) over the rows k_start[s] .. + k_len[s]
+    of K and V (bf16 [Tk, Hkv, D]) into O; lse: optional fp32 [T, Hq].  q_start, k_start, k_len: int32 on the GPU, [S + 1], [S], [S]."""
+    S, T, Tk, Hq, Hkv, _, _, _, qt, qh, kt, kh, _ = _cross_fields(cfg)
+    device = Q.get_device()
+    for x, rows, heads, t, h in ((Q, T, Hq, qt, qh), (O, T, Hq, qt, qh), (K, Tk, Hkv, kt, kh), (V, Tk, Hkv, kt, kh)):
+        if (x.dtype is not torch.bfloat16 or x.numel() != rows * heads * 128 or x.get_device() != device or
+                not (_has_strides(x, rows, heads, t, h) if t else x.is_contiguous())):
+            raise ValueError(f"packed tensors have to be bf16, {rows} rows x {heads} heads x 128, on one GPU, contiguous or with their strides in the "
+                             f"config: got {x.dtype} {tuple(x.shape)}, strides {x.stride()}, on {x.device}")
+    for x, n in ((q_start, S + 1), (k_start, S), (k_len, S)):
+        if x.dtype is not torch.int32 or x.numel() != n or x.get_device() != device or not x.is_contiguous():
+            raise ValueError(f"q_start, k_start and k_len have to be contiguous int32 of {S + 1}, {S} and {S} entries beside Q: got {x.dtype} "
+                             f"{tuple(x.shape)} on {x.device}")
+    if lse is not None and (lse.dtype is not torch.float32 or lse.numel() != T * Hq or lse.get_device() != device or not lse.is_contiguous()):
+        raise ValueError(f"lse has to be contiguous fp32 [{T}, {Hq}] beside Q: got {lse.dtype} {tuple(lse.shape)} on {lse.device}")
+    if device < 0 or ws.get_device() != device or not ws.is_contiguous() or ws.nbytes < _cross_workspace_bytes():
+        raise ValueError(f"the workspace has to have cross_workspace_bytes(cfg) = {cross_workspace_bytes(cfg)} bytes beside Q, on a GPU")
+    _launch(lib().heart_cross_attn, device, C.byref(cfg), Q.data_ptr(), K.data_ptr(), V.data_ptr(), q_start.data_ptr(), k_start.data_ptr(),
+            k_len.data_ptr(), O.data_ptr(), _ptr(lse), ws.data_ptr())
 
 
 def heart_full_token_drift(cfg, Qa, Ka, Qb, Kb, drift_out, ws):
