@@ -43,6 +43,7 @@
 
 #include "cache.cuh"
 #include "tc_ptx.cuh"
+#include "tiles.cuh"
 
 namespace heart {
 using namespace tc;
@@ -158,27 +159,6 @@ struct TileParams {
   __device__ __forceinline__ int token_of(int row) const { return (int)(((uint32_t)row * inv_G) >> 16); }
 };
 
-__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-// Weights 2^(s*c - m) of 32 scores of a row, packed to bf16 or f16, and their sums (of the weights before they are rounded: the log-sum-exp
-// is then good to 32 bits).
-template <bool F16>
-__device__ __forceinline__ void exp32(const uint32_t *s, uint64_t c2, uint64_t neg_m2, uint32_t *pk, uint64_t (&sums)[2]) {
-#pragma unroll
-  for (int i = 0; i < 32; i += 4) {
-    float x0, x1, x2, x3;
-    unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), c2, neg_m2), x0, x1);
-    unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(s[i + 2]), __uint_as_float(s[i + 3])), c2, neg_m2), x2, x3);
-    x0 = ex2(x0), x1 = ex2(x1), x2 = ex2(x2), x3 = ex2(x3);
-    sums[0] = add_f32x2(sums[0], pack_f32x2(x0, x1));
-    sums[1] = add_f32x2(sums[1], pack_f32x2(x2, x3));
-    pk[i >> 1] = F16 ? pack_f16x2(x0, x1) : pack_bf16x2(x0, x1);
-    pk[(i >> 1) + 1] = F16 ? pack_f16x2(x2, x3) : pack_bf16x2(x2, x3);
-  }
-}
 // D[tmem] (+)= A[smem] * B[smem], e4m3
 __device__ __forceinline__ void mma_ss_e4m3(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -201,9 +181,6 @@ __device__ __forceinline__ uint2 lds_u2(uint32_t addr) {
   return v;
 }
 __device__ __forceinline__ void sts_u1(uint32_t addr, uint32_t v) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
-__device__ __forceinline__ void sts_u4(uint32_t addr, uint4 v) {
-  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
-}
 // Zero as long as all of the bf16 numbers so far are finite, NaN from the first one on that is not: 0 * x + sum.
 __device__ __forceinline__ uint32_t add_zero_times(const uint4 &x, uint32_t sum) {
   auto add = [&](uint32_t w) { asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(sum) : "r"(w), "r"(0u)); };
@@ -1453,18 +1430,6 @@ __global__ void __launch_bounds__(Layout<E4m3>::kThreads, 1)
     tmem_dealloc(tmem, 512);
   }
   if (tid == 0 && sh.abort) atomicExch(ix.status, HEART_ERR_DEVICE_CHECK);
-}
-
-// Q as (64 dims, query head of its key head, token, dim half, key head): a box is the tokens of a tile with their G heads.
-bool make_query_map(CUtensorMap *m, const void *Q, const CacheGeom &g) {
-  EncodeTiledFn fn = encode_tiled_fn();
-  if (!fn) return false;
-  cuuint64_t dims[5] = {64, (cuuint64_t)g.G, (cuuint64_t)g.T, 2, (cuuint64_t)g.Hkv};
-  cuuint64_t strides[4] = {(cuuint64_t)g.qh * 2, (cuuint64_t)g.qt * 2, 128, (cuuint64_t)g.qh * g.G * 2};
-  cuuint32_t box[5] = {64, (cuuint32_t)g.G, (cuuint32_t)(128 / g.G), 1, 1};
-  cuuint32_t estr[5] = {1, 1, 1, 1, 1};
-  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void *>(Q), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <bool E4m3>

@@ -42,6 +42,8 @@ int make_cross_geom(const heart_cross_config *c, CrossGeom *g);
 // ix: row_start and kv_len are the starts of the queries and the numbers of keys, table the first rows of the keys, table_stride the rows of K.
 cudaError_t launch_cross_rows(const CrossGeom &g, const CacheIndex &ix, const CrossWorkspace &w, const void *Q, const void *K, const void *V, void *O,
                               float *lse, cudaStream_t s, int *launches);
+cudaError_t launch_cross_tiles(const CrossGeom &g, const CacheIndex &ix, const CrossWorkspace &w, const void *Q, const void *K, const void *V, void *O,
+                               float *lse, cudaStream_t s, int *launches);
 
 // K or V as (64 dims, row, dim half, head): a box is both halves of `rows` rows of one head, from any row on, 128-byte rows, swizzled.
 bool make_states_map(CUtensorMap *m, const void *base, const CrossGeom &g, int rows);
