@@ -4,8 +4,10 @@
 // softmax warpgroups that take the CTA's key steps in turn, scores double-buffered in tensor memory; the reasons are those at the top of attn_tc.cu, and so
 // are what bounds it (the tensor pipe 1024 clocks a step, the special-function units 1024, shared memory 1280) and the way two warpgroups agree on a
 // row's reference.  What differs, since all rows of a tile see the same keys and these are few (a text: 512, four steps):
-//   * The end of a tile is the common case.  A warpgroup of its own takes the sums out of tensor memory and writes the rows, straight from
-//     registers (a thread has a row, 32 bytes a store), while the others are in the next tile's first steps.
+//   * The end of a tile is the common case.  A warpgroup of its own takes the sums out of tensor memory, by way of registers, as bf16, into shared memory, from
+//     where bulk copies write them, while the others are in the next tile's first steps.  That has room for a whole tile, which the one before leaves
+//     meanwhile: stores of all SMs go at some 10 bytes a clock and SM, 3000 clocks a tile, and whoever waits for them (the warps where they store themselves, or a
+//     half that waits for the other's place) is late for the next tile's sums.  The room is found by putting the row sums in the place of the tile's Q.
 //   * A tile's last step may have fewer than 128 keys: the products are cut to the next 16 keys (columns of the scores, steps of the values' product),
 //     the softmax to the next 32; scores behind the last key become -inf, values of up to 15 rows behind it, which are anyone's, zeros in shared memory.
 //   * There is no plan: all tiles of a sequence take the same number of steps, so a CTA finds its share of the line of all tiles' steps, (sequence, head,
@@ -26,9 +28,9 @@ namespace heart {
 using namespace tc;
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kThreads = 512;
 constexpr int kWarpQK = 8, kWarpV = 9, kWarpK = 10, kWarpPV = 11, kWarpOut = 12;
-constexpr int kRegsSoftmax = 192, kRegsOut = 72, kRegsHelper = 56;  // 192 * 256 + 72 * 128 + 56 * 128 = the CTA's 512 x 128
+constexpr int kRegsSoftmax = 184, kRegsOut = 104, kRegsHelper = 40;  // 184 * 256 + 104 * 128 + 40 * 128 = the CTA's 512 x 128
 static_assert(kRegsSoftmax * 256 + kRegsOut * 128 + kRegsHelper * 128 <= kThreads * 128, "registers at launch");
 constexpr int kTileBytes = 32768;  // 128 rows x 128 dims: [2 dim halves][128 rows][64] bf16, 128-byte swizzle
 constexpr int kTileCost = 1;       // of a tile besides its steps, in steps
@@ -52,34 +54,43 @@ static_assert(sizeof(Part) % 16 == 0, "copied by words");
 // Where a CTA is in the line of all tiles' costs.
 struct Walk {
   Sequence q;
-  int s, h, tile, off;  // off: what of the tile's cost lies before the share
-  long long u, end, share;
+  int tiles, steps;         // of the sequence and a head, of a tile
+  int s, h, tile, off;      // off: what of the tile's cost lies before the share
+  long long u, end, share;  // of the line
   bool whole;           // tiles are not shared: a CTA takes those that begin in its share
 };
 
+// Sequences in a row: the length of their line, the largest cost of a tile.
+struct alignas(16) Chunk {
+  long long line;
+  int longest;
+};
+static_assert(kThreads * sizeof(Chunk) <= kTileBytes, "they lie where rows are staged later");
+
 struct CrossShared {
   uint64_t q_full[2], k_full[2], v_full[2];
-  uint64_t v_ready[2];     // V_g has nothing behind its last key that a product reads
+  uint64_t l_ready[2][4], l_read[2];  // the row sum of the steps of the warpgroup without the last one is there, per lane quarter; the row sums have been read
+  uint64_t v_tail;         // V_g is there, but for what is behind its last key
   uint64_t s_full[2], s_free[2], p_full[2], pv_done[2], m_ready[2][4];  // as in attn_tc.cu
   uint64_t o_full[2], o_free;
   uint64_t part_full[kPartRing], part_empty[kPartRing];
   uint64_t drain[2];
+  uint64_t staged, stage_free;  // 64 dims of a tile's rows are in shared memory; have left it
+  uint64_t finished;       // the other warps are through
   uint64_t stored, told;   // this CTA's part of a tile is in the workspace; it is the last one or not
   Part part[kPartRing];
-  float m[2][128];         // references after step g
-  float2 l[4][2][128];     // row sums and references: per part & 3 and warpgroup
-  long long sums[kWarps];
-  int longest[kWarps];
+  float m[128];            // references after the last step that has found them
+  float l[2][128];         // of the row sums: the other warpgroup's part, then one over them, per part & 1
   Walk walk;
-  Sequence found;          // the share's first sequence
-  int found_s;
-  long long found_at;      // cost before it
   uint32_t tmem_base;
   int shared_parts;        // parts of shared tiles that have been announced
+  Part spare;
+  int4 owed[2];            // this CTA's parts of shared tiles: place in the workspace, first CTA of the tile, number of its parts
+  int n_owed;
   int last;
   int abort;
 };
-constexpr int kOffQ = 0, kOffK = 2 * kTileBytes, kOffV = 4 * kTileBytes, kOffShared = 6 * kTileBytes;
+constexpr int kOffQ = 0, kOffK = 2 * kTileBytes, kOffV = 4 * kTileBytes, kOffStage = 6 * kTileBytes, kOffShared = kOffStage + kTileBytes;
 constexpr int kSmem = kOffShared + sizeof(CrossShared);
 static_assert(kSmem <= 232448, "shared memory of an SM");
 
@@ -94,24 +105,32 @@ struct CrossParams {
   int Hq, Hkv, G;
   uint32_t inv_G;          // row / G = row * inv_G >> 16 for the rows of a tile
   float scale_log2;
-  bool wide;               // rows of O begin on 32 bytes
   int test_skip;           // test-hook builds only: CTA 0 leaves out its second copy of values
 };
 
-__device__ __forceinline__ void store32(uint16_t *to, const uint32_t *x, bool wide) {  // 32 bytes
-  if (wide) {
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]),
-                 "r"(x[6]), "r"(x[7])
-                 : "memory");
-  } else {
-    *reinterpret_cast<uint4 *>(to) = make_uint4(x[0], x[1], x[2], x[3]);
-    *reinterpret_cast<uint4 *>(to + 8) = make_uint4(x[4], x[5], x[6], x[7]);
-  }
+// Waits for the barrier's phase of this parity; false if *abort is raised before.
+__device__ __forceinline__ bool wait_unless(uint32_t bar, uint32_t parity, uint32_t abort) {
+  uint32_t there;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b32 a;\n"
+      "again:\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 200000;\n\t"
+      "@p bra done;\n\t"
+      "ld.volatile.shared.u32 a, [%3];\n\t"
+      "setp.eq.u32 p, a, 0;\n\t"
+      "@p bra again;\n\t"
+      "setp.ne.u32 p, a, a;\n"
+      "done:\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(there)
+      : "r"(bar), "r"(parity), "r"(abort)
+      : "memory");
+  return there != 0;
 }
 
 __global__ void __launch_bounds__(kThreads, 1)
     cross_tile_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
-                      const __grid_constant__ CUtensorMap map_v, const CrossParams p) {
+                      const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_o, const CrossParams p) {
   extern __shared__ __align__(1024) unsigned char smem[];
   CrossShared &sh = *reinterpret_cast<CrossShared *>(smem + kOffShared);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -122,14 +141,17 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sh.q_full[i], 1);
+      mbar_init(&sh.l_read[i], 4);
       mbar_init(&sh.k_full[i], 1);
       mbar_init(&sh.v_full[i], 1);
-      mbar_init(&sh.v_ready[i], 1);
       mbar_init(&sh.s_full[i], 1);
       mbar_init(&sh.s_free[i], 4);
       mbar_init(&sh.p_full[i], 4);
       mbar_init(&sh.pv_done[i], 1);
-      for (int q = 0; q < 4; ++q) mbar_init(&sh.m_ready[i][q], 1);
+      for (int q = 0; q < 4; ++q) {
+        mbar_init(&sh.m_ready[i][q], 1);
+        mbar_init(&sh.l_ready[i][q], 1);
+      }
       mbar_init(&sh.o_full[i], 1);
       mbar_init(&sh.drain[i], 1);
     }
@@ -137,17 +159,26 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&sh.part_full[i], 1);
       mbar_init(&sh.part_empty[i], kReaders);
     }
+    mbar_init(&sh.v_tail, 1);
     mbar_init(&sh.o_free, 4);
+    mbar_init(&sh.staged, 4);
+    mbar_init(&sh.stage_free, 1);
     mbar_init(&sh.stored, 4);
     mbar_init(&sh.told, 1);
+    mbar_init(&sh.finished, kThreads / 32 - 1);
     sh.abort = 0;
-    sh.shared_parts = 0;
+    sh.shared_parts = sh.n_owed = 0;
     mbar_fence_init();
   }
   if (warp == kWarpK && lane == 0) {
     tma_prefetch_desc(&map_q);
     tma_prefetch_desc(&map_k);
     tma_prefetch_desc(&map_v);
+    tma_prefetch_desc(&map_o);
+  }
+  if (warp == kWarpQK) {
+    tmem_alloc(&sh.tmem_base, 512);
+    tmem_relinquish();
   }
   pdl_wait();
   pdl_launch_dependents();
@@ -157,89 +188,58 @@ __global__ void __launch_bounds__(kThreads, 1)
   auto tiles_of = [&](const Sequence &q) { return (int)(((long long)q.n + tokens_per_tile - 1) / tokens_per_tile); };
   auto steps_of = [&](const Sequence &q) { return max((q.len + kKeyStep - 1) / kKeyStep, 1); };  // (one without any key: the rows are written)
   auto cost_of = [&](const Sequence &q) { return steps_of(q) + kTileCost; };
-  {
-    Sequence q = {0, 0, 0, 0};
-    long long mine = 0, total = 0;
-    int longest = 1;
-    for (int i = tid; i < ix.S; i += kThreads) {
-      const Sequence x = cross_sequence(ix, i);
-      const int tiles = tiles_of(x), cost = cost_of(x);
-      const long long all = (long long)tiles * cost * p.Hkv;
-      if (i < kThreads) q = x, mine = all;
-      if (tiles > 0) longest = max(longest, cost);
-      total += all;
+  auto quotient = [](long long a, long long b) -> long long {  // (small code: of numbers that fit 32 bits as a rule, of others a bit at a time)
+    if (((a | b) >> 32) == 0) return (long long)((uint32_t)a / (uint32_t)b);
+    long long q = 0, r = 0;
+#pragma unroll 1
+    for (int i = 62; i >= 0; --i) {
+      r = r << 1 | (a >> i & 1);
+      q <<= 1;
+      if (r >= b) r -= b, q |= 1;
     }
-    const long long first_mine = mine;
-#pragma unroll
-    for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-    longest = __reduce_max_sync(0xffffffffu, longest);
-    if (lane == 0) sh.sums[warp] = total, sh.longest[warp] = longest;
-    __syncthreads();
-    total = 0;
-    for (int i = 0; i < kWarps; ++i) {
-      total += sh.sums[i];
-      longest = max(longest, sh.longest[i]);
+    return q;
+  };
+  auto line_of = [&](const Sequence &q) { return (long long)tiles_of(q) * cost_of(q) * p.Hkv; };
+  // what the sequences cost, some in a row a thread
+  Chunk *const chunks = reinterpret_cast<Chunk *>(smem + kOffStage);
+  const int per_chunk = (ix.S + kThreads - 1) / kThreads, n_chunks = (ix.S + per_chunk - 1) / per_chunk;
+  if (tid < n_chunks) {
+    Chunk mine = {0, 1};
+#pragma unroll 1
+    for (int i = tid * per_chunk; i < min(ix.S, (tid + 1) * per_chunk); ++i) {
+      const Sequence q = cross_sequence(ix, i);
+      const long long line = line_of(q);
+      mine.line += line;
+      if (line > 0) mine.longest = max(mine.longest, cost_of(q));
     }
-    const bool whole = longest <= kWholeSteps + kTileCost;
-    const long long share = max((total + gridDim.x - 1) / gridDim.x, whole ? 1LL : (long long)(longest + kMaxParts - 1) / kMaxParts);
-    const long long u0 = blockIdx.x * share, u1 = min(total, u0 + share);
-    if (u0 >= u1) return;
-    if (tid == 0) sh.walk.end = u1, sh.walk.share = share, sh.walk.whole = whole;
-    long long before = 0;
-    mine = first_mine;
-    for (int base = 0; base < ix.S; base += kThreads) {
-      if (base > 0) {
-        mine = 0;
-        if (base + tid < ix.S) {
-          q = cross_sequence(ix, base + tid);
-          mine = (long long)tiles_of(q) * cost_of(q) * p.Hkv;
-        }
-      }
-      long long upto = mine;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const long long x = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += x;
-      }
-      __syncthreads();
-      if (lane == 31) sh.sums[warp] = upto;
-      __syncthreads();
-      long long at = before + upto - mine, all = 0;
-      for (int i = 0; i < kWarps; ++i) {
-        if (i < warp) at += sh.sums[i];
-        all += sh.sums[i];
-      }
-      if (at <= u0 && u0 < at + mine) {
-        sh.found = q;
-        sh.found_s = base + tid;
-        sh.found_at = at;
-      }
-      before += all;
-      if (before > u0) break;
-    }
-  }
-  if (warp == kWarpQK) {
-    tmem_alloc(&sh.tmem_base, 512);
-    tmem_relinquish();
+    chunks[tid] = mine;
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = sh.tmem_base;
 
-  // Bounded waits of a whole warp; ok turns false when one runs out or the CTA aborts.
+  // Waits of a whole warp; ok turns false when the CTA aborts.  Little code: it stands in many places.  What bounds them all is the K producer's clock: nothing goes
+  // on for long when one of its copies' places does not become free, and at the end it waits for the other warps.
   bool ok = true;
   auto wait = [&](uint64_t *bar, uint32_t parity) {
-    uint32_t since = 0;
+    return ok = __all_sync(0xffffffffu, wait_unless(smem_u32(bar), parity, smem_u32(&sh.abort)));
+  };
+  auto timed_wait = [&](uint64_t *bar, uint32_t parity) {
+    const uint32_t since = clock();
 #pragma unroll 1
     while (__builtin_expect(!__all_sync(0xffffffffu, mbar_try_wait(bar, parity)), 0)) {
-      const uint32_t now = clock() | 1u;
-      if (since == 0) since = now;
-      if (__any_sync(0xffffffffu, *abort != 0 || now - since > (uint32_t)kWaitLimitCycles)) {
+      if (__any_sync(0xffffffffu, *abort != 0 || (uint32_t)clock() - since > (uint32_t)kWaitLimitCycles)) {
         *abort = 1;
         return ok = false;
       }
     }
+    return ok;
+  };
+  auto wait2 = [&](uint64_t *bar0, uint32_t parity0, uint64_t *bar1, uint32_t parity1) {  // (one after the other, by the same instructions)
+#pragma unroll 1
+    for (int i = 0; i < 2; ++i)
+      if (!wait(i == 0 ? bar0 : bar1, i == 0 ? parity0 : parity1)) break;
     return ok;
   };
   // The announced part n; nullptr: none left (or abort).
@@ -279,37 +279,31 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   };
   // ------------------------------------------------------------------ the CTA's parts, in order (by one thread, in shared memory)
-  auto walk_begins = [&](Walk &w) {
-    w.q = sh.found;
-    w.s = sh.found_s;
-    const int tiles = tiles_of(w.q), cost = cost_of(w.q);
-    w.u = blockIdx.x * w.share;
-    const long long rest = w.u - sh.found_at;
-    const long long at = rest / cost;  // tile of all heads
-    w.off = (int)(rest - at * cost);
-    w.h = (int)(at / tiles);
-    w.tile = (int)(at - (long long)w.h * tiles);
+  auto next_sequence = [&](Walk &w) {
+    w.q = cross_sequence(ix, ++w.s);
+    w.tiles = tiles_of(w.q);
+    w.steps = steps_of(w.q);
   };
   auto walk_on = [&](Walk &w) {  // to the next tile, whose cost begins at u
     w.off = 0;
-    if (++w.tile < tiles_of(w.q)) return;
+    if (++w.tile < w.tiles) return;
     w.tile = 0;
     if (++w.h < p.Hkv) return;
     w.h = 0;
-    do w.q = cross_sequence(ix, ++w.s);
-    while (w.q.n == 0 && w.s + 1 < ix.S);
+#pragma unroll 1
+    do next_sequence(w);
+    while (w.tiles == 0 && w.s + 1 < ix.S);
   };
-  // The part at w, behind which w then is; false: none left.
-  auto next_part = [&](Walk &w, Part &x) {
-    if (w.whole && w.off > 0) {
-      w.u += cost_of(w.q) - w.off;
-      if (w.u < w.end) walk_on(w);
-    }
+  auto next_part = [&](Walk &w, Part &x) {  // false: none left
     x.b = -1;
-    if (w.u >= w.end) return false;
-    const int steps = steps_of(w.q);
-    const int a = max(w.off - kTileCost, 0);
-    const int b = w.whole ? steps : (int)min((long long)steps, w.off + (w.end - w.u) - kTileCost);
+    if (w.u >= w.end) return false;  // (the rest of w is nothing where the CTA has no share)
+    if (w.whole && w.off > 0) {
+      w.u += w.steps + kTileCost - w.off;
+      if (w.u >= w.end) return false;
+      walk_on(w);
+    }
+    const int off = w.off, steps = w.steps, a = max(off - kTileCost, 0);
+    const int b = w.whole ? steps : (int)min((long long)steps, off + (w.end - w.u) - kTileCost);
     if (b <= a) return false;  // (the share ends before the tile's first step)
     x.row = w.q.row + w.tile * tokens_per_tile;
     x.tokens = min(tokens_per_tile, w.q.n - w.tile * tokens_per_tile);
@@ -319,237 +313,111 @@ __global__ void __launch_bounds__(kThreads, 1)
     x.steps = steps;
     x.a = a;
     x.b = b;
-    const long long first = w.u - w.off + kTileCost;
     x.c0 = blockIdx.x;
     x.parts = 1;
     if (b - a < steps) {
-      x.c0 = (int)(first / w.share);
-      x.parts = (int)((first + steps - 1) / w.share) - x.c0 + 1;
+      const long long first = w.u - off + kTileCost;
+      x.c0 = (int)quotient(first, w.share);
+      x.parts = (int)quotient(first + steps - 1, w.share) - x.c0 + 1;
     }
-    w.u += b + kTileCost - w.off;
+    w.u += b + kTileCost - off;
     if (w.u < w.end) walk_on(w);
     return true;
   };
 
+  auto lse_of = [&](const Part *x, int row) {
+    const int t = (int)(((uint32_t)row * p.inv_G) >> 16);
+    return p.lse + (long long)(x->row + t) * p.Hq + x->h * p.G + row - t * p.G;
+  };
+
   // ------------------------------------------------------------------ roles
+  // (Each warpgroup's registers are set where its code begins: behind a place where two come together again the compiler counts on the smaller number.)
   if (warp >= kWarpOut) {
-    setmaxnreg_dec<kRegsOut>();
-  } else if (warp >= kWarpQK) {
-    setmaxnreg_dec<kRegsHelper>();
-  }
-  if (warp == kWarpK) {
-    // ===== the CTA's parts; K and Q producer
-    if (lane == 0) walk_begins(sh.walk);
-    auto announce = [&](int m) {
-      if (m >= kPartRing && !wait(&sh.part_empty[m % kPartRing], (m / kPartRing - 1) & 1)) return false;
-      Part &x = sh.part[m % kPartRing];
-      if (lane == 0) {
-        next_part(sh.walk, x);
-        mbar_arrive(&sh.part_full[m % kPartRing]);
-      }
-      __syncwarp();
-      return x.b >= 0;
-    };
-    int g = 0, n = 0;
-    bool any = announce(0);
-#pragma unroll 1
-    for (; ok && any; ++n) {
-      const Part &x = sh.part[n % kPartRing];  // (this warp alone writes the ring)
-      const int a = x.a, b = x.b, h = x.h, key = x.key, row = x.row;
-#pragma unroll 1
-      for (int i = a; i < b; ++i, ++g) {
-        if (g >= 2 && !wait(&sh.s_full[g & 1], ((g - 2) >> 1) & 1)) break;
-        load_tile(smem + kOffK + (g & 1) * kTileBytes, &map_k, &sh.k_full[g & 1], key + i * kKeyStep, h);
-        if (i == a && lane == 0) {  // (the scores of step g - 2 are complete, and with them those of part n - 2: its Q has been read)
-          unsigned char *q = smem + kOffQ + (n & 1) * kTileBytes;
-          mbar_expect_tx(&sh.q_full[n & 1], 2 * (128 / p.G * p.G) * 128);
-          tma_load_5d(q, &map_q, &sh.q_full[n & 1], 0, 0, row, 0, h);
-          tma_load_5d(q + kTileBytes / 2, &map_q, &sh.q_full[n & 1], 0, 0, row, 1, h);
-        }
-        __syncwarp();
-      }
-      if (ok) any = announce(n + 1);
-    }
-    if (*abort) {
-      settle_pair(sh.k_full, g);
-      settle_pair(sh.q_full, n);  // (n counts a part that was broken off too: its Q came with its first step, or not at all)
-    }
-  } else if (warp == kWarpV) {
-    // ===== V producer
-    int g = 0;
-#pragma unroll 1
-    for (int n = 0; ok; ++n) {
-      const Part *x = part_at(n);
-      if (x == nullptr) break;
-      const int a = x->a, b = x->b, h = x->h, key = x->key, ends = last_keys(x);
-      done_with_part(n);
-#pragma unroll 1
-      for (int i = a; i < b; ++i, ++g) {
-        const int at = g & 1;
-        if (g >= 2 && !wait(&sh.pv_done[at], ((g - 2) >> 1) & 1)) break;
-        unsigned char *const to = smem + kOffV + at * kTileBytes;
-#ifdef HEART_TEST_HOOKS
-        if (!(p.test_skip && blockIdx.x == 0 && g == 1))
-#endif
-        load_tile(to, &map_v, &sh.v_full[at], key + i * kKeyStep, h);
-        const int keys = i == b - 1 ? ends : kKeyStep;
-        if ((keys & 15) || keys == 0) {  // rows that a product reads behind the last key
-          if (!wait(&sh.v_full[at], (g >> 1) & 1)) {
-            ++g;
-            break;
-          }
-          const int out = keys == 0 ? 16 : 16 - (keys & 15);
-          for (int j = lane; j < out * 16; j += 32)
-            sts_u4(smem_u32(to) + ((j >> 3) & 1) * (kTileBytes / 2) + (keys + (j >> 4)) * 128 + (j & 7) * 16, make_uint4(0u, 0u, 0u, 0u));
-          async_proxy_fence();
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.v_ready[at]);
-      }
-    }
-    if (*abort) settle_pair(sh.v_full, g);
-  } else if (warp == kWarpQK) {
-    // ===== issuer of the score products
-    const uint64_t q_desc = smem_desc_sw128(smem_u32(smem + kOffQ), 16, 1024);
-    const uint64_t k_desc = smem_desc_sw128(smem_u32(smem + kOffK), 16, 1024);
-    const bool leader = elect_one();
-    uint32_t g = 0;
-#pragma unroll 1
-    for (int n = 0; ok; ++n) {
-      const Part *x = part_at(n);
-      if (x == nullptr) break;
-      const int n_steps = x->b - x->a, ends = last_keys(x);
-      done_with_part(n);
-      wait(&sh.q_full[n & 1], (n >> 1) & 1);
-      const uint64_t qd = desc_at(q_desc, (n & 1) * (kTileBytes >> 4));
-#pragma unroll 1
-      for (int i = 0; i < n_steps; ++i, ++g) {  // S_g = Q K_g^T
-        const uint32_t b = g & 1;
-        if (g >= 2) wait(&sh.s_free[b], ((g - 2) >> 1) & 1);
-        if (!wait(&sh.k_full[b], (g >> 1) & 1)) break;
-        tc_fence_after();
-        if (leader) {
-          const uint64_t kd = desc_at(k_desc, b * (kTileBytes >> 4));
-          const int keys = i == n_steps - 1 ? max((ends + 15) & ~15, 16) : kKeyStep;
-          const uint32_t idesc = idesc_bf16_f32(128, 0, false, false) | (uint32_t)(keys >> 3) << 17;
-#pragma unroll
-          for (int ks = 0; ks < 8; ++ks)
-            mma_ss(tmem + 128 + b * 128, desc_at(qd, (ks >> 2) * 1024 + (ks & 3) * 2), desc_at(kd, (ks >> 2) * 1024 + (ks & 3) * 2), idesc, ks > 0 ? 1u : 0u);
-          tc_commit(&sh.s_full[b]);
-        }
-        __syncwarp();
-      }
-    }
-    drain_products(leader, &sh.drain[0]);
-  } else if (warp == kWarpPV) {
-    // ===== issuer of the value products
-    constexpr uint32_t idesc = idesc_bf16_f32(128, 128, false, true);
-    const uint64_t v_desc = smem_desc_sw128(smem_u32(smem + kOffV), kTileBytes / 2, 1024);
-    const bool leader = elect_one();
-    uint32_t g = 0;
-#pragma unroll 1
-    for (int n = 0; ok; ++n) {
-      const Part *x = part_at(n);
-      if (x == nullptr) break;
-      const int n_steps = x->b - x->a, ends = last_keys(x);
-      done_with_part(n);
-      if (n > 0) wait(&sh.o_free, (n - 1) & 1);
-#pragma unroll 1
-      for (int i = 0; i < n_steps; ++i, ++g) {  // O (+)= P_g V_g
-        const uint32_t b = g & 1;
-        wait(&sh.v_full[b], (g >> 1) & 1);
-        wait(&sh.v_ready[b], (g >> 1) & 1);
-        if (!wait(&sh.p_full[b], (g >> 1) & 1)) break;
-        tc_fence_after();
-        if (leader) {
-          const uint64_t vd = desc_at(v_desc, b * (kTileBytes >> 4));
-          const int ks_end = i == n_steps - 1 ? max((ends + 15) >> 4, 1) : 8;
-          if (ks_end == 8) {
-#pragma unroll
-            for (int ks = 0; ks < 8; ++ks) mma_ts(tmem, tmem + 384 + b * 64 + ks * 8, desc_at(vd, ks * 128), idesc, (i > 0 || ks > 0) ? 1u : 0u);
-          } else {
-#pragma unroll 1
-            for (int ks = 0; ks < ks_end; ++ks) mma_ts(tmem, tmem + 384 + b * 64 + ks * 8, desc_at(vd, ks * 128), idesc, (i > 0 || ks > 0) ? 1u : 0u);
-          }
-          if (i == n_steps - 1) tc_commit(&sh.o_full[n & 1]);
-          tc_commit(&sh.pv_done[b]);
-        }
-        __syncwarp();
-      }
-    }
-    drain_products(leader, &sh.drain[1]);
-  } else if (warp >= kWarpOut) {
     // ===== output: thread = one row
+    setmaxnreg_dec<kRegsOut>();
     const uint32_t quarter = warp & 3;
     const int row = quarter * 32 + lane;
     const uint32_t o_addr = tmem + (quarter << 21);
-    const int token = (int)(((uint32_t)row * p.inv_G) >> 16);
-    uint32_t g_end = 0, n_stored = 0;
+    const uint32_t stage_at = smem_u32(smem + kOffStage) + row * 128;
+    uint32_t n_stored = 0, n_staged = 0;
+    auto load = [&](uint32_t (&v)[32], int quad) {
+      tmem_ld32(o_addr + quad * 32, v);
+      tmem_wait_ld();
+    };
+    auto loaded = [&]() {
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.o_free);
+    };
+    // 32 dims of the row as bf16, O / l, and into shared memory
+    auto pack = [&](const uint32_t (&v)[32], float inv, uint32_t (&y)[16]) {
+      const uint64_t inv2 = pack_f32x2(inv, inv);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        float a0, a1;
+        unpack_f32x2(mul_f32x2(pack_f32x2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), inv2), a0, a1);
+        y[i] = pack_bf16x2(a0, a1);
+      }
+    };
+    auto stage = [&](const uint32_t (&y)[16], int quad) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        sts_u4(stage_at + (quad >> 1) * (kTileBytes / 2) + ((((quad & 1) * 4 + i ^ lane) & 7) << 4), make_uint4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]));
+    };
+    auto stage_free = [&]() {  // once the tile before has left
+      if (n_staged == 0) return true;
+      if (quarter == 0 && lane == 0) {
+        bulk_wait_read();
+        mbar_arrive(&sh.stage_free);
+      }
+      __syncwarp();
+      return wait(&sh.stage_free, (n_staged - 1) & 1);
+    };
 #pragma unroll 1
     for (int n = 0; ok; ++n) {
       const Part *x = part_at(n);
       if (x == nullptr) break;
-      const int n_steps = x->b - x->a, n_rows = x->tokens * p.G, c0 = x->c0, parts = x->parts, first_row = x->row, h = x->h;
-      const bool all = n_steps == x->steps, begins = x->a == 0;
-      done_with_part(n);
-      g_end += n_steps;
+      const bool all = x->b - x->a == x->steps;
       if (!wait(&sh.o_full[n & 1], (n >> 1) & 1)) break;
       tc_fence_after();
-      const uint32_t w_last = (g_end - 1) & 1;
-      const float2 last = sh.l[n & 3][w_last][row];
-      float l = last.x, m = last.y;
-      if (n_steps > 1) {
-        const float2 other = sh.l[n & 3][w_last ^ 1][row];
-        l += other.x * ex2(other.y - m);
-      }
-      uint16_t *const o_row = p.O + (long long)(first_row + token) * p.qt + (long long)(h * p.G + row - token * p.G) * p.qh;
-      const bool real = row < n_rows;
-      auto write32 = [&](const uint32_t (&v)[32], int d, float inv) {
-        const uint64_t inv2 = pack_f32x2(inv, inv);
+      if (__builtin_expect(all, 1)) {
+        const float inv = sh.l[n & 1][row];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.l_read[n & 1]);
+        uint32_t v[32], y[4][16];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          uint32_t y[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            float a0, a1;
-            unpack_f32x2(mul_f32x2(pack_f32x2(__uint_as_float(v[k * 16 + 2 * i]), __uint_as_float(v[k * 16 + 2 * i + 1])), inv2), a0, a1);
-            y[i] = pack_bf16x2(a0, a1);
-          }
-          if (real) store32(o_row + d + k * 16, y, p.wide);
+        for (int quad = 0; quad < 4; ++quad) {
+          load(v, quad);
+          if (quad == 3) loaded();
+          pack(v, inv, y[quad]);
         }
-      };
-      const int slot = 2 * blockIdx.x + (begins ? 1 : 0);
-      float inv = l == 0.f ? 0.f : 1.f / l;
+        if (!stage_free()) break;
+#pragma unroll
+        for (int quad = 0; quad < 4; ++quad) stage(y[quad], quad);
+      } else {
+        // part of a shared tile: its sums to the workspace (the row sums are there), and if it is the last one, those of all put together
+        if (lane == 0) mbar_arrive(&sh.l_read[n & 1]);
+        const bool real = row < x->tokens * p.G;
+        const int slot = 2 * blockIdx.x + (x->a == 0 ? 1 : 0);
 #pragma unroll 1
-      for (int c = 0; c < 4; ++c) {
-        uint32_t v[32];
-        tmem_ld32(o_addr + c * 32, v);
-        tmem_wait_ld();
-        if (c == 3) {
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&sh.o_free);
-        }
-        if (all) {
-          write32(v, c * 32, inv);
-        } else if (real) {
+        for (int d = 0; d < 128; d += 32) {
+          uint32_t v[32];
+          load(v, d >> 5);
+          if (d == 96) loaded();
+          float4 *const to = &p.parts[(size_t)(slot * 32 + (d >> 2)) * 128 + row];
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            __stcg(&p.parts[((size_t)slot * 32 + c * 8 + i) * 128 + row],
-                   make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3])));
+          for (int k = 0; k < 8; ++k)
+            if (real)
+              __stcg(to + k * 128, make_float4(__uint_as_float(v[4 * k]), __uint_as_float(v[4 * k + 1]), __uint_as_float(v[4 * k + 2]), __uint_as_float(v[4 * k + 3])));
         }
-      }
-      bool write = all;
-      if (!all) {
-        if (real) __stcg(&p.part_l[slot * 128 + row], make_float2(l, m));
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.stored);
         if (quarter == 0) {
           if (!wait(&sh.stored, n_stored & 1)) break;
           if (lane == 0) {
-            __threadfence();  // (of what the warpgroup has stored, which the barrier has shown this thread)
-            const bool is_last = atomicAdd(&p.arrivals[c0], 1) == parts - 1;
-            if (is_last) p.arrivals[c0] = 0;
+            __threadfence();  // (of what the CTA has stored, which the barriers have shown this thread)
+            const bool is_last = atomicAdd(&p.arrivals[x->c0], 1) == x->parts - 1;
+            if (is_last) p.arrivals[x->c0] = 0;
             sh.last = is_last;
             ++sh.shared_parts;
             __threadfence();
@@ -559,45 +427,264 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (!wait(&sh.told, n_stored & 1)) break;
         ++n_stored;
-        write = sh.last != 0;
-        if (write && real) {
-          auto place = [&](int i) { return 2 * (c0 + i) + (i == 0 ? 1 : 0); };
-          m = kNoReference;
-          l = 0.f;
-#pragma unroll 4
-          for (int i = 0; i < parts; ++i) m = fmaxf(m, __ldcg(&p.part_l[place(i) * 128 + row]).y);
-#pragma unroll 4
-          for (int i = 0; i < parts; ++i) {
-            const float2 lm = __ldcg(&p.part_l[place(i) * 128 + row]);
-            l = fmaf(lm.x, ex2(lm.y - m), l);
-          }
-          inv = l == 0.f ? 0.f : 1.f / l;
+        if (sh.last == 0) {
+          done_with_part(n);
+          continue;
+        }
+        auto place = [&](int i) { return 2 * (x->c0 + i) + (i == 0 ? 1 : 0); };
+        float m = kNoReference, l = 0.f;
 #pragma unroll 1
-          for (int c = 0; c < 4; ++c) {
-            uint32_t v[32];
-#pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = 0u;
+        for (int k = 0; k < x->parts; ++k) {
+          const float2 lm = __ldcg(&p.part_l[place(k) * 128 + row]);
+          const float top = fmaxf(m, lm.y);
+          l = fmaf(l, ex2(m - top), lm.x * ex2(lm.y - top));
+          m = top;
+        }
+        if (!stage_free()) break;
 #pragma unroll 1
-            for (int i = 0; i < parts; ++i) {
-              const float f = ex2(__ldcg(&p.part_l[place(i) * 128 + row]).y - m);
-              const float4 *src = &p.parts[((size_t)place(i) * 32 + c * 8) * 128 + row];
-              float4 y[8];
+        for (int quad = 0; quad < 4; ++quad) {
+          uint32_t v[32], y[16];
 #pragma unroll
-              for (int k = 0; k < 8; ++k) y[k] = __ldcg(src + k * 128);
+          for (int k = 0; k < 32; ++k) v[k] = 0u;
+#pragma unroll 1
+          for (int k = 0; k < x->parts; ++k) {
+            const int at = place(k);
+            const float f = ex2(__ldcg(&p.part_l[at * 128 + row]).y - m);
+            const float4 *src = &p.parts[(size_t)(at * 32 + quad * 8) * 128 + row];
+            float4 z[8];
 #pragma unroll
-              for (int k = 0; k < 8; ++k) {
-                v[4 * k] = __float_as_uint(fmaf(y[k].x, f, __uint_as_float(v[4 * k])));
-                v[4 * k + 1] = __float_as_uint(fmaf(y[k].y, f, __uint_as_float(v[4 * k + 1])));
-                v[4 * k + 2] = __float_as_uint(fmaf(y[k].z, f, __uint_as_float(v[4 * k + 2])));
-                v[4 * k + 3] = __float_as_uint(fmaf(y[k].w, f, __uint_as_float(v[4 * k + 3])));
-              }
+            for (int j = 0; j < 8; ++j) z[j] = __ldcg(src + j * 128);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              v[4 * j] = __float_as_uint(fmaf(z[j].x, f, __uint_as_float(v[4 * j])));
+              v[4 * j + 1] = __float_as_uint(fmaf(z[j].y, f, __uint_as_float(v[4 * j + 1])));
+              v[4 * j + 2] = __float_as_uint(fmaf(z[j].z, f, __uint_as_float(v[4 * j + 2])));
+              v[4 * j + 3] = __float_as_uint(fmaf(z[j].w, f, __uint_as_float(v[4 * j + 3])));
             }
-            write32(v, c * 32, inv);
           }
+          pack(v, l == 0.f ? 0.f : 1.f / l, y);
+          stage(y, quad);
+        }
+        if (real && p.lse != nullptr) *lse_of(x, row) = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+      }
+      async_proxy_fence();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.staged);
+      const bool whole_tile = x->tokens == tokens_per_tile;
+      if (quarter == 0) {
+        if (!wait(&sh.staged, n_staged & 1)) break;
+        if (lane == 0 && whole_tile) {
+          tma_store_5d(&map_o, smem + kOffStage, 0, 0, x->row, 0, x->h);
+          tma_store_5d(&map_o, smem + kOffStage + kTileBytes / 2, 0, 0, x->row, 1, x->h);
+        }
+        __syncwarp();
+      }
+      ++n_staged;
+      if (__builtin_expect(!whole_tile, 0)) {  // the rows that there are, two at a time, 16 lanes each
+        uint16_t *const to = p.O + (long long)x->row * p.qt + (long long)(x->h * p.G) * p.qh + (lane & 15) * 8;
+        const uint32_t from = smem_u32(smem + kOffStage) + ((lane & 15) >> 3) * (kTileBytes / 2);
+#pragma unroll 1
+        for (int r = (int)quarter * 32 + (lane >> 4); r < min(x->tokens * p.G, (int)quarter * 32 + 32); r += 2) {
+          const int t = (int)(((uint32_t)r * p.inv_G) >> 16);
+          *reinterpret_cast<uint4 *>(to + (long long)t * p.qt + (long long)(r - t * p.G) * p.qh) = lds_u4(from + r * 128 + (((lane ^ r) & 7) << 4));
         }
       }
-      if (write && real && p.lse != nullptr)
-        p.lse[(long long)(first_row + token) * p.Hq + h * p.G + row - token * p.G] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+      done_with_part(n);
+    }
+    if (quarter == 0 && lane == 0) bulk_wait_read();
+  } else if (warp >= kWarpQK) {
+    setmaxnreg_dec<kRegsHelper>();
+    if (warp == kWarpK) {
+      // ===== the CTA's parts; K and Q producer
+      {
+        auto upto_lane = [&](long long x) {  // inclusive, over the warp
+#pragma unroll 1
+          for (int o = 1; o < 32; o <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, x, o);
+            if (lane >= o) x += y;
+          }
+          return x;
+        };
+        Walk &w = sh.walk;
+        long long total = 0;
+        int longest = 1;
+#pragma unroll 1
+        for (int i = lane; i < n_chunks; i += 32) {
+          total += chunks[i].line;
+          longest = max(longest, chunks[i].longest);
+        }
+        total = __shfl_sync(0xffffffffu, upto_lane(total), 31);
+        longest = __reduce_max_sync(0xffffffffu, longest);
+        const bool whole = longest <= kWholeSteps + kTileCost;
+        const long long share = max(quotient(total + gridDim.x - 1, gridDim.x), whole ? 1LL : (long long)(longest + kMaxParts - 1) / kMaxParts);
+        const long long u = blockIdx.x * share, end = min(total, u + share);
+        long long before = 0;
+        int chunk = 0;
+        if (u < end) {  // the chunk in which the share begins
+          for (;; chunk += 32) {
+            const long long mine = chunk + lane < n_chunks ? chunks[chunk + lane].line : 0, upto = before + upto_lane(mine);
+            const uint32_t here = __ballot_sync(0xffffffffu, u < upto);
+            const int at = here ? __ffs(here) - 1 : 31;
+            before = __shfl_sync(0xffffffffu, here ? upto - mine : upto, at);
+            if (here) {
+              chunk += at;
+              break;
+            }
+          }
+        }
+        if (lane == 0) {
+          w.u = u;
+          w.end = end;
+          w.share = share;
+          w.whole = whole;
+          if (u < end) {
+            w.s = chunk * per_chunk - 1;
+            for (long long line = 0;; before += line) {
+              next_sequence(w);
+              line = (long long)w.tiles * (w.steps + kTileCost) * p.Hkv;
+              if (u < before + line) break;
+            }
+            const long long rest = u - before, at = quotient(rest, w.steps + kTileCost);  // tile of all heads
+            w.off = (int)(rest - at * (w.steps + kTileCost));
+            w.h = (int)quotient(at, w.tiles);
+            w.tile = (int)(at - (long long)w.h * w.tiles);
+          }
+        }
+        __syncwarp();
+      }
+      int g = 0, n = 0;
+#pragma unroll 1
+      for (;; ++n) {
+        if (n >= kPartRing) timed_wait(&sh.part_empty[n % kPartRing], (n / kPartRing - 1) & 1);
+        Part &x = ok ? sh.part[n % kPartRing] : sh.spare;  // (after an abort only what is owed is put down; this warp alone writes the ring)
+        if (lane == 0) {
+          if (next_part(sh.walk, x) && x.parts > 1) sh.owed[sh.n_owed++] = make_int4(2 * blockIdx.x + (x.a == 0 ? 1 : 0), x.c0, x.parts, 0);
+          if (ok) mbar_arrive(&sh.part_full[n % kPartRing]);
+        }
+        __syncwarp();
+        const int a = x.a, b = x.b, h = x.h, key = x.key, row = x.row;
+        if (b < 0) break;
+#pragma unroll 1
+        for (int i = a; ok && i < b; ++i, ++g) {
+          if (g >= 2 && !timed_wait(&sh.s_full[g & 1], ((g - 2) >> 1) & 1)) break;
+          load_tile(smem + kOffK + (g & 1) * kTileBytes, &map_k, &sh.k_full[g & 1], key + i * kKeyStep, h);
+          if (i == a && lane == 0) {  // (the scores of step g - 2 are complete, and with them those of part n - 2: its Q has been read)
+            unsigned char *q = smem + kOffQ + (n & 1) * kTileBytes;
+            mbar_expect_tx(&sh.q_full[n & 1], 2 * (128 / p.G * p.G) * 128);
+            tma_load_5d(q, &map_q, &sh.q_full[n & 1], 0, 0, row, 0, h);
+            tma_load_5d(q + kTileBytes / 2, &map_q, &sh.q_full[n & 1], 0, 0, row, 1, h);
+          }
+          __syncwarp();
+        }
+      }
+      if (ok) timed_wait(&sh.finished, 0);
+      if (*abort) {
+        settle_pair(sh.k_full, g);
+        settle(&sh.q_full[0], 0), settle(&sh.q_full[0], 1);  // (one of the two is past)
+        settle(&sh.q_full[1], 0), settle(&sh.q_full[1], 1);
+      }
+    } else if (warp == kWarpV) {
+      // ===== V producer
+      int g = 0;
+      uint32_t tails = 0;
+#pragma unroll 1
+      for (int n = 0; ok; ++n) {
+        const Part *x = part_at(n);
+        if (x == nullptr) break;
+        const int a = x->a, b = x->b, h = x->h, key = x->key, ends = last_keys(x);
+        done_with_part(n);
+#pragma unroll 1
+        for (int i = a; i < b; ++i, ++g) {
+          const int at = g & 1;
+          if (g >= 2 && !wait(&sh.pv_done[at], ((g - 2) >> 1) & 1)) break;
+          unsigned char *const to = smem + kOffV + at * kTileBytes;
+          const int keys = i == b - 1 ? ends : kKeyStep;
+          const bool tail = (keys & 15) || keys == 0;
+#ifdef HEART_TEST_HOOKS
+          if (!(p.test_skip && blockIdx.x == 0 && g == 1))
+#endif
+          load_tile(to, &map_v, tail ? &sh.v_tail : &sh.v_full[at], key + i * kKeyStep, h);
+          if (tail) {  // rows that a product reads behind the last key
+            if (!wait(&sh.v_tail, tails & 1)) break;
+            ++tails;
+            const int out = keys == 0 ? 16 : 16 - (keys & 15);
+#pragma unroll 1
+            for (int j = lane; j < out * 16; j += 32)
+              sts_u4(smem_u32(to) + ((j >> 3) & 1) * (kTileBytes / 2) + (keys + (j >> 4)) * 128 + (j & 7) * 16, make_uint4(0u, 0u, 0u, 0u));
+            async_proxy_fence();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.v_full[at]);
+          }
+          __syncwarp();
+        }
+      }
+      if (*abort) {
+        settle_pair(sh.v_full, g);
+        settle(&sh.v_tail, tails & 1);
+      }
+    } else if (warp == kWarpQK) {
+      // ===== issuer of the score products
+      const uint64_t q_desc = smem_desc_sw128(smem_u32(smem + kOffQ), 16, 1024);
+      const uint64_t k_desc = smem_desc_sw128(smem_u32(smem + kOffK), 16, 1024);
+      const bool leader = elect_one();
+      uint32_t g = 0;
+#pragma unroll 1
+      for (int n = 0; ok; ++n) {
+        const Part *x = part_at(n);
+        if (x == nullptr) break;
+        const int n_steps = x->b - x->a, ends = last_keys(x);
+        done_with_part(n);
+        wait(&sh.q_full[n & 1], (n >> 1) & 1);
+        const uint64_t qd = desc_at(q_desc, (n & 1) * (kTileBytes >> 4));
+#pragma unroll 1
+        for (int i = 0; i < n_steps; ++i, ++g) {  // S_g = Q K_g^T
+          const uint32_t b = g & 1;
+          if (!wait2(&sh.s_free[b], ((g - 2) >> 1) & 1, &sh.k_full[b], (g >> 1) & 1)) break;  // (the phase before the first one counts as past)
+          tc_fence_after();
+          if (leader) {
+            const uint64_t kd = desc_at(k_desc, b * (kTileBytes >> 4));
+            const int keys = i == n_steps - 1 ? max((ends + 15) & ~15, 16) : kKeyStep;
+            const uint32_t idesc = idesc_bf16_f32(128, 0, false, false) | (uint32_t)(keys >> 3) << 17;
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks)
+              mma_ss(tmem + 128 + b * 128, desc_at(qd, (ks >> 2) * 1024 + (ks & 3) * 2), desc_at(kd, (ks >> 2) * 1024 + (ks & 3) * 2), idesc, ks > 0 ? 1u : 0u);
+            tc_commit(&sh.s_full[b]);
+          }
+          __syncwarp();
+        }
+      }
+      drain_products(leader, &sh.drain[0]);
+    } else if (warp == kWarpPV) {
+      // ===== issuer of the value products
+      constexpr uint32_t idesc = idesc_bf16_f32(128, 128, false, true);
+      const uint64_t v_desc = smem_desc_sw128(smem_u32(smem + kOffV), kTileBytes / 2, 1024);
+      const bool leader = elect_one();
+      uint32_t g = 0;
+#pragma unroll 1
+      for (int n = 0; ok; ++n) {
+        const Part *x = part_at(n);
+        if (x == nullptr) break;
+        const int n_steps = x->b - x->a, ends = last_keys(x);
+        done_with_part(n);
+        if (n > 0) wait(&sh.o_free, (n - 1) & 1);
+#pragma unroll 1
+        for (int i = 0; i < n_steps; ++i, ++g) {  // O (+)= P_g V_g
+          const uint32_t b = g & 1;
+          if (!wait2(&sh.v_full[b], (g >> 1) & 1, &sh.p_full[b], (g >> 1) & 1)) break;
+          tc_fence_after();
+          if (leader) {
+            const uint64_t vd = desc_at(v_desc, b * (kTileBytes >> 4));
+            const int ks_end = i == n_steps - 1 ? max((ends + 15) >> 4, 1) : 8;
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks)
+              if (ks < ks_end) mma_ts(tmem, tmem + 384 + b * 64 + ks * 8, desc_at(vd, ks * 128), idesc, (i > 0 || ks > 0) ? 1u : 0u);
+            if (i == n_steps - 1) tc_commit(&sh.o_full[n & 1]);
+            tc_commit(&sh.pv_done[b]);
+          }
+          __syncwarp();
+        }
+      }
+      drain_products(leader, &sh.drain[1]);
     }
   } else {
     // ===== softmax: thread = one row; warpgroup w takes the steps g with g & 1 == w
@@ -618,21 +705,19 @@ __global__ void __launch_bounds__(kThreads, 1)
       const Part *x = part_at(n);
       if (x == nullptr) break;
       const int n_steps = x->b - x->a, ends = last_keys(x);
-      done_with_part(n);
       float m_ref = kNoReference, l_run = 0.f;
 #pragma unroll 1
       for (int h = (w ^ g0) & 1; h < n_steps; h += 2) {
         const uint32_t g = g0 + h;
-        if (g > 0 && !wait(&sh.m_ready[w ^ 1][quarter], ((g - 1) >> 1) & 1)) break;
-        if (!wait(&sh.s_full[w], (g >> 1) & 1)) break;
+        if (!wait2(&sh.m_ready[w ^ 1][quarter], ((g - 1) >> 1) & 1, &sh.s_full[w], (g >> 1) & 1)) break;  // (the phase before the first one counts as past)
         tc_fence_after();
-        const float m_prev = h > 0 ? sh.m[w ^ 1][row] : kNoReference;
+        const float m_prev = h > 0 ? sh.m[row] : kNoReference;
         bool moved = false;
         float alpha = 1.f;
         auto new_reference = [&](float x_max) -> bool {  // true: it has moved (some row's of the warp)
           const bool grow = x_max > m_ref + kMaxGrowth;
           const float m_new = grow ? x_max + kHeadroom : m_ref;
-          sh.m[w][row] = m_new;
+          sh.m[row] = m_new;
           __syncwarp();
           if (lane == 0) mbar_arrive(&sh.m_ready[w][quarter]);
           if (__builtin_expect(!__any_sync(0xffffffffu, grow), 1)) return false;
@@ -672,35 +757,31 @@ __global__ void __launch_bounds__(kThreads, 1)
           tmem_st32(p_at + 32, pk);
         } else {
           // 32 keys at a time: once for the maximum, once for the weights
-          uint32_t s[32], pk[16];
-          auto load = [&](int k0) {
-            tmem_ld32(s_at + k0, s);
-            tmem_wait_ld();
-            if (k0 + 32 > keys) {
-#pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (k0 + i >= keys) s[i] = 0xff800000u;
-            }
-          };
           l_run *= ex2(m_ref - m_prev);
           m_ref = m_prev;
           float x_max = -INFINITY;
-          const int end = max(keys, 1);
+          const int chunks = max((keys + 31) >> 5, 1);
 #pragma unroll 1
-          for (int k0 = 0; k0 < end; k0 += 32) {
-            load(k0);
+          for (int i = 0; i < 2 * chunks; ++i) {
+            const int k0 = (i < chunks ? i : i - chunks) * 32;
+            if (i == chunks) {
+              new_reference(x_max * c);
+              if (!wait(&sh.pv_done[w], ((g - 2) >> 1) & 1)) break;
+              tc_fence_after();
+            }
+            uint32_t s[32], pk[16];
+            tmem_ld32(s_at + k0, s);
+            tmem_wait_ld();
 #pragma unroll
-            for (int i = 0; i < 32; i += 2) x_max = fmax3(x_max, __uint_as_float(s[i]), __uint_as_float(s[i + 1]));
-          }
-          new_reference(x_max * c);
-          if (g >= 2 && !wait(&sh.pv_done[w], ((g - 2) >> 1) & 1)) break;
-          tc_fence_after();
-          const uint64_t neg_m2 = pack_f32x2(-m_ref, -m_ref);
-#pragma unroll 1
-          for (int k0 = 0; k0 < end; k0 += 32) {
-            load(k0);
-            exp32<false>(s, c2, neg_m2, pk, sums);
-            tmem_st16(p_at + (k0 >> 1), pk);
+            for (int j = 0; j < 32; ++j)
+              if (k0 + j >= keys) s[j] = 0xff800000u;
+            if (i < chunks) {
+#pragma unroll
+              for (int j = 0; j < 32; j += 2) x_max = fmax3(x_max, __uint_as_float(s[j]), __uint_as_float(s[j + 1]));
+            } else {
+              exp32<false>(s, c2, pack_f32x2(-m_ref, -m_ref), pk, sums);
+              tmem_st16(p_at + (k0 >> 1), pk);
+            }
           }
           arrive(&sh.s_free[w]);
         }
@@ -708,7 +789,28 @@ __global__ void __launch_bounds__(kThreads, 1)
         unpack_f32x2(sums[0], s0, s1);
         unpack_f32x2(sums[1], s2, s3);
         l_run += (s0 + s1) + (s2 + s3);
-        if (h >= n_steps - 2) sh.l[n & 3][w][row] = make_float2(l_run, m_ref);
+        if (h >= n_steps - 2) {  // the row sum, by way of the other warpgroup to those who write
+          const int at = n & 1;
+          const uint32_t phase = (n >> 1) & 1;
+          if ((h < n_steps - 1 || h == 0) && !wait(&sh.l_read[at], phase ^ 1)) break;  // (the first one's place has been free before)
+          if (h == n_steps - 1) {
+            float l = l_run;
+            if (h > 0) {
+              if (!wait(&sh.l_ready[at][quarter], phase)) break;
+              l = fmaf(sh.l[at][row], ex2(m_prev - m_ref), l);
+            }
+            if (__builtin_expect(x->b - x->a == x->steps, 1)) {
+              sh.l[at][row] = l == 0.f ? 0.f : 1.f / l;
+              if (p.lse != nullptr && row < x->tokens * p.G) *lse_of(x, row) = l == 0.f ? -INFINITY : (m_ref + log2f(l)) * 0.6931471805599453f;
+            } else {
+              __stcg(&p.part_l[(2 * blockIdx.x + (x->a == 0 ? 1 : 0)) * 128 + row], make_float2(l, m_ref));
+            }
+          } else {
+            sh.l[at][row] = l_run;
+          }
+          __syncwarp();
+          if (lane == 0 && (h < n_steps - 1 || h == 0)) mbar_arrive(&sh.l_ready[at][quarter]);
+        }
         if (!ok) break;
         if (__builtin_expect(moved && h > 0, 0)) {
           // O changes scale: the products of the steps before have to be complete
@@ -734,10 +836,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         arrive(&sh.p_full[w]);
       }
       g0 += n_steps;
+      done_with_part(n);
     }
   }
 
   // ------------------------------------------------------------------ tear-down
+  __syncwarp();
+  if (warp != kWarpK && lane == 0) mbar_arrive(&sh.finished);
   tc_fence_before();
   __syncthreads();
   if (warp == kWarpQK) {
@@ -746,15 +851,13 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   if (sh.abort && tid == 0) {
     atomicExch(ix.status, HEART_ERR_DEVICE_CHECK);
-    // what this CTA still owes to shared tiles: no numbers
-    walk_begins(sh.walk);
-    Part &x = sh.part[0];
-    for (int i = 0; next_part(sh.walk, x);) {
-      if (x.parts == 1 || i++ < sh.shared_parts) continue;
-      const int slot = 2 * blockIdx.x + (x.a == 0 ? 1 : 0);
-      for (int r = 0; r < 128; ++r) __stcg(&p.part_l[slot * 128 + r], make_float2(__uint_as_float(0x7fc00000u), 0.f));
+#pragma unroll 1
+    for (int i = sh.shared_parts; i < sh.n_owed; ++i) {  // what this CTA still owes to shared tiles: no numbers
+      const int4 x = sh.owed[i];
+#pragma unroll 1
+      for (int r = 0; r < 128; ++r) __stcg(&p.part_l[x.x * 128 + r], make_float2(__uint_as_float(0x7fc00000u), 0.f));
       __threadfence();
-      if (atomicAdd(&p.arrivals[x.c0], 1) == x.parts - 1) p.arrivals[x.c0] = 0;
+      if (atomicAdd(&p.arrivals[x.y], 1) == x.z - 1) p.arrivals[x.y] = 0;
     }
   }
 }
@@ -763,8 +866,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 cudaError_t launch_cross_tiles(const CrossGeom &g, const CacheIndex &ix, const CrossWorkspace &w, const void *Q, const void *K, const void *V, void *O,
                                float *lse, cudaStream_t s, int *launches) {
-  CUtensorMap mq, mk, mv;
-  if (!make_query_map(&mq, Q, g) || !make_states_map(&mk, K, g, kKeyStep) || !make_states_map(&mv, V, g, kKeyStep)) return cudaErrorInvalidValue;
+  CUtensorMap mq, mk, mv, mo;
+  if (!make_query_map(&mq, Q, g) || !make_query_map(&mo, O, g) || !make_states_map(&mk, K, g, kKeyStep) || !make_states_map(&mv, V, g, kKeyStep)) return cudaErrorInvalidValue;
   CrossParams p = {};
   p.ix = ix;
   p.arrivals = w.arrivals;
@@ -779,12 +882,11 @@ cudaError_t launch_cross_tiles(const CrossGeom &g, const CacheIndex &ix, const C
   p.G = g.G;
   p.inv_G = (65536u + g.G - 1) / g.G;
   p.scale_log2 = (float)(g.scale * 1.4426950408889634);
-  p.wide = (reinterpret_cast<uintptr_t>(O) & 31u) == 0 && g.qt % 16 == 0 && g.qh % 16 == 0;
   p.test_skip = g.test_skip;
   cudaError_t e = allow_shared_memory(cross_tile_kernel, kSmem);
   if (e != cudaSuccess) return e;
   ++*launches;
-  return launch_pdl(cross_tile_kernel, dim3(kCacheCtas), dim3(kThreads), kSmem, s, mq, mk, mv, p);
+  return launch_pdl(cross_tile_kernel, dim3(kCacheCtas), dim3(kThreads), kSmem, s, mq, mk, mv, mo, p);
 }
 
 }  // namespace heart
