@@ -8,8 +8,9 @@
 //     where bulk copies write them, while the others are in the next tile's first steps.  That has room for a whole tile, which the one before leaves
 //     meanwhile: stores of all SMs go at some 10 bytes a clock and SM, 3000 clocks a tile, and whoever waits for them (the warps where they store themselves, or a
 //     half that waits for the other's place) is late for the next tile's sums.  The room is found by putting the row sums in the place of the tile's Q.
-//   * A tile's last step may have fewer than 128 keys: the products are cut to the next 16 keys (columns of the scores, steps of the values' product),
-//     the softmax to the next 32; scores behind the last key become -inf, values of up to 15 rows behind it, which are anyone's, zeros in shared memory.
+//   * A tile's last step may have fewer than 128 keys: the products are cut to the next 16 keys (columns of the scores, steps of the values' product), the
+//     softmax of up to 32 to these; scores behind the last key become -inf in tensor memory, values of up to 15 rows behind it, which are
+//     anyone's, zeros in shared memory.  (By 32 keys at a time, twice, 12 heads x 32760 over 226 took 100 us, where 256 took 73.)
 //   * There is no plan: all tiles of a sequence take the same number of steps, so a CTA finds its share of the line of all tiles' steps, (sequence, head,
 //     tile, step), from the lengths alone, each beginning of a tile counted as kTileCost steps.
 //     Parts of a tile go to the workspace; the CTA that brings the last one puts them together, in order: the result does not depend on which one
@@ -729,7 +730,15 @@ __global__ void __launch_bounds__(kThreads, 1)
         };
         uint64_t sums[2] = {0ull, 0ull};
         const int keys = h == n_steps - 1 ? ends : kKeyStep;
-        if (keys == kKeyStep) {
+        if (__builtin_expect(keys > 32, 1)) {
+          if (__builtin_expect(keys < kKeyStep, 0)) {  // scores behind the last key
+            int k = keys;
+#pragma unroll 1
+            for (; k & 7; ++k) tmem_st1(s_at + k, 0xff800000u);
+#pragma unroll 1
+            for (; k < kKeyStep; k += 8) tmem_st8_fill(s_at + k, 0xff800000u);
+            tmem_wait_st();
+          }
           uint32_t s[128], pk[32];
 #pragma unroll
           for (int q = 0; q < 4; ++q) tmem_ld32(s_at + q * 32, *reinterpret_cast<uint32_t(*)[32]>(&s[q * 32]));
@@ -756,34 +765,23 @@ __global__ void __launch_bounds__(kThreads, 1)
           exp32<false>(&s[96], c2, neg_m2, &pk[16], sums);
           tmem_st32(p_at + 32, pk);
         } else {
-          // 32 keys at a time: once for the maximum, once for the weights
+          uint32_t s[32], pk[16];
+          tmem_ld32(s_at, s);
           l_run *= ex2(m_ref - m_prev);
           m_ref = m_prev;
-          float x_max = -INFINITY;
-          const int chunks = max((keys + 31) >> 5, 1);
-#pragma unroll 1
-          for (int i = 0; i < 2 * chunks; ++i) {
-            const int k0 = (i < chunks ? i : i - chunks) * 32;
-            if (i == chunks) {
-              new_reference(x_max * c);
-              if (!wait(&sh.pv_done[w], ((g - 2) >> 1) & 1)) break;
-              tc_fence_after();
-            }
-            uint32_t s[32], pk[16];
-            tmem_ld32(s_at + k0, s);
-            tmem_wait_ld();
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-              if (k0 + j >= keys) s[j] = 0xff800000u;
-            if (i < chunks) {
-#pragma unroll
-              for (int j = 0; j < 32; j += 2) x_max = fmax3(x_max, __uint_as_float(s[j]), __uint_as_float(s[j + 1]));
-            } else {
-              exp32<false>(s, c2, pack_f32x2(-m_ref, -m_ref), pk, sums);
-              tmem_st16(p_at + (k0 >> 1), pk);
-            }
-          }
+          tmem_wait_ld();
           arrive(&sh.s_free[w]);
+          float x_max = -INFINITY;
+#pragma unroll
+          for (int j = 0; j < 32; ++j) {
+            if (j >= keys) s[j] = 0xff800000u;
+            x_max = fmaxf(x_max, __uint_as_float(s[j]));
+          }
+          new_reference(x_max * c);
+          if (!wait(&sh.pv_done[w], ((g - 2) >> 1) & 1)) break;
+          tc_fence_after();
+          exp32<false>(s, c2, pack_f32x2(-m_ref, -m_ref), pk, sums);
+          tmem_st16(p_at, pk);
         }
         float s0, s1, s2, s3;
         unpack_f32x2(sums[0], s0, s1);
