@@ -43,22 +43,18 @@ constexpr float kNoReference = -3.0e38f;
 constexpr float kHeadroom = 16.f, kMaxGrowth = 8.f;  // see attn_tc.cu
 
 // Part of a tile that a CTA takes: steps a .. b - 1.
-struct Part {
-  int row, tokens, h;     // first packed row, tokens, key head
-  int key, len, steps;    // first row of its keys, how many, in steps
-  int a, b;               // b < 0: no part left
-  int c0, parts;          // first CTA with a part of the tile, and how many there are
-  int pad[2];
+struct alignas(16) Part {  // (written by fours)
+  int row, tokens, h, key;  // first packed row, tokens, key head, first row of its keys
+  int len, steps, a, b;     // keys of the tile, in steps; b < 0: no part left
+  int c0, parts, pad[2];    // first CTA with a part of the tile, and how many there are
 };
-static_assert(sizeof(Part) % 16 == 0, "copied by words");
 
 // Where a CTA is in the line of all tiles' costs.
 struct Walk {
   Sequence q;
-  int tiles, steps;         // of the sequence and a head, of a tile
-  int s, h, tile, off;      // off: what of the tile's cost lies before the share
-  long long u, end, share;  // of the line
-  bool whole;           // tiles are not shared: a CTA takes those that begin in its share
+  int tiles, steps;      // of the sequence and a head, of a tile
+  int s, h, tile, off;   // off: what of the tile's cost lies before the share
+  long long u, end;      // of the line
 };
 
 // Sequences in a row: the length of their line, the largest cost of a tile.
@@ -82,10 +78,8 @@ struct CrossShared {
   Part part[kPartRing];
   float m[128];            // references after the last step that has found them
   float l[2][128];         // of the row sums: the other warpgroup's part, then one over them, per part & 1
-  Walk walk;
   uint32_t tmem_base;
   int shared_parts;        // parts of shared tiles that have been announced
-  Part spare;
   int4 owed[2];            // this CTA's parts of shared tiles: place in the workspace, first CTA of the tile, number of its parts
   int n_owed;
   int last;
@@ -279,53 +273,6 @@ __global__ void __launch_bounds__(kThreads, 1)
       tma_load_5d(dst, map, bar, 0, row, 0, h, 0);
     }
   };
-  // ------------------------------------------------------------------ the CTA's parts, in order (by one thread, in shared memory)
-  auto next_sequence = [&](Walk &w) {
-    w.q = cross_sequence(ix, ++w.s);
-    w.tiles = tiles_of(w.q);
-    w.steps = steps_of(w.q);
-  };
-  auto walk_on = [&](Walk &w) {  // to the next tile, whose cost begins at u
-    w.off = 0;
-    if (++w.tile < w.tiles) return;
-    w.tile = 0;
-    if (++w.h < p.Hkv) return;
-    w.h = 0;
-#pragma unroll 1
-    do next_sequence(w);
-    while (w.tiles == 0 && w.s + 1 < ix.S);
-  };
-  auto next_part = [&](Walk &w, Part &x) {  // false: none left
-    x.b = -1;
-    if (w.u >= w.end) return false;  // (the rest of w is nothing where the CTA has no share)
-    if (w.whole && w.off > 0) {
-      w.u += w.steps + kTileCost - w.off;
-      if (w.u >= w.end) return false;
-      walk_on(w);
-    }
-    const int off = w.off, steps = w.steps, a = max(off - kTileCost, 0);
-    const int b = w.whole ? steps : (int)min((long long)steps, off + (w.end - w.u) - kTileCost);
-    if (b <= a) return false;  // (the share ends before the tile's first step)
-    x.row = w.q.row + w.tile * tokens_per_tile;
-    x.tokens = min(tokens_per_tile, w.q.n - w.tile * tokens_per_tile);
-    x.h = w.h;
-    x.key = w.q.key;
-    x.len = w.q.len;
-    x.steps = steps;
-    x.a = a;
-    x.b = b;
-    x.c0 = blockIdx.x;
-    x.parts = 1;
-    if (b - a < steps) {
-      const long long first = w.u - off + kTileCost;
-      x.c0 = (int)quotient(first, w.share);
-      x.parts = (int)quotient(first + steps - 1, w.share) - x.c0 + 1;
-    }
-    w.u += b + kTileCost - off;
-    if (w.u < w.end) walk_on(w);
-    return true;
-  };
-
   auto lse_of = [&](const Part *x, int row) {
     const int t = (int)(((uint32_t)row * p.inv_G) >> 16);
     return p.lse + (long long)(x->row + t) * p.Hq + x->h * p.G + row - t * p.G;
@@ -497,6 +444,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     setmaxnreg_dec<kRegsHelper>();
     if (warp == kWarpK) {
       // ===== the CTA's parts; K and Q producer
+      Walk w = {};
+      long long share;
+      bool whole;  // tiles are not shared: a CTA takes those that begin in its share
+      auto next_sequence = [&]() {
+        w.q = cross_sequence(ix, ++w.s);
+        w.tiles = tiles_of(w.q);
+        w.steps = steps_of(w.q);
+      };
       {
         auto upto_lane = [&](long long x) {  // inclusive, over the warp
 #pragma unroll 1
@@ -506,7 +461,6 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           return x;
         };
-        Walk &w = sh.walk;
         long long total = 0;
         int longest = 1;
 #pragma unroll 1
@@ -516,15 +470,16 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         total = __shfl_sync(0xffffffffu, upto_lane(total), 31);
         longest = __reduce_max_sync(0xffffffffu, longest);
-        const bool whole = longest <= kWholeSteps + kTileCost;
-        const long long share = max(quotient(total + gridDim.x - 1, gridDim.x), whole ? 1LL : (long long)(longest + kMaxParts - 1) / kMaxParts);
-        const long long u = blockIdx.x * share, end = min(total, u + share);
-        long long before = 0;
-        int chunk = 0;
-        if (u < end) {  // the chunk in which the share begins
+        whole = longest <= kWholeSteps + kTileCost;
+        share = max(quotient(total + gridDim.x - 1, gridDim.x), whole ? 1LL : (long long)(longest + kMaxParts - 1) / kMaxParts);
+        w.u = blockIdx.x * share;
+        w.end = min(total, w.u + share);
+        if (w.u < w.end) {  // the chunk in which the share begins, then the sequence (all lanes alike)
+          long long before = 0;
+          int chunk = 0;
           for (;; chunk += 32) {
             const long long mine = chunk + lane < n_chunks ? chunks[chunk + lane].line : 0, upto = before + upto_lane(mine);
-            const uint32_t here = __ballot_sync(0xffffffffu, u < upto);
+            const uint32_t here = __ballot_sync(0xffffffffu, w.u < upto);
             const int at = here ? __ffs(here) - 1 : 31;
             before = __shfl_sync(0xffffffffu, here ? upto - mine : upto, at);
             if (here) {
@@ -532,51 +487,94 @@ __global__ void __launch_bounds__(kThreads, 1)
               break;
             }
           }
-        }
-        if (lane == 0) {
-          w.u = u;
-          w.end = end;
-          w.share = share;
-          w.whole = whole;
-          if (u < end) {
-            w.s = chunk * per_chunk - 1;
-            for (long long line = 0;; before += line) {
-              next_sequence(w);
-              line = (long long)w.tiles * (w.steps + kTileCost) * p.Hkv;
-              if (u < before + line) break;
-            }
-            const long long rest = u - before, at = quotient(rest, w.steps + kTileCost);  // tile of all heads
-            w.off = (int)(rest - at * (w.steps + kTileCost));
-            w.h = (int)quotient(at, w.tiles);
-            w.tile = (int)(at - (long long)w.h * w.tiles);
+          w.s = chunk * per_chunk - 1;
+          for (long long line = 0;; before += line) {
+            next_sequence();
+            line = (long long)w.tiles * (w.steps + kTileCost) * p.Hkv;
+            if (w.u < before + line) break;
+          }
+          const long long rest = w.u - before, at = quotient(rest, w.steps + kTileCost);  // tile of all heads
+          w.off = (int)(rest - at * (w.steps + kTileCost));
+          w.h = (int)quotient(at, w.tiles);
+          w.tile = (int)(at - (long long)w.h * w.tiles);
+          if (whole && w.off > 0) {
+            w.u += w.steps + kTileCost - w.off;
+            ++w.tile;
+            w.off = 0;
           }
         }
-        __syncwarp();
       }
-      int g = 0, n = 0;
+      // Part n + 1 is announced with the first step of part n, and its Q brought to L2: it comes from memory, in 3000 clocks, and copies behind it would wait as long.
+      // (Little code for a tile like the one before, in registers: K waits for it.  By one thread from shared memory it took 2400 clocks, and 12 heads x 32760 over 512
+      // 112 us.)  n = -1: no steps.
+      int g = 0, a = 0, b = 1, h = 0, key = 0, row = 0;
 #pragma unroll 1
-      for (;; ++n) {
-        if (n >= kPartRing) timed_wait(&sh.part_empty[n % kPartRing], (n / kPartRing - 1) & 1);
-        Part &x = ok ? sh.part[n % kPartRing] : sh.spare;  // (after an abort only what is owed is put down; this warp alone writes the ring)
-        if (lane == 0) {
-          if (next_part(sh.walk, x) && x.parts > 1) sh.owed[sh.n_owed++] = make_int4(2 * blockIdx.x + (x.a == 0 ? 1 : 0), x.c0, x.parts, 0);
-          if (ok) mbar_arrive(&sh.part_full[n % kPartRing]);
-        }
-        __syncwarp();
-        const int a = x.a, b = x.b, h = x.h, key = x.key, row = x.row;
-        if (b < 0) break;
+      for (int n = -1; b >= 0; ++n) {
+        int next_a = 0, next_b = 0, next_h = 0, next_key = 0, next_row = 0;
 #pragma unroll 1
-        for (int i = a; ok && i < b; ++i, ++g) {
-          if (g >= 2 && !timed_wait(&sh.s_full[g & 1], ((g - 2) >> 1) & 1)) break;
-          load_tile(smem + kOffK + (g & 1) * kTileBytes, &map_k, &sh.k_full[g & 1], key + i * kKeyStep, h);
-          if (i == a && lane == 0) {  // (the scores of step g - 2 are complete, and with them those of part n - 2: its Q has been read)
-            unsigned char *q = smem + kOffQ + (n & 1) * kTileBytes;
-            mbar_expect_tx(&sh.q_full[n & 1], 2 * (128 / p.G * p.G) * 128);
-            tma_load_5d(q, &map_q, &sh.q_full[n & 1], 0, 0, row, 0, h);
-            tma_load_5d(q + kTileBytes / 2, &map_q, &sh.q_full[n & 1], 0, 0, row, 1, h);
+        for (int i = a; i < b; ++i) {
+          if (n >= 0 && ok && (g < 2 || timed_wait(&sh.s_full[g & 1], ((g - 2) >> 1) & 1))) {
+            load_tile(smem + kOffK + (g & 1) * kTileBytes, &map_k, &sh.k_full[g & 1], key + i * kKeyStep, h);
+            if (i == a && lane == 0) {  // (the scores of step g - 2 are complete, and with them those of part n - 2: its Q has been read)
+              unsigned char *q = smem + kOffQ + (n & 1) * kTileBytes;
+              mbar_expect_tx(&sh.q_full[n & 1], 2 * (128 / p.G * p.G) * 128);
+              tma_load_5d(q, &map_q, &sh.q_full[n & 1], 0, 0, row, 0, h);
+              tma_load_5d(q + kTileBytes / 2, &map_q, &sh.q_full[n & 1], 0, 0, row, 1, h);
+            }
+            ++g;
+            __syncwarp();
           }
-          __syncwarp();
+          if (i == a) {
+            const int m = n + 1;
+            if (ok && m >= kPartRing) timed_wait(&sh.part_empty[m % kPartRing], (m / kPartRing - 1) & 1);
+            // the tile at u
+            next_b = -1;
+            if (w.u < w.end) {
+              if (__builtin_expect(w.tile == w.tiles, 0)) {
+                w.tile = 0;
+                if (++w.h == p.Hkv) {
+                  w.h = 0;
+#pragma unroll 1
+                  do next_sequence();
+                  while (w.tiles == 0 && w.s + 1 < ix.S);
+                }
+              }
+              next_a = 0, next_b = w.steps, next_h = w.h, next_key = w.q.key, next_row = w.q.row + w.tile * tokens_per_tile;
+              int c0 = blockIdx.x, parts = 1;
+              const long long tile_at = w.u - w.off;
+              if (__builtin_expect(!whole && (w.off > 0 || w.end - w.u < w.steps + kTileCost), 0)) {
+                next_a = max(w.off - kTileCost, 0);
+                next_b = (int)min((long long)w.steps, w.end - tile_at - kTileCost);
+                if (next_b - next_a < w.steps) {
+                  c0 = (int)quotient(tile_at + kTileCost, share);
+                  parts = (int)quotient(tile_at + kTileCost + w.steps - 1, share) - c0 + 1;
+                }
+                if (next_b <= next_a) next_b = -1;  // (the share ends before the tile's first step)
+              }
+              w.u = next_b < 0 ? w.end : tile_at + kTileCost + next_b;
+              w.off = 0;
+              if (lane == 0 && next_b >= 0) {
+                if (parts > 1) sh.owed[sh.n_owed++] = make_int4(2 * blockIdx.x + (next_a == 0 ? 1 : 0), c0, parts, 0);
+                if (ok) {
+                  int4 *const x = reinterpret_cast<int4 *>(&sh.part[m % kPartRing]);
+                  x[0] = make_int4(next_row, min(tokens_per_tile, w.q.n - w.tile * tokens_per_tile), next_h, next_key);
+                  x[1] = make_int4(w.q.len, w.steps, next_a, next_b);
+                  x[2] = make_int4(c0, parts, 0, 0);
+                  tma_prefetch_5d(&map_q, 0, 0, next_row, 0, next_h);
+                  tma_prefetch_5d(&map_q, 0, 0, next_row, 1, next_h);
+                }
+              }
+              ++w.tile;
+            }
+            if (lane == 0 && ok) {  // (after an abort only what is owed is put down)
+              if (next_b < 0) sh.part[m % kPartRing].b = -1;
+              mbar_arrive(&sh.part_full[m % kPartRing]);
+            }
+            __syncwarp();
+          }
+          if (!ok) break;
         }
+        a = next_a, b = next_b, h = next_h, key = next_key, row = next_row;
       }
       if (ok) timed_wait(&sh.finished, 0);
       if (*abort) {
