@@ -873,12 +873,12 @@ bool make_pool_map(CUtensorMap *m, const void *base, const CacheGeom &g, int row
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-bool make_states_map(CUtensorMap *m, const void *base, const CrossGeom &g, int rows) {
+bool make_states_map(CUtensorMap *m, const void *base, const CrossGeom &g, int rows, int halves) {
   EncodeTiledFn fn = encode_tiled_fn();
   if (!fn) return false;
   cuuint64_t dims[5] = {64, (cuuint64_t)g.Tk, 2, (cuuint64_t)g.Hkv, 1};
   cuuint64_t strides[4] = {(cuuint64_t)g.kt * 2, 128, (cuuint64_t)g.kh * 2, (cuuint64_t)g.kh * 2};
-  cuuint32_t box[5] = {64, (cuuint32_t)rows, 2, 1, 1};
+  cuuint32_t box[5] = {64, (cuuint32_t)rows, (cuuint32_t)halves, 1, 1};
   cuuint32_t estr[5] = {1, 1, 1, 1, 1};
   return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
@@ -936,7 +936,7 @@ cudaError_t launch_cache_rows(const CacheGeom &g, const CacheIndex &ix, const Ca
 cudaError_t launch_cross_rows(const CrossGeom &g, const CacheIndex &ix, const CrossWorkspace &w, const void *Q, const void *K, const void *V, void *O,
                               float *lse, cudaStream_t s, int *launches) {
   CUtensorMap mk, mv;
-  if (!make_states_map(&mk, K, g, keys_of(false)) || !make_states_map(&mv, V, g, keys_of(false))) return cudaErrorInvalidValue;
+  if (!make_states_map(&mk, K, g, keys_of(false), 2) || !make_states_map(&mv, V, g, keys_of(false), 2)) return cudaErrorInvalidValue;
   RowsParams p = {};
   p.ix = ix;
   p.Q = static_cast<const uint16_t *>(Q);

@@ -45,8 +45,8 @@ cudaError_t launch_cross_rows(const CrossGeom &g, const CacheIndex &ix, const Cr
 cudaError_t launch_cross_tiles(const CrossGeom &g, const CacheIndex &ix, const CrossWorkspace &w, const void *Q, const void *K, const void *V, void *O,
                                float *lse, cudaStream_t s, int *launches);
 
-// K or V as (64 dims, row, dim half, head): a box is both halves of `rows` rows of one head, from any row on, 128-byte rows, swizzled.
-bool make_states_map(CUtensorMap *m, const void *base, const CrossGeom &g, int rows);
+// K or V as (64 dims, row, dim half, head): a box is one or both halves of `rows` rows of one head, from any row on, 128-byte rows, swizzled.
+bool make_states_map(CUtensorMap *m, const void *base, const CrossGeom &g, int rows, int halves);
 
 #ifdef __CUDACC__
 // Sequence s as its arrays describe it, brought into range (and reported) where they do not hold what they should.

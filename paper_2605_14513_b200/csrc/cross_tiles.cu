@@ -64,8 +64,15 @@ struct alignas(16) Chunk {
 };
 static_assert(kThreads * sizeof(Chunk) <= kTileBytes, "they lie where rows are staged later");
 
+template <bool Pair>
+struct Ring {  // of keys and of values, of which a CTA of a pair has half
+  static constexpr int kBytes = Pair ? kTileBytes / 2 : kTileBytes, kStages = 2 * kTileBytes / kBytes;
+};
+constexpr int kMostStages = 4;
+
 struct CrossShared {
-  uint64_t q_full[2], k_full[2], v_full[2];
+  uint64_t q_full[2], k_full[kMostStages], v_full[kMostStages];     // (those that an issuer waits for: of a pair, in its first CTA)
+  uint64_t q_empty[2], k_empty[kMostStages], v_empty[kMostStages];  // the products have read it
   uint64_t l_ready[2][4], l_read[2];  // the row sum of the steps of the warpgroup without the last one is there, per lane quarter; the row sums have been read
   uint64_t v_tail;         // V_g is there, but for what is behind its last key
   uint64_t s_full[2], s_free[2], p_full[2], pv_done[2], m_ready[2][4];  // as in attn_tc.cu
@@ -123,6 +130,7 @@ __device__ __forceinline__ bool wait_unless(uint32_t bar, uint32_t parity, uint3
   return there != 0;
 }
 
+template <bool Pair>
 __global__ void __launch_bounds__(kThreads, 1)
     cross_tile_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                       const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_o, const CrossParams p) {
@@ -131,17 +139,37 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const CacheIndex &ix = p.ix;
   volatile int *abort = &sh.abort;
+  using R = Ring<Pair>;
+  constexpr int kCtas = Pair ? 2 : 1;
+  const int rank = Pair ? (int)cluster_ctarank() : 0, worker = blockIdx.x / kCtas, workers = gridDim.x / kCtas;
+  // An arrival at, and a copy that counts on, a barrier of the CTA whose issuers wait for it.  (What an arrival says is ordered by the tensor memory's and the
+  // copies' own fences.  As releases to the cluster two arrivals a step took 1000 clocks each.)
+  auto arrive_first = [&](uint64_t *bar) {
+    if (Pair) mbar_arrive_at(bar, 0);
+    else mbar_arrive(bar);
+  };
+  auto expect = [&](uint64_t *bar, uint32_t bytes) {
+    if (Pair) mbar_expect_tx_at(bar, 0, bytes);
+    else mbar_expect_tx(bar, bytes);
+  };
+  auto copy = [&](void *dst, const CUtensorMap *map, uint64_t *bar, int c1, int c2, int c3, int c4) {
+    if (Pair) tma_load_5d_pair(dst, map, cluster_address(smem_u32(bar), 0), 0, c1, c2, c3, c4);
+    else tma_load_5d(dst, map, bar, 0, c1, c2, c3, c4);
+  };
+  auto commit = [&](uint64_t *bar) {  // in both CTAs
+    if (Pair) tc_commit_pair(bar);
+    else tc_commit(bar);
+  };
 
   // ------------------------------------------------------------------ set-up
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&sh.q_full[i], 1);
+      mbar_init(&sh.q_full[i], kCtas);
+      mbar_init(&sh.q_empty[i], 1);
       mbar_init(&sh.l_read[i], 4);
-      mbar_init(&sh.k_full[i], 1);
-      mbar_init(&sh.v_full[i], 1);
       mbar_init(&sh.s_full[i], 1);
-      mbar_init(&sh.s_free[i], 4);
-      mbar_init(&sh.p_full[i], 4);
+      mbar_init(&sh.s_free[i], 4 * kCtas);
+      mbar_init(&sh.p_full[i], 4 * kCtas);
       mbar_init(&sh.pv_done[i], 1);
       for (int q = 0; q < 4; ++q) {
         mbar_init(&sh.m_ready[i][q], 1);
@@ -150,12 +178,18 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&sh.o_full[i], 1);
       mbar_init(&sh.drain[i], 1);
     }
+    for (int i = 0; i < R::kStages; ++i) {
+      mbar_init(&sh.k_full[i], kCtas);
+      mbar_init(&sh.v_full[i], kCtas);
+      mbar_init(&sh.k_empty[i], 1);
+      mbar_init(&sh.v_empty[i], 1);
+    }
     for (int i = 0; i < kPartRing; ++i) {
       mbar_init(&sh.part_full[i], 1);
-      mbar_init(&sh.part_empty[i], kReaders);
+      mbar_init(&sh.part_empty[i], rank == 0 ? kReaders : kReaders - 2);  // (the second CTA has no issuers)
     }
     mbar_init(&sh.v_tail, 1);
-    mbar_init(&sh.o_free, 4);
+    mbar_init(&sh.o_free, 4 * kCtas);
     mbar_init(&sh.staged, 4);
     mbar_init(&sh.stage_free, 1);
     mbar_init(&sh.stored, 4);
@@ -172,15 +206,21 @@ __global__ void __launch_bounds__(kThreads, 1)
     tma_prefetch_desc(&map_o);
   }
   if (warp == kWarpQK) {
-    tmem_alloc(&sh.tmem_base, 512);
-    tmem_relinquish();
+    if (Pair) {
+      tmem_alloc_pair(&sh.tmem_base, 512);
+    } else {
+      tmem_alloc(&sh.tmem_base, 512);
+      tmem_relinquish();
+    }
   }
   pdl_wait();
   pdl_launch_dependents();
 
   // ------------------------------------------------------------------ the CTA's share of the line
   const int tokens_per_tile = 128 / p.G;
-  auto tiles_of = [&](const Sequence &q) { return (int)(((long long)q.n + tokens_per_tile - 1) / tokens_per_tile); };
+  auto tiles_of = [&](const Sequence &q) {  // or pairs of them
+    return (int)(((long long)q.n + kCtas * tokens_per_tile - 1) / (kCtas * tokens_per_tile));
+  };
   auto steps_of = [&](const Sequence &q) { return max((q.len + kKeyStep - 1) / kKeyStep, 1); };  // (one without any key: the rows are written)
   auto cost_of = [&](const Sequence &q) { return steps_of(q) + kTileCost; };
   auto quotient = [](long long a, long long b) -> long long {  // (small code: of numbers that fit 32 bits as a rule, of others a bit at a time)
@@ -210,7 +250,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     chunks[tid] = mine;
   }
   tc_fence_before();
-  __syncthreads();
+  if (Pair) cluster_sync();  // (the other CTA's barriers are there)
+  else __syncthreads();
   tc_fence_after();
   const uint32_t tmem = sh.tmem_base;
 
@@ -226,6 +267,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     while (__builtin_expect(!__all_sync(0xffffffffu, mbar_try_wait(bar, parity)), 0)) {
       if (__any_sync(0xffffffffu, *abort != 0 || (uint32_t)clock() - since > (uint32_t)kWaitLimitCycles)) {
         *abort = 1;
+        if (Pair) cluster_st1(cluster_address(smem_u32(&sh.abort), rank ^ 1), 1u);
         return ok = false;
       }
     }
@@ -248,30 +290,23 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (lane == 0) mbar_arrive(&sh.part_empty[n % kPartRing]);
   };
   // Keys of a part's last step: fewer than 128 if that is the tile's last one.
+  // Of up to 128 keys, those that the products take: of values 16 at a time, of scores 16 or, by pairs, 32.
+  auto values_read = [](int keys) { return min(max((keys + 15) & ~15, 16), kKeyStep); };
+  auto keys_read = [](int keys) { return min(max((keys + 16 * kCtas - 1) & ~(16 * kCtas - 1), 16 * kCtas), kKeyStep); };
   auto last_keys = [&](const Part *x) { return x->b < x->steps ? kKeyStep : x->len - (x->steps - 1) * kKeyStep; };
   auto settle = [&](uint64_t *bar, uint32_t parity) {
     const uint32_t t0 = clock();
     while (!mbar_try_wait(bar, parity) && (uint32_t)clock() - t0 < 40000000u) {
     }
   };
-  auto settle_pair = [&](uint64_t *bar, int issued) {  // the last two of `issued` copies on a pair of barriers
-#pragma unroll 1
-    for (int i = issued > 2 ? issued - 2 : 0; i < issued; ++i) settle(&bar[i & 1], (i >> 1) & 1);
-  };
   auto desc_at = [](uint64_t desc, uint32_t off16) -> uint64_t {
     return (desc & 0xffffffff00000000ull) | (uint32_t)((uint32_t)desc + off16);
   };
   auto drain_products = [&](bool leader, uint64_t *bar) {
     if (!*abort) return;
-    if (leader) tc_commit(bar);
+    if (leader) commit(bar);
     __syncwarp();
     settle(bar, 0);
-  };
-  auto load_tile = [&](unsigned char *dst, const CUtensorMap *map, uint64_t *bar, int row, int h) {
-    if (lane == 0) {
-      mbar_expect_tx(bar, kTileBytes);
-      tma_load_5d(dst, map, bar, 0, row, 0, h, 0);
-    }
   };
   auto lse_of = [&](const Part *x, int row) {
     const int t = (int)(((uint32_t)row * p.inv_G) >> 16);
@@ -295,7 +330,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto loaded = [&]() {
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&sh.o_free);
+      if (lane == 0) arrive_first(&sh.o_free);
     };
     // 32 dims of the row as bf16, O / l, and into shared memory
     auto pack = [&](const uint32_t (&v)[32], float inv, uint32_t (&y)[16]) {
@@ -364,8 +399,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (!wait(&sh.stored, n_stored & 1)) break;
           if (lane == 0) {
             __threadfence();  // (of what the CTA has stored, which the barriers have shown this thread)
-            const bool is_last = atomicAdd(&p.arrivals[x->c0], 1) == x->parts - 1;
-            if (is_last) p.arrivals[x->c0] = 0;
+            int32_t *const arrivals = &p.arrivals[x->c0 * kCtas + rank];
+            const bool is_last = atomicAdd(arrivals, 1) == x->parts - 1;
+            if (is_last) *arrivals = 0;
             sh.last = is_last;
             ++sh.shared_parts;
             __threadfence();
@@ -379,7 +415,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           done_with_part(n);
           continue;
         }
-        auto place = [&](int i) { return 2 * (x->c0 + i) + (i == 0 ? 1 : 0); };
+        auto place = [&](int i) { return 2 * ((x->c0 + i) * kCtas + rank) + (i == 0 ? 1 : 0); };
         float m = kNoReference, l = 0.f;
 #pragma unroll 1
         for (int k = 0; k < x->parts; ++k) {
@@ -471,8 +507,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         total = __shfl_sync(0xffffffffu, upto_lane(total), 31);
         longest = __reduce_max_sync(0xffffffffu, longest);
         whole = longest <= kWholeSteps + kTileCost;
-        share = max(quotient(total + gridDim.x - 1, gridDim.x), whole ? 1LL : (long long)(longest + kMaxParts - 1) / kMaxParts);
-        w.u = blockIdx.x * share;
+        share = max(quotient(total + workers - 1, workers), whole ? 1LL : (long long)(longest + kMaxParts - 1) / kMaxParts);
+        w.u = worker * share;
         w.end = min(total, w.u + share);
         if (w.u < w.end) {  // the chunk in which the share begins, then the sequence (all lanes alike)
           long long before = 0;
@@ -507,21 +543,25 @@ __global__ void __launch_bounds__(kThreads, 1)
       // Part n + 1 is announced with the first step of part n, and its Q brought to L2: it comes from memory, in 3000 clocks, and copies behind it would wait as long.
       // (Little code for a tile like the one before, in registers: K waits for it.  By one thread from shared memory it took 2400 clocks, and 12 heads x 32760 over 512
       // 112 us.)  n = -1: no steps.
-      int g = 0, a = 0, b = 1, h = 0, key = 0, row = 0;
+      int g = 0, a = 0, b = 1, h = 0, key = 0, row = 0, len = 0;
 #pragma unroll 1
       for (int n = -1; b >= 0; ++n) {
-        int next_a = 0, next_b = 0, next_h = 0, next_key = 0, next_row = 0;
+        int next_a = 0, next_b = 0, next_h = 0, next_key = 0, next_row = 0, next_len = 0;
 #pragma unroll 1
         for (int i = a; i < b; ++i) {
-          if (n >= 0 && ok && (g < 2 || timed_wait(&sh.s_full[g & 1], ((g - 2) >> 1) & 1))) {
-            load_tile(smem + kOffK + (g & 1) * kTileBytes, &map_k, &sh.k_full[g & 1], key + i * kKeyStep, h);
-            if (i == a && lane == 0) {  // (the scores of step g - 2 are complete, and with them those of part n - 2: its Q has been read)
-              unsigned char *q = smem + kOffQ + (n & 1) * kTileBytes;
-              mbar_expect_tx(&sh.q_full[n & 1], 2 * (128 / p.G * p.G) * 128);
-              tma_load_5d(q, &map_q, &sh.q_full[n & 1], 0, 0, row, 0, h);
-              tma_load_5d(q + kTileBytes / 2, &map_q, &sh.q_full[n & 1], 0, 0, row, 1, h);
+          const int st = g % R::kStages;
+          if (n >= 0 && ok && (g < R::kStages || timed_wait(&sh.k_empty[st], (g / R::kStages - 1) & 1))) {
+            if (lane == 0) {  // (of a pair's products each CTA has half of the keys that they take)
+              expect(&sh.k_full[st], R::kBytes);
+              copy(smem + kOffK + st * R::kBytes, &map_k, &sh.k_full[st], key + i * kKeyStep + rank * (keys_read(len - i * kKeyStep) >> 1), 0, h, 0);
             }
             ++g;
+            if (i == a && (n < 2 || timed_wait(&sh.q_empty[n & 1], ((n - 2) >> 1) & 1)) && lane == 0) {
+              unsigned char *q = smem + kOffQ + (n & 1) * kTileBytes;
+              expect(&sh.q_full[n & 1], 2 * (128 / p.G * p.G) * 128);
+              copy(q, &map_q, &sh.q_full[n & 1], 0, row, 0, h);
+              copy(q + kTileBytes / 2, &map_q, &sh.q_full[n & 1], 0, row, 1, h);
+            }
             __syncwarp();
           }
           if (i == a) {
@@ -539,8 +579,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                   while (w.tiles == 0 && w.s + 1 < ix.S);
                 }
               }
-              next_a = 0, next_b = w.steps, next_h = w.h, next_key = w.q.key, next_row = w.q.row + w.tile * tokens_per_tile;
-              int c0 = blockIdx.x, parts = 1;
+              const int first = (w.tile * kCtas + rank) * tokens_per_tile;
+              next_a = 0, next_b = w.steps, next_h = w.h, next_key = w.q.key, next_row = w.q.row + first, next_len = w.q.len;
+              int c0 = worker, parts = 1;
               const long long tile_at = w.u - w.off;
               if (__builtin_expect(!whole && (w.off > 0 || w.end - w.u < w.steps + kTileCost), 0)) {
                 next_a = max(w.off - kTileCost, 0);
@@ -554,10 +595,10 @@ __global__ void __launch_bounds__(kThreads, 1)
               w.u = next_b < 0 ? w.end : tile_at + kTileCost + next_b;
               w.off = 0;
               if (lane == 0 && next_b >= 0) {
-                if (parts > 1) sh.owed[sh.n_owed++] = make_int4(2 * blockIdx.x + (next_a == 0 ? 1 : 0), c0, parts, 0);
+                if (parts > 1) sh.owed[sh.n_owed++] = make_int4(2 * blockIdx.x + (next_a == 0 ? 1 : 0), c0 * kCtas + rank, parts, 0);
                 if (ok) {
                   int4 *const x = reinterpret_cast<int4 *>(&sh.part[m % kPartRing]);
-                  x[0] = make_int4(next_row, min(tokens_per_tile, w.q.n - w.tile * tokens_per_tile), next_h, next_key);
+                  x[0] = make_int4(next_row, min(tokens_per_tile, max(w.q.n - first, 0)), next_h, next_key);
                   x[1] = make_int4(w.q.len, w.steps, next_a, next_b);
                   x[2] = make_int4(c0, parts, 0, 0);
                   tma_prefetch_5d(&map_q, 0, 0, next_row, 0, next_h);
@@ -574,14 +615,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           if (!ok) break;
         }
-        a = next_a, b = next_b, h = next_h, key = next_key, row = next_row;
+        a = next_a, b = next_b, h = next_h, key = next_key, row = next_row, len = next_len;
       }
       if (ok) timed_wait(&sh.finished, 0);
-      if (*abort) {
-        settle_pair(sh.k_full, g);
-        settle(&sh.q_full[0], 0), settle(&sh.q_full[0], 1);  // (one of the two is past)
-        settle(&sh.q_full[1], 0), settle(&sh.q_full[1], 1);
-      }
     } else if (warp == kWarpV) {
       // ===== V producer
       int g = 0;
@@ -594,33 +630,44 @@ __global__ void __launch_bounds__(kThreads, 1)
         done_with_part(n);
 #pragma unroll 1
         for (int i = a; i < b; ++i, ++g) {
-          const int at = g & 1;
-          if (g >= 2 && !wait(&sh.pv_done[at], ((g - 2) >> 1) & 1)) break;
-          unsigned char *const to = smem + kOffV + at * kTileBytes;
+          const int st = g % R::kStages;
+          if (g >= R::kStages && !wait(&sh.v_empty[st], (g / R::kStages - 1) & 1)) break;
+          unsigned char *const to = smem + kOffV + st * R::kBytes;
           const int keys = i == b - 1 ? ends : kKeyStep;
           const bool tail = (keys & 15) || keys == 0;
 #ifdef HEART_TEST_HOOKS
           if (!(p.test_skip && blockIdx.x == 0 && g == 1))
 #endif
-          load_tile(to, &map_v, tail ? &sh.v_tail : &sh.v_full[at], key + i * kKeyStep, h);
+          if (lane == 0) {  // (of a pair's products each CTA has half of the dims)
+            if (tail) {
+              mbar_expect_tx(&sh.v_tail, R::kBytes);
+              tma_load_5d(to, &map_v, &sh.v_tail, 0, key + i * kKeyStep, rank, h, 0);
+            } else {
+              expect(&sh.v_full[st], R::kBytes);
+              copy(to, &map_v, &sh.v_full[st], key + i * kKeyStep, rank, h, 0);
+            }
+          }
+          __syncwarp();
           if (tail) {  // rows that a product reads behind the last key
             if (!wait(&sh.v_tail, tails & 1)) break;
             ++tails;
             const int out = keys == 0 ? 16 : 16 - (keys & 15);
 #pragma unroll 1
-            for (int j = lane; j < out * 16; j += 32)
-              sts_u4(smem_u32(to) + ((j >> 3) & 1) * (kTileBytes / 2) + (keys + (j >> 4)) * 128 + (j & 7) * 16, make_uint4(0u, 0u, 0u, 0u));
+            for (int j = lane; j < out * 8 * (2 / kCtas); j += 32) {
+              const int half = Pair ? 0 : j & 1, at = Pair ? j : j >> 1;
+              sts_u4(smem_u32(to) + half * (kTileBytes / 2) + (keys + (at >> 3)) * 128 + (at & 7) * 16, make_uint4(0u, 0u, 0u, 0u));
+            }
             async_proxy_fence();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&sh.v_full[at]);
+            if (lane == 0) {
+              if (Pair) mbar_arrive_in(&sh.v_full[st], 0);
+              else mbar_arrive(&sh.v_full[st]);
+            }
           }
-          __syncwarp();
         }
       }
-      if (*abort) {
-        settle_pair(sh.v_full, g);
-        settle(&sh.v_tail, tails & 1);
-      }
+    } else if (rank != 0) {
+      // (the issuers of a pair are the first CTA's)
     } else if (warp == kWarpQK) {
       // ===== issuer of the score products
       const uint64_t q_desc = smem_desc_sw128(smem_u32(smem + kOffQ), 16, 1024);
@@ -638,16 +685,22 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll 1
         for (int i = 0; i < n_steps; ++i, ++g) {  // S_g = Q K_g^T
           const uint32_t b = g & 1;
-          if (!wait2(&sh.s_free[b], ((g - 2) >> 1) & 1, &sh.k_full[b], (g >> 1) & 1)) break;  // (the phase before the first one counts as past)
+          const uint32_t st = g % R::kStages;
+          if (!wait2(&sh.s_free[b], ((g - 2) >> 1) & 1, &sh.k_full[st], (g / R::kStages) & 1)) break;  // (the phase before the first one counts as past)
           tc_fence_after();
           if (leader) {
-            const uint64_t kd = desc_at(k_desc, b * (kTileBytes >> 4));
-            const int keys = i == n_steps - 1 ? max((ends + 15) & ~15, 16) : kKeyStep;
-            const uint32_t idesc = idesc_bf16_f32(128, 0, false, false) | (uint32_t)(keys >> 3) << 17;
+            const uint64_t kd = desc_at(k_desc, st * (R::kBytes >> 4));
+            const int keys = i == n_steps - 1 ? keys_read(ends) : kKeyStep;
+            const uint32_t idesc = idesc_bf16_f32(128 * kCtas, 0, false, false) | (uint32_t)(keys >> 3) << 17;
 #pragma unroll
-            for (int ks = 0; ks < 8; ++ks)
-              mma_ss(tmem + 128 + b * 128, desc_at(qd, (ks >> 2) * 1024 + (ks & 3) * 2), desc_at(kd, (ks >> 2) * 1024 + (ks & 3) * 2), idesc, ks > 0 ? 1u : 0u);
-            tc_commit(&sh.s_full[b]);
+            for (int ks = 0; ks < 8; ++ks) {
+              const uint64_t qk = desc_at(qd, (ks >> 2) * 1024 + (ks & 3) * 2), kk = desc_at(kd, (ks >> 2) * (R::kBytes >> 5) + (ks & 3) * 2);
+              if (Pair) mma_ss_pair(tmem + 128 + b * 128, qk, kk, idesc, ks > 0 ? 1u : 0u);
+              else mma_ss(tmem + 128 + b * 128, qk, kk, idesc, ks > 0 ? 1u : 0u);
+            }
+            commit(&sh.s_full[b]);
+            commit(&sh.k_empty[st]);
+            if (i == n_steps - 1) commit(&sh.q_empty[n & 1]);
           }
           __syncwarp();
         }
@@ -655,7 +708,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       drain_products(leader, &sh.drain[0]);
     } else if (warp == kWarpPV) {
       // ===== issuer of the value products
-      constexpr uint32_t idesc = idesc_bf16_f32(128, 128, false, true);
+      constexpr uint32_t idesc = idesc_bf16_f32(128 * kCtas, 128, false, true);
       const uint64_t v_desc = smem_desc_sw128(smem_u32(smem + kOffV), kTileBytes / 2, 1024);
       const bool leader = elect_one();
       uint32_t g = 0;
@@ -669,16 +722,21 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll 1
         for (int i = 0; i < n_steps; ++i, ++g) {  // O (+)= P_g V_g
           const uint32_t b = g & 1;
-          if (!wait2(&sh.v_full[b], (g >> 1) & 1, &sh.p_full[b], (g >> 1) & 1)) break;
+          const uint32_t st = g % R::kStages;
+          if (!wait2(&sh.v_full[st], (g / R::kStages) & 1, &sh.p_full[b], (g >> 1) & 1)) break;
           tc_fence_after();
           if (leader) {
-            const uint64_t vd = desc_at(v_desc, b * (kTileBytes >> 4));
-            const int ks_end = i == n_steps - 1 ? max((ends + 15) >> 4, 1) : 8;
+            const uint64_t vd = desc_at(v_desc, st * (R::kBytes >> 4));
+            const int ks_end = i == n_steps - 1 ? values_read(ends) >> 4 : 8;
 #pragma unroll
-            for (int ks = 0; ks < 8; ++ks)
-              if (ks < ks_end) mma_ts(tmem, tmem + 384 + b * 64 + ks * 8, desc_at(vd, ks * 128), idesc, (i > 0 || ks > 0) ? 1u : 0u);
-            if (i == n_steps - 1) tc_commit(&sh.o_full[n & 1]);
-            tc_commit(&sh.pv_done[b]);
+            for (int ks = 0; ks < 8; ++ks) {
+              if (ks >= ks_end) break;
+              if (Pair) mma_ts_pair(tmem, tmem + 384 + b * 64 + ks * 8, desc_at(vd, ks * 128), idesc, (i > 0 || ks > 0) ? 1u : 0u);
+              else mma_ts(tmem, tmem + 384 + b * 64 + ks * 8, desc_at(vd, ks * 128), idesc, (i > 0 || ks > 0) ? 1u : 0u);
+            }
+            if (i == n_steps - 1) commit(&sh.o_full[n & 1]);
+            commit(&sh.pv_done[b]);
+            commit(&sh.v_empty[st]);
           }
           __syncwarp();
         }
@@ -696,7 +754,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto arrive = [&](uint64_t *bar) {  // this warp's tensor-memory accesses so far are ordered before it
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar);
+      if (lane == 0) arrive_first(bar);
     };
     uint32_t g0 = 0;  // key steps before the present part
 #pragma unroll 1
@@ -840,10 +898,23 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncwarp();
   if (warp != kWarpK && lane == 0) mbar_arrive(&sh.finished);
   tc_fence_before();
-  __syncthreads();
+  // Neither CTA of a pair leaves while the other one's products read its shared memory or arrivals are under way; after an abort copies in flight get time to
+  // land (bounded: a copy takes microseconds).
+  if (Pair) cluster_sync();
+  else __syncthreads();
+  int gave_up = *abort;
+  if (Pair) gave_up |= (int)cluster_ld1(cluster_address(smem_u32(&sh.abort), rank ^ 1));
+  if (gave_up) {
+    const uint32_t since = clock();
+    while ((uint32_t)clock() - since < 2000000u) {
+    }
+  }
+  if (Pair) cluster_sync();
+  else __syncthreads();
   if (warp == kWarpQK) {
     tc_fence_after();
-    tmem_dealloc(tmem, 512);
+    if (Pair) tmem_dealloc_pair(tmem, 512);
+    else tmem_dealloc(tmem, 512);
   }
   if (sh.abort && tid == 0) {
     atomicExch(ix.status, HEART_ERR_DEVICE_CHECK);
@@ -862,8 +933,12 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 cudaError_t launch_cross_tiles(const CrossGeom &g, const CacheIndex &ix, const CrossWorkspace &w, const void *Q, const void *K, const void *V, void *O,
                                float *lse, cudaStream_t s, int *launches) {
+  // Pairs of CTAs, where a sequence may have more rows than a tile.
+  const bool pair = (long long)g.max_q > 128 / g.G;
   CUtensorMap mq, mk, mv, mo;
-  if (!make_query_map(&mq, Q, g) || !make_query_map(&mo, O, g) || !make_states_map(&mk, K, g, kKeyStep) || !make_states_map(&mv, V, g, kKeyStep)) return cudaErrorInvalidValue;
+  if (!make_query_map(&mq, Q, g) || !make_query_map(&mo, O, g) || !make_states_map(&mk, K, g, pair ? kKeyStep / 2 : kKeyStep, 2) ||
+      !make_states_map(&mv, V, g, kKeyStep, pair ? 1 : 2))
+    return cudaErrorInvalidValue;
   CrossParams p = {};
   p.ix = ix;
   p.arrivals = w.arrivals;
@@ -879,10 +954,11 @@ cudaError_t launch_cross_tiles(const CrossGeom &g, const CacheIndex &ix, const C
   p.inv_G = (65536u + g.G - 1) / g.G;
   p.scale_log2 = (float)(g.scale * 1.4426950408889634);
   p.test_skip = g.test_skip;
-  cudaError_t e = allow_shared_memory(cross_tile_kernel, kSmem);
+  auto *const kernel = pair ? cross_tile_kernel<true> : cross_tile_kernel<false>;
+  cudaError_t e = allow_shared_memory(kernel, kSmem);
   if (e != cudaSuccess) return e;
   ++*launches;
-  return launch_pdl(cross_tile_kernel, dim3(kCacheCtas), dim3(kThreads), kSmem, s, mq, mk, mv, mo, p);
+  return launch_pdl(kernel, dim3(kCacheCtas), dim3(kThreads), kSmem, s, Cluster{pair ? 2 : 1}, mq, mk, mv, mo, p);
 }
 
 }  // namespace heart

@@ -168,6 +168,9 @@ __device__ __forceinline__ void bulk_copy_to_cluster(uint32_t dst, const void *s
                "r"(bytes), "r"(bar)
                : "memory");
 }
+__device__ __forceinline__ void cluster_st1(uint32_t addr, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
 __device__ __forceinline__ float2 lds2(uint32_t addr) {
   float2 v;
   asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
@@ -300,6 +303,23 @@ __device__ __forceinline__ void tma_load_5d_pair(void *smem_dst, const CUtensorM
 // Arrival on the barrier at this address in CTA `rank` of the cluster.
 __device__ __forceinline__ void mbar_arrive_in(uint64_t *bar, uint32_t rank) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_address(smem_u32(bar), rank)) : "memory");
+}
+
+// The same with no more order than within this CTA; with `bytes` more to come.
+__device__ __forceinline__ void mbar_arrive_at(uint64_t *bar, uint32_t rank) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_address(smem_u32(bar), rank)) : "memory");
+}
+__device__ __forceinline__ void mbar_expect_tx_at(uint64_t *bar, uint32_t rank, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cluster.b64 _, [%0], %1;" ::"r"(cluster_address(smem_u32(bar), rank)), "r"(bytes) : "memory");
+}
+// D[tmem] (+)= A[tmem] * B[smem], each CTA with its half of A's rows and of B's columns.
+__device__ __forceinline__ void mma_ts_pair(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
 }
 
 // ---------------------------------------------------------------- fp64 matrix instruction
