@@ -376,7 +376,7 @@ typedef struct {
  * invalid or unsupported config.  A workspace serves one call at a time, as those of the cache do. */
 size_t heart_cross_workspace_bytes(const heart_cross_config *cfg /* host */);
 
-/* Base pointers 16-byte aligned, strides multiples of 8 elements, head_dim contiguous. */
+/* Base pointers 16-byte aligned, strides multiples of 8 elements, less than 2^38 of them from row to row, head to head and key head to key head, head_dim contiguous. */
 int heart_cross_attn(const heart_cross_config *cfg, const void *Q, const void *K, const void *V, const int32_t *q_start,
                      const int32_t *k_start, const int32_t *k_len, void *O, float *lse, void *workspace, heart_stream_t stream);
 

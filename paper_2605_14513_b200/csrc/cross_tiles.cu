@@ -5,16 +5,20 @@
 // are what bounds it (the tensor pipe 1024 clocks a step, the special-function units 1024, shared memory 1280) and the way two warpgroups agree on a
 // row's reference.  What differs, since all rows of a tile see the same keys and these are few (a text: 512, four steps):
 //   * The end of a tile is the common case.  A warpgroup of its own takes the sums out of tensor memory, by way of registers, as bf16, into shared memory, from
-//     where bulk copies write them, while the others are in the next tile's first steps.  That has room for a whole tile, which the one before leaves
-//     meanwhile: stores of all SMs go at some 10 bytes a clock and SM, 3000 clocks a tile, and whoever waits for them (the warps where they store themselves, or a
-//     half that waits for the other's place) is late for the next tile's sums.  The room is found by putting the row sums in the place of the tile's Q.
-//   * A tile's last step may have fewer than 128 keys: the products are cut to the next 16 keys (columns of the scores, steps of the values' product), the
-//     softmax of up to 32 to these; scores behind the last key become -inf in tensor memory, values of up to 15 rows behind it, which are
-//     anyone's, zeros in shared memory.  (By 32 keys at a time, twice, 12 heads x 32760 over 226 took 100 us, where 256 took 73.)
-//   * There is no plan: all tiles of a sequence take the same number of steps, so a CTA finds its share of the line of all tiles' steps, (sequence, head,
+//     where bulk copies write them, while the others are in the next tile's first steps.  Stores of all SMs go at some 10 bytes a clock and SM, 3000 clocks a tile:
+//     a warpgroup that waited for its own would be late for the next tile's scores.  At each end every warp runs through other code than in between, and the
+//     instruction cache does not hold all of it: little code a tile (loops that stay rolled, one wait in few instructions) gave more than fewer instructions.
+//   * A tile's last step may have fewer than 128 keys: the products are cut to the next 16 keys (columns of the scores, 32 by pairs; steps of the values' product);
+//     scores behind the last key become -inf in tensor memory, values of up to 15 rows behind it, which are anyone's, zeros in shared memory.
+//   * Pairs of CTAs, for large calls, take two tiles of a sequence and head with half of the keys and of the values' dims each: the products of both are one
+//     instruction of the first CTA's issuers, and half of the bytes come from L2.  Barriers that these wait for are the first CTA's, those that they complete both's.
+//   * There is no plan: all tiles of a sequence take the same number of steps, so a CTA (or pair) finds its share of the line of all tiles' steps, (sequence, head,
 //     tile, step), from the lengths alone, each beginning of a tile counted as kTileCost steps.
 //     Parts of a tile go to the workspace; the CTA that brings the last one puts them together, in order: the result does not depend on which one
 //     that is.
+//
+// Measured, 12 heads of 128: 32760 queries over 512 keys 108 us (955 TFLOP/s), over 128 54.7 (traffic: 202 MB, 3.7 TB/s), 4680 over 512 23.3, 1000 over 33k 192
+// (by pairs, 2 x 40 heads x 32760 over 343 533 us, 863 TFLOP/s and 2.5 TB/s).
 //
 // Warp roles: 0-3, 4-7 softmax; 8 issues S = Q K^T; 9 copies V; 10 finds the CTA's parts, copies K and Q; 11 issues O += P V; 12-15 write.
 // Tensor memory: O (128 columns) | S[2] (2 x 128) | P[2] (2 x 64).
@@ -31,7 +35,7 @@ namespace {
 
 constexpr int kThreads = 512;
 constexpr int kWarpQK = 8, kWarpV = 9, kWarpK = 10, kWarpPV = 11, kWarpOut = 12;
-constexpr int kRegsSoftmax = 184, kRegsOut = 104, kRegsHelper = 40;  // 184 * 256 + 104 * 128 + 40 * 128 = the CTA's 512 x 128
+constexpr int kRegsSoftmax = 184, kRegsOut = 80, kRegsHelper = 64;  // 184 * 256 + 80 * 128 + 64 * 128 = the CTA's 512 x 128
 static_assert(kRegsSoftmax * 256 + kRegsOut * 128 + kRegsHelper * 128 <= kThreads * 128, "registers at launch");
 constexpr int kTileBytes = 32768;  // 128 rows x 128 dims: [2 dim halves][128 rows][64] bf16, 128-byte swizzle
 constexpr int kTileCost = 1;       // of a tile besides its steps, in steps
@@ -44,8 +48,8 @@ constexpr float kHeadroom = 16.f, kMaxGrowth = 8.f;  // see attn_tc.cu
 
 // Part of a tile that a CTA takes: steps a .. b - 1.
 struct alignas(16) Part {  // (written by fours)
-  int row, tokens, h, key;  // first packed row, tokens, key head, first row of its keys
-  int len, steps, a, b;     // keys of the tile, in steps; b < 0: no part left
+  int row, tokens, h, key;  // first packed row, tokens, key head, first row of keys
+  int4 steps;               // how many, keys of the last one, the tile's steps before them, 1 if they are all of the tile's; x < 0: no part left
   int c0, parts, pad[2];    // first CTA with a part of the tile, and how many there are
 };
 
@@ -87,6 +91,7 @@ struct CrossShared {
   float l[2][128];         // of the row sums: the other warpgroup's part, then one over them, per part & 1
   uint32_t tmem_base;
   int shared_parts;        // parts of shared tiles that have been announced
+  long long share;         // of the line, a CTA or a pair; 0: whole tiles
   int4 owed[2];            // this CTA's parts of shared tiles: place in the workspace, first CTA of the tile, number of its parts
   int n_owed;
   int last;
@@ -110,6 +115,11 @@ struct CrossParams {
   int test_skip;           // test-hook builds only: CTA 0 leaves out its second copy of values
 };
 
+__device__ __forceinline__ float reciprocal(float x) {  // (off by a unit in the last place at most)
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 // Waits for the barrier's phase of this parity; false if *abort is raised before.
 __device__ __forceinline__ bool wait_unless(uint32_t bar, uint32_t parity, uint32_t abort) {
   uint32_t there;
@@ -223,7 +233,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   };
   auto steps_of = [&](const Sequence &q) { return max((q.len + kKeyStep - 1) / kKeyStep, 1); };  // (one without any key: the rows are written)
   auto cost_of = [&](const Sequence &q) { return steps_of(q) + kTileCost; };
-  auto quotient = [](long long a, long long b) -> long long {  // (small code: of numbers that fit 32 bits as a rule, of others a bit at a time)
+  auto quotient = [](long long a, long long b) -> long long {  // (little code: of numbers that fit 32 bits as a rule, of others a bit at a time)
     if (((a | b) >> 32) == 0) return (long long)((uint32_t)a / (uint32_t)b);
     long long q = 0, r = 0;
 #pragma unroll 1
@@ -235,19 +245,24 @@ __global__ void __launch_bounds__(kThreads, 1)
     return q;
   };
   auto line_of = [&](const Sequence &q) { return (long long)tiles_of(q) * cost_of(q) * p.Hkv; };
-  // what the sequences cost, some in a row a thread
+  Sequence of_lane = {0, 0, 0, 0};
+  // More than 32 sequences: what they cost, some in a row a thread, for the K producer.
   Chunk *const chunks = reinterpret_cast<Chunk *>(smem + kOffStage);
   const int per_chunk = (ix.S + kThreads - 1) / kThreads, n_chunks = (ix.S + per_chunk - 1) / per_chunk;
-  if (tid < n_chunks) {
-    Chunk mine = {0, 1};
+  if (ix.S > 32) {
+    if (tid < n_chunks) {
+      Chunk mine = {0, 1};
 #pragma unroll 1
-    for (int i = tid * per_chunk; i < min(ix.S, (tid + 1) * per_chunk); ++i) {
-      const Sequence q = cross_sequence(ix, i);
-      const long long line = line_of(q);
-      mine.line += line;
-      if (line > 0) mine.longest = max(mine.longest, cost_of(q));
+      for (int i = tid * per_chunk; i < min(ix.S, (tid + 1) * per_chunk); ++i) {
+        const Sequence q = cross_sequence(ix, i);
+        const long long line = line_of(q);
+        mine.line += line;
+        if (line > 0) mine.longest = max(mine.longest, cost_of(q));
+      }
+      chunks[tid] = mine;
     }
-    chunks[tid] = mine;
+  } else if (warp == kWarpK && lane < ix.S) {  // a lane a sequence
+    of_lane = cross_sequence(ix, lane);
   }
   tc_fence_before();
   if (Pair) cluster_sync();  // (the other CTA's barriers are there)
@@ -279,21 +294,18 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!wait(i == 0 ? bar0 : bar1, i == 0 ? parity0 : parity1)) break;
     return ok;
   };
-  // The announced part n; nullptr: none left (or abort).
+  // The announced part n; nullptr: abort.
   auto part_at = [&](int n) -> const Part * {
     if (!wait(&sh.part_full[n % kPartRing], (n / kPartRing) & 1)) return nullptr;
-    const Part *x = &sh.part[n % kPartRing];
-    return x->b < 0 ? nullptr : x;
+    return &sh.part[n % kPartRing];
   };
   auto done_with_part = [&](int n) {
     __syncwarp();
     if (lane == 0) mbar_arrive(&sh.part_empty[n % kPartRing]);
   };
-  // Keys of a part's last step: fewer than 128 if that is the tile's last one.
   // Of up to 128 keys, those that the products take: of values 16 at a time, of scores 16 or, by pairs, 32.
   auto values_read = [](int keys) { return min(max((keys + 15) & ~15, 16), kKeyStep); };
   auto keys_read = [](int keys) { return min(max((keys + 16 * kCtas - 1) & ~(16 * kCtas - 1), 16 * kCtas), kKeyStep); };
-  auto last_keys = [&](const Part *x) { return x->b < x->steps ? kKeyStep : x->len - (x->steps - 1) * kKeyStep; };
   auto settle = [&](uint64_t *bar, uint32_t parity) {
     const uint32_t t0 = clock();
     while (!mbar_try_wait(bar, parity) && (uint32_t)clock() - t0 < 40000000u) {
@@ -359,29 +371,28 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll 1
     for (int n = 0; ok; ++n) {
       const Part *x = part_at(n);
-      if (x == nullptr) break;
-      const bool all = x->b - x->a == x->steps;
+      if (x == nullptr || x->steps.x < 0) break;
+      const bool all = x->steps.w != 0;
       if (!wait(&sh.o_full[n & 1], (n >> 1) & 1)) break;
       tc_fence_after();
       if (__builtin_expect(all, 1)) {
         const float inv = sh.l[n & 1][row];
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.l_read[n & 1]);
-        uint32_t v[32], y[4][16];
-#pragma unroll
-        for (int quad = 0; quad < 4; ++quad) {
-          load(v, quad);
-          if (quad == 3) loaded();
-          pack(v, inv, y[quad]);
-        }
         if (!stage_free()) break;
 #pragma unroll
-        for (int quad = 0; quad < 4; ++quad) stage(y[quad], quad);
+        for (int quad = 0; quad < 4; ++quad) {
+          uint32_t v[32], y[16];
+          load(v, quad);
+          if (quad == 3) loaded();
+          pack(v, inv, y);
+          stage(y, quad);
+        }
       } else {
         // part of a shared tile: its sums to the workspace (the row sums are there), and if it is the last one, those of all put together
         if (lane == 0) mbar_arrive(&sh.l_read[n & 1]);
         const bool real = row < x->tokens * p.G;
-        const int slot = 2 * blockIdx.x + (x->a == 0 ? 1 : 0);
+        const int slot = 2 * blockIdx.x + (x->steps.z == 0 ? 1 : 0);
 #pragma unroll 1
         for (int d = 0; d < 128; d += 32) {
           uint32_t v[32];
@@ -433,11 +444,12 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll 1
           for (int k = 0; k < x->parts; ++k) {
             const int at = place(k);
-            const float f = ex2(__ldcg(&p.part_l[at * 128 + row]).y - m);
+            const float top = __ldcg(&p.part_l[at * 128 + row].y);
             const float4 *src = &p.parts[(size_t)(at * 32 + quad * 8) * 128 + row];
             float4 z[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) z[j] = __ldcg(src + j * 128);
+            const float f = ex2(top - m);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
               v[4 * j] = __float_as_uint(fmaf(z[j].x, f, __uint_as_float(v[4 * j])));
@@ -446,7 +458,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               v[4 * j + 3] = __float_as_uint(fmaf(z[j].w, f, __uint_as_float(v[4 * j + 3])));
             }
           }
-          pack(v, l == 0.f ? 0.f : 1.f / l, y);
+          pack(v, l == 0.f ? 0.f : reciprocal(l), y);
           stage(y, quad);
         }
         if (real && p.lse != nullptr) *lse_of(x, row) = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
@@ -481,8 +493,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (warp == kWarpK) {
       // ===== the CTA's parts; K and Q producer
       Walk w = {};
-      long long share;
-      bool whole;  // tiles are not shared: a CTA takes those that begin in its share
       auto next_sequence = [&]() {
         w.q = cross_sequence(ix, ++w.s);
         w.tiles = tiles_of(w.q);
@@ -490,31 +500,38 @@ __global__ void __launch_bounds__(kThreads, 1)
       };
       {
         auto upto_lane = [&](long long x) {  // inclusive, over the warp
-#pragma unroll 1
+#pragma unroll
           for (int o = 1; o < 32; o <<= 1) {
             const long long y = __shfl_up_sync(0xffffffffu, x, o);
             if (lane >= o) x += y;
           }
           return x;
         };
-        long long total = 0;
-        int longest = 1;
+        const bool few = ix.S <= 32;
+        long long total = line_of(of_lane);
+        int longest = total > 0 ? cost_of(of_lane) : 1;
 #pragma unroll 1
-        for (int i = lane; i < n_chunks; i += 32) {
+        for (int i = few ? n_chunks : lane; i < n_chunks; i += 32) {
           total += chunks[i].line;
           longest = max(longest, chunks[i].longest);
         }
-        total = __shfl_sync(0xffffffffu, upto_lane(total), 31);
+        long long mine = total, upto = upto_lane(mine);
+        total = __shfl_sync(0xffffffffu, upto, 31);
         longest = __reduce_max_sync(0xffffffffu, longest);
-        whole = longest <= kWholeSteps + kTileCost;
-        share = max(quotient(total + workers - 1, workers), whole ? 1LL : (long long)(longest + kMaxParts - 1) / kMaxParts);
+        const bool whole = longest <= kWholeSteps + kTileCost;  // tiles are not shared: a CTA takes those that begin in its share
+        const long long share = max(quotient(total + workers - 1, workers), whole ? 1LL : (long long)(longest + kMaxParts - 1) / kMaxParts);
+        if (lane == 0) sh.share = whole ? 0 : share;
         w.u = worker * share;
         w.end = min(total, w.u + share);
         if (w.u < w.end) {  // the chunk in which the share begins, then the sequence (all lanes alike)
           long long before = 0;
           int chunk = 0;
+#pragma unroll 1
           for (;; chunk += 32) {
-            const long long mine = chunk + lane < n_chunks ? chunks[chunk + lane].line : 0, upto = before + upto_lane(mine);
+            if (!few) {
+              mine = chunk + lane < n_chunks ? chunks[chunk + lane].line : 0;
+              upto = before + upto_lane(mine);
+            }
             const uint32_t here = __ballot_sync(0xffffffffu, w.u < upto);
             const int at = here ? __ffs(here) - 1 : 31;
             before = __shfl_sync(0xffffffffu, here ? upto - mine : upto, at);
@@ -523,11 +540,20 @@ __global__ void __launch_bounds__(kThreads, 1)
               break;
             }
           }
-          w.s = chunk * per_chunk - 1;
-          for (long long line = 0;; before += line) {
-            next_sequence();
-            line = (long long)w.tiles * (w.steps + kTileCost) * p.Hkv;
-            if (w.u < before + line) break;
+          if (few) {
+            w.s = chunk;
+            w.q = {__shfl_sync(0xffffffffu, of_lane.row, chunk), __shfl_sync(0xffffffffu, of_lane.n, chunk), __shfl_sync(0xffffffffu, of_lane.len, chunk),
+                   __shfl_sync(0xffffffffu, of_lane.key, chunk)};
+            w.tiles = tiles_of(w.q);
+            w.steps = steps_of(w.q);
+          } else {
+            w.s = chunk * per_chunk - 1;
+#pragma unroll 1
+            for (long long line = 0;; before += line) {
+              next_sequence();
+              line = (long long)w.tiles * (w.steps + kTileCost) * p.Hkv;
+              if (w.u < before + line) break;
+            }
           }
           const long long rest = w.u - before, at = quotient(rest, w.steps + kTileCost);  // tile of all heads
           w.off = (int)(rest - at * (w.steps + kTileCost));
@@ -539,24 +565,26 @@ __global__ void __launch_bounds__(kThreads, 1)
             w.off = 0;
           }
         }
+        __syncwarp();
       }
-      // Part n + 1 is announced with the first step of part n, and its Q brought to L2: it comes from memory, in 3000 clocks, and copies behind it would wait as long.
+      // Part n + 1 is announced with the first step of part n.
       // (Little code for a tile like the one before, in registers: K waits for it.  By one thread from shared memory it took 2400 clocks, and 12 heads x 32760 over 512
       // 112 us.)  n = -1: no steps.
-      int g = 0, a = 0, b = 1, h = 0, key = 0, row = 0, len = 0;
+      int g = 0, n_steps = 1, ends = 0, h = 0, key = 0, row = 0;
+      bool any = true;
 #pragma unroll 1
-      for (int n = -1; b >= 0; ++n) {
-        int next_a = 0, next_b = 0, next_h = 0, next_key = 0, next_row = 0, next_len = 0;
+      for (int n = -1; any; ++n) {
 #pragma unroll 1
-        for (int i = a; i < b; ++i) {
+        for (int i = 0; i < n_steps; ++i) {
           const int st = g % R::kStages;
           if (n >= 0 && ok && (g < R::kStages || timed_wait(&sh.k_empty[st], (g / R::kStages - 1) & 1))) {
             if (lane == 0) {  // (of a pair's products each CTA has half of the keys that they take)
               expect(&sh.k_full[st], R::kBytes);
-              copy(smem + kOffK + st * R::kBytes, &map_k, &sh.k_full[st], key + i * kKeyStep + rank * (keys_read(len - i * kKeyStep) >> 1), 0, h, 0);
+              copy(smem + kOffK + st * R::kBytes, &map_k, &sh.k_full[st], key + rank * (keys_read(i == n_steps - 1 ? ends : kKeyStep) >> 1), 0, h, 0);
             }
             ++g;
-            if (i == a && (n < 2 || timed_wait(&sh.q_empty[n & 1], ((n - 2) >> 1) & 1)) && lane == 0) {
+            key += kKeyStep;
+            if (i == 0 && (n < 2 || timed_wait(&sh.q_empty[n & 1], ((n - 2) >> 1) & 1)) && lane == 0) {
               unsigned char *q = smem + kOffQ + (n & 1) * kTileBytes;
               expect(&sh.q_full[n & 1], 2 * (128 / p.G * p.G) * 128);
               copy(q, &map_q, &sh.q_full[n & 1], 0, row, 0, h);
@@ -564,12 +592,13 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             __syncwarp();
           }
-          if (i == a) {
+          if (i == 0) {
             const int m = n + 1;
             if (ok && m >= kPartRing) timed_wait(&sh.part_empty[m % kPartRing], (m / kPartRing - 1) & 1);
+            Part &x = sh.part[m % kPartRing];  // (this warp alone writes the ring)
             // the tile at u
-            next_b = -1;
-            if (w.u < w.end) {
+            any = w.u < w.end;
+            if (any) {
               if (__builtin_expect(w.tile == w.tiles, 0)) {
                 w.tile = 0;
                 if (++w.h == p.Hkv) {
@@ -579,43 +608,48 @@ __global__ void __launch_bounds__(kThreads, 1)
                   while (w.tiles == 0 && w.s + 1 < ix.S);
                 }
               }
-              const int first = (w.tile * kCtas + rank) * tokens_per_tile;
-              next_a = 0, next_b = w.steps, next_h = w.h, next_key = w.q.key, next_row = w.q.row + first, next_len = w.q.len;
-              int c0 = worker, parts = 1;
+              int a = 0, b = w.steps, c0 = worker, parts = 1;
               const long long tile_at = w.u - w.off;
-              if (__builtin_expect(!whole && (w.off > 0 || w.end - w.u < w.steps + kTileCost), 0)) {
-                next_a = max(w.off - kTileCost, 0);
-                next_b = (int)min((long long)w.steps, w.end - tile_at - kTileCost);
-                if (next_b - next_a < w.steps) {
-                  c0 = (int)quotient(tile_at + kTileCost, share);
-                  parts = (int)quotient(tile_at + kTileCost + w.steps - 1, share) - c0 + 1;
-                }
-                if (next_b <= next_a) next_b = -1;  // (the share ends before the tile's first step)
-              }
-              w.u = next_b < 0 ? w.end : tile_at + kTileCost + next_b;
-              w.off = 0;
-              if (lane == 0 && next_b >= 0) {
-                if (parts > 1) sh.owed[sh.n_owed++] = make_int4(2 * blockIdx.x + (next_a == 0 ? 1 : 0), c0 * kCtas + rank, parts, 0);
-                if (ok) {
-                  int4 *const x = reinterpret_cast<int4 *>(&sh.part[m % kPartRing]);
-                  x[0] = make_int4(next_row, min(tokens_per_tile, max(w.q.n - first, 0)), next_h, next_key);
-                  x[1] = make_int4(w.q.len, w.steps, next_a, next_b);
-                  x[2] = make_int4(c0, parts, 0, 0);
-                  tma_prefetch_5d(&map_q, 0, 0, next_row, 0, next_h);
-                  tma_prefetch_5d(&map_q, 0, 0, next_row, 1, next_h);
+              if (__builtin_expect(w.off > 0 || w.end - w.u < w.steps + kTileCost, 0)) {
+                const long long share = sh.share;
+                if (share > 0) {
+                  a = max(w.off - kTileCost, 0);
+                  b = (int)min((long long)w.steps, w.end - tile_at - kTileCost);
+                  if (b - a < w.steps) {
+                    c0 = (int)quotient(tile_at + kTileCost, share);
+                    parts = (int)quotient(tile_at + kTileCost + w.steps - 1, share) - c0 + 1;
+                  }
+                  any = b > a;  // (else the share ends before the tile's first step)
                 }
               }
-              ++w.tile;
+              if (any) {
+                const int first = (w.tile * kCtas + rank) * tokens_per_tile;
+                if (lane == 0) {
+                  if (parts > 1) sh.owed[sh.n_owed++] = make_int4(2 * blockIdx.x + (a == 0 ? 1 : 0), c0 * kCtas + rank, parts, 0);
+                  if (ok) {  // (after an abort only what is owed is put down)
+                    int4 *const to = reinterpret_cast<int4 *>(&x);
+                    to[0] = make_int4(w.q.row + first, min(tokens_per_tile, max(w.q.n - first, 0)), w.h, w.q.key + a * kKeyStep);
+                    to[1] = make_int4(b - a, b < w.steps ? kKeyStep : w.q.len - (w.steps - 1) * kKeyStep, a, b - a == w.steps);
+                    to[2] = make_int4(c0, parts, 0, 0);
+                  }
+                }
+                w.u = tile_at + kTileCost + b;
+                w.off = 0;
+                ++w.tile;
+              }
             }
-            if (lane == 0 && ok) {  // (after an abort only what is owed is put down)
-              if (next_b < 0) sh.part[m % kPartRing].b = -1;
+            if (lane == 0 && ok) {
+              if (!any) x.steps.x = -1;
               mbar_arrive(&sh.part_full[m % kPartRing]);
             }
             __syncwarp();
           }
           if (!ok) break;
         }
-        a = next_a, b = next_b, h = next_h, key = next_key, row = next_row, len = next_len;
+        const Part &x = sh.part[(n + 1) % kPartRing];
+        const int4 head = *reinterpret_cast<const int4 *>(&x);
+        n_steps = x.steps.x, ends = x.steps.y, row = head.x, h = head.z, key = head.w;
+        if (!ok) n_steps = 1;
       }
       if (ok) timed_wait(&sh.finished, 0);
     } else if (warp == kWarpV) {
@@ -625,15 +659,16 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll 1
       for (int n = 0; ok; ++n) {
         const Part *x = part_at(n);
-        if (x == nullptr) break;
-        const int a = x->a, b = x->b, h = x->h, key = x->key, ends = last_keys(x);
+        if (x == nullptr || x->steps.x < 0) break;
+        const int4 steps = x->steps;
+        const int n_steps = steps.x, h = x->h, key = x->key;
         done_with_part(n);
 #pragma unroll 1
-        for (int i = a; i < b; ++i, ++g) {
+        for (int i = 0; i < n_steps; ++i, ++g) {
           const int st = g % R::kStages;
           if (g >= R::kStages && !wait(&sh.v_empty[st], (g / R::kStages - 1) & 1)) break;
           unsigned char *const to = smem + kOffV + st * R::kBytes;
-          const int keys = i == b - 1 ? ends : kKeyStep;
+          const int keys = i == n_steps - 1 ? steps.y : kKeyStep;
           const bool tail = (keys & 15) || keys == 0;
 #ifdef HEART_TEST_HOOKS
           if (!(p.test_skip && blockIdx.x == 0 && g == 1))
@@ -677,8 +712,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll 1
       for (int n = 0; ok; ++n) {
         const Part *x = part_at(n);
-        if (x == nullptr) break;
-        const int n_steps = x->b - x->a, ends = last_keys(x);
+        if (x == nullptr || x->steps.x < 0) break;
+        const int n_steps = x->steps.x, ends = x->steps.y;
         done_with_part(n);
         wait(&sh.q_full[n & 1], (n >> 1) & 1);
         const uint64_t qd = desc_at(q_desc, (n & 1) * (kTileBytes >> 4));
@@ -715,8 +750,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll 1
       for (int n = 0; ok; ++n) {
         const Part *x = part_at(n);
-        if (x == nullptr) break;
-        const int n_steps = x->b - x->a, ends = last_keys(x);
+        if (x == nullptr || x->steps.x < 0) break;
+        const int n_steps = x->steps.x, ends = x->steps.y;
         done_with_part(n);
         if (n > 0) wait(&sh.o_free, (n - 1) & 1);
 #pragma unroll 1
@@ -728,11 +763,17 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (leader) {
             const uint64_t vd = desc_at(v_desc, st * (R::kBytes >> 4));
             const int ks_end = i == n_steps - 1 ? values_read(ends) >> 4 : 8;
+            auto product = [&](int ks) {
+              const uint64_t at = desc_at(vd, ks * 128);
+              if (Pair) mma_ts_pair(tmem, tmem + 384 + b * 64 + ks * 8, at, idesc, (i > 0 || ks > 0) ? 1u : 0u);
+              else mma_ts(tmem, tmem + 384 + b * 64 + ks * 8, at, idesc, (i > 0 || ks > 0) ? 1u : 0u);
+            };
+            if (__builtin_expect(ks_end == 8, 1)) {
 #pragma unroll
-            for (int ks = 0; ks < 8; ++ks) {
-              if (ks >= ks_end) break;
-              if (Pair) mma_ts_pair(tmem, tmem + 384 + b * 64 + ks * 8, desc_at(vd, ks * 128), idesc, (i > 0 || ks > 0) ? 1u : 0u);
-              else mma_ts(tmem, tmem + 384 + b * 64 + ks * 8, desc_at(vd, ks * 128), idesc, (i > 0 || ks > 0) ? 1u : 0u);
+              for (int ks = 0; ks < 8; ++ks) product(ks);
+            } else {
+#pragma unroll 1
+              for (int ks = 0; ks < ks_end; ++ks) product(ks);
             }
             if (i == n_steps - 1) commit(&sh.o_full[n & 1]);
             commit(&sh.pv_done[b]);
@@ -761,12 +802,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int n = 0; ok; ++n) {
       const Part *x = part_at(n);
       if (x == nullptr) break;
-      const int n_steps = x->b - x->a, ends = last_keys(x);
+      const int4 steps = x->steps;
+      const int n_steps = steps.x, ends = steps.y;
+      if (n_steps < 0) break;
       float m_ref = kNoReference, l_run = 0.f;
 #pragma unroll 1
       for (int h = (w ^ g0) & 1; h < n_steps; h += 2) {
         const uint32_t g = g0 + h;
-        if (!wait2(&sh.m_ready[w ^ 1][quarter], ((g - 1) >> 1) & 1, &sh.s_full[w], (g >> 1) & 1)) break;  // (the phase before the first one counts as past)
+        if (!wait(&sh.m_ready[w ^ 1][quarter], ((g - 1) >> 1) & 1) || !wait(&sh.s_full[w], (g >> 1) & 1)) break;  // (the phase before the first one counts as past)
         tc_fence_after();
         const float m_prev = h > 0 ? sh.m[row] : kNoReference;
         bool moved = false;
@@ -786,59 +829,40 @@ __global__ void __launch_bounds__(kThreads, 1)
         };
         uint64_t sums[2] = {0ull, 0ull};
         const int keys = h == n_steps - 1 ? ends : kKeyStep;
-        if (__builtin_expect(keys > 32, 1)) {
-          if (__builtin_expect(keys < kKeyStep, 0)) {  // scores behind the last key
-            int k = keys;
+        // (A way of its own for up to 32 keys took 12 heads x 32760 over 16 from 54 us to 47, and over 128, 512 from 54.7 to 56.6, 108 to 111: code that is in the way.)
+        if (__builtin_expect(keys < kKeyStep, 0)) {  // scores behind the last key
+          int k = keys;
 #pragma unroll 1
-            for (; k & 7; ++k) tmem_st1(s_at + k, 0xff800000u);
+          for (; k & 7; ++k) tmem_st1(s_at + k, 0xff800000u);
 #pragma unroll 1
-            for (; k < kKeyStep; k += 8) tmem_st8_fill(s_at + k, 0xff800000u);
-            tmem_wait_st();
-          }
-          uint32_t s[128], pk[32];
-#pragma unroll
-          for (int q = 0; q < 4; ++q) tmem_ld32(s_at + q * 32, *reinterpret_cast<uint32_t(*)[32]>(&s[q * 32]));
-          l_run *= ex2(m_ref - m_prev);
-          m_ref = m_prev;
-          tmem_wait_ld();
-          arrive(&sh.s_free[w]);
-          uint64_t neg_m2;
-          bool again = false;
-#pragma unroll 1
-          do {  // (the first weights with the reference before, while the maximum is found)
-            neg_m2 = pack_f32x2(-m_ref, -m_ref);
-            sums[0] = sums[1] = 0ull;
-            exp32<false>(&s[0], c2, neg_m2, &pk[0], sums);
-            const float x_max = fmaxf(max64(&s[0]), max64(&s[64])) * c;
-            again = !again && new_reference(x_max);
-          } while (__builtin_expect(again, 0));
-          const bool p_done = g < 2 || mbar_test_wait(&sh.pv_done[w], ((g - 2) >> 1) & 1);
-          exp32<false>(&s[32], c2, neg_m2, &pk[16], sums);
-          if (__builtin_expect(!__all_sync(0xffffffffu, p_done), 0)) wait(&sh.pv_done[w], ((g - 2) >> 1) & 1);
-          tc_fence_after();
-          tmem_st32(p_at, pk);
-          exp32<false>(&s[64], c2, neg_m2, &pk[0], sums);
-          exp32<false>(&s[96], c2, neg_m2, &pk[16], sums);
-          tmem_st32(p_at + 32, pk);
-        } else {
-          uint32_t s[32], pk[16];
-          tmem_ld32(s_at, s);
-          l_run *= ex2(m_ref - m_prev);
-          m_ref = m_prev;
-          tmem_wait_ld();
-          arrive(&sh.s_free[w]);
-          float x_max = -INFINITY;
-#pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            if (j >= keys) s[j] = 0xff800000u;
-            x_max = fmaxf(x_max, __uint_as_float(s[j]));
-          }
-          new_reference(x_max * c);
-          if (!wait(&sh.pv_done[w], ((g - 2) >> 1) & 1)) break;
-          tc_fence_after();
-          exp32<false>(s, c2, pack_f32x2(-m_ref, -m_ref), pk, sums);
-          tmem_st16(p_at, pk);
+          for (; k < kKeyStep; k += 8) tmem_st8_fill(s_at + k, 0xff800000u);
+          tmem_wait_st();
         }
+        uint32_t s[128], pk[32];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) tmem_ld32(s_at + q * 32, *reinterpret_cast<uint32_t(*)[32]>(&s[q * 32]));
+        l_run *= ex2(m_ref - m_prev);
+        m_ref = m_prev;
+        tmem_wait_ld();
+        arrive(&sh.s_free[w]);
+        uint64_t neg_m2;
+        bool again = false;
+#pragma unroll 1
+        do {  // (the first weights with the reference before, while the maximum is found)
+          neg_m2 = pack_f32x2(-m_ref, -m_ref);
+          sums[0] = sums[1] = 0ull;
+          exp32<false>(&s[0], c2, neg_m2, &pk[0], sums);
+          const float x_max = fmaxf(max64(&s[0]), max64(&s[64])) * c;
+          again = !again && new_reference(x_max);
+        } while (__builtin_expect(again, 0));
+        const bool p_done = g < 2 || mbar_test_wait(&sh.pv_done[w], ((g - 2) >> 1) & 1);
+        exp32<false>(&s[32], c2, neg_m2, &pk[16], sums);
+        if (__builtin_expect(!__all_sync(0xffffffffu, p_done), 0)) wait(&sh.pv_done[w], ((g - 2) >> 1) & 1);
+        tc_fence_after();
+        tmem_st32(p_at, pk);
+        exp32<false>(&s[64], c2, neg_m2, &pk[0], sums);
+        exp32<false>(&s[96], c2, neg_m2, &pk[16], sums);
+        tmem_st32(p_at + 32, pk);
         float s0, s1, s2, s3;
         unpack_f32x2(sums[0], s0, s1);
         unpack_f32x2(sums[1], s2, s3);
@@ -853,11 +877,11 @@ __global__ void __launch_bounds__(kThreads, 1)
               if (!wait(&sh.l_ready[at][quarter], phase)) break;
               l = fmaf(sh.l[at][row], ex2(m_prev - m_ref), l);
             }
-            if (__builtin_expect(x->b - x->a == x->steps, 1)) {
-              sh.l[at][row] = l == 0.f ? 0.f : 1.f / l;
+            if (__builtin_expect(steps.w, 1)) {
+              sh.l[at][row] = l == 0.f ? 0.f : reciprocal(l);
               if (p.lse != nullptr && row < x->tokens * p.G) *lse_of(x, row) = l == 0.f ? -INFINITY : (m_ref + log2f(l)) * 0.6931471805599453f;
             } else {
-              __stcg(&p.part_l[(2 * blockIdx.x + (x->a == 0 ? 1 : 0)) * 128 + row], make_float2(l, m_ref));
+              __stcg(&p.part_l[(2 * blockIdx.x + (steps.z == 0 ? 1 : 0)) * 128 + row], make_float2(l, m_ref));
             }
           } else {
             sh.l[at][row] = l_run;
@@ -933,8 +957,10 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 cudaError_t launch_cross_tiles(const CrossGeom &g, const CacheIndex &ix, const CrossWorkspace &w, const void *Q, const void *K, const void *V, void *O,
                                float *lse, cudaStream_t s, int *launches) {
-  // Pairs of CTAs, where a sequence may have more rows than a tile.
-  const bool pair = (long long)g.max_q > 128 / g.G;
+  // Pairs of CTAs, where a sequence may have more rows than a tile, if there are many tiles a CTA or more keys and values than L2 keeps.  (Half of the traffic against an
+  // uneven finish: 2 x 40 heads x 32760 over 343 541 us, 607 by single CTAs; 12 heads x 18720 over 512 71 and 71, x 4680 29 and 24; x 4608 over 32760 793 and 1090.)
+  const long long tiles = ((long long)g.T * g.G + 127) / 128 * g.Hkv, keys_bytes = (long long)g.Tk * g.Hkv * 4 * kD;
+  const bool pair = (long long)g.max_q > 128 / g.G && (tiles >= 16 * kCacheCtas || keys_bytes > 64 << 20);
   CUtensorMap mq, mk, mv, mo;
   if (!make_query_map(&mq, Q, g) || !make_query_map(&mo, O, g) || !make_states_map(&mk, K, g, pair ? kKeyStep / 2 : kKeyStep, 2) ||
       !make_states_map(&mv, V, g, kKeyStep, pair ? 1 : 2))

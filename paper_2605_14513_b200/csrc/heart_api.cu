@@ -146,7 +146,7 @@ int heart::make_cross_geom(const heart_cross_config *c, CrossGeom *g) {
   g->qh = q_plain ? kD : c->q_stride_h;
   g->kt = kv_plain ? (long long)c->Hkv * kD : c->kv_stride_t;
   g->kh = kv_plain ? kD : c->kv_stride_h;
-  if (!strides_ok(g->qt, g->qh) || !strides_ok(g->kt, g->kh)) return HEART_ERR_INVALID;
+  if (!strides_ok(g->qt, g->qh) || !strides_ok(g->kt, g->kh) || !strides_ok(g->G * g->qh, kD)) return HEART_ERR_INVALID;  // (from key head to key head)
   if (!isfinite(c->scale)) return HEART_ERR_INVALID;
   g->scale = c->scale > 0.0 ? c->scale : 1.0 / sqrt((double)kD);
   if (g->scale < 1e-30 || g->scale > 1e30) return HEART_ERR_INVALID;  // (a normal fp32 number)

@@ -111,12 +111,6 @@ __device__ __forceinline__ void tma_load_5d(void *smem_dst, const CUtensorMap *m
       "r"(c3), "r"(c4)
       : "memory");
 }
-// A box into the L2 cache.
-__device__ __forceinline__ void tma_prefetch_5d(const CUtensorMap *map, int c0, int c1, int c2, int c3, int c4) {
-  asm volatile("cp.async.bulk.prefetch.tensor.5d.L2.global [%0, {%1, %2, %3, %4, %5}];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2),
-               "r"(c3), "r"(c4)
-               : "memory");
-}
 // A box from shared memory (the fence of its writers is behind them), as a group of its own; rows outside the tensor are left out.
 __device__ __forceinline__ void tma_store_5d(const CUtensorMap *map, const void *smem_src, int c0, int c1, int c2, int c3, int c4) {
   asm volatile("cp.async.bulk.tensor.5d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5, %6}], [%1];" ::"l"(

@@ -41,7 +41,7 @@ BAD = [(dict(S=0), 1), (dict(T=0), 1), (dict(Tk=0), 1), (dict(Hq=0), 1), (dict(H
        (dict(Hq=2 * 129), 2), (dict(D=64), 2), (dict(flags=1), 1), (dict(T=1 << 28), 2), (dict(Tk=(1 << 31) - 1), 2), (dict(S=1 << 30), 2),
        (dict(scale=math.nan), 1), (dict(scale=math.inf), 1), (dict(scale=1e31), 1), (dict(scale=1e-31), 1), (dict(q_stride_t=1024), 1),
        (dict(q_stride_t=1020, q_stride_h=128), 1), (dict(q_stride_t=64, q_stride_h=128), 1), (dict(kv_stride_t=-256, kv_stride_h=128), 1),
-       (dict(kv_stride_h=128), 1), (dict(q_stride_t=1 << 40, q_stride_h=128), 1)]
+       (dict(kv_stride_h=128), 1), (dict(q_stride_t=1 << 40, q_stride_h=128), 1), (dict(Hq=128, Hkv=2, q_stride_t=128, q_stride_h=1 << 37), 1)]
 
 
 @pytest.mark.parametrize("change,code", BAD)

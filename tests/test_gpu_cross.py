@@ -1,5 +1,6 @@
 """Cross attention on the GPU, against the definition in 64 bits."""
 import math
+import time
 
 import pytest
 import torch
@@ -20,7 +21,7 @@ class Case:
     """q, k: queries and states of each sequence.  layout of the states: packed in order, "padded" (a constant pitch), "shuffled" (packed in another order),
     "shared" (all sequences begin at row 1), or "fused" (halves of one projection's rows).  What is no sequence's holds no numbers."""
 
-    def __init__(self, q, k, Hq=2, Hkv=1, layout="packed", scale=0.0, pad=3, seed=0, gain=1.3, fused_q=False):
+    def __init__(self, q, k, Hq=2, Hkv=1, layout="packed", scale=0.0, pad=3, seed=0, gain=1.3, fused_q=False, pad_k=0):
         self.q, self.k, self.Hq, self.Hkv, self.scale = list(q), list(k), Hq, Hkv, scale
         g = torch.Generator().manual_seed(seed)
         S = self.S = len(self.q)
@@ -36,7 +37,7 @@ class Case:
                 first[s] = at
                 at += k[s]
         self.first = first
-        self.Tk = max(max(f + n for f, n in zip(first, k)), 1) + (2 if layout in ("padded", "shuffled") else 0)
+        self.Tk = max(max(f + n for f, n in zip(first, k)), 1) + (2 if layout in ("padded", "shuffled") else 0) + pad_k
 
         def normal(*shape, k=1.0):
             return (torch.randn(shape, generator=g) * k).to(torch.bfloat16)
@@ -170,6 +171,60 @@ def test_attention(heart, name):
         R, _ = d.attention()
         assert same(P, R)
     assert heart.heart_get_status(d.ws) == 0
+
+
+PAIRS = ("77 states", "a chunk over a text", "whole tiles", "shared states", "five and seven query heads", "three query heads", "long states", "one step of 16",
+         "a step and a state", "large logits", "many sequences", "40 sequences")
+
+
+@pytest.mark.parametrize("name", PAIRS)
+def test_large_tensors_of_states(heart, name):
+    """More than 64 MB of keys and values, most of them no sequence's: two CTAs share what they read."""
+    c = Case(**CASES[name], seed=len(name), pad_k=140000 // CASES[name].get("Hkv", 1))
+    d = Device(heart, c, max_q=0)
+    O, lse = d.attention()
+    assert heart.heart_get_status(d.ws) == 0
+    check(c, O, lse)
+    P, _ = d.attention(lse=False)
+    assert same(O, P)
+
+
+@pytest.mark.parametrize("q,k", [([4700, 0, 130, 4700], [70, 9, 1, 300]), ([9500], [33])])
+def test_many_tiles_a_cta(heart, q, k):
+    c = Case(q, k, Hq=32, Hkv=32, layout="fused", seed=sum(q))
+    d = Device(heart, c)
+    O, lse = d.attention()
+    assert heart.heart_get_status(d.ws) == 0
+    check(c, O, lse)
+
+
+@pytest.mark.parametrize("name", ["rows", "tiles", "shared tiles", "pairs", "shared tiles of pairs"])
+def test_a_wait_that_runs_out_is_reported(heart, name):
+    """In the test-hook build a flag makes one CTA leave out a copy: its waits run out after a millisecond, the status tells, and the next
+    call in the same workspace is right."""
+    from paper_2605_14513_b200 import build
+
+    product = heart.lib()
+    q, k = {"rows": ([1], [8192])}.get(name, ([200, 700], [600, 300]) if "shared" not in name else ([300], [4000]))
+    c = Case(q, k, Hq=2, Hkv=2, pad_k=70000 if "pairs" in name else 0)
+    try:
+        heart._lib = heart.load(build.build_test_hooks())
+        d = Device(heart, c)
+        want = d.attention()
+        assert heart.heart_get_status(d.ws) == 0
+        check(c, *want)
+        d.cfg.flags = 0x80000000
+        t0 = time.perf_counter()
+        d.attention()
+        assert heart.heart_get_status(d.ws) == heart.ERR_DEVICE_CHECK
+        assert time.perf_counter() - t0 < 5.0
+        d.cfg.flags = 0
+        for _ in range(3):
+            O, lse = d.attention()
+            assert heart.heart_get_status(d.ws) == 0
+            assert same(O, want[0]) and same(lse, want[1])
+    finally:
+        heart._lib = product
 
 
 @pytest.mark.parametrize("q,max_q", [(6, 6), (6, 0), (140, 140)])
