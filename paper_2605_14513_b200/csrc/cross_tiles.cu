@@ -17,8 +17,8 @@
 //     Parts of a tile go to the workspace; the CTA that brings the last one puts them together, in order: the result does not depend on which one
 //     that is.
 //
-// Measured, 12 heads of 128: 32760 queries over 512 keys 108 us (955 TFLOP/s), over 128 54.7 (traffic: 202 MB, 3.7 TB/s), 4680 over 512 23.3, 1000 over 33k 192
-// (by pairs, 2 x 40 heads x 32760 over 343 533 us, 863 TFLOP/s and 2.5 TB/s).
+// Measured, 12 heads of 128: 32760 queries over 512 keys 108 us (955 TFLOP/s), over 128 54.7 (traffic: 202 MB, 3.7 TB/s), 4680 over 512 23.4, 1000 over 33k 181
+// (by pairs, 2 x 40 heads x 32760 over 343 523 us, 880 TFLOP/s and 2.5 TB/s).
 //
 // Warp roles: 0-3, 4-7 softmax; 8 issues S = Q K^T; 9 copies V; 10 finds the CTA's parts, copies K and Q; 11 issues O += P V; 12-15 write.
 // Tensor memory: O (128 columns) | S[2] (2 x 128) | P[2] (2 x 64).
@@ -39,8 +39,10 @@ constexpr int kRegsSoftmax = 184, kRegsOut = 80, kRegsHelper = 64;  // 184 * 256
 static_assert(kRegsSoftmax * 256 + kRegsOut * 128 + kRegsHelper * 128 <= kThreads * 128, "registers at launch");
 constexpr int kTileBytes = 32768;  // 128 rows x 128 dims: [2 dim halves][128 rows][64] bf16, 128-byte swizzle
 constexpr int kTileCost = 1;       // of a tile besides its steps, in steps
-constexpr int kWholeSteps = 8;     // tiles of no more steps are not shared
-constexpr int kMaxParts = 12;      // of a tile, about
+// Tiles of no more steps are not shared: an uneven finish costs half of a tile, parts 5 us.  (12 heads x 9000 over 1500, 12 steps, 78 us, 84 with parts; over 2000, 16
+// steps, 100 and 105, but x 3500 53.6 and 52.5; over 2600, 21 steps, 127 and 133, but x 3500 66.9 and 63.)
+constexpr int kWholeSteps = 16;
+constexpr int kMaxParts = 16;      // of a tile, about (8 heads of one key head x 64 over 32760 40.9 us, with 32 parts 46.8)
 constexpr int kPartRing = 4;
 constexpr int kReaders = 15;       // of announced parts: softmax and writing warps, issuers, V producer
 constexpr float kNoReference = -3.0e38f;
@@ -85,7 +87,7 @@ struct CrossShared {
   uint64_t drain[2];
   uint64_t staged, stage_free;  // 64 dims of a tile's rows are in shared memory; have left it
   uint64_t finished;       // the other warps are through
-  uint64_t stored, told;   // this CTA's part of a tile is in the workspace; it is the last one or not
+  uint64_t stored;         // this CTA's part of a tile is in the workspace
   Part part[kPartRing];
   float m[128];            // references after the last step that has found them
   float l[2][128];         // of the row sums: the other warpgroup's part, then one over them, per part & 1
@@ -94,7 +96,8 @@ struct CrossShared {
   long long share;         // of the line, a CTA or a pair; 0: whole tiles
   int4 owed[2];            // this CTA's parts of shared tiles: place in the workspace, first CTA of the tile, number of its parts
   int n_owed;
-  int last;
+  int4 merges[2];          // shared tiles that this CTA has brought the last part of: first row, tokens and key head, first CTA, number of parts
+  int n_merges;
   int abort;
 };
 constexpr int kOffQ = 0, kOffK = 2 * kTileBytes, kOffV = 4 * kTileBytes, kOffStage = 6 * kTileBytes, kOffShared = kOffStage + kTileBytes;
@@ -203,10 +206,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_init(&sh.staged, 4);
     mbar_init(&sh.stage_free, 1);
     mbar_init(&sh.stored, 4);
-    mbar_init(&sh.told, 1);
     mbar_init(&sh.finished, kThreads / 32 - 1);
     sh.abort = 0;
-    sh.shared_parts = sh.n_owed = 0;
+    sh.shared_parts = sh.n_owed = sh.n_merges = 0;
     mbar_fence_init();
   }
   if (warp == kWarpK && lane == 0) {
@@ -320,9 +322,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     __syncwarp();
     settle(bar, 0);
   };
-  auto lse_of = [&](const Part *x, int row) {
+  auto lse_of = [&](int first, int h, int row) {
     const int t = (int)(((uint32_t)row * p.inv_G) >> 16);
-    return p.lse + (long long)(x->row + t) * p.Hq + x->h * p.G + row - t * p.G;
+    return p.lse + (long long)(first + t) * p.Hq + h * p.G + row - t * p.G;
   };
 
   // ------------------------------------------------------------------ roles
@@ -389,7 +391,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           stage(y, quad);
         }
       } else {
-        // part of a shared tile: its sums to the workspace (the row sums are there), and if it is the last one, those of all put together
+        // part of a shared tile: its sums to the workspace (the row sums are there); whoever brings the last one puts them together when all else is done
         if (lane == 0) mbar_arrive(&sh.l_read[n & 1]);
         const bool real = row < x->tokens * p.G;
         const int slot = 2 * blockIdx.x + (x->steps.z == 0 ? 1 : 0);
@@ -411,57 +413,18 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (lane == 0) {
             __threadfence();  // (of what the CTA has stored, which the barriers have shown this thread)
             int32_t *const arrivals = &p.arrivals[x->c0 * kCtas + rank];
-            const bool is_last = atomicAdd(arrivals, 1) == x->parts - 1;
-            if (is_last) *arrivals = 0;
-            sh.last = is_last;
+            if (atomicAdd(arrivals, 1) == x->parts - 1) {
+              *arrivals = 0;
+              sh.merges[sh.n_merges++] = make_int4(x->row, x->tokens | x->h << 8, x->c0, x->parts);
+            }
             ++sh.shared_parts;
             __threadfence();
-            mbar_arrive(&sh.told);
           }
           __syncwarp();
         }
-        if (!wait(&sh.told, n_stored & 1)) break;
         ++n_stored;
-        if (sh.last == 0) {
-          done_with_part(n);
-          continue;
-        }
-        auto place = [&](int i) { return 2 * ((x->c0 + i) * kCtas + rank) + (i == 0 ? 1 : 0); };
-        float m = kNoReference, l = 0.f;
-#pragma unroll 1
-        for (int k = 0; k < x->parts; ++k) {
-          const float2 lm = __ldcg(&p.part_l[place(k) * 128 + row]);
-          const float top = fmaxf(m, lm.y);
-          l = fmaf(l, ex2(m - top), lm.x * ex2(lm.y - top));
-          m = top;
-        }
-        if (!stage_free()) break;
-#pragma unroll 1
-        for (int quad = 0; quad < 4; ++quad) {
-          uint32_t v[32], y[16];
-#pragma unroll
-          for (int k = 0; k < 32; ++k) v[k] = 0u;
-#pragma unroll 1
-          for (int k = 0; k < x->parts; ++k) {
-            const int at = place(k);
-            const float top = __ldcg(&p.part_l[at * 128 + row].y);
-            const float4 *src = &p.parts[(size_t)(at * 32 + quad * 8) * 128 + row];
-            float4 z[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) z[j] = __ldcg(src + j * 128);
-            const float f = ex2(top - m);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              v[4 * j] = __float_as_uint(fmaf(z[j].x, f, __uint_as_float(v[4 * j])));
-              v[4 * j + 1] = __float_as_uint(fmaf(z[j].y, f, __uint_as_float(v[4 * j + 1])));
-              v[4 * j + 2] = __float_as_uint(fmaf(z[j].z, f, __uint_as_float(v[4 * j + 2])));
-              v[4 * j + 3] = __float_as_uint(fmaf(z[j].w, f, __uint_as_float(v[4 * j + 3])));
-            }
-          }
-          pack(v, l == 0.f ? 0.f : reciprocal(l), y);
-          stage(y, quad);
-        }
-        if (real && p.lse != nullptr) *lse_of(x, row) = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+        done_with_part(n);
+        continue;
       }
       async_proxy_fence();
       __syncwarp();
@@ -879,7 +842,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             if (__builtin_expect(steps.w, 1)) {
               sh.l[at][row] = l == 0.f ? 0.f : reciprocal(l);
-              if (p.lse != nullptr && row < x->tokens * p.G) *lse_of(x, row) = l == 0.f ? -INFINITY : (m_ref + log2f(l)) * 0.6931471805599453f;
+              if (p.lse != nullptr && row < x->tokens * p.G) *lse_of(x->row, x->h, row) = l == 0.f ? -INFINITY : (m_ref + log2f(l)) * 0.6931471805599453f;
             } else {
               __stcg(&p.part_l[(2 * blockIdx.x + (steps.z == 0 ? 1 : 0)) * 128 + row], make_float2(l, m_ref));
             }
@@ -939,6 +902,39 @@ __global__ void __launch_bounds__(kThreads, 1)
     tc_fence_after();
     if (Pair) tmem_dealloc_pair(tmem, 512);
     else tmem_dealloc(tmem, 512);
+  }
+  // Shared tiles whose last part is here, by all threads: 16 dims of a row at a time.  (By the warpgroup that writes, as soon as a part was the last one, 4 heads x 300 over
+  // 4000, 11 parts a tile, took 94 us.)
+#pragma unroll 1
+  for (int i = 0; i < (gave_up ? 0 : sh.n_merges); ++i) {
+    const int4 x = sh.merges[i];
+    const int row = tid & 127, tokens = x.y & 255, h = x.y >> 8;
+    if (row >= tokens * p.G) continue;
+    const int t = (int)(((uint32_t)row * p.inv_G) >> 16);
+    uint16_t *const to = p.O + (long long)(x.x + t) * p.qt + (long long)(h * p.G + row - t * p.G) * p.qh;
+#pragma unroll 1
+    for (int d = (tid >> 7) * 32, end = d + 32; d < end; d += 16) {
+      float m = kNoReference, l = 0.f, v[16] = {};
+#pragma unroll 2
+      for (int k = 0; k < x.w; ++k) {
+        const int at = 2 * ((x.z + k) * kCtas + rank) + (k == 0 ? 1 : 0);
+        const float2 lm = __ldcg(&p.part_l[at * 128 + row]);
+        const float4 *src = &p.parts[(size_t)(at * 32 + (d >> 2)) * 128 + row];
+        const float4 z0 = __ldcg(src), z1 = __ldcg(src + 128), z2 = __ldcg(src + 256), z3 = __ldcg(src + 384);
+        const float top = fmaxf(m, lm.y), a = ex2(m - top), f = ex2(lm.y - top), z[16] = {z0.x, z0.y, z0.z, z0.w, z1.x, z1.y, z1.z, z1.w, z2.x, z2.y, z2.z, z2.w, z3.x, z3.y, z3.z, z3.w};
+        m = top;
+        l = fmaf(l, a, lm.x * f);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) v[j] = fmaf(z[j], f, v[j] * a);
+      }
+      const float inv = l == 0.f ? 0.f : reciprocal(l);
+      uint32_t y[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[j] = pack_bf16x2(v[2 * j] * inv, v[2 * j + 1] * inv);
+      *reinterpret_cast<uint4 *>(to + d) = make_uint4(y[0], y[1], y[2], y[3]);
+      *reinterpret_cast<uint4 *>(to + d + 8) = make_uint4(y[4], y[5], y[6], y[7]);
+      if (d == 0 && p.lse != nullptr) *lse_of(x.x, h, row) = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+    }
   }
   if (sh.abort && tid == 0) {
     atomicExch(ix.status, HEART_ERR_DEVICE_CHECK);

@@ -148,6 +148,7 @@ CASES = {
     "long states": dict(q=[20, 1], k=[9000, 2100], Hq=2, Hkv=1),
     "one step of 16": dict(q=[500], k=[16], Hq=3, Hkv=3),
     "a step and a state": dict(q=[140, 140], k=[129, 1], layout="shuffled"),
+    "long states of several": dict(q=[200, 70, 300], k=[3000, 2200, 5000], Hq=6, Hkv=2, layout="shuffled"),
     "large logits": dict(q=[140], k=[400], gain=20.0, scale=0.05),
     "small scale": dict(q=[20], k=[400], scale=1e-6),
     "many sequences": dict(q=[(i * 7) % 5 for i in range(700)], k=[(i * 37) % 90 for i in range(700)]),
@@ -173,7 +174,7 @@ def test_attention(heart, name):
     assert heart.heart_get_status(d.ws) == 0
 
 
-PAIRS = ("77 states", "a chunk over a text", "whole tiles", "shared states", "five and seven query heads", "three query heads", "long states", "one step of 16",
+PAIRS = ("77 states", "a chunk over a text", "whole tiles", "shared states", "five and seven query heads", "three query heads", "long states", "long states of several", "one step of 16",
          "a step and a state", "large logits", "many sequences", "40 sequences")
 
 
