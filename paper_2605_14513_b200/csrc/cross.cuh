@@ -49,9 +49,15 @@ cudaError_t launch_cross_tiles(const CrossGeom &g, const CacheIndex &ix, const C
 bool make_states_map(CUtensorMap *m, const void *base, const CrossGeom &g, int rows, int halves);
 
 #ifdef __CUDACC__
-// Sequence s as its arrays describe it, brought into range (and reported) where they do not hold what they should.
-__device__ __forceinline__ Sequence cross_sequence(const CacheIndex &ix, int s) {
-  int r0 = __ldcg(&ix.row_start[s]), r1 = __ldcg(&ix.row_start[s + 1]), len = __ldcg(&ix.kv_len[s]), k0 = __ldcg(&ix.table[s]);
+struct SequenceWords {
+  int r0, r1, len, k0;
+};
+__device__ __forceinline__ SequenceWords cross_sequence_words(const CacheIndex &ix, int s) {
+  return {__ldcg(&ix.row_start[s]), __ldcg(&ix.row_start[s + 1]), __ldcg(&ix.kv_len[s]), __ldcg(&ix.table[s])};
+}
+// A sequence as its arrays describe it, brought into range (and reported) where they do not hold what they should.
+__device__ __forceinline__ Sequence cross_sequence(const CacheIndex &ix, const SequenceWords &w) {
+  int r0 = w.r0, r1 = w.r1, len = w.len, k0 = w.k0;
   const int rows = ix.table_stride;
   if (r0 < 0 || r1 < r0 || r1 > ix.T || len < 0 || len > rows || (len > 0 && (k0 < 0 || k0 > rows - len))) {
     atomicExch(ix.status, HEART_ERR_DEVICE_CHECK);
@@ -61,6 +67,7 @@ __device__ __forceinline__ Sequence cross_sequence(const CacheIndex &ix, int s) 
   }
   return {r0, r1 - r0, len, min(max(k0, 0), rows - len)};
 }
+__device__ __forceinline__ Sequence cross_sequence(const CacheIndex &ix, int s) { return cross_sequence(ix, cross_sequence_words(ix, s)); }
 #endif
 
 }  // namespace heart

@@ -17,7 +17,7 @@
 //     Parts of a tile go to the workspace; the CTA that brings the last one puts them together, in order: the result does not depend on which one
 //     that is.
 //
-// Measured, 12 heads of 128: 32760 queries over 512 keys 108 us (955 TFLOP/s), over 128 54.7 (traffic: 202 MB, 3.7 TB/s), 4680 over 512 23.4, 1000 over 33k 181
+// Measured, 12 heads of 128: 32760 queries over 512 keys 108 us (955 TFLOP/s), over 128 54.7 (traffic: 202 MB, 3.7 TB/s), 4680 over 512 23.4, 1000 over 33k 177
 // (by pairs, 2 x 40 heads x 32760 over 343 523 us, 880 TFLOP/s and 2.5 TB/s).
 //
 // Warp roles: 0-3, 4-7 softmax; 8 issues S = Q K^T; 9 copies V; 10 finds the CTA's parts, copies K and Q; 11 issues O += P V; 12-15 write.
@@ -42,7 +42,6 @@ constexpr int kTileCost = 1;       // of a tile besides its steps, in steps
 // Tiles of no more steps are not shared: an uneven finish costs half of a tile, parts 5 us.  (12 heads x 9000 over 1500, 12 steps, 78 us, 84 with parts; over 2000, 16
 // steps, 100 and 105, but x 3500 53.6 and 52.5; over 2600, 21 steps, 127 and 133, but x 3500 66.9 and 63.)
 constexpr int kWholeSteps = 16;
-constexpr int kMaxParts = 16;      // of a tile, about (8 heads of one key head x 64 over 32760 40.9 us, with 32 parts 46.8)
 constexpr int kPartRing = 4;
 constexpr int kReaders = 15;       // of announced parts: softmax and writing warps, issuers, V producer
 constexpr float kNoReference = -3.0e38f;
@@ -247,7 +246,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     return q;
   };
   auto line_of = [&](const Sequence &q) { return (long long)tiles_of(q) * cost_of(q) * p.Hkv; };
-  Sequence of_lane = {0, 0, 0, 0};
+  SequenceWords of_lane = {0, 0, 0, 0};
   // More than 32 sequences: what they cost, some in a row a thread, for the K producer.
   Chunk *const chunks = reinterpret_cast<Chunk *>(smem + kOffStage);
   const int per_chunk = (ix.S + kThreads - 1) / kThreads, n_chunks = (ix.S + per_chunk - 1) / per_chunk;
@@ -264,7 +263,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       chunks[tid] = mine;
     }
   } else if (warp == kWarpK && lane < ix.S) {  // a lane a sequence
-    of_lane = cross_sequence(ix, lane);
+    of_lane = cross_sequence_words(ix, lane);  // (they are looked at behind the barrier)
   }
   tc_fence_before();
   if (Pair) cluster_sync();  // (the other CTA's barriers are there)
@@ -462,27 +461,31 @@ __global__ void __launch_bounds__(kThreads, 1)
         w.steps = steps_of(w.q);
       };
       {
-        auto upto_lane = [&](long long x) {  // inclusive, over the warp
-#pragma unroll
-          for (int o = 1; o < 32; o <<= 1) {
+        const bool few = ix.S <= 32;
+        const Sequence sequence = few && lane < ix.S ? cross_sequence(ix, of_lane) : Sequence{0, 0, 0, 0};
+        const int lanes = few ? ix.S : 32;  // that there are sequences or chunks for
+        auto upto_lane = [&](long long x) {  // inclusive, over those
+#pragma unroll 1
+          for (int o = 1; o < lanes; o <<= 1) {
             const long long y = __shfl_up_sync(0xffffffffu, x, o);
             if (lane >= o) x += y;
           }
           return x;
         };
-        const bool few = ix.S <= 32;
-        long long total = line_of(of_lane);
-        int longest = total > 0 ? cost_of(of_lane) : 1;
+        long long total = line_of(sequence);
+        int longest = total > 0 ? cost_of(sequence) : 1;
 #pragma unroll 1
         for (int i = few ? n_chunks : lane; i < n_chunks; i += 32) {
           total += chunks[i].line;
           longest = max(longest, chunks[i].longest);
         }
         long long mine = total, upto = upto_lane(mine);
-        total = __shfl_sync(0xffffffffu, upto, 31);
+        total = __shfl_sync(0xffffffffu, upto, lanes - 1);
         longest = __reduce_max_sync(0xffffffffu, longest);
         const bool whole = longest <= kWholeSteps + kTileCost;  // tiles are not shared: a CTA takes those that begin in its share
-        const long long share = max(quotient(total + workers - 1, workers), whole ? 1LL : (long long)(longest + kMaxParts - 1) / kMaxParts);
+        // (A part takes the CTA that puts a tile together 0.6 us, 64 KB at 55 bytes a clock, a step 0.8: of few long tiles about as many parts as steps a part.  4 heads x 300
+        // over 4000 23.0 us, with 11 parts a tile 24.8; x 128 over 9000 25.6, with 16 29.9.)
+        const long long share = max(quotient(total + workers - 1, workers), whole ? 1LL : (long long)sqrtf((float)longest));
         if (lane == 0) sh.share = whole ? 0 : share;
         w.u = worker * share;
         w.end = min(total, w.u + share);
@@ -495,7 +498,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               mine = chunk + lane < n_chunks ? chunks[chunk + lane].line : 0;
               upto = before + upto_lane(mine);
             }
-            const uint32_t here = __ballot_sync(0xffffffffu, w.u < upto);
+            const uint32_t here = __ballot_sync(0xffffffffu, lane < lanes && w.u < upto);
             const int at = here ? __ffs(here) - 1 : 31;
             before = __shfl_sync(0xffffffffu, here ? upto - mine : upto, at);
             if (here) {
@@ -505,8 +508,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           if (few) {
             w.s = chunk;
-            w.q = {__shfl_sync(0xffffffffu, of_lane.row, chunk), __shfl_sync(0xffffffffu, of_lane.n, chunk), __shfl_sync(0xffffffffu, of_lane.len, chunk),
-                   __shfl_sync(0xffffffffu, of_lane.key, chunk)};
+            w.q = {__shfl_sync(0xffffffffu, sequence.row, chunk), __shfl_sync(0xffffffffu, sequence.n, chunk), __shfl_sync(0xffffffffu, sequence.len, chunk),
+                   __shfl_sync(0xffffffffu, sequence.key, chunk)};
             w.tiles = tiles_of(w.q);
             w.steps = steps_of(w.q);
           } else {
@@ -904,7 +907,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     else tmem_dealloc(tmem, 512);
   }
   // Shared tiles whose last part is here, by all threads: 16 dims of a row at a time.  (By the warpgroup that writes, as soon as a part was the last one, 4 heads x 300 over
-  // 4000, 11 parts a tile, took 94 us.)
+  // 4000, 11 parts a tile, took 97 us, now 25.)
 #pragma unroll 1
   for (int i = 0; i < (gave_up ? 0 : sh.n_merges); ++i) {
     const int4 x = sh.merges[i];
