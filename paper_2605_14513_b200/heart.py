@@ -403,41 +403,41 @@ def heart_cache_attn(cfg, Q, cache: Cache, page_table, row_start, kv_len, O, ws,
                   O.data_ptr(), _ptr(lse), ws.data_ptr())
 
 
-def _table_call(cfg, arrays, ws):
-    """Checks the arrays of a table call, (name, tensor, type, entries), and the workspace: on one device, which it returns."""
-    device = ws.get_device()
-    for name, x, dtype, n in arrays:
-        if x.dtype is not dtype or x.numel() != n or x.get_device() != device or not x.is_contiguous():
-            raise ValueError(f"{name} has to be contiguous {dtype} of {n} entries beside the workspace: got {x.dtype} {tuple(x.shape)} on {x.device}")
-    if device < 0 or not ws.is_contiguous() or ws.nbytes < _cache_workspace_bytes(cfg.S, cfg.T, cfg.Hq, cfg.Hkv):
-        raise ValueError(f"the workspace has to have cache_workspace_bytes(cfg) = {cache_workspace_bytes(cfg)} bytes on a GPU")
+def _table_call(fields, names, tensors, sizes, ws):
+    """Checks the int32 arrays of a table call and the workspace: on one device, which it returns."""
+    device, i32 = ws.get_device(), torch.int32
+    for x, n in zip(tensors, sizes):
+        if x.dtype is not i32 or x.numel() != n or x.get_device() != device or not x.is_contiguous():
+            name = names.split()[next(i for i, y in enumerate(tensors) if y is x)]
+            raise ValueError(f"{name} has to be contiguous {i32} of {n} entries beside the workspace: got {x.dtype} {tuple(x.shape)} on {x.device}")
+    if device < 0 or not ws.is_contiguous() or ws.nbytes < _cache_workspace_bytes(*fields[:4]):
+        raise ValueError(f"the workspace has to have cache_workspace_bytes(cfg) = {_cache_workspace_bytes(*fields[:4])} bytes on a GPU")
     return device
 
 
 def heart_cache_extend(cfg, new_len, kv_len, free_pages, free_count, page_table, row_start, ws, slots=None, kv_len_out=None, free_count_out=None):
     """Gives the sequences (kv_len: int32 [S]) pages for new_len more tokens from the stack free_pages (int32 [n_pages], free_count [1] of them) and
     writes page_table, row_start and, if given, slots (int64 [T]).  Lengths and count go to kv_len_out and free_count_out, or are updated in place."""
-    kv_len_out = kv_len if kv_len_out is None else kv_len_out
-    free_count_out = free_count if free_count_out is None else free_count_out
-    S, i32 = cfg.S, torch.int32
-    arrays = [("new_len", new_len, i32, S), ("kv_len", kv_len, i32, S), ("free_pages", free_pages, i32, cfg.n_pages), ("free_count", free_count, i32, 1),
-              ("page_table", page_table, i32, S * cfg.table_stride), ("row_start", row_start, i32, S + 1), ("kv_len_out", kv_len_out, i32, S),
-              ("free_count_out", free_count_out, i32, 1)]
-    if slots is not None:
-        arrays.append(("slots", slots, torch.int64, cfg.T))
-    device = _table_call(cfg, arrays, ws)
-    _launch(lib().heart_cache_extend, device, C.byref(cfg), *(x.data_ptr() for _, x, _, _ in arrays[:8]), _ptr(slots), ws.data_ptr())
+    f = _cache_fields(cfg)
+    S = f[0]
+    tensors = (new_len, kv_len, free_pages, free_count, page_table, row_start, kv_len if kv_len_out is None else kv_len_out,
+               free_count if free_count_out is None else free_count_out)
+    device = _table_call(f, "new_len kv_len free_pages free_count page_table row_start kv_len_out free_count_out", tensors,
+                         (S, S, f[6], 1, S * f[7], S + 1, S, 1), ws)
+    if slots is not None and (slots.dtype is not torch.int64 or slots.numel() != f[1] or slots.get_device() != device or not slots.is_contiguous()):
+        raise ValueError(f"slots has to be contiguous {torch.int64} of {f[1]} entries beside the workspace: got {slots.dtype} {tuple(slots.shape)} on {slots.device}")
+    _launch(lib().heart_cache_extend, device, C.byref(cfg), *[x.data_ptr() for x in tensors], _ptr(slots), ws.data_ptr())
 
 
 def heart_cache_release(cfg, ended, kv_len, free_pages, free_count, page_table, ws, kv_len_out=None, free_count_out=None):
     """Puts the pages of the sequences with ended (uint8 [S]) back on the stack; lengths (0 for those) and count as in heart_cache_extend."""
-    kv_len_out = kv_len if kv_len_out is None else kv_len_out
-    free_count_out = free_count if free_count_out is None else free_count_out
-    S, i32 = cfg.S, torch.int32
-    arrays = [("ended", ended, torch.uint8, S), ("kv_len", kv_len, i32, S), ("free_pages", free_pages, i32, cfg.n_pages), ("free_count", free_count, i32, 1),
-              ("page_table", page_table, i32, S * cfg.table_stride), ("kv_len_out", kv_len_out, i32, S), ("free_count_out", free_count_out, i32, 1)]
-    device = _table_call(cfg, arrays, ws)
-    _launch(lib().heart_cache_release, device, C.byref(cfg), *(x.data_ptr() for _, x, _, _ in arrays), ws.data_ptr())
+    f = _cache_fields(cfg)
+    S = f[0]
+    tensors = (kv_len, free_pages, free_count, page_table, kv_len if kv_len_out is None else kv_len_out, free_count if free_count_out is None else free_count_out)
+    device = _table_call(f, "kv_len free_pages free_count page_table kv_len_out free_count_out", tensors, (S, f[6], 1, S * f[7], S, 1), ws)
+    if ended.dtype is not torch.uint8 or ended.numel() != S or ended.get_device() != device or not ended.is_contiguous():
+        raise ValueError(f"ended has to be contiguous {torch.uint8} of {S} entries beside the workspace: got {ended.dtype} {tuple(ended.shape)} on {ended.device}")
+    _launch(lib().heart_cache_release, device, C.byref(cfg), ended.data_ptr(), *[x.data_ptr() for x in tensors], ws.data_ptr())
 
 
 # ---- Cross attention: to states of another length.
