@@ -308,6 +308,57 @@ def test_captured_calls_follow_the_lengths(heart, max_q):
         check(c, O, lse)
 
 
+@pytest.mark.parametrize("max_q", [4, 200])
+def test_two_graphs_share_a_workspace(heart, max_q):
+    """One after the other, in any order, between plain calls; shared tiles among them."""
+    cases = [Case([max_q, 1], [3000, 20], Hq=2, Hkv=2, seed=1), Case([2, max_q], [5000, 2300], Hq=2, Hkv=1, seed=2)]
+    devices = [Device(heart, c, max_q=max_q) for c in cases]
+    ws = devices[0].ws
+    want = []
+    for d in devices:
+        d.ws = ws
+        want.append(d.attention())
+    for c, w in zip(cases, want):
+        check(c, *w)
+    graphs, out = [], []
+    for d in devices:
+        stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+        stream.wait_stream(torch.cuda.current_stream())
+        O, lse = torch.zeros_like(d.Q), torch.zeros((d.c.T, d.c.Hq), device="cuda")
+        with torch.cuda.graph(graph, stream=stream):
+            heart.heart_cross_attn(d.cfg, d.Q, d.K, d.V, *d.where, O, ws, lse=lse)
+        graphs.append(graph)
+        out.append((O, lse))
+    for i in (0, 1, 1, 0, 0, 1):
+        for x in out[i]:
+            x.fill_(9)
+        graphs[i].replay()
+        other = devices[1 - i].attention()
+        rows = cases[i].rows
+        assert same(out[i][0][:rows], want[i][0][:rows]) and same(out[i][1][:rows], want[i][1][:rows])
+        assert same(other[0], want[1 - i][0]) and same(other[1], want[1 - i][1])
+    assert heart.heart_get_status(ws) == 0
+
+
+@pytest.mark.parametrize("q,k", [([3, 1], [40, 170]), ([150, 60], [200, 33])])
+def test_heads_first_and_rows_ahead(heart, q, k):
+    """Heads are the outer dimension of all tensors; rows before the first sequence are left as they are."""
+    c = Case(q, k, Hq=6, Hkv=2, seed=7)
+    ahead = 5
+    want, want_lse, _ = c.attention()
+    O = torch.full((c.Hq, c.T + ahead, D), 77.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((c.T + ahead, c.Hq), 55.0, device="cuda")
+    Q = torch.full_like(O, math.nan)
+    Q[:, ahead:] = c.Q.transpose(0, 1).cuda()
+    K, V = (x.transpose(0, 1).contiguous().cuda() for x in (c.K, c.V))
+    cfg = heart.make_cross_config(c.S, c.T + ahead, c.Tk, c.Hq, c.Hkv, max_q=max(q), q_strides=(D, (c.T + ahead) * D), kv_strides=(D, c.Tk * D))
+    ws = heart.new_cross_workspace(cfg)
+    heart.heart_cross_attn(cfg, Q, K, V, (c.q_start + ahead).cuda(), c.k_start.cuda(), c.k_len.cuda(), O, ws, lse=lse)
+    assert heart.heart_get_status(ws) == 0
+    assert (O[:, :ahead] == 77).all() and (lse[:ahead] == 55).all()
+    check(c, O[:, ahead:].transpose(0, 1).contiguous(), lse[ahead:])
+
+
 def test_two_streams_with_workspaces_of_their_own(heart):
     cases = [Case([300, 40], [900, 70], Hq=4, Hkv=2, seed=i) for i in range(2)]
     devices = [Device(heart, c) for c in cases]
