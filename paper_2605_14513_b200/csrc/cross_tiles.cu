@@ -40,8 +40,9 @@ static_assert(kRegsSoftmax * 256 + kRegsOut * 128 + kRegsHelper * 128 <= kThread
 constexpr int kTileBytes = 32768;  // 128 rows x 128 dims: [2 dim halves][128 rows][64] bf16, 128-byte swizzle
 constexpr int kTileCost = 1;       // of a tile besides its steps, in steps
 // Tiles of no more steps are not shared: an uneven finish costs half of a tile, parts 5 us.  (12 heads x 9000 over 1500, 12 steps, 78 us, 84 with parts; over 2000, 16
-// steps, 100 and 105, but x 3500 53.6 and 52.5; over 2600, 21 steps, 127 and 133, but x 3500 66.9 and 63.)
-constexpr int kWholeSteps = 16;
+// steps, 100 and 105, but x 3500 53.6 and 52.5; over 2600, 21 steps, 127 and 133, but x 3500 66.9 and 63.)  Nor are tiles of no more than kPartsCost steps beside a CTA's share:
+// where CTAs are left over, parts cost some ten steps.  (8 heads of 8 x 5 over 1250, 10 steps, 16.6 us, 16.3 with parts; over 2000, 16 steps, 21.2 and 17.6.)
+constexpr long long kWholeSteps = 16, kPartsCost = 10;
 constexpr int kPartRing = 4;
 constexpr int kReaders = 15;       // of announced parts: softmax and writing warps, issuers, V producer
 constexpr float kNoReference = -3.0e38f;
@@ -482,10 +483,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         long long mine = total, upto = upto_lane(mine);
         total = __shfl_sync(0xffffffffu, upto, lanes - 1);
         longest = __reduce_max_sync(0xffffffffu, longest);
-        const bool whole = longest <= kWholeSteps + kTileCost;  // tiles are not shared: a CTA takes those that begin in its share
         // (A part takes the CTA that puts a tile together 0.6 us, 64 KB at 55 bytes a clock, a step 0.8: of few long tiles about as many parts as steps a part.  4 heads x 300
         // over 4000 23.0 us, with 11 parts a tile 24.8; x 128 over 9000 25.6, with 16 29.9.)
-        const long long share = max(quotient(total + workers - 1, workers), whole ? 1LL : (long long)sqrtf((float)longest));
+        const long long even = quotient(total + workers - 1, workers), least = (long long)sqrtf((float)longest);
+        const bool whole = longest <= min(kWholeSteps + kTileCost, max(even, least) + kPartsCost);  // tiles are not shared: a CTA takes those that begin in its share
+        const long long share = whole ? max(even, 1LL) : max(even, least);
         if (lane == 0) sh.share = whole ? 0 : share;
         w.u = worker * share;
         w.end = min(total, w.u + share);
