@@ -952,7 +952,8 @@ cudaError_t launch_cross_rows(const CrossGeom &g, const CacheIndex &ix, const Cr
   p.arrivals = w.arrivals;
   p.parts = w.parts;
   p.part_l = w.part_l;
-  return (long long)g.max_q * g.G <= 8 ? launch<1, false, false, true>(p, mk, mv, s, launches) : launch<2, false, false, true>(p, mk, mv, s, launches);
+  const bool eight = (long long)g.max_q * g.G <= 8 || few_rows(g);
+  return eight ? launch<1, false, false, true>(p, mk, mv, s, launches) : launch<2, false, false, true>(p, mk, mv, s, launches);
 }
 
 cudaError_t launch_cache_redo(const CacheGeom &g, const CacheIndex &ix, const CacheWorkspace &w, const void *Q, const heart_cache &c,

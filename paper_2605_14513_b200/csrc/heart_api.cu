@@ -552,8 +552,8 @@ int heart_cross_attn(const heart_cross_config *cfg, const void *Q, const void *K
   ix.table_stride = g.Tk;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   g_launches = 0;
-  cudaError_t e = (long long)g.max_q * g.G <= kRowsOfRowsKernel ? launch_cross_rows(g, ix, w, Q, K, V, O, lse, s, &g_launches)
-                                                                : launch_cross_tiles(g, ix, w, Q, K, V, O, lse, s, &g_launches);
+  const bool rows = (long long)g.max_q * g.G <= kRowsOfRowsKernel || few_rows(g);
+  cudaError_t e = rows ? launch_cross_rows(g, ix, w, Q, K, V, O, lse, s, &g_launches) : launch_cross_tiles(g, ix, w, Q, K, V, O, lse, s, &g_launches);
   if (e != cudaSuccess) return cuda_fail(e, "cross_attention");
   return HEART_OK;
 }

@@ -147,9 +147,14 @@ CASES = {
     "100 query heads a key head": dict(q=[3, 2], k=[150, 33], Hq=100, Hkv=1),
     "long states": dict(q=[20, 1], k=[9000, 2100], Hq=2, Hkv=1),
     "one step of 16": dict(q=[500], k=[16], Hq=3, Hkv=3),
+    "tokens among rows": dict(q=[1, 400, 1, 1], k=[300, 1, 0, 129], Hq=6, Hkv=2),
+    "no state of many rows": dict(q=[300, 200], k=[0, 0], Hq=2, Hkv=2),
+    "no query of many": dict(q=[0, 300, 0, 1], k=[5, 0, 9, 77], Hq=4, Hkv=4),
     "a step and a state": dict(q=[140, 140], k=[129, 1], layout="shuffled"),
     "long states of several": dict(q=[200, 70, 300], k=[3000, 2200, 5000], Hq=6, Hkv=2, layout="shuffled"),
     "large logits": dict(q=[140], k=[400], gain=20.0, scale=0.05),
+    "large logits of many": dict(q=[240], k=[400], gain=20.0, scale=0.05),
+    "small scale of many": dict(q=[420], k=[400], scale=1e-6),
     "small scale": dict(q=[20], k=[400], scale=1e-6),
     "many sequences": dict(q=[(i * 7) % 5 for i in range(700)], k=[(i * 37) % 90 for i in range(700)]),
     "40 sequences": dict(q=[(i * 53) % 150 for i in range(40)], k=[(i * 37) % 190 for i in range(40)], layout="shuffled", Hq=3, Hkv=3),
@@ -250,11 +255,11 @@ def test_only_rows_that_see_a_nan_get_one(heart, q, max_q):
     assert (a[:q].float() - b[:q].float()).abs().max() <= 2 ** -7 * 5
 
 
-@pytest.mark.parametrize("max_q", [1, 0])
-def test_bad_arrays_are_reported(heart, max_q):
+@pytest.mark.parametrize("max_q,many", [(1, 1), (0, 1), (0, 60)])
+def test_bad_arrays_are_reported(heart, max_q, many):
     """Entries out of range: nothing is touched outside the tensors, the status tells, the other sequence is right."""
     for what in ("starts", "end", "descending", "length", "negative length", "first", "negative first"):
-        c = Case([4, 3], [100, 80], Hq=2, Hkv=2, pad=0)
+        c = Case([4 * many, 3 * many], [100, 80], Hq=2, Hkv=2, pad=0)
         d = Device(heart, c, max_q=max_q)
         q_start, k_start, k_len = d.where
         if what == "starts":
@@ -262,7 +267,7 @@ def test_bad_arrays_are_reported(heart, max_q):
         elif what == "end":
             q_start[2] = c.T + 1
         elif what == "descending":
-            q_start[1] = 9
+            q_start[1] = c.T + 2
         elif what == "length":
             k_len[0] = c.Tk + 1
         elif what == "negative length":
@@ -276,9 +281,9 @@ def test_bad_arrays_are_reported(heart, max_q):
         assert heart.heart_get_status(d.ws) == 0
         if what not in ("starts", "end", "descending"):
             want, _, _ = c.attention()
-            assert (O[4:].cpu().double() - want[4:]).abs().max() < 0.05, what
+            assert (O[4 * many:].cpu().double() - want[4 * many:]).abs().max() < 0.05, what
     # of a sequence without states it does not matter where they begin
-    c = Case([4, 3], [0, 80], Hq=2, Hkv=2)
+    c = Case([4 * many, 3 * many], [0, 80], Hq=2, Hkv=2)
     d = Device(heart, c, max_q=max_q)
     d.where[1][0] = -9
     O, lse = d.attention()
@@ -378,10 +383,10 @@ def test_two_streams_with_workspaces_of_their_own(heart):
         check(c, O, lse)
 
 
-@pytest.mark.parametrize("max_q", [1, 0])
-def test_offsets_beyond_32_bits(heart, max_q):
+@pytest.mark.parametrize("max_q,Hq,Hkv", [(1, 2, 1), (0, 2, 1), (0, 10, 5)])
+def test_offsets_beyond_32_bits(heart, max_q, Hq, Hkv):
     """K, V, Q and O of more than 2^32 elements, by their strides."""
-    rows, Hq, Hkv, far = 40, 2, 1, 1 << 27  # (elements between rows)
+    rows, far = 40, 1 << 27  # (elements between rows)
     c = Case([rows], [rows], Hq=Hq, Hkv=Hkv, pad=0)
     room = (rows - 1) * far + Hq * D
     Q, O, K, V = (torch.empty(room, dtype=torch.bfloat16, device="cuda") for _ in range(4))
