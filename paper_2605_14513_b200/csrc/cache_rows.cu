@@ -41,6 +41,10 @@ namespace {
 constexpr int kWarps = 8, kThreads = 32 * kWarps;
 constexpr int kRing = 24576;           // bytes a warp
 constexpr int kMaxStages = 3;
+// Of cross attention, where CTAs have some steps each, a tile's beginning and end count as two more (its copies are waited for with little else in flight, the warps meet
+// twice).  64 single tokens, 12 heads, over 100 to 4000 states took 150 us by steps alone, the CTA with 23 tiles 146 and the middle one 112, and takes 131.  Over 1 to 1000, 60 to 76
+// and 41 to 44 (counted as one 48 to 55, as three or four the same).
+constexpr int kTileCost = 2, kShareWithCost = 4;
 constexpr int kMaxParts = 31;          // of a tile, and one more where shares cross tiles: the last CTA reads them, a lane a part
 constexpr int kApartRows = 6;          // rows of a tile whose sums have a place beside the rings
 constexpr float kNoReference = -3.0e38f;
@@ -77,7 +81,7 @@ struct alignas(16) RowsShared {
   alignas(16) uint8_t scales[kWarps][kMaxStages][64];  // e4m3: of the keys and of the values of a stage
   float2 l[kWarps][16];   // row sums and their references
   float o_ref[kWarps][16];  // e4m3: references of the sums of values
-  long long total[kWarps];
+  long long total[kWarps], tiles[kWarps];
   int longest[kWarps];
   int found;              // sequence of the CTA's first step
   int found_q[4];
@@ -178,6 +182,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   long long share, u, u1, sequence_at, per_head;  // units of a CTA, its first one and the one behind its last; of the sequence, and of one of its heads
   bool one_tile = false;                          // shares do not cross tiles
   int h = 0, t = 0, done = 0;                     // head, tile and the tile's steps before this share
+  int cost = 0, paid = 0;                         // units of a tile ahead of its steps, and how many of this one's lie before the share
+  auto costs = [&](long long steps) { return Cross && steps >= (long long)kShareWithCost * gridDim.x; };
   // to be done again: the next tile of this CTA, whole
   long long pair = 0;
   auto next_redo = [&]() {
@@ -232,6 +238,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     };
     long long total;
     sequence_at = before_lane(per_head * p.Hkv, total);
+    if (costs(total)) {
+      cost = kTileCost;
+      longest += kTileCost;
+      per_head += (long long)kTileCost * tiles_of(q);
+      sequence_at = before_lane(per_head * p.Hkv, total);
+    }
     share = max(quotient(total + gridDim.x - 1, gridDim.x), (long long)(longest + kMaxParts - 1) / kMaxParts);
     // Where each sequence and head is one tile and CTAs are enough, tiles begin with a share (a CTA with the end of one and the beginning of
     // another takes twice as long as the others: 8 heads x 4100 tokens).
@@ -257,28 +269,38 @@ __global__ void __launch_bounds__(kThreads, 1)
     sequence_at = __shfl_sync(0xffffffffu, sequence_at, s);
     per_head = __shfl_sync(0xffffffffu, per_head, s);
   } else {
-    long long total = 0, mine = 0;
+    long long total = 0, tiles = 0, mine = 0;
     for (int i = tid; i < ix.S; i += kThreads) {
       const Sequence x = sequence_at_place(i);
       const long long n = steps_of(x, longest);
       if (i < kThreads) mine = n, q = x;
       total += n * p.Hkv;
+      if (Cross) tiles += (long long)tiles_of(x) * p.Hkv;
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
       total += __shfl_xor_sync(0xffffffffu, total, o);
+      if (Cross) tiles += __shfl_xor_sync(0xffffffffu, tiles, o);
       longest = max(longest, __shfl_xor_sync(0xffffffffu, longest, o));
     }
     if (lane == 0) {
       sh.total[warp] = total;
+      if (Cross) sh.tiles[warp] = tiles;
       sh.longest[warp] = longest;
     }
     __syncthreads();
-    total = 0;
+    total = tiles = 0;
 #pragma unroll
     for (int i = 0; i < kWarps; ++i) {
       total += sh.total[i];
+      if (Cross) tiles += sh.tiles[i];
       longest = max(longest, sh.longest[i]);
+    }
+    if (costs(total)) {
+      cost = kTileCost;
+      longest += kTileCost;
+      total += kTileCost * tiles;
+      mine += (long long)kTileCost * tiles_of(q);
     }
     share = max(quotient(total + gridDim.x - 1, gridDim.x), (long long)(longest + kMaxParts - 1) / kMaxParts);
     u = blockIdx.x * share;
@@ -290,6 +312,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (base > 0) {
         q = base + tid < ix.S ? sequence_at_place(base + tid) : Sequence{0, 0, 0, 0};
         mine = steps_of(q, dummy);
+        mine += (long long)cost * tiles_of(q);
       }
       long long upto = mine * p.Hkv;
 #pragma unroll
@@ -327,8 +350,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     h = (int)quotient(rest, per_head);
     rest -= h * per_head;
     if (!one_tile)
-      for (int k; rest >= (k = span(q, t).steps); ++t) rest -= k;
-    done = (int)rest;
+      for (int k; rest >= (k = span(q, t).steps + cost); ++t) rest -= k;
+    paid = (int)min(rest, (long long)cost);
+    done = (int)rest - paid;
+    if (Cross && u1 - u <= cost - paid) return;  // (no step of the tile; none where shares are as long as those with a cost)
   }
 
   int put = 0, take = 0;            // the stages that come next, to fill and to use
@@ -399,7 +424,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     n_rows = min(kRows, (int)((long long)q.n * p.G) - first_row);
     p0 = position(q, first_row / p.G);
     const int p1 = position(q, (first_row + n_rows - 1) / p.G);
-    end_step = (int)min((long long)steps, done + (u1 - u));
+    end_step = (int)min((long long)steps, done + (u1 - u) - (cost - paid));
     next = done;
     next_batch = done;
     entry = entries(done);
@@ -746,13 +771,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     // this tile's, for the rest of it, before the next one's take their places
     const int rows = n_rows, row0 = first_row, out_row = q.row, out_head = h;
     const bool all = done == 0 && end_step == steps;
-    const long long tile_at = u - done;  // the tile's first step
+    const long long tile_at = u - done + (cost - paid);  // the tile's first step
     const int tile_steps = steps;
     const int part = 2 * blockIdx.x + (done == 0 ? 1 : 0);
-    u += end_step - done;
-    const bool more = Redo ? next_redo() : !one_tile && u < u1;
+    u += end_step - done + (cost - paid);
+    const bool more = Redo ? next_redo() : !one_tile && u + cost < u1;
     if (more) {
-      done = 0;
+      done = paid = 0;
       if (!Redo && ++t == tiles_of(q)) {
         t = 0;
         if (++h == p.Hkv) {
