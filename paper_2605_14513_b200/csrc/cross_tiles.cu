@@ -17,7 +17,7 @@
 //     Parts of a tile go to the workspace; the CTA that brings the last one puts them together, in order: the result does not depend on which one
 //     that is.
 //
-// Measured, 12 heads of 128: 32760 queries over 512 keys 108 us (955 TFLOP/s), over 128 54.7 (traffic: 202 MB, 3.7 TB/s), 4680 over 512 23.4, 1000 over 33k 177
+// Measured, 12 heads of 128: 32760 queries over 512 keys 108 us (955 TFLOP/s), over 128 54.1 (traffic: 202 MB, 3.7 TB/s), 4680 over 512 23.5, 1000 over 33k 177
 // (by pairs, 2 x 40 heads x 32760 over 343 523 us, 880 TFLOP/s and 2.5 TB/s).
 //
 // Warp roles: 0-3, 4-7 softmax; 8 issues S = Q K^T; 9 copies V; 10 finds the CTA's parts, copies K and Q; 11 issues O += P V; 12-15 write.
@@ -958,10 +958,11 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 cudaError_t launch_cross_tiles(const CrossGeom &g, const CacheIndex &ix, const CrossWorkspace &w, const void *Q, const void *K, const void *V, void *O,
                                float *lse, cudaStream_t s, int *launches) {
-  // Pairs of CTAs, where a sequence may have more rows than a tile, if there are many tiles a CTA or more keys and values than L2 keeps.  (Half of the traffic against an
-  // uneven finish: 2 x 40 heads x 32760 over 343 541 us, 607 by single CTAs; 12 heads x 18720 over 512 71 and 71, x 4680 29 and 24; x 4608 over 32760 793 and 1090.)
+  // Pairs of CTAs, where a sequence may have more rows than a tile, if there are many tiles a CTA or more keys and values than L2 keeps.  (Half of the traffic, and of its power, against
+  // an uneven finish: 2 x 40 heads x 32760 over 343 531 us, 545 by single CTAs, and 589 and 603 for half a second on end; 12 heads x 32760 over 512 110 and 108, x 4680 29 and 23; over
+  // 32760 x 4608 794 and 1071, x 1000 182 and 242; 8 x 8 heads x 2000 over 8000 492 and 530.)
   const long long tiles = ((long long)g.T * g.G + 127) / 128 * g.Hkv, keys_bytes = (long long)g.Tk * g.Hkv * 4 * kD;
-  const bool pair = (long long)g.max_q > 128 / g.G && (tiles >= 16 * kCacheCtas || keys_bytes > 64 << 20);
+  const bool pair = (long long)g.max_q > 128 / g.G && (tiles >= 32 * kCacheCtas || keys_bytes > 64 << 20);
   CUtensorMap mq, mk, mv, mo;
   if (!make_query_map(&mq, Q, g) || !make_query_map(&mo, O, g) || !make_states_map(&mk, K, g, pair ? kKeyStep / 2 : kKeyStep, 2) ||
       !make_states_map(&mv, V, g, kKeyStep, pair ? 1 : 2))

@@ -197,7 +197,7 @@ def test_large_tensors_of_states(heart, name):
     assert same(O, P)
 
 
-@pytest.mark.parametrize("q,k", [([4700, 0, 130, 4700], [70, 9, 1, 300]), ([9500], [33])])
+@pytest.mark.parametrize("q,k", [([4700, 0, 130, 4700], [70, 9, 1, 300]), ([9500], [33]), ([19100], [33])])
 def test_many_tiles_a_cta(heart, q, k):
     c = Case(q, k, Hq=32, Hkv=32, layout="fused", seed=sum(q))
     d = Device(heart, c)
