@@ -17,8 +17,8 @@
 //     Parts of a tile go to the workspace; the CTA that brings the last one puts them together, in order: the result does not depend on which one
 //     that is.
 //
-// Measured, 12 heads of 128: 32760 queries over 512 keys 108 us (955 TFLOP/s), over 128 54.1 (traffic: 202 MB, 3.7 TB/s), 4680 over 512 23.5, 1000 over 33k 177
-// (by pairs, 2 x 40 heads x 32760 over 343 523 us, 880 TFLOP/s and 2.5 TB/s).
+// Measured, 12 heads of 128: 32760 queries over 512 keys 108 us (955 TFLOP/s), over 128 54.1 (traffic: 202 MB, 3.7 TB/s), 4680 over 512 23.5, 1000 over 33k 182
+// (by pairs, 2 x 40 heads x 32760 over 343 531 us, 866 TFLOP/s and 2.5 TB/s).
 //
 // Warp roles: 0-3, 4-7 softmax; 8 issues S = Q K^T; 9 copies V; 10 finds the CTA's parts, copies K and Q; 11 issues O += P V; 12-15 write.
 // Tensor memory: O (128 columns) | S[2] (2 x 128) | P[2] (2 x 64).
