@@ -45,6 +45,9 @@ constexpr int kMaxStages = 3;
 // twice).  64 single tokens, 12 heads, over 100 to 4000 states took 150 us by steps alone, the CTA with 23 tiles 146 and the middle one 112, and takes 131.  Over 1 to 1000, 60 to 76
 // and 41 to 44 (counted as one 48 to 55, as three or four the same).
 constexpr int kTileCost = 2, kShareWithCost = 4;
+// Nor are its tiles of so few steps cut (8 heads x one token over 200 states 5.9 us, by parts 7.6; over 500 7.6 and 8.0; over 700, 6 steps, 8.9 and 8.1), and shares may be four
+// steps longer where tiles then begin with one (8 x 12 heads over 1000 14.0 us, 18.0 where CTAs had two ends of tiles).
+constexpr int kWholeSteps = 4;
 constexpr int kMaxParts = 31;          // of a tile, and one more where shares cross tiles: the last CTA reads them, a lane a part
 constexpr int kApartRows = 6;          // rows of a tile whose sums have a place beside the rings
 constexpr float kNoReference = -3.0e38f;
@@ -245,11 +248,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       sequence_at = before_lane(per_head * p.Hkv, total);
     }
     share = max(quotient(total + gridDim.x - 1, gridDim.x), (long long)(longest + kMaxParts - 1) / kMaxParts);
+    if (Cross && longest <= kWholeSteps) share = max(share, (long long)longest);
     // Where each sequence and head is one tile and CTAs are enough, tiles begin with a share (a CTA with the end of one and the beginning of
     // another takes twice as long as the others: 8 heads x 4100 tokens).
     if (total < (1 << 20) && __all_sync(0xffffffffu, per_head == 0 || tiles_of(q) == 1)) {
       const int steps = (int)per_head;
-      for (int more = 0; more <= (int)share / 4 + 1 && !one_tile; ++more) {
+      const int most = Cross ? max((int)share / 4, 3) : (int)share / 4;
+      for (int more = 0; more <= most + 1 && !one_tile; ++more) {
         const int sh1 = (int)share + more, parts = (steps + sh1 - 1) / sh1;
         if (__reduce_add_sync(0xffffffffu, parts * p.Hkv) <= (int)gridDim.x) {
           one_tile = true;
