@@ -45,11 +45,15 @@ constexpr int kMaxStages = 3;
 // twice).  64 single tokens, 12 heads, over 100 to 4000 states took 150 us by steps alone, the CTA with 23 tiles 146 and the middle one 112, and takes 131.  Over 1 to 1000, 60 to 76
 // and 41 to 44 (counted as one 48 to 55, as three or four the same).
 constexpr int kTileCost = 2, kShareWithCost = 4;
-// Nor are its tiles of so few steps cut (8 heads x one token over 200 states 5.9 us, by parts 7.6; over 500 7.6 and 8.0; over 700, 6 steps, 8.9 and 8.1), and shares may be four
-// steps longer where tiles then begin with one (8 x 12 heads over 1000 14.0 us, 18.0 where CTAs had two ends of tiles).
+// Nor are its tiles of so few steps cut, or of twice as many where they are not much longer than a share: a CTA takes those that begin in its share.  (8 heads x one token over
+// 200 states 5.9 us, by parts 7.6; over 700, 6 steps, 9.1 and 8.1.  32 tokens x 8 heads of 8 over 350 15.2 and 20.0, over 1000, 8 steps, 27.9 and 31.5; 64 tokens 48.8 and 47.6.)
+// Where they are, shares may be four steps longer if tiles then begin with one (8 x 12 heads over 1400 17.4 us, 20.7 where CTAs had two ends of tiles).
 constexpr int kWholeSteps = 4;
 constexpr int kMaxParts = 31;          // of a tile, and one more where shares cross tiles: the last CTA reads them, a lane a part
-constexpr int kApartRows = 6;          // rows of a tile whose sums have a place beside the rings
+// Rows of a tile whose sums have a place beside the rings.  (Cross attention: without an e4m3 cache's scales there is room for all of a tile of 8.  32 tokens, 64 heads on 8, over
+// 200 states took 13.5 us with six, not 11.6.)
+template <bool Cross>
+constexpr int kApartRows = Cross ? 8 : 6;
 constexpr float kNoReference = -3.0e38f;
 constexpr float kMaxGrowth = 8.f;      // log2: the reference of a row moves when a maximum exceeds it by more
 constexpr float kHeadroomE4m3 = 6.f;   // log2 of the largest weight when the reference has moved
@@ -79,11 +83,12 @@ struct RowsParams {
   int looked;
 };
 
+template <bool Cross>
 struct alignas(16) RowsShared {
   uint64_t full[kWarps][kMaxStages];
-  alignas(16) uint8_t scales[kWarps][kMaxStages][64];  // e4m3: of the keys and of the values of a stage
+  alignas(16) uint8_t scales[kWarps][kMaxStages][Cross ? 16 : 64];  // e4m3: of the keys and of the values of a stage
   float2 l[kWarps][16];   // row sums and their references
-  float o_ref[kWarps][16];  // e4m3: references of the sums of values
+  float o_ref[kWarps][Cross ? 1 : 16];  // e4m3: references of the sums of values
   long long total[kWarps], tiles[kWarps];
   int longest[kWarps];
   int found;              // sequence of the CTA's first step
@@ -92,8 +97,9 @@ struct alignas(16) RowsShared {
   int last;
   int abort;
 };
-constexpr int kRowsSmem = kWarps * kRing + sizeof(RowsShared) + kWarps * kApartRows * 512;
-static_assert(kRowsSmem <= 232448 && sizeof(RowsShared) % 16 == 0, "shared memory of an SM");
+template <bool Cross>
+constexpr int kRowsSmem = kWarps * kRing + sizeof(RowsShared<Cross>) + kWarps * kApartRows<Cross> * 512;
+static_assert(kRowsSmem<false> <= 232448 && kRowsSmem<true> <= 232448, "shared memory of an SM");
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -142,7 +148,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   constexpr int kHalf = kKeys * kD * (E4m3 ? 1 : 2), kStage = 2 * kHalf, kStages = kRing / kStage;  // bytes of a warp's keys, or values
   static_assert(kStages <= kMaxStages, "barriers");
   extern __shared__ __align__(1024) unsigned char smem[];
-  RowsShared &sh = *reinterpret_cast<RowsShared *>(smem + kWarps * kRing);
+  using Shared = RowsShared<Cross>;
+  static_assert(!(Cross && E4m3) && sizeof(Shared) % 16 == 0, "places of scales and sums");
+  Shared &sh = *reinterpret_cast<Shared *>(smem + kWarps * kRing);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   unsigned char *ring = smem + warp * kRing;
   const uint32_t ring_at = smem_u32(ring);
@@ -186,6 +194,17 @@ __global__ void __launch_bounds__(kThreads, 1)
   bool one_tile = false;                          // shares do not cross tiles
   int h = 0, t = 0, done = 0;                     // head, tile and the tile's steps before this share
   int cost = 0, paid = 0;                         // units of a tile ahead of its steps, and how many of this one's lie before the share
+  bool whole_tiles = false;                       // a CTA takes those that begin in its share
+  auto next_tile = [&]() {
+    if (++t == tiles_of(q)) {
+      t = 0;
+      if (++h == p.Hkv) {
+        h = 0;
+        do q = sequence_at_place(++s);
+        while (q.n == 0 && s + 1 < ix.S);
+      }
+    }
+  };
   auto costs = [&](long long steps) { return Cross && steps >= (long long)kShareWithCost * gridDim.x; };
   // to be done again: the next tile of this CTA, whole
   long long pair = 0;
@@ -248,7 +267,6 @@ __global__ void __launch_bounds__(kThreads, 1)
       sequence_at = before_lane(per_head * p.Hkv, total);
     }
     share = max(quotient(total + gridDim.x - 1, gridDim.x), (long long)(longest + kMaxParts - 1) / kMaxParts);
-    if (Cross && longest <= kWholeSteps) share = max(share, (long long)longest);
     // Where each sequence and head is one tile and CTAs are enough, tiles begin with a share (a CTA with the end of one and the beginning of
     // another takes twice as long as the others: 8 heads x 4100 tokens).
     if (total < (1 << 20) && __all_sync(0xffffffffu, per_head == 0 || tiles_of(q) == 1)) {
@@ -356,9 +374,17 @@ __global__ void __launch_bounds__(kThreads, 1)
     rest -= h * per_head;
     if (!one_tile)
       for (int k; rest >= (k = span(q, t).steps + cost); ++t) rest -= k;
+    const int most = longest - cost;
+    whole_tiles = Cross && (most <= kWholeSteps || (most <= 2 * kWholeSteps && most <= 2 * share));
+    if (whole_tiles && rest > 0) {
+      u += span(q, t).steps + cost - rest;
+      if (one_tile || u >= u1) return;  // (shares that begin with a tile hold no second one)
+      rest = 0;
+      next_tile();
+    }
     paid = (int)min(rest, (long long)cost);
     done = (int)rest - paid;
-    if (Cross && u1 - u <= cost - paid) return;  // (no step of the tile; none where shares are as long as those with a cost)
+    if (Cross && !whole_tiles && u1 - u <= cost - paid) return;  // (no step of the tile; none where shares are as long as those with a cost)
   }
 
   int put = 0, take = 0;            // the stages that come next, to fill and to use
@@ -429,7 +455,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     n_rows = min(kRows, (int)((long long)q.n * p.G) - first_row);
     p0 = position(q, first_row / p.G);
     const int p1 = position(q, (first_row + n_rows - 1) / p.G);
-    end_step = (int)min((long long)steps, done + (u1 - u) - (cost - paid));
+    end_step = whole_tiles ? steps : (int)min((long long)steps, done + (u1 - u) - (cost - paid));
     next = done;
     next_batch = done;
     entry = entries(done);
@@ -747,9 +773,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ---------------------------------------------------------------- the warps' sums put together
     // A few rows have a place of their own, and the next tile's first copies go out ahead of this; more rows lie where the copies were.
     // (Pieces of 32 bytes are swizzled by the row.)
-    const bool apart = n_rows <= kApartRows;
-    unsigned char *sums = apart ? smem + kWarps * kRing + sizeof(RowsShared) : smem;
-    const int sums_pitch = apart ? kApartRows * 512 : kRing;
+    const bool apart = n_rows <= kApartRows<Cross>;
+    unsigned char *sums = apart ? smem + kWarps * kRing + sizeof(Shared) : smem;
+    const int sums_pitch = apart ? kApartRows<Cross> * 512 : kRing;
 #pragma unroll
     for (int m = 0; m < NT; ++m)
 #pragma unroll
@@ -787,17 +813,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int tile_steps = steps;
     const int part = 2 * blockIdx.x + (done == 0 ? 1 : 0);
     u += end_step - done + (cost - paid);
-    const bool more = Redo ? next_redo() : !one_tile && u + cost < u1;
+    const bool more = Redo ? next_redo() : !one_tile && u + (whole_tiles ? 0 : cost) < u1;
     if (more) {
       done = paid = 0;
-      if (!Redo && ++t == tiles_of(q)) {
-        t = 0;
-        if (++h == p.Hkv) {
-          h = 0;
-          do q = sequence_at_place(++s);
-          while (q.n == 0 && s + 1 < ix.S);
-        }
-      }
+      if (!Redo) next_tile();
       if (apart) start();
     }
     __syncthreads();
@@ -925,10 +944,10 @@ namespace {
 
 template <int NT, bool E4m3, bool Redo, bool Cross>
 cudaError_t launch(const RowsParams &p, const CUtensorMap &mk, const CUtensorMap &mv, cudaStream_t s, int *launches) {
-  cudaError_t e = allow_shared_memory(cache_rows_kernel<NT, E4m3, Redo, Cross>, kRowsSmem);
+  cudaError_t e = allow_shared_memory(cache_rows_kernel<NT, E4m3, Redo, Cross>, kRowsSmem<Cross>);
   if (e != cudaSuccess) return e;
   ++*launches;
-  return launch_pdl(cache_rows_kernel<NT, E4m3, Redo, Cross>, dim3(kCacheCtas), dim3(kThreads), kRowsSmem, s, mk, mv, p);
+  return launch_pdl(cache_rows_kernel<NT, E4m3, Redo, Cross>, dim3(kCacheCtas), dim3(kThreads), kRowsSmem<Cross>, s, mk, mv, p);
 }
 
 template <int NT, bool E4m3, bool Redo>

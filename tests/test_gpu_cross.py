@@ -157,6 +157,8 @@ CASES = {
     "small scale of many": dict(q=[420], k=[400], scale=1e-6),
     "small scale": dict(q=[20], k=[400], scale=1e-6),
     "tokens of short and long states": dict(q=[1, 0, 1, 1, 1, 0, 1, 1], k=[2000, 5, 1, 0, 130, 700, 90, 1500], Hq=24, Hkv=24, layout="shuffled"),
+    "tokens of short states": dict(q=[(i * 5 + 1) % 4 for i in range(20)], k=[(i * 137 + 60) % 512 for i in range(20)], Hq=24, Hkv=12, layout="shuffled"),
+    "tokens of middling states": dict(q=[(i * 5 + 1) % 3 for i in range(30)], k=[(i * 137 + 60) % 1000 for i in range(30)], Hq=24, Hkv=24, layout="fused"),
     "batch of tokens": dict(q=[(i * 5) % 3 for i in range(400)], k=[(i * 137) % 600 for i in range(400)], Hq=8, Hkv=4),
     "many sequences": dict(q=[(i * 7) % 5 for i in range(700)], k=[(i * 37) % 90 for i in range(700)]),
     "40 sequences": dict(q=[(i * 53) % 150 for i in range(40)], k=[(i * 37) % 190 for i in range(40)], layout="shuffled", Hq=3, Hkv=3),
