@@ -40,7 +40,7 @@ __host__ inline CrossWorkspace carve_cross(void *base) {
 int make_cross_geom(const heart_cross_config *c, CrossGeom *g);
 
 // Whether all rows are few tiles of 16.  The kernel for few rows takes any number of them, and reads keys and values as often as it has tiles: its smaller share of fixed costs
-// is worth that here, with tiles of 8 rows.  (16 tiles, 8 heads of 8 x 4 over 500: 8.4 us, with tiles of 16 11.5, by the kernel for tiles of 128 11.6; over 2000 10.7, 12.5 and
+// is worth that here, with tiles of 8 rows.  (16 tiles, 8 heads of 8 x 4 over 500: 8.1 us, with tiles of 16 11.5, by the kernel for tiles of 128 11.6; over 2000 10.9, 12.5 and
 // 17.3; over 8000 22.5, 18.3 and 24.6.  24 tiles, 12 heads x 32 over 500, 8000: 9.1 and 27.4, of 128 11.8 and 26.5.  36, 12 heads x 48: 9.3 and 35.1, of 128 11.9 and
 // 26.3.)
 __host__ inline bool few_rows(const CrossGeom &g) {

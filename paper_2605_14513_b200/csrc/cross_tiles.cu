@@ -38,7 +38,7 @@ constexpr int kWarpQK = 8, kWarpV = 9, kWarpK = 10, kWarpPV = 11, kWarpOut = 12;
 constexpr int kRegsSoftmax = 184, kRegsOut = 80, kRegsHelper = 64;  // 184 * 256 + 80 * 128 + 64 * 128 = the CTA's 512 x 128
 static_assert(kRegsSoftmax * 256 + kRegsOut * 128 + kRegsHelper * 128 <= kThreads * 128, "registers at launch");
 constexpr int kTileBytes = 32768;  // 128 rows x 128 dims: [2 dim halves][128 rows][64] bf16, 128-byte swizzle
-constexpr int kTileCost = 1;       // of a tile besides its steps, in steps
+constexpr int kTileCost = 1;       // of a tile besides its steps, in steps (as two the same; as three six prompts of 284 to 1256 over up to 474 states 35.8 us, not 32.2)
 // Tiles of no more steps are not shared: an uneven finish costs half of a tile, parts 5 us.  (12 heads x 9000 over 1500, 12 steps, 78 us, 84 with parts; over 2000, 16
 // steps, 100 and 105, but x 3500 53.6 and 52.5; over 2600, 21 steps, 127 and 133, but x 3500 66.9 and 63.)  Nor are tiles of no more than kPartsCost steps beside a CTA's share:
 // where CTAs are left over, parts cost some ten steps.  (8 heads of 8 x 5 over 1250, 10 steps, 16.6 us, 16.3 with parts; over 2000, 16 steps, 21.2 and 17.6.)
