@@ -364,8 +364,8 @@ typedef struct {
   int32_t S, T, Tk;            /* sequences, rows of Q and O, rows of K and V (>= 1 each)                      */
   int32_t Hq, Hkv, D;          /* as in heart_cache_config                                                    */
   int32_t max_q;               /* most queries of a sequence: selects kernels by it; any lengths give the
-                                  right results.  0 = unknown: taken as many, so that single tokens are right
-                                  but slow (tiles of 128 rows); a program that decodes says 1                 */
+                                  right results.  0 = unknown: taken as many, so that a batch of single tokens is
+                                  right but slow (tiles of 128 rows); a program that decodes says 1           */
   uint32_t flags;              /* 0                                                                           */
   int64_t q_stride_t, q_stride_h;   /* elements, of Q and O; both 0 = contiguous [T,Hq,D]                     */
   int64_t kv_stride_t, kv_stride_h; /* of K and V; both 0 = contiguous [Tk,Hkv,D]                             */
