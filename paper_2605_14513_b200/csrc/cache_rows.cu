@@ -382,7 +382,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       rest = 0;
       next_tile();
     }
-    paid = (int)min(rest, (long long)cost);
+    if (Cross) paid = (int)min(rest, (long long)cost);  // (a constant elsewhere)
     done = (int)rest - paid;
     if (Cross && !whole_tiles && u1 - u <= cost - paid) return;  // (no step of the tile; none where shares are as long as those with a cost)
   }
