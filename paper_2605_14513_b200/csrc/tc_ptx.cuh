@@ -308,13 +308,10 @@ __device__ __forceinline__ void mbar_expect_tx_at(uint64_t *bar, uint32_t rank, 
 }
 // Of a phase that this thread has seen the end of: what other CTAs of the cluster released with their arrivals comes before what it does next.
 __device__ __forceinline__ void mbar_acquire_cluster(uint64_t *bar, uint32_t parity) {
-  uint32_t there;
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
-      "mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(there)
-      : "r"(smem_u32(bar)), "r"(parity)
+      "mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%0], %1;\n\t}" ::"r"(smem_u32(bar)),
+      "r"(parity)
       : "memory");
 }
 // D[tmem] (+)= A[tmem] * B[smem], each CTA with its half of A's rows and of B's columns.
