@@ -990,7 +990,7 @@ cudaError_t launch_cache_rows(const CacheGeom &g, const CacheIndex &ix, const Ca
 }
 
 cudaError_t launch_cross_rows(const CrossGeom &g, const CacheIndex &ix, const CrossWorkspace &w, const void *Q, const void *K, const void *V, void *O,
-                              float *lse, cudaStream_t s, int *launches) {
+                              float *lse, bool eight, cudaStream_t s, int *launches) {
   CUtensorMap mk, mv;
   if (!make_states_map(&mk, K, g, keys_of(false), 2) || !make_states_map(&mv, V, g, keys_of(false), 2)) return cudaErrorInvalidValue;
   RowsParams p = {};
@@ -1008,7 +1008,6 @@ cudaError_t launch_cross_rows(const CrossGeom &g, const CacheIndex &ix, const Cr
   p.arrivals = w.arrivals;
   p.parts = w.parts;
   p.part_l = w.part_l;
-  const bool eight = (long long)g.max_q * g.G <= 8 || few_rows(g);
   return eight ? launch<1, false, false, true>(p, mk, mv, s, launches) : launch<2, false, false, true>(p, mk, mv, s, launches);
 }
 

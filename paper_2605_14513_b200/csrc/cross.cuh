@@ -48,11 +48,25 @@ __host__ inline bool few_rows(const CrossGeom &g) {
   return ((long long)g.T * g.G + 15LL * (g.S < g.T ? g.S : g.T)) / 16 * g.Hkv <= kFewTiles;
 }
 
+// The kernel that a call takes: by 8 or 16 rows, by tiles, by pairs of CTAs.
+enum class CrossKernel { kRows8, kRows16, kTiles, kPairs };
+__host__ inline CrossKernel cross_kernel(const CrossGeom &g) {
+  const long long most_rows = (long long)g.max_q * g.G;  // of a sequence and key head
+  if (most_rows <= 8 || few_rows(g)) return CrossKernel::kRows8;
+  if (most_rows <= kRowsOfRowsKernel) return CrossKernel::kRows16;
+  // Pairs of CTAs, where a sequence may have more rows than a tile, if there are many tiles a CTA or more keys and values than L2 keeps.  (Half of the traffic, and of its power, against
+  // an uneven finish: 2 x 40 heads x 32760 over 343 531 us, 545 by single CTAs, and 589 and 603 for half a second on end; 12 heads x 32760 over 512 110 and 108, x 4680 29 and 23; over
+  // 32760 x 4608 794 and 1071, x 1000 182 and 242; 8 x 8 heads x 2000 over 8000 492 and 530.)
+  const long long tiles = ((long long)g.T * g.G + 127) / 128 * g.Hkv, keys_bytes = (long long)g.Tk * g.Hkv * 4 * kD;
+  const bool pairs = (long long)g.max_q > 128 / g.G && (tiles >= 32 * kCacheCtas || keys_bytes > 64 << 20);
+  return pairs ? CrossKernel::kPairs : CrossKernel::kTiles;
+}
+
 // ix: row_start and kv_len are the starts of the queries and the numbers of keys, table the first rows of the keys, table_stride the rows of K.
 cudaError_t launch_cross_rows(const CrossGeom &g, const CacheIndex &ix, const CrossWorkspace &w, const void *Q, const void *K, const void *V, void *O,
-                              float *lse, cudaStream_t s, int *launches);
+                              float *lse, bool eight, cudaStream_t s, int *launches);
 cudaError_t launch_cross_tiles(const CrossGeom &g, const CacheIndex &ix, const CrossWorkspace &w, const void *Q, const void *K, const void *V, void *O,
-                               float *lse, cudaStream_t s, int *launches);
+                               float *lse, bool pair, cudaStream_t s, int *launches);
 
 // K or V as (64 dims, row, dim half, head): a box is one or both halves of `rows` rows of one head, from any row on, 128-byte rows, swizzled.
 bool make_states_map(CUtensorMap *m, const void *base, const CrossGeom &g, int rows, int halves);

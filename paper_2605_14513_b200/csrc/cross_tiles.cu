@@ -963,12 +963,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 }  // namespace
 
 cudaError_t launch_cross_tiles(const CrossGeom &g, const CacheIndex &ix, const CrossWorkspace &w, const void *Q, const void *K, const void *V, void *O,
-                               float *lse, cudaStream_t s, int *launches) {
-  // Pairs of CTAs, where a sequence may have more rows than a tile, if there are many tiles a CTA or more keys and values than L2 keeps.  (Half of the traffic, and of its power, against
-  // an uneven finish: 2 x 40 heads x 32760 over 343 531 us, 545 by single CTAs, and 589 and 603 for half a second on end; 12 heads x 32760 over 512 110 and 108, x 4680 29 and 23; over
-  // 32760 x 4608 794 and 1071, x 1000 182 and 242; 8 x 8 heads x 2000 over 8000 492 and 530.)
-  const long long tiles = ((long long)g.T * g.G + 127) / 128 * g.Hkv, keys_bytes = (long long)g.Tk * g.Hkv * 4 * kD;
-  const bool pair = (long long)g.max_q > 128 / g.G && (tiles >= 32 * kCacheCtas || keys_bytes > 64 << 20);
+                               float *lse, bool pair, cudaStream_t s, int *launches) {
   CUtensorMap mq, mk, mv, mo;
   if (!make_query_map(&mq, Q, g) || !make_query_map(&mo, O, g) || !make_states_map(&mk, K, g, pair ? kKeyStep / 2 : kKeyStep, 2) ||
       !make_states_map(&mv, V, g, kKeyStep, pair ? 1 : 2))

@@ -552,8 +552,10 @@ int heart_cross_attn(const heart_cross_config *cfg, const void *Q, const void *K
   ix.table_stride = g.Tk;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   g_launches = 0;
-  const bool rows = (long long)g.max_q * g.G <= kRowsOfRowsKernel || few_rows(g);
-  cudaError_t e = rows ? launch_cross_rows(g, ix, w, Q, K, V, O, lse, s, &g_launches) : launch_cross_tiles(g, ix, w, Q, K, V, O, lse, s, &g_launches);
+  const CrossKernel kernel = cross_kernel(g);
+  const bool rows = kernel == CrossKernel::kRows8 || kernel == CrossKernel::kRows16;
+  cudaError_t e = rows ? launch_cross_rows(g, ix, w, Q, K, V, O, lse, kernel == CrossKernel::kRows8, s, &g_launches)
+                       : launch_cross_tiles(g, ix, w, Q, K, V, O, lse, kernel == CrossKernel::kPairs, s, &g_launches);
   if (e != cudaSuccess) return cuda_fail(e, "cross_attention");
   return HEART_OK;
 }
@@ -653,5 +655,13 @@ const char *heart_strerror(int code) {
 }
 
 int heart_last_launch_count(void) { return g_launches; }
+
+#ifdef HEART_TEST_HOOKS
+// Test-hook builds only: the kernel that a call takes (a CrossKernel), or -1.
+int heart_test_cross_kernel(const heart_cross_config *cfg) {
+  CrossGeom g;
+  return make_cross_geom(cfg, &g) == HEART_OK ? static_cast<int>(cross_kernel(g)) : -1;
+}
+#endif
 
 }  // extern "C"
