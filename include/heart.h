@@ -361,7 +361,8 @@ int heart_cache_release(const heart_cache_config *cfg, const uint8_t *ended, con
  * Roundings besides that of the result: a weight is rounded to bf16 for the product with the values (the row sum takes it unrounded); sums and the
  * softmax's statistics have 32 bits. */
 typedef struct {
-  int32_t S, T, Tk;            /* sequences, rows of Q and O, rows of K and V (>= 1 each)                      */
+  int32_t S, T, Tk;            /* sequences, rows of Q and O, rows of K and V (>= 1 each).  Of few queries Tk / S
+                                  stands for a sequence's keys where a kernel is chosen                       */
   int32_t Hq, Hkv, D;          /* as in heart_cache_config                                                    */
   int32_t max_q;               /* most queries of a sequence: selects kernels by it; any lengths give the
                                   right results.  0 = unknown: taken as many, so that a batch of single tokens is

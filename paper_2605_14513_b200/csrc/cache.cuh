@@ -79,6 +79,7 @@ cudaError_t launch_cache_read(const CacheGeom &g, const CacheIndex &ix, const he
 // Attention by 8 or 16 query rows in registers, or by tiles of 128: the former where a sequence and key head has so few rows.  (20 sequences of 4000
 // tokens, 32 heads on 8, bf16: four new tokens, 16 rows, 71 us; eight, 32 rows, 189 by rows and 75 by tiles.)
 constexpr int kRowsOfRowsKernel = 16;
+constexpr int kMaxParts = 31;  // of a tile of the former, and one more where shares cross tiles: the last CTA reads them, a lane a part
 cudaError_t launch_cache_rows(const CacheGeom &g, const CacheIndex &ix, const CacheWorkspace &w, const void *Q, const heart_cache &c,
                               void *O, float *lse, cudaStream_t s, int *launches);
 // Behind the tile kernel, for e4m3: by rows what `looked` CTAs have put down in w.redo (most often nothing).

@@ -49,7 +49,6 @@ constexpr int kTileCost = 2, kShareWithCost = 4;
 // 200 states 5.9 us, by parts 7.6; over 700, 6 steps, 9.1 and 8.1.  32 tokens x 8 heads of 8 over 350 15.2 and 20.0, over 1000, 8 steps, 27.9 and 31.5; 64 tokens 48.8 and 47.6.)
 // Where they are, shares may be four steps longer if tiles then begin with one (8 x 12 heads over 1400 17.4 us, 20.7 where CTAs had two ends of tiles).
 constexpr int kWholeSteps = 4;
-constexpr int kMaxParts = 31;          // of a tile, and one more where shares cross tiles: the last CTA reads them, a lane a part
 // Rows of a tile whose sums have a place beside the rings.  (Cross attention: without an e4m3 cache's scales there is room for all of a tile of 8.  32 tokens, 64 heads on 8, over
 // 200 states took 13.5 us with six, not 11.6.)
 template <bool Cross>

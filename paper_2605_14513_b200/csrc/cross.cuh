@@ -1,5 +1,7 @@
 // Cross attention: geometry, workspace, and what its two kernels share.
 #pragma once
+#include <algorithm>
+
 #include "cache.cuh"
 
 namespace heart {
@@ -40,19 +42,34 @@ __host__ inline CrossWorkspace carve_cross(void *base) {
 int make_cross_geom(const heart_cross_config *c, CrossGeom *g);
 
 // Whether all rows are few tiles of 16.  The kernel for few rows takes any number of them, and reads keys and values as often as it has tiles: its smaller share of fixed costs
-// is worth that here, with tiles of 8 rows.  (16 tiles, 8 heads of 8 x 4 over 500: 8.1 us, with tiles of 16 11.5, by the kernel for tiles of 128 11.6; over 2000 10.9, 12.5 and
-// 17.3; over 8000 22.5, 18.3 and 24.6.  24 tiles, 12 heads x 32 over 500, 8000: 9.1 and 27.4, of 128 11.8 and 26.5.  36, 12 heads x 48: 9.3 and 35.1, of 128 11.9 and
-// 26.3.)
+// is worth that here, as long as the keys are not many.  (16 tiles, 8 heads of 8 x 4 over 500: 7.8 us by tiles of 8 rows, 9.6 of 16, 11.3 by the kernel for tiles of 128; over 2000
+// 10.4, 12.0 and 17.5.  24 tiles, 12 heads x 32 over 500: 7.8, 9.5 and 11.5.  36, 12 heads x 48: 9.3, of 128 11.9.)
 __host__ inline bool few_rows(const CrossGeom &g) {
   constexpr long long kFewTiles = 24;
   return ((long long)g.T * g.G + 15LL * (g.S < g.T ? g.S : g.T)) / 16 * g.Hkv <= kFewTiles;
+}
+// Key steps that a CTA has by tiles of `rows` rows: of sequences taken as alike, with Tk / S keys each.
+__host__ inline double key_steps(const CrossGeom &g, int rows) {
+  const long long sequences = g.S < g.T ? g.S : g.T, each = ((long long)g.T * g.G + sequences - 1) / sequences;
+  const double steps = g.Tk / g.S / kKeyStep + 1, tiles = (double)(sequences * ((each + rows - 1) / rows) * g.Hkv);
+  return steps * std::max(tiles / kCacheCtas, 1.0 / kMaxParts);
 }
 
 // The kernel that a call takes: by 8 or 16 rows, by tiles, by pairs of CTAs.
 enum class CrossKernel { kRows8, kRows16, kTiles, kPairs };
 __host__ inline CrossKernel cross_kernel(const CrossGeom &g) {
   const long long most_rows = (long long)g.max_q * g.G;  // of a sequence and key head
-  if (most_rows <= 8 || few_rows(g)) return CrossKernel::kRows8;
+  if (most_rows <= 8) return CrossKernel::kRows8;
+  if (few_rows(g)) {
+    // Tiles of 16 rows where a CTA then has this many steps less (a step of 16 rows takes 1.06 us, of 8 rows 0.8, and the launch 3 us more), and tiles of 128 where it would still have
+    // many.  8, 16 and 128 rows of one head x 370 over 4000 18.1, 18.2 and 20.9 us, over 8000 25.6, 22.9 and 23.2, over 32 000 69.0, 50.2 and 38.8; 8 heads of 8 x 4 over 8000 20.5, 20.1 and
+    // 23.5, over 32 000 56.9, 37.0 and 44.9; 12 heads x 32 over 8000 25.6, 22.7 and 24.6, over 32 000 69.9, 51.7 and 51.2; 24 heads x 16 over 4000 18.2 and 16.1.  (Of 306
+    // sizes, over 64 to 150 000, what is chosen takes 1.3 % longer than the best one in the mean, 23 % at most: one head x 370 over 1000, where 8 rows take 14.7 and 16 rows 12.0.)
+    constexpr double kStepsSaved = 5, kManySteps = 28;
+    const double by16 = key_steps(g, 16);
+    if (key_steps(g, 8) - by16 < kStepsSaved) return CrossKernel::kRows8;
+    if (by16 <= kManySteps) return CrossKernel::kRows16;
+  }
   if (most_rows <= kRowsOfRowsKernel) return CrossKernel::kRows16;
   // Pairs of CTAs, where a sequence may have more rows than a tile, if there are many tiles a CTA or more keys and values than L2 keeps.  (Half of the traffic, and of its power, against
   // an uneven finish: 2 x 40 heads x 32760 over 343 531 us, 545 by single CTAs, and 589 and 603 for half a second on end; 12 heads x 32760 over 512 110 and 108, x 4680 29 and 23; over

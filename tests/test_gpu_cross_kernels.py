@@ -174,3 +174,21 @@ def test_bad_arrays_touch_nothing_outside(heart, kernel_of, kernel):
         near(c, [x for x in of if sure[x[0]:x[0] + x[1]].any()], sure, O, lse)
         none = owners == 0
         assert (O.cpu()[none] == 77).all() and (lse.cpu()[none] == 55).all()
+
+
+LONG = [(ROWS16, dict(q=[4], k=[20000], Hq=64, Hkv=8, pad=0)), (TILES, dict(q=[370], k=[32761], Hq=1, Hkv=1)), (ROWS16, dict(q=[150], k=[9001], Hq=2, Hkv=2, layout="fused")),
+        (ROWS16, dict(q=[30, 1, 0, 30], k=[14000, 77, 5, 16001], Hq=4, Hkv=2, layout="shuffled")), (PAIRS, dict(q=[260], k=[140000], Hq=1, Hkv=1))]
+
+
+@pytest.mark.parametrize("case", range(len(LONG)))
+def test_few_rows_over_long_states(heart, kernel_of, case):
+    """Few tiles of many steps, which several CTAs share."""
+    kernel, kw = LONG[case]
+    c = Case(**kw, seed=case)
+    d = Device(heart, c)
+    assert kernel_of(d.cfg) == kernel
+    O, lse = d.attention()
+    assert heart.heart_get_status(d.ws) == 0
+    near(c, sequences(c), torch.arange(c.T) < c.rows, O, lse)
+    P, M = d.attention()
+    assert same(O, P) and same(lse, M)
