@@ -45,6 +45,7 @@ constexpr int kMaxStages = 3;
 // twice).  64 single tokens, 12 heads, over 100 to 4000 states took 150 us by steps alone, the CTA with 23 tiles 146 and the middle one 112, and takes 131.  Over 1 to 1000, 60 to 76
 // and 41 to 44 (counted as one 48 to 55, as three or four the same).
 constexpr int kTileCost = 2, kShareWithCost = 4;
+static_assert(kShareWithCost > kTileCost, "a share has a step of its first tile");
 // Nor are its tiles of so few steps cut, or of twice as many where they are not much longer than a share: a CTA takes those that begin in its share.  (8 heads x one token over
 // 200 states 5.9 us, by parts 7.6; over 700, 6 steps, 9.1 and 8.1.  32 tokens x 8 heads of 8 over 350 15.2 and 20.0, over 1000, 8 steps, 27.9 and 31.5; 64 tokens 48.8 and 47.6.)
 // Where they are, shares may be four steps longer if tiles then begin with one (8 x 12 heads over 1400 17.4 us, 20.7 where CTAs had two ends of tiles).
@@ -177,10 +178,16 @@ __global__ void __launch_bounds__(kThreads, 1)
   auto steps_of = [&](const Sequence &q, int &longest) -> long long {  // of one head
     long long n = 0;
     const int tiles = tiles_of(q);
-    for (int t = 0; t < tiles; ++t) {
-      const int k = span(q, t).steps;
-      n += k;
+    if constexpr (Cross) {  // (they are alike: a million rows with max_q = 1, over 16 states, 2.0 ms, one by one 4.5)
+      const int k = tiles > 0 ? span(q, 0).steps : 0;
+      n = (long long)tiles * k;
       longest = max(longest, k);
+    } else {
+      for (int t = 0; t < tiles; ++t) {
+        const int k = span(q, t).steps;
+        n += k;
+        longest = max(longest, k);
+      }
     }
     return n;
   };
@@ -371,8 +378,15 @@ __global__ void __launch_bounds__(kThreads, 1)
     long long rest = u - sequence_at;
     h = (int)quotient(rest, per_head);
     rest -= h * per_head;
-    if (!one_tile)
-      for (int k; rest >= (k = span(q, t).steps + cost); ++t) rest -= k;
+    if (Cross) {
+      if (!one_tile) {
+        const int k = span(q, 0).steps + cost;
+        t = (int)quotient(rest, k);
+        rest -= (long long)t * k;
+      }
+    } else if (!one_tile) {
+      for (int k; rest >= (k = span(q, t).steps); ++t) rest -= k;
+    }
     const int most = longest - cost;
     whole_tiles = Cross && (most <= kWholeSteps || (most <= 2 * kWholeSteps && most <= 2 * share));
     if (whole_tiles && rest > 0) {
@@ -383,7 +397,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     if (Cross) paid = (int)min(rest, (long long)cost);  // (a constant elsewhere)
     done = (int)rest - paid;
-    if (Cross && !whole_tiles && u1 - u <= cost - paid) return;  // (no step of the tile; none where shares are as long as those with a cost)
   }
 
   int put = 0, take = 0;            // the stages that come next, to fill and to use

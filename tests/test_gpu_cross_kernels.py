@@ -192,3 +192,14 @@ def test_few_rows_over_long_states(heart, kernel_of, case):
     near(c, sequences(c), torch.arange(c.T) < c.rows, O, lse)
     P, M = d.attention()
     assert same(O, P) and same(lse, M)
+
+
+@pytest.mark.parametrize("kernel,max_q,q,k", [(ROWS8, 1, [30000, 1, 0, 20000], [33, 1, 7, 0]), (ROWS16, 16, [20001, 16], [200, 33]), (ROWS8, 1, [1] * 40 + [30000], [20] * 41)])
+def test_many_more_rows_than_max_q(heart, kernel_of, kernel, max_q, q, k):
+    """The kernel for few rows with thousands of tiles of a sequence: right, if slow."""
+    c = Case(q, k, Hq=2, Hkv=2, seed=max_q)
+    d = Device(heart, c, max_q=max_q)
+    assert kernel_of(d.cfg) == kernel
+    O, lse = d.attention()
+    assert heart.heart_get_status(d.ws) == 0
+    near(c, sequences(c), torch.arange(c.T) < c.rows, O, lse)
