@@ -363,11 +363,6 @@ def _cache_call(cfg, cache, query, tensors, page_table, row_start, kv_len, ws):
         raise ValueError(f"the workspace has to have cache_workspace_bytes(cfg) = {cache_workspace_bytes(cfg)} bytes beside the cache")
 
 
-def _cache_launch(call, cache, *args):
-    """The call on the current stream of the cache's device."""
-    _launch(call, cache.device, *args)
-
-
 def _launch(call, device, *args):
     """The call on the device's current stream."""
     if device == torch._C._cuda_getDevice():
@@ -382,15 +377,15 @@ def _launch(call, device, *args):
 def heart_cache_write(cfg, K, V, cache: Cache, page_table, row_start, kv_len, ws):
     """Stores the packed rows of K and V (bf16 [T, Hkv, D]), the last tokens of their sequences, in their pages."""
     _cache_call(cfg, cache, False, (K, V), page_table, row_start, kv_len, ws)
-    _cache_launch(lib().heart_cache_write, cache, C.byref(cfg), K.data_ptr(), V.data_ptr(), cache.ref, page_table.data_ptr(), row_start.data_ptr(),
-                  kv_len.data_ptr(), ws.data_ptr())
+    _launch(lib().heart_cache_write, cache.device, C.byref(cfg), K.data_ptr(), V.data_ptr(), cache.ref, page_table.data_ptr(), row_start.data_ptr(),
+            kv_len.data_ptr(), ws.data_ptr())
 
 
 def heart_cache_read(cfg, cache: Cache, page_table, row_start, kv_len, K_out, V_out, ws):
     """The last tokens of the sequences out of their pages into the packed rows of K_out and V_out (bf16 [T, Hkv, D])."""
     _cache_call(cfg, cache, False, (K_out, V_out), page_table, row_start, kv_len, ws)
-    _cache_launch(lib().heart_cache_read, cache, C.byref(cfg), cache.ref, page_table.data_ptr(), row_start.data_ptr(), kv_len.data_ptr(),
-                  K_out.data_ptr(), V_out.data_ptr(), ws.data_ptr())
+    _launch(lib().heart_cache_read, cache.device, C.byref(cfg), cache.ref, page_table.data_ptr(), row_start.data_ptr(), kv_len.data_ptr(),
+            K_out.data_ptr(), V_out.data_ptr(), ws.data_ptr())
 
 
 def heart_cache_attn(cfg, Q, cache: Cache, page_table, row_start, kv_len, O, ws, lse=None):
@@ -399,8 +394,8 @@ def heart_cache_attn(cfg, Q, cache: Cache, page_table, row_start, kv_len, O, ws,
     _cache_call(cfg, cache, True, (Q, O), page_table, row_start, kv_len, ws)
     if lse is not None and (lse.dtype is not torch.float32 or lse.numel() != cfg.T * cfg.Hq or lse.get_device() != cache.device or not lse.is_contiguous()):
         raise ValueError(f"lse has to be contiguous fp32 [{cfg.T}, {cfg.Hq}] beside the cache: got {lse.dtype} {tuple(lse.shape)} on {lse.device}")
-    _cache_launch(lib().heart_cache_attn, cache, C.byref(cfg), Q.data_ptr(), cache.ref, page_table.data_ptr(), row_start.data_ptr(), kv_len.data_ptr(),
-                  O.data_ptr(), _ptr(lse), ws.data_ptr())
+    _launch(lib().heart_cache_attn, cache.device, C.byref(cfg), Q.data_ptr(), cache.ref, page_table.data_ptr(), row_start.data_ptr(), kv_len.data_ptr(),
+            O.data_ptr(), _ptr(lse), ws.data_ptr())
 
 
 def _table_call(fields, names, tensors, sizes, ws):
