@@ -72,8 +72,8 @@ __host__ inline CrossKernel cross_kernel(const CrossGeom &g) {
   }
   if (most_rows <= kRowsOfRowsKernel) return CrossKernel::kRows16;
   // Pairs of CTAs, where a sequence may have more rows than a tile, if there are many tiles a CTA or more keys and values than L2 keeps.  (Half of the traffic, and of its power, against
-  // an uneven finish: 2 x 40 heads x 32760 over 343 531 us, 545 by single CTAs, and 589 and 603 for half a second on end; 12 heads x 32760 over 512 110 and 108, x 4680 29 and 23; over
-  // 32760 x 4608 794 and 1071, x 1000 182 and 242; 8 x 8 heads x 2000 over 8000 492 and 530.)
+  // an uneven finish: 2 x 40 heads x 32760 over 343 518 us, 537 by single CTAs, and 598 and 614 for most of a second on end; 12 heads x 32760 over 512 111 and 108, x 4680 29 and 23; x 1000 over
+  // 32760 182 and 244; 8 x 8 heads x 2000 over 8000 494 and 520.)
   const long long tiles = ((long long)g.T * g.G + 127) / 128 * g.Hkv, keys_bytes = (long long)g.Tk * g.Hkv * 4 * kD;
   const bool pairs = (long long)g.max_q > 128 / g.G && (tiles >= 32 * kCacheCtas || keys_bytes > 64 << 20);
   return pairs ? CrossKernel::kPairs : CrossKernel::kTiles;

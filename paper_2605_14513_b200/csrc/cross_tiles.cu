@@ -17,8 +17,8 @@
 //     Parts of a tile go to the workspace; the CTA that brings the last one puts them together, in order: the result does not depend on which one
 //     that is.
 //
-// Measured, 12 heads of 128: 32760 queries over 512 keys 108 us (955 TFLOP/s), over 128 54.1 (traffic: 202 MB, 3.7 TB/s), 4680 over 512 23.5, 1000 over 33k 182
-// (by pairs, 2 x 40 heads x 32760 over 343 531 us, 866 TFLOP/s and 2.5 TB/s).
+// Measured, 12 heads of 128, 20 calls after a pause: 32760 queries over 512 keys 108 us (955 TFLOP/s), over 128 54.7 (traffic: 202 MB, 3.7 TB/s), 4680 over 512 22.9, 1000 over 33k
+// 182 (by pairs; 2 x 40 heads x 32760 over 343 518 us, 887 TFLOP/s and 2.6 TB/s).  Back to back for a second, at the power limit: 123, 58, 21, 212 and 600.
 //
 // Warp roles: 0-3, 4-7 softmax; 8 issues S = Q K^T; 9 copies V; 10 finds the CTA's parts, copies K and Q; 11 issues O += P V; 12-15 write.
 // Tensor memory: O (128 columns) | S[2] (2 x 128) | P[2] (2 x 64).
@@ -377,7 +377,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const Part *x = part_at(n);
       if (x == nullptr || x->steps.x < 0) break;
       const bool all = x->steps.w != 0;
-      // (The row sums are ordinary stores of this CTA's threads.  By pairs o_full comes by way of the first CTA's issuers, which orders tensor memory only.)
+      // (The row sums are ordinary stores of this CTA's threads.  By pairs o_full comes by way of the first CTA's issuers, which orders tensor memory only.  A barrier more a tile: no difference.)
       if (!wait2(&sh.o_full[n & 1], (n >> 1) & 1, &sh.l_final[n & 1], (n >> 1) & 1)) break;
       tc_fence_after();
       if (__builtin_expect(all, 1)) {
