@@ -4,7 +4,8 @@
 (libheart_testhooks.so) from the same sources with HEART_TEST_HOOKS defined and a short bounded-wait
 limit: in it reserved flag bits make the attention kernel's V or K producer, or the antidiagonal kernel's
 producer, leave out one copy, or keep a CTA's part of a shared tile from the others, so that the kernels' time-out / abort / drain
-paths can be exercised by a test without faulting or hanging anything.  The product library does not contain those hooks.
+paths can be exercised by a test without faulting or hanging anything, and heart_test_cross_kernel tells which kernel a call of cross
+attention takes.  The product library does not contain those hooks.
 """
 from __future__ import annotations
 
